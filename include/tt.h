@@ -430,6 +430,132 @@ tt_status tt_render_layers(const uint8_t* src_dev, int32_t K, int64_t src_frame_
                            const uint8_t* palette_host, int32_t layers, int32_t carve_ctas, uint8_t* dst_dev,
                            void* cuda_stream);
 
+/* ---------------------------------------------------------------------------------------
+ * Operators over tokens, on caller-owned device buffers (no context needed): what a recurrent model of K streams
+ * (paper, Section III-A) needs where it works on tokens, the places of a map or one query per tool, instead
+ * of whole maps.  A tick's usual order is tt_qk_norm_rope on the projected queries and keys, tt_linear_attention as
+ * the recurrent cell with a state per stream slot, and tt_cross_attention of the tools' queries to an encoder's map.
+ *
+ * Common to all of them:
+ *   - precision TT_BF16 or TT_FP32 is the type of q, k, v and the outputs; sums, statistics and states are fp32;
+ *   - an operand is a tt_tokens view [batch][token][head][head_dim]: the last axis is contiguous, the strides of the others are
+ *     counted in elements and may come in any order; they are 0 or more (inputs: 0 shares the data along that axis) and, like
+ *     the data pointer, whole multiples of 16 bytes.  Outputs overlap no input, unless a call says otherwise;
+ *   - heads shared by groups: kv_heads divides heads, head h uses key and value head h / (heads / kv_heads);
+ *   - `lengths` arrays (device, int32 [batch], NULL: all tokens) say how many tokens an entry of the batch has, and are taken
+ *     as 0 or as the tensor's extent where they lie outside.  Rows behind an entry's last token are neither read
+ *     nor written, whatever they hold;
+ *   - head_dim is 32, 64 or 128, anything else is TT_ERR_UNSUPPORTED;
+ *   - calls are asynchronous on `cuda_stream` and may be captured into a graph; equal inputs give equal bits.  `scratch` is device memory
+ *     of the size that the call's ..._scratch_bytes gives (0: none needed), 16-byte aligned, contents on entry ignored; calls that may
+ *     overlap on the GPU, two graphs among them, need scratch of their own each.  The current device is the data's;
+ *   - bad arguments are refused with TT_ERR_INVALID_ARG before anything is launched; tt_last_error(NULL) says which.
+ * ------------------------------------------------------------------------------------ */
+typedef struct {
+  void* data;
+  int64_t batch_stride, token_stride, head_stride;   /* in elements */
+} tt_tokens;
+
+/*
+ * tt_qk_norm_rope — queries' and keys' RMS norm per head and position rotation, in one pass over both.
+ *   norm != 0: y = x / sqrt(mean(x^2) + eps) * weight   (weight fp32 [head_dim] on the device, NULL: ones);
+ *   then the first rot_dim elements of y are turned in pairs by t = position * inv_freq[i], i < rot_dim / 2:
+ *   (a, b) -> rot_scale * (a cos t - b sin t, b cos t + a sin t); a pair is elements (2i, 2i + 1) when interleaved != 0, else
+ *   (i, i + rot_dim / 2).  The rest of the head is not turned (nor scaled).  rot_dim is a multiple of 8 up to head_dim; 0: no rotation.
+ * positions: device int64, entry b's at positions + b * position_stride.  inv_freq: device fp64 [rot_dim / 2], radians per position;
+ * t is formed in 64 bits, so far positions (frame counters) keep their angles.
+ * q_heads or k_heads may be 0, then that side is not looked at.  q_out may be q and k_out may be k (same pointer and strides).
+ */
+typedef struct {
+  uint32_t struct_size;            /* = sizeof(tt_qk_norm_rope_args) */
+  int32_t precision;               /* tt_precision */
+  int32_t batch, tokens, q_heads, k_heads, head_dim, rot_dim;
+  int32_t interleaved, norm;
+  float eps, rot_scale;
+  tt_tokens q, k, q_out, k_out;
+  const float* q_weight;
+  const float* k_weight;
+  const int64_t* positions;
+  int64_t position_stride;
+  const double* inv_freq;
+  const int32_t* lengths;
+} tt_qk_norm_rope_args;
+tt_status tt_qk_norm_rope(const tt_qk_norm_rope_args* args, void* cuda_stream);
+
+/*
+ * tt_rope_frequencies — fills inv_freq[rot_dim / 2] (host, fp64) for tt_qk_norm_rope: base^(-2i / rot_dim), scaled for
+ * contexts `factor` times (>= 1) as long as the `trained` positions that a model has seen:
+ *   TT_ROPE_PLAIN     as it is;
+ *   TT_ROPE_LINEAR    all divided by factor;
+ *   TT_ROPE_BASE      base replaced by base * factor^(rot_dim / (rot_dim - 2)): the fastest pair stays, the slowest is divided by factor;
+ *   TT_ROPE_BY_PARTS  pairs that turn fewer than slow_turns times within `trained` positions are divided by factor, those that turn more than
+ *                     fast_turns times are kept, and a ramp linear in the number of turns joins the two; *rot_scale = 0.1 ln(factor) + 1.
+ * *rot_scale is 1 for the others.  Host logic only.
+ */
+typedef enum { TT_ROPE_PLAIN = 0, TT_ROPE_LINEAR = 1, TT_ROPE_BASE = 2, TT_ROPE_BY_PARTS = 3 } tt_rope_scaling;
+tt_status tt_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor, double trained, double slow_turns,
+                              double fast_turns, double* inv_freq, float* rot_scale);
+
+/*
+ * tt_linear_attention — linear attention with a decay per head: a recurrent cell over tokens.  For every entry of the batch
+ * and head, in order of the tokens, with S the head's state [head_dim (key)][head_dim (value)]:
+ *   S = exp(log_decay[head]) * S + k_t v_t^T;   out_t = scale * q_t S.
+ * A call of several tokens works in chunks, one of a single token per entry reads and writes the states once.
+ * log_decay: device fp32 [heads], 0 or below (-infinity: the state is the newest token's alone).
+ * state, state_out: device fp32 [num_slots][heads][head_dim][head_dim], 16-byte aligned; entry b starts from its slot of `state` and leaves its last
+ * state in the same slot of state_out.  The two may be one buffer; slots that no entry names are left as they were.
+ * slots: device int32 [batch], NULL: entry b has slot b.  An entry whose slot is out of range, or is an earlier entry's too, is passed over:
+ * nothing of it is read or written.
+ * status_dev: device word or NULL; a bounded device-side wait that ran out (which no healthy device produces) leaves its code there, and
+ * outputs incomplete.
+ */
+typedef struct {
+  uint32_t struct_size;            /* = sizeof(tt_linear_attention_args) */
+  int32_t precision;
+  int32_t batch, tokens, heads, kv_heads, head_dim, num_slots;
+  float scale;
+  int32_t reserved_;
+  tt_tokens q, k, v, out;
+  const float* log_decay;
+  const float* state;
+  float* state_out;
+  const int32_t* slots;
+  const int32_t* lengths;
+  int32_t* status_dev;
+  void* scratch;
+  uint64_t scratch_bytes;          /* capacity of scratch */
+} tt_linear_attention_args;
+uint64_t tt_linear_attention_scratch_bytes(const tt_linear_attention_args* args);   /* 0 also for arguments that the call refuses */
+tt_status tt_linear_attention(const tt_linear_attention_args* args, void* cuda_stream);
+
+/*
+ * tt_cross_attention — attention of q_tokens queries to an encoder's kv_tokens states:
+ *   out_i = sum_j w_ij v_j,  w_i = softmax over the visible j of scale * (q_i . k_j).
+ * Key j is visible to query i of entry b when j < kv_lengths[b] and, with a mask, mask[b * mask_batch_stride + i *
+ * mask_query_stride + j] is not 0: the bytes that tt_postprocess and tt_submit_frames write ([K][n_tools][Hm * Wm]) let each tool's query
+ * read the places of its own mask.  Mask strides are in bytes, 0 or more; a query stride of 0 is one mask for all queries.
+ * What a query does not see has no influence on its row, NaN and infinity included.  A query that sees nothing gets zeros.
+ * scale is above 0 and below 1e38.  q_lengths: rows of out behind them are left as they were.
+ * status_dev: as in tt_linear_attention.
+ */
+typedef struct {
+  uint32_t struct_size;            /* = sizeof(tt_cross_attention_args) */
+  int32_t precision;
+  int32_t batch, q_tokens, kv_tokens, heads, kv_heads, head_dim;
+  float scale;
+  int32_t reserved_;
+  tt_tokens q, k, v, out;
+  const int32_t* q_lengths;
+  const int32_t* kv_lengths;
+  const uint8_t* mask;
+  int64_t mask_batch_stride, mask_query_stride;
+  int32_t* status_dev;
+  void* scratch;
+  uint64_t scratch_bytes;
+} tt_cross_attention_args;
+uint64_t tt_cross_attention_scratch_bytes(const tt_cross_attention_args* args);   /* 0 also for arguments that the call refuses */
+tt_status tt_cross_attention(const tt_cross_attention_args* args, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Dict, List, Optional, Sequence
 
 import numpy as np
@@ -34,6 +35,8 @@ EXPORTED_SYMBOLS = [
     "tt_sched_create", "tt_sched_destroy", "tt_sched_admit", "tt_sched_release", "tt_sched_arrive", "tt_sched_next",
     "tt_sched_complete", "tt_sched_predict_ms", "tt_sched_stats",
     "tt_preprocess", "tt_postprocess_scratch_bytes", "tt_postprocess", "tt_postprocess_static", "tt_overlay", "tt_render_layers",
+    "tt_qk_norm_rope", "tt_rope_frequencies", "tt_linear_attention", "tt_linear_attention_scratch_bytes",
+    "tt_cross_attention", "tt_cross_attention_scratch_bytes",
 ]
 TT_POSTPROCESS_STATIC_SCRATCH_BYTES = 32 << 10
 STAGE_NAMES = ["h2d", "preprocess", "enc0", "enc1", "enc2", "enc3", "convlstm", "postprocess", "overlay"]
@@ -43,6 +46,34 @@ class TTError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"{STATUS_NAMES.get(status, status)}: {message}")
         self.status = status
+
+
+class tt_tokens(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("batch_stride", C.c_int64), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class tt_qk_norm_rope_args(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32)] + [(n, C.c_int32) for n in (
+        "precision", "batch", "tokens", "q_heads", "k_heads", "head_dim", "rot_dim", "interleaved", "norm")] + [
+        ("eps", C.c_float), ("rot_scale", C.c_float)] + [(n, tt_tokens) for n in ("q", "k", "q_out", "k_out")] + [
+        ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("positions", C.c_void_p), ("position_stride", C.c_int64),
+        ("inv_freq", C.c_void_p), ("lengths", C.c_void_p)]
+
+
+class tt_linear_attention_args(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32)] + [(n, C.c_int32) for n in (
+        "precision", "batch", "tokens", "heads", "kv_heads", "head_dim", "num_slots")] + [
+        ("scale", C.c_float), ("reserved_", C.c_int32)] + [(n, tt_tokens) for n in ("q", "k", "v", "out")] + [
+        (n, C.c_void_p) for n in ("log_decay", "state", "state_out", "slots", "lengths", "status_dev", "scratch")] + [
+        ("scratch_bytes", C.c_uint64)]
+
+
+class tt_cross_attention_args(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32)] + [(n, C.c_int32) for n in (
+        "precision", "batch", "q_tokens", "kv_tokens", "heads", "kv_heads", "head_dim")] + [
+        ("scale", C.c_float), ("reserved_", C.c_int32)] + [(n, tt_tokens) for n in ("q", "k", "v", "out")] + [
+        ("q_lengths", C.c_void_p), ("kv_lengths", C.c_void_p), ("mask", C.c_void_p), ("mask_batch_stride", C.c_int64),
+        ("mask_query_stride", C.c_int64), ("status_dev", C.c_void_p), ("scratch", C.c_void_p), ("scratch_bytes", C.c_uint64)]
 
 
 class tt_config(C.Structure):
@@ -140,6 +171,12 @@ def load_library(build_if_missing: bool = True) -> C.CDLL:
     lib.tt_postprocess_static.argtypes = [vp, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, i32, f32, vp, vp, vp, vp, vp]
     lib.tt_overlay.argtypes = [vp, i32, i64, i32, i32, i32, vp, i32, i32, i32, vp, vp, vp]
     lib.tt_render_layers.argtypes = [vp, i32, i64, i32, i32, i32, vp, i32, i32, i32, vp, i32, i32, vp, vp]
+    lib.tt_qk_norm_rope.argtypes = [vp, vp]
+    lib.tt_rope_frequencies.argtypes = [i32, C.c_double, i32, C.c_double, C.c_double, C.c_double, C.c_double, vp, C.POINTER(f32)]
+    for name in ("tt_linear_attention", "tt_cross_attention"):
+        getattr(lib, name).argtypes = [vp, vp]
+        getattr(lib, name + "_scratch_bytes").argtypes = [vp]
+        getattr(lib, name + "_scratch_bytes").restype = C.c_uint64
     for name in EXPORTED_SYMBOLS:
         getattr(lib, name)  # AttributeError here means the library does not export what tt.h declares
     _LIB = lib
@@ -587,3 +624,206 @@ def render_layers(src, src_w: int, src_h: int, src_pitch: int, masks, palette, l
                               pal.ctypes.data, layers, carve_ctas, dst.data_ptr(), _stream_ptr(stream))
     _check(lib, st, None)
     return dst
+
+
+# -------------------------------------------------------------------- operators over tokens
+TT_ROPE_SCALING = {"plain": 0, "linear": 1, "base": 2, "by_parts": 3}
+# the argument structures as one packed string each: a ctypes.Structure filled field by field costs 5 us of a call, this 1 us
+_ROPE_ARGS = struct.Struct("@I9i2f" + 4 * "Pqqq" + "PPPqPP")
+_LINEAR_ARGS = struct.Struct("@I7ifi" + 4 * "Pqqq" + "PPPPPPPQ")
+_CROSS_ARGS = struct.Struct("@I7ifi" + 4 * "Pqqq" + "PPPqqPPQ")
+
+
+def _refuse(message: str):
+    raise TTError(1, message)
+
+
+def _tokens(name: str, x, like=None):
+    """Data pointer and strides of a [batch][token][head][head_dim] tensor."""
+    if x.dim() != 4 or (x.shape[3] > 1 and x.stride(3) != 1):
+        _refuse(f"{name} must be [batch][token][head][head_dim] with a contiguous last axis")
+    if like is not None and (x.dtype != like.dtype or x.device != like.device):
+        _refuse(f"{name} has another type or device than the rest")
+    s = x.stride()
+    return x.data_ptr(), s[0], s[1], s[2]
+
+
+def _array(name: str, x, dtype, like, shape=None) -> int:
+    """Data pointer of a contiguous helper array, 0 for None."""
+    if x is None:
+        return 0
+    if x.dtype != dtype or x.device != like.device or not x.is_contiguous() or (shape is not None and tuple(x.shape) != shape):
+        _refuse(f"{name} must be a contiguous {dtype} tensor{'' if shape is None else f' of shape {shape}'} on {like.device}")
+    return x.data_ptr()
+
+
+def _precision(x) -> int:
+    import torch
+    if not x.is_cuda:
+        _refuse("the operators take CUDA tensors; there is no CPU fallback")
+    if x.dtype == torch.bfloat16:
+        return TT_BF16
+    if x.dtype == torch.float32:
+        return TT_FP32
+    _refuse(f"{x.dtype} is not a type of this operator (bfloat16, float32)")
+
+
+def _elsewhere(x, stream):
+    """None where a call on x's device and `stream` needs nothing special, else a context that makes both current: what the
+    call allocates then belongs to the stream that its kernels run on."""
+    import torch
+    if stream is None and x.device.index == torch.cuda.current_device():
+        return None
+    return _Current(x.device, stream)
+
+
+class _Current:
+    def __init__(self, device, stream):
+        import torch
+        if stream is not None and not hasattr(stream, "cuda_stream"):
+            stream = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+        if stream is not None and stream.device != device:
+            _refuse(f"the stream is on {stream.device}, the tensors on {device}")
+        self.contexts = [torch.cuda.device(device)] + ([torch.cuda.stream(stream)] if stream is not None else [])
+
+    def __enter__(self):
+        for c in self.contexts:
+            c.__enter__()
+
+    def __exit__(self, *e):
+        for c in reversed(self.contexts):
+            c.__exit__(*e)
+
+
+def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0, trained: float = 0.0,
+                     slow_turns: float = 1.0, fast_turns: float = 32.0):
+    """tt_rope_frequencies -> (fp64 numpy array of rot_dim / 2 radians per position, rot_scale)."""
+    lib = load_library()
+    inv, gain = np.zeros(max(rot_dim, 0) // 2, np.float64), C.c_float()
+    if scaling not in TT_ROPE_SCALING:
+        _refuse(f"scaling must be one of {sorted(TT_ROPE_SCALING)}")
+    _check(lib, lib.tt_rope_frequencies(rot_dim, base, TT_ROPE_SCALING[scaling], factor, trained, slow_turns, fast_turns,
+                                        inv.ctypes.data, C.byref(gain)))
+    return inv, gain.value
+
+
+def qk_norm_rope(q, k, positions=None, inv_freq=None, q_weight=None, k_weight=None, eps: float = 1e-6, norm: bool = True,
+                 interleaved: bool = False, rot_scale: float = 1.0, lengths=None, out=None, stream=None):
+    """tt_qk_norm_rope: q [B][T][Hq][D] and k [B][T][Hk][D] (either may be None), bf16 or fp32 -> (q', k').
+
+    positions int64 [B][T] or [T]; inv_freq fp64 [rot_dim / 2] (None: no rotation); weights fp32 [D]; lengths int32 [B].
+    out: (q', k') to write to, which may be q and k themselves; without it rows behind an entry's length are zeros."""
+    import torch
+    x = q if q is not None else k
+    if x is None:
+        _refuse("q and k are both None")
+    prec = _precision(x)
+    away = _elsewhere(x, stream)
+    if away is not None:
+        with away:
+            return qk_norm_rope(q, k, positions, inv_freq, q_weight, k_weight, eps, norm, interleaved, rot_scale, lengths, out)
+    lib = load_library()
+    B, T, _, D = x.shape if x.dim() == 4 else _refuse("q and k must be [batch][token][head][head_dim]")
+    if out is None:
+        new = torch.empty if lengths is None else torch.zeros
+        out = tuple(None if y is None else new(y.shape, dtype=y.dtype, device=y.device) for y in (q, k))
+    views, heads = [], []
+    for name, y in (("q", q), ("k", k), ("q_out", out[0]), ("k_out", out[1])):
+        if y is None:
+            views += (0, 0, 0, 0)
+            heads.append(0)
+            continue
+        views += _tokens(name, y, x)
+        if y.shape[0] != B or y.shape[1] != T or y.shape[3] != D:
+            _refuse(f"{name} has another batch, number of tokens or head_dim")
+        heads.append(y.shape[2])
+    if heads[0] != heads[2] or heads[1] != heads[3]:
+        _refuse("out must have the heads of q and k")
+    pos, pos_stride, rot = 0, 0, 0
+    if inv_freq is not None:
+        rot = 2 * inv_freq.shape[0]
+        if rot:
+            if positions is None or positions.dtype != torch.int64 or positions.device != x.device or positions.shape[-1] != T or \
+                    (T > 1 and positions.stride(-1) != 1) or (positions.dim() != 1 and (positions.dim() != 2 or positions.shape[0] != B)):
+                _refuse("positions must be int64 [B][T] or [T] on the tensors' device, contiguous along T")
+            pos, pos_stride = positions.data_ptr(), positions.stride(0) if positions.dim() == 2 and B > 1 else 0
+    args = _ROPE_ARGS.pack(_ROPE_ARGS.size, prec, B, T, heads[0], heads[1], D, rot, interleaved, norm, eps, rot_scale, *views,
+                           _array("q_weight", q_weight, torch.float32, x, (D,)), _array("k_weight", k_weight, torch.float32, x, (D,)),
+                           pos, pos_stride, _array("inv_freq", inv_freq, torch.float64, x), _array("lengths", lengths, torch.int32, x, (B,)))
+    _check(lib, lib.tt_qk_norm_rope(args, _stream_ptr(None)))
+    return tuple(out)
+
+
+def _scratch(lib, query, args: bytes, fmt: struct.Struct, x):
+    """The call's scratch, and the arguments with it (they end in scratch and scratch_bytes)."""
+    import torch
+    n = query(args)
+    if n == 0:
+        return None, args
+    buf = torch.empty(n, dtype=torch.uint8, device=x.device)
+    return buf, args[:-16] + struct.pack("@PQ", buf.data_ptr(), n)
+
+
+def linear_attention(q, k, v, log_decay, state, scale: float = 1.0, slots=None, lengths=None, out=None, state_out=None, status=None,
+                     stream=None):
+    """tt_linear_attention: q [B][T][H][D], k and v [B][T][Hkv][D], bf16 or fp32 -> (out [B][T][H][D], state_out).
+
+    log_decay fp32 [H]; state fp32 [num_slots][H][D][D], advanced in place unless state_out is given; slots and lengths int32 [B].
+    Without out, rows behind an entry's length, and those of entries that are passed over, are zeros."""
+    import torch
+    prec = _precision(q)
+    away = _elsewhere(q, stream)
+    if away is not None:
+        with away:
+            return linear_attention(q, k, v, log_decay, state, scale, slots, lengths, out, state_out, status)
+    lib = load_library()
+    if out is None:
+        out = (torch.empty if lengths is None and slots is None else torch.zeros)(q.shape, dtype=q.dtype, device=q.device)
+    if state_out is None:
+        state_out = state
+    views = _tokens("q", q) + _tokens("k", k, q) + _tokens("v", v, q) + _tokens("out", out, q)
+    B, T, H, D = q.shape
+    Hk = k.shape[2]
+    if k.shape != v.shape or k.shape != (B, T, Hk, D) or out.shape != q.shape:
+        _refuse("q, k, v and out do not fit together")
+    n = state.shape[0]
+    args = _LINEAR_ARGS.pack(_LINEAR_ARGS.size, prec, B, T, H, Hk, D, n, scale, 0, *views, _array("log_decay", log_decay, torch.float32, q, (H,)),
+                             _array("state", state, torch.float32, q, (n, H, D, D)), _array("state_out", state_out, torch.float32, q, (n, H, D, D)),
+                             _array("slots", slots, torch.int32, q, (B,)), _array("lengths", lengths, torch.int32, q, (B,)),
+                             _array("status", status, torch.int32, q), 0, 0)
+    buf, args = _scratch(lib, lib.tt_linear_attention_scratch_bytes, args, _LINEAR_ARGS, q)
+    _check(lib, lib.tt_linear_attention(args, _stream_ptr(None)))
+    return out, state_out
+
+
+def cross_attention(q, k, v, scale: Optional[float] = None, kv_lengths=None, q_lengths=None, mask=None, out=None, status=None, stream=None):
+    """tt_cross_attention: q [B][Tq][H][D], k and v [B][Tk][Hkv][D], bf16 or fp32 -> [B][Tq][H][D].
+
+    scale: 1 / sqrt(D) unless given; lengths int32 [B]; mask uint8 or bool [B][Tk] (one for all queries) or [B][Tq][Tk], 0 or False where a
+    key is not seen, for instance the masks of tt_postprocess as [K][n_tools][Hm * Wm].  Without out, rows behind q_lengths are zeros."""
+    import torch
+    prec = _precision(q)
+    away = _elsewhere(q, stream)
+    if away is not None:
+        with away:
+            return cross_attention(q, k, v, scale, kv_lengths, q_lengths, mask, out, status)
+    lib = load_library()
+    if out is None:
+        out = (torch.empty if q_lengths is None else torch.zeros)(q.shape, dtype=q.dtype, device=q.device)
+    views = _tokens("q", q) + _tokens("k", k, q) + _tokens("v", v, q) + _tokens("out", out, q)
+    B, Tq, H, D = q.shape
+    Tk, Hk = k.shape[1], k.shape[2]
+    if k.shape != v.shape or k.shape != (B, Tk, Hk, D) or out.shape != q.shape:
+        _refuse("q, k, v and out do not fit together")
+    at, mask_b, mask_q = 0, 0, 0
+    if mask is not None:
+        if mask.dtype not in (torch.uint8, torch.bool) or mask.device != q.device or tuple(mask.shape) not in ((B, Tk), (B, Tq, Tk)) or \
+                (Tk > 1 and mask.stride(-1) != 1):
+            _refuse("mask must be uint8 or bool [B][Tk] or [B][Tq][Tk] on the tensors' device, contiguous along Tk")
+        at, mask_b, mask_q = mask.data_ptr(), mask.stride(0), mask.stride(1) if mask.dim() == 3 else 0
+    args = _CROSS_ARGS.pack(_CROSS_ARGS.size, prec, B, Tq, Tk, H, Hk, D, D ** -0.5 if scale is None else scale, 0, *views,
+                            _array("q_lengths", q_lengths, torch.int32, q, (B,)), _array("kv_lengths", kv_lengths, torch.int32, q, (B,)),
+                            at, mask_b, mask_q, _array("status", status, torch.int32, q), 0, 0)
+    buf, args = _scratch(lib, lib.tt_cross_attention_scratch_bytes, args, _CROSS_ARGS, q)
+    _check(lib, lib.tt_cross_attention(args, _stream_ptr(None)))
+    return out

@@ -36,8 +36,9 @@ def _stale(target: str, deps) -> bool:
 def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) -> str:
     nvcc = _nvcc()
     os.makedirs(OBJ_DIR, exist_ok=True)
-    sources = sorted(glob.glob(os.path.join(CSRC, "*.cu")))
+    sources = sorted(glob.glob(os.path.join(CSRC, "*.cu")) + glob.glob(os.path.join(CSRC, "tokens", "*.cu")))
     headers = sorted(glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(CSRC, "*.cuh"))
+                     + glob.glob(os.path.join(CSRC, "tokens", "*.h")) + glob.glob(os.path.join(CSRC, "tokens", "*.cuh"))
                      + glob.glob(os.path.join(INCLUDE, "*.h")))
     jobs = []
     objs = []

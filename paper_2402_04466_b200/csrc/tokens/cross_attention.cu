@@ -1,0 +1,261 @@
+// Cross attention on the fp32 units (tt_cross_attention, fp32; bf16 as well where no faster kernel applies), and the join of split keys.
+//
+//   out_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = 2^(s_ij - m_i),  s_ij = scale * log2(e) * q_i k_j,  m_i the running maximum.
+//
+// One pass over the keys in tiles of 64.  The rows of a block's tile are queries x heads of one key and value head (row r: query
+// r / group, head r % group), so that shared heads read K and V once.  Where the row tiles alone do not fill the device the keys
+// are split over blocks, each leaves its sum, maximum and total, and cross_join_kernel joins them in order.
+//
+// A masked weight is kept as -0: it adds nothing to a finite value, and where a tile of V holds an infinity or NaN its sign
+// tells the slow loop to leave it out.
+#include "linear_common.cuh"
+
+namespace tt {
+namespace tok {
+namespace {
+
+constexpr int THREADS = 256;           // 16 x 16
+constexpr int BN = 64;                 // keys of a tile
+
+template <int D, int BM>
+struct Shape {
+  static constexpr int A = BM / 16;                     // rows to a thread
+  static constexpr int N = BN / 16;                     // keys to a thread
+  static constexpr int E = D / 16;                      // columns to a thread
+  static constexpr int QP = D + 4, PP = BN + 4;
+  static constexpr size_t smem = sizeof(float) * (BM * QP + BN * QP + BN * D + BM * PP);
+};
+
+template <typename T>
+__device__ __forceinline__ float4 load4(const T* p) {
+  if constexpr (sizeof(T) == 4) {
+    return *reinterpret_cast<const float4*>(p);
+  } else {
+    const uint2 u = *reinterpret_cast<const uint2*>(p);
+    return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xFFFF0000u));
+  }
+}
+__device__ __forceinline__ bool all_finite(float4 f) {
+  return isfinite(f.x) && isfinite(f.y) && isfinite(f.z) && isfinite(f.w);
+}
+
+// Where a row's partial results lie: [batch][kv head][row][split], maximum and total first, then the sums.
+struct Part {
+  float2* stat;
+  float* sum;
+};
+__device__ __forceinline__ Part part_of(const CrossParams& p, int D, int b, int hk, int row) {
+  const int64_t rows = (int64_t)p.q_tokens * p.group, all = rows * p.batch * (p.heads / p.group);
+  const int64_t at = (((int64_t)b * (p.heads / p.group) + hk) * rows + row) * p.splits;
+  return {reinterpret_cast<float2*>(p.part + all * p.splits * D) + at, p.part + at * D};
+}
+
+template <typename T, int D, int BM>
+__global__ void __launch_bounds__(THREADS) cross_kernel(const __grid_constant__ CrossParams p) {
+  using S = Shape<D, BM>;
+  constexpr int A = S::A, N = S::N, E = S::E, QP = S::QP, PP = S::PP;
+  extern __shared__ float4 raw[];
+  float* qs = reinterpret_cast<float*>(raw);
+  float* ks = qs + BM * QP;
+  float* vs = ks + BN * QP;
+  float* ps = vs + BN * D;
+  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+  const int split = blockIdx.x % p.splits, row0 = (int)(blockIdx.x / p.splits) * BM, hk = blockIdx.y, b = blockIdx.z;
+  const int rows = clamp_length(p.q_lengths, b, p.q_tokens) * p.group;
+  const int keys = clamp_length(p.kv_lengths, b, p.kv_tokens);
+  const int j0 = split * p.split_keys, j1 = min(keys, j0 + p.split_keys);
+  if (row0 >= rows || (split > 0 && j0 >= keys)) return;
+  const T* q = reinterpret_cast<const T*>(p.q.p) + b * p.q.b + (int64_t)hk * p.group * p.q.h;
+  const T* k = reinterpret_cast<const T*>(p.k.p) + b * p.k.b + hk * p.k.h;
+  const T* v = reinterpret_cast<const T*>(p.v.p) + b * p.v.b + hk * p.v.h;
+  for (int i = threadIdx.x; i < BM * (D / 4); i += THREADS) {
+    const int r = i / (D / 4), c = i % (D / 4) * 4;
+    float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (row0 + r < rows) f = load4<T>(q + (int64_t)((row0 + r) / p.group) * p.q.t + (row0 + r) % p.group * p.q.h + c);
+    *reinterpret_cast<float4*>(qs + r * QP + c) = f;
+  }
+  float m[A], l[A], o[A][E];
+#pragma unroll
+  for (int a = 0; a < A; ++a) {
+    m[a] = -INFINITY;
+    l[a] = 0.f;
+#pragma unroll
+    for (int c = 0; c < E; ++c) o[a][c] = 0.f;
+  }
+  for (int j = j0; j < j1; j += BN) {
+    __syncthreads();                   // the last tile's reads
+    bool odd = false;
+    for (int i = threadIdx.x; i < BN * (D / 4); i += THREADS) {
+      const int r = i / (D / 4), c = i % (D / 4) * 4;
+      float4 f = make_float4(0.f, 0.f, 0.f, 0.f), g = f;
+      if (j + r < j1) {
+        f = load4<T>(k + (int64_t)(j + r) * p.k.t + c);
+        g = load4<T>(v + (int64_t)(j + r) * p.v.t + c);
+      }
+      odd |= !all_finite(g);
+      *reinterpret_cast<float4*>(ks + r * QP + c) = f;
+      *reinterpret_cast<float4*>(vs + r * D + c) = g;
+    }
+    const bool careful = __syncthreads_or(odd) && p.mask;
+    float s[A][N] = {};
+    for (int e = 0; e < D; e += 4) {
+      float4 x[A], y[N];
+#pragma unroll
+      for (int a = 0; a < A; ++a) x[a] = *reinterpret_cast<const float4*>(qs + (ty + 16 * a) * QP + e);
+#pragma unroll
+      for (int c = 0; c < N; ++c) y[c] = *reinterpret_cast<const float4*>(ks + (tx + 16 * c) * QP + e);
+#pragma unroll
+      for (int a = 0; a < A; ++a)
+#pragma unroll
+        for (int c = 0; c < N; ++c)
+          s[a][c] = fmaf(x[a].x, y[c].x, fmaf(x[a].y, y[c].y, fmaf(x[a].z, y[c].z, fmaf(x[a].w, y[c].w, s[a][c]))));
+    }
+#pragma unroll
+    for (int a = 0; a < A; ++a) {
+      const int row = row0 + ty + 16 * a;
+      const uint8_t* mask = p.mask && row < rows ? p.mask + b * p.mask_b + (int64_t)(row / p.group) * p.mask_q + j : nullptr;
+      bool seen[N];
+      float top = -INFINITY;
+#pragma unroll
+      for (int c = 0; c < N; ++c) {
+        const int at = tx + 16 * c;
+        seen[c] = j + at < j1 && (!mask || mask[at]);
+        s[a][c] *= p.scale_log2;
+        if (seen[c]) top = fmaxf(top, s[a][c]);
+      }
+#pragma unroll
+      for (int x = 8; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
+      const float now = fmaxf(m[a], top), base = now == -INFINITY ? 0.f : now;
+      const float fade = exp2f(m[a] - base);
+      m[a] = now;
+      float add = 0.f;
+#pragma unroll
+      for (int c = 0; c < N; ++c) {
+        const float w = seen[c] ? exp2f(s[a][c] - base) : -0.f;
+        add += w;
+        ps[(ty + 16 * a) * PP + tx + 16 * c] = w;
+      }
+      l[a] = fmaf(l[a], fade, add);    // this thread's share of the keys
+#pragma unroll
+      for (int c = 0; c < E; ++c) o[a][c] *= fade;
+    }
+    __syncwarp();                      // a row's 16 threads are half a warp
+#pragma unroll 4
+    for (int i = 0; i < BN; ++i) {
+      float y[E];
+      if constexpr (D == 32) {
+        const float2 f = *reinterpret_cast<const float2*>(vs + i * D + 2 * tx);
+        y[0] = f.x; y[1] = f.y;
+      } else {
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) {
+          const float4 f = *reinterpret_cast<const float4*>(vs + i * D + 4 * tx + 64 * c);
+          y[4 * c] = f.x; y[4 * c + 1] = f.y; y[4 * c + 2] = f.z; y[4 * c + 3] = f.w;
+        }
+      }
+#pragma unroll
+      for (int a = 0; a < A; ++a) {
+        const float w = ps[(ty + 16 * a) * PP + i];
+        if (!careful || !signbit(w))
+#pragma unroll
+          for (int c = 0; c < E; ++c) o[a][c] = fmaf(w, y[c], o[a][c]);
+      }
+    }
+  }
+#pragma unroll
+  for (int a = 0; a < A; ++a) {
+#pragma unroll
+    for (int x = 8; x > 0; x >>= 1) l[a] += __shfl_xor_sync(0xFFFFFFFFu, l[a], x);
+    const int row = row0 + ty + 16 * a;
+    if (row >= rows) continue;
+    if (p.splits > 1) {
+      const Part to = part_of(p, D, b, hk, row);
+      if (tx == 0) to.stat[split] = make_float2(m[a], l[a]);
+#pragma unroll
+      for (int c = 0; c < E; ++c) to.sum[(int64_t)split * D + (D == 32 ? 2 * tx + c : 4 * tx + (c & 3) + (c >> 2) * 64)] = o[a][c];
+    } else {
+      const float inv = l[a] == 0.f ? 0.f : 1.f / l[a];
+      T* dst = reinterpret_cast<T*>(p.o.p) + b * p.o.b + (int64_t)(row / p.group) * p.o.t + ((int64_t)hk * p.group + row % p.group) * p.o.h;
+#pragma unroll
+      for (int c = 0; c < E; ++c) dst[D == 32 ? 2 * tx + c : 4 * tx + (c & 3) + (c >> 2) * 64] = (T)(o[a][c] * inv);
+    }
+  }
+}
+
+// One warp per row: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.
+template <typename T, int D>
+__global__ void __launch_bounds__(128) cross_join_kernel(const __grid_constant__ CrossParams p) {
+  constexpr int E = D / 32;
+  const int lane = threadIdx.x % 32, row = (int)blockIdx.x * 4 + (int)threadIdx.x / 32, hk = blockIdx.y, b = blockIdx.z;
+  if (row >= clamp_length(p.q_lengths, b, p.q_tokens) * p.group) return;
+  const int keys = clamp_length(p.kv_lengths, b, p.kv_tokens);
+  const int n = keys > p.split_keys ? (keys + p.split_keys - 1) / p.split_keys : 1;
+  const Part from = part_of(p, D, b, hk, row);
+  float top = -INFINITY;
+  for (int s = lane; s < n; s += 32) top = fmaxf(top, from.stat[s].x);
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
+  if (top == -INFINITY) top = 0.f;
+  float o[E] = {}, l = 0.f;
+  for (int s = 0; s < n; ++s) {
+    const float2 st = from.stat[s];
+    const float f = exp2f(st.x - top);
+    l = fmaf(f, st.y, l);
+#pragma unroll
+    for (int c = 0; c < E; ++c) o[c] = fmaf(f, from.sum[(int64_t)s * D + lane * E + c], o[c]);
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  T* dst = reinterpret_cast<T*>(p.o.p) + b * p.o.b + (int64_t)(row / p.group) * p.o.t + ((int64_t)hk * p.group + row % p.group) * p.o.h;
+#pragma unroll
+  for (int c = 0; c < E; ++c) dst[lane * E + c] = (T)(o[c] * inv);
+}
+
+template <typename T, int D, int BM>
+cudaError_t launch_scalar(const CrossParams& p, cudaStream_t s) {
+  const size_t smem = Shape<D, BM>::smem;
+  static OncePerContext once;
+  cudaError_t e = once([&] { return cudaFuncSetAttribute(cross_kernel<T, D, BM>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
+  if (e != cudaSuccess) return e;
+  const int64_t tiles = ((int64_t)p.q_tokens * p.group + BM - 1) / BM;
+  cross_kernel<T, D, BM><<<dim3((unsigned)(tiles * p.splits), (unsigned)(p.heads / p.group), (unsigned)p.batch), THREADS, smem, s>>>(p);
+  return cudaGetLastError();
+}
+template <typename T, int D>
+cudaError_t launch_typed(const CrossParams& p, const CrossPlan& plan, cudaStream_t s) {
+  cudaError_t e = plan.rows == 16 ? launch_scalar<T, D, 16>(p, s) : launch_scalar<T, D, 64>(p, s);
+  if (e != cudaSuccess || p.splits == 1) return e;
+  const int64_t rows = (int64_t)p.q_tokens * p.group;
+  cross_join_kernel<T, D><<<dim3((unsigned)((rows + 3) / 4), (unsigned)(p.heads / p.group), (unsigned)p.batch), 128, 0, s>>>(p);
+  return cudaGetLastError();
+}
+template <typename T>
+cudaError_t launch_typed(const CrossParams& p, const CrossPlan& plan, int D, cudaStream_t s) {
+  return D == 32 ? launch_typed<T, 32>(p, plan, s) : D == 64 ? launch_typed<T, 64>(p, plan, s) : launch_typed<T, 128>(p, plan, s);
+}
+
+}  // namespace
+
+CrossPlan cross_plan(int batch, int q_tokens, int kv_tokens, int heads, int group, int D, bool bf16, bool mask) {
+  (void)bf16; (void)mask;
+  CrossPlan plan{};
+  const int64_t rows = (int64_t)q_tokens * group;
+  plan.rows = rows <= 16 ? 16 : 64;
+  const int64_t blocks = (rows + plan.rows - 1) / plan.rows * batch * (heads / group);
+  // split the keys where the row tiles are fewer than two to a multiprocessor, down to two tiles of keys to a block
+  int64_t splits = blocks > 0 ? 2 * PLAN_SMS / blocks : 1;
+  const int64_t most = ((int64_t)kv_tokens + 2 * BN - 1) / (2 * BN);
+  if (splits > most) splits = most;
+  if (splits < 1) splits = 1;
+  const int64_t each = (((int64_t)kv_tokens + splits - 1) / splits + BN - 1) / BN * BN;
+  plan.split_keys = each > 0 ? (int)each : BN;
+  plan.splits = kv_tokens > 0 ? (int)(((int64_t)kv_tokens + each - 1) / each) : 1;
+  plan.scratch = plan.splits > 1 ? (uint64_t)(rows * batch * (heads / group)) * (uint64_t)plan.splits * (uint64_t)(D + 2) * 4u : 0u;
+  return plan;
+}
+
+cudaError_t launch_cross(const CrossParams& p, const CrossPlan& plan, bool bf16, int D, cudaStream_t s) {
+  return bf16 ? launch_typed<__nv_bfloat16>(p, plan, D, s) : launch_typed<float>(p, plan, D, s);
+}
+
+}  // namespace tok
+}  // namespace tt

@@ -1,0 +1,263 @@
+// Linear attention over several tokens (tt_linear_attention): chunks of C tokens, on the fp32 units.
+//
+// With the state S before a chunk, l the head's decay, tokens i, j of the chunk counted from 0 and m their number:
+//   out_i = scale * ( l^(i+1) q_i S + sum_{j <= i} l^(i-j) (q_i k_j) v_j ),     S' = l^m S + sum_j l^(m-1-j) k_j v_j^T.
+// Every exponent is 0 or more, so nothing overflows however strong the decay.
+//
+// A sequence (entry and head) is sequential over its chunks.  Where there are too few sequences to fill the device the tokens are cut into
+// segments: linear_segment_kernel forms what each segment adds to the state, linear_scan_kernel turns that into the state
+// before each segment, and linear_chunk_kernel then runs all segments at once.  K and V are read twice then.
+#include "linear_common.cuh"
+
+namespace tt {
+namespace tok {
+namespace {
+
+constexpr int THREADS = 256;           // 16 x 16
+
+template <int D>
+struct ChunkShape {
+  static constexpr int C = D == 128 ? 32 : 64;          // tokens of a chunk
+  static constexpr int A = C / 16;                      // rows of the chunk to a thread
+  static constexpr int E = D / 16;                      // rows of the state, and columns, to a thread
+  static constexpr int QP = D + 4;                      // pitch of rows that 16 threads read side by side
+  static constexpr int PP = C + 4;
+  static constexpr size_t smem = sizeof(float) * (2 * C * QP + C * D + D * D + C * PP + C + 1);
+};
+
+// columns of a thread: four neighbours at 4 tx (and 64 + 4 tx), two at 2 tx where D is 32
+template <int D>
+__device__ __forceinline__ int column(int tx, int j) { return D == 32 ? 2 * tx + j : 4 * tx + (j & 3) + (j >> 2) * 64; }
+
+template <int D>
+__device__ __forceinline__ void load_columns(const float* row, int tx, float (&f)[D / 16]) {
+  if constexpr (D == 32) {
+    const float2 v = *reinterpret_cast<const float2*>(row + 2 * tx);
+    f[0] = v.x; f[1] = v.y;
+  } else {
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) {
+      const float4 v = *reinterpret_cast<const float4*>(row + 4 * tx + 64 * j);
+      f[4 * j] = v.x; f[4 * j + 1] = v.y; f[4 * j + 2] = v.z; f[4 * j + 3] = v.w;
+    }
+  }
+}
+
+// m rows of D elements into shared memory as fp32, zeros behind them
+template <typename T, int D>
+__device__ __forceinline__ void fetch(float* dst, int pitch, const T* src, int64_t stride, int m, int rows) {
+  for (int i = threadIdx.x; i < rows * (D / 4); i += THREADS) {
+    const int r = i / (D / 4), c = i % (D / 4) * 4;
+    float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (r < m) {
+      if constexpr (sizeof(T) == 4) {
+        f = *reinterpret_cast<const float4*>(src + r * stride + c);
+      } else {
+        const uint2 u = *reinterpret_cast<const uint2*>(src + r * stride + c);
+        f = make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xFFFF0000u));
+      }
+    }
+    *reinterpret_cast<float4*>(dst + r * pitch + c) = f;
+  }
+}
+
+template <typename T, int D, bool WITH_OUT>
+__device__ __forceinline__ void run_chunks(const LinearParams& p, int b, int h, int t0, int t1, float* S, float* smem) {
+  using Shape = ChunkShape<D>;
+  constexpr int C = Shape::C, A = Shape::A, E = Shape::E, QP = Shape::QP, PP = Shape::PP;
+  float* q = smem;
+  float* k = q + C * QP;
+  float* v = k + C * QP;
+  float* P = v + C * D + D * D;        // S lies between
+  float* pw = P + C * PP;              // decay^0 .. decay^C
+  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16, hk = h / p.group;
+  const T* gq = reinterpret_cast<const T*>(p.q.p) + b * p.q.b + h * p.q.h;
+  const T* gk = reinterpret_cast<const T*>(p.k.p) + b * p.k.b + hk * p.k.h;
+  const T* gv = reinterpret_cast<const T*>(p.v.p) + b * p.v.b + hk * p.v.h;
+  T* go = reinterpret_cast<T*>(p.o.p) + b * p.o.b + h * p.o.h;
+  if (threadIdx.x <= C) pw[threadIdx.x] = decay_power(p.log_decay[h], threadIdx.x);
+  for (int t = t0; t < t1; t += C) {
+    const int m = min(C, t1 - t);
+    __syncthreads();                   // the state, and the last chunk's reads
+    if (WITH_OUT) fetch<T, D>(q, QP, gq + t * p.q.t, p.q.t, m, C);
+    fetch<T, D>(k, QP, gk + t * p.k.t, p.k.t, m, C);
+    fetch<T, D>(v, D, gv + t * p.v.t, p.v.t, m, C);
+    __syncthreads();
+    if (WITH_OUT) {
+      float acc[A][A] = {};
+      for (int e = 0; e < D; e += 4) {
+        float4 x[A], y[A];
+#pragma unroll
+        for (int a = 0; a < A; ++a) {
+          x[a] = *reinterpret_cast<const float4*>(q + (ty + 16 * a) * QP + e);
+          y[a] = *reinterpret_cast<const float4*>(k + (tx + 16 * a) * QP + e);
+        }
+#pragma unroll
+        for (int a = 0; a < A; ++a)
+#pragma unroll
+          for (int c = 0; c < A; ++c)
+            acc[a][c] = fmaf(x[a].x, y[c].x, fmaf(x[a].y, y[c].y, fmaf(x[a].z, y[c].z, fmaf(x[a].w, y[c].w, acc[a][c]))));
+      }
+#pragma unroll
+      for (int a = 0; a < A; ++a)
+#pragma unroll
+        for (int c = 0; c < A; ++c) {
+          const int i = ty + 16 * a, j = tx + 16 * c;
+          P[i * PP + j] = i >= j ? acc[a][c] * pw[i - j] : 0.f;
+        }
+      float inter[A][E] = {}, o[A][E] = {};
+      for (int e = 0; e < D; ++e) {
+        float s[E];
+        load_columns<D>(S + e * D, tx, s);
+#pragma unroll
+        for (int a = 0; a < A; ++a) {
+          const float x = q[(ty + 16 * a) * QP + e];
+#pragma unroll
+          for (int c = 0; c < E; ++c) inter[a][c] = fmaf(x, s[c], inter[a][c]);
+        }
+      }
+      __syncthreads();                 // P
+      for (int j = 0; j < m; ++j) {
+        float s[E];
+        load_columns<D>(v + j * D, tx, s);
+#pragma unroll
+        for (int a = 0; a < A; ++a) {
+          const float x = P[(ty + 16 * a) * PP + j];
+#pragma unroll
+          for (int c = 0; c < E; ++c) o[a][c] = fmaf(x, s[c], o[a][c]);
+        }
+      }
+#pragma unroll
+      for (int a = 0; a < A; ++a) {
+        const int i = ty + 16 * a;
+        if (i < m) {
+          T* dst = go + (int64_t)(t + i) * p.o.t;
+#pragma unroll
+          for (int c = 0; c < E; ++c) dst[column<D>(tx, c)] = (T)(p.scale * fmaf(pw[i + 1], inter[a][c], o[a][c]));
+        }
+      }
+    }
+    // own rows and columns of the state: read by the block above, written here behind a barrier
+    float s[E][E] = {};
+    for (int j = 0; j < m; ++j) {
+      float x[E], y[E];
+      load_columns<D>(v + j * D, tx, y);
+      const float d = pw[m - 1 - j];
+#pragma unroll
+      for (int a = 0; a < E; ++a) x[a] = k[j * QP + ty + 16 * a] * d;
+#pragma unroll
+      for (int a = 0; a < E; ++a)
+#pragma unroll
+        for (int c = 0; c < E; ++c) s[a][c] = fmaf(x[a], y[c], s[a][c]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int a = 0; a < E; ++a)
+#pragma unroll
+      for (int c = 0; c < E; ++c) {
+        float& at = S[(ty + 16 * a) * D + column<D>(tx, c)];
+        at = fmaf(pw[m], at, s[a][c]);
+      }
+  }
+  __syncthreads();
+}
+
+template <int D>
+__device__ __forceinline__ float* state_in_shared(float* smem) { return smem + ChunkShape<D>::C * (2 * ChunkShape<D>::QP + D); }
+
+// What segment s of a sequence leaves behind when it starts from nothing.
+template <typename T, int D>
+__global__ void __launch_bounds__(THREADS) linear_segment_kernel(const __grid_constant__ LinearParams p) {
+  extern __shared__ float4 raw[];
+  float* smem = reinterpret_cast<float*>(raw);
+  float* S = state_in_shared<D>(smem);
+  const int b = blockIdx.z, h = blockIdx.y, seg = blockIdx.x;
+  if (slot_of(p.slots, p.num_slots, b) < 0) return;
+  const int n = clamp_length(p.lengths, b, p.tokens), t0 = seg * p.seg_tokens;
+  if (t0 + p.seg_tokens >= n) return;      // the last one's is not needed
+  for (int i = threadIdx.x; i < D * D; i += THREADS) S[i] = 0.f;
+  run_chunks<T, D, false>(p, b, h, t0, t0 + p.seg_tokens, S, smem);
+  float* dst = p.seg_state + (((int64_t)b * p.heads + h) * p.segments + seg) * D * D;
+  for (int i = threadIdx.x; i < D * D; i += THREADS) dst[i] = S[i];
+}
+
+// In place: what each segment adds becomes the state before it.
+template <int D>
+__global__ void __launch_bounds__(THREADS) linear_scan_kernel(const __grid_constant__ LinearParams p) {
+  const int b = blockIdx.z, h = blockIdx.y, i = (int)blockIdx.x * THREADS + (int)threadIdx.x;
+  const int slot = slot_of(p.slots, p.num_slots, b);
+  if (slot < 0) return;
+  const int n = clamp_length(p.lengths, b, p.tokens);
+  const float decay = decay_power(p.log_decay[h], p.seg_tokens);
+  float* seg = p.seg_state + ((int64_t)b * p.heads + h) * p.segments * D * D + i;
+  float cur = p.state[((int64_t)slot * p.heads + h) * D * D + i];
+  for (int s = 0;; ++s) {
+    const bool last = (int64_t)(s + 1) * p.seg_tokens >= n;
+    const float add = last ? 0.f : seg[(int64_t)s * D * D];
+    seg[(int64_t)s * D * D] = cur;
+    if (last) break;
+    cur = fmaf(decay, cur, add);
+  }
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(THREADS) linear_chunk_kernel(const __grid_constant__ LinearParams p) {
+  extern __shared__ float4 raw[];
+  float* smem = reinterpret_cast<float*>(raw);
+  float* S = state_in_shared<D>(smem);
+  const int b = blockIdx.z, h = blockIdx.y, seg = blockIdx.x;
+  const int slot = slot_of(p.slots, p.num_slots, b);
+  if (slot < 0) return;
+  const int n = clamp_length(p.lengths, b, p.tokens), t0 = seg * p.seg_tokens, t1 = min(n, t0 + p.seg_tokens);
+  if (seg > 0 && t0 >= n) return;
+  const int64_t at = ((int64_t)slot * p.heads + h) * D * D;
+  const float* src = p.segments > 1 ? p.seg_state + (((int64_t)b * p.heads + h) * p.segments + seg) * D * D : p.state + at;
+  for (int i = threadIdx.x; i < D * D; i += THREADS) S[i] = src[i];
+  run_chunks<T, D, true>(p, b, h, t0, t1, S, smem);
+  if (t1 == n)
+    for (int i = threadIdx.x; i < D * D; i += THREADS) p.state_out[at + i] = S[i];
+}
+
+template <typename T, int D>
+cudaError_t launch(const LinearParams& p, cudaStream_t s) {
+  const size_t smem = ChunkShape<D>::smem;
+  static OncePerContext once;
+  cudaError_t e = once([&] {
+    cudaError_t r = cudaFuncSetAttribute(linear_segment_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    return r != cudaSuccess ? r : cudaFuncSetAttribute(linear_chunk_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  });
+  if (e != cudaSuccess) return e;
+  if (p.segments > 1) {
+    linear_segment_kernel<T, D><<<dim3((unsigned)p.segments - 1, (unsigned)p.heads, (unsigned)p.batch), THREADS, smem, s>>>(p);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    linear_scan_kernel<D><<<dim3(D * D / THREADS, (unsigned)p.heads, (unsigned)p.batch), THREADS, 0, s>>>(p);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  }
+  linear_chunk_kernel<T, D><<<dim3((unsigned)p.segments, (unsigned)p.heads, (unsigned)p.batch), THREADS, smem, s>>>(p);
+  return cudaGetLastError();
+}
+template <typename T>
+cudaError_t launch(const LinearParams& p, int D, cudaStream_t s) {
+  return D == 32 ? launch<T, 32>(p, s) : D == 64 ? launch<T, 64>(p, s) : launch<T, 128>(p, s);
+}
+
+}  // namespace
+
+void linear_plan(int batch, int tokens, int heads, int D, bool bf16, int* segments, int* seg_tokens) {
+  (void)D; (void)bf16;
+  const int64_t sequences = (int64_t)batch * heads;
+  const int step = 128;
+  const int64_t most = (tokens + step - 1) / step, want = 2 * PLAN_SMS / sequences;
+  int64_t n = want < most ? want : most;
+  if (n < 1) n = 1;
+  const int64_t each = tokens > 0 ? ((tokens + n - 1) / n + step - 1) / step * step : step;
+  *seg_tokens = (int)each;
+  *segments = tokens > 0 ? (int)((tokens + each - 1) / each) : 1;
+}
+
+cudaError_t launch_linear_chunk(const LinearParams& p, bool bf16, int D, cudaStream_t s) {
+  return bf16 ? launch<__nv_bfloat16>(p, D, s) : launch<float>(p, D, s);
+}
+
+}  // namespace tok
+}  // namespace tt

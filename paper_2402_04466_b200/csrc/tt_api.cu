@@ -254,6 +254,25 @@ tt_status fail(tt_ctx* ctx, tt_status st, const char* fmt, ...) {
   return st;
 }
 
+}  // namespace
+
+tt_status tt::set_error(tt_status st, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof(buf), fmt, ap);
+  va_end(ap);
+  try {
+    fail(nullptr, st, "%s", buf);
+  } catch (...) {      // no memory for the text: the status says enough
+  }
+  return st;
+}
+
+void* tt::tensor_map_encoder() { return reinterpret_cast<void*>(get_encode_fn()); }
+
+namespace {
+
 void bind_slot(tt_ctx* ctx, int i) {
   const tt_ctx::Slot& sl = ctx->slots[i];
   ctx->frames_stage = sl.frames_stage; ctx->logits = sl.logits; ctx->probs = sl.probs; ctx->masks = sl.masks;

@@ -67,6 +67,11 @@ struct OncePerContext {
   }
 };
 
+// For entry points outside tt_api.cu: records what tt_last_error(NULL) returns, gives `st` back, and throws nothing.
+tt_status set_error(tt_status st, const char* fmt, ...);
+// cuTensorMapEncodeTiled's address, null where the driver has none.
+void* tensor_map_encoder();
+
 // Maps batch position n (0..K-1) of a launch to an image index inside a tensor that holds
 // more images than the batch (state slots, ping-pong halves).
 struct IdxMap {
