@@ -235,9 +235,14 @@ cudaError_t launch_typed(const CrossParams& p, const CrossPlan& plan, int D, cud
 
 }  // namespace
 
-CrossPlan cross_plan(int batch, int q_tokens, int kv_tokens, int heads, int group, int D, bool bf16, bool mask) {
-  (void)bf16; (void)mask;
+CrossPlan cross_plan(int batch, int q_tokens, int kv_tokens, int heads, int group, int D, bool bf16, bool mask, bool maps) {
   CrossPlan plan{};
+  plan.splits = 1;
+  plan.split_keys = kv_tokens;
+  if (bf16 && !mask && maps && q_tokens > 64) {
+    plan.kernel = CROSS_TC;
+    return plan;
+  }
   const int64_t rows = (int64_t)q_tokens * group;
   plan.rows = rows <= 16 ? 16 : 64;
   const int64_t blocks = (rows + plan.rows - 1) / plan.rows * batch * (heads / group);
@@ -254,6 +259,7 @@ CrossPlan cross_plan(int batch, int q_tokens, int kv_tokens, int heads, int grou
 }
 
 cudaError_t launch_cross(const CrossParams& p, const CrossPlan& plan, bool bf16, int D, cudaStream_t s) {
+  if (plan.kernel == CROSS_TC) return launch_cross_tc(p, D, s);
   return bf16 ? launch_typed<__nv_bfloat16>(p, plan, D, s) : launch_typed<float>(p, plan, D, s);
 }
 

@@ -59,14 +59,22 @@ struct alignas(32) CrossParams {
   int32_t splits, split_keys;   // keys to a split
   float scale_log2;             // scale * log2(e)
 };
+enum { CROSS_SCALAR = 0, CROSS_TC = 1 };
 struct CrossPlan {
-  int32_t kernel;               // 0: scalar
+  int32_t kernel;               // one of CROSS_...
   int32_t rows;                 // rows (queries x heads of a group) of a block's tile
   int32_t splits, split_keys;
   uint64_t scratch;
 };
-CrossPlan cross_plan(int batch, int q_tokens, int kv_tokens, int heads, int group, int D, bool bf16, bool mask);
+// `maps`: q, k and v can be read through tensor maps (token_map_fits)
+CrossPlan cross_plan(int batch, int q_tokens, int kv_tokens, int heads, int group, int D, bool bf16, bool mask, bool maps);
 cudaError_t launch_cross(const CrossParams& p, const CrossPlan& plan, bool bf16, int D, cudaStream_t s);
+
+cudaError_t launch_cross_tc(const CrossParams& p, int D, cudaStream_t s);
+
+// Tensor map of a bf16 view, boxes of 128 tokens of one head.  An axis of stride 0 has one place.
+bool token_map(TensorMap128* map, const View& v, int D, int tokens, int heads, int batch);
+bool token_map_fits(const View& v, int tokens, int heads, int batch);   // strides that a map can hold, tokens apart from each other
 
 // ------------------------------------------------------------------------------- device helpers
 __device__ __forceinline__ int clamp_length(const int32_t* lengths, int b, int extent) {

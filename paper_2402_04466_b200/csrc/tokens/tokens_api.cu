@@ -168,7 +168,9 @@ static tt_status check_cross(const char* who, const tt_cross_attention_args* a) 
   return TT_OK;
 }
 static CrossPlan plan_of(const tt_cross_attention_args* a) {
-  return cross_plan(a->batch, a->q_tokens, a->kv_tokens, a->heads, a->heads / a->kv_heads, a->head_dim, a->precision == TT_BF16, a->mask != nullptr);
+  return cross_plan(a->batch, a->q_tokens, a->kv_tokens, a->heads, a->heads / a->kv_heads, a->head_dim, a->precision == TT_BF16, a->mask != nullptr,
+                    token_map_fits(view(a->q), a->q_tokens, a->heads, a->batch) && token_map_fits(view(a->k), a->kv_tokens, a->kv_heads, a->batch) &&
+                        token_map_fits(view(a->v), a->kv_tokens, a->kv_heads, a->batch));
 }
 
 uint64_t tt_cross_attention_scratch_bytes(const tt_cross_attention_args* a) {
