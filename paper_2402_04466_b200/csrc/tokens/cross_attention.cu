@@ -1,4 +1,4 @@
-// Cross attention on the fp32 units (tt_cross_attention, fp32; bf16 as well where no faster kernel applies), and the join of split keys.
+// Cross attention of fp32 operands, on the fp32 units (tt_cross_attention), the join of split keys, and the choice between the kernels.
 //
 //   out_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = 2^(s_ij - m_i),  s_ij = scale * log2(e) * q_i k_j,  m_i the running maximum.
 //
@@ -26,31 +26,11 @@ struct Shape {
   static constexpr size_t smem = sizeof(float) * (BM * QP + BN * QP + BN * D + BM * PP);
 };
 
-template <typename T>
-__device__ __forceinline__ float4 load4(const T* p) {
-  if constexpr (sizeof(T) == 4) {
-    return *reinterpret_cast<const float4*>(p);
-  } else {
-    const uint2 u = *reinterpret_cast<const uint2*>(p);
-    return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xFFFF0000u));
-  }
-}
 __device__ __forceinline__ bool all_finite(float4 f) {
   return isfinite(f.x) && isfinite(f.y) && isfinite(f.z) && isfinite(f.w);
 }
 
-// Where a row's partial results lie: [batch][kv head][row][split], maximum and total first, then the sums.
-struct Part {
-  float2* stat;
-  float* sum;
-};
-__device__ __forceinline__ Part part_of(const CrossParams& p, int D, int b, int hk, int row) {
-  const int64_t rows = (int64_t)p.q_tokens * p.group, all = rows * p.batch * (p.heads / p.group);
-  const int64_t at = (((int64_t)b * (p.heads / p.group) + hk) * rows + row) * p.splits;
-  return {reinterpret_cast<float2*>(p.part + all * p.splits * D) + at, p.part + at * D};
-}
-
-template <typename T, int D, int BM>
+template <int D, int BM>
 __global__ void __launch_bounds__(THREADS) cross_kernel(const __grid_constant__ CrossParams p) {
   using S = Shape<D, BM>;
   constexpr int A = S::A, N = S::N, E = S::E, QP = S::QP, PP = S::PP;
@@ -65,13 +45,13 @@ __global__ void __launch_bounds__(THREADS) cross_kernel(const __grid_constant__ 
   const int keys = clamp_length(p.kv_lengths, b, p.kv_tokens);
   const int j0 = split * p.split_keys, j1 = min(keys, j0 + p.split_keys);
   if (row0 >= rows || (split > 0 && j0 >= keys)) return;
-  const T* q = reinterpret_cast<const T*>(p.q.p) + b * p.q.b + (int64_t)hk * p.group * p.q.h;
-  const T* k = reinterpret_cast<const T*>(p.k.p) + b * p.k.b + hk * p.k.h;
-  const T* v = reinterpret_cast<const T*>(p.v.p) + b * p.v.b + hk * p.v.h;
+  const float* q = reinterpret_cast<const float*>(p.q.p) + b * p.q.b + (int64_t)hk * p.group * p.q.h;
+  const float* k = reinterpret_cast<const float*>(p.k.p) + b * p.k.b + hk * p.k.h;
+  const float* v = reinterpret_cast<const float*>(p.v.p) + b * p.v.b + hk * p.v.h;
   for (int i = threadIdx.x; i < BM * (D / 4); i += THREADS) {
     const int r = i / (D / 4), c = i % (D / 4) * 4;
     float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (row0 + r < rows) f = load4<T>(q + (int64_t)((row0 + r) / p.group) * p.q.t + (row0 + r) % p.group * p.q.h + c);
+    if (row0 + r < rows) f = *reinterpret_cast<const float4*>(q + (int64_t)((row0 + r) / p.group) * p.q.t + (row0 + r) % p.group * p.q.h + c);
     *reinterpret_cast<float4*>(qs + r * QP + c) = f;
   }
   float m[A], l[A], o[A][E];
@@ -89,8 +69,8 @@ __global__ void __launch_bounds__(THREADS) cross_kernel(const __grid_constant__ 
       const int r = i / (D / 4), c = i % (D / 4) * 4;
       float4 f = make_float4(0.f, 0.f, 0.f, 0.f), g = f;
       if (j + r < j1) {
-        f = load4<T>(k + (int64_t)(j + r) * p.k.t + c);
-        g = load4<T>(v + (int64_t)(j + r) * p.v.t + c);
+        f = *reinterpret_cast<const float4*>(k + (int64_t)(j + r) * p.k.t + c);
+        g = *reinterpret_cast<const float4*>(v + (int64_t)(j + r) * p.v.t + c);
       }
       odd |= !all_finite(g);
       *reinterpret_cast<float4*>(ks + r * QP + c) = f;
@@ -175,9 +155,9 @@ __global__ void __launch_bounds__(THREADS) cross_kernel(const __grid_constant__ 
       for (int c = 0; c < E; ++c) to.sum[(int64_t)split * D + (D == 32 ? 2 * tx + c : 4 * tx + (c & 3) + (c >> 2) * 64)] = o[a][c];
     } else {
       const float inv = l[a] == 0.f ? 0.f : 1.f / l[a];
-      T* dst = reinterpret_cast<T*>(p.o.p) + b * p.o.b + (int64_t)(row / p.group) * p.o.t + ((int64_t)hk * p.group + row % p.group) * p.o.h;
+      float* dst = reinterpret_cast<float*>(p.o.p) + b * p.o.b + (int64_t)(row / p.group) * p.o.t + ((int64_t)hk * p.group + row % p.group) * p.o.h;
 #pragma unroll
-      for (int c = 0; c < E; ++c) dst[D == 32 ? 2 * tx + c : 4 * tx + (c & 3) + (c >> 2) * 64] = (T)(o[a][c] * inv);
+      for (int c = 0; c < E; ++c) dst[D == 32 ? 2 * tx + c : 4 * tx + (c & 3) + (c >> 2) * 64] = o[a][c] * inv;
     }
   }
 }
@@ -210,19 +190,21 @@ __global__ void __launch_bounds__(128) cross_join_kernel(const __grid_constant__
   for (int c = 0; c < E; ++c) dst[lane * E + c] = (T)(o[c] * inv);
 }
 
-template <typename T, int D, int BM>
+template <int D, int BM>
 cudaError_t launch_scalar(const CrossParams& p, cudaStream_t s) {
   const size_t smem = Shape<D, BM>::smem;
   static OncePerContext once;
-  cudaError_t e = once([&] { return cudaFuncSetAttribute(cross_kernel<T, D, BM>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
+  cudaError_t e = once([&] { return cudaFuncSetAttribute(cross_kernel<D, BM>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
   if (e != cudaSuccess) return e;
   const int64_t tiles = ((int64_t)p.q_tokens * p.group + BM - 1) / BM;
-  cross_kernel<T, D, BM><<<dim3((unsigned)(tiles * p.splits), (unsigned)(p.heads / p.group), (unsigned)p.batch), THREADS, smem, s>>>(p);
+  cross_kernel<D, BM><<<dim3((unsigned)(tiles * p.splits), (unsigned)(p.heads / p.group), (unsigned)p.batch), THREADS, smem, s>>>(p);
   return cudaGetLastError();
 }
 template <typename T, int D>
 cudaError_t launch_typed(const CrossParams& p, const CrossPlan& plan, cudaStream_t s) {
-  cudaError_t e = plan.rows == 16 ? launch_scalar<T, D, 16>(p, s) : launch_scalar<T, D, 64>(p, s);
+  cudaError_t e = cudaSuccess;
+  if constexpr (sizeof(T) == 2) e = launch_cross_few(p, D, s);
+  else e = plan.rows == 16 ? launch_scalar<D, 16>(p, s) : launch_scalar<D, 64>(p, s);
   if (e != cudaSuccess || p.splits == 1) return e;
   const int64_t rows = (int64_t)p.q_tokens * p.group;
   cross_join_kernel<T, D><<<dim3((unsigned)((rows + 3) / 4), (unsigned)(p.heads / p.group), (unsigned)p.batch), 128, 0, s>>>(p);
@@ -244,11 +226,14 @@ CrossPlan cross_plan(int batch, int q_tokens, int kv_tokens, int heads, int grou
     return plan;
   }
   const int64_t rows = (int64_t)q_tokens * group;
-  plan.rows = rows <= 16 ? 16 : 64;
+  plan.kernel = bf16 ? CROSS_FEW : CROSS_SCALAR;
+  plan.rows = bf16 || rows <= 16 ? 16 : 64;
   const int64_t blocks = (rows + plan.rows - 1) / plan.rows * batch * (heads / group);
-  // split the keys where the row tiles are fewer than two to a multiprocessor, down to two tiles of keys to a block
-  int64_t splits = blocks > 0 ? 2 * PLAN_SMS / blocks : 1;
-  const int64_t most = ((int64_t)kv_tokens + 2 * BN - 1) / (2 * BN);
+  // split the keys where the row tiles do not fill the device a few times over (lengths may differ), down to 256 keys to a block where
+  // that is needed to reach every multiprocessor twice, and 512 beyond; the scalar kernel to two tiles of keys
+  int64_t splits = blocks > 0 ? (bf16 ? 6 : 2) * PLAN_SMS / blocks : 1;
+  const int64_t least = !bf16 ? 2 * BN : (int64_t)kv_tokens * blocks >= 2 * PLAN_SMS * 512 ? 512 : 256;
+  const int64_t most = ((int64_t)kv_tokens + least - 1) / least;
   if (splits > most) splits = most;
   if (splits < 1) splits = 1;
   const int64_t each = (((int64_t)kv_tokens + splits - 1) / splits + BN - 1) / BN * BN;

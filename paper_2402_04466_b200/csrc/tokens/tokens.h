@@ -59,7 +59,7 @@ struct alignas(32) CrossParams {
   int32_t splits, split_keys;   // keys to a split
   float scale_log2;             // scale * log2(e)
 };
-enum { CROSS_SCALAR = 0, CROSS_TC = 1 };
+enum { CROSS_SCALAR = 0, CROSS_TC = 1, CROSS_FEW = 2 };
 struct CrossPlan {
   int32_t kernel;               // one of CROSS_...
   int32_t rows;                 // rows (queries x heads of a group) of a block's tile
@@ -70,6 +70,7 @@ struct CrossPlan {
 CrossPlan cross_plan(int batch, int q_tokens, int kv_tokens, int heads, int group, int D, bool bf16, bool mask, bool maps);
 cudaError_t launch_cross(const CrossParams& p, const CrossPlan& plan, bool bf16, int D, cudaStream_t s);
 
+cudaError_t launch_cross_few(const CrossParams& p, int D, cudaStream_t s);   // splits > 1: the join is the caller's
 cudaError_t launch_cross_tc(const CrossParams& p, int D, cudaStream_t s);
 
 // Tensor map of a bf16 view, boxes of 128 tokens of one head.  An axis of stride 0 has one place.
@@ -81,6 +82,17 @@ __device__ __forceinline__ int clamp_length(const int32_t* lengths, int b, int e
   if (!lengths) return extent;
   const int n = lengths[b];
   return n < 0 ? 0 : n > extent ? extent : n;
+}
+
+// Where a row's partial results lie: [batch][kv head][row][split], maximum and total first, then the sums.
+struct Part {
+  float2* stat;
+  float* sum;
+};
+__device__ __forceinline__ Part part_of(const CrossParams& p, int D, int b, int hk, int row) {
+  const int64_t rows = (int64_t)p.q_tokens * p.group, all = rows * p.batch * (p.heads / p.group);
+  const int64_t at = (((int64_t)b * (p.heads / p.group) + hk) * rows + row) * p.splits;
+  return {reinterpret_cast<float2*>(p.part + all * p.splits * D) + at, p.part + at * D};
 }
 
 }  // namespace tok
