@@ -230,8 +230,7 @@ cudaError_t launch(const LinearParams& p, cudaStream_t s) {
   if (p.segments > 1) {
     linear_segment_kernel<T, D><<<dim3((unsigned)p.segments - 1, (unsigned)p.heads, (unsigned)p.batch), THREADS, smem, s>>>(p);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    linear_scan_kernel<D><<<dim3(D * D / THREADS, (unsigned)p.heads, (unsigned)p.batch), THREADS, 0, s>>>(p);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    if ((e = launch_linear_scan(p, D, s)) != cudaSuccess) return e;
   }
   linear_chunk_kernel<T, D><<<dim3((unsigned)p.segments, (unsigned)p.heads, (unsigned)p.batch), THREADS, smem, s>>>(p);
   return cudaGetLastError();
@@ -253,6 +252,14 @@ void linear_plan(int batch, int tokens, int heads, int D, bool bf16, int* segmen
   const int64_t each = tokens > 0 ? ((tokens + n - 1) / n + step - 1) / step * step : step;
   *seg_tokens = (int)each;
   *segments = tokens > 0 ? (int)((tokens + each - 1) / each) : 1;
+}
+
+cudaError_t launch_linear_scan(const LinearParams& p, int D, cudaStream_t s) {
+  const dim3 grid((unsigned)(D * D / THREADS), (unsigned)p.heads, (unsigned)p.batch);
+  if (D == 32) linear_scan_kernel<32><<<grid, THREADS, 0, s>>>(p);
+  else if (D == 64) linear_scan_kernel<64><<<grid, THREADS, 0, s>>>(p);
+  else linear_scan_kernel<128><<<grid, THREADS, 0, s>>>(p);
+  return cudaGetLastError();
 }
 
 cudaError_t launch_linear_chunk(const LinearParams& p, bool bf16, int D, cudaStream_t s) {

@@ -46,6 +46,8 @@ struct alignas(32) LinearParams {
 void linear_plan(int batch, int tokens, int heads, int D, bool bf16, int* segments, int* seg_tokens);
 cudaError_t launch_linear_step(const LinearParams& p, bool bf16, int D, cudaStream_t s);
 cudaError_t launch_linear_chunk(const LinearParams& p, bool bf16, int D, cudaStream_t s);
+cudaError_t launch_linear_tc(const LinearParams& p, int D, cudaStream_t s);       // bf16, views that tensor maps can hold
+cudaError_t launch_linear_scan(const LinearParams& p, int D, cudaStream_t s);     // what segments add -> the states before them
 
 struct alignas(32) CrossParams {
   View q, k, v, o;

@@ -154,7 +154,11 @@ tt_status tt_linear_attention(const tt_linear_attention_args* a, void* cuda_stre
   p.scale = a->scale;
   linear_plan(a->batch, a->tokens, a->heads, a->head_dim, bf16, &p.segments, &p.seg_tokens);
   const cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
-  const cudaError_t e = a->tokens == 1 ? launch_linear_step(p, bf16, a->head_dim, s) : launch_linear_chunk(p, bf16, a->head_dim, s);
+  const bool maps = bf16 && a->tokens > 1 && token_map_fits(p.q, a->tokens, a->heads, a->batch) &&
+                    token_map_fits(p.k, a->tokens, a->kv_heads, a->batch) && token_map_fits(p.v, a->tokens, a->kv_heads, a->batch);
+  const cudaError_t e = a->tokens == 1 ? launch_linear_step(p, bf16, a->head_dim, s)
+                        : maps         ? launch_linear_tc(p, a->head_dim, s)
+                                       : launch_linear_chunk(p, bf16, a->head_dim, s);
   return e == cudaSuccess ? TT_OK : set_error(TT_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
 }
 
