@@ -632,54 +632,48 @@ TT_ROPE_SCALING = {"plain": 0, "linear": 1, "base": 2, "by_parts": 3}
 _ROPE_ARGS = struct.Struct("@I9i2f" + 4 * "Pqqq" + "PPPqPP")
 _LINEAR_ARGS = struct.Struct("@I7ifi" + 4 * "Pqqq" + "PPPPPPPQ")
 _CROSS_ARGS = struct.Struct("@I7ifi" + 4 * "Pqqq" + "PPPqqPPQ")
+_SCRATCH = struct.Struct("@PQ")      # the last two members of both
 
 
 def _refuse(message: str):
     raise TTError(1, message)
 
 
-def _tokens(name: str, x, like=None):
-    """Data pointer and strides of a [batch][token][head][head_dim] tensor."""
-    if x.dim() != 4 or (x.shape[3] > 1 and x.stride(3) != 1):
-        _refuse(f"{name} must be [batch][token][head][head_dim] with a contiguous last axis")
-    if like is not None and (x.dtype != like.dtype or x.device != like.device):
-        _refuse(f"{name} has another type or device than the rest")
-    s = x.stride()
-    return x.data_ptr(), s[0], s[1], s[2]
+class _Torch:
+    """What the calls below take from torch, looked up once: an import statement or a device object costs 0.3 to 1 us of a call."""
+
+    def __init__(self):
+        import torch
+        self.mod, self.types = torch, {torch.bfloat16: TT_BF16, torch.float32: TT_FP32}
+        self.i32, self.i64, self.f32, self.f64, self.u8, self.bool = torch.int32, torch.int64, torch.float32, torch.float64, torch.uint8, torch.bool
+        self.empty, self.zeros = torch.empty, torch.zeros
+        # names that torch does not promise to keep
+        self.current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        self.current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
-def _array(name: str, x, dtype, like, shape=None) -> int:
-    """Data pointer of a contiguous helper array, 0 for None."""
-    if x is None:
-        return 0
-    if x.dtype != dtype or x.device != like.device or not x.is_contiguous() or (shape is not None and tuple(x.shape) != shape):
-        _refuse(f"{name} must be a contiguous {dtype} tensor{'' if shape is None else f' of shape {shape}'} on {like.device}")
-    return x.data_ptr()
+_TORCH: Optional[_Torch] = None
 
 
-def _precision(x) -> int:
-    import torch
-    if not x.is_cuda:
+def _operator(x, stream):
+    """(library, torch, precision, device index, away) of a call on x; away: a context that has to be entered first, where the call is
+    for another device than the current one or for a stream.  What the call allocates then belongs to the stream its kernels run on."""
+    global _TORCH
+    if _TORCH is None:
+        _TORCH = _Torch()
+    th, device = _TORCH, x.get_device()
+    prec = th.types.get(x.dtype)
+    if device < 0:
         _refuse("the operators take CUDA tensors; there is no CPU fallback")
-    if x.dtype == torch.bfloat16:
-        return TT_BF16
-    if x.dtype == torch.float32:
-        return TT_FP32
-    _refuse(f"{x.dtype} is not a type of this operator (bfloat16, float32)")
-
-
-def _elsewhere(x, stream):
-    """None where a call on x's device and `stream` needs nothing special, else a context that makes both current: what the
-    call allocates then belongs to the stream that its kernels run on."""
-    import torch
-    if stream is None and x.device.index == torch.cuda.current_device():
-        return None
-    return _Current(x.device, stream)
+    if prec is None:
+        _refuse(f"{x.dtype} is not a type of these operators (bfloat16, float32)")
+    away = None if stream is None and device == th.current_device() else _Current(x.device, stream)
+    return _LIB or load_library(), th, prec, device, away
 
 
 class _Current:
     def __init__(self, device, stream):
-        import torch
+        torch = _TORCH.mod
         if stream is not None and not hasattr(stream, "cuda_stream"):
             stream = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
         if stream is not None and stream.device != device:
@@ -693,6 +687,25 @@ class _Current:
     def __exit__(self, *e):
         for c in reversed(self.contexts):
             c.__exit__(*e)
+
+
+def _tokens(name: str, x, dtype, device):
+    """Data pointer and strides of a [batch][token][head][head_dim] tensor."""
+    s = x.stride()
+    if len(s) != 4 or s[3] != 1:
+        _refuse(f"{name} must be [batch][token][head][head_dim] with a contiguous last axis")
+    if x.dtype is not dtype or x.get_device() != device:
+        _refuse(f"{name} has another type or device than the rest")
+    return x.data_ptr(), s[0], s[1], s[2]
+
+
+def _array(name: str, x, dtype, device, shape=None) -> int:
+    """Data pointer of a contiguous helper array, 0 for None."""
+    if x is None:
+        return 0
+    if x.dtype is not dtype or x.get_device() != device or not x.is_contiguous() or (shape is not None and x.shape != shape):
+        _refuse(f"{name} must be a contiguous {dtype} tensor{'' if shape is None else f' of shape {shape}'} on the other tensors' device")
+    return x.data_ptr()
 
 
 def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0, trained: float = 0.0,
@@ -713,55 +726,49 @@ def qk_norm_rope(q, k, positions=None, inv_freq=None, q_weight=None, k_weight=No
 
     positions int64 [B][T] or [T]; inv_freq fp64 [rot_dim / 2] (None: no rotation); weights fp32 [D]; lengths int32 [B].
     out: (q', k') to write to, which may be q and k themselves; without it rows behind an entry's length are zeros."""
-    import torch
     x = q if q is not None else k
     if x is None:
         _refuse("q and k are both None")
-    prec = _precision(x)
-    away = _elsewhere(x, stream)
+    lib, th, prec, device, away = _operator(x, stream)
     if away is not None:
         with away:
             return qk_norm_rope(q, k, positions, inv_freq, q_weight, k_weight, eps, norm, interleaved, rot_scale, lengths, out)
-    lib = load_library()
-    B, T, _, D = x.shape if x.dim() == 4 else _refuse("q and k must be [batch][token][head][head_dim]")
+    dtype, shape = x.dtype, x.shape
+    if len(shape) != 4:
+        _refuse("q and k must be [batch][token][head][head_dim]")
+    B, T, _, D = shape
     if out is None:
-        new = torch.empty if lengths is None else torch.zeros
+        new = th.empty if lengths is None else th.zeros
         out = tuple(None if y is None else new(y.shape, dtype=y.dtype, device=y.device) for y in (q, k))
-    views, heads = [], []
+    views, heads = (), []
     for name, y in (("q", q), ("k", k), ("q_out", out[0]), ("k_out", out[1])):
         if y is None:
             views += (0, 0, 0, 0)
             heads.append(0)
             continue
-        views += _tokens(name, y, x)
-        if y.shape[0] != B or y.shape[1] != T or y.shape[3] != D:
+        views += _tokens(name, y, dtype, device)
+        b, t, h, d = y.shape
+        if b != B or t != T or d != D:
             _refuse(f"{name} has another batch, number of tokens or head_dim")
-        heads.append(y.shape[2])
+        heads.append(h)
     if heads[0] != heads[2] or heads[1] != heads[3]:
         _refuse("out must have the heads of q and k")
-    pos, pos_stride, rot = 0, 0, 0
+    pos, pos_stride, rot, freq = 0, 0, 0, 0
     if inv_freq is not None:
-        rot = 2 * inv_freq.shape[0]
+        rot, freq = 2 * inv_freq.shape[0], _array("inv_freq", inv_freq, th.f64, device)
         if rot:
-            if positions is None or positions.dtype != torch.int64 or positions.device != x.device or positions.shape[-1] != T or \
-                    (T > 1 and positions.stride(-1) != 1) or (positions.dim() != 1 and (positions.dim() != 2 or positions.shape[0] != B)):
+            n = positions.dim() if positions is not None else 0
+            if n not in (1, 2) or positions.dtype is not th.i64 or positions.get_device() != device or positions.shape[-1] != T or \
+                    (T > 1 and positions.stride(-1) != 1) or (n == 2 and positions.shape[0] != B):
                 _refuse("positions must be int64 [B][T] or [T] on the tensors' device, contiguous along T")
-            pos, pos_stride = positions.data_ptr(), positions.stride(0) if positions.dim() == 2 and B > 1 else 0
+            pos, pos_stride = positions.data_ptr(), positions.stride(0) if n == 2 and B > 1 else 0
     args = _ROPE_ARGS.pack(_ROPE_ARGS.size, prec, B, T, heads[0], heads[1], D, rot, interleaved, norm, eps, rot_scale, *views,
-                           _array("q_weight", q_weight, torch.float32, x, (D,)), _array("k_weight", k_weight, torch.float32, x, (D,)),
-                           pos, pos_stride, _array("inv_freq", inv_freq, torch.float64, x), _array("lengths", lengths, torch.int32, x, (B,)))
-    _check(lib, lib.tt_qk_norm_rope(args, _stream_ptr(None)))
+                           _array("q_weight", q_weight, th.f32, device, (D,)), _array("k_weight", k_weight, th.f32, device, (D,)),
+                           pos, pos_stride, freq, _array("lengths", lengths, th.i32, device, (B,)))
+    st = lib.tt_qk_norm_rope(args, th.current_stream(device))
+    if st:
+        _check(lib, st)
     return tuple(out)
-
-
-def _scratch(lib, query, args: bytes, fmt: struct.Struct, x):
-    """The call's scratch, and the arguments with it (they end in scratch and scratch_bytes)."""
-    import torch
-    n = query(args)
-    if n == 0:
-        return None, args
-    buf = torch.empty(n, dtype=torch.uint8, device=x.device)
-    return buf, args[:-16] + struct.pack("@PQ", buf.data_ptr(), n)
 
 
 def linear_attention(q, k, v, log_decay, state, scale: float = 1.0, slots=None, lengths=None, out=None, state_out=None, status=None,
@@ -770,29 +777,32 @@ def linear_attention(q, k, v, log_decay, state, scale: float = 1.0, slots=None, 
 
     log_decay fp32 [H]; state fp32 [num_slots][H][D][D], advanced in place unless state_out is given; slots and lengths int32 [B].
     Without out, rows behind an entry's length, and those of entries that are passed over, are zeros."""
-    import torch
-    prec = _precision(q)
-    away = _elsewhere(q, stream)
+    lib, th, prec, device, away = _operator(q, stream)
     if away is not None:
         with away:
             return linear_attention(q, k, v, log_decay, state, scale, slots, lengths, out, state_out, status)
-    lib = load_library()
+    dtype, shape, kv_shape = q.dtype, q.shape, k.shape
     if out is None:
-        out = (torch.empty if lengths is None and slots is None else torch.zeros)(q.shape, dtype=q.dtype, device=q.device)
+        out = (th.empty if lengths is None and slots is None else th.zeros)(shape, dtype=dtype, device=q.device)
     if state_out is None:
         state_out = state
-    views = _tokens("q", q) + _tokens("k", k, q) + _tokens("v", v, q) + _tokens("out", out, q)
-    B, T, H, D = q.shape
-    Hk = k.shape[2]
-    if k.shape != v.shape or k.shape != (B, T, Hk, D) or out.shape != q.shape:
+    views = _tokens("q", q, dtype, device) + _tokens("k", k, dtype, device) + _tokens("v", v, dtype, device) + _tokens("out", out, dtype, device)
+    B, T, H, D = shape
+    Hk, n = kv_shape[2], state.shape[0]
+    if v.shape != kv_shape or kv_shape != (B, T, Hk, D) or out.shape != shape:
         _refuse("q, k, v and out do not fit together")
-    n = state.shape[0]
-    args = _LINEAR_ARGS.pack(_LINEAR_ARGS.size, prec, B, T, H, Hk, D, n, scale, 0, *views, _array("log_decay", log_decay, torch.float32, q, (H,)),
-                             _array("state", state, torch.float32, q, (n, H, D, D)), _array("state_out", state_out, torch.float32, q, (n, H, D, D)),
-                             _array("slots", slots, torch.int32, q, (B,)), _array("lengths", lengths, torch.int32, q, (B,)),
-                             _array("status", status, torch.int32, q), 0, 0)
-    buf, args = _scratch(lib, lib.tt_linear_attention_scratch_bytes, args, _LINEAR_ARGS, q)
-    _check(lib, lib.tt_linear_attention(args, _stream_ptr(None)))
+    states = (n, H, D, D)
+    args = _LINEAR_ARGS.pack(_LINEAR_ARGS.size, prec, B, T, H, Hk, D, n, scale, 0, *views, _array("log_decay", log_decay, th.f32, device, (H,)),
+                             _array("state", state, th.f32, device, states), _array("state_out", state_out, th.f32, device, states),
+                             _array("slots", slots, th.i32, device, (B,)), _array("lengths", lengths, th.i32, device, (B,)),
+                             _array("status", status, th.i32, device), 0, 0)
+    room = lib.tt_linear_attention_scratch_bytes(args) if T > 1 else 0
+    if room:
+        buf = th.empty(room, dtype=th.u8, device=q.device)
+        args = args[:-16] + _SCRATCH.pack(buf.data_ptr(), room)
+    st = lib.tt_linear_attention(args, th.current_stream(device))
+    if st:
+        _check(lib, st)
     return out, state_out
 
 
@@ -801,29 +811,33 @@ def cross_attention(q, k, v, scale: Optional[float] = None, kv_lengths=None, q_l
 
     scale: 1 / sqrt(D) unless given; lengths int32 [B]; mask uint8 or bool [B][Tk] (one for all queries) or [B][Tq][Tk], 0 or False where a
     key is not seen, for instance the masks of tt_postprocess as [K][n_tools][Hm * Wm].  Without out, rows behind q_lengths are zeros."""
-    import torch
-    prec = _precision(q)
-    away = _elsewhere(q, stream)
+    lib, th, prec, device, away = _operator(q, stream)
     if away is not None:
         with away:
             return cross_attention(q, k, v, scale, kv_lengths, q_lengths, mask, out, status)
-    lib = load_library()
+    dtype, shape, kv_shape = q.dtype, q.shape, k.shape
     if out is None:
-        out = (torch.empty if q_lengths is None else torch.zeros)(q.shape, dtype=q.dtype, device=q.device)
-    views = _tokens("q", q) + _tokens("k", k, q) + _tokens("v", v, q) + _tokens("out", out, q)
-    B, Tq, H, D = q.shape
-    Tk, Hk = k.shape[1], k.shape[2]
-    if k.shape != v.shape or k.shape != (B, Tk, Hk, D) or out.shape != q.shape:
+        out = (th.empty if q_lengths is None else th.zeros)(shape, dtype=dtype, device=q.device)
+    views = _tokens("q", q, dtype, device) + _tokens("k", k, dtype, device) + _tokens("v", v, dtype, device) + _tokens("out", out, dtype, device)
+    B, Tq, H, D = shape
+    _, Tk, Hk, _ = kv_shape
+    if v.shape != kv_shape or kv_shape != (B, Tk, Hk, D) or out.shape != shape:
         _refuse("q, k, v and out do not fit together")
     at, mask_b, mask_q = 0, 0, 0
     if mask is not None:
-        if mask.dtype not in (torch.uint8, torch.bool) or mask.device != q.device or tuple(mask.shape) not in ((B, Tk), (B, Tq, Tk)) or \
+        n = mask.dim()
+        if (mask.dtype is not th.u8 and mask.dtype is not th.bool) or mask.get_device() != device or mask.shape != ((B, Tq, Tk) if n == 3 else (B, Tk)) or \
                 (Tk > 1 and mask.stride(-1) != 1):
             _refuse("mask must be uint8 or bool [B][Tk] or [B][Tq][Tk] on the tensors' device, contiguous along Tk")
-        at, mask_b, mask_q = mask.data_ptr(), mask.stride(0), mask.stride(1) if mask.dim() == 3 else 0
+        at, mask_b, mask_q = mask.data_ptr(), mask.stride(0), mask.stride(1) if n == 3 else 0
     args = _CROSS_ARGS.pack(_CROSS_ARGS.size, prec, B, Tq, Tk, H, Hk, D, D ** -0.5 if scale is None else scale, 0, *views,
-                            _array("q_lengths", q_lengths, torch.int32, q, (B,)), _array("kv_lengths", kv_lengths, torch.int32, q, (B,)),
-                            at, mask_b, mask_q, _array("status", status, torch.int32, q), 0, 0)
-    buf, args = _scratch(lib, lib.tt_cross_attention_scratch_bytes, args, _CROSS_ARGS, q)
-    _check(lib, lib.tt_cross_attention(args, _stream_ptr(None)))
+                            _array("q_lengths", q_lengths, th.i32, device, (B,)), _array("kv_lengths", kv_lengths, th.i32, device, (B,)),
+                            at, mask_b, mask_q, _array("status", status, th.i32, device), 0, 0)
+    room = lib.tt_cross_attention_scratch_bytes(args)
+    if room:
+        buf = th.empty(room, dtype=th.u8, device=q.device)
+        args = args[:-16] + _SCRATCH.pack(buf.data_ptr(), room)
+    st = lib.tt_cross_attention(args, th.current_stream(device))
+    if st:
+        _check(lib, st)
     return out

@@ -169,7 +169,7 @@ __global__ void __launch_bounds__(128) cross_join_kernel(const __grid_constant__
   const int lane = threadIdx.x % 32, row = (int)blockIdx.x * 4 + (int)threadIdx.x / 32, hk = blockIdx.y, b = blockIdx.z;
   if (row >= clamp_length(p.q_lengths, b, p.q_tokens) * p.group) return;
   const int keys = clamp_length(p.kv_lengths, b, p.kv_tokens);
-  const int n = keys > p.split_keys ? (keys + p.split_keys - 1) / p.split_keys : 1;
+  const int n = p.split_keys == 0 ? p.splits : keys > p.split_keys ? (keys + p.split_keys - 1) / p.split_keys : 1;
   const Part from = part_of(p, D, b, hk, row);
   float top = -INFINITY;
   for (int s = lane; s < n; s += 32) top = fmaxf(top, from.stat[s].x);
@@ -177,6 +177,7 @@ __global__ void __launch_bounds__(128) cross_join_kernel(const __grid_constant__
   for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
   if (top == -INFINITY) top = 0.f;
   float o[E] = {}, l = 0.f;
+#pragma unroll 8                       // the loads of eight splits in flight together
   for (int s = 0; s < n; ++s) {
     const float2 st = from.stat[s];
     const float f = exp2f(st.x - top);
@@ -217,28 +218,38 @@ cudaError_t launch_typed(const CrossParams& p, const CrossPlan& plan, int D, cud
 
 }  // namespace
 
-CrossPlan cross_plan(int batch, int q_tokens, int kv_tokens, int heads, int group, int D, bool bf16, bool mask, bool maps) {
+CrossPlan cross_plan(int batch, int q_tokens, int kv_tokens, int heads, int group, int D, bool bf16, bool mask) {
   CrossPlan plan{};
-  plan.splits = 1;
-  plan.split_keys = kv_tokens;
-  if (bf16 && !mask && maps && q_tokens > 64) {
+  plan.splits = plan.cluster = 1;
+  if (bf16 && !mask && q_tokens > 64) {
     plan.kernel = CROSS_TC;
     return plan;
   }
   const int64_t rows = (int64_t)q_tokens * group;
-  plan.kernel = bf16 ? CROSS_FEW : CROSS_SCALAR;
-  plan.rows = bf16 || rows <= 16 ? 16 : 64;
-  const int64_t blocks = (rows + plan.rows - 1) / plan.rows * batch * (heads / group);
-  // split the keys where the row tiles do not fill the device a few times over (lengths may differ), down to 256 keys to a block where
-  // that is needed to reach every multiprocessor twice, and 512 beyond; the scalar kernel to two tiles of keys
-  int64_t splits = blocks > 0 ? (bf16 ? 6 : 2) * PLAN_SMS / blocks : 1;
-  const int64_t least = !bf16 ? 2 * BN : (int64_t)kv_tokens * blocks >= 2 * PLAN_SMS * 512 ? 512 : 256;
-  const int64_t most = ((int64_t)kv_tokens + least - 1) / least;
-  if (splits > most) splits = most;
-  if (splits < 1) splits = 1;
-  const int64_t each = (((int64_t)kv_tokens + splits - 1) / splits + BN - 1) / BN * BN;
-  plan.split_keys = each > 0 ? (int)each : BN;
-  plan.splits = kv_tokens > 0 ? (int)(((int64_t)kv_tokens + each - 1) / each) : 1;
+  if (bf16) {
+    plan.kernel = CROSS_FEW;
+    plan.split_keys = 0;
+    const int64_t tiles = (rows + 15) / 16 * batch * (heads / group);
+    // a tile's keys over a cluster of blocks, down to 128 keys to a block, until there are two blocks to a multiprocessor
+    while (plan.cluster < 8 && tiles * plan.cluster < 2 * PLAN_SMS && kv_tokens / (2 * plan.cluster) >= 128) plan.cluster *= 2;
+    // and over several clusters, which takes a second kernel, where those leave half of the device idle and more than 1024 keys to a block
+    int64_t splits = tiles > 0 && 2 * tiles * plan.cluster < PLAN_SMS ? 2 * PLAN_SMS / (tiles * plan.cluster) : 1;
+    const int64_t most = kv_tokens / ((int64_t)plan.cluster * 512);
+    if (kv_tokens / plan.cluster <= 1024) splits = 1;
+    plan.splits = (int)(splits < most ? splits : most > 1 ? most : 1);
+  } else {
+    plan.kernel = CROSS_SCALAR;
+    plan.rows = rows <= 16 ? 16 : 64;
+    const int64_t blocks = (rows + plan.rows - 1) / plan.rows * batch * (heads / group);
+    // split the keys where the row tiles are fewer than two to a multiprocessor, down to two tiles of keys to a block
+    int64_t splits = blocks > 0 ? 2 * PLAN_SMS / blocks : 1;
+    const int64_t most = ((int64_t)kv_tokens + 2 * BN - 1) / (2 * BN);
+    if (splits > most) splits = most;
+    if (splits < 1) splits = 1;
+    const int64_t each = (((int64_t)kv_tokens + splits - 1) / splits + BN - 1) / BN * BN;
+    plan.split_keys = each > 0 ? (int)each : BN;
+    plan.splits = kv_tokens > 0 ? (int)(((int64_t)kv_tokens + each - 1) / each) : 1;
+  }
   plan.scratch = plan.splits > 1 ? (uint64_t)(rows * batch * (heads / group)) * (uint64_t)plan.splits * (uint64_t)(D + 2) * 4u : 0u;
   return plan;
 }

@@ -313,8 +313,7 @@ cudaError_t launch(const CrossTcParams& p, int batch, cudaStream_t s) {
 
 }  // namespace
 
-// Tensor map of a bf16 view, boxes of 128 tokens.  An axis of stride 0 has one place.
-bool token_map(TensorMap128* map, const View& v, int D, int tokens, int heads, int batch) {
+bool token_map(TensorMap128* map, const View& v, int D, int tokens, int heads, int batch, int box_tokens) {
   typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                              const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
   const Encode fn = reinterpret_cast<Encode>(tensor_map_encoder());
@@ -327,17 +326,11 @@ bool token_map(TensorMap128* map, const View& v, int D, int tokens, int heads, i
     dims[i + 1] = one ? 1u : (cuuint64_t)extent[i];
     bytes[i] = one ? (cuuint64_t)D * 2u : (cuuint64_t)stride[i] * 2u;
   }
-  const cuuint32_t box[4] = {(cuuint32_t)(D == 128 ? 64 : D), 128, 1, 1}, ones[4] = {1, 1, 1, 1};
+  const cuuint32_t box[4] = {(cuuint32_t)(D == 128 ? 64 : D), (cuuint32_t)box_tokens, 1, 1}, ones[4] = {1, 1, 1, 1};
   return fn(reinterpret_cast<CUtensorMap*>(map), CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, v.p, dims, bytes, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
             D == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-// Whether a view can be read through such a map: strides up to 2^40 bytes, tokens apart from each other.
-bool token_map_fits(const View& v, int tokens, int heads, int batch) {
-  const int64_t most = (1ll << 39) - 1;
-  return (tokens == 1 || (v.t > 0 && v.t <= most)) && (heads == 1 || v.h <= most) && (batch == 1 || v.b <= most);
-}
-
 cudaError_t launch_cross_tc(const CrossParams& c, int D, cudaStream_t s) {
   CrossTcParams p{};
   const int kv_heads = c.heads / c.group;

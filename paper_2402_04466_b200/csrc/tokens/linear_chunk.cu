@@ -1,4 +1,4 @@
-// Linear attention over several tokens (tt_linear_attention): chunks of C tokens, on the fp32 units.
+// Linear attention over several fp32 tokens (tt_linear_attention): chunks of C tokens, on the fp32 units.
 //
 // With the state S before a chunk, l the head's decay, tokens i, j of the chunk counted from 0 and m their number:
 //   out_i = scale * ( l^(i+1) q_i S + sum_{j <= i} l^(i-j) (q_i k_j) v_j ),     S' = l^m S + sum_j l^(m-1-j) k_j v_j^T.
@@ -44,24 +44,17 @@ __device__ __forceinline__ void load_columns(const float* row, int tx, float (&f
 }
 
 // m rows of D elements into shared memory as fp32, zeros behind them
-template <typename T, int D>
-__device__ __forceinline__ void fetch(float* dst, int pitch, const T* src, int64_t stride, int m, int rows) {
+template <int D>
+__device__ __forceinline__ void fetch(float* dst, int pitch, const float* src, int64_t stride, int m, int rows) {
   for (int i = threadIdx.x; i < rows * (D / 4); i += THREADS) {
     const int r = i / (D / 4), c = i % (D / 4) * 4;
     float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (r < m) {
-      if constexpr (sizeof(T) == 4) {
-        f = *reinterpret_cast<const float4*>(src + r * stride + c);
-      } else {
-        const uint2 u = *reinterpret_cast<const uint2*>(src + r * stride + c);
-        f = make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xFFFF0000u));
-      }
-    }
+    if (r < m) f = *reinterpret_cast<const float4*>(src + r * stride + c);
     *reinterpret_cast<float4*>(dst + r * pitch + c) = f;
   }
 }
 
-template <typename T, int D, bool WITH_OUT>
+template <int D, bool WITH_OUT>
 __device__ __forceinline__ void run_chunks(const LinearParams& p, int b, int h, int t0, int t1, float* S, float* smem) {
   using Shape = ChunkShape<D>;
   constexpr int C = Shape::C, A = Shape::A, E = Shape::E, QP = Shape::QP, PP = Shape::PP;
@@ -71,17 +64,17 @@ __device__ __forceinline__ void run_chunks(const LinearParams& p, int b, int h, 
   float* P = v + C * D + D * D;        // S lies between
   float* pw = P + C * PP;              // decay^0 .. decay^C
   const int tx = threadIdx.x % 16, ty = threadIdx.x / 16, hk = h / p.group;
-  const T* gq = reinterpret_cast<const T*>(p.q.p) + b * p.q.b + h * p.q.h;
-  const T* gk = reinterpret_cast<const T*>(p.k.p) + b * p.k.b + hk * p.k.h;
-  const T* gv = reinterpret_cast<const T*>(p.v.p) + b * p.v.b + hk * p.v.h;
-  T* go = reinterpret_cast<T*>(p.o.p) + b * p.o.b + h * p.o.h;
+  const float* gq = reinterpret_cast<const float*>(p.q.p) + b * p.q.b + h * p.q.h;
+  const float* gk = reinterpret_cast<const float*>(p.k.p) + b * p.k.b + hk * p.k.h;
+  const float* gv = reinterpret_cast<const float*>(p.v.p) + b * p.v.b + hk * p.v.h;
+  float* go = reinterpret_cast<float*>(p.o.p) + b * p.o.b + h * p.o.h;
   if (threadIdx.x <= C) pw[threadIdx.x] = decay_power(p.log_decay[h], threadIdx.x);
   for (int t = t0; t < t1; t += C) {
     const int m = min(C, t1 - t);
     __syncthreads();                   // the state, and the last chunk's reads
-    if (WITH_OUT) fetch<T, D>(q, QP, gq + t * p.q.t, p.q.t, m, C);
-    fetch<T, D>(k, QP, gk + t * p.k.t, p.k.t, m, C);
-    fetch<T, D>(v, D, gv + t * p.v.t, p.v.t, m, C);
+    if (WITH_OUT) fetch<D>(q, QP, gq + t * p.q.t, p.q.t, m, C);
+    fetch<D>(k, QP, gk + t * p.k.t, p.k.t, m, C);
+    fetch<D>(v, D, gv + t * p.v.t, p.v.t, m, C);
     __syncthreads();
     if (WITH_OUT) {
       float acc[A][A] = {};
@@ -131,9 +124,9 @@ __device__ __forceinline__ void run_chunks(const LinearParams& p, int b, int h, 
       for (int a = 0; a < A; ++a) {
         const int i = ty + 16 * a;
         if (i < m) {
-          T* dst = go + (int64_t)(t + i) * p.o.t;
+          float* dst = go + (int64_t)(t + i) * p.o.t;
 #pragma unroll
-          for (int c = 0; c < E; ++c) dst[column<D>(tx, c)] = (T)(p.scale * fmaf(pw[i + 1], inter[a][c], o[a][c]));
+          for (int c = 0; c < E; ++c) dst[column<D>(tx, c)] = p.scale * fmaf(pw[i + 1], inter[a][c], o[a][c]);
         }
       }
     }
@@ -166,7 +159,7 @@ template <int D>
 __device__ __forceinline__ float* state_in_shared(float* smem) { return smem + ChunkShape<D>::C * (2 * ChunkShape<D>::QP + D); }
 
 // What segment s of a sequence leaves behind when it starts from nothing.
-template <typename T, int D>
+template <int D>
 __global__ void __launch_bounds__(THREADS) linear_segment_kernel(const __grid_constant__ LinearParams p) {
   extern __shared__ float4 raw[];
   float* smem = reinterpret_cast<float*>(raw);
@@ -176,7 +169,7 @@ __global__ void __launch_bounds__(THREADS) linear_segment_kernel(const __grid_co
   const int n = clamp_length(p.lengths, b, p.tokens), t0 = seg * p.seg_tokens;
   if (t0 + p.seg_tokens >= n) return;      // the last one's is not needed
   for (int i = threadIdx.x; i < D * D; i += THREADS) S[i] = 0.f;
-  run_chunks<T, D, false>(p, b, h, t0, t0 + p.seg_tokens, S, smem);
+  run_chunks<D, false>(p, b, h, t0, t0 + p.seg_tokens, S, smem);
   float* dst = p.seg_state + (((int64_t)b * p.heads + h) * p.segments + seg) * D * D;
   for (int i = threadIdx.x; i < D * D; i += THREADS) dst[i] = S[i];
 }
@@ -200,7 +193,7 @@ __global__ void __launch_bounds__(THREADS) linear_scan_kernel(const __grid_const
   }
 }
 
-template <typename T, int D>
+template <int D>
 __global__ void __launch_bounds__(THREADS) linear_chunk_kernel(const __grid_constant__ LinearParams p) {
   extern __shared__ float4 raw[];
   float* smem = reinterpret_cast<float*>(raw);
@@ -213,33 +206,28 @@ __global__ void __launch_bounds__(THREADS) linear_chunk_kernel(const __grid_cons
   const int64_t at = ((int64_t)slot * p.heads + h) * D * D;
   const float* src = p.segments > 1 ? p.seg_state + (((int64_t)b * p.heads + h) * p.segments + seg) * D * D : p.state + at;
   for (int i = threadIdx.x; i < D * D; i += THREADS) S[i] = src[i];
-  run_chunks<T, D, true>(p, b, h, t0, t1, S, smem);
+  run_chunks<D, true>(p, b, h, t0, t1, S, smem);
   if (t1 == n)
     for (int i = threadIdx.x; i < D * D; i += THREADS) p.state_out[at + i] = S[i];
 }
 
-template <typename T, int D>
+template <int D>
 cudaError_t launch(const LinearParams& p, cudaStream_t s) {
   const size_t smem = ChunkShape<D>::smem;
   static OncePerContext once;
   cudaError_t e = once([&] {
-    cudaError_t r = cudaFuncSetAttribute(linear_segment_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    return r != cudaSuccess ? r : cudaFuncSetAttribute(linear_chunk_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    cudaError_t r = cudaFuncSetAttribute(linear_segment_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    return r != cudaSuccess ? r : cudaFuncSetAttribute(linear_chunk_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   });
   if (e != cudaSuccess) return e;
   if (p.segments > 1) {
-    linear_segment_kernel<T, D><<<dim3((unsigned)p.segments - 1, (unsigned)p.heads, (unsigned)p.batch), THREADS, smem, s>>>(p);
+    linear_segment_kernel<D><<<dim3((unsigned)p.segments - 1, (unsigned)p.heads, (unsigned)p.batch), THREADS, smem, s>>>(p);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     if ((e = launch_linear_scan(p, D, s)) != cudaSuccess) return e;
   }
-  linear_chunk_kernel<T, D><<<dim3((unsigned)p.segments, (unsigned)p.heads, (unsigned)p.batch), THREADS, smem, s>>>(p);
+  linear_chunk_kernel<D><<<dim3((unsigned)p.segments, (unsigned)p.heads, (unsigned)p.batch), THREADS, smem, s>>>(p);
   return cudaGetLastError();
 }
-template <typename T>
-cudaError_t launch(const LinearParams& p, int D, cudaStream_t s) {
-  return D == 32 ? launch<T, 32>(p, s) : D == 64 ? launch<T, 64>(p, s) : launch<T, 128>(p, s);
-}
-
 }  // namespace
 
 void linear_plan(int batch, int tokens, int heads, int D, bool bf16, int* segments, int* seg_tokens) {
@@ -262,8 +250,8 @@ cudaError_t launch_linear_scan(const LinearParams& p, int D, cudaStream_t s) {
   return cudaGetLastError();
 }
 
-cudaError_t launch_linear_chunk(const LinearParams& p, bool bf16, int D, cudaStream_t s) {
-  return bf16 ? launch<__nv_bfloat16>(p, D, s) : launch<float>(p, D, s);
+cudaError_t launch_linear_chunk(const LinearParams& p, int D, cudaStream_t s) {
+  return D == 32 ? launch<32>(p, s) : D == 64 ? launch<64>(p, s) : launch<128>(p, s);
 }
 
 }  // namespace tok

@@ -10,7 +10,7 @@ namespace tok {
 using namespace tt::tc;
 
 // Codes of waits that ran out: own hundreds beside those of tc_ptx.cuh.
-constexpr int WAIT_CROSS_TC = 0xB00, WAIT_LINEAR_TC = 0xC00;
+constexpr int WAIT_CROSS_TC = 0xB00, WAIT_LINEAR_TC = 0xC00, WAIT_CROSS_FEW = 0xD00;
 
 // D[tmem] += A[tmem] * B[shared]: A's row i is lane i, two bf16 to a column.
 __device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {

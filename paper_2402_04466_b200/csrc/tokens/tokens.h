@@ -45,8 +45,8 @@ struct alignas(32) LinearParams {
 // How many segments the tokens are cut into, and of how many tokens.
 void linear_plan(int batch, int tokens, int heads, int D, bool bf16, int* segments, int* seg_tokens);
 cudaError_t launch_linear_step(const LinearParams& p, bool bf16, int D, cudaStream_t s);
-cudaError_t launch_linear_chunk(const LinearParams& p, bool bf16, int D, cudaStream_t s);
-cudaError_t launch_linear_tc(const LinearParams& p, int D, cudaStream_t s);       // bf16, views that tensor maps can hold
+cudaError_t launch_linear_chunk(const LinearParams& p, int D, cudaStream_t s);    // fp32, and calls without tokens
+cudaError_t launch_linear_tc(const LinearParams& p, int D, cudaStream_t s);       // bf16
 cudaError_t launch_linear_scan(const LinearParams& p, int D, cudaStream_t s);     // what segments add -> the states before them
 
 struct alignas(32) CrossParams {
@@ -58,26 +58,25 @@ struct alignas(32) CrossParams {
   float* part;                  // partial results where splits > 1: see cross_attention.cu
   int32_t* status;
   int32_t batch, q_tokens, kv_tokens, heads, group;
-  int32_t splits, split_keys;   // keys to a split
+  int32_t splits, split_keys;   // keys to a split; 0: an entry's keys in `splits` equal pieces
+  int32_t cluster;              // blocks that share a piece
   float scale_log2;             // scale * log2(e)
 };
 enum { CROSS_SCALAR = 0, CROSS_TC = 1, CROSS_FEW = 2 };
 struct CrossPlan {
   int32_t kernel;               // one of CROSS_...
   int32_t rows;                 // rows (queries x heads of a group) of a block's tile
-  int32_t splits, split_keys;
+  int32_t splits, split_keys, cluster;
   uint64_t scratch;
 };
-// `maps`: q, k and v can be read through tensor maps (token_map_fits)
-CrossPlan cross_plan(int batch, int q_tokens, int kv_tokens, int heads, int group, int D, bool bf16, bool mask, bool maps);
+CrossPlan cross_plan(int batch, int q_tokens, int kv_tokens, int heads, int group, int D, bool bf16, bool mask);
 cudaError_t launch_cross(const CrossParams& p, const CrossPlan& plan, bool bf16, int D, cudaStream_t s);
 
 cudaError_t launch_cross_few(const CrossParams& p, int D, cudaStream_t s);   // splits > 1: the join is the caller's
 cudaError_t launch_cross_tc(const CrossParams& p, int D, cudaStream_t s);
 
-// Tensor map of a bf16 view, boxes of 128 tokens of one head.  An axis of stride 0 has one place.
-bool token_map(TensorMap128* map, const View& v, int D, int tokens, int heads, int batch);
-bool token_map_fits(const View& v, int tokens, int heads, int batch);   // strides that a map can hold, tokens apart from each other
+// Tensor map of a bf16 view, boxes of `box` tokens of one head.  An axis of stride 0 has one place.
+bool token_map(TensorMap128* map, const View& v, int D, int tokens, int heads, int batch, int box = 128);
 
 // ------------------------------------------------------------------------------- device helpers
 __device__ __forceinline__ int clamp_length(const int32_t* lengths, int b, int extent) {

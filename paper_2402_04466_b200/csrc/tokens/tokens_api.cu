@@ -11,6 +11,7 @@ using namespace tt::tok;
 namespace {
 
 constexpr int64_t MAX_EXTENT = 1 << 28;      // tokens of an entry
+constexpr int64_t MAX_STRIDE = 1ll << 38;    // elements: what a tensor map holds, in bytes of either type
 constexpr int64_t MAX_REACH = 1ll << 46;     // elements between a view's first and last
 
 bool misaligned(const void* p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
@@ -22,10 +23,11 @@ bool bad_view(const char* who, const char* name, const tt_tokens& v, int64_t bat
   const int64_t unit = 16 / size, limit = MAX_REACH;
   if (misaligned(v.data, 16) || v.batch_stride % unit || v.token_stride % unit || v.head_stride % unit)
     return set_error(TT_ERR_INVALID_ARG, "%s: %s must start on 16 bytes, and its strides be whole multiples of them", who, name), true;
+  if (tokens > 1 && v.token_stride == 0) return set_error(TT_ERR_INVALID_ARG, "%s: token_stride of %s is 0", who, name), true;
   const int64_t strides[3] = {v.batch_stride, v.token_stride, v.head_stride}, extents[3] = {batch, tokens, heads};
   int64_t reach = 0;
   for (int i = 0; i < 3; ++i) {
-    if (strides[i] < 0 || strides[i] > limit || (extents[i] > 1 && strides[i] > (limit - reach) / (extents[i] - 1)))
+    if (strides[i] < 0 || strides[i] > MAX_STRIDE || (extents[i] > 1 && strides[i] > (limit - reach) / (extents[i] - 1)))
       return set_error(TT_ERR_INVALID_ARG, "%s: a stride of %s is negative or too large", who, name), true;
     reach += strides[i] * (extents[i] - 1);
   }
@@ -154,11 +156,9 @@ tt_status tt_linear_attention(const tt_linear_attention_args* a, void* cuda_stre
   p.scale = a->scale;
   linear_plan(a->batch, a->tokens, a->heads, a->head_dim, bf16, &p.segments, &p.seg_tokens);
   const cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
-  const bool maps = bf16 && a->tokens > 1 && token_map_fits(p.q, a->tokens, a->heads, a->batch) &&
-                    token_map_fits(p.k, a->tokens, a->kv_heads, a->batch) && token_map_fits(p.v, a->tokens, a->kv_heads, a->batch);
-  const cudaError_t e = a->tokens == 1 ? launch_linear_step(p, bf16, a->head_dim, s)
-                        : maps         ? launch_linear_tc(p, a->head_dim, s)
-                                       : launch_linear_chunk(p, bf16, a->head_dim, s);
+  const cudaError_t e = a->tokens == 1             ? launch_linear_step(p, bf16, a->head_dim, s)
+                        : bf16 && a->tokens > 0 ? launch_linear_tc(p, a->head_dim, s)
+                                                : launch_linear_chunk(p, a->head_dim, s);
   return e == cudaSuccess ? TT_OK : set_error(TT_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
 }
 
@@ -172,9 +172,7 @@ static tt_status check_cross(const char* who, const tt_cross_attention_args* a) 
   return TT_OK;
 }
 static CrossPlan plan_of(const tt_cross_attention_args* a) {
-  return cross_plan(a->batch, a->q_tokens, a->kv_tokens, a->heads, a->heads / a->kv_heads, a->head_dim, a->precision == TT_BF16, a->mask != nullptr,
-                    token_map_fits(view(a->q), a->q_tokens, a->heads, a->batch) && token_map_fits(view(a->k), a->kv_tokens, a->kv_heads, a->batch) &&
-                        token_map_fits(view(a->v), a->kv_tokens, a->kv_heads, a->batch));
+  return cross_plan(a->batch, a->q_tokens, a->kv_tokens, a->heads, a->heads / a->kv_heads, a->head_dim, a->precision == TT_BF16, a->mask != nullptr);
 }
 
 uint64_t tt_cross_attention_scratch_bytes(const tt_cross_attention_args* a) {
@@ -204,7 +202,7 @@ tt_status tt_cross_attention(const tt_cross_attention_args* a, void* cuda_stream
   p.q_lengths = a->q_lengths; p.kv_lengths = a->kv_lengths; p.mask = a->mask; p.mask_b = a->mask_batch_stride; p.mask_q = a->mask_query_stride;
   p.part = static_cast<float*>(a->scratch); p.status = a->status_dev;
   p.batch = a->batch; p.q_tokens = a->q_tokens; p.kv_tokens = a->kv_tokens; p.heads = a->heads; p.group = a->heads / a->kv_heads;
-  p.splits = plan.splits; p.split_keys = plan.split_keys;
+  p.splits = plan.splits; p.split_keys = plan.split_keys; p.cluster = plan.cluster;
   p.scale_log2 = (float)((double)a->scale * 1.4426950408889634074);
   const cudaError_t e = launch_cross(p, plan, bf16, a->head_dim, reinterpret_cast<cudaStream_t>(cuda_stream));
   return e == cudaSuccess ? TT_OK : set_error(TT_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
