@@ -204,7 +204,7 @@ cudaError_t launch_scalar(const CrossParams& p, cudaStream_t s) {
 template <typename T, int D>
 cudaError_t launch_typed(const CrossParams& p, const CrossPlan& plan, cudaStream_t s) {
   cudaError_t e = cudaSuccess;
-  if constexpr (sizeof(T) == 2) e = launch_cross_few(p, D, s);
+  if constexpr (sizeof(T) == 2) e = launch_cross_few(p, D, plan.warps, s);
   else e = plan.rows == 16 ? launch_scalar<D, 16>(p, s) : launch_scalar<D, 64>(p, s);
   if (e != cudaSuccess || p.splits == 1) return e;
   const int64_t rows = (int64_t)p.q_tokens * p.group;
@@ -233,10 +233,12 @@ CrossPlan cross_plan(int batch, int q_tokens, int kv_tokens, int heads, int grou
     // a tile's keys over a cluster of blocks, down to 128 keys to a block, until there are two blocks to a multiprocessor
     while (plan.cluster < 8 && tiles * plan.cluster < 2 * PLAN_SMS && kv_tokens / (2 * plan.cluster) >= 128) plan.cluster *= 2;
     // and over several clusters, which takes a second kernel, where those leave half of the device idle and more than 1024 keys to a block
-    int64_t splits = tiles > 0 && 2 * tiles * plan.cluster < PLAN_SMS ? 2 * PLAN_SMS / (tiles * plan.cluster) : 1;
-    const int64_t most = kv_tokens / ((int64_t)plan.cluster * 512);
-    if (kv_tokens / plan.cluster <= 1024) splits = 1;
+    const int64_t blocks = tiles * plan.cluster;
+    int64_t splits = blocks > 0 && 2 * blocks <= PLAN_SMS && kv_tokens / plan.cluster > 1024 ? PLAN_SMS / blocks : 1;
+    const int64_t most = kv_tokens / ((int64_t)plan.cluster * 256);
     plan.splits = (int)(splits < most ? splits : most > 1 ? most : 1);
+    // blocks of eight warps where there is but one to a multiprocessor
+    plan.warps = blocks * plan.splits <= PLAN_SMS ? 8 : 4;
   } else {
     plan.kernel = CROSS_SCALAR;
     plan.rows = rows <= 16 ? 16 : 64;

@@ -21,14 +21,14 @@ namespace {
 constexpr int MAX_CLUSTER = 8;
 
 struct CrossFewParams {
-  TensorMap128 map_k, map_v;                   // [D][token][head][batch], box of Few<D>::KEYS tokens
+  TensorMap128 map_k, map_v;                   // [D][token][head][batch], box of Few::KEYS tokens
   CrossParams c;
   int32_t k_h, k_b, v_h, v_b;                  // 0 where the axis is shared, else 1
 };
 
-template <int D>
+template <int D, int W>
 struct Few {
-  static constexpr int WARPS = 4;
+  static constexpr int WARPS = W;
   static constexpr int THREADS = WARPS * 32;
   static constexpr int STAGES = 3;
   static constexpr int KEYS = 2048 / D;        // of a tile
@@ -41,6 +41,7 @@ struct Few {
   static constexpr int NT = D / 8;             // products across the columns of the sums
   static constexpr int OP = D + 8;             // pitch of the joint sums
   static constexpr int SMEM = WARPS * RING + 1024;
+  static constexpr int BLOCKS = W == 4 ? 2 : 1;                   // to a multiprocessor
   static_assert(WARPS * 16 * OP * 4 <= WARPS * RING, "the sums take the rings' place");
 };
 
@@ -58,12 +59,7 @@ __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
 template <int D>
 __device__ __forceinline__ uint32_t run_at(int row, int run) {
   if (D == 32) return (uint32_t)(row * 64 + ((run ^ (row >> 1 & 3)) << 4));
-  return (uint32_t)((run >> 3) * Few<D>::SLAB_BYTES + row * 128 + (((run & 7) ^ (row & 7)) << 4));
-}
-// Two neighbouring mask bytes; behind the last key none is looked at.
-__device__ __forceinline__ uint32_t mask_pair(const uint8_t* row, int key, int j1, bool pairs) {
-  if (pairs && key + 1 < j1) return *reinterpret_cast<const uint16_t*>(row + key);
-  return (key < j1 ? row[key] : 0u) | (key + 1 < j1 ? (uint32_t)row[key + 1] << 8 : 0u);
+  return (uint32_t)((run >> 3) * Few<D, 4>::SLAB_BYTES + row * 128 + (((run & 7) ^ (row & 7)) << 4));
 }
 // A pair of floats from the same place in the shared memory of block `rank` of the cluster.
 __device__ __forceinline__ float2 cluster_load(const float2* at, int rank, int cluster) {
@@ -73,9 +69,9 @@ __device__ __forceinline__ float2 cluster_load(const float2* at, int rank, int c
   return v;
 }
 
-template <int D, bool MASK>
-__global__ void __launch_bounds__(Few<D>::THREADS, 2) cross_few_kernel(const __grid_constant__ CrossFewParams pp) {
-  using F = Few<D>;
+template <int D, bool MASK, int W>
+__global__ void __launch_bounds__(Few<D, W>::THREADS, Few<D, W>::BLOCKS) cross_few_kernel(const __grid_constant__ CrossFewParams pp) {
+  using F = Few<D, W>;
   const CrossParams& p = pp.c;
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t s_full[F::WARPS][F::STAGES];
@@ -129,10 +125,20 @@ __global__ void __launch_bounds__(Few<D>::THREADS, 2) cross_few_kernel(const __g
   const bool pairs = MASK && (((uintptr_t)p.mask | (uintptr_t)p.mask_b | (uintptr_t)p.mask_q | (uintptr_t)(uint32_t)first) & 1u) == 0u;
   uint32_t seen[MASK ? F::NK : 1][2], coming[MASK ? F::NK : 1][2];    // mask bytes of keys 8 n + 2t and 8 n + 2t + 1 for both rows
   auto fetch_mask = [&](int j) {
+    if (pairs && j + F::KEYS <= j1) {
 #pragma unroll
-    for (int n = 0; n < F::NK; ++n)
+      for (int n = 0; n < F::NK; ++n)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) coming[n][i] = mask_pair(mask[i], j + 8 * n + 2 * t, j1, pairs);
+        for (int i = 0; i < 2; ++i) coming[n][i] = __ldg(reinterpret_cast<const uint16_t*>(mask[i] + j + 8 * n + 2 * t));
+    } else {
+#pragma unroll
+      for (int n = 0; n < F::NK; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int key = j + 8 * n + 2 * t;
+          coming[n][i] = (key < j1 ? mask[i][key] : 0u) | (key + 1 < j1 ? (uint32_t)mask[i][key + 1] << 8 : 0u);
+        }
+    }
   };
   if (MASK) {
 #pragma unroll
@@ -356,30 +362,32 @@ __global__ void __launch_bounds__(Few<D>::THREADS, 2) cross_few_kernel(const __g
   if (p.cluster > 1) cluster_sync_all();       // no block leaves while another reads its sums
 }
 
-template <int D, bool MASK>
+template <int D, bool MASK, int W>
 cudaError_t launch(const CrossFewParams& p, cudaStream_t s) {
+  using F = Few<D, W>;
   static OncePerContext once;
-  const cudaError_t e = once([] { return cudaFuncSetAttribute(cross_few_kernel<D, MASK>, cudaFuncAttributeMaxDynamicSharedMemorySize, Few<D>::SMEM); });
+  const cudaError_t e = once([] { return cudaFuncSetAttribute(cross_few_kernel<D, MASK, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::SMEM); });
   if (e != cudaSuccess) return e;
   const int64_t tiles = ((int64_t)p.c.q_tokens * p.c.group + 15) / 16;
-  return launch_kernel(cross_few_kernel<D, MASK>, dim3((unsigned)(tiles * p.c.splits * p.c.cluster), (unsigned)(p.c.heads / p.c.group), (unsigned)p.c.batch),
-                       Few<D>::THREADS, Few<D>::SMEM, s, p, false, p.c.cluster);
+  return launch_kernel(cross_few_kernel<D, MASK, W>, dim3((unsigned)(tiles * p.c.splits * p.c.cluster), (unsigned)(p.c.heads / p.c.group), (unsigned)p.c.batch),
+                       F::THREADS, F::SMEM, s, p, false, p.c.cluster);
 }
 template <int D>
-cudaError_t launch(const CrossParams& c, cudaStream_t s) {
+cudaError_t launch(const CrossParams& c, int warps, cudaStream_t s) {
   CrossFewParams p{};
-  const int kv_heads = c.heads / c.group;
-  if (c.kv_tokens > 0 && (!token_map(&p.map_k, c.k, D, c.kv_tokens, kv_heads, c.batch, Few<D>::KEYS) || !token_map(&p.map_v, c.v, D, c.kv_tokens, kv_heads, c.batch, Few<D>::KEYS)))
+  const int kv_heads = c.heads / c.group, keys = Few<D, 4>::KEYS;
+  if (c.kv_tokens > 0 && (!token_map(&p.map_k, c.k, D, c.kv_tokens, kv_heads, c.batch, keys) || !token_map(&p.map_v, c.v, D, c.kv_tokens, kv_heads, c.batch, keys)))
     return cudaErrorInvalidValue;
   p.c = c;
   p.k_h = c.k.h != 0; p.k_b = c.k.b != 0; p.v_h = c.v.h != 0; p.v_b = c.v.b != 0;
-  return p.c.mask ? launch<D, true>(p, s) : launch<D, false>(p, s);
+  if (warps == 8) return p.c.mask ? launch<D, true, 8>(p, s) : launch<D, false, 8>(p, s);
+  return p.c.mask ? launch<D, true, 4>(p, s) : launch<D, false, 4>(p, s);
 }
 
 }  // namespace
 
-cudaError_t launch_cross_few(const CrossParams& p, int D, cudaStream_t s) {
-  return D == 32 ? launch<32>(p, s) : D == 64 ? launch<64>(p, s) : launch<128>(p, s);
+cudaError_t launch_cross_few(const CrossParams& p, int D, int warps, cudaStream_t s) {
+  return D == 32 ? launch<32>(p, warps, s) : D == 64 ? launch<64>(p, warps, s) : launch<128>(p, warps, s);
 }
 
 }  // namespace tok

@@ -74,6 +74,11 @@ __device__ __forceinline__ unsigned long long mul2_of(unsigned long long a, unsi
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
+__device__ __forceinline__ unsigned long long sub2_of(unsigned long long a, unsigned long long b) {
+  unsigned long long r;
+  asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
 // 2^x by the special-function unit: relative error about 2^-22, results below the normal range are 0
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;

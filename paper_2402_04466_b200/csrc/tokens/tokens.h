@@ -65,14 +65,15 @@ struct alignas(32) CrossParams {
 enum { CROSS_SCALAR = 0, CROSS_TC = 1, CROSS_FEW = 2 };
 struct CrossPlan {
   int32_t kernel;               // one of CROSS_...
-  int32_t rows;                 // rows (queries x heads of a group) of a block's tile
+  int32_t rows;                 // CROSS_SCALAR: rows (queries x heads of a group) of a block's tile
+  int32_t warps;                // CROSS_FEW: of a block
   int32_t splits, split_keys, cluster;
   uint64_t scratch;
 };
 CrossPlan cross_plan(int batch, int q_tokens, int kv_tokens, int heads, int group, int D, bool bf16, bool mask);
 cudaError_t launch_cross(const CrossParams& p, const CrossPlan& plan, bool bf16, int D, cudaStream_t s);
 
-cudaError_t launch_cross_few(const CrossParams& p, int D, cudaStream_t s);   // splits > 1: the join is the caller's
+cudaError_t launch_cross_few(const CrossParams& p, int D, int warps, cudaStream_t s);   // splits > 1: the join is the caller's
 cudaError_t launch_cross_tc(const CrossParams& p, int D, cudaStream_t s);
 
 // Tensor map of a bf16 view, boxes of `box` tokens of one head.  An axis of stride 0 has one place.
