@@ -221,8 +221,9 @@ cudaError_t launch_typed(const CrossParams& p, const CrossPlan& plan, int D, cud
 CrossPlan cross_plan(int batch, int q_tokens, int kv_tokens, int heads, int group, int D, bool bf16, bool mask) {
   CrossPlan plan{};
   plan.splits = plan.cluster = 1;
-  if (bf16 && !mask && q_tokens > 64) {
+  if (bf16 && !mask && q_tokens > 64 && kv_tokens > 0) {
     plan.kernel = CROSS_TC;
+    plan.scratch = cross_tc_scratch(batch, q_tokens, kv_tokens, heads, D);
     return plan;
   }
   const int64_t rows = (int64_t)q_tokens * group;

@@ -1,6 +1,16 @@
 // Cross attention of many bf16 queries on the tensor cores (tt_cross_attention without a mask).
 //
-//   S = Q K^T (128 queries x 128 keys),  P = 2^(c S - c m),  O += P V,  l += sum P,  c = scale * log2(e)
+//   S = Q K^T (tiles of 128 queries x 64 or 128 keys),  P = 2^(c S - c m),  O += P V,  l += sum P,  c = scale * log2(e)
+//
+// A thread owns a query's row: its scores come from tensor memory into registers, its weights go back there as the second product's
+// operand, the sums O stay there.  The running maximum m only moves when a weight would pass 2^8, so O is hardly ever rescaled.
+// The work is tiles of queries x tiles of keys; a block takes an equal run of it, whatever tiles that cuts in two (a
+// grid of one block per tile left half of the device idle in its last round), and where a tile is cut its blocks
+// leave partial sums that cross_tc_join_kernel adds in order.
+//
+// Bound by the warps that turn scores into weights: the exponentials alone (16 a cycle and multiprocessor) take 1024 cycles for a
+// tile of 128 x 128 whose two products take 512 with heads of 64, and a warp needs about 1400 more for the rest, of which the
+// other tile's warps hide a part: 1500 cycles a tile and multiprocessor.
 #include "tokens.h"
 
 #include <cuda.h>
@@ -11,79 +21,157 @@ namespace tt {
 namespace tok {
 namespace {
 
-constexpr int BM = 128, BN = 128;
+constexpr int BM = 128;                      // queries of a tile
+constexpr int MAX_ENTRIES = 256;             // of the batch in a launch: their work is added up in shared memory
+constexpr int LEAST = 512;                     // keys to a block
 
 struct CrossTcParams {
-  TensorMap128 map_q, map_k, map_v;      // [D][token][head][batch], box of 128 tokens
+  TensorMap128 map_q, map_k, map_v;      // [D][token][head][batch], boxes of 128 queries and of BN keys
   View o;
   const int32_t* q_lengths;
   const int32_t* kv_lengths;
+  float* part;                           // two places a block: rows' maximum and total, then their sums
   int32_t* status;
-  int32_t q_tokens, kv_tokens, heads, group, q_tiles;
+  int32_t q_tokens, kv_tokens, heads, group, batch, b0;   // entries b0 .. b0 + batch - 1
   int32_t q_h, q_b, k_h, k_b, v_h, v_b;  // 0 where the axis is shared, else 1
   float scale_log2;
 };
 
-template <int D, int TILES>
+template <int D>
 struct Cfg {
+  // Tiles of queries of a block, blocks of a multiprocessor and keys of a tile: two tiles of queries to a multiprocessor either way, each
+  // with columns of tensor memory of its own for scores (BN), weights (BN / 2) and sums (D).  Heads of 128 share their keys
+  // between the two, or the copies into shared memory would be too many.
+  static constexpr int TILES = D == 128 ? 2 : 1, BLOCKS = D == 128 ? 1 : 2, BN = D == 128 ? 64 : 128;
+  static constexpr int HALVES = BN / 64;                            // weights are handed over 64 keys at a time
+  static constexpr int ROWS = TILES * BM;
   static constexpr int ROW = D == 32 ? 64 : 128;                    // bytes of a row in a slab
   static constexpr int SLABS = D == 128 ? 2 : 1;
-  static constexpr int SLAB_BYTES = BM * ROW;
-  static constexpr int TILE_BYTES = SLABS * SLAB_BYTES;             // 128 tokens of one operand
+  static constexpr int Q_SLAB = BM * ROW, KV_SLAB = BN * ROW;
+  static constexpr int Q_BYTES = SLABS * Q_SLAB, KV_BYTES = SLABS * KV_SLAB;
   static constexpr uint32_t LAYOUT = D == 32 ? 4u : 2u;             // 64- or 128-byte swizzle
-  static constexpr int STAGES = 2;
-  static constexpr int THREADS = TILES * 128 + 64;
-  static constexpr int BLOCKS = TILES == 1 ? 2 : 1;                 // to a multiprocessor
-  static constexpr int O_COL = TILES * BN;
-  static constexpr uint32_t TMEM = TILES * (BN + D) <= 256 ? 256 : 512;
-  static constexpr int BAR_BYTES = 256;
-  static constexpr int SMEM = (TILES + 2 * STAGES) * TILE_BYTES + BAR_BYTES + 1024;
-  static_assert(SMEM * BLOCKS <= 227 * 1024, "shared memory");
+  static constexpr int STAGES = D == 128 ? 4 : 2;
+  static constexpr int THREADS = TILES * (128 + 64);
+  static constexpr uint32_t P_COL = TILES * BN, O_COL = P_COL + TILES * BN / 2, TMEM = D == 128 ? 512 : 256;
+  static constexpr int SMEM = TILES * Q_BYTES + 2 * STAGES * KV_BYTES + 256 + 1024;
+  static constexpr int64_t PLACE = (int64_t)ROWS * (D + 2);         // floats of a partial result
+  static_assert(O_COL + TILES * D <= TMEM && TMEM * BLOCKS <= 512 && (SMEM + 6 * 1024) * BLOCKS <= 227 * 1024, "tensor and shared memory");
 };
 
-template <int D, int TILES>
-__global__ void __launch_bounds__(Cfg<D, TILES>::THREADS, Cfg<D, TILES>::BLOCKS) cross_tc_kernel(const __grid_constant__ CrossTcParams p) {
-  using C = Cfg<D, TILES>;
-  constexpr int STAGES = C::STAGES;
+// The launch's work: iterations (tile of queries x tile of keys) in the order entry, head, tile of queries, tile of keys.
+struct Work {
+  int64_t before[MAX_ENTRIES + 1];       // iterations before an entry's
+  int32_t rows[MAX_ENTRIES], keys[MAX_ENTRIES];
+};
+template <int D>
+__device__ __forceinline__ void add_up(Work& w, const CrossTcParams& p) {
+  for (int i = threadIdx.x; i < p.batch; i += blockDim.x) {
+    w.rows[i] = clamp_length(p.q_lengths, p.b0 + i, p.q_tokens);
+    w.keys[i] = clamp_length(p.kv_lengths, p.b0 + i, p.kv_tokens);
+  }
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    int64_t sum = 0;
+    for (int i0 = 0; i0 < p.batch; i0 += 32) {
+      const int i = i0 + threadIdx.x;
+      int64_t mine = i < p.batch ? (int64_t)((w.rows[i] + Cfg<D>::ROWS - 1) / Cfg<D>::ROWS) * p.heads * max(1, (w.keys[i] + Cfg<D>::BN - 1) / Cfg<D>::BN) : 0;
+      for (int o = 1; o < 32; o <<= 1) {
+        const int64_t other = __shfl_up_sync(0xffffffffu, mine, o);
+        if ((int)threadIdx.x >= o) mine += other;
+      }
+      if (i < p.batch) w.before[i + 1] = sum + mine;
+      sum += __shfl_sync(0xffffffffu, mine, 31);
+    }
+    if (threadIdx.x == 0) w.before[0] = 0;
+  }
+  __syncthreads();
+}
+template <int D>
+__device__ __forceinline__ int64_t share_of(const Work& w, const CrossTcParams& p) {
+  const int64_t each = (w.before[p.batch] + gridDim.x - 1) / gridDim.x;
+  return each < LEAST / Cfg<D>::BN ? LEAST / Cfg<D>::BN : each;
+}
+
+// A block's way through its work: the run it is at, and the step to the next.
+struct Cursor {
+  int64_t at, end;
+  int b, h, row0, j0, j1, n;             // entry, head, first row; of the tile's n tiles of keys those from j0 to j1
+  __device__ __forceinline__ bool done() const { return at >= end; }
+  template <int D>
+  __device__ __forceinline__ void find(const Work& w, const CrossTcParams& p) {
+    if (done()) return;
+    while (w.before[b + 1] <= at) ++b;
+    n = max(1, (w.keys[b] + Cfg<D>::BN - 1) / Cfg<D>::BN);
+    const int tiles = (w.rows[b] + Cfg<D>::ROWS - 1) / Cfg<D>::ROWS;
+    const int64_t rel = at - w.before[b], t = rel / n;
+    h = (int)(t / tiles);
+    row0 = (int)(t - (int64_t)h * tiles) * Cfg<D>::ROWS;
+    j0 = (int)(rel - t * n);
+    j1 = (int)min((int64_t)n, j0 + (end - at));
+  }
+  template <int D>
+  __device__ __forceinline__ void start(const Work& w, const CrossTcParams& p) {
+    const int64_t each = share_of<D>(w, p);
+    at = min((int64_t)blockIdx.x * each, w.before[p.batch]);
+    end = min(at + each, w.before[p.batch]);
+    b = 0;
+    find<D>(w, p);
+  }
+  template <int D>
+  __device__ __forceinline__ void next(const Work& w, const CrossTcParams& p) {
+    at += j1 - j0;
+    find<D>(w, p);
+  }
+};
+
+template <int D>
+__global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::BLOCKS) cross_tc_kernel(const __grid_constant__ CrossTcParams p) {
+  using C = Cfg<D>;
+  constexpr int STAGES = C::STAGES, TILES = C::TILES;
   extern __shared__ uint8_t smem_raw[];
+  __shared__ Work work;
   uint8_t* s_q = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  uint8_t* s_k = s_q + TILES * C::TILE_BYTES;
-  uint8_t* s_v = s_k + STAGES * C::TILE_BYTES;
-  uint64_t* qfull = reinterpret_cast<uint64_t*>(s_v + STAGES * C::TILE_BYTES);
-  uint64_t* kfull = qfull + 1;                 // [STAGES]
-  uint64_t* kempty = kfull + STAGES;
-  uint64_t* vfull = kempty + STAGES;
-  uint64_t* vempty = vfull + STAGES;
-  uint64_t* sfull = vempty + STAGES;           // [TILES] scores are there
-  uint64_t* pfull = sfull + TILES;             // [TILES] weights are there
-  uint64_t* ofull = pfull + TILES;             // [TILES] last product is done
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ofull + TILES);
+  uint8_t* s_k = s_q + TILES * C::Q_BYTES;
+  uint8_t* s_v = s_k + STAGES * C::KV_BYTES;
+  uint64_t* qfull = reinterpret_cast<uint64_t*>(s_v + STAGES * C::KV_BYTES);
+  uint64_t* qempty = qfull + 1;                // the empty ones, signalled by every tile's warp, where a block has several tiles
+  uint64_t* kfull = qempty + 1;                // [STAGES]
+  uint64_t* kempty = kfull + STAGES;           // [STAGES]
+  uint64_t* vfull = kempty + STAGES;           // [STAGES]
+  uint64_t* vempty = vfull + STAGES;           // [STAGES]
+  uint64_t* sfull = vempty + STAGES;           // [TILES] scores are there, and the keys have been read
+  uint64_t* sread = sfull + TILES;             // [TILES] scores are in registers
+  uint64_t* pfull = sread + TILES;             // [TILES][HALVES] weights are there, 64 keys each
+  uint64_t* pdone = pfull + C::HALVES * TILES; // [TILES] their product is done, and the values have been read
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(pdone + TILES);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* s_status = reinterpret_cast<int*>(tmem_slot + 2);
 
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
-  const int b = blockIdx.z, h = blockIdx.y, row0 = (int)blockIdx.x * (BM * TILES);
-  const int rows = clamp_length(p.q_lengths, b, p.q_tokens), keys = clamp_length(p.kv_lengths, b, p.kv_tokens);
-  if (row0 >= rows) return;
-  const int n = (keys + BN - 1) / BN;
   if (threadIdx.x == 0) {
     mbar_init(smem_u32(qfull), 1);
+    mbar_init(smem_u32(qempty), TILES);
     for (int s = 0; s < STAGES; ++s) {
       mbar_init(smem_u32(kfull + s), 1);
-      mbar_init(smem_u32(kempty + s), 1);
       mbar_init(smem_u32(vfull + s), 1);
-      mbar_init(smem_u32(vempty + s), 1);
+      mbar_init(smem_u32(kempty + s), TILES);
+      mbar_init(smem_u32(vempty + s), TILES);
     }
     for (int t = 0; t < TILES; ++t) {
       mbar_init(smem_u32(sfull + t), 1);
-      mbar_init(smem_u32(pfull + t), 4);
-      mbar_init(smem_u32(ofull + t), 1);
+      mbar_init(smem_u32(sread + t), 4);
+      for (int x = 0; x < C::HALVES; ++x) mbar_init(smem_u32(pfull + C::HALVES * t + x), 4);
+      mbar_init(smem_u32(pdone + t), 1);
     }
     *abort_flag = 0;
     *s_status = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == TILES * 4 + 1) {
+  add_up<D>(work, p);
+  Cursor cur;
+  cur.start<D>(work, p);
+  if (cur.done()) return;                      // the whole block
+  if (warp == TILES * 4) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(C::TMEM) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -92,135 +180,206 @@ __global__ void __launch_bounds__(Cfg<D, TILES>::THREADS, Cfg<D, TILES>::BLOCKS)
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
 
-  if (warp == TILES * 4) {
-    // ------------------------------------------------------------------------------ loads
-    if (lane == 0 && n > 0) {
-      const int hk = h / p.group;
-      auto load = [&](uint8_t* dst, const void* map, uint64_t* bar, int row, int hh, int bb) {
-        for (int s = 0; s < C::SLABS; ++s) tma_load_4d(smem_u32(dst + s * C::SLAB_BYTES), map, smem_u32(bar), s * 64, row, hh, bb);
-      };
-      mbar_arrive_expect_tx(smem_u32(qfull), TILES * C::TILE_BYTES);
-      for (int t = 0; t < TILES; ++t) load(s_q + t * C::TILE_BYTES, &p.map_q, qfull, row0 + t * BM, h * p.q_h, b * p.q_b);
-      uint32_t stage = 0, phase = 0;
-      for (int j = 0; j < n; ++j) {
-        if (!mbar_wait(smem_u32(kempty + stage), phase ^ 1u, abort_flag, s_status, WAIT_CROSS_TC + (int)stage, WAIT_LIMIT)) break;
-        mbar_arrive_expect_tx(smem_u32(kfull + stage), C::TILE_BYTES);
-        load(s_k + stage * C::TILE_BYTES, &p.map_k, kfull + stage, j * BN, hk * p.k_h, b * p.k_b);
-        if (!mbar_wait(smem_u32(vempty + stage), phase ^ 1u, abort_flag, s_status, WAIT_CROSS_TC + 0x10 + (int)stage, WAIT_LIMIT)) break;
-        mbar_arrive_expect_tx(smem_u32(vfull + stage), C::TILE_BYTES);
-        load(s_v + stage * C::TILE_BYTES, &p.map_v, vfull + stage, j * BN, hk * p.v_h, b * p.v_b);
-        if (++stage == STAGES) { stage = 0; phase ^= 1u; }
-      }
-    }
-  } else if (warp == TILES * 4 + 1) {
-    // ----------------------------------------------------------------------------- products
+  bool ok = true;
+  auto wait_all = [&](uint64_t* bar, uint32_t phase, int code) {      // a whole warp: its lanes go on or stop together
+    if (__builtin_expect(__all_sync(0xffffffffu, mbar_test(smem_u32(bar), phase & 1u)), 1)) return true;
+    ok = __all_sync(0xffffffffu, mbar_wait_uniform(smem_u32(bar), phase & 1u, abort_flag, s_status, WAIT_CROSS_TC + code, WAIT_LIMIT));
+    return ok;
+  };
+
+  if (warp >= TILES * 4) {
+    // ------------------------------------------------------------------------- loads and products
+    // Two warps for each tile of queries: one issues the scores' products, the other the weights'; the first tile's also load queries and
+    // keys, and values.  What an iteration costs
+    // here is latency: about 10 cycles an instruction, 50 a product, 200 a wait.  One warp for both kinds took 3200 cycles an iteration,
+    // and the weights' warps waited for it half of the time.  Loops run on values that the compiler knows to be the whole
+    // warp's (broadcast, or counted), waits are straight-line code, and lanes vote once an iteration.
     const bool issuer = elect_one();
-    constexpr uint32_t QK = make_idesc(BM, BN), PV = make_idesc(BM, D) | B_BY_ROWS;
-    const uint64_t q0 = make_smem_desc(smem_u32(s_q), 8 * C::ROW, C::LAYOUT), k0 = make_smem_desc(smem_u32(s_k), 8 * C::ROW, C::LAYOUT);
-    const uint64_t v0 = make_rows_desc(smem_u32(s_v), C::SLAB_BYTES, 8 * C::ROW, C::LAYOUT);
-    bool ok = true;
-    auto scores = [&](int t, uint32_t stage) {
-      if (issuer) {
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          const uint64_t at = (uint64_t)((k / 4) * (C::SLAB_BYTES >> 4) + (k % 4) * 2);
-          umma_bf16(tmem + (uint32_t)(t * BN), q0 + (uint64_t)(t * (C::TILE_BYTES >> 4)) + at, k0 + (uint64_t)stage * (C::TILE_BYTES >> 4) + at, QK, k > 0);
-        }
-        umma_commit(smem_u32(sfull + t));
-      }
-      __syncwarp();
+    const int role = warp - TILES * 4, t = role >> 1;
+    const bool keys = (role & 1) == 0, loads = t == 0;
+    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), scores = tm + (uint32_t)(t * C::BN), weights = tm + C::P_COL + (uint32_t)(t * (C::BN / 2)),
+                   sums = tm + C::O_COL + (uint32_t)(t * D);
+    auto arrived = [&](uint64_t* bar, uint32_t parity, int code) {
+      if (__all_sync(0xffffffffu, mbar_test(smem_u32(bar), parity & 1u))) return;
+      ok &= mbar_wait_uniform(smem_u32(bar), parity & 1u, abort_flag, s_status, WAIT_CROSS_TC + code, WAIT_LIMIT);
     };
-    uint32_t stage = 0, phase = 0;               // of K one tile ahead of V's
-    uint32_t vstage = 0, vphase = 0;
-    if (n > 0) {
-      ok = mbar_wait(smem_u32(qfull), 0, abort_flag, s_status, WAIT_CROSS_TC + 0x20, WAIT_LIMIT) &&
-           mbar_wait(smem_u32(kfull), 0, abort_flag, s_status, WAIT_CROSS_TC + 0x30, WAIT_LIMIT);
-      ok = __all_sync(0xffffffffu, ok);
-      if (ok) {
-        for (int t = 0; t < TILES; ++t) scores(t, 0);
-        if (issuer) umma_commit(smem_u32(kempty));
-        if (++stage == STAGES) { stage = 0; phase ^= 1u; }
-      }
-    }
-    for (int j = 0; j < n && ok; ++j) {
-      ok = mbar_wait(smem_u32(vfull + vstage), vphase, abort_flag, s_status, WAIT_CROSS_TC + 0x40 + (int)vstage, WAIT_LIMIT);
-      if (j + 1 < n) ok = ok && mbar_wait(smem_u32(kfull + stage), phase, abort_flag, s_status, WAIT_CROSS_TC + 0x30 + (int)stage, WAIT_LIMIT);
-      if (!__all_sync(0xffffffffu, ok)) break;
-      const int rem = keys - j * BN;
-      if (rem < BN) {
-        // rows behind the last key may hold anything, and their weights of 0 would make NaN of it
-        for (int s = 0; s < C::SLABS; ++s)
-          for (int i = rem * C::ROW + lane * 16; i < C::SLAB_BYTES; i += 512)
-            *reinterpret_cast<uint4*>(s_v + vstage * C::TILE_BYTES + s * C::SLAB_BYTES + i) = make_uint4(0u, 0u, 0u, 0u);
-        fence_proxy_async_smem();
-        __syncwarp();
-      }
-      for (int t = 0; t < TILES; ++t) {
-        ok = mbar_wait(smem_u32(pfull + t), (uint32_t)(j & 1), abort_flag, s_status, WAIT_CROSS_TC + 0x50 + t, WAIT_LIMIT);
-        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-        tc_fence_after();
-        if (issuer) {
+    // tiles of keys are loaded STAGES ahead of their use: `ahead` is the next to load
+    Cursor ahead = cur;
+    int ab = __shfl_sync(0xffffffffu, p.b0 + ahead.b, 0), ah = __shfl_sync(0xffffffffu, ahead.h / p.group, 0), aj = __shfl_sync(0xffffffffu, ahead.j0, 0),
+        left = __shfl_sync(0xffffffffu, ahead.j1 - ahead.j0, 0);      // of its run
+    uint8_t* ring = keys ? s_k : s_v;
+    uint64_t* full = keys ? kfull : vfull;
+    const void* map = keys ? &p.map_k : &p.map_v;
+    const int mul_h = keys ? p.k_h : p.v_h, mul_b = keys ? p.k_b : p.v_b;
+    auto load_next = [&](uint32_t stage) {
+      if (!loads || left == 0) return;
+      if (issuer) {
+        mbar_arrive_expect_tx(smem_u32(full + stage), C::KV_BYTES);
 #pragma unroll
-          for (int k = 0; k < BN / 16; ++k)
-            umma_bf16_ts(tmem + (uint32_t)(C::O_COL + t * D), tmem + (uint32_t)(t * BN + k * 8),
-                         v0 + (uint64_t)vstage * (C::TILE_BYTES >> 4) + (uint64_t)(k * (16 * C::ROW >> 4)), PV, j > 0 || k > 0);
-          if (j + 1 == n) umma_commit(smem_u32(ofull + t));
+        for (int s = 0; s < C::SLABS; ++s)
+          tma_load_4d(smem_u32(ring + stage * C::KV_BYTES + s * C::KV_SLAB), map, smem_u32(full + stage), s * 64, aj * C::BN, ah * mul_h, ab * mul_b);
+      }
+      ++aj;
+      if (--left == 0) {                       // on to the next run
+        ahead.next<D>(work, p);
+        if (__shfl_sync(0xffffffffu, (int)ahead.done(), 0) == 0) {
+          ab = __shfl_sync(0xffffffffu, p.b0 + ahead.b, 0);
+          ah = __shfl_sync(0xffffffffu, ahead.h / p.group, 0);
+          aj = __shfl_sync(0xffffffffu, ahead.j0, 0);
+          left = __shfl_sync(0xffffffffu, ahead.j1 - ahead.j0, 0);
+        }
+      }
+    };
+    uint32_t stage = 0, phase = 0, runs = 0, it = 0;
+    if (keys) {
+      constexpr uint32_t QK = make_idesc(BM, C::BN);
+      const uint64_t q0 = make_smem_desc(smem_u32(s_q + t * C::Q_BYTES), 8 * C::ROW, C::LAYOUT), k0 = make_smem_desc(smem_u32(s_k), 8 * C::ROW, C::LAYOUT);
+      auto load_queries = [&]() {
+        if (issuer && loads) {
+          mbar_arrive_expect_tx(smem_u32(qfull), TILES * C::Q_BYTES);
+          for (int i = 0; i < TILES; ++i)
+            for (int s = 0; s < C::SLABS; ++s)
+              tma_load_4d(smem_u32(s_q + i * C::Q_BYTES + s * C::Q_SLAB), &p.map_q, smem_u32(qfull), s * 64, cur.row0 + i * BM, cur.h * p.q_h, (p.b0 + cur.b) * p.q_b);
         }
         __syncwarp();
-        if (j + 1 < n) scores(t, stage);
+      };
+      load_queries();
+#pragma unroll
+      for (int s = 0; s < STAGES; ++s) load_next(s);
+      while (__shfl_sync(0xffffffffu, (int)cur.done(), 0) == 0) {
+        const int n = __shfl_sync(0xffffffffu, cur.j1 - cur.j0, 0);
+        arrived(qfull, runs++, 0x20);
+        for (int j = 0; j < n; ++j, ++it) {
+          arrived(full + stage, phase, 0x28 + (int)stage);
+          if (it > 0) arrived(sread + t, it - 1, 0x30 + t);
+          tc_fence_after();
+          if (issuer) {
+            const uint64_t kd = k0 + (uint64_t)stage * (C::KV_BYTES >> 4);
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k)
+              umma_bf16(scores, q0 + (uint64_t)((k / 4) * (C::Q_SLAB >> 4) + (k % 4) * 2), kd + (uint64_t)((k / 4) * (C::KV_SLAB >> 4) + (k % 4) * 2), QK, k > 0);
+            umma_commit(smem_u32(sfull + t));
+            if (TILES > 1) {
+              umma_commit(smem_u32(kempty + stage));
+              if (j + 1 == n) umma_commit(smem_u32(qempty));
+            }
+          }
+          if (j + 1 == n) {                    // the run's queries have been read behind this product
+            cur.next<D>(work, p);
+          }
+          // the tile's place is free when every tile of queries has read it (a parity of another tile's sfull would not do: that tile may
+          // be two iterations ahead)
+          if (loads) {
+            if (TILES > 1) arrived(kempty + stage, phase, 0x10 + (int)stage);
+            else arrived(sfull, it, 0x58);
+            load_next(stage);
+          }
+          if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+          if (__any_sync(0xffffffffu, !ok)) break;
+        }
+        if (__any_sync(0xffffffffu, !ok)) break;
+        if (__shfl_sync(0xffffffffu, (int)cur.done(), 0) == 0) {
+          if (TILES > 1 && loads) arrived(qempty, runs - 1, 0x00);
+          load_queries();
+        }
       }
-      if (!ok) break;
-      if (issuer) {
-        umma_commit(smem_u32(vempty + vstage));
-        if (j + 1 < n) umma_commit(smem_u32(kempty + stage));
+    } else {
+      constexpr uint32_t PV = make_idesc(BM, D) | B_BY_ROWS;
+      const uint64_t v0 = make_rows_desc(smem_u32(s_v), C::KV_SLAB, 8 * C::ROW, C::LAYOUT);
+#pragma unroll
+      for (int s = 0; s < STAGES; ++s) load_next(s);
+      while (__shfl_sync(0xffffffffu, (int)cur.done(), 0) == 0) {
+        const int n = __shfl_sync(0xffffffffu, cur.j1 - cur.j0, 0);
+        // keys of the run's last tile: fewer than BN where it is the last of all
+        const int rem = __shfl_sync(0xffffffffu, work.keys[cur.b] - (cur.j1 - 1) * C::BN, 0);
+        cur.next<D>(work, p);
+        for (int j = 0; j < n; ++j, ++it) {
+          arrived(full + stage, phase, 0x38 + (int)stage);
+          if (j + 1 == n && rem < C::BN) {
+            // rows behind the last key may hold anything, and their weights of 0 would make NaN of it
+            for (int s = 0; s < C::SLABS; ++s)
+              for (int i = rem * C::ROW + lane * 16; i < C::KV_SLAB; i += 512)
+                *reinterpret_cast<uint4*>(s_v + stage * C::KV_BYTES + s * C::KV_SLAB + i) = make_uint4(0u, 0u, 0u, 0u);
+            fence_proxy_async_smem();
+            __syncwarp();
+          }
+          const uint64_t vd = v0 + (uint64_t)stage * (C::KV_BYTES >> 4);
+#pragma unroll
+          for (int x = 0; x < C::HALVES; ++x) {
+            arrived(pfull + C::HALVES * t + x, it, 0x40 + C::HALVES * t + x);
+            tc_fence_after();
+            if (issuer) {
+#pragma unroll
+              for (int k = 4 * x; k < 4 * x + 4; ++k)
+                umma_bf16_ts(sums, weights + (uint32_t)(k * 8), vd + (uint64_t)(k * C::ROW), PV, k > 0 ? 1u : j > 0 ? 1u : 0u);
+            }
+          }
+          if (issuer) {
+            umma_commit(smem_u32(pdone + t));
+            if (TILES > 1) umma_commit(smem_u32(vempty + stage));
+          }
+          if (loads) {
+            if (TILES > 1) arrived(vempty + stage, phase, 0x18 + (int)stage);
+            else arrived(pdone, it, 0x60);
+            load_next(stage);
+          }
+          if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+          if (__any_sync(0xffffffffu, !ok)) break;
+        }
+        if (__any_sync(0xffffffffu, !ok)) break;
       }
-      __syncwarp();
-      if (++vstage == STAGES) { vstage = 0; vphase ^= 1u; }
-      if (++stage == STAGES) { stage = 0; phase ^= 1u; }
     }
   } else {
     // ------------------------------------------------------------------------------ weights
-    const int t = warp >> 2, quarter = warp & 3, row = row0 + t * BM + quarter * 32 + lane;
-    const uint32_t s_addr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(t * BN);
-    const uint32_t o_addr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(C::O_COL + t * D);
+    const int t = warp >> 2, quarter = warp & 3, r = t * BM + quarter * 32 + lane;      // row of the block's tile
+    const uint32_t s_addr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(t * C::BN);
+    const uint32_t p_addr = tmem + ((uint32_t)(quarter * 32) << 16) + C::P_COL + (uint32_t)(t * (C::BN / 2));
+    const uint32_t o_addr = tmem + ((uint32_t)(quarter * 32) << 16) + C::O_COL + (uint32_t)(t * D);
     const float c = p.scale_log2;
     const unsigned long long c2 = pack2(c, c);
-    float m = -INFINITY;
-    unsigned long long l0 = pack2(0.f, 0.f), l1 = l0;
-    bool ok = true;
-    for (int j = 0; j < n; ++j) {
-      ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(sfull + t), (uint32_t)(j & 1), abort_flag, s_status, WAIT_CROSS_TC + 0x60 + t, WAIT_LIMIT));
-      if (!ok) break;
+    uint32_t it = 0;
+    while (ok && !cur.done()) {
+      const int count = cur.j1 - cur.j0, last_keys = work.keys[cur.b] - (cur.j1 - 1) * C::BN;      // of the run's last tile: all of its places or fewer
+      float m = -INFINITY;
+      unsigned long long l[4] = {pack2(0.f, 0.f), pack2(0.f, 0.f), pack2(0.f, 0.f), pack2(0.f, 0.f)};      // four chains
+      for (int j = 0; j < count; ++j, ++it) {
+      if (!wait_all(sfull + t, it, 0x50 + t)) break;
       tc_fence_after();
-      uint32_t v[4][32];
+      uint32_t v[C::BN / 32][32];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) tmem_ld32_async(s_addr + 32 * i, v[i]);
+      for (int i = 0; i < C::BN / 32; ++i) tmem_ld32_async(s_addr + 32 * i, v[i]);
       tmem_wait_ld();
-      const int rem = keys - j * BN;
-      if (rem < BN) {
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(sread + t));
+      if (__builtin_expect(j + 1 == count && last_keys < C::BN, 0)) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < C::BN / 32; ++i)
 #pragma unroll
           for (int x = 0; x < 32; ++x)
-            if (32 * i + x >= rem) v[i][x] = 0xFF800000u;
+            if (32 * i + x >= last_keys) v[i][x] = 0xFF800000u;
       }
-      float top[4];
+      float top[C::BN / 32];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        top[i] = __uint_as_float(v[i][0]);
+      for (int i = 0; i < C::BN / 32; ++i) {
+        top[i] = max3(__uint_as_float(v[i][0]), __uint_as_float(v[i][1]), __uint_as_float(v[i][31]));
 #pragma unroll
-        for (int x = 1; x < 31; x += 2) top[i] = max3(top[i], __uint_as_float(v[i][x]), __uint_as_float(v[i][x + 1]));
-        top[i] = fmaxf(top[i], __uint_as_float(v[i][31]));
+        for (int x = 2; x < 30; x += 2) top[i] = max3(top[i], __uint_as_float(v[i][x]), __uint_as_float(v[i][x + 1]));
+        top[i] = max3(top[i], top[i], __uint_as_float(v[i][30]));
       }
-      const float now = fmaxf(max3(top[0], top[1], top[2]), top[3]);
+      float now = max3(top[0], top[0], top[1]);
+      if constexpr (C::BN == 128) now = max3(now, top[2], top[3]);
+      // the product before must be done: its weights make room, and the sums may be rescaled
+      if (it > 0 && !wait_all(pdone + t, it - 1, 0x58 + t)) break;
       // the maximum only moves when a weight would pass 2^8: until then the sums keep their scale, which loses nothing in fp32
       const bool moved = (now - m) * c > 8.f;
-      if (__any_sync(0xffffffffu, moved)) {
+      if (__builtin_expect(__any_sync(0xffffffffu, moved), 0)) {
         if (j > 0) {
+          tc_fence_after();
           const float fade = moved ? exp2_fast((m - now) * c) : 1.f;
           const unsigned long long f2 = pack2(fade, fade);
-          l0 = mul2_of(l0, f2);
-          l1 = mul2_of(l1, f2);
+#pragma unroll
+          for (int x = 0; x < 4; ++x) l[x] = mul2_of(l[x], f2);
 #pragma unroll 1
           for (int i = 0; i < D / 8; ++i) {
             uint32_t o[8];
@@ -235,54 +394,65 @@ __global__ void __launch_bounds__(Cfg<D, TILES>::THREADS, Cfg<D, TILES>::BLOCKS)
       const float mc = m == -INFINITY ? 0.f : -m * c;
       const unsigned long long mc2 = pack2(mc, mc);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < C::BN / 32; ++i) {
         uint32_t w[16];
 #pragma unroll
         for (int x = 0; x < 16; ++x) {
           float lo, hi;
-          unpack2(fma2_of(pack2(__uint_as_float(v[i][2 * x]), __uint_as_float(v[i][2 * x + 1])), c2, mc2), lo, hi);
+          const unsigned long long a = fma2_of(pack2(__uint_as_float(v[i][2 * x]), __uint_as_float(v[i][2 * x + 1])), c2, mc2);
+          unpack2(a, lo, hi);
           lo = exp2_fast(lo);
           hi = exp2_fast(hi);
-          if (x & 1) l1 = add2_of(l1, pack2(lo, hi));
-          else l0 = add2_of(l0, pack2(lo, hi));
+          l[x & 3] = add2_of(l[x & 3], pack2(lo, hi));
           w[x] = pack_bf16(lo, hi);
         }
-        tmem_st16(s_addr + 16 * i, w);
+        tmem_st16(p_addr + 16 * i, w);
+        if (i & 1) {
+          tmem_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(pfull + C::HALVES * t + (i >> 1)));
+        }
       }
-      tmem_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(pfull + t));
-    }
-    if (ok) {
-      float inv = 0.f;
-      if (n > 0) {
-        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(ofull + t), 0, abort_flag, s_status, WAIT_CROSS_TC + 0x70 + t, WAIT_LIMIT));
-        tc_fence_after();
-        float a0, a1, a2, a3;
-        unpack2(l0, a0, a1);
-        unpack2(l1, a2, a3);
-        inv = 1.f / ((a0 + a1) + (a2 + a3));
       }
-      if (ok) {
-        __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.o.p) + b * p.o.b + (int64_t)row * p.o.t + h * p.o.h;
+      // the run's end
+      if (!ok || !wait_all(pdone + t, it - 1, 0x60 + t)) break;
+      tc_fence_after();
+      float a0, a1;
+      unpack2(add2_of(add2_of(l[0], l[1]), add2_of(l[2], l[3])), a0, a1);
+      const float total = a0 + a1;
+      const bool here = cur.row0 + r < work.rows[cur.b];
+      if (cur.j0 == 0 && cur.j1 == cur.n) {
+        const float inv = total == 0.f ? 0.f : 1.f / total;      // nothing seen: zeros
+        __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.o.p) + (p.b0 + cur.b) * p.o.b + (int64_t)(cur.row0 + r) * p.o.t + cur.h * p.o.h;
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) {
           uint32_t o[32];
-          if (n > 0) tmem_ld32(o_addr + 32 * i, o);
-          if (row < rows) {
+          tmem_ld32(o_addr + 32 * i, o);
+          if (here) {
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-              uint4 u = make_uint4(0u, 0u, 0u, 0u);
-              if (n > 0) {
-                auto two = [&](int y) { return pack_bf16(__uint_as_float(o[8 * x + y]) * inv, __uint_as_float(o[8 * x + y + 1]) * inv); };
-                u = make_uint4(two(0), two(2), two(4), two(6));
-              }
-              *reinterpret_cast<uint4*>(dst + 32 * i + 8 * x) = u;
+              auto two = [&](int y) { return pack_bf16(__uint_as_float(o[8 * x + y]) * inv, __uint_as_float(o[8 * x + y + 1]) * inv); };
+              *reinterpret_cast<uint4*>(dst + 32 * i + 8 * x) = make_uint4(two(0), two(2), two(4), two(6));
             }
           }
         }
+      } else {
+        float* place = p.part + ((int64_t)blockIdx.x * 2 + (cur.j0 == 0)) * C::PLACE;
+        reinterpret_cast<float2*>(place)[r] = make_float2(m * c, total);
+        float* dst = place + 2 * C::ROWS + r * D;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+          uint32_t o[32];
+          tmem_ld32(o_addr + 32 * i, o);
+          if (here) {
+#pragma unroll
+            for (int x = 0; x < 32; x += 4)
+              *reinterpret_cast<float4*>(dst + 32 * i + x) = make_float4(__uint_as_float(o[x]), __uint_as_float(o[x + 1]), __uint_as_float(o[x + 2]), __uint_as_float(o[x + 3]));
+          }
+        }
       }
+      cur.next<D>(work, p);
     }
   }
 
@@ -295,20 +465,73 @@ __global__ void __launch_bounds__(Cfg<D, TILES>::THREADS, Cfg<D, TILES>::BLOCKS)
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == TILES * 4 + 1) {
+  if (warp == TILES * 4) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::TMEM) : "memory");
   }
 }
 
-template <int D, int TILES>
-cudaError_t launch(const CrossTcParams& p, int batch, cudaStream_t s) {
-  using C = Cfg<D, TILES>;
+// One block per block of the kernel above: if its run begins inside a tile and is the first to do so, it joins the tile's parts, from the
+// run that the tile begins in (second place) to the one that it ends in (first places).  out = sum 2^(m_s - m) o_s / sum 2^(m_s - m) l_s.
+template <int D>
+__global__ void __launch_bounds__(256) cross_tc_join_kernel(const __grid_constant__ CrossTcParams p) {
+  using C = Cfg<D>;
+  __shared__ Work work;
+  add_up<D>(work, p);
+  Cursor cur;
+  cur.start<D>(work, p);
+  if (cur.done() || cur.j0 == 0) return;
+  const int64_t each = share_of<D>(work, p), from = cur.at - cur.j0, first = from / each;
+  if (first + 1 != blockIdx.x) return;
+  const int64_t last = (from + cur.n - 1) / each;
+  const float* before = p.part + (first * 2 + 1) * C::PLACE;
+  constexpr int LANES = D / 4;
+  for (int r = threadIdx.x / LANES + (int)blockIdx.y * (256 / LANES); r < C::ROWS && cur.row0 + r < work.rows[cur.b]; r += 256 / LANES * (int)gridDim.y) {
+    const int d = threadIdx.x % LANES * 4;
+    float2 st = reinterpret_cast<const float2*>(before)[r];
+    float m = st.x, l = st.y;
+    float4 o = *reinterpret_cast<const float4*>(before + 2 * C::ROWS + r * D + d);
+    for (int64_t i = first + 1; i <= last; ++i) {
+      const float* place = p.part + i * 2 * C::PLACE;
+      st = reinterpret_cast<const float2*>(place)[r];
+      const float4 x = *reinterpret_cast<const float4*>(place + 2 * C::ROWS + r * D + d);
+      const float now = fmaxf(m, st.x), base = now == -INFINITY ? 0.f : now;
+      const float f = exp2_fast(m - base), g = exp2_fast(st.x - base);
+      m = now;
+      l = l * f + st.y * g;
+      o = make_float4(o.x * f + x.x * g, o.y * f + x.y * g, o.z * f + x.z * g, o.w * f + x.w * g);
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.o.p) + (p.b0 + cur.b) * p.o.b + (int64_t)(cur.row0 + r) * p.o.t + cur.h * p.o.h + d;
+    *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+  }
+}
+
+// Blocks of a launch over `batch` entries: one to each place on the device, fewer where a block would get less than LEAST keys.
+template <int D>
+int64_t grid_of(int batch, int q_tokens, int kv_tokens, int heads) {
+  using C = Cfg<D>;
+  const int64_t most = (int64_t)PLAN_SMS * C::BLOCKS, tiles = (int64_t)((q_tokens + C::ROWS - 1) / C::ROWS) * heads * batch, n = (kv_tokens + C::BN - 1) / C::BN;
+  if (tiles >= most * (LEAST / C::BN)) return most;
+  const int64_t blocks = (tiles * n + LEAST / C::BN - 1) / (LEAST / C::BN);
+  return blocks < most ? blocks : most;
+}
+
+template <int D>
+cudaError_t launch(CrossTcParams& p, int batch, cudaStream_t s) {
+  using C = Cfg<D>;
   static OncePerContext once;
-  const cudaError_t e = once([] { return cudaFuncSetAttribute(cross_tc_kernel<D, TILES>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM); });
+  cudaError_t e = once([] { return cudaFuncSetAttribute(cross_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM); });
   if (e != cudaSuccess) return e;
-  cross_tc_kernel<D, TILES><<<dim3((unsigned)((p.q_tokens + BM * TILES - 1) / (BM * TILES)), (unsigned)p.heads, (unsigned)batch), C::THREADS, C::SMEM, s>>>(p);
-  return cudaGetLastError();
+  for (p.b0 = 0; p.b0 < batch; p.b0 += MAX_ENTRIES) {
+    p.batch = batch - p.b0 < MAX_ENTRIES ? batch - p.b0 : MAX_ENTRIES;
+    const unsigned blocks = (unsigned)grid_of<D>(p.batch, p.q_tokens, p.kv_tokens, p.heads);
+    cross_tc_kernel<D><<<blocks, C::THREADS, C::SMEM, s>>>(p);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    cross_tc_join_kernel<D><<<dim3(blocks, 4), 256, 0, s>>>(p);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  }
+  return cudaSuccess;
 }
 
 }  // namespace
@@ -331,17 +554,25 @@ bool token_map(TensorMap128* map, const View& v, int D, int tokens, int heads, i
             D == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+uint64_t cross_tc_scratch(int batch, int q_tokens, int kv_tokens, int heads, int D) {
+  const int entries = batch < MAX_ENTRIES ? batch : MAX_ENTRIES;
+  const int64_t floats = D == 32   ? grid_of<32>(entries, q_tokens, kv_tokens, heads) * Cfg<32>::PLACE
+                         : D == 64 ? grid_of<64>(entries, q_tokens, kv_tokens, heads) * Cfg<64>::PLACE
+                                   : grid_of<128>(entries, q_tokens, kv_tokens, heads) * Cfg<128>::PLACE;
+  return (uint64_t)floats * 2u * 4u;
+}
+
 cudaError_t launch_cross_tc(const CrossParams& c, int D, cudaStream_t s) {
   CrossTcParams p{};
-  const int kv_heads = c.heads / c.group;
-  if (!token_map(&p.map_q, c.q, D, c.q_tokens, c.heads, c.batch) ||
-      (c.kv_tokens > 0 && (!token_map(&p.map_k, c.k, D, c.kv_tokens, kv_heads, c.batch) || !token_map(&p.map_v, c.v, D, c.kv_tokens, kv_heads, c.batch))))
+  const int kv_heads = c.heads / c.group, keys = D == 128 ? Cfg<128>::BN : Cfg<64>::BN;
+  if (!token_map(&p.map_q, c.q, D, c.q_tokens, c.heads, c.batch) || !token_map(&p.map_k, c.k, D, c.kv_tokens, kv_heads, c.batch, keys) ||
+      !token_map(&p.map_v, c.v, D, c.kv_tokens, kv_heads, c.batch, keys))
     return cudaErrorInvalidValue;
-  p.o = c.o; p.q_lengths = c.q_lengths; p.kv_lengths = c.kv_lengths; p.status = c.status;
+  p.o = c.o; p.q_lengths = c.q_lengths; p.kv_lengths = c.kv_lengths; p.part = c.part; p.status = c.status;
   p.q_tokens = c.q_tokens; p.kv_tokens = c.kv_tokens; p.heads = c.heads; p.group = c.group;
   p.q_h = c.q.h != 0; p.q_b = c.q.b != 0; p.k_h = c.k.h != 0; p.k_b = c.k.b != 0; p.v_h = c.v.h != 0; p.v_b = c.v.b != 0;
   p.scale_log2 = c.scale_log2;
-  return D == 32 ? launch<32, 1>(p, c.batch, s) : D == 64 ? launch<64, 1>(p, c.batch, s) : launch<128, 2>(p, c.batch, s);
+  return D == 32 ? launch<32>(p, c.batch, s) : D == 64 ? launch<64>(p, c.batch, s) : launch<128>(p, c.batch, s);
 }
 
 }  // namespace tok
