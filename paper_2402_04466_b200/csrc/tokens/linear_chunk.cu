@@ -183,13 +183,20 @@ __global__ void __launch_bounds__(THREADS) linear_scan_kernel(const __grid_const
   const int n = clamp_length(p.lengths, b, p.tokens);
   const float decay = decay_power(p.log_decay[h], p.seg_tokens);
   float* seg = p.seg_state + ((int64_t)b * p.heads + h) * p.segments * D * D + i;
+  const int segments = max(1, (n + p.seg_tokens - 1) / p.seg_tokens);
   float cur = p.state[((int64_t)slot * p.heads + h) * D * D + i];
-  for (int s = 0;; ++s) {
-    const bool last = (int64_t)(s + 1) * p.seg_tokens >= n;
-    const float add = last ? 0.f : seg[(int64_t)s * D * D];
-    seg[(int64_t)s * D * D] = cur;
-    if (last) break;
-    cur = fmaf(decay, cur, add);
+  // eight segments' loads are in flight together
+  for (int s0 = 0; s0 < segments; s0 += 8) {
+    float add[8];
+#pragma unroll
+    for (int s = 0; s < 8; ++s)
+      if (s0 + s + 1 < segments) add[s] = seg[(int64_t)(s0 + s) * D * D];
+#pragma unroll
+    for (int s = 0; s < 8; ++s)
+      if (s0 + s < segments) {
+        seg[(int64_t)(s0 + s) * D * D] = cur;
+        if (s0 + s + 1 < segments) cur = fmaf(decay, cur, add[s]);
+      }
   }
 }
 

@@ -12,8 +12,11 @@ namespace tt {
 namespace tok {
 namespace {
 
+typedef unsigned long long Two;        // two floats
+
 constexpr int CT = 128;                // tokens of a chunk
-constexpr int THREADS = 160;           // four warps that compute, one that loads and issues products
+constexpr int WORKERS = 8;             // warps that compute: two to a quarter of the tokens, for half of the columns each
+constexpr int THREADS = WORKERS * 32 + 32;   // and one that loads and issues products
 
 struct LinearTcParams {
   TensorMap128 map_q, map_k, map_v;    // [D][token][head][batch], box of 128 tokens
@@ -84,13 +87,13 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, WITH_OUT>::BLOCKS) linear_tc_k
     mbar_init(smem_u32(vfull), 1);
     mbar_init(smem_u32(first), 1);
     mbar_init(smem_u32(second), 1);
-    mbar_init(smem_u32(pready), 4);
-    mbar_init(smem_u32(sready), 4);
+    mbar_init(smem_u32(pready), WORKERS);
+    mbar_init(smem_u32(sready), WORKERS);
     *abort_flag = 0;
     *s_status = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 4) {
+  if (warp == WORKERS) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(C::TMEM) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -102,7 +105,7 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, WITH_OUT>::BLOCKS) linear_tc_k
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
 
-  if (warp == 4) {
+  if (warp == WORKERS) {
     // ----------------------------------------------------------------- loads and products
     const bool issuer = elect_one();
     const int hk = h / p.group;
@@ -154,7 +157,7 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, WITH_OUT>::BLOCKS) linear_tc_k
       if (issuer) {
         if (WITH_OUT) {
 #pragma unroll
-          for (int k = 0; k < CT / 16; ++k) umma_bf16_ts(tmem + C::O_COL, tmem + (uint32_t)(k * 8), v0 + (uint64_t)(k * C::ROW), PV, 1);
+          for (int k = 0; k < CT / 16; ++k) umma_bf16_ts(tmem + C::O_COL, tmem + (uint32_t)(k / 4 * 64 + k % 4 * 8), v0 + (uint64_t)(k * C::ROW), PV, 1);
         }
 #pragma unroll
         for (int term = 0; term < 3; ++term)
@@ -174,10 +177,10 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, WITH_OUT>::BLOCKS) linear_tc_k
     }
   } else {
     // ------------------------------------------------------------------------- the rest
-    const int r = threadIdx.x;                                     // token of the chunk, lane of tensor memory
-    const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
-    // row of the state in this lane: a product of 64 rows leaves 16 to each warp's first lanes
-    const int row = C::M == 128 ? r : warp * 16 + (lane & 15);
+    const int quarter = warp & 3, half = warp >> 2, r = quarter * 32 + lane;      // r: token of the chunk, lane of tensor memory
+    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
+    // row of the state in this lane: a product of 64 rows leaves 16 to each quarter's first lanes
+    const int row = C::M == 128 ? r : quarter * 16 + (lane & 15);
     const bool has_row = (C::M == 128 || lane < 16) && row < D;
     bool ok = true;
     auto wait = [&](uint64_t* bar, int c, int code) {
@@ -190,27 +193,44 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, WITH_OUT>::BLOCKS) linear_tc_k
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(bar));
     };
-    // 32 columns of this lane's row of the state into the operand's rows
-    auto put_state = [&](int i, const uint32_t (&v)[32]) {
+    // the columns of state and sums that are this warp's: pieces of 16 from c0 on
+    constexpr int PIECES = D / 32;
+    const int c0 = half * (D / 2);
+    // 16 columns of this lane's row of the state into the operand's rows
+    auto put_state = [&](int col, const uint32_t (&v)[16]) {
       if (!has_row) return;
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const int chunk = (D == 32 ? 0 : (i % 2) * 4) + x, to = D == 32 ? chunk ^ ((row >> 1) & 3) : chunk ^ (row & 7);
+      for (int x = 0; x < 2; ++x) {
+        const int run = (col & 63) / 8 + x, to = D == 32 ? run ^ ((row >> 1) & 3) : run ^ (row & 7);
         auto two = [&](int y) { return pack_bf16(__uint_as_float(v[8 * x + y]), __uint_as_float(v[8 * x + y + 1])); };
-        *reinterpret_cast<uint4*>(s_s + (i / 2) * C::STATE_SLAB + row * C::ROW + to * 16) = make_uint4(two(0), two(2), two(4), two(6));
+        *reinterpret_cast<uint4*>(s_s + (col / 64) * C::STATE_SLAB + row * C::ROW + to * 16) = make_uint4(two(0), two(2), two(4), two(6));
+      }
+    };
+    // all of this warp's columns times f
+    auto scale_columns = [&](uint32_t first, float f) {
+      uint32_t v[PIECES][16];
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) tmem_ld16_async(lanes + first + (uint32_t)(c0 + 16 * i), v[i]);
+      tmem_wait_ld();
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) v[i][x] = __float_as_uint(__uint_as_float(v[i][x]) * f);
+        tmem_st16(lanes + first + (uint32_t)(c0 + 16 * i), v[i]);
       }
     };
     if (WITH_OUT) {
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i) {
-        uint32_t v[32];
+      for (int i = 0; i < PIECES; ++i) {
+        const int col = c0 + 16 * i;
+        uint32_t v[16];
 #pragma unroll
-        for (int x = 0; x < 32; x += 4) {
-          const float4 f = has_row ? *reinterpret_cast<const float4*>(from + row * D + 32 * i + x) : make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int x = 0; x < 16; x += 4) {
+          const float4 f = has_row ? *reinterpret_cast<const float4*>(from + row * D + col + x) : make_float4(0.f, 0.f, 0.f, 0.f);
           v[x] = __float_as_uint(f.x); v[x + 1] = __float_as_uint(f.y); v[x + 2] = __float_as_uint(f.z); v[x + 3] = __float_as_uint(f.w);
         }
-        tmem_st32(lanes + C::S_COL + 32 * i, v);
-        put_state(i, v);
+        tmem_st16(lanes + C::S_COL + (uint32_t)col, v);
+        put_state(col, v);
       }
       tmem_wait_st();
       arrive(sready);
@@ -222,23 +242,28 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, WITH_OUT>::BLOCKS) linear_tc_k
       if (WITH_OUT) {
         if (!wait(first, c, 0x11)) break;
         tc_fence_after();
-        // weights within the chunk: blocks of 32 columns below the diagonal, on it, and above it
+        // weights within the chunk: blocks of 32 columns below the diagonal, on it, and above it; either half lies over scores of its own
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int y = 0; y < 2; ++y) {
+          const int i = 2 * half + y;
           uint32_t w[16];
-          if (i > warp) {
+          if (i > quarter) {
 #pragma unroll
             for (int x = 0; x < 16; ++x) w[x] = 0u;
           } else {
             uint32_t v[32];
             tmem_ld32(lanes + 32 * i, v);
-            if (i < warp) {
+            if (i < quarter) {
               const float f = pw[r - 32 * i - 31];      // decay^(r - j) = decay^(r - 32 i - 31) decay^(31 - (j - 32 i))
+              const Two f2 = pack2(f, f);
 #pragma unroll
               for (int x = 0; x < 16; x += 2) {
                 const float4 g = *reinterpret_cast<const float4*>(pr + 2 * x);
-                w[x] = pack_bf16(__uint_as_float(v[2 * x]) * (f * g.x), __uint_as_float(v[2 * x + 1]) * (f * g.y));
-                w[x + 1] = pack_bf16(__uint_as_float(v[2 * x + 2]) * (f * g.z), __uint_as_float(v[2 * x + 3]) * (f * g.w));
+                float a0, a1, a2, a3;
+                unpack2(mul2_of(pack2(__uint_as_float(v[2 * x]), __uint_as_float(v[2 * x + 1])), mul2_of(f2, pack2(g.x, g.y))), a0, a1);
+                unpack2(mul2_of(pack2(__uint_as_float(v[2 * x + 2]), __uint_as_float(v[2 * x + 3])), mul2_of(f2, pack2(g.z, g.w))), a2, a3);
+                w[x] = pack_bf16(a0, a1);
+                w[x + 1] = pack_bf16(a2, a3);
               }
             } else {
 #pragma unroll
@@ -249,95 +274,79 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, WITH_OUT>::BLOCKS) linear_tc_k
               }
             }
           }
-          // block i of the weights lies over scores that have been read: columns 16 i .. 16 i + 15
-          tmem_st16(lanes + 16 * i, w);
+          tmem_st16(lanes + 64 * half + 16 * y, w);
         }
-        const float f = pw[r + 1];
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
-          uint32_t v[32];
-          tmem_ld32(lanes + C::O_COL + 32 * i, v);
-#pragma unroll
-          for (int x = 0; x < 32; ++x) v[x] = __float_as_uint(__uint_as_float(v[x]) * f);
-          tmem_st32(lanes + C::O_COL + 32 * i, v);
-        }
+        scale_columns(C::O_COL, pw[r + 1]);
       }
-      if (WITH_OUT || c > 0) {
-        const float f = pw[m];
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
-          uint32_t v[32];
-          tmem_ld32(lanes + C::S_COL + 32 * i, v);
-#pragma unroll
-          for (int x = 0; x < 32; ++x) v[x] = __float_as_uint(__uint_as_float(v[x]) * f);
-          tmem_st32(lanes + C::S_COL + 32 * i, v);
-        }
-      }
+      if (WITH_OUT || c > 0) scale_columns(C::S_COL, pw[m]);
       // K' = decay^(m-1-r) k in three bf16 terms, 24 bits: the state is as good as fp32.  Runs of 16 bytes in a turned order, so that
       // eight rows of 128 bytes do not meet in the same banks; the swizzle moves runs within a row and need not be undone.
       const bool here = r < m;
       const float f = here ? pw[m - 1 - r] : 0.f;
       if (!wait(vfull, c, 0x12)) break;
+      const Two f2 = pack2(f, f);
 #pragma unroll
-      for (int s = 0; s < C::SLABS; ++s)
+      for (int i = 0; i < C::SLABS * C::ROW / 32; ++i) {
+        const int run = half * (C::SLABS * C::ROW / 32) + i, s = run / (C::ROW / 16);
+        const int o = s * C::SLAB_BYTES + r * C::ROW + ((run + (D == 32 ? r >> 1 : r)) & (C::ROW / 16 - 1)) * 16;
+        const uint4 u = *reinterpret_cast<const uint4*>(s_k + o);
+        const uint32_t in[4] = {u.x, u.y, u.z, u.w};
+        uint32_t a[3][4];
 #pragma unroll
-        for (int i = 0; i < C::ROW / 16; ++i) {
-          const int o = s * C::SLAB_BYTES + r * C::ROW + ((i + (D == 32 ? r >> 1 : r)) & (C::ROW / 16 - 1)) * 16;
-          const uint4 u = *reinterpret_cast<const uint4*>(s_k + o);
-          const uint32_t in[4] = {u.x, u.y, u.z, u.w};
-          uint32_t a0[4], a1[4], a2[4];
+        for (int x = 0; x < 4; ++x) {
+          Two y = mul2_of(pack2(__uint_as_float(in[x] << 16), __uint_as_float(in[x] & 0xFFFF0000u)), f2);
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            float lo = here ? __uint_as_float(in[x] << 16) * f : 0.f, hi = here ? __uint_as_float(in[x] & 0xFFFF0000u) * f : 0.f;
-            a0[x] = pack_bf16(lo, hi);
-            lo -= __uint_as_float(a0[x] << 16);
-            hi -= __uint_as_float(a0[x] & 0xFFFF0000u);
-            a1[x] = pack_bf16(lo, hi);
-            lo -= __uint_as_float(a1[x] << 16);
-            hi -= __uint_as_float(a1[x] & 0xFFFF0000u);
-            a2[x] = pack_bf16(lo, hi);
+          for (int term = 0; term < 3; ++term) {
+            float lo, hi;
+            unpack2(y, lo, hi);
+            a[term][x] = here ? pack_bf16(lo, hi) : 0u;
+            if (term < 2) y = sub2_of(y, pack2(__uint_as_float(a[term][x] << 16), __uint_as_float(a[term][x] & 0xFFFF0000u)));
           }
-          *reinterpret_cast<uint4*>(s_k + o) = make_uint4(a0[0], a0[1], a0[2], a0[3]);
-          *reinterpret_cast<uint4*>(s_k1 + o) = make_uint4(a1[0], a1[1], a1[2], a1[3]);
-          *reinterpret_cast<uint4*>(s_k2 + o) = make_uint4(a2[0], a2[1], a2[2], a2[3]);
-          // rows behind the last token may hold anything, and weights of 0 would make NaN of it
-          if (!here) *reinterpret_cast<uint4*>(s_v + o) = make_uint4(0u, 0u, 0u, 0u);
         }
+        *reinterpret_cast<uint4*>(s_k + o) = make_uint4(a[0][0], a[0][1], a[0][2], a[0][3]);
+        *reinterpret_cast<uint4*>(s_k1 + o) = make_uint4(a[1][0], a[1][1], a[1][2], a[1][3]);
+        *reinterpret_cast<uint4*>(s_k2 + o) = make_uint4(a[2][0], a[2][1], a[2][2], a[2][3]);
+        // rows behind the last token may hold anything, and weights of 0 would make NaN of it
+        if (!here) *reinterpret_cast<uint4*>(s_v + o) = make_uint4(0u, 0u, 0u, 0u);
+      }
       tmem_wait_st();
       arrive(pready);
       if (!wait(second, c, 0x13)) break;
       tc_fence_after();
-      if (WITH_OUT) {
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
-          uint32_t v[32];
-          tmem_ld32(lanes + C::O_COL + 32 * i, v);
-          if (here) {
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              auto two = [&](int y) { return pack_bf16(__uint_as_float(v[8 * x + y]) * p.scale, __uint_as_float(v[8 * x + y + 1]) * p.scale); };
-              *reinterpret_cast<uint4*>(out + (int64_t)(t + r) * p.o.t + 32 * i + 8 * x) = make_uint4(two(0), two(2), two(4), two(6));
-            }
-          }
-        }
-      }
       const bool last = c + 1 == chunks;
+      // the state first: the next chunk's products wait for it, and for out having been read
       if (WITH_OUT || last) {
-        float* to = WITH_OUT ? p.state_out + at : seg_state;
-        const bool keep = last && (!WITH_OUT || t1 == len);
+        uint32_t v[PIECES][16], y[PIECES][16];
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
-          uint32_t v[32];
-          tmem_ld32(lanes + C::S_COL + 32 * i, v);
-          if (WITH_OUT && !last) put_state(i, v);
-          if (keep && has_row)
+        for (int i = 0; i < PIECES; ++i) {
+          tmem_ld16_async(lanes + C::S_COL + (uint32_t)(c0 + 16 * i), v[i]);
+          if (WITH_OUT) tmem_ld16_async(lanes + C::O_COL + (uint32_t)(c0 + 16 * i), y[i]);
+        }
+        tmem_wait_ld();
+        if (WITH_OUT && !last) {
 #pragma unroll
-            for (int x = 0; x < 32; x += 4)
-              *reinterpret_cast<float4*>(to + row * D + 32 * i + x) =
-                  make_float4(__uint_as_float(v[x]), __uint_as_float(v[x + 1]), __uint_as_float(v[x + 2]), __uint_as_float(v[x + 3]));
+          for (int i = 0; i < PIECES; ++i) put_state(c0 + 16 * i, v[i]);
+          arrive(sready);
+        }
+        if (last && (!WITH_OUT || t1 == len) && has_row) {
+          float* to = WITH_OUT ? p.state_out + at : seg_state;
+#pragma unroll
+          for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+            for (int x = 0; x < 16; x += 4)
+              *reinterpret_cast<float4*>(to + row * D + c0 + 16 * i + x) =
+                  make_float4(__uint_as_float(v[i][x]), __uint_as_float(v[i][x + 1]), __uint_as_float(v[i][x + 2]), __uint_as_float(v[i][x + 3]));
+        }
+        if (WITH_OUT && here) {
+#pragma unroll
+          for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              auto two = [&](int e) { return pack_bf16(__uint_as_float(y[i][8 * x + e]) * p.scale, __uint_as_float(y[i][8 * x + e + 1]) * p.scale); };
+              *reinterpret_cast<uint4*>(out + (int64_t)(t + r) * p.o.t + c0 + 16 * i + 8 * x) = make_uint4(two(0), two(2), two(4), two(6));
+            }
         }
       }
-      if (WITH_OUT && !last) arrive(sready);
     }
   }
 
@@ -350,7 +359,7 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, WITH_OUT>::BLOCKS) linear_tc_k
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 4) {
+  if (warp == WORKERS) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::TMEM) : "memory");
   }
