@@ -237,11 +237,11 @@ cudaError_t launch(const LinearParams& p, cudaStream_t s) {
 }
 }  // namespace
 
-void linear_plan(int batch, int tokens, int heads, int D, bool bf16, int* segments, int* seg_tokens) {
-  (void)D; (void)bf16;
+// Two blocks of fp32, one of bf16 (whose chunks overlap in a block) to a multiprocessor.
+void linear_plan(int batch, int tokens, int heads, bool bf16, int* segments, int* seg_tokens) {
   const int64_t sequences = (int64_t)batch * heads;
   const int step = 128;
-  const int64_t most = (tokens + step - 1) / step, want = 2 * PLAN_SMS / sequences;
+  const int64_t most = ((int64_t)tokens + step - 1) / step, want = (bf16 ? 1 : 2) * PLAN_SMS / sequences;
   int64_t n = want < most ? want : most;
   if (n < 1) n = 1;
   const int64_t each = tokens > 0 ? ((tokens + n - 1) / n + step - 1) / step * step : step;

@@ -4,7 +4,15 @@
 //   scores  A = Q K^T;   P_ij = l^(i-j) A_ij for i >= j, else 0
 //   out_i   = scale * ( l^(i+1) (Q S)_i + (P V)_i )
 //   state   S' = l^m S + K'^T V,  K'_j = l^(m-1-j) k_j
-// The state stays in tensor memory as the fp32 accumulator of its own product, scaled in place before each chunk's is added.
+// The state stays in tensor memory as the fp32 accumulator of its own product, scaled in place before each chunk's is added; K' goes into
+// that product as three bf16 terms, 24 bits, so the state is as good as fp32.  P and, for Q S, a copy of the state are
+// rounded to bf16 once each, as far as out itself is.
+//
+// A sequence is sequential in its chunks, and a chunk is a chain of copies, products and register work, 12 000 cycles when one follows the
+// other (two blocks to a multiprocessor then took 125 us for eight maps of 14400 tokens, 4 heads of 64).  So one block holds the
+// chunks of a sequence in flight: a warp loads, one issues the products of out (A), one those of the state (B), eight warps make P and out
+// from scores and sums, and eight make K' and carry the state.  Scores, sums, operands and K' have two places each where
+// the memory allows (heads of up to 64).  What is left in sequence is the state's product and its scaling.
 #include "linear_common.cuh"
 #include "token_ptx.cuh"
 
@@ -15,8 +23,9 @@ namespace {
 typedef unsigned long long Two;        // two floats
 
 constexpr int CT = 128;                // tokens of a chunk
-constexpr int WORKERS = 8;             // warps that compute: two to a quarter of the tokens, for half of the columns each
-constexpr int THREADS = WORKERS * 32 + 32;   // and one that loads and issues products
+constexpr int GROUP = 8;               // warps of a group: two to a quarter of the tokens, for half of the columns each
+// warps: the state's group, B, loads, A, one that idles, out's group (whose first warp has to be a multiple of four)
+constexpr int W_B = GROUP, W_LOAD = GROUP + 1, W_A = GROUP + 2, W_OUT = GROUP + 4;
 
 struct LinearTcParams {
   TensorMap128 map_q, map_k, map_v;    // [D][token][head][batch], box of 128 tokens
@@ -26,6 +35,7 @@ struct LinearTcParams {
 
 template <int D, bool WITH_OUT>
 struct Cfg {
+  static constexpr int THREADS = (WITH_OUT ? W_OUT + GROUP : W_LOAD + 1) * 32;
   static constexpr int ROW = D == 32 ? 64 : 128;                    // bytes of a row in a slab
   static constexpr int SLABS = D == 128 ? 2 : 1;
   static constexpr int SLAB_BYTES = CT * ROW;
@@ -33,35 +43,46 @@ struct Cfg {
   static constexpr int STATE_SLAB = D * ROW, STATE_BYTES = SLABS * STATE_SLAB;
   static constexpr uint32_t LAYOUT = D == 32 ? 4u : 2u;             // 64- or 128-byte swizzle
   static constexpr int M = D == 128 ? 128 : 64;                     // rows of the state's product
-  static constexpr uint32_t O_COL = CT, S_COL = WITH_OUT ? CT + D : 0;
-  static constexpr uint32_t COLS = S_COL + D;
+  static constexpr int PLACES = D == 128 && WITH_OUT ? 1 : 2;       // of operands, K', scores and sums
+  static constexpr int KP_PLACES = D == 128 ? 1 : 2;
+  static constexpr uint32_t S_COL = 0;                              // the state
+  static constexpr uint32_t A_COL = D, P_COL = A_COL + PLACES * CT, O_COL = P_COL + CT / 2;    // scores, weights, sums
+  static constexpr uint32_t COLS = WITH_OUT ? O_COL + PLACES * D : D;
   static constexpr uint32_t TMEM = COLS <= 32 ? 32 : COLS <= 64 ? 64 : COLS <= 128 ? 128 : COLS <= 256 ? 256 : 512;
   static constexpr int TABLE_BYTES = (CT + 4) * 4 + 128;
-  static constexpr int SMEM = (WITH_OUT ? 5 : 4) * TILE_BYTES + (WITH_OUT ? STATE_BYTES : 0) + TABLE_BYTES + 128 + 1024;
-  static constexpr int BLOCKS = D == 128 ? 1 : WITH_OUT ? 2 : 3;
-  static_assert(SMEM * BLOCKS <= 227 * 1024, "shared memory");
+  static constexpr int SMEM = (WITH_OUT ? 3 : 2) * PLACES * TILE_BYTES + 3 * KP_PLACES * TILE_BYTES + (WITH_OUT ? STATE_BYTES : 0) + TABLE_BYTES + 256 + 1024;
+  static_assert(COLS <= 512 && SMEM <= 227 * 1024, "tensor and shared memory");
 };
 
 template <int D, bool WITH_OUT>
-__global__ void __launch_bounds__(THREADS, Cfg<D, WITH_OUT>::BLOCKS) linear_tc_kernel(const __grid_constant__ LinearTcParams pp) {
+__global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel(const __grid_constant__ LinearTcParams pp) {
   using C = Cfg<D, WITH_OUT>;
+  constexpr int PLACES = C::PLACES, KPP = C::KP_PLACES;
   const LinearParams& p = pp.c;
   extern __shared__ uint8_t smem_raw[];
-  uint8_t* s_k = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);   // the keys, then K' first term
-  uint8_t* s_k1 = s_k + C::TILE_BYTES;                                                           // second and third term
-  uint8_t* s_k2 = s_k1 + C::TILE_BYTES;
-  uint8_t* s_v = s_k2 + C::TILE_BYTES;
-  uint8_t* s_q = s_v + C::TILE_BYTES;                                                            // WITH_OUT only, as the next
-  uint8_t* s_s = s_q + (WITH_OUT ? C::TILE_BYTES : 0);                                           // the state as an operand, rows along K
-  float* pw = reinterpret_cast<float*>(s_s + (WITH_OUT ? C::STATE_BYTES : 0));                   // decay^0 .. decay^128
-  float* pr = pw + CT + 4;                                                                       // decay^31 .. decay^0
-  uint64_t* qfull = reinterpret_cast<uint64_t*>(pr + 32);
-  uint64_t* kfull = qfull + 1;
-  uint64_t* vfull = kfull + 1;
-  uint64_t* first = vfull + 1;         // scores and Q S are there
-  uint64_t* second = first + 1;        // out and state are there
-  uint64_t* pready = second + 1;       // P, K', scaled accumulators
-  uint64_t* sready = pready + 1;       // the state is an operand, out has been read
+  uint8_t* s_k = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  // K': [KPP][three terms].  The values lie behind it: heads of 32 fill half of the 64 rows of the state's product, and the other half is
+  // read, for nothing, from one slab further on, which has to be the block's own memory.
+  uint8_t* s_kp = s_k + PLACES * C::TILE_BYTES;
+  uint8_t* s_v = s_kp + 3 * KPP * C::TILE_BYTES;
+  uint8_t* s_q = s_v + PLACES * C::TILE_BYTES;                       // WITH_OUT only, as the next
+  uint8_t* s_s = s_q + (WITH_OUT ? PLACES * C::TILE_BYTES : 0);      // the state as an operand, rows along K
+  float* pw = reinterpret_cast<float*>(s_s + (WITH_OUT ? C::STATE_BYTES : 0));   // decay^0 .. decay^128
+  float* pr = pw + CT + 4;                                           // decay^31 .. decay^0
+  uint64_t* qfull = reinterpret_cast<uint64_t*>(pr + 32);            // [PLACES], as the next five
+  uint64_t* kfull = qfull + 2;
+  uint64_t* vfull = kfull + 2;
+  uint64_t* qempty = vfull + 2;        // Q S is done
+  uint64_t* kempty = qempty + 2;       // scores are done, K' is made
+  uint64_t* vempty = kempty + 2;       // both products of V are done
+  uint64_t* afull = vempty + 2;        // [PLACES] scores are there
+  uint64_t* kready = afull + 2;        // [KP_PLACES] K' is there, and the state is scaled
+  uint64_t* sdone = kready + 2;        // [KP_PLACES] the state is there
+  uint64_t* ofirst = sdone + 2;        // Q S is there
+  uint64_t* pready = ofirst + 1;       // P is there, and the sums are scaled
+  uint64_t* odone = pready + 1;        // out is there
+  uint64_t* oread = odone + 1;         // out is in registers
+  uint64_t* sready = oread + 1;        // the state is an operand
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sready + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* s_status = reinterpret_cast<int*>(tmem_slot + 2);
@@ -72,28 +93,39 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, WITH_OUT>::BLOCKS) linear_tc_k
   if (slot < 0) return;
   const int len = clamp_length(p.lengths, b, p.tokens), t0 = seg * p.seg_tokens, t1 = min(len, t0 + p.seg_tokens);
   if (WITH_OUT ? seg > 0 && t0 >= len : t0 + p.seg_tokens >= len) return;      // what the last segment adds is not needed
-  const int chunks = (t1 - t0 + CT - 1) / CT;
+  const int chunks = __shfl_sync(0xffffffffu, (t1 - t0 + CT - 1) / CT, 0);
   const int64_t at = ((int64_t)slot * p.heads + h) * D * D;
   float* seg_state = p.segments > 1 ? p.seg_state + (((int64_t)b * p.heads + h) * p.segments + seg) * D * D : nullptr;
   const float* from = p.segments > 1 ? seg_state : p.state + at;
   if (chunks == 0) {                   // an entry without tokens: its state as it was
     if (WITH_OUT && p.state_out + at != from)
-      for (int i = threadIdx.x; i < D * D; i += THREADS) p.state_out[at + i] = from[i];
+      for (int i = threadIdx.x; i < D * D; i += C::THREADS) p.state_out[at + i] = from[i];
     return;
   }
   if (threadIdx.x == 0) {
-    mbar_init(smem_u32(qfull), 1);
-    mbar_init(smem_u32(kfull), 1);
-    mbar_init(smem_u32(vfull), 1);
-    mbar_init(smem_u32(first), 1);
-    mbar_init(smem_u32(second), 1);
-    mbar_init(smem_u32(pready), WORKERS);
-    mbar_init(smem_u32(sready), WORKERS);
+    for (int s = 0; s < PLACES; ++s) {
+      mbar_init(smem_u32(qfull + s), 1);
+      mbar_init(smem_u32(kfull + s), 1);
+      mbar_init(smem_u32(vfull + s), 1);
+      mbar_init(smem_u32(qempty + s), 1);
+      mbar_init(smem_u32(kempty + s), WITH_OUT ? GROUP + 1 : GROUP);
+      mbar_init(smem_u32(vempty + s), WITH_OUT ? 2 : 1);
+    }
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(smem_u32(afull + s), 1);
+      mbar_init(smem_u32(sdone + s), 1);
+      mbar_init(smem_u32(kready + s), GROUP);
+    }
+    mbar_init(smem_u32(ofirst), 1);
+    mbar_init(smem_u32(odone), 1);
+    mbar_init(smem_u32(pready), GROUP);
+    mbar_init(smem_u32(oread), GROUP);
+    mbar_init(smem_u32(sready), GROUP);
     *abort_flag = 0;
     *s_status = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == WORKERS) {
+  if (warp == W_B) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(C::TMEM) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -103,193 +135,270 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, WITH_OUT>::BLOCKS) linear_tc_k
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
 
-  if (warp == WORKERS) {
-    // ----------------------------------------------------------------- loads and products
+  bool ok = true;
+  // A whole warp waits and stops together.  Each thing of chunk c is the c-th of its barrier, or the c / PLACES-th of its place's.  Only parities are
+  // told apart: a barrier that may be two things ahead of one who waits for the first has a place for each.
+  auto wait = [&](uint64_t* bar, int phase, int code) {
+    if (__builtin_expect(__all_sync(0xffffffffu, mbar_test(smem_u32(bar), (uint32_t)phase & 1u)), 1)) return ok;
+    ok = __all_sync(0xffffffffu, ok && mbar_wait_uniform(smem_u32(bar), (uint32_t)phase & 1u, abort_flag, s_status, WAIT_LINEAR_TC + code, WAIT_LIMIT));
+    return ok;
+  };
+  auto place = [](int c) { return PLACES == 2 ? c & 1 : 0; };
+  auto turn = [](int c) { return PLACES == 2 ? c >> 1 : c; };
+  auto kp_place = [](int c) { return KPP == 2 ? c & 1 : 0; };
+  auto kp_turn = [](int c) { return KPP == 2 ? c >> 1 : c; };
+  // where only a segment's sum is wanted, its chunks are taken from the last to the first: their weights are then a product
+  auto token_of = [&](int c) { return t0 + (WITH_OUT ? c : chunks - 1 - c) * CT; };
+
+  if (warp == W_LOAD) {
+    // ------------------------------------------------------------------------------ loads
     const bool issuer = elect_one();
     const int hk = h / p.group;
     auto load = [&](uint8_t* dst, const void* map, uint64_t* bar, int t, int hh, int bb) {
       mbar_arrive_expect_tx(smem_u32(bar), C::TILE_BYTES);
+#pragma unroll
       for (int s = 0; s < C::SLABS; ++s) tma_load_4d(smem_u32(dst + s * C::SLAB_BYTES), map, smem_u32(bar), s * 64, t, hh, bb);
     };
-    auto load_q = [&](int c) { if (WITH_OUT && issuer) load(s_q, &pp.map_q, qfull, t0 + c * CT, h * pp.q_h, b * pp.q_b); };
-    auto load_k = [&](int c) { if (issuer) load(s_k, &pp.map_k, kfull, t0 + c * CT, hk * pp.k_h, b * pp.k_b); };
-    auto load_v = [&](int c) { if (issuer) load(s_v, &pp.map_v, vfull, t0 + c * CT, hk * pp.v_h, b * pp.v_b); };
-    load_q(0);
-    load_k(0);
-    load_v(0);
-    __syncwarp();
-    constexpr uint32_t QK = make_idesc(CT, CT), QS = make_idesc(CT, D) | B_BY_ROWS, PV = QS, KV = make_idesc(C::M, D) | A_BY_ROWS | B_BY_ROWS;
-    const uint64_t q0 = make_smem_desc(smem_u32(s_q), 8 * C::ROW, C::LAYOUT), k0 = make_smem_desc(smem_u32(s_k), 8 * C::ROW, C::LAYOUT);
-    const uint64_t st0 = make_rows_desc(smem_u32(s_s), C::STATE_SLAB, 8 * C::ROW, C::LAYOUT);
-    const uint64_t v0 = make_rows_desc(smem_u32(s_v), C::SLAB_BYTES, 8 * C::ROW, C::LAYOUT);
-    const uint64_t kr0 = make_rows_desc(smem_u32(s_k), C::SLAB_BYTES, 8 * C::ROW, C::LAYOUT);
-    bool ok = true;
-    auto wait = [&](uint64_t* bar, int c, int code) {
-      ok = __all_sync(0xffffffffu, ok && mbar_wait(smem_u32(bar), (uint32_t)(c & 1), abort_flag, s_status, WAIT_LINEAR_TC + code, WAIT_LIMIT));
-      return ok;
-    };
     for (int c = 0; c < chunks; ++c) {
+      const int s = place(c), t = token_of(c);
+      if (c >= PLACES && !wait(kempty + s, turn(c) - 1, 0x00)) break;
+      if (issuer) load(s_k + s * C::TILE_BYTES, &pp.map_k, kfull + s, t, hk * pp.k_h, b * pp.k_b);
       if (WITH_OUT) {
-        if (!wait(qfull, c, 0x00) || !wait(kfull, c, 0x01) || !wait(sready, c, 0x02)) break;
-        tc_fence_after();
-        if (issuer) {
-#pragma unroll
-          for (int k = 0; k < D / 16; ++k) {
-            const uint64_t o = (uint64_t)((k / 4) * (C::SLAB_BYTES >> 4) + (k % 4) * 2);
-            umma_bf16(tmem, q0 + o, k0 + o, QK, k > 0);
-          }
-#pragma unroll
-          for (int k = 0; k < D / 16; ++k) {
-            const uint64_t o = (uint64_t)((k / 4) * (C::SLAB_BYTES >> 4) + (k % 4) * 2);
-            umma_bf16(tmem + C::O_COL, q0 + o, st0 + (uint64_t)(k * C::ROW), QS, k > 0);
-          }
-          umma_commit(smem_u32(first));
-        }
-        __syncwarp();
-        if (!wait(first, c, 0x03)) break;
-        if (c + 1 < chunks) load_q(c + 1);
-        __syncwarp();
+        if (c >= PLACES && !wait(qempty + s, turn(c) - 1, 0x01)) break;
+        if (issuer) load(s_q + s * C::TILE_BYTES, &pp.map_q, qfull + s, t, h * pp.q_h, b * pp.q_b);
       }
-      if (!wait(pready, c, 0x04)) break;
+      if (c >= PLACES && !wait(vempty + s, turn(c) - 1, 0x02)) break;
+      if (issuer) load(s_v + s * C::TILE_BYTES, &pp.map_v, vfull + s, t, hk * pp.v_h, b * pp.v_b);
+    }
+  } else if (warp == W_B) {
+    // --------------------------------------------------------------- products of the state
+    const bool issuer = elect_one();
+    constexpr uint32_t KV = make_idesc(C::M, D) | A_BY_ROWS | B_BY_ROWS;
+    const uint64_t v0 = make_rows_desc(smem_u32(s_v), C::SLAB_BYTES, 8 * C::ROW, C::LAYOUT);
+    const uint64_t k0 = make_rows_desc(smem_u32(s_kp), C::SLAB_BYTES, 8 * C::ROW, C::LAYOUT);
+    for (int c = 0; c < chunks; ++c) {
+      if (!wait(kready + kp_place(c), kp_turn(c), 0x10)) break;
       tc_fence_after();
       if (issuer) {
-        if (WITH_OUT) {
-#pragma unroll
-          for (int k = 0; k < CT / 16; ++k) umma_bf16_ts(tmem + C::O_COL, tmem + (uint32_t)(k / 4 * 64 + k % 4 * 8), v0 + (uint64_t)(k * C::ROW), PV, 1);
-        }
+        const uint64_t v = v0 + (uint64_t)(place(c) * (C::TILE_BYTES >> 4)), k = k0 + (uint64_t)(kp_place(c) * 3 * (C::TILE_BYTES >> 4));
 #pragma unroll
         for (int term = 0; term < 3; ++term)
 #pragma unroll
-          for (int k = 0; k < CT / 16; ++k)
-            umma_bf16(tmem + C::S_COL, kr0 + (uint64_t)(term * (C::TILE_BYTES >> 4) + k * C::ROW), v0 + (uint64_t)(k * C::ROW), KV,
-                      WITH_OUT || c > 0 || term > 0 || k > 0);
-        umma_commit(smem_u32(second));
-      }
-      __syncwarp();
-      if (!wait(second, c, 0x05)) break;
-      if (c + 1 < chunks) {
-        load_k(c + 1);
-        load_v(c + 1);
+          for (int i = 0; i < CT / 16; ++i)
+            umma_bf16(tmem + C::S_COL, k + (uint64_t)(term * (C::TILE_BYTES >> 4) + i * C::ROW), v + (uint64_t)(i * C::ROW), KV, term > 0 || i > 0 ? 1u : WITH_OUT || c > 0 ? 1u : 0u);
+        umma_commit(smem_u32(sdone + kp_place(c)));
+        umma_commit(smem_u32(vempty + place(c)));
       }
       __syncwarp();
     }
-  } else {
-    // ------------------------------------------------------------------------- the rest
-    const int quarter = warp & 3, half = warp >> 2, r = quarter * 32 + lane;      // r: token of the chunk, lane of tensor memory
+    // the last commits arrive before the block goes
+    if (ok) wait(vempty + place(chunks - 1), turn(chunks - 1), 0x11);
+  } else if (WITH_OUT && warp == W_A) {
+    // ------------------------------------------------------------------- products of out
+    const bool issuer = elect_one();
+    constexpr uint32_t QK = make_idesc(CT, CT), QS = make_idesc(CT, D) | B_BY_ROWS;
+    const uint64_t q0 = make_smem_desc(smem_u32(s_q), 8 * C::ROW, C::LAYOUT), k0 = make_smem_desc(smem_u32(s_k), 8 * C::ROW, C::LAYOUT);
+    const uint64_t st0 = make_rows_desc(smem_u32(s_s), C::STATE_SLAB, 8 * C::ROW, C::LAYOUT);
+    const uint64_t v0 = make_rows_desc(smem_u32(s_v), C::SLAB_BYTES, 8 * C::ROW, C::LAYOUT);
+    auto scores = [&](int c) {
+      const int s = place(c);
+      if (!wait(qfull + s, turn(c), 0x20) || !wait(kfull + s, turn(c), 0x21)) return false;
+      tc_fence_after();
+      if (issuer) {
+        const uint64_t o = (uint64_t)(s * (C::TILE_BYTES >> 4));
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          const uint64_t x = (uint64_t)((k / 4) * (C::SLAB_BYTES >> 4) + (k % 4) * 2);
+          umma_bf16(tmem + C::A_COL + (uint32_t)(s * CT), q0 + o + x, k0 + o + x, QK, k > 0);
+        }
+        umma_commit(smem_u32(afull + s));
+        umma_commit(smem_u32(kempty + s));
+      }
+      __syncwarp();
+      return true;
+    };
+    scores(0);
+    for (int c = 0; c < chunks && ok; ++c) {
+      const int s = place(c);
+      // sums of an earlier chunk in the same place have been read
+      if (!wait(sready, c, 0x22) || (c >= PLACES && !wait(oread, c - PLACES, 0x23))) break;
+      tc_fence_after();
+      if (issuer) {
+        const uint64_t q = q0 + (uint64_t)(s * (C::TILE_BYTES >> 4));
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k)
+          umma_bf16(tmem + C::O_COL + (uint32_t)(s * D), q + (uint64_t)((k / 4) * (C::SLAB_BYTES >> 4) + (k % 4) * 2), st0 + (uint64_t)(k * C::ROW), QS, k > 0);
+        umma_commit(smem_u32(ofirst));
+        umma_commit(smem_u32(qempty + s));
+      }
+      __syncwarp();
+      // with two places the next scores are formed meanwhile: theirs were read before the last P was there
+      if (PLACES == 2 && c + 1 < chunks && !scores(c + 1)) break;
+      if (!wait(pready, c, 0x24)) break;
+      tc_fence_after();
+      if (issuer) {
+        const uint64_t v = v0 + (uint64_t)(s * (C::TILE_BYTES >> 4));
+#pragma unroll
+        for (int k = 0; k < CT / 16; ++k) umma_bf16_ts(tmem + C::O_COL + (uint32_t)(s * D), tmem + C::P_COL + (uint32_t)(k * 8), v + (uint64_t)(k * C::ROW), QS, 1);
+        umma_commit(smem_u32(odone));
+        umma_commit(smem_u32(vempty + s));
+      }
+      __syncwarp();
+      if (PLACES == 1 && c + 1 < chunks && !scores(c + 1)) break;
+    }
+  } else if (WITH_OUT && warp >= W_OUT) {
+    // ---------------------------------------------------------------------------- P and out
+    const int quarter = warp & 3, half = (warp - W_OUT) >> 2, r = quarter * 32 + lane;      // r: token of the chunk, lane of tensor memory
     const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
+    constexpr int PIECES = D / 32;     // of 16 columns, from c0 on
+    const int c0 = half * (D / 2);
+    const float scale = p.scale;
+    __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.o.p) + b * p.o.b + h * p.o.h;
+    auto arrive = [&](uint64_t* bar) {
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(bar));
+    };
+    auto store = [&](int c) {          // out of chunk c, which is there
+      tc_fence_after();
+      uint32_t y[PIECES][16];
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) tmem_ld16_async(lanes + C::O_COL + (uint32_t)(place(c) * D + c0 + 16 * i), y[i]);
+      tmem_wait_ld();
+      arrive(oread);
+      const int t = t0 + c * CT + r;
+      if (t < t1) {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            auto two = [&](int e) { return pack_bf16(__uint_as_float(y[i][8 * x + e]) * scale, __uint_as_float(y[i][8 * x + e + 1]) * scale); };
+            *reinterpret_cast<uint4*>(out + (int64_t)t * p.o.t + c0 + 16 * i + 8 * x) = make_uint4(two(0), two(2), two(4), two(6));
+          }
+      }
+    };
+    for (int c = 0; c < chunks; ++c) {
+      const int s = place(c);
+      if (!wait(afull + s, turn(c), 0x31) || (PLACES == 2 && c > 0 && !wait(odone, c - 1, 0x32))) break;      // the last P has been used
+      tc_fence_after();
+      // weights within the chunk: blocks of 32 columns below the diagonal, on it, and above it
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const int i = 2 * half + y;
+        uint32_t w[16];
+        if (i > quarter) {
+#pragma unroll
+          for (int x = 0; x < 16; ++x) w[x] = 0u;
+        } else {
+          uint32_t v[32];
+          tmem_ld32(lanes + C::A_COL + (uint32_t)(s * CT + 32 * i), v);
+          if (i < quarter) {
+            const float f = pw[r - 32 * i - 31];      // decay^(r - j) = decay^(r - 32 i - 31) decay^(31 - (j - 32 i))
+            const Two f2 = pack2(f, f);
+#pragma unroll
+            for (int x = 0; x < 16; x += 2) {
+              const float4 g = *reinterpret_cast<const float4*>(pr + 2 * x);
+              float a0, a1, a2, a3;
+              unpack2(mul2_of(pack2(__uint_as_float(v[2 * x]), __uint_as_float(v[2 * x + 1])), mul2_of(f2, pack2(g.x, g.y))), a0, a1);
+              unpack2(mul2_of(pack2(__uint_as_float(v[2 * x + 2]), __uint_as_float(v[2 * x + 3])), mul2_of(f2, pack2(g.z, g.w))), a2, a3);
+              w[x] = pack_bf16(a0, a1);
+              w[x + 1] = pack_bf16(a2, a3);
+            }
+          } else {
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+              const float lo = lane >= 2 * x ? __uint_as_float(v[2 * x]) * pw[lane - 2 * x] : 0.f;
+              const float hi = lane >= 2 * x + 1 ? __uint_as_float(v[2 * x + 1]) * pw[lane - 2 * x - 1] : 0.f;
+              w[x] = pack_bf16(lo, hi);
+            }
+          }
+        }
+        tmem_st16(lanes + C::P_COL + (uint32_t)(16 * i), w);
+      }
+      if (!wait(ofirst, c, 0x33)) break;
+      tc_fence_after();
+      {
+        const float f = pw[r + 1];
+        uint32_t v[PIECES][16];
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) tmem_ld16_async(lanes + C::O_COL + (uint32_t)(s * D + c0 + 16 * i), v[i]);
+        tmem_wait_ld();
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+#pragma unroll
+          for (int x = 0; x < 16; ++x) v[i][x] = __float_as_uint(__uint_as_float(v[i][x]) * f);
+          tmem_st16(lanes + C::O_COL + (uint32_t)(s * D + c0 + 16 * i), v[i]);
+        }
+      }
+      tmem_wait_st();
+      arrive(pready);
+      // with two places the chunk before is stored while this one's product runs
+      if (PLACES == 2) {
+        if (c > 0) store(c - 1);
+      } else {
+        if (!wait(odone, c, 0x30)) break;
+        store(c);
+      }
+    }
+    if (PLACES == 2 && ok && wait(odone, chunks - 1, 0x34)) store(chunks - 1);
+  } else if (warp < GROUP) {
+    // ------------------------------------------------------------------------ K' and the state
+    const int quarter = warp & 3, half = warp >> 2, r = quarter * 32 + lane;      // r: token of the chunk
+    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + C::S_COL;
     // row of the state in this lane: a product of 64 rows leaves 16 to each quarter's first lanes
     const int row = C::M == 128 ? r : quarter * 16 + (lane & 15);
     const bool has_row = (C::M == 128 || lane < 16) && row < D;
-    bool ok = true;
-    auto wait = [&](uint64_t* bar, int c, int code) {
-      ok = __all_sync(0xffffffffu, ok && mbar_wait(smem_u32(bar), (uint32_t)(c & 1), abort_flag, s_status, WAIT_LINEAR_TC + code, WAIT_LIMIT));
-      return ok;
-    };
+    constexpr int PIECES = D / 32;     // of 16 columns, from c0 on
+    const int c0 = half * (D / 2);
     auto arrive = [&](uint64_t* bar) {
       tc_fence_before();
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(bar));
     };
-    // the columns of state and sums that are this warp's: pieces of 16 from c0 on
-    constexpr int PIECES = D / 32;
-    const int c0 = half * (D / 2);
-    // 16 columns of this lane's row of the state into the operand's rows
-    auto put_state = [&](int col, const uint32_t (&v)[16]) {
+    auto put_state = [&](const uint32_t (&v)[PIECES][16]) {      // into the operand's rows
       if (!has_row) return;
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int run = (col & 63) / 8 + x, to = D == 32 ? run ^ ((row >> 1) & 3) : run ^ (row & 7);
-        auto two = [&](int y) { return pack_bf16(__uint_as_float(v[8 * x + y]), __uint_as_float(v[8 * x + y + 1])); };
-        *reinterpret_cast<uint4*>(s_s + (col / 64) * C::STATE_SLAB + row * C::ROW + to * 16) = make_uint4(two(0), two(2), two(4), two(6));
-      }
+      for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int col = c0 + 16 * i, run = (col & 63) / 8 + x, to = D == 32 ? run ^ ((row >> 1) & 3) : run ^ (row & 7);
+          auto two = [&](int e) { return pack_bf16(__uint_as_float(v[i][8 * x + e]), __uint_as_float(v[i][8 * x + e + 1])); };
+          *reinterpret_cast<uint4*>(s_s + (col / 64) * C::STATE_SLAB + row * C::ROW + to * 16) = make_uint4(two(0), two(2), two(4), two(6));
+        }
     };
-    // all of this warp's columns times f
-    auto scale_columns = [&](uint32_t first, float f) {
-      uint32_t v[PIECES][16];
-#pragma unroll
-      for (int i = 0; i < PIECES; ++i) tmem_ld16_async(lanes + first + (uint32_t)(c0 + 16 * i), v[i]);
-      tmem_wait_ld();
-#pragma unroll
-      for (int i = 0; i < PIECES; ++i) {
-#pragma unroll
-        for (int x = 0; x < 16; ++x) v[i][x] = __float_as_uint(__uint_as_float(v[i][x]) * f);
-        tmem_st16(lanes + first + (uint32_t)(c0 + 16 * i), v[i]);
-      }
-    };
+    uint32_t v[PIECES][16];
     if (WITH_OUT) {
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) {
-        const int col = c0 + 16 * i;
-        uint32_t v[16];
+      for (int i = 0; i < PIECES; ++i)
 #pragma unroll
         for (int x = 0; x < 16; x += 4) {
-          const float4 f = has_row ? *reinterpret_cast<const float4*>(from + row * D + col + x) : make_float4(0.f, 0.f, 0.f, 0.f);
-          v[x] = __float_as_uint(f.x); v[x + 1] = __float_as_uint(f.y); v[x + 2] = __float_as_uint(f.z); v[x + 3] = __float_as_uint(f.w);
+          const float4 f = has_row ? *reinterpret_cast<const float4*>(from + row * D + c0 + 16 * i + x) : make_float4(0.f, 0.f, 0.f, 0.f);
+          v[i][x] = __float_as_uint(f.x); v[i][x + 1] = __float_as_uint(f.y); v[i][x + 2] = __float_as_uint(f.z); v[i][x + 3] = __float_as_uint(f.w);
         }
-        tmem_st16(lanes + C::S_COL + (uint32_t)col, v);
-        put_state(col, v);
-      }
-      tmem_wait_st();
-      arrive(sready);
     }
-    __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.o.p) + b * p.o.b + h * p.o.h;
+    float behind = 1.f;                // decay^(tokens behind the chunk), where only the sum is wanted
     for (int c = 0; c < chunks; ++c) {
-      const int t = t0 + c * CT, m = min(CT, t1 - t);
-      if (!wait(kfull, c, 0x10)) break;
-      if (WITH_OUT) {
-        if (!wait(first, c, 0x11)) break;
-        tc_fence_after();
-        // weights within the chunk: blocks of 32 columns below the diagonal, on it, and above it; either half lies over scores of its own
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const int i = 2 * half + y;
-          uint32_t w[16];
-          if (i > quarter) {
-#pragma unroll
-            for (int x = 0; x < 16; ++x) w[x] = 0u;
-          } else {
-            uint32_t v[32];
-            tmem_ld32(lanes + 32 * i, v);
-            if (i < quarter) {
-              const float f = pw[r - 32 * i - 31];      // decay^(r - j) = decay^(r - 32 i - 31) decay^(31 - (j - 32 i))
-              const Two f2 = pack2(f, f);
-#pragma unroll
-              for (int x = 0; x < 16; x += 2) {
-                const float4 g = *reinterpret_cast<const float4*>(pr + 2 * x);
-                float a0, a1, a2, a3;
-                unpack2(mul2_of(pack2(__uint_as_float(v[2 * x]), __uint_as_float(v[2 * x + 1])), mul2_of(f2, pack2(g.x, g.y))), a0, a1);
-                unpack2(mul2_of(pack2(__uint_as_float(v[2 * x + 2]), __uint_as_float(v[2 * x + 3])), mul2_of(f2, pack2(g.z, g.w))), a2, a3);
-                w[x] = pack_bf16(a0, a1);
-                w[x + 1] = pack_bf16(a2, a3);
-              }
-            } else {
-#pragma unroll
-              for (int x = 0; x < 16; ++x) {
-                const float lo = lane >= 2 * x ? __uint_as_float(v[2 * x]) * pw[lane - 2 * x] : 0.f;
-                const float hi = lane >= 2 * x + 1 ? __uint_as_float(v[2 * x + 1]) * pw[lane - 2 * x - 1] : 0.f;
-                w[x] = pack_bf16(lo, hi);
-              }
-            }
-          }
-          tmem_st16(lanes + 64 * half + 16 * y, w);
-        }
-        scale_columns(C::O_COL, pw[r + 1]);
-      }
-      if (WITH_OUT || c > 0) scale_columns(C::S_COL, pw[m]);
-      // K' = decay^(m-1-r) k in three bf16 terms, 24 bits: the state is as good as fp32.  Runs of 16 bytes in a turned order, so that
-      // eight rows of 128 bytes do not meet in the same banks; the swizzle moves runs within a row and need not be undone.
+      const int s = place(c), m = min(CT, t1 - token_of(c));
+      // the K' that lay here has been used (with out and two places the state's wait below has seen to it)
+      if (c >= KPP && (KPP == 1 || !WITH_OUT) && !wait(sdone + kp_place(c), kp_turn(c) - 1, 0x40)) break;
+      // K' = decay^(m-1-r) k in three bf16 terms; where only the segment's sum is wanted, decay^(tokens behind it) k, and the state is never
+      // scaled.  Runs of 16 bytes in a turned order, so that eight rows of 128 bytes do not meet in the same banks; the
+      // swizzle moves runs within a row and need not be undone.
       const bool here = r < m;
-      const float f = here ? pw[m - 1 - r] : 0.f;
-      if (!wait(vfull, c, 0x12)) break;
+      const float f = here ? pw[m - 1 - r] * behind : 0.f;
+      if (!WITH_OUT) behind *= pw[CT];
+      if (!wait(kfull + s, turn(c), 0x42) || !wait(vfull + s, turn(c), 0x43)) break;
       const Two f2 = pack2(f, f);
+      const uint8_t* kk = s_k + s * C::TILE_BYTES;
+      uint8_t* kp = s_kp + kp_place(c) * 3 * C::TILE_BYTES;
 #pragma unroll
       for (int i = 0; i < C::SLABS * C::ROW / 32; ++i) {
-        const int run = half * (C::SLABS * C::ROW / 32) + i, s = run / (C::ROW / 16);
-        const int o = s * C::SLAB_BYTES + r * C::ROW + ((run + (D == 32 ? r >> 1 : r)) & (C::ROW / 16 - 1)) * 16;
-        const uint4 u = *reinterpret_cast<const uint4*>(s_k + o);
+        const int run = half * (C::SLABS * C::ROW / 32) + i, slab = run / (C::ROW / 16);
+        const int o = slab * C::SLAB_BYTES + r * C::ROW + ((run + (D == 32 ? r >> 1 : r)) & (C::ROW / 16 - 1)) * 16;
+        const uint4 u = *reinterpret_cast<const uint4*>(kk + o);
         const uint32_t in[4] = {u.x, u.y, u.z, u.w};
         uint32_t a[3][4];
 #pragma unroll
@@ -303,49 +412,47 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, WITH_OUT>::BLOCKS) linear_tc_k
             if (term < 2) y = sub2_of(y, pack2(__uint_as_float(a[term][x] << 16), __uint_as_float(a[term][x] & 0xFFFF0000u)));
           }
         }
-        *reinterpret_cast<uint4*>(s_k + o) = make_uint4(a[0][0], a[0][1], a[0][2], a[0][3]);
-        *reinterpret_cast<uint4*>(s_k1 + o) = make_uint4(a[1][0], a[1][1], a[1][2], a[1][3]);
-        *reinterpret_cast<uint4*>(s_k2 + o) = make_uint4(a[2][0], a[2][1], a[2][2], a[2][3]);
+#pragma unroll
+        for (int term = 0; term < 3; ++term) *reinterpret_cast<uint4*>(kp + term * C::TILE_BYTES + o) = make_uint4(a[term][0], a[term][1], a[term][2], a[term][3]);
         // rows behind the last token may hold anything, and weights of 0 would make NaN of it
-        if (!here) *reinterpret_cast<uint4*>(s_v + o) = make_uint4(0u, 0u, 0u, 0u);
+        if (!here) *reinterpret_cast<uint4*>(s_v + s * C::TILE_BYTES + o) = make_uint4(0u, 0u, 0u, 0u);
       }
-      tmem_wait_st();
-      arrive(pready);
-      if (!wait(second, c, 0x13)) break;
-      tc_fence_after();
-      const bool last = c + 1 == chunks;
-      // the state first: the next chunk's products wait for it, and for out having been read
-      if (WITH_OUT || last) {
-        uint32_t v[PIECES][16], y[PIECES][16];
+      arrive(kempty + s);
+      if (WITH_OUT) {
+        if (c > 0) {
+          // the chunk before has left its state; its copy as an operand has been used
+          if (!wait(sdone + kp_place(c - 1), kp_turn(c - 1), 0x44) || !wait(ofirst, c - 1, 0x45)) break;
+          tc_fence_after();
+#pragma unroll
+          for (int i = 0; i < PIECES; ++i) tmem_ld16_async(lanes + (uint32_t)(c0 + 16 * i), v[i]);
+          tmem_wait_ld();
+        }
+        put_state(v);
+        arrive(sready);
+        const float g = pw[m];
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-          tmem_ld16_async(lanes + C::S_COL + (uint32_t)(c0 + 16 * i), v[i]);
-          if (WITH_OUT) tmem_ld16_async(lanes + C::O_COL + (uint32_t)(c0 + 16 * i), y[i]);
+#pragma unroll
+          for (int x = 0; x < 16; ++x) v[i][x] = __float_as_uint(__uint_as_float(v[i][x]) * g);
+          tmem_st16(lanes + (uint32_t)(c0 + 16 * i), v[i]);
         }
-        tmem_wait_ld();
-        if (WITH_OUT && !last) {
+        tmem_wait_st();
+      }
+      arrive(kready + kp_place(c));
+    }
+    if (ok && wait(sdone + kp_place(chunks - 1), kp_turn(chunks - 1), 0x46)) {
+      tc_fence_after();
 #pragma unroll
-          for (int i = 0; i < PIECES; ++i) put_state(c0 + 16 * i, v[i]);
-          arrive(sready);
-        }
-        if (last && (!WITH_OUT || t1 == len) && has_row) {
-          float* to = WITH_OUT ? p.state_out + at : seg_state;
+      for (int i = 0; i < PIECES; ++i) tmem_ld16_async(lanes + (uint32_t)(c0 + 16 * i), v[i]);
+      tmem_wait_ld();
+      if ((!WITH_OUT || t1 == len) && has_row) {
+        float* to = WITH_OUT ? p.state_out + at : seg_state;
 #pragma unroll
-          for (int i = 0; i < PIECES; ++i)
+        for (int i = 0; i < PIECES; ++i)
 #pragma unroll
-            for (int x = 0; x < 16; x += 4)
-              *reinterpret_cast<float4*>(to + row * D + c0 + 16 * i + x) =
-                  make_float4(__uint_as_float(v[i][x]), __uint_as_float(v[i][x + 1]), __uint_as_float(v[i][x + 2]), __uint_as_float(v[i][x + 3]));
-        }
-        if (WITH_OUT && here) {
-#pragma unroll
-          for (int i = 0; i < PIECES; ++i)
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              auto two = [&](int e) { return pack_bf16(__uint_as_float(y[i][8 * x + e]) * p.scale, __uint_as_float(y[i][8 * x + e + 1]) * p.scale); };
-              *reinterpret_cast<uint4*>(out + (int64_t)(t + r) * p.o.t + c0 + 16 * i + 8 * x) = make_uint4(two(0), two(2), two(4), two(6));
-            }
-        }
+          for (int x = 0; x < 16; x += 4)
+            *reinterpret_cast<float4*>(to + row * D + c0 + 16 * i + x) =
+                make_float4(__uint_as_float(v[i][x]), __uint_as_float(v[i][x + 1]), __uint_as_float(v[i][x + 2]), __uint_as_float(v[i][x + 3]));
       }
     }
   }
@@ -359,7 +466,7 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, WITH_OUT>::BLOCKS) linear_tc_k
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == WORKERS) {
+  if (warp == W_B) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::TMEM) : "memory");
   }
@@ -375,10 +482,10 @@ cudaError_t launch(const LinearTcParams& p, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   const LinearParams& c = p.c;
   if (c.segments > 1) {
-    linear_tc_kernel<D, false><<<dim3((unsigned)c.segments - 1, (unsigned)c.heads, (unsigned)c.batch), THREADS, Cfg<D, false>::SMEM, s>>>(p);
+    linear_tc_kernel<D, false><<<dim3((unsigned)c.segments - 1, (unsigned)c.heads, (unsigned)c.batch), Cfg<D, false>::THREADS, Cfg<D, false>::SMEM, s>>>(p);
     if ((e = cudaGetLastError()) != cudaSuccess || (e = launch_linear_scan(c, D, s)) != cudaSuccess) return e;
   }
-  linear_tc_kernel<D, true><<<dim3((unsigned)c.segments, (unsigned)c.heads, (unsigned)c.batch), THREADS, Cfg<D, true>::SMEM, s>>>(p);
+  linear_tc_kernel<D, true><<<dim3((unsigned)c.segments, (unsigned)c.heads, (unsigned)c.batch), Cfg<D, true>::THREADS, Cfg<D, true>::SMEM, s>>>(p);
   return cudaGetLastError();
 }
 

@@ -43,7 +43,7 @@ struct alignas(32) LinearParams {
   float scale;
 };
 // How many segments the tokens are cut into, and of how many tokens.
-void linear_plan(int batch, int tokens, int heads, int D, bool bf16, int* segments, int* seg_tokens);
+void linear_plan(int batch, int tokens, int heads, bool bf16, int* segments, int* seg_tokens);
 cudaError_t launch_linear_step(const LinearParams& p, bool bf16, int D, cudaStream_t s);
 cudaError_t launch_linear_chunk(const LinearParams& p, int D, cudaStream_t s);    // fp32, and calls without tokens
 cudaError_t launch_linear_tc(const LinearParams& p, int D, cudaStream_t s);       // bf16

@@ -128,7 +128,7 @@ static tt_status check_linear(const char* who, const tt_linear_attention_args* a
 uint64_t tt_linear_attention_scratch_bytes(const tt_linear_attention_args* a) {
   if (check_linear("tt_linear_attention_scratch_bytes", a) != TT_OK) return 0;
   int segments, seg_tokens;
-  linear_plan(a->batch, a->tokens, a->heads, a->head_dim, a->precision == TT_BF16, &segments, &seg_tokens);
+  linear_plan(a->batch, a->tokens, a->heads, a->precision == TT_BF16, &segments, &seg_tokens);
   return segments > 1 ? (uint64_t)a->batch * (uint64_t)a->heads * (uint64_t)segments * (uint64_t)(a->head_dim * a->head_dim) * 4u : 0u;
 }
 
@@ -154,7 +154,7 @@ tt_status tt_linear_attention(const tt_linear_attention_args* a, void* cuda_stre
   p.seg_state = static_cast<float*>(a->scratch); p.status = a->status_dev;
   p.batch = a->batch; p.tokens = a->tokens; p.heads = a->heads; p.group = a->heads / a->kv_heads; p.num_slots = a->num_slots;
   p.scale = a->scale;
-  linear_plan(a->batch, a->tokens, a->heads, a->head_dim, bf16, &p.segments, &p.seg_tokens);
+  linear_plan(a->batch, a->tokens, a->heads, bf16, &p.segments, &p.seg_tokens);
   const cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
   const cudaError_t e = a->tokens == 1             ? launch_linear_step(p, bf16, a->head_dim, s)
                         : bf16 && a->tokens > 0 ? launch_linear_tc(p, a->head_dim, s)

@@ -133,7 +133,8 @@ def _linear_check(got, got_state, q, k, v, decay, state, scale, lengths, name, r
 @pytest.mark.parametrize("B,T,H,K,D", [
     (1, 1, 1, 1, 32), (5, 1, 2, 2, 64), (3, 1, 6, 2, 128), (40, 1, 8, 8, 64), (75, 1, 8, 4, 32), (38, 1, 8, 8, 128),
     (1, 2, 1, 1, 64), (2, 31, 3, 1, 32), (1, 32, 2, 2, 128), (2, 33, 2, 2, 128), (3, 63, 2, 1, 64), (1, 64, 6, 6, 64), (2, 65, 2, 2, 64),
-    (1, 127, 2, 2, 32), (1, 128, 6, 3, 128), (2, 129, 1, 1, 64), (1, 257, 6, 6, 64), (2, 300, 2, 1, 128), (1, 700, 4, 2, 32), (1, 1025, 1, 1, 64)])
+    (1, 127, 2, 2, 32), (1, 128, 6, 3, 128), (2, 129, 1, 1, 64), (1, 257, 6, 6, 64), (2, 300, 2, 1, 128), (1, 700, 4, 2, 32), (1, 1025, 1, 1, 64),
+    (8, 1300, 4, 4, 32), (8, 1300, 4, 2, 64), (8, 1300, 4, 4, 128), (40, 300, 8, 8, 64)])      # segments of several chunks; sequences enough without
 def test_linear_attention(cuda_device, dtype, B, T, H, K, D):
     for i, layout in enumerate(("plain", "fused", "heads first", "padded")):
         q, k, v, decay, state = _linear_case(cuda_device, 17 * T + i, B, T, H, K, D, dtype, layout)

@@ -42,13 +42,13 @@ def linear(q, k, v, log_decay, state, scale, lengths=None):
     S, A = state.double().clone(), state.double().abs()
     out, size = torch.zeros(B, T, H, D, dtype=torch.float64, device=q.device), torch.zeros(B, T, H, D, dtype=torch.float64, device=q.device)
     n = [T] * B if lengths is None else [max(0, min(T, int(x))) for x in lengths]
-    for b in range(B):
-        for t in range(n[b]):
-            kv = k[b, t, :, :, None] * v[b, t, :, None, :]
+    for b in range(B) if lengths is not None else [slice(None)]:
+        for t in range(n[b] if lengths is not None else T):
+            kv = k[b, t][..., :, None] * v[b, t][..., None, :]
             S[b] = torch.where(d[0] == 0, 0.0, S[b] * d[0]) + kv
             A[b] = torch.where(d[0] == 0, 0.0, A[b] * d[0]) + kv.abs()
-            out[b, t] = (q[b, t, :, None, :] @ S[b])[:, 0]
-            size[b, t] = (q[b, t, :, None, :].abs() @ A[b])[:, 0]
+            out[b, t] = (q[b, t][..., None, :] @ S[b])[..., 0, :]
+            size[b, t] = (q[b, t][..., None, :].abs() @ A[b])[..., 0, :]
     return out, size, S, A
 
 
