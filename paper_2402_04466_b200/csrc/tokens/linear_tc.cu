@@ -369,15 +369,23 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
           *reinterpret_cast<uint4*>(s_s + (col / 64) * C::STATE_SLAB + row * C::ROW + to * 16) = make_uint4(two(0), two(2), two(4), two(6));
         }
     };
-    uint32_t v[PIECES][16];
+    auto get_state = [&](uint32_t (&v)[PIECES][16]) {
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) tmem_ld16_async(lanes + (uint32_t)(c0 + 16 * i), v[i]);
+      tmem_wait_ld();
+    };
     if (WITH_OUT) {
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i)
+      for (int i = 0; i < PIECES; ++i) {
+        uint32_t v[16];
 #pragma unroll
         for (int x = 0; x < 16; x += 4) {
           const float4 f = has_row ? *reinterpret_cast<const float4*>(from + row * D + c0 + 16 * i + x) : make_float4(0.f, 0.f, 0.f, 0.f);
-          v[i][x] = __float_as_uint(f.x); v[i][x + 1] = __float_as_uint(f.y); v[i][x + 2] = __float_as_uint(f.z); v[i][x + 3] = __float_as_uint(f.w);
+          v[x] = __float_as_uint(f.x); v[x + 1] = __float_as_uint(f.y); v[x + 2] = __float_as_uint(f.z); v[x + 3] = __float_as_uint(f.w);
         }
+        tmem_st16(lanes + (uint32_t)(c0 + 16 * i), v);
+      }
+      tmem_wait_st();
     }
     float behind = 1.f;                // decay^(tokens behind the chunk), where only the sum is wanted
     for (int c = 0; c < chunks; ++c) {
@@ -394,28 +402,42 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
       const Two f2 = pack2(f, f);
       const uint8_t* kk = s_k + s * C::TILE_BYTES;
       uint8_t* kp = s_kp + kp_place(c) * 3 * C::TILE_BYTES;
+      // all reads come first: a store might, for all the compiler knows, change what a later read finds
+      constexpr int RUNS = C::SLABS * C::ROW / 32;      // to a thread
+      constexpr int BATCH = 2;
 #pragma unroll
-      for (int i = 0; i < C::SLABS * C::ROW / 32; ++i) {
-        const int run = half * (C::SLABS * C::ROW / 32) + i, slab = run / (C::ROW / 16);
-        const int o = slab * C::SLAB_BYTES + r * C::ROW + ((run + (D == 32 ? r >> 1 : r)) & (C::ROW / 16 - 1)) * 16;
-        const uint4 u = *reinterpret_cast<const uint4*>(kk + o);
-        const uint32_t in[4] = {u.x, u.y, u.z, u.w};
-        uint32_t a[3][4];
+      for (int i0 = 0; i0 < RUNS; i0 += BATCH) {
+        uint4 u[BATCH];
+        int o[BATCH];
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          Two y = mul2_of(pack2(__uint_as_float(in[x] << 16), __uint_as_float(in[x] & 0xFFFF0000u)), f2);
-#pragma unroll
-          for (int term = 0; term < 3; ++term) {
-            float lo, hi;
-            unpack2(y, lo, hi);
-            a[term][x] = here ? pack_bf16(lo, hi) : 0u;
-            if (term < 2) y = sub2_of(y, pack2(__uint_as_float(a[term][x] << 16), __uint_as_float(a[term][x] & 0xFFFF0000u)));
-          }
+        for (int i = 0; i < BATCH; ++i) {
+          const int run = half * RUNS + i0 + i, slab = run / (C::ROW / 16);
+          o[i] = slab * C::SLAB_BYTES + r * C::ROW + ((run + (D == 32 ? r >> 1 : r)) & (C::ROW / 16 - 1)) * 16;
+          u[i] = *reinterpret_cast<const uint4*>(kk + o[i]);
+          if (!here) u[i] = make_uint4(0u, 0u, 0u, 0u);
         }
 #pragma unroll
-        for (int term = 0; term < 3; ++term) *reinterpret_cast<uint4*>(kp + term * C::TILE_BYTES + o) = make_uint4(a[term][0], a[term][1], a[term][2], a[term][3]);
-        // rows behind the last token may hold anything, and weights of 0 would make NaN of it
-        if (!here) *reinterpret_cast<uint4*>(s_v + s * C::TILE_BYTES + o) = make_uint4(0u, 0u, 0u, 0u);
+        for (int i = 0; i < BATCH; ++i) {
+          const uint32_t in[4] = {u[i].x, u[i].y, u[i].z, u[i].w};
+          uint32_t a[3][4];
+          Two y[4];
+#pragma unroll
+          for (int x = 0; x < 4; ++x) y[x] = mul2_of(pack2(__uint_as_float(in[x] << 16), __uint_as_float(in[x] & 0xFFFF0000u)), f2);
+          // cut off, not rounded: three times eight bits are all of fp32's 24
+#pragma unroll
+          for (int term = 0; term < 3; ++term)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              float lo, hi;
+              unpack2(y[x], lo, hi);
+              a[term][x] = __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);
+              if (term < 2) y[x] = sub2_of(y[x], pack2(__uint_as_float(__float_as_uint(lo) & 0xFFFF0000u), __uint_as_float(__float_as_uint(hi) & 0xFFFF0000u)));
+            }
+#pragma unroll
+          for (int term = 0; term < 3; ++term) *reinterpret_cast<uint4*>(kp + term * C::TILE_BYTES + o[i]) = make_uint4(a[term][0], a[term][1], a[term][2], a[term][3]);
+          // rows behind the last token may hold anything, and weights of 0 would make NaN of it
+          if (!here) *reinterpret_cast<uint4*>(s_v + s * C::TILE_BYTES + o[i]) = make_uint4(0u, 0u, 0u, 0u);
+        }
       }
       arrive(kempty + s);
       if (WITH_OUT) {
@@ -423,28 +445,30 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
           // the chunk before has left its state; its copy as an operand has been used
           if (!wait(sdone + kp_place(c - 1), kp_turn(c - 1), 0x44) || !wait(ofirst, c - 1, 0x45)) break;
           tc_fence_after();
-#pragma unroll
-          for (int i = 0; i < PIECES; ++i) tmem_ld16_async(lanes + (uint32_t)(c0 + 16 * i), v[i]);
-          tmem_wait_ld();
         }
-        put_state(v);
-        arrive(sready);
+        uint32_t v[PIECES][16];
+        get_state(v);
+        // first what the state's next product waits for
         const float g = pw[m];
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
+          uint32_t y[16];
 #pragma unroll
-          for (int x = 0; x < 16; ++x) v[i][x] = __float_as_uint(__uint_as_float(v[i][x]) * g);
-          tmem_st16(lanes + (uint32_t)(c0 + 16 * i), v[i]);
+          for (int x = 0; x < 16; ++x) y[x] = __float_as_uint(__uint_as_float(v[i][x]) * g);
+          tmem_st16(lanes + (uint32_t)(c0 + 16 * i), y);
         }
         tmem_wait_st();
+        arrive(kready + kp_place(c));
+        put_state(v);
+        arrive(sready);
+      } else {
+        arrive(kready + kp_place(c));
       }
-      arrive(kready + kp_place(c));
     }
     if (ok && wait(sdone + kp_place(chunks - 1), kp_turn(chunks - 1), 0x46)) {
       tc_fence_after();
-#pragma unroll
-      for (int i = 0; i < PIECES; ++i) tmem_ld16_async(lanes + (uint32_t)(c0 + 16 * i), v[i]);
-      tmem_wait_ld();
+      uint32_t v[PIECES][16];
+      get_state(v);
       if ((!WITH_OUT || t1 == len) && has_row) {
         float* to = WITH_OUT ? p.state_out + at : seg_state;
 #pragma unroll
