@@ -274,7 +274,7 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
         for (int i = 0; i < PIECES; ++i)
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            auto two = [&](int e) { return pack_bf16(__uint_as_float(y[i][8 * x + e]) * scale, __uint_as_float(y[i][8 * x + e + 1]) * scale); };
+            auto two = [&](int e) { return pack_bf16(__uint_as_float(y[i][8 * x + e]), __uint_as_float(y[i][8 * x + e + 1])); };
             *reinterpret_cast<uint4*>(out + (int64_t)t * p.o.t + c0 + 16 * i + 8 * x) = make_uint4(two(0), two(2), two(4), two(6));
           }
       }
@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
           uint32_t v[32];
           tmem_ld32(lanes + C::A_COL + (uint32_t)(s * CT + 32 * i), v);
           if (i < quarter) {
-            const float f = pw[r - 32 * i - 31];      // decay^(r - j) = decay^(r - 32 i - 31) decay^(31 - (j - 32 i))
+            const float f = scale * pw[r - 32 * i - 31];      // decay^(r - j) = decay^(r - 32 i - 31) decay^(31 - (j - 32 i))
             const Two f2 = pack2(f, f);
 #pragma unroll
             for (int x = 0; x < 16; x += 2) {
@@ -309,8 +309,8 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
           } else {
 #pragma unroll
             for (int x = 0; x < 16; ++x) {
-              const float lo = lane >= 2 * x ? __uint_as_float(v[2 * x]) * pw[lane - 2 * x] : 0.f;
-              const float hi = lane >= 2 * x + 1 ? __uint_as_float(v[2 * x + 1]) * pw[lane - 2 * x - 1] : 0.f;
+              const float lo = lane >= 2 * x ? __uint_as_float(v[2 * x]) * (scale * pw[lane - 2 * x]) : 0.f;
+              const float hi = lane >= 2 * x + 1 ? __uint_as_float(v[2 * x + 1]) * (scale * pw[lane - 2 * x - 1]) : 0.f;
               w[x] = pack_bf16(lo, hi);
             }
           }
@@ -320,7 +320,7 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
       if (!wait(ofirst, c, 0x33)) break;
       tc_fence_after();
       {
-        const float f = pw[r + 1];
+        const float f = scale * pw[r + 1];
         uint32_t v[PIECES][16];
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) tmem_ld16_async(lanes + C::O_COL + (uint32_t)(s * D + c0 + 16 * i), v[i]);
@@ -439,7 +439,8 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
           if (!here) *reinterpret_cast<uint4*>(s_v + s * C::TILE_BYTES + o[i]) = make_uint4(0u, 0u, 0u, 0u);
         }
       }
-      arrive(kempty + s);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(kempty + s));
       if (WITH_OUT) {
         if (c > 0) {
           // the chunk before has left its state; its copy as an operand has been used
