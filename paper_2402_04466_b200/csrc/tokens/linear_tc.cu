@@ -3,10 +3,9 @@
 // With the fp32 state S before a chunk, l the head's decay, tokens i, j counted from 0, m their number:
 //   scores  A = Q K^T;   P_ij = l^(i-j) A_ij for i >= j, else 0
 //   out_i   = scale * ( l^(i+1) (Q S)_i + (P V)_i )
-//   state   S' = l^m S + K'^T V,  K'_j = l^(m-1-j) k_j
-// The state stays in tensor memory as the fp32 accumulator of its own product, scaled in place before each chunk's is added; K' goes into
-// that product as three bf16 terms, 24 bits, so the state is as good as fp32.  P and, for Q S, a copy of the state are
-// rounded to bf16 once each, as far as out itself is.
+//   state   S' = l^m S + K'^T V,  K'_j = l^(m-1-j) k_j      (formed as its transpose, V^T K')
+// K' goes into the state's product as three bf16 terms, 24 bits, and the state is kept in fp32.  P and, for Q S, a copy of the state
+// are rounded to bf16 once each, as far as out itself is.
 //
 // A sequence is sequential in its chunks, and a chunk is a chain of copies, products and register work, 12 000 cycles when one follows the
 // other (two blocks to a multiprocessor then took 125 us for eight maps of 14400 tokens, 4 heads of 64).  So one block holds the
@@ -43,14 +42,18 @@ struct Cfg {
   static constexpr int STATE_SLAB = D * ROW, STATE_BYTES = SLABS * STATE_SLAB;
   static constexpr uint32_t LAYOUT = D == 32 ? 4u : 2u;             // 64- or 128-byte swizzle
   static constexpr int M = D == 128 ? 128 : 64;                     // rows of the state's product
-  static constexpr int PLACES = D == 128 && WITH_OUT ? 1 : 2;       // of operands, K', scores and sums
-  static constexpr int KP_PLACES = D == 128 ? 1 : 2;
-  static constexpr uint32_t S_COL = 0;                              // the state
-  static constexpr uint32_t A_COL = D, P_COL = A_COL + PLACES * CT, O_COL = P_COL + CT / 2;    // scores, weights, sums
-  static constexpr uint32_t COLS = WITH_OUT ? O_COL + PLACES * D : D;
+  static constexpr int PLACES = WITH_OUT ? (D == 128 ? 1 : 2) : D == 128 ? 2 : 4;       // of operands, scores and sums
+  static constexpr int KP_PLACES = D == 128 ? 1 : 2;                // of K'
+  // Where only a segment's sum is wanted and heads are of up to 64, K's three terms are side by side, one operand of 3 D columns: the product is
+  // 8 instructions, not 24, and the three parts are added at the end.  Else the terms follow one another into the state.  (Side by
+  // side with out as well, adding each chunk's product to a state in registers: 118 us where this takes 107.)
+  static constexpr bool SIDE = !WITH_OUT && D <= 64;
+  static constexpr int N = SIDE ? 3 * D : D;                        // columns of the state's product
+  static constexpr uint32_t A_COL = N, P_COL = A_COL + (PLACES < 2 ? 1 : 2) * CT, O_COL = P_COL + CT / 2;    // scores, weights, sums; the state's lies first
+  static constexpr uint32_t COLS = WITH_OUT ? O_COL + PLACES * D : N;
   static constexpr uint32_t TMEM = COLS <= 32 ? 32 : COLS <= 64 ? 64 : COLS <= 128 ? 128 : COLS <= 256 ? 256 : 512;
   static constexpr int TABLE_BYTES = (CT + 4) * 4 + 128;
-  static constexpr int SMEM = (WITH_OUT ? 3 : 2) * PLACES * TILE_BYTES + 3 * KP_PLACES * TILE_BYTES + (WITH_OUT ? STATE_BYTES : 0) + TABLE_BYTES + 256 + 1024;
+  static constexpr int SMEM = (WITH_OUT ? 3 : 2) * PLACES * TILE_BYTES + 3 * KP_PLACES * TILE_BYTES + (WITH_OUT ? STATE_BYTES : 0) + TABLE_BYTES + 512 + 1024;
   static_assert(COLS <= 512 && SMEM <= 227 * 1024, "tensor and shared memory");
 };
 
@@ -61,24 +64,24 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
   const LinearParams& p = pp.c;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* s_k = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  // K': [KPP][three terms].  The values lie behind it: heads of 32 fill half of the 64 rows of the state's product, and the other half is
+  uint8_t* s_v = s_k + PLACES * C::TILE_BYTES;
+  // K': [KPP][three terms].  It lies behind the values: heads of 32 fill half of the 64 rows of the state's product, and the other half is
   // read, for nothing, from one slab further on, which has to be the block's own memory.
-  uint8_t* s_kp = s_k + PLACES * C::TILE_BYTES;
-  uint8_t* s_v = s_kp + 3 * KPP * C::TILE_BYTES;
-  uint8_t* s_q = s_v + PLACES * C::TILE_BYTES;                       // WITH_OUT only, as the next
+  uint8_t* s_kp = s_v + PLACES * C::TILE_BYTES;
+  uint8_t* s_q = s_kp + 3 * KPP * C::TILE_BYTES;                     // WITH_OUT only, as the next
   uint8_t* s_s = s_q + (WITH_OUT ? PLACES * C::TILE_BYTES : 0);      // the state as an operand, rows along K
   float* pw = reinterpret_cast<float*>(s_s + (WITH_OUT ? C::STATE_BYTES : 0));   // decay^0 .. decay^128
   float* pr = pw + CT + 4;                                           // decay^31 .. decay^0
   uint64_t* qfull = reinterpret_cast<uint64_t*>(pr + 32);            // [PLACES], as the next five
-  uint64_t* kfull = qfull + 2;
-  uint64_t* vfull = kfull + 2;
-  uint64_t* qempty = vfull + 2;        // Q S is done
-  uint64_t* kempty = qempty + 2;       // scores are done, K' is made
-  uint64_t* vempty = kempty + 2;       // both products of V are done
-  uint64_t* afull = vempty + 2;        // [PLACES] scores are there
-  uint64_t* kready = afull + 2;        // [KP_PLACES] K' is there, and the state is scaled
-  uint64_t* sdone = kready + 2;        // [KP_PLACES] the state is there
-  uint64_t* ofirst = sdone + 2;        // Q S is there
+  uint64_t* kfull = qfull + 4;
+  uint64_t* vfull = kfull + 4;
+  uint64_t* qempty = vfull + 4;        // Q S is done
+  uint64_t* kempty = qempty + 4;       // scores are done, K' is made
+  uint64_t* vempty = kempty + 4;       // both products of V are done
+  uint64_t* kready = vempty + 4;       // [KP_PLACES] K' is there and the state is scaled
+  uint64_t* sdone = kready + 2;        // [KP_PLACES] the state's product is done
+  uint64_t* afull = sdone + 2;         // [PLACES] scores are there
+  uint64_t* ofirst = afull + 2;       // Q S is there
   uint64_t* pready = ofirst + 1;       // P is there, and the sums are scaled
   uint64_t* odone = pready + 1;        // out is there
   uint64_t* oread = odone + 1;         // out is in registers
@@ -145,8 +148,8 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
     ok = __all_sync(0xffffffffu, ok && mbar_wait_uniform(smem_u32(bar), (uint32_t)phase & 1u, abort_flag, s_status, WAIT_LINEAR_TC + code, WAIT_LIMIT));
     return ok;
   };
-  auto place = [](int c) { return PLACES == 2 ? c & 1 : 0; };
-  auto turn = [](int c) { return PLACES == 2 ? c >> 1 : c; };
+  auto place = [](int c) { return c & (PLACES - 1); };
+  auto turn = [](int c) { return PLACES == 4 ? c >> 2 : PLACES == 2 ? c >> 1 : c; };
   auto kp_place = [](int c) { return KPP == 2 ? c & 1 : 0; };
   auto kp_turn = [](int c) { return KPP == 2 ? c >> 1 : c; };
   // where only a segment's sum is wanted, its chunks are taken from the last to the first: their weights are then a product
@@ -175,19 +178,21 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
   } else if (warp == W_B) {
     // --------------------------------------------------------------- products of the state
     const bool issuer = elect_one();
-    constexpr uint32_t KV = make_idesc(C::M, D) | A_BY_ROWS | B_BY_ROWS;
+    constexpr uint32_t VK = make_idesc(C::M, C::N) | A_BY_ROWS | B_BY_ROWS;
     const uint64_t v0 = make_rows_desc(smem_u32(s_v), C::SLAB_BYTES, 8 * C::ROW, C::LAYOUT);
-    const uint64_t k0 = make_rows_desc(smem_u32(s_kp), C::SLAB_BYTES, 8 * C::ROW, C::LAYOUT);
+    // the terms' runs of columns are a tile apart, where they are one operand
+    const uint64_t k0 = make_rows_desc(smem_u32(s_kp), C::SIDE ? C::TILE_BYTES : C::SLAB_BYTES, 8 * C::ROW, C::LAYOUT);
     for (int c = 0; c < chunks; ++c) {
       if (!wait(kready + kp_place(c), kp_turn(c), 0x10)) break;
       tc_fence_after();
       if (issuer) {
         const uint64_t v = v0 + (uint64_t)(place(c) * (C::TILE_BYTES >> 4)), k = k0 + (uint64_t)(kp_place(c) * 3 * (C::TILE_BYTES >> 4));
+        const uint32_t more = WITH_OUT || c > 0 ? 1u : 0u;
 #pragma unroll
-        for (int term = 0; term < 3; ++term)
+        for (int term = 0; term < (C::SIDE ? 1 : 3); ++term)
 #pragma unroll
           for (int i = 0; i < CT / 16; ++i)
-            umma_bf16(tmem + C::S_COL, k + (uint64_t)(term * (C::TILE_BYTES >> 4) + i * C::ROW), v + (uint64_t)(i * C::ROW), KV, term > 0 || i > 0 ? 1u : WITH_OUT || c > 0 ? 1u : 0u);
+            umma_bf16(tmem, v + (uint64_t)(i * C::ROW), k + (uint64_t)(term * (C::TILE_BYTES >> 4) + i * C::ROW), VK, term > 0 || i > 0 ? 1u : more);
         umma_commit(smem_u32(sdone + kp_place(c)));
         umma_commit(smem_u32(vempty + place(c)));
       }
@@ -198,9 +203,9 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
   } else if (WITH_OUT && warp == W_A) {
     // ------------------------------------------------------------------- products of out
     const bool issuer = elect_one();
-    constexpr uint32_t QK = make_idesc(CT, CT), QS = make_idesc(CT, D) | B_BY_ROWS;
+    constexpr uint32_t QK = make_idesc(CT, CT), QS = make_idesc(CT, D), PV = QS | B_BY_ROWS;
     const uint64_t q0 = make_smem_desc(smem_u32(s_q), 8 * C::ROW, C::LAYOUT), k0 = make_smem_desc(smem_u32(s_k), 8 * C::ROW, C::LAYOUT);
-    const uint64_t st0 = make_rows_desc(smem_u32(s_s), C::STATE_SLAB, 8 * C::ROW, C::LAYOUT);
+    const uint64_t st0 = make_smem_desc(smem_u32(s_s), 8 * C::ROW, C::LAYOUT);      // rows are value columns, along them the keys'
     const uint64_t v0 = make_rows_desc(smem_u32(s_v), C::SLAB_BYTES, 8 * C::ROW, C::LAYOUT);
     auto scores = [&](int c) {
       const int s = place(c);
@@ -229,7 +234,7 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
         const uint64_t q = q0 + (uint64_t)(s * (C::TILE_BYTES >> 4));
 #pragma unroll
         for (int k = 0; k < D / 16; ++k)
-          umma_bf16(tmem + C::O_COL + (uint32_t)(s * D), q + (uint64_t)((k / 4) * (C::SLAB_BYTES >> 4) + (k % 4) * 2), st0 + (uint64_t)(k * C::ROW), QS, k > 0);
+          umma_bf16(tmem + C::O_COL + (uint32_t)(s * D), q + (uint64_t)((k / 4) * (C::SLAB_BYTES >> 4) + (k % 4) * 2), st0 + (uint64_t)((k / 4) * (C::STATE_SLAB >> 4) + (k % 4) * 2), QS, k > 0);
         umma_commit(smem_u32(ofirst));
         umma_commit(smem_u32(qempty + s));
       }
@@ -241,7 +246,7 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
       if (issuer) {
         const uint64_t v = v0 + (uint64_t)(s * (C::TILE_BYTES >> 4));
 #pragma unroll
-        for (int k = 0; k < CT / 16; ++k) umma_bf16_ts(tmem + C::O_COL + (uint32_t)(s * D), tmem + C::P_COL + (uint32_t)(k * 8), v + (uint64_t)(k * C::ROW), QS, 1);
+        for (int k = 0; k < CT / 16; ++k) umma_bf16_ts(tmem + C::O_COL + (uint32_t)(s * D), tmem + C::P_COL + (uint32_t)(k * 8), v + (uint64_t)(k * C::ROW), PV, 1);
         umma_commit(smem_u32(odone));
         umma_commit(smem_u32(vempty + s));
       }
@@ -346,8 +351,8 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
   } else if (warp < GROUP) {
     // ------------------------------------------------------------------------ K' and the state
     const int quarter = warp & 3, half = warp >> 2, r = quarter * 32 + lane;      // r: token of the chunk
-    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + C::S_COL;
-    // row of the state in this lane: a product of 64 rows leaves 16 to each quarter's first lanes
+    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
+    // value column of the state in this lane (its columns are the keys'): a product of 64 rows leaves 16 to each quarter's first lanes
     const int row = C::M == 128 ? r : quarter * 16 + (lane & 15);
     const bool has_row = (C::M == 128 || lane < 16) && row < D;
     constexpr int PIECES = D / 32;     // of 16 columns, from c0 on
@@ -379,10 +384,7 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
       for (int i = 0; i < PIECES; ++i) {
         uint32_t v[16];
 #pragma unroll
-        for (int x = 0; x < 16; x += 4) {
-          const float4 f = has_row ? *reinterpret_cast<const float4*>(from + row * D + c0 + 16 * i + x) : make_float4(0.f, 0.f, 0.f, 0.f);
-          v[x] = __float_as_uint(f.x); v[x + 1] = __float_as_uint(f.y); v[x + 2] = __float_as_uint(f.z); v[x + 3] = __float_as_uint(f.w);
-        }
+        for (int x = 0; x < 16; ++x) v[x] = has_row ? __float_as_uint(from[(c0 + 16 * i + x) * D + row]) : 0u;
         tmem_st16(lanes + (uint32_t)(c0 + 16 * i), v);
       }
       tmem_wait_st();
@@ -442,11 +444,9 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(kempty + s));
       if (WITH_OUT) {
-        if (c > 0) {
-          // the chunk before has left its state; its copy as an operand has been used
-          if (!wait(sdone + kp_place(c - 1), kp_turn(c - 1), 0x44) || !wait(ofirst, c - 1, 0x45)) break;
-          tc_fence_after();
-        }
+        // the chunk before has left the state
+        if (c > 0 && !wait(sdone + kp_place(c - 1), kp_turn(c - 1), 0x44)) break;
+        tc_fence_after();
         uint32_t v[PIECES][16];
         get_state(v);
         // first what the state's next product waits for
@@ -460,6 +460,7 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
         }
         tmem_wait_st();
         arrive(kready + kp_place(c));
+        if (c > 0 && !wait(ofirst, c - 1, 0x45)) break;      // the state's copy as an operand has been used
         put_state(v);
         arrive(sready);
       } else {
@@ -470,14 +471,23 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
       tc_fence_after();
       uint32_t v[PIECES][16];
       get_state(v);
+      if (C::SIDE) {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+          uint32_t y[2][16];
+#pragma unroll
+          for (int term = 0; term < 2; ++term) tmem_ld16_async(lanes + (uint32_t)((term + 1) * D + c0 + 16 * i), y[term]);
+          tmem_wait_ld();
+#pragma unroll
+          for (int x = 0; x < 16; ++x) v[i][x] = __float_as_uint(__uint_as_float(v[i][x]) + (__uint_as_float(y[0][x]) + __uint_as_float(y[1][x])));
+        }
+      }
       if ((!WITH_OUT || t1 == len) && has_row) {
         float* to = WITH_OUT ? p.state_out + at : seg_state;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i)
 #pragma unroll
-          for (int x = 0; x < 16; x += 4)
-            *reinterpret_cast<float4*>(to + row * D + c0 + 16 * i + x) =
-                make_float4(__uint_as_float(v[i][x]), __uint_as_float(v[i][x + 1]), __uint_as_float(v[i][x + 2]), __uint_as_float(v[i][x + 3]));
+          for (int x = 0; x < 16; ++x) to[(c0 + 16 * i + x) * D + row] = __uint_as_float(v[i][x]);
       }
     }
   }
