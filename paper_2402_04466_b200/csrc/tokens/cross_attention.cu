@@ -8,11 +8,14 @@
 //
 // A masked weight is kept as -0: it adds nothing to a finite value, and where a tile of V holds an infinity or NaN its sign
 // tells the slow loop to leave it out.
-#include "linear_common.cuh"
+#include "token_ptx.cuh"
+#include "tokens.h"
 
 namespace tt {
 namespace tok {
 namespace {
+
+typedef unsigned long long Two;        // two floats
 
 constexpr int THREADS = 256;           // 16 x 16
 constexpr int BN = 64;                 // keys of a tile
@@ -54,13 +57,14 @@ __global__ void __launch_bounds__(THREADS) cross_kernel(const __grid_constant__ 
     if (row0 + r < rows) f = *reinterpret_cast<const float4*>(q + (int64_t)((row0 + r) / p.group) * p.q.t + (row0 + r) % p.group * p.q.h + c);
     *reinterpret_cast<float4*>(qs + r * QP + c) = f;
   }
-  float m[A], l[A], o[A][E];
+  float m[A], l[A];
+  Two o[A][E / 2];                     // pairs of neighbouring columns
 #pragma unroll
   for (int a = 0; a < A; ++a) {
     m[a] = -INFINITY;
     l[a] = 0.f;
 #pragma unroll
-    for (int c = 0; c < E; ++c) o[a][c] = 0.f;
+    for (int c = 0; c < E / 2; ++c) o[a][c] = pack2(0.f, 0.f);
   }
   for (int j = j0; j < j1; j += BN) {
     __syncthreads();                   // the last tile's reads
@@ -77,18 +81,33 @@ __global__ void __launch_bounds__(THREADS) cross_kernel(const __grid_constant__ 
       *reinterpret_cast<float4*>(vs + r * D + c) = g;
     }
     const bool careful = __syncthreads_or(odd) && p.mask;
-    float s[A][N] = {};
-    for (int e = 0; e < D; e += 4) {
-      float4 x[A], y[N];
-#pragma unroll
-      for (int a = 0; a < A; ++a) x[a] = *reinterpret_cast<const float4*>(qs + (ty + 16 * a) * QP + e);
-#pragma unroll
-      for (int c = 0; c < N; ++c) y[c] = *reinterpret_cast<const float4*>(ks + (tx + 16 * c) * QP + e);
+    float s[A][N];
+    {
+      Two acc[A][N];                   // even and odd elements
 #pragma unroll
       for (int a = 0; a < A; ++a)
 #pragma unroll
-        for (int c = 0; c < N; ++c)
-          s[a][c] = fmaf(x[a].x, y[c].x, fmaf(x[a].y, y[c].y, fmaf(x[a].z, y[c].z, fmaf(x[a].w, y[c].w, s[a][c]))));
+        for (int c = 0; c < N; ++c) acc[a][c] = pack2(0.f, 0.f);
+#pragma unroll 4
+      for (int e = 0; e < D; e += 4) {
+        ulonglong2 x[A], y[N];
+#pragma unroll
+        for (int a = 0; a < A; ++a) x[a] = *reinterpret_cast<const ulonglong2*>(qs + (ty + 16 * a) * QP + e);
+#pragma unroll
+        for (int c = 0; c < N; ++c) y[c] = *reinterpret_cast<const ulonglong2*>(ks + (tx + 16 * c) * QP + e);
+#pragma unroll
+        for (int a = 0; a < A; ++a)
+#pragma unroll
+          for (int c = 0; c < N; ++c) acc[a][c] = fma2_of(x[a].y, y[c].y, fma2_of(x[a].x, y[c].x, acc[a][c]));
+      }
+#pragma unroll
+      for (int a = 0; a < A; ++a)
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+          float lo, hi;
+          unpack2(acc[a][c], lo, hi);
+          s[a][c] = lo + hi;
+        }
     }
 #pragma unroll
     for (int a = 0; a < A; ++a) {
@@ -116,29 +135,37 @@ __global__ void __launch_bounds__(THREADS) cross_kernel(const __grid_constant__ 
         ps[(ty + 16 * a) * PP + tx + 16 * c] = w;
       }
       l[a] = fmaf(l[a], fade, add);    // this thread's share of the keys
+      const Two f2 = pack2(fade, fade);
 #pragma unroll
-      for (int c = 0; c < E; ++c) o[a][c] *= fade;
+      for (int c = 0; c < E / 2; ++c) o[a][c] = mul2_of(o[a][c], f2);
     }
     __syncwarp();                      // a row's 16 threads are half a warp
-#pragma unroll 4
-    for (int i = 0; i < BN; ++i) {
-      float y[E];
-      if constexpr (D == 32) {
-        const float2 f = *reinterpret_cast<const float2*>(vs + i * D + 2 * tx);
-        y[0] = f.x; y[1] = f.y;
-      } else {
+#pragma unroll 2
+    for (int i = 0; i < BN; i += 4) {  // four keys: a row's weights in one load
+      float4 w[A];
 #pragma unroll
-        for (int c = 0; c < D / 64; ++c) {
-          const float4 f = *reinterpret_cast<const float4*>(vs + i * D + 4 * tx + 64 * c);
-          y[4 * c] = f.x; y[4 * c + 1] = f.y; y[4 * c + 2] = f.z; y[4 * c + 3] = f.w;
+      for (int a = 0; a < A; ++a) w[a] = *reinterpret_cast<const float4*>(ps + (ty + 16 * a) * PP + i);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        Two y[E / 2];
+        if constexpr (D == 32) {
+          y[0] = *reinterpret_cast<const Two*>(vs + (i + k) * D + 2 * tx);
+        } else {
+#pragma unroll
+          for (int c = 0; c < D / 64; ++c) {
+            const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(vs + (i + k) * D + 4 * tx + 64 * c);
+            y[2 * c] = f.x; y[2 * c + 1] = f.y;
+          }
         }
-      }
 #pragma unroll
-      for (int a = 0; a < A; ++a) {
-        const float w = ps[(ty + 16 * a) * PP + i];
-        if (!careful || !signbit(w))
+        for (int a = 0; a < A; ++a) {
+          const float x = k == 0 ? w[a].x : k == 1 ? w[a].y : k == 2 ? w[a].z : w[a].w;
+          if (!careful || !signbit(x)) {
+            const Two x2 = pack2(x, x);
 #pragma unroll
-          for (int c = 0; c < E; ++c) o[a][c] = fmaf(w, y[c], o[a][c]);
+            for (int c = 0; c < E / 2; ++c) o[a][c] = fma2_of(x2, y[c], o[a][c]);
+          }
+        }
       }
     }
   }
@@ -148,17 +175,14 @@ __global__ void __launch_bounds__(THREADS) cross_kernel(const __grid_constant__ 
     for (int x = 8; x > 0; x >>= 1) l[a] += __shfl_xor_sync(0xFFFFFFFFu, l[a], x);
     const int row = row0 + ty + 16 * a;
     if (row >= rows) continue;
-    if (p.splits > 1) {
-      const Part to = part_of(p, D, b, hk, row);
-      if (tx == 0) to.stat[split] = make_float2(m[a], l[a]);
+    const float inv = p.splits > 1 ? 1.f : l[a] == 0.f ? 0.f : 1.f / l[a];
+    const Part to = part_of(p, D, b, hk, row);
+    if (p.splits > 1 && tx == 0) to.stat[split] = make_float2(m[a], l[a]);
+    float* dst = p.splits > 1 ? to.sum + (int64_t)split * D
+                              : reinterpret_cast<float*>(p.o.p) + b * p.o.b + (int64_t)(row / p.group) * p.o.t + ((int64_t)hk * p.group + row % p.group) * p.o.h;
+    const Two i2 = pack2(inv, inv);
 #pragma unroll
-      for (int c = 0; c < E; ++c) to.sum[(int64_t)split * D + (D == 32 ? 2 * tx + c : 4 * tx + (c & 3) + (c >> 2) * 64)] = o[a][c];
-    } else {
-      const float inv = l[a] == 0.f ? 0.f : 1.f / l[a];
-      float* dst = reinterpret_cast<float*>(p.o.p) + b * p.o.b + (int64_t)(row / p.group) * p.o.t + ((int64_t)hk * p.group + row % p.group) * p.o.h;
-#pragma unroll
-      for (int c = 0; c < E; ++c) dst[D == 32 ? 2 * tx + c : 4 * tx + (c & 3) + (c >> 2) * 64] = o[a][c] * inv;
-    }
+    for (int c = 0; c < E / 2; ++c) *reinterpret_cast<Two*>(dst + (D == 32 ? 2 * tx : 4 * tx + (c & 1) * 2 + (c >> 1) * 64)) = mul2_of(o[a][c], i2);
   }
 }
 

@@ -8,10 +8,13 @@
 // segments: linear_segment_kernel forms what each segment adds to the state, linear_scan_kernel turns that into the state
 // before each segment, and linear_chunk_kernel then runs all segments at once.  K and V are read twice then.
 #include "linear_common.cuh"
+#include "token_ptx.cuh"
 
 namespace tt {
 namespace tok {
 namespace {
+
+typedef unsigned long long Two;        // two floats
 
 constexpr int THREADS = 256;           // 16 x 16
 
@@ -39,6 +42,41 @@ __device__ __forceinline__ void load_columns(const float* row, int tx, float (&f
     for (int j = 0; j < D / 64; ++j) {
       const float4 v = *reinterpret_cast<const float4*>(row + 4 * tx + 64 * j);
       f[4 * j] = v.x; f[4 * j + 1] = v.y; f[4 * j + 2] = v.z; f[4 * j + 3] = v.w;
+    }
+  }
+}
+
+template <int D>
+__device__ __forceinline__ void load_pairs(const float* row, int tx, Two (&f)[D / 32]) {
+  if constexpr (D == 32) {
+    f[0] = *reinterpret_cast<const Two*>(row + 2 * tx);
+  } else {
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) {
+      const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(row + 4 * tx + 64 * j);
+      f[2 * j] = v.x; f[2 * j + 1] = v.y;
+    }
+  }
+}
+// o += x y for rows ty + 16 a of x and this thread's columns of y; `n` inner steps, four at a time: a row's factors in one load
+template <int D, int A>
+__device__ __forceinline__ void multiply(Two (&o)[A][D / 32], const float* x, int pitch, const float* y, int n, int ty, int tx) {
+#pragma unroll 2
+  for (int e = 0; e < n; e += 4) {
+    float4 f[A];
+#pragma unroll
+    for (int a = 0; a < A; ++a) f[a] = *reinterpret_cast<const float4*>(x + (ty + 16 * a) * pitch + e);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      Two g[D / 32];
+      load_pairs<D>(y + (e + k) * D, tx, g);
+#pragma unroll
+      for (int a = 0; a < A; ++a) {
+        const float w = k == 0 ? f[a].x : k == 1 ? f[a].y : k == 2 ? f[a].z : f[a].w;
+        const Two w2 = pack2(w, w);
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) o[a][c] = fma2_of(w2, g[c], o[a][c]);
+      }
     }
   }
 }
@@ -77,79 +115,87 @@ __device__ __forceinline__ void run_chunks(const LinearParams& p, int b, int h, 
     fetch<D>(v, D, gv + t * p.v.t, p.v.t, m, C);
     __syncthreads();
     if (WITH_OUT) {
-      float acc[A][A] = {};
+      Two acc[A][A];                   // even and odd elements
+#pragma unroll
+      for (int a = 0; a < A; ++a)
+#pragma unroll
+        for (int c = 0; c < A; ++c) acc[a][c] = pack2(0.f, 0.f);
+#pragma unroll 4
       for (int e = 0; e < D; e += 4) {
-        float4 x[A], y[A];
+        ulonglong2 x[A], y[A];
 #pragma unroll
         for (int a = 0; a < A; ++a) {
-          x[a] = *reinterpret_cast<const float4*>(q + (ty + 16 * a) * QP + e);
-          y[a] = *reinterpret_cast<const float4*>(k + (tx + 16 * a) * QP + e);
+          x[a] = *reinterpret_cast<const ulonglong2*>(q + (ty + 16 * a) * QP + e);
+          y[a] = *reinterpret_cast<const ulonglong2*>(k + (tx + 16 * a) * QP + e);
         }
 #pragma unroll
         for (int a = 0; a < A; ++a)
 #pragma unroll
-          for (int c = 0; c < A; ++c)
-            acc[a][c] = fmaf(x[a].x, y[c].x, fmaf(x[a].y, y[c].y, fmaf(x[a].z, y[c].z, fmaf(x[a].w, y[c].w, acc[a][c]))));
+          for (int c = 0; c < A; ++c) acc[a][c] = fma2_of(x[a].y, y[c].y, fma2_of(x[a].x, y[c].x, acc[a][c]));
       }
 #pragma unroll
       for (int a = 0; a < A; ++a)
 #pragma unroll
         for (int c = 0; c < A; ++c) {
           const int i = ty + 16 * a, j = tx + 16 * c;
-          P[i * PP + j] = i >= j ? acc[a][c] * pw[i - j] : 0.f;
+          float lo, hi;
+          unpack2(acc[a][c], lo, hi);
+          P[i * PP + j] = i >= j ? (lo + hi) * pw[i - j] : 0.f;
         }
-      float inter[A][E] = {}, o[A][E] = {};
-      for (int e = 0; e < D; ++e) {
-        float s[E];
-        load_columns<D>(S + e * D, tx, s);
+      Two o[A][E / 2];                 // pairs of neighbouring columns
 #pragma unroll
-        for (int a = 0; a < A; ++a) {
-          const float x = q[(ty + 16 * a) * QP + e];
+      for (int a = 0; a < A; ++a)
 #pragma unroll
-          for (int c = 0; c < E; ++c) inter[a][c] = fmaf(x, s[c], inter[a][c]);
-        }
+        for (int c = 0; c < E / 2; ++c) o[a][c] = pack2(0.f, 0.f);
+      multiply<D, A>(o, q, QP, S, D, ty, tx);
+#pragma unroll
+      for (int a = 0; a < A; ++a) {
+        const float f = pw[ty + 16 * a + 1];
+        const Two f2 = pack2(f, f);
+#pragma unroll
+        for (int c = 0; c < E / 2; ++c) o[a][c] = mul2_of(o[a][c], f2);
       }
       __syncthreads();                 // P
-      for (int j = 0; j < m; ++j) {
-        float s[E];
-        load_columns<D>(v + j * D, tx, s);
-#pragma unroll
-        for (int a = 0; a < A; ++a) {
-          const float x = P[(ty + 16 * a) * PP + j];
-#pragma unroll
-          for (int c = 0; c < E; ++c) o[a][c] = fmaf(x, s[c], o[a][c]);
-        }
-      }
+      multiply<D, A>(o, P, PP, v, (m + 3) & ~3, ty, tx);
 #pragma unroll
       for (int a = 0; a < A; ++a) {
         const int i = ty + 16 * a;
         if (i < m) {
           float* dst = go + (int64_t)(t + i) * p.o.t;
+          const Two s2 = pack2(p.scale, p.scale);
 #pragma unroll
-          for (int c = 0; c < E; ++c) dst[column<D>(tx, c)] = p.scale * fmaf(pw[i + 1], inter[a][c], o[a][c]);
+          for (int c = 0; c < E / 2; ++c) *reinterpret_cast<Two*>(dst + column<D>(tx, 2 * c)) = mul2_of(o[a][c], s2);
         }
       }
     }
     // own rows and columns of the state: read by the block above, written here behind a barrier
-    float s[E][E] = {};
-    for (int j = 0; j < m; ++j) {
-      float x[E], y[E];
-      load_columns<D>(v + j * D, tx, y);
-      const float d = pw[m - 1 - j];
-#pragma unroll
-      for (int a = 0; a < E; ++a) x[a] = k[j * QP + ty + 16 * a] * d;
-#pragma unroll
-      for (int a = 0; a < E; ++a)
-#pragma unroll
-        for (int c = 0; c < E; ++c) s[a][c] = fmaf(x[a], y[c], s[a][c]);
-    }
-    __syncthreads();
+    Two s[E][E / 2];
 #pragma unroll
     for (int a = 0; a < E; ++a)
 #pragma unroll
-      for (int c = 0; c < E; ++c) {
-        float& at = S[(ty + 16 * a) * D + column<D>(tx, c)];
-        at = fmaf(pw[m], at, s[a][c]);
+      for (int c = 0; c < E / 2; ++c) s[a][c] = pack2(0.f, 0.f);
+#pragma unroll 2
+    for (int j = 0; j < m; ++j) {
+      float x[E];
+      Two y[E / 2];
+      load_columns<D>(k + j * QP, ty, x);
+      load_pairs<D>(v + j * D, tx, y);
+      const float d = pw[m - 1 - j];
+#pragma unroll
+      for (int a = 0; a < E; ++a) {
+        const Two x2 = pack2(x[a] * d, x[a] * d);
+#pragma unroll
+        for (int c = 0; c < E / 2; ++c) s[a][c] = fma2_of(x2, y[c], s[a][c]);
+      }
+    }
+    __syncthreads();
+    const Two d2 = pack2(pw[m], pw[m]);
+#pragma unroll
+    for (int a = 0; a < E; ++a)
+#pragma unroll
+      for (int c = 0; c < E / 2; ++c) {
+        Two* at = reinterpret_cast<Two*>(S + column<D>(ty, a) * D + column<D>(tx, 2 * c));
+        *at = fma2_of(d2, *at, s[a][c]);
       }
   }
   __syncthreads();

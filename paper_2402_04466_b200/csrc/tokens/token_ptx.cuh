@@ -2,6 +2,8 @@
 // to an optional status word.
 #pragma once
 
+#include "tokens.h"
+
 #include "../tc_ptx.cuh"
 
 namespace tt {
