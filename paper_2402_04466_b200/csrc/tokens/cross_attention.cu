@@ -29,6 +29,19 @@ struct Shape {
   static constexpr size_t smem = sizeof(float) * (BM * QP + BN * QP + BN * D + BM * PP);
 };
 
+// this thread's columns of a row, as pairs: four neighbours at 4 tx (and 64 + 4 tx), two at 2 tx where D is 32
+template <int D>
+__device__ __forceinline__ void load_pairs(const float* row, int tx, Two (&f)[D / 32]) {
+  if constexpr (D == 32) {
+    f[0] = *reinterpret_cast<const Two*>(row + 2 * tx);
+  } else {
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) {
+      const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(row + 4 * tx + 64 * j);
+      f[2 * j] = v.x; f[2 * j + 1] = v.y;
+    }
+  }
+}
 __device__ __forceinline__ bool all_finite(float4 f) {
   return isfinite(f.x) && isfinite(f.y) && isfinite(f.z) && isfinite(f.w);
 }
@@ -76,7 +89,7 @@ __global__ void __launch_bounds__(THREADS) cross_kernel(const __grid_constant__ 
         f = *reinterpret_cast<const float4*>(k + (int64_t)(j + r) * p.k.t + c);
         g = *reinterpret_cast<const float4*>(v + (int64_t)(j + r) * p.v.t + c);
       }
-      odd |= !all_finite(g);
+      if (p.mask) odd |= !all_finite(g);
       *reinterpret_cast<float4*>(ks + r * QP + c) = f;
       *reinterpret_cast<float4*>(vs + r * D + c) = g;
     }
@@ -109,28 +122,35 @@ __global__ void __launch_bounds__(THREADS) cross_kernel(const __grid_constant__ 
           s[a][c] = lo + hi;
         }
     }
+    const bool whole = !p.mask && j + BN <= j1;      // every key of the tile is seen by every row
 #pragma unroll
     for (int a = 0; a < A; ++a) {
-      const int row = row0 + ty + 16 * a;
-      const uint8_t* mask = p.mask && row < rows ? p.mask + b * p.mask_b + (int64_t)(row / p.group) * p.mask_q + j : nullptr;
       bool seen[N];
-      float top = -INFINITY;
 #pragma unroll
-      for (int c = 0; c < N; ++c) {
-        const int at = tx + 16 * c;
-        seen[c] = j + at < j1 && (!mask || mask[at]);
-        s[a][c] *= p.scale_log2;
-        if (seen[c]) top = fmaxf(top, s[a][c]);
+      for (int c = 0; c < N; ++c) seen[c] = true;
+      if (!whole) {
+        const int row = row0 + ty + 16 * a;
+        const uint8_t* mask = p.mask && row < rows ? p.mask + b * p.mask_b + (int64_t)(row / p.group) * p.mask_q + j : nullptr;
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+          const int at = tx + 16 * c;
+          seen[c] = j + at < j1 && (!mask || mask[at]);
+          if (!seen[c]) s[a][c] = -INFINITY;
+        }
       }
+      float top = s[a][0];
+#pragma unroll
+      for (int c = 1; c < N; ++c) top = fmaxf(top, s[a][c]);
 #pragma unroll
       for (int x = 8; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
+      top *= p.scale_log2;
       const float now = fmaxf(m[a], top), base = now == -INFINITY ? 0.f : now;
       const float fade = exp2f(m[a] - base);
       m[a] = now;
       float add = 0.f;
 #pragma unroll
       for (int c = 0; c < N; ++c) {
-        const float w = seen[c] ? exp2f(s[a][c] - base) : -0.f;
+        const float w = seen[c] ? exp2f(fmaf(s[a][c], p.scale_log2, -base)) : -0.f;
         add += w;
         ps[(ty + 16 * a) * PP + tx + 16 * c] = w;
       }
@@ -140,31 +160,36 @@ __global__ void __launch_bounds__(THREADS) cross_kernel(const __grid_constant__ 
       for (int c = 0; c < E / 2; ++c) o[a][c] = mul2_of(o[a][c], f2);
     }
     __syncwarp();                      // a row's 16 threads are half a warp
+    if (!careful) {
 #pragma unroll 2
-    for (int i = 0; i < BN; i += 4) {  // four keys: a row's weights in one load
-      float4 w[A];
+      for (int i = 0; i < BN; i += 4) {  // four keys: a row's weights in one load
+        float4 w[A];
 #pragma unroll
-      for (int a = 0; a < A; ++a) w[a] = *reinterpret_cast<const float4*>(ps + (ty + 16 * a) * PP + i);
+        for (int a = 0; a < A; ++a) w[a] = *reinterpret_cast<const float4*>(ps + (ty + 16 * a) * PP + i);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        Two y[E / 2];
-        if constexpr (D == 32) {
-          y[0] = *reinterpret_cast<const Two*>(vs + (i + k) * D + 2 * tx);
-        } else {
+        for (int k = 0; k < 4; ++k) {
+          Two y[E / 2];
+          load_pairs<D>(vs + (i + k) * D, tx, y);
 #pragma unroll
-          for (int c = 0; c < D / 64; ++c) {
-            const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(vs + (i + k) * D + 4 * tx + 64 * c);
-            y[2 * c] = f.x; y[2 * c + 1] = f.y;
-          }
-        }
-#pragma unroll
-        for (int a = 0; a < A; ++a) {
-          const float x = k == 0 ? w[a].x : k == 1 ? w[a].y : k == 2 ? w[a].z : w[a].w;
-          if (!careful || !signbit(x)) {
+          for (int a = 0; a < A; ++a) {
+            const float x = k == 0 ? w[a].x : k == 1 ? w[a].y : k == 2 ? w[a].z : w[a].w;
             const Two x2 = pack2(x, x);
 #pragma unroll
             for (int c = 0; c < E / 2; ++c) o[a][c] = fma2_of(x2, y[c], o[a][c]);
           }
+        }
+      }
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < BN; ++i) {
+        Two y[E / 2];
+        load_pairs<D>(vs + i * D, tx, y);
+#pragma unroll
+        for (int a = 0; a < A; ++a) {
+          const float x = ps[(ty + 16 * a) * PP + i];
+          if (!signbit(x))
+#pragma unroll
+            for (int c = 0; c < E / 2; ++c) o[a][c] = fma2_of(pack2(x, x), y[c], o[a][c]);
         }
       }
     }
