@@ -44,6 +44,7 @@ struct Cfg {
   // between the two, or the copies into shared memory would be too many.
   static constexpr int TILES = D == 128 ? 2 : 1, BLOCKS = D == 128 ? 1 : 2, BN = D == 128 ? 64 : 128;
   static constexpr int HALVES = BN / 64;                            // weights are handed over 64 keys at a time
+  static constexpr int PLACES = D == 128 ? 2 : 1;                   // of a tile's weights: those of one tile of keys are made while the last ones' product runs
   static constexpr int ROWS = TILES * BM;
   static constexpr int ROW = D == 32 ? 64 : 128;                    // bytes of a row in a slab
   static constexpr int SLABS = D == 128 ? 2 : 1;
@@ -52,9 +53,9 @@ struct Cfg {
   static constexpr uint32_t LAYOUT = D == 32 ? 4u : 2u;             // 64- or 128-byte swizzle
   static constexpr int STAGES = D == 128 ? 4 : 2;
   static constexpr int THREADS = TILES * (128 + 64);
-  static constexpr uint32_t P_COL = TILES * BN, O_COL = P_COL + TILES * BN / 2, TMEM = D == 128 ? 512 : 256;
-  static constexpr int SMEM = TILES * Q_BYTES + 2 * STAGES * KV_BYTES + 256 + 1024;
-  static constexpr int64_t PLACE = (int64_t)ROWS * (D + 2);         // floats of a partial result
+  static constexpr uint32_t P_COL = TILES * BN, O_COL = P_COL + TILES * PLACES * BN / 2, TMEM = D == 128 ? 512 : 256;
+  static constexpr int SMEM = TILES * Q_BYTES + 2 * STAGES * KV_BYTES + 512 + 1024;
+  static constexpr int64_t PART = (int64_t)ROWS * (D + 2);          // floats of a partial result
   static_assert(O_COL + TILES * D <= TMEM && TMEM * BLOCKS <= 512 && (SMEM + 6 * 1024) * BLOCKS <= 227 * 1024, "tensor and shared memory");
 };
 
@@ -141,9 +142,9 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::BLOCKS) cross_tc_kern
   uint64_t* vempty = vfull + STAGES;           // [STAGES]
   uint64_t* sfull = vempty + STAGES;           // [TILES] scores are there, and the keys have been read
   uint64_t* sread = sfull + TILES;             // [TILES] scores are in registers
-  uint64_t* pfull = sread + TILES;             // [TILES][HALVES] weights are there, 64 keys each
-  uint64_t* pdone = pfull + C::HALVES * TILES; // [TILES] their product is done, and the values have been read
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(pdone + TILES);
+  uint64_t* pfull = sread + TILES;             // [TILES][PLACES][HALVES] weights are there, 64 keys each
+  uint64_t* pdone = pfull + C::HALVES * C::PLACES * TILES;      // [TILES][PLACES] their product is done, and the values have been read
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(pdone + C::PLACES * TILES);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* s_status = reinterpret_cast<int*>(tmem_slot + 2);
 
@@ -160,8 +161,8 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::BLOCKS) cross_tc_kern
     for (int t = 0; t < TILES; ++t) {
       mbar_init(smem_u32(sfull + t), 1);
       mbar_init(smem_u32(sread + t), 4);
-      for (int x = 0; x < C::HALVES; ++x) mbar_init(smem_u32(pfull + C::HALVES * t + x), 4);
-      mbar_init(smem_u32(pdone + t), 1);
+      for (int x = 0; x < C::HALVES * C::PLACES; ++x) mbar_init(smem_u32(pfull + C::HALVES * C::PLACES * t + x), 4);
+      for (int x = 0; x < C::PLACES; ++x) mbar_init(smem_u32(pdone + C::PLACES * t + x), 1);
     }
     *abort_flag = 0;
     *s_status = 0;
@@ -180,6 +181,9 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::BLOCKS) cross_tc_kern
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
 
+  // the it-th weights of tile t: their place among all, and how often that has been used before
+  auto at_place = [](int t, uint32_t it) { return t * C::PLACES + (int)(it & (C::PLACES - 1)); };
+  auto turn = [](uint32_t it) { return C::PLACES == 2 ? it >> 1 : it; };
   bool ok = true;
   auto wait_all = [&](uint64_t* bar, uint32_t phase, int code) {      // a whole warp: its lanes go on or stop together
     if (__builtin_expect(__all_sync(0xffffffffu, mbar_test(smem_u32(bar), phase & 1u)), 1)) return true;
@@ -197,7 +201,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::BLOCKS) cross_tc_kern
     const bool issuer = elect_one();
     const int role = warp - TILES * 4, t = role >> 1;
     const bool keys = (role & 1) == 0, loads = t == 0;
-    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), scores = tm + (uint32_t)(t * C::BN), weights = tm + C::P_COL + (uint32_t)(t * (C::BN / 2)),
+    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), scores = tm + (uint32_t)(t * C::BN), weights = tm + C::P_COL + (uint32_t)(t * C::PLACES * (C::BN / 2)),
                    sums = tm + C::O_COL + (uint32_t)(t * D);
     auto arrived = [&](uint64_t* bar, uint32_t parity, int code) {
       if (__all_sync(0xffffffffu, mbar_test(smem_u32(bar), parity & 1u))) return;
@@ -306,21 +310,21 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::BLOCKS) cross_tc_kern
           const uint64_t vd = v0 + (uint64_t)stage * (C::KV_BYTES >> 4);
 #pragma unroll
           for (int x = 0; x < C::HALVES; ++x) {
-            arrived(pfull + C::HALVES * t + x, it, 0x40 + C::HALVES * t + x);
+            arrived(pfull + C::HALVES * at_place(t, it) + x, turn(it), 0x40 + C::HALVES * t + x);
             tc_fence_after();
             if (issuer) {
 #pragma unroll
               for (int k = 4 * x; k < 4 * x + 4; ++k)
-                umma_bf16_ts(sums, weights + (uint32_t)(k * 8), vd + (uint64_t)(k * C::ROW), PV, k > 0 ? 1u : j > 0 ? 1u : 0u);
+                umma_bf16_ts(sums, weights + (uint32_t)((it & (C::PLACES - 1)) * (C::BN / 2) + k * 8), vd + (uint64_t)(k * C::ROW), PV, k > 0 ? 1u : j > 0 ? 1u : 0u);
             }
           }
           if (issuer) {
-            umma_commit(smem_u32(pdone + t));
+            umma_commit(smem_u32(pdone + at_place(t, it)));
             if (TILES > 1) umma_commit(smem_u32(vempty + stage));
           }
           if (loads) {
             if (TILES > 1) arrived(vempty + stage, phase, 0x18 + (int)stage);
-            else arrived(pdone, it, 0x60);
+            else arrived(pdone, it, 0x60);      // (one place)
             load_next(stage);
           }
           if (++stage == STAGES) { stage = 0; phase ^= 1u; }
@@ -333,7 +337,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::BLOCKS) cross_tc_kern
     // ------------------------------------------------------------------------------ weights
     const int t = warp >> 2, quarter = warp & 3, r = t * BM + quarter * 32 + lane;      // row of the block's tile
     const uint32_t s_addr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(t * C::BN);
-    const uint32_t p_addr = tmem + ((uint32_t)(quarter * 32) << 16) + C::P_COL + (uint32_t)(t * (C::BN / 2));
+    const uint32_t p_addr = tmem + ((uint32_t)(quarter * 32) << 16) + C::P_COL + (uint32_t)(t * C::PLACES * (C::BN / 2));
     const uint32_t o_addr = tmem + ((uint32_t)(quarter * 32) << 16) + C::O_COL + (uint32_t)(t * D);
     const float c = p.scale_log2;
     const unsigned long long c2 = pack2(c, c);
@@ -369,12 +373,14 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::BLOCKS) cross_tc_kern
       }
       float now = max3(top[0], top[0], top[1]);
       if constexpr (C::BN == 128) now = max3(now, top[2], top[3]);
-      // the product before must be done: its weights make room, and the sums may be rescaled
-      if (it > 0 && !wait_all(pdone + t, it - 1, 0x58 + t)) break;
+      // the product of the weights that lay here must be done
+      if (it >= C::PLACES && !wait_all(pdone + at_place(t, it), turn(it) - 1, 0x58 + t)) break;
       // the maximum only moves when a weight would pass 2^8: until then the sums keep their scale, which loses nothing in fp32
       const bool moved = (now - m) * c > 8.f;
       if (__builtin_expect(__any_sync(0xffffffffu, moved), 0)) {
         if (j > 0) {
+          // the sums are rescaled: the last product must be done as well
+          if (C::PLACES > 1 && !wait_all(pdone + at_place(t, it - 1), turn(it - 1), 0x5C + t)) break;
           tc_fence_after();
           const float fade = moved ? exp2_fast((m - now) * c) : 1.f;
           const unsigned long long f2 = pack2(fade, fade);
@@ -406,17 +412,17 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::BLOCKS) cross_tc_kern
           l[x & 3] = add2_of(l[x & 3], pack2(lo, hi));
           w[x] = pack_bf16(lo, hi);
         }
-        tmem_st16(p_addr + 16 * i, w);
+        tmem_st16(p_addr + (uint32_t)((it & (C::PLACES - 1)) * (C::BN / 2) + 16 * i), w);
         if (i & 1) {
           tmem_wait_st();
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(pfull + C::HALVES * t + (i >> 1)));
+          if (lane == 0) mbar_arrive(smem_u32(pfull + C::HALVES * at_place(t, it) + (i >> 1)));
         }
       }
       }
       // the run's end
-      if (!ok || !wait_all(pdone + t, it - 1, 0x60 + t)) break;
+      if (!ok || !wait_all(pdone + at_place(t, it - 1), turn(it - 1), 0x60 + t)) break;
       tc_fence_after();
       float a0, a1;
       unpack2(add2_of(add2_of(l[0], l[1]), add2_of(l[2], l[3])), a0, a1);
@@ -438,7 +444,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::BLOCKS) cross_tc_kern
           }
         }
       } else {
-        float* place = p.part + ((int64_t)blockIdx.x * 2 + (cur.j0 == 0)) * C::PLACE;
+        float* place = p.part + ((int64_t)blockIdx.x * 2 + (cur.j0 == 0)) * C::PART;
         reinterpret_cast<float2*>(place)[r] = make_float2(m * c, total);
         float* dst = place + 2 * C::ROWS + r * D;
 #pragma unroll
@@ -484,7 +490,7 @@ __global__ void __launch_bounds__(256) cross_tc_join_kernel(const __grid_constan
   const int64_t each = share_of<D>(work, p), from = cur.at - cur.j0, first = from / each;
   if (first + 1 != blockIdx.x) return;
   const int64_t last = (from + cur.n - 1) / each;
-  const float* before = p.part + (first * 2 + 1) * C::PLACE;
+  const float* before = p.part + (first * 2 + 1) * C::PART;
   constexpr int LANES = D / 4;
   for (int r = threadIdx.x / LANES + (int)blockIdx.y * (256 / LANES); r < C::ROWS && cur.row0 + r < work.rows[cur.b]; r += 256 / LANES * (int)gridDim.y) {
     const int d = threadIdx.x % LANES * 4;
@@ -492,7 +498,7 @@ __global__ void __launch_bounds__(256) cross_tc_join_kernel(const __grid_constan
     float m = st.x, l = st.y;
     float4 o = *reinterpret_cast<const float4*>(before + 2 * C::ROWS + r * D + d);
     for (int64_t i = first + 1; i <= last; ++i) {
-      const float* place = p.part + i * 2 * C::PLACE;
+      const float* place = p.part + i * 2 * C::PART;
       st = reinterpret_cast<const float2*>(place)[r];
       const float4 x = *reinterpret_cast<const float4*>(place + 2 * C::ROWS + r * D + d);
       const float now = fmaxf(m, st.x), base = now == -INFINITY ? 0.f : now;
@@ -556,9 +562,9 @@ bool token_map(TensorMap128* map, const View& v, int D, int tokens, int heads, i
 }
 uint64_t cross_tc_scratch(int batch, int q_tokens, int kv_tokens, int heads, int D) {
   const int entries = batch < MAX_ENTRIES ? batch : MAX_ENTRIES;
-  const int64_t floats = D == 32   ? grid_of<32>(entries, q_tokens, kv_tokens, heads) * Cfg<32>::PLACE
-                         : D == 64 ? grid_of<64>(entries, q_tokens, kv_tokens, heads) * Cfg<64>::PLACE
-                                   : grid_of<128>(entries, q_tokens, kv_tokens, heads) * Cfg<128>::PLACE;
+  const int64_t floats = D == 32   ? grid_of<32>(entries, q_tokens, kv_tokens, heads) * Cfg<32>::PART
+                         : D == 64 ? grid_of<64>(entries, q_tokens, kv_tokens, heads) * Cfg<64>::PART
+                                   : grid_of<128>(entries, q_tokens, kv_tokens, heads) * Cfg<128>::PART;
   return (uint64_t)floats * 2u * 4u;
 }
 
