@@ -39,10 +39,12 @@ struct CrossTcParams {
 
 template <int D>
 struct Cfg {
-  // Tiles of queries of a block, blocks of a multiprocessor and keys of a tile: two tiles of queries to a multiprocessor either way, each
-  // with columns of tensor memory of its own for scores (BN), weights (BN / 2) and sums (D).  Heads of 128 share their keys
-  // between the two, or the copies into shared memory would be too many.
-  static constexpr int TILES = D == 128 ? 2 : 1, BLOCKS = D == 128 ? 1 : 2, BN = D == 128 ? 64 : 128;
+  // Two tiles of queries to a block, one block to a multiprocessor; each tile has columns of tensor memory of its own for scores (BN),
+  // weights (BN / 2) and sums (D).
+  static constexpr int TILES = 2, BN = D == 128 ? 64 : 128;
+  // With heads of up to 64 the special-function units are what there is least of: the two tiles' warps of a quarter, which share one, take
+  // turns at their exponentials, and one does the rest of its work meanwhile.
+  static constexpr bool TURNS = D != 128;
   static constexpr int HALVES = BN / 64;                            // weights are handed over 64 keys at a time
   static constexpr int PLACES = D == 128 ? 2 : 1;                   // of a tile's weights: those of one tile of keys are made while the last ones' product runs
   static constexpr int ROWS = TILES * BM;
@@ -51,12 +53,12 @@ struct Cfg {
   static constexpr int Q_SLAB = BM * ROW, KV_SLAB = BN * ROW;
   static constexpr int Q_BYTES = SLABS * Q_SLAB, KV_BYTES = SLABS * KV_SLAB;
   static constexpr uint32_t LAYOUT = D == 32 ? 4u : 2u;             // 64- or 128-byte swizzle
-  static constexpr int STAGES = D == 128 ? 4 : 2;
+  static constexpr int STAGES = 4;
   static constexpr int THREADS = TILES * (128 + 64);
-  static constexpr uint32_t P_COL = TILES * BN, O_COL = P_COL + TILES * PLACES * BN / 2, TMEM = D == 128 ? 512 : 256;
+  static constexpr uint32_t P_COL = TILES * BN, O_COL = P_COL + TILES * PLACES * BN / 2, TMEM = 512;
   static constexpr int SMEM = TILES * Q_BYTES + 2 * STAGES * KV_BYTES + 512 + 1024;
   static constexpr int64_t PART = (int64_t)ROWS * (D + 2);          // floats of a partial result
-  static_assert(O_COL + TILES * D <= TMEM && TMEM * BLOCKS <= 512 && (SMEM + 6 * 1024) * BLOCKS <= 227 * 1024, "tensor and shared memory");
+  static_assert(O_COL + TILES * D <= TMEM && SMEM + 6 * 1024 <= 227 * 1024, "tensor and shared memory");
 };
 
 // The launch's work: iterations (tile of queries x tile of keys) in the order entry, head, tile of queries, tile of keys.
@@ -126,7 +128,7 @@ struct Cursor {
 };
 
 template <int D>
-__global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::BLOCKS) cross_tc_kernel(const __grid_constant__ CrossTcParams p) {
+__global__ void __launch_bounds__(Cfg<D>::THREADS, 1) cross_tc_kernel(const __grid_constant__ CrossTcParams p) {
   using C = Cfg<D>;
   constexpr int STAGES = C::STAGES, TILES = C::TILES;
   extern __shared__ uint8_t smem_raw[];
@@ -144,7 +146,8 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::BLOCKS) cross_tc_kern
   uint64_t* sread = sfull + TILES;             // [TILES] scores are in registers
   uint64_t* pfull = sread + TILES;             // [TILES][PLACES][HALVES] weights are there, 64 keys each
   uint64_t* pdone = pfull + C::HALVES * C::PLACES * TILES;      // [TILES][PLACES] their product is done, and the values have been read
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(pdone + C::PLACES * TILES);
+  uint64_t* turns = pdone + C::PLACES * TILES;      // [4][2] a quarter's turn at the exponentials: the other tile's warp has had its own
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(turns + 8);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* s_status = reinterpret_cast<int*>(tmem_slot + 2);
 
@@ -164,6 +167,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::BLOCKS) cross_tc_kern
       for (int x = 0; x < C::HALVES * C::PLACES; ++x) mbar_init(smem_u32(pfull + C::HALVES * C::PLACES * t + x), 4);
       for (int x = 0; x < C::PLACES; ++x) mbar_init(smem_u32(pdone + C::PLACES * t + x), 1);
     }
+    for (int x = 0; x < 8; ++x) mbar_init(smem_u32(turns + x), 1);
     *abort_flag = 0;
     *s_status = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -397,6 +401,8 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::BLOCKS) cross_tc_kern
         }
         if (moved) m = now;
       }
+      // the first tile begins, then they alternate: both go through the same iterations
+      if (C::TURNS && (t == 1 || it > 0) && !wait_all(turns + 2 * quarter + t, t == 1 ? it : it - 1, 0x64 + t)) break;
       const float mc = m == -INFINITY ? 0.f : -m * c;
       const unsigned long long mc2 = pack2(mc, mc);
 #pragma unroll
@@ -412,6 +418,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::BLOCKS) cross_tc_kern
           l[x & 3] = add2_of(l[x & 3], pack2(lo, hi));
           w[x] = pack_bf16(lo, hi);
         }
+        if (C::TURNS && i == C::BN / 32 - 2 && lane == 0) mbar_arrive(smem_u32(turns + 2 * quarter + 1 - t));      // the other's wait takes about as long as the rest
         tmem_st16(p_addr + (uint32_t)((it & (C::PLACES - 1)) * (C::BN / 2) + 16 * i), w);
         if (i & 1) {
           tmem_wait_st();
@@ -513,11 +520,11 @@ __global__ void __launch_bounds__(256) cross_tc_join_kernel(const __grid_constan
   }
 }
 
-// Blocks of a launch over `batch` entries: one to each place on the device, fewer where a block would get less than LEAST keys.
+// Blocks of a launch over `batch` entries: one to a multiprocessor, fewer where a block would get less than LEAST keys.
 template <int D>
 int64_t grid_of(int batch, int q_tokens, int kv_tokens, int heads) {
   using C = Cfg<D>;
-  const int64_t most = (int64_t)PLAN_SMS * C::BLOCKS, tiles = (int64_t)((q_tokens + C::ROWS - 1) / C::ROWS) * heads * batch, n = (kv_tokens + C::BN - 1) / C::BN;
+  const int64_t most = (int64_t)PLAN_SMS, tiles = (int64_t)((q_tokens + C::ROWS - 1) / C::ROWS) * heads * batch, n = (kv_tokens + C::BN - 1) / C::BN;
   if (tiles >= most * (LEAST / C::BN)) return most;
   const int64_t blocks = (tiles * n + LEAST / C::BN - 1) / (LEAST / C::BN);
   return blocks < most ? blocks : most;
