@@ -270,7 +270,11 @@ cudaError_t launch_typed(const CrossParams& p, const CrossPlan& plan, int D, cud
 CrossPlan cross_plan(int batch, int q_tokens, int kv_tokens, int heads, int group, int D, bool bf16, bool mask) {
   CrossPlan plan{};
   plan.splits = plan.cluster = 1;
-  if (bf16 && !mask && q_tokens > 64 && kv_tokens > 0) {
+  // The kernel for many queries costs 16 us and 108 us per 10^6 keys x tiles of 256 queries, the one for few 6 us and 21 us per 10^6
+  // keys x tiles of 16 rows (heads of 64): 128 queries of 5 x 2 heads on 4800 keys take 23.2 us with the one and 24.4 with the other, 256 take 30.0
+  // and 36.9, of one entry 28.0 and 10.6; 64 of 8 x 4 heads on 14400 keys 56.5 and 52.4, 128 take 60.0 and 90.7.
+  if (bf16 && !mask && q_tokens > 64 && kv_tokens > 0 &&
+      ((int64_t)q_tokens * group + 15) / 16 * batch * (heads / group) >= 500000 / kv_tokens + 1) {
     plan.kernel = CROSS_TC;
     plan.scratch = cross_tc_scratch(batch, q_tokens, kv_tokens, heads, D);
     return plan;

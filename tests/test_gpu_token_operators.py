@@ -216,8 +216,19 @@ def test_cross_attention(cuda_device, dtype, B, Tq, Tk, H, K, D):
         _cross_check(binding.cross_attention(q, k, v), q, k, v, D ** -0.5, None, None, layout)
 
 
+@pytest.mark.parametrize("B,Tq,Tk,H,K,D", [
+    (3, 513, 4001, 4, 4, 64), (2, 700, 3001, 6, 3, 64), (4, 129, 4100, 8, 8, 32), (1, 1000, 2500, 4, 2, 128), (2, 257, 9000, 2, 2, 128),
+    (1, 8000, 130, 8, 8, 64), (1, 4000, 64, 32, 32, 64), (1, 66000, 1, 128, 128, 32), (300, 70, 60, 8, 8, 32), (2, 1300, 777, 8, 8, 128)])
+def test_cross_attention_of_many_queries(cuda_device, B, Tq, Tk, H, K, D):
+    """Work enough for the tensor-core kernel: tiles of queries and of keys that are not whole, more entries than one launch takes, tiles
+    that several blocks share."""
+    for i, layout in enumerate(("fused", "heads first")):
+        q, k, v = _cross_case(cuda_device, Tq * 31 + Tk + i, B, Tq, Tk, H, K, D, BF16, layout, sharp=(1.0, 8.0)[i])
+        _cross_check(binding.cross_attention(q, k, v), q, k, v, D ** -0.5, None, None, layout)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("Tq,Tk,D", [(7, 700, 64), (150, 300, 64), (300, 130, 128), (260, 1000, 32)])
+@pytest.mark.parametrize("Tq,Tk,D", [(7, 700, 64), (150, 300, 64), (300, 130, 128), (260, 1000, 32), (400, 3000, 64), (300, 2001, 128), (700, 1100, 32)])
 def test_cross_attention_lengths(cuda_device, dtype, Tq, Tk, D):
     """Rows behind the lengths hold NaN; rows of the output behind q_lengths are left alone."""
     B = 6
@@ -272,7 +283,7 @@ def test_cross_attention_masks(cuda_device, dtype, Tq, Tk, H, K, D):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("Tq", [5, 200])
+@pytest.mark.parametrize("Tq", [5, 200, 3001])
 def test_cross_attention_of_sharp_and_large_scores(cuda_device, dtype, Tq):
     """Scores in the thousands, rising along the keys so that the running maximum changes in every tile; and one key far above all others."""
     q, k, v = _cross_case(cuda_device, 9, 2, Tq, 700, 2, 2, 64, dtype, "plain")
@@ -294,9 +305,9 @@ def test_cross_attention_of_no_keys(cuda_device):
 
 
 # ------------------------------------------------------------------------------- common to all
-def _calls(dev, dtype, small):
+def _calls(dev, dtype, size):
     """(name, call) of each operator on fixed inputs; a call takes keyword arguments and returns a tuple of tensors."""
-    T, Tk = (1, 300) if small else (260, 700)
+    T, Tk = [(1, 300), (260, 700), (1100, 2000)][size]
     q, k, w, pos, inv = _rope_case(dev, 21, 2, T, 2, 2, 64, 64, dtype)
     lq, lk, lv, decay, state = _linear_case(dev, 22, 2, T, 2, 2, 64, dtype)
     cq, ck, cv = _cross_case(dev, 23, 2, T, Tk, 2, 2, 64, dtype)
@@ -307,9 +318,9 @@ def _calls(dev, dtype, small):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("small", [True, False])
-def test_streams_and_graphs_give_the_same_bits(cuda_device, dtype, small):
-    for name, call in _calls(cuda_device, dtype, small):
+@pytest.mark.parametrize("size", [0, 1, 2])
+def test_streams_and_graphs_give_the_same_bits(cuda_device, dtype, size):
+    for name, call in _calls(cuda_device, dtype, size):
         want = [x.clone() for x in call()]
         for _ in range(3):
             assert all(torch.equal(a, b) for a, b in zip(call(), want)), name
@@ -331,10 +342,11 @@ def test_streams_and_graphs_give_the_same_bits(cuda_device, dtype, small):
             assert all(torch.equal(a, b) for a, b in zip(got, want)), name
 
 
-def test_two_graphs_at_once(cuda_device):
+@pytest.mark.parametrize("Tq,Tk", [(7, 90000), (1100, 2000)])
+def test_two_graphs_at_once(cuda_device, Tq, Tk):
     """Captured apart, replayed side by side on two streams: each has scratch of its own."""
-    q, k, v = _cross_case(cuda_device, 5, 1, 7, 9000, 2, 2, 64, BF16)
-    q2, k2, v2 = _cross_case(cuda_device, 6, 1, 7, 9000, 2, 2, 64, BF16)
+    q, k, v = _cross_case(cuda_device, 5, 1, Tq, Tk, 4, 4, 64, BF16)
+    q2, k2, v2 = _cross_case(cuda_device, 6, 1, Tq, Tk, 4, 4, 64, BF16)
     want, want2 = binding.cross_attention(q, k, v), binding.cross_attention(q2, k2, v2)
     graphs, outs = [], []
     for a in ((q, k, v), (q2, k2, v2)):
@@ -355,15 +367,15 @@ def test_two_graphs_at_once(cuda_device):
 def test_rows_more_than_32_bits_apart(cuda_device):
     """Entries, tokens and heads whose offsets pass 2^32 elements."""
     far = 2 ** 32 + 64
-    room = torch.empty(far + 64 * 300, dtype=BF16, device=cuda_device)
+    room = torch.empty(far + 64 * 4000, dtype=BF16, device=cuda_device)
     g = _gen(cuda_device, 8)
     for strides in ((far, 64, 64), (64, far, 64)):
         # two entries, or two tokens of one
-        B, T = (2, 20) if strides[0] == far else (1, 2)
+        B, T = (2, 4000) if strides[0] == far else (1, 2)
         x = room.as_strided((B, T, 1, 64), strides[:2] + (64, 1))
         x.copy_(torch.randn(B, T, 1, 64, generator=g, device=cuda_device).to(BF16))
         near = x.contiguous()
-        q = torch.randn(B, 200, 1, 64, generator=g, device=cuda_device).to(BF16)
+        q = torch.randn(B, 2000, 1, 64, generator=g, device=cuda_device).to(BF16)
         assert torch.equal(binding.cross_attention(q, x, x), binding.cross_attention(q, near, near))
         assert torch.equal(binding.cross_attention(q[:, :3], x, x), binding.cross_attention(q[:, :3], near, near))
         assert torch.equal(binding.qk_norm_rope(x, None)[0], binding.qk_norm_rope(near, None)[0])
@@ -377,8 +389,8 @@ def test_rows_more_than_32_bits_apart(cuda_device):
 
 def test_shared_inputs(cuda_device):
     """Keys and values that all entries, or all heads, share through a stride of 0."""
-    for Tq in (3, 300):
-        q, k, v = _cross_case(cuda_device, 3, 3, Tq, 200, 2, 2, 64, BF16, "plain")
+    for Tq, Tk in ((3, 200), (300, 200), (1000, 1500)):
+        q, k, v = _cross_case(cuda_device, 3, 3, Tq, Tk, 2, 2, 64, BF16, "plain")
         for a, b in ((k[:1].expand(3, -1, -1, -1), v[:1].expand(3, -1, -1, -1)), (k[:, :, :1].expand(-1, -1, 2, -1), v[:, :, :1].expand(-1, -1, 2, -1))):
             assert torch.equal(binding.cross_attention(q, a, b), binding.cross_attention(q, a.contiguous(), b.contiguous()))
             d, s = torch.tensor([-0.1, 0.0], device=cuda_device), torch.zeros(3, 2, 64, 64, device=cuda_device)
