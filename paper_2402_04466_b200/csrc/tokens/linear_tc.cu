@@ -49,13 +49,31 @@ struct Cfg {
   // side with out as well, adding each chunk's product to a state in registers: 118 us where this takes 107.)
   static constexpr bool SIDE = !WITH_OUT && D <= 64;
   static constexpr int N = SIDE ? 3 * D : D;                        // columns of the state's product
-  static constexpr uint32_t A_COL = N, P_COL = A_COL + (PLACES < 2 ? 1 : 2) * CT, O_COL = P_COL + CT / 2;    // scores, weights, sums; the state's lies first
-  static constexpr uint32_t COLS = WITH_OUT ? O_COL + PLACES * D : N;
+  // the state's product lies first, then scores (weights take the place of those of the same warps), P V and Q S
+  static constexpr uint32_t A_COL = N, PV_COL = A_COL + (PLACES < 2 ? 1 : 2) * CT, QS_COL = PV_COL + PLACES * D;
+  static constexpr uint32_t COLS = WITH_OUT ? QS_COL + D : N;
   static constexpr uint32_t TMEM = COLS <= 32 ? 32 : COLS <= 64 ? 64 : COLS <= 128 ? 128 : COLS <= 256 ? 256 : 512;
   static constexpr int TABLE_BYTES = (CT + 4) * 4 + 128;
   static constexpr int SMEM = (WITH_OUT ? 3 : 2) * PLACES * TILE_BYTES + 3 * KP_PLACES * TILE_BYTES + (WITH_OUT ? STATE_BYTES : 0) + TABLE_BYTES + 512 + 1024;
   static_assert(COLS <= 512 && SMEM <= 227 * 1024, "tensor and shared memory");
 };
+
+// (P V) of token t, the r-th of its chunk, in one column, term by term on the fp32 units.
+template <int D>
+__device__ __noinline__ float own_sum(const LinearParams& p, int b, int h, int t, int r, int col, const float* pw) {
+  const int hk = h / p.group;
+  const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(p.q.p) + b * p.q.b + h * p.q.h + (int64_t)t * p.q.t;
+  const __nv_bfloat16* k = reinterpret_cast<const __nv_bfloat16*>(p.k.p) + b * p.k.b + hk * p.k.h + (int64_t)(t - r) * p.k.t;
+  const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(p.v.p) + b * p.v.b + hk * p.v.h + (int64_t)(t - r) * p.v.t + col;
+  float sum = 0.f;
+  for (int j = 0; j <= r; ++j) {
+    float w = 0.f;
+#pragma unroll 8
+    for (int i = 0; i < D; ++i) w = fmaf(__bfloat162float(q[i]), __bfloat162float(k[j * p.k.t + i]), w);
+    sum = fmaf(w * (p.scale * pw[r - j]), __bfloat162float(v[j * p.v.t]), sum);
+  }
+  return sum;
+}
 
 template <int D, bool WITH_OUT>
 __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel(const __grid_constant__ LinearTcParams pp) {
@@ -75,16 +93,15 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
   uint64_t* qfull = reinterpret_cast<uint64_t*>(pr + 32);            // [PLACES], as the next five
   uint64_t* kfull = qfull + 4;
   uint64_t* vfull = kfull + 4;
-  uint64_t* qempty = vfull + 4;        // Q S is done
+  uint64_t* qempty = vfull + 4;        // scores and Q S are done
   uint64_t* kempty = qempty + 4;       // scores are done, K' is made
   uint64_t* vempty = kempty + 4;       // both products of V are done
   uint64_t* kready = vempty + 4;       // [KP_PLACES] K' is there and the state is scaled
   uint64_t* sdone = kready + 2;        // [KP_PLACES] the state's product is done
   uint64_t* afull = sdone + 2;         // [PLACES] scores are there
-  uint64_t* ofirst = afull + 2;       // Q S is there
-  uint64_t* pready = ofirst + 1;       // P is there, and the sums are scaled
-  uint64_t* odone = pready + 1;        // out is there
-  uint64_t* oread = odone + 1;         // out is in registers
+  uint64_t* pready = afull + 2;        // [PLACES] P is there
+  uint64_t* odone = pready + 2;        // P V and Q S are there
+  uint64_t* oread = odone + 1;         // they are in registers
   uint64_t* sready = oread + 1;        // the state is an operand
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sready + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -116,12 +133,11 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
     }
     for (int s = 0; s < 2; ++s) {
       mbar_init(smem_u32(afull + s), 1);
+      mbar_init(smem_u32(pready + s), GROUP);
       mbar_init(smem_u32(sdone + s), 1);
       mbar_init(smem_u32(kready + s), GROUP);
     }
-    mbar_init(smem_u32(ofirst), 1);
     mbar_init(smem_u32(odone), 1);
-    mbar_init(smem_u32(pready), GROUP);
     mbar_init(smem_u32(oread), GROUP);
     mbar_init(smem_u32(sready), GROUP);
     *abort_flag = 0;
@@ -224,34 +240,40 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
       __syncwarp();
       return true;
     };
+    auto state_part = [&](int c) {     // Q S: the state is an operand, and the last chunk's Q S and P V have been read
+      if (!wait(sready, c, 0x22) || (c > 0 && !wait(oread, c - 1, 0x23))) return false;
+      tc_fence_after();
+      if (issuer) {
+        const uint64_t q = q0 + (uint64_t)(place(c) * (C::TILE_BYTES >> 4));
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k)
+          umma_bf16(tmem + C::QS_COL, q + (uint64_t)((k / 4) * (C::SLAB_BYTES >> 4) + (k % 4) * 2), st0 + (uint64_t)((k / 4) * (C::STATE_SLAB >> 4) + (k % 4) * 2), QS, k > 0);
+        umma_commit(smem_u32(qempty + place(c)));
+      }
+      __syncwarp();
+      return true;
+    };
     scores(0);
     for (int c = 0; c < chunks && ok; ++c) {
       const int s = place(c);
-      // sums of an earlier chunk in the same place have been read
-      if (!wait(sready, c, 0x22) || (c >= PLACES && !wait(oread, c - PLACES, 0x23))) break;
-      tc_fence_after();
-      if (issuer) {
-        const uint64_t q = q0 + (uint64_t)(s * (C::TILE_BYTES >> 4));
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k)
-          umma_bf16(tmem + C::O_COL + (uint32_t)(s * D), q + (uint64_t)((k / 4) * (C::SLAB_BYTES >> 4) + (k % 4) * 2), st0 + (uint64_t)((k / 4) * (C::STATE_SLAB >> 4) + (k % 4) * 2), QS, k > 0);
-        umma_commit(smem_u32(ofirst));
-        umma_commit(smem_u32(qempty + s));
-      }
-      __syncwarp();
-      // with two places the next scores are formed meanwhile: theirs were read before the last P was there
-      if (PLACES == 2 && c + 1 < chunks && !scores(c + 1)) break;
-      if (!wait(pready, c, 0x24)) break;
+      // with two places the next scores are formed meanwhile, where the last but one's weights have been used
+      if (PLACES == 2 && c + 1 < chunks && ((c > 0 && !wait(odone, c - 1, 0x25)) || !scores(c + 1))) break;
+      if (PLACES == 1 && !state_part(c)) break;
+      // the values have landed, and their rows behind the last token are zeros, when K' is there
+      if (!wait(kready + kp_place(c), kp_turn(c), 0x27) || !wait(pready + s, turn(c), 0x24)) break;
       tc_fence_after();
       if (issuer) {
         const uint64_t v = v0 + (uint64_t)(s * (C::TILE_BYTES >> 4));
 #pragma unroll
-        for (int k = 0; k < CT / 16; ++k) umma_bf16_ts(tmem + C::O_COL + (uint32_t)(s * D), tmem + C::P_COL + (uint32_t)(k * 8), v + (uint64_t)(k * C::ROW), PV, 1);
-        umma_commit(smem_u32(odone));
+        for (int k = 0; k < CT / 16; ++k)
+          umma_bf16_ts(tmem + C::PV_COL + (uint32_t)(s * D), tmem + C::A_COL + (uint32_t)(s * CT + (k >> 2) * 64 + (k & 3) * 8), v + (uint64_t)(k * C::ROW), PV, k > 0);
         umma_commit(smem_u32(vempty + s));
       }
       __syncwarp();
-      if (PLACES == 1 && c + 1 < chunks && !scores(c + 1)) break;
+      if (PLACES == 2 && !state_part(c)) break;
+      if (issuer) umma_commit(smem_u32(odone));
+      __syncwarp();
+      if (PLACES == 1 && c + 1 < chunks && (!wait(odone, c, 0x26) || !scores(c + 1))) break;
     }
   } else if (WITH_OUT && warp >= W_OUT) {
     // ---------------------------------------------------------------------------- P and out
@@ -266,27 +288,54 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(bar));
     };
-    auto store = [&](int c) {          // out of chunk c, which is there
+    auto store = [&](int c) {          // out of chunk c, whose products are there
       tc_fence_after();
-      uint32_t y[PIECES][16];
-#pragma unroll
-      for (int i = 0; i < PIECES; ++i) tmem_ld16_async(lanes + C::O_COL + (uint32_t)(place(c) * D + c0 + 16 * i), y[i]);
-      tmem_wait_ld();
-      arrive(oread);
       const int t = t0 + c * CT + r;
-      if (t < t1) {
+      const float f = scale * pw[r + 1];
+      const Two f2 = pack2(f, f);
+      constexpr int BATCH = PIECES < 2 ? PIECES : 2;      // pieces at a time
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i)
+      for (int i0 = 0; i0 < PIECES; i0 += BATCH) {
+        uint32_t y[BATCH][16], z[BATCH][16];
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            auto two = [&](int e) { return pack_bf16(__uint_as_float(y[i][8 * x + e]), __uint_as_float(y[i][8 * x + e + 1])); };
-            *reinterpret_cast<uint4*>(out + (int64_t)t * p.o.t + c0 + 16 * i + 8 * x) = make_uint4(two(0), two(2), two(4), two(6));
+        for (int i = 0; i < BATCH; ++i) {
+          tmem_ld16_async(lanes + C::PV_COL + (uint32_t)(place(c) * D + c0 + 16 * (i0 + i)), y[i]);
+          tmem_ld16_async(lanes + C::QS_COL + (uint32_t)(c0 + 16 * (i0 + i)), z[i]);
+        }
+        tmem_wait_ld();
+        if (i0 + BATCH == PIECES) arrive(oread);
+        Two bad = pack2(0.f, 0.f);     // stays 0 unless one of P V is an infinity or NaN
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i)
+#pragma unroll
+          for (int x = 0; x < 16; x += 2) bad = fma2_of(pack2(__uint_as_float(y[i][x]), __uint_as_float(y[i][x + 1])), pack2(0.f, 0.f), bad);
+        float b0, b1;
+        unpack2(bad, b0, b1);
+        if (t >= t1) continue;
+        // the weights of 0 behind a token make NaN of what is not finite in a later token's values: such sums are taken again, of the tokens up to this
+        // one only
+        const bool again = b0 + b1 != 0.f;
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+          __nv_bfloat16* dst = out + (int64_t)t * p.o.t + c0 + 16 * (i0 + i);
+#pragma unroll
+          for (int x = 0; x < 16; x += 2) {
+            float lo, hi;
+            unpack2(fma2_of(pack2(__uint_as_float(z[i][x]), __uint_as_float(z[i][x + 1])), f2, pack2(__uint_as_float(y[i][x]), __uint_as_float(y[i][x + 1]))), lo, hi);
+            y[i][x / 2] = pack_bf16(lo, hi);
           }
+          *reinterpret_cast<uint4*>(dst) = make_uint4(y[i][0], y[i][1], y[i][2], y[i][3]);
+          *reinterpret_cast<uint4*>(dst + 8) = make_uint4(y[i][4], y[i][5], y[i][6], y[i][7]);
+          if (__builtin_expect(again, 0)) {
+#pragma unroll
+            for (int x = 0; x < 16; ++x) dst[x] = __float2bfloat16(fmaf(__uint_as_float(z[i][x]), f, own_sum<D>(p, b, h, t, r, c0 + 16 * (i0 + i) + x, pw)));
+          }
+        }
       }
     };
     for (int c = 0; c < chunks; ++c) {
       const int s = place(c);
-      if (!wait(afull + s, turn(c), 0x31) || (PLACES == 2 && c > 0 && !wait(odone, c - 1, 0x32))) break;      // the last P has been used
+      if (!wait(afull + s, turn(c), 0x31)) break;
       tc_fence_after();
       // weights within the chunk: blocks of 32 columns below the diagonal, on it, and above it
 #pragma unroll
@@ -320,28 +369,16 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
             }
           }
         }
-        tmem_st16(lanes + C::P_COL + (uint32_t)(16 * i), w);
-      }
-      if (!wait(ofirst, c, 0x33)) break;
-      tc_fence_after();
-      {
-        const float f = scale * pw[r + 1];
-        uint32_t v[PIECES][16];
-#pragma unroll
-        for (int i = 0; i < PIECES; ++i) tmem_ld16_async(lanes + C::O_COL + (uint32_t)(s * D + c0 + 16 * i), v[i]);
-        tmem_wait_ld();
-#pragma unroll
-        for (int i = 0; i < PIECES; ++i) {
-#pragma unroll
-          for (int x = 0; x < 16; ++x) v[i][x] = __float_as_uint(__uint_as_float(v[i][x]) * f);
-          tmem_st16(lanes + C::O_COL + (uint32_t)(s * D + c0 + 16 * i), v[i]);
-        }
+        tmem_st16(lanes + C::A_COL + (uint32_t)(s * CT + 64 * half + 16 * y), w);
       }
       tmem_wait_st();
-      arrive(pready);
+      arrive(pready + s);
       // with two places the chunk before is stored while this one's product runs
       if (PLACES == 2) {
-        if (c > 0) store(c - 1);
+        if (c > 0) {
+          if (!wait(odone, c - 1, 0x32)) break;
+          store(c - 1);
+        }
       } else {
         if (!wait(odone, c, 0x30)) break;
         store(c);
@@ -460,7 +497,7 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
         }
         tmem_wait_st();
         arrive(kready + kp_place(c));
-        if (c > 0 && !wait(ofirst, c - 1, 0x45)) break;      // the state's copy as an operand has been used
+        if (c > 0 && !wait(odone, c - 1, 0x45)) break;      // the state's copy as an operand has been used
         put_state(v);
         arrive(sready);
       } else {

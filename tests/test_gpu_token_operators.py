@@ -181,6 +181,32 @@ def test_linear_attention_slots_and_lengths(cuda_device, dtype, T):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D", [32, 64, 128])
+def test_linear_attention_does_not_look_ahead(cuda_device, dtype, D):
+    """What is not finite in a token's key or value reaches that token's row and later ones, and no earlier one."""
+    B, T, H, K = 2, 333, 2, 1
+    for name, at in (("v", 200), ("k", 200), ("v", 332), ("v", 128), ("v", 1)):
+        q, k, v, decay, state = _linear_case(cuda_device, at + D, B, T, H, K, D, dtype, "plain")
+        decay = torch.tensor([-0.01, -0.5], device=cuda_device)
+        x = {"k": k, "v": v}[name]
+        clean = x.clone()
+        clean[:, at:] = 0
+        args = (q, clean, v) if name == "k" else (q, k, clean)
+        want, _ = binding.linear_attention(*args, decay, state.clone(), scale=0.1)
+        x[0, at, 0, D // 2], x[1, at, 0, 1] = math.inf, math.nan
+        x[1, at, 0, D - 1] = -math.inf
+        got, new = binding.linear_attention(q, k, v, decay, state.clone(), scale=0.1)
+        out, size, _, A = ref.linear(args[0], args[1], args[2], decay, state, 0.1, None)
+        bound, _ = ref.linear_bounds(out, size, A, D, T, dtype, dtype == FP32)
+        check(got[:, :at], out[:, :at], bound[:, :at], f"{name} before {at}")
+        assert not torch.isfinite(got[0, at:]).all(-1).any() and torch.isnan(got[1, at:]).any(-1).all()
+        assert not torch.isfinite(new).flatten(2).all(-1).any()
+        if name == "v":                # columns of the state are apart from each other
+            others = [c for c in range(D) if c not in (1, D // 2, D - 1)]
+            assert torch.isfinite(got[..., others]).all() and torch.isfinite(new[..., others]).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_linear_attention_in_pieces_is_linear_attention(cuda_device, dtype):
     """A clip and then single tokens, as a stream that is brought up to date and goes on: the states meet."""
     q, k, v, decay, state = _linear_case(cuda_device, 1, 3, 210, 2, 2, 64, dtype)
