@@ -81,19 +81,17 @@ __device__ __forceinline__ void multiply(Two (&o)[A][D / 32], const float* x, in
   }
 }
 
-// a row's out before its scale, terms of later tokens left out
+// a thread's columns of a row's out once more, terms of later tokens left out
 template <int D>
-__device__ __noinline__ void own_sums(Two (&o)[D / 32], const float* q, const float* S, const float* P, const float* v, int i, float decay, int tx) {
-  Two g[D / 32];
-  for (int c = 0; c < D / 32; ++c) o[c] = pack2(0.f, 0.f);
-  for (int e = 0; e < D; ++e) {
-    load_pairs<D>(S + e * D, tx, g);
-    for (int c = 0; c < D / 32; ++c) o[c] = fma2_of(pack2(q[e], q[e]), g[c], o[c]);
-  }
-  for (int c = 0; c < D / 32; ++c) o[c] = mul2_of(o[c], pack2(decay, decay));
-  for (int j = 0; j <= i; ++j) {
-    load_pairs<D>(v + j * D, tx, g);
-    for (int c = 0; c < D / 32; ++c) o[c] = fma2_of(pack2(P[j], P[j]), g[c], o[c]);
+__device__ __noinline__ void own_sums(float* out, const float* q, const float* S, const float* P, const float* v, int i, float decay, float scale, int tx) {
+#pragma unroll
+  for (int c = 0; c < D / 16; ++c) {
+    const int at = column<D>(tx, c);
+    float sum = 0.f;
+    for (int e = 0; e < D; ++e) sum = fmaf(q[e], S[e * D + at], sum);
+    sum *= decay;
+    for (int j = 0; j <= i; ++j) sum = fmaf(P[j], v[j * D + at], sum);
+    out[at] = sum * scale;
   }
 }
 
@@ -177,17 +175,17 @@ __device__ __forceinline__ void run_chunks(const LinearParams& p, int b, int h, 
       for (int a = 0; a < A; ++a) {
         const int i = ty + 16 * a;
         if (i < m) {
+          float* dst = go + (int64_t)(t + i) * p.o.t;
+          const Two s2 = pack2(p.scale, p.scale);
+#pragma unroll
+          for (int c = 0; c < E / 2; ++c) *reinterpret_cast<Two*>(dst + column<D>(tx, 2 * c)) = mul2_of(o[a][c], s2);
           // the weights of 0 behind a token make NaN of what is not finite in a later token's values: sums of its own and earlier tokens only
           Two bad = pack2(0.f, 0.f);
 #pragma unroll
           for (int c = 0; c < E / 2; ++c) bad = fma2_of(o[a][c], pack2(0.f, 0.f), bad);
           float b0, b1;
           unpack2(bad, b0, b1);
-          if (__builtin_expect(b0 + b1 != 0.f, 0)) own_sums<D>(o[a], q + i * QP, S, P + i * PP, v, i, pw[i + 1], tx);
-          float* dst = go + (int64_t)(t + i) * p.o.t;
-          const Two s2 = pack2(p.scale, p.scale);
-#pragma unroll
-          for (int c = 0; c < E / 2; ++c) *reinterpret_cast<Two*>(dst + column<D>(tx, 2 * c)) = mul2_of(o[a][c], s2);
+          if (__builtin_expect(b0 + b1 != 0.f, 0)) own_sums<D>(dst, q + i * QP, S, P + i * PP, v, i, pw[i + 1], p.scale, tx);
         }
       }
     }

@@ -58,21 +58,27 @@ struct Cfg {
   static_assert(COLS <= 512 && SMEM <= 227 * 1024, "tensor and shared memory");
 };
 
-// (P V) of token t, the r-th of its chunk, in one column, term by term on the fp32 units.
-template <int D>
-__device__ __noinline__ float own_sum(const LinearParams& p, int b, int h, int t, int r, int col, const float* pw) {
+// out of token t, the r-th of its chunk, in N columns from `col` on, P V term by term on the fp32 units; q_s: what Q S contributes.
+template <int D, int N>
+__device__ __noinline__ void own_sums(const LinearParams& p, int b, int h, int t, int r, int col, const float* pw, const float (&q_s)[N]) {
   const int hk = h / p.group;
   const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(p.q.p) + b * p.q.b + h * p.q.h + (int64_t)t * p.q.t;
   const __nv_bfloat16* k = reinterpret_cast<const __nv_bfloat16*>(p.k.p) + b * p.k.b + hk * p.k.h + (int64_t)(t - r) * p.k.t;
   const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(p.v.p) + b * p.v.b + hk * p.v.h + (int64_t)(t - r) * p.v.t + col;
-  float sum = 0.f;
+  float sum[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) sum[i] = q_s[i];
   for (int j = 0; j <= r; ++j) {
     float w = 0.f;
-#pragma unroll 8
+#pragma unroll 4
     for (int i = 0; i < D; ++i) w = fmaf(__bfloat162float(q[i]), __bfloat162float(k[j * p.k.t + i]), w);
-    sum = fmaf(w * (p.scale * pw[r - j]), __bfloat162float(v[j * p.v.t]), sum);
+    w *= p.scale * pw[r - j];
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum[i] = fmaf(w, __bfloat162float(v[j * p.v.t + i]), sum[i]);
   }
-  return sum;
+  __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.o.p) + b * p.o.b + h * p.o.h + (int64_t)t * p.o.t + col;
+#pragma unroll
+  for (int i = 0; i < N; ++i) out[i] = __float2bfloat16(sum[i]);
 }
 
 template <int D, bool WITH_OUT>
@@ -293,7 +299,7 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
       const int t = t0 + c * CT + r;
       const float f = scale * pw[r + 1];
       const Two f2 = pack2(f, f);
-      constexpr int BATCH = PIECES < 2 ? PIECES : 2;      // pieces at a time
+      constexpr int BATCH = PIECES == 2 ? 2 : 1;      // pieces at a time
 #pragma unroll
       for (int i0 = 0; i0 < PIECES; i0 += BATCH) {
         uint32_t y[BATCH][16], z[BATCH][16];
@@ -326,10 +332,14 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
           }
           *reinterpret_cast<uint4*>(dst) = make_uint4(y[i][0], y[i][1], y[i][2], y[i][3]);
           *reinterpret_cast<uint4*>(dst + 8) = make_uint4(y[i][4], y[i][5], y[i][6], y[i][7]);
-          if (__builtin_expect(again, 0)) {
+        }
+        if (__builtin_expect(again, 0)) {
+          float a[16 * BATCH];
 #pragma unroll
-            for (int x = 0; x < 16; ++x) dst[x] = __float2bfloat16(fmaf(__uint_as_float(z[i][x]), f, own_sum<D>(p, b, h, t, r, c0 + 16 * (i0 + i) + x, pw)));
-          }
+          for (int i = 0; i < BATCH; ++i)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) a[16 * i + x] = __uint_as_float(z[i][x]) * f;
+          own_sums<D>(p, b, h, t, r, c0 + 16 * i0, pw, a);
         }
       }
     };
