@@ -185,6 +185,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) cross_tc_kernel(const __gr
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  pdl_launch_dependents();                     // the join gets ready meanwhile
   const uint32_t tmem = *tmem_slot;
 
   // the it-th weights of tile t: their place among all, and how often that has been used before
@@ -488,6 +489,7 @@ __global__ void __launch_bounds__(256) cross_tc_join_kernel(const __grid_constan
   add_up<D>(work, p);
   Cursor cur;
   cur.start<D>(work, p);
+  pdl_wait();                                  // also of blocks that have nothing to do: the grid ends behind the kernel above
   if (cur.done() || cur.j0 == 0) return;
   const int64_t each = share_of<D>(work, p), from = cur.at - cur.j0, first = from / each;
   if (first + 1 != blockIdx.x) return;
@@ -526,7 +528,7 @@ int64_t grid_of(int batch, int q_tokens, int kv_tokens, int heads) {
 }
 
 template <int D>
-cudaError_t launch(CrossTcParams& p, int batch, cudaStream_t s) {
+cudaError_t launch(CrossTcParams& p, int batch, cudaStream_t s) {      // (the join is launched ahead of the end of the kernel: 2 us)
   using C = Cfg<D>;
   static OncePerContext once;
   cudaError_t e = once([] { return cudaFuncSetAttribute(cross_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM); });
@@ -536,8 +538,7 @@ cudaError_t launch(CrossTcParams& p, int batch, cudaStream_t s) {
     const unsigned blocks = (unsigned)grid_of<D>(p.batch, p.q_tokens, p.kv_tokens, p.heads);
     cross_tc_kernel<D><<<blocks, C::THREADS, C::SMEM, s>>>(p);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    cross_tc_join_kernel<D><<<dim3(blocks, 4), 256, 0, s>>>(p);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    if ((e = launch_kernel(cross_tc_join_kernel<D>, dim3(blocks, 4), 256, 0, s, p, true)) != cudaSuccess) return e;
   }
   return cudaSuccess;
 }

@@ -235,6 +235,7 @@ __global__ void __launch_bounds__(THREADS) linear_segment_kernel(const __grid_co
   float* smem = reinterpret_cast<float*>(raw);
   float* S = state_in_shared<D>(smem);
   const int b = blockIdx.z, h = blockIdx.y, seg = blockIdx.x;
+  pdl_launch_dependents();
   if (slot_of(p.slots, p.num_slots, b) < 0) return;
   const int n = clamp_length(p.lengths, b, p.tokens), t0 = seg * p.seg_tokens;
   if (t0 + p.seg_tokens >= n) return;      // the last one's is not needed
@@ -248,6 +249,8 @@ __global__ void __launch_bounds__(THREADS) linear_segment_kernel(const __grid_co
 template <int D>
 __global__ void __launch_bounds__(THREADS) linear_scan_kernel(const __grid_constant__ LinearParams p) {
   const int b = blockIdx.z, h = blockIdx.y, i = (int)blockIdx.x * THREADS + (int)threadIdx.x;
+  pdl_wait();
+  pdl_launch_dependents();             // (fp32 only: bf16's next grid, launched ahead of this one's end, made eight maps 112 us of 104)
   const int slot = slot_of(p.slots, p.num_slots, b);
   if (slot < 0) return;
   const int n = clamp_length(p.lengths, b, p.tokens);
@@ -277,6 +280,7 @@ __global__ void __launch_bounds__(THREADS) linear_chunk_kernel(const __grid_cons
   float* S = state_in_shared<D>(smem);
   const int b = blockIdx.z, h = blockIdx.y, seg = blockIdx.x;
   const int slot = slot_of(p.slots, p.num_slots, b);
+  pdl_wait();
   if (slot < 0) return;
   const int n = clamp_length(p.lengths, b, p.tokens), t0 = seg * p.seg_tokens, t1 = min(n, t0 + p.seg_tokens);
   if (seg > 0 && t0 >= n) return;
@@ -302,8 +306,7 @@ cudaError_t launch(const LinearParams& p, cudaStream_t s) {
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     if ((e = launch_linear_scan(p, D, s)) != cudaSuccess) return e;
   }
-  linear_chunk_kernel<D><<<dim3((unsigned)p.segments, (unsigned)p.heads, (unsigned)p.batch), THREADS, smem, s>>>(p);
-  return cudaGetLastError();
+  return launch_kernel(linear_chunk_kernel<D>, dim3((unsigned)p.segments, (unsigned)p.heads, (unsigned)p.batch), THREADS, smem, s, p, p.segments > 1);
 }
 }  // namespace
 
@@ -321,10 +324,7 @@ void linear_plan(int batch, int tokens, int heads, bool bf16, int* segments, int
 
 cudaError_t launch_linear_scan(const LinearParams& p, int D, cudaStream_t s) {
   const dim3 grid((unsigned)(D * D / THREADS), (unsigned)p.heads, (unsigned)p.batch);
-  if (D == 32) linear_scan_kernel<32><<<grid, THREADS, 0, s>>>(p);
-  else if (D == 64) linear_scan_kernel<64><<<grid, THREADS, 0, s>>>(p);
-  else linear_scan_kernel<128><<<grid, THREADS, 0, s>>>(p);
-  return cudaGetLastError();
+  return launch_kernel(D == 32 ? linear_scan_kernel<32> : D == 64 ? linear_scan_kernel<64> : linear_scan_kernel<128>, grid, THREADS, 0, s, p, true);
 }
 
 cudaError_t launch_linear_chunk(const LinearParams& p, int D, cudaStream_t s) {
