@@ -10,7 +10,7 @@
 //
 // Bound by the warps that turn scores into weights: the exponentials alone (16 a cycle and multiprocessor) take 1024 cycles for a
 // tile of 128 x 128 whose two products take 512 with heads of 64 and 1024 with heads of 128.  Eight entries of 4 heads of 64, 4800 queries on
-// 4800 keys: 287 us, 657 TFLOP/s, 1750 cycles a tile of 128 x 128; four entries of 2 heads of 128, 4800 queries on 9100 to 14400 keys: 224 us, 1027
+// 4800 keys: 286 us, 660 TFLOP/s, 1750 cycles a tile of 128 x 128; four entries of 2 heads of 128, 4800 queries on 9100 to 14400 keys: 224 us, 1027
 // TFLOP/s.  Weights are rounded to bf16 once, as far as out itself is; their sum is of the weights before that.
 #include "tokens.h"
 

@@ -8,8 +8,8 @@
 // segments: linear_segment_kernel forms what each segment adds to the state, linear_scan_kernel turns that into the state
 // before each segment, and linear_chunk_kernel then runs all segments at once.  K and V are read twice then.
 //
-// Bound by the fp32 units and what feeds them from shared memory.  Two sequences of 4801 tokens, 2 heads of 64 over one of keys and values: 59.5 us (28
-// segments' sums, 29 out), one or two blocks to a multiprocessor, each a chain of 3 chunks.
+// Bound by the fp32 units and what feeds them from shared memory.  Two sequences of 4801 tokens, 2 heads of 64 over one of keys and values: 58 us, 20
+// of them the segments' sums and 33 out: one or two blocks to a multiprocessor, each a chain of two chunks.
 #include "linear_common.cuh"
 #include "token_ptx.cuh"
 

@@ -15,8 +15,8 @@
 // from scores and sums, and eight make K' and carry the state.  Scores, P V, operands and K' have two places each where
 // the memory allows (heads of up to 64).  What is left in sequence is the state's product and its scaling.
 //
-// Those eight maps take 101 us, 28 of them the segments' sums: 1.8 TB/s, 5100 cycles for a chunk's out and state.  What bounds it is not memory (36 us)
-// but the instructions of the 16 warps that make operands of what the products left, 3200 a chunk and scheduler with the waits between.
+// Those eight maps take 104 us, 33 of them the segments' sums and 4 the scan: 2.3 TB/s, 4800 cycles for a chunk's out and state.  What bounds it is
+// not memory (36 us) but shared memory, 290 KB moved a chunk, of which K' is half, and the 16 warps that make operands of what the products left.
 #include "linear_common.cuh"
 #include "token_ptx.cuh"
 
