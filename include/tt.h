@@ -501,7 +501,7 @@ tt_status tt_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, dou
  * and head, in order of the tokens, with S the head's state [head_dim (key)][head_dim (value)]:
  *   S = exp(log_decay[head]) * S + k_t v_t^T;   out_t = scale * q_t S.
  * A call of several tokens works in chunks, one of a single token per entry reads and writes the states once.
- * log_decay: device fp32 [heads], 0 or below (-infinity: the state is the newest token's alone).
+ * log_decay: device fp32 [heads], 0 or below (-infinity: a state that was finite is the newest token's alone).
  * state, state_out: device fp32 [num_slots][heads][head_dim][head_dim], 16-byte aligned; entry b starts from its slot of `state` and leaves its last
  * state in the same slot of state_out.  The two may be one buffer; slots that no entry names are left as they were.
  * slots: device int32 [batch], NULL: entry b has slot b.  An entry whose slot is out of range, or is an earlier entry's too, is passed over:
