@@ -29,7 +29,8 @@ struct Shape {
   static constexpr int N = BN / 16;                     // keys to a thread
   static constexpr int E = D / 16;                      // columns to a thread
   static constexpr int QP = D + 4, PP = BN + 4;
-  static constexpr size_t smem = sizeof(float) * (BM * QP + BN * QP + BN * D + BM * PP);
+  static constexpr int KV = BN * (QP + D);              // a tile's keys and values, of which two are in shared memory
+  static constexpr size_t smem = sizeof(float) * (BM * QP + 2 * KV + BM * PP);
 };
 
 // this thread's columns of a row, as pairs: four neighbours at 4 tx (and 64 + 4 tx), two at 2 tx where D is 32
@@ -45,6 +46,10 @@ __device__ __forceinline__ void load_pairs(const float* row, int tx, Two (&f)[D 
     }
   }
 }
+// 16 bytes to shared memory without waiting for them, or zeros
+__device__ __forceinline__ void copy16(float* dst, const float* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
 __device__ __forceinline__ bool all_finite(float4 f) {
   return isfinite(f.x) && isfinite(f.y) && isfinite(f.z) && isfinite(f.w);
 }
@@ -55,9 +60,8 @@ __global__ void __launch_bounds__(THREADS) cross_kernel(const __grid_constant__ 
   constexpr int A = S::A, N = S::N, E = S::E, QP = S::QP, PP = S::PP;
   extern __shared__ float4 raw[];
   float* qs = reinterpret_cast<float*>(raw);
-  float* ks = qs + BM * QP;
-  float* vs = ks + BN * QP;
-  float* ps = vs + BN * D;
+  float* kv = qs + BM * QP;
+  float* ps = kv + 2 * S::KV;
   const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
   const int split = blockIdx.x % p.splits, row0 = (int)(blockIdx.x / p.splits) * BM, hk = blockIdx.y, b = blockIdx.z;
   const int rows = clamp_length(p.q_lengths, b, p.q_tokens) * p.group;
@@ -82,21 +86,26 @@ __global__ void __launch_bounds__(THREADS) cross_kernel(const __grid_constant__ 
 #pragma unroll
     for (int c = 0; c < E / 2; ++c) o[a][c] = pack2(0.f, 0.f);
   }
-  for (int j = j0; j < j1; j += BN) {
-    __syncthreads();                   // the last tile's reads
-    bool odd = false;
+  auto fetch = [&](int j, float* dst) {
     for (int i = threadIdx.x; i < BN * (D / 4); i += THREADS) {
       const int r = i / (D / 4), c = i % (D / 4) * 4;
-      float4 f = make_float4(0.f, 0.f, 0.f, 0.f), g = f;
-      if (j + r < j1) {
-        f = *reinterpret_cast<const float4*>(k + (int64_t)(j + r) * p.k.t + c);
-        g = *reinterpret_cast<const float4*>(v + (int64_t)(j + r) * p.v.t + c);
-      }
-      if (p.mask) odd |= !all_finite(g);
-      *reinterpret_cast<float4*>(ks + r * QP + c) = f;
-      *reinterpret_cast<float4*>(vs + r * D + c) = g;
+      const bool there = j + r < j1;
+      const int64_t at = there ? j + r : 0;
+      copy16(dst + r * QP + c, k + at * p.k.t + c, there);
+      copy16(dst + BN * QP + r * D + c, v + at * p.v.t + c, there);
     }
-    const bool careful = __syncthreads_or(odd) && p.mask;
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  if (j0 < j1) fetch(j0, kv);
+  for (int j = j0; j < j1; j += BN) {
+    const float* ks = kv + ((j - j0) / BN & 1) * S::KV;
+    const float* vs = ks + BN * QP;
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    bool odd = false;
+    if (p.mask)
+      for (int i = threadIdx.x; i < BN * (D / 4); i += THREADS) odd |= !all_finite(*reinterpret_cast<const float4*>(vs + i * 4));      // its own copies
+    const bool careful = __syncthreads_or(odd) && p.mask;      // the tile is there, and the one before has been read: the next one takes its place
+    if (j + BN < j1) fetch(j + BN, kv + ((j - j0) / BN + 1 & 1) * S::KV);
     float s[A][N];
     {
       Two acc[A][N];                   // even and odd elements
@@ -148,12 +157,12 @@ __global__ void __launch_bounds__(THREADS) cross_kernel(const __grid_constant__ 
       for (int x = 8; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
       top *= p.scale_log2;
       const float now = fmaxf(m[a], top), base = now == -INFINITY ? 0.f : now;
-      const float fade = exp2f(m[a] - base);
+      const float fade = exp2_fast(m[a] - base);
       m[a] = now;
       float add = 0.f;
 #pragma unroll
       for (int c = 0; c < N; ++c) {
-        const float w = seen[c] ? exp2f(fmaf(s[a][c], p.scale_log2, -base)) : -0.f;
+        const float w = seen[c] ? exp2_fast(fmaf(s[a][c], p.scale_log2, -base)) : -0.f;
         add += w;
         ps[(ty + 16 * a) * PP + tx + 16 * c] = w;
       }
