@@ -6,8 +6,9 @@
 // r / group, head r % group), so that shared heads read K and V once.  Where the row tiles alone do not fill the device the keys
 // are split over blocks, each leaves its sum, maximum and total, and cross_join_kernel joins them in order.
 //
-// Bound by the fp32 units: 1023 queries of 2 heads of 32 over one of keys and values on 4096 keys take 50 us, 1.1 GFLOP of products beside as many
-// exponentials as the special-function units make in 2 us.
+// Bound by what the fp32 units read from shared memory, a load of 16 bytes for four packed multiply-adds at most: 1023 queries of 2 heads of 32
+// over one of keys and values on 4096 keys take 46.6 us, 1.1 GFLOP of products (15 us of the units alone) and 2 us of exponentials.  (Weights kept
+// twice, as the pairs that the multiply-adds take: fewer instructions, more loads, 55 us.)
 //
 // A masked weight is kept as -0: it adds nothing to a finite value, and where a tile of V holds an infinity or NaN its sign
 // tells the slow loop to leave it out.
