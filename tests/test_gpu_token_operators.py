@@ -180,6 +180,46 @@ def test_linear_attention_slots_and_lengths(cuda_device, dtype, T):
     assert torch.equal(state[rest], old[rest])
 
 
+@pytest.mark.parametrize("B,T,H", [(38, 4000, 4), (8, 6000, 4), (1, 9000, 2)])      # a block to a sequence, segments of many chunks and of few
+def test_linear_attention_state_of_a_long_sequence_is_not_cut_short(cuda_device, B, T, H):
+    """Keys and values above 0 and no decay: sums that only grow, of which every addition that cuts off where it should round takes a part."""
+    g = _gen(cuda_device, T)
+    q, k, v = (torch.rand(B, T, H, 64, generator=g, device=cuda_device).to(BF16) for _ in range(3))
+    state = torch.zeros(B, H, 64, 64, device=cuda_device)
+    out, new = binding.linear_attention(q, k, v, torch.zeros(H, device=cuda_device), state.clone(), scale=0.01)
+    want = torch.einsum("bthd,bthe->bhde", k.double(), v.double())
+    # a product of two chunks is 48 instructions, whose sums may each be short of two steps of fp32; products, segments and the state are added with a
+    # rounding each.  (A sum of all chunks in one accumulator is short of a step for every instruction: 24 in a chunk, 1.1e-4 of 6000 tokens.)
+    check(new, want, (48 * 2.0 ** -22 + (T // 128 + 8) * 2.0 ** -24) * want, "state")
+
+
+def test_two_linear_calls_at_once(cuda_device):
+    """Side by side on two streams, eager and captured: each has scratch of its own."""
+    cases = [_linear_case(cuda_device, 40 + i, 3, 2000, 4, 2, 64, BF16) for i in range(2)]
+    want = [[x.clone() for x in binding.linear_attention(q, k, v, d, s.clone(), scale=0.1)] for q, k, v, d, s in cases]
+    streams, graphs, got = [torch.cuda.Stream() for _ in range(2)], [], []
+    torch.cuda.synchronize()
+    for (q, k, v, d, s), st in zip(cases, streams):
+        graph, out = torch.cuda.CUDAGraph(), (torch.empty_like(want[0][0]), torch.empty_like(s))
+        with torch.cuda.graph(graph, stream=st):
+            binding.linear_attention(q, k, v, d, s, scale=0.1, out=out[0], state_out=out[1])
+        graphs.append(graph)
+        got.append(out)
+    for _ in range(5):
+        for graph, st in zip(graphs, streams):
+            with torch.cuda.stream(st):
+                graph.replay()
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    for _ in range(5):
+        for i, ((q, k, v, d, s), st) in enumerate(zip(cases, streams)):
+            binding.linear_attention(q, k, v, d, s, scale=0.1, out=got[i][0], state_out=got[i][1], stream=st)
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("D", [32, 64, 128])
 def test_linear_attention_does_not_look_ahead(cuda_device, dtype, D):
