@@ -98,16 +98,28 @@ __device__ __noinline__ void own_sums(float* out, const float* q, const float* S
   }
 }
 
-// m rows of D elements into shared memory as fp32, zeros behind them
-template <int D>
-__device__ __forceinline__ void fetch(float* dst, int pitch, const float* src, int64_t stride, int m, int rows) {
-  for (int i = threadIdx.x; i < rows * (D / 4); i += THREADS) {
-    const int r = i / (D / 4), c = i % (D / 4) * 4;
-    float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (r < m) f = *reinterpret_cast<const float4*>(src + r * stride + c);
-    *reinterpret_cast<float4*>(dst + r * pitch + c) = f;
+// Rows of D elements on their way into shared memory, zeros behind the m-th.  All loads come before the first store, which might, for all the
+// compiler knows, change what a later load finds: one latency for a tile, not one for each of a thread's loads.
+template <int D, int ROWS>
+struct Tile {
+  static constexpr int N = ROWS * (D / 4) / THREADS;
+  static_assert(ROWS * (D / 4) % THREADS == 0, "whole rounds");
+  float4 f[N];
+  __device__ __forceinline__ void load(const float* src, int64_t stride, int m) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int i = threadIdx.x + n * THREADS, r = i / (D / 4);
+      f[n] = r < m ? *reinterpret_cast<const float4*>(src + r * stride + i % (D / 4) * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
   }
-}
+  __device__ __forceinline__ void store(float* dst, int pitch) const {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int i = threadIdx.x + n * THREADS;
+      *reinterpret_cast<float4*>(dst + i / (D / 4) * pitch + i % (D / 4) * 4) = f[n];
+    }
+  }
+};
 
 template <int D, bool WITH_OUT>
 __device__ __forceinline__ void run_chunks(const LinearParams& p, int b, int h, int t0, int t1, float* S, float* smem) {
@@ -126,10 +138,14 @@ __device__ __forceinline__ void run_chunks(const LinearParams& p, int b, int h, 
   if (threadIdx.x <= C) pw[threadIdx.x] = decay_power(p.log_decay[h], threadIdx.x);
   for (int t = t0; t < t1; t += C) {
     const int m = min(C, t1 - t);
+    Tile<D, C> tq, tk, tv;
+    if (WITH_OUT) tq.load(gq + t * p.q.t, p.q.t, m);
+    tk.load(gk + t * p.k.t, p.k.t, m);
+    tv.load(gv + t * p.v.t, p.v.t, m);
     __syncthreads();                   // the state, and the last chunk's reads
-    if (WITH_OUT) fetch<D>(q, QP, gq + t * p.q.t, p.q.t, m, C);
-    fetch<D>(k, QP, gk + t * p.k.t, p.k.t, m, C);
-    fetch<D>(v, D, gv + t * p.v.t, p.v.t, m, C);
+    if (WITH_OUT) tq.store(q, QP);
+    tk.store(k, QP);
+    tv.store(v, D);
     __syncthreads();
     if (WITH_OUT) {
       Two acc[A][A];                   // even and odd elements
@@ -286,7 +302,9 @@ __global__ void __launch_bounds__(THREADS) linear_chunk_kernel(const __grid_cons
   if (seg > 0 && t0 >= n) return;
   const int64_t at = ((int64_t)slot * p.heads + h) * D * D;
   const float* src = p.segments > 1 ? p.seg_state + (((int64_t)b * p.heads + h) * p.segments + seg) * D * D : p.state + at;
-  for (int i = threadIdx.x; i < D * D; i += THREADS) S[i] = src[i];
+  Tile<D, D> first;
+  first.load(src, D, D);
+  first.store(S, D);
   run_chunks<D, true>(p, b, h, t0, t1, S, smem);
   if (t1 == n)
     for (int i = threadIdx.x; i < D * D; i += THREADS) p.state_out[at + i] = S[i];
