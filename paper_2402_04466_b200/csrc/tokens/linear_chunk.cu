@@ -8,8 +8,8 @@
 // segments: linear_segment_kernel forms what each segment adds to the state, linear_scan_kernel turns that into the state
 // before each segment, and linear_chunk_kernel then runs all segments at once.  K and V are read twice then.
 //
-// Bound by the fp32 units and what feeds them from shared memory.  Two sequences of 4801 tokens, 2 heads of 64 over one of keys and values: 58 us, 20
-// of them the segments' sums and 33 out: one or two blocks to a multiprocessor, each a chain of two chunks.
+// Bound by the fp32 units and what feeds them from shared memory, with eight warps to a multiprocessor.  Two sequences of 4801 tokens, 2 heads of 64 over
+// one of keys and values: 43 us, a third of it the segments' sums; a block has a chain of three chunks.
 #include "linear_common.cuh"
 #include "token_ptx.cuh"
 
@@ -328,11 +328,12 @@ cudaError_t launch(const LinearParams& p, cudaStream_t s) {
 }
 }  // namespace
 
-// Two blocks of fp32, one of bf16 (whose chunks overlap in a block) to a multiprocessor.
+// One block to a multiprocessor: a few with two would be what the rest waits for (fp32, 2 x 2 heads of 64 on 4801 tokens: 152 segments of 128
+// tokens 49 us, 124 of 160 tokens 43).  bf16 segments are whole chunks; three launches are not worth it for less than 128 tokens more.
 void linear_plan(int batch, int tokens, int heads, bool bf16, int* segments, int* seg_tokens) {
   const int64_t sequences = (int64_t)batch * heads;
-  const int step = 128;
-  const int64_t most = ((int64_t)tokens + step - 1) / step, want = (bf16 ? 1 : 2) * PLAN_SMS / sequences;
+  const int step = bf16 ? 128 : 32;
+  const int64_t most = ((int64_t)tokens + 127) / 128, want = PLAN_SMS / sequences;
   int64_t n = want < most ? want : most;
   if (n < 1) n = 1;
   const int64_t each = tokens > 0 ? ((tokens + n - 1) / n + step - 1) / step * step : step;
