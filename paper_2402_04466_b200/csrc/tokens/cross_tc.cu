@@ -415,6 +415,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) cross_tc_kernel(const __gr
           w[x] = pack_bf16(lo, hi);
         }
         if (C::TURNS && i == C::BN / 32 - 2 && lane == 0) mbar_arrive(smem_u32(turns + 2 * quarter + 1 - t));      // the other's wait takes about as long as the rest
+        __syncwarp();                  // its first lane has signalled
         tmem_st16(p_addr + (uint32_t)((it & (C::PLACES - 1)) * (C::BN / 2) + 16 * i), w);
         if (i & 1) {
           tmem_wait_st();
@@ -437,6 +438,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) cross_tc_kernel(const __gr
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) {
           uint32_t o[32];
+          __syncwarp();                // only some lanes' rows are stored
           tmem_ld32(o_addr + 32 * i, o);
           if (here) {
 #pragma unroll
@@ -453,6 +455,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) cross_tc_kernel(const __gr
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) {
           uint32_t o[32];
+          __syncwarp();                // only some lanes' rows are stored
           tmem_ld32(o_addr + 32 * i, o);
           if (here) {
 #pragma unroll

@@ -313,6 +313,7 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
 #pragma unroll
       for (int i0 = 0; i0 < PIECES; i0 += BATCH) {
         uint32_t y[BATCH][16], z[BATCH][16];
+        __syncwarp();                  // lanes whose token is none, or whose sums were taken again, have parted from the rest
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
           tmem_ld16_async(lanes + C::PV_COL + (uint32_t)(place(c) * D + c0 + 16 * (i0 + i)), y[i]);
@@ -389,6 +390,7 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
             }
           }
         }
+        __syncwarp();                  // on the diagonal every lane has weights of its own number
         tmem_st16(lanes + C::A_COL + (uint32_t)(s * CT + 64 * half + 16 * y), w);
       }
       tmem_wait_st();
@@ -433,6 +435,7 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
         }
     };
     auto add_product = [&](int group, float g) {      // S = g S + product, which is done
+      __syncwarp();
       tc_fence_after();
       const uint32_t from_col = lanes + (uint32_t)((group & (C::S_PLACES - 1)) * C::N + c0);
       if constexpr (C::SIDE) {

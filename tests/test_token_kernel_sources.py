@@ -73,3 +73,36 @@ def test_tensor_memory_is_given_back_on_every_way_out(name):
 def test_no_spin_without_a_limit():
     for name, code in SOURCES.items():
         assert "cuda::barrier" not in code and not re.search(r"while \(true\)|for \(;;\)|ld\.acquire|volatile.*while", code), name
+
+
+def _block(code, at):
+    """From the brace that opens at or behind `at` to the one that closes it."""
+    start = code.index("{", at)
+    depth, end = 1, start + 1
+    while depth:
+        depth += {"{": 1, "}": -1}.get(code[end], 0)
+        end += 1
+    return code[start:end]
+
+
+PARTS = r"if \(lane == 0\)|if \(here\)|if \(has_row\)|if \(!has_row\)|\? __uint_as_float|\bcontinue;|\bown_\w+<|\barrive\(\w"
+MEETS = r"__syncwarp\(\)|__syncthreads\(\)|__(?:all|any)_sync\(|\bwait\w*\(\w+ [+,]"
+
+
+@pytest.mark.parametrize("name,loops", [("cross_tc.cu", 3), ("linear_tc.cu", 3)])
+def test_lanes_meet_before_a_warp_touches_tensor_memory(name, loops):
+    """Loads and stores of tensor memory are of a whole warp in step.  Going round each loop that has one, no lane-dependent step comes last
+    before it: the lanes have met in between."""
+    code = SOURCES[name]
+    bodies = [b for b in (_block(code, m.end() - 1) for m in re.finditer(r"\bfor \([^;{}]*;[^;{}]*;[^{};]*\)\s*\{", code))
+              if re.search(r"\btmem_(?:ld|st)\d", b) and re.search(PARTS, b)]
+    assert len(bodies) >= loops
+    for body in bodies:
+        apart = None
+        for e in re.finditer(f"(?P<part>{PARTS})|(?P<meet>{MEETS})|(?P<take>\\btmem_(?:ld|st)\\d\\w*\\()", body + body):
+            if e.lastgroup == "part":
+                apart = e.group()
+            elif e.lastgroup == "meet":
+                apart = None
+            else:
+                assert apart is None, (name, apart, (body + body)[max(0, e.start() - 400):e.end()])
