@@ -554,10 +554,11 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
   if (*abort_flag) {
     // a wait ran out: give copies and MMAs in flight time to land before their memory is released
     for (int i = 0; i < 64; ++i) __nanosleep(16000);
-    if (threadIdx.x == 0 && p.status) atomicCAS(p.status, 0, *(volatile int*)s_status);
   }
   tc_fence_before();
   __syncthreads();
+  // behind the barrier: the first thread may have been through with its own work when another warp's wait ran out
+  if (threadIdx.x == 0 && *abort_flag && p.status) atomicCAS(p.status, 0, *(volatile int*)s_status);
   if (warp == W_B) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::TMEM) : "memory");

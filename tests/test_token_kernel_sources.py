@@ -106,3 +106,13 @@ def test_lanes_meet_before_a_warp_touches_tensor_memory(name, loops):
                 apart = None
             else:
                 assert apart is None, (name, apart, (body + body)[max(0, e.start() - 400):e.end()])
+
+
+@pytest.mark.parametrize("name", ["cross_tc.cu", "linear_tc.cu"])
+def test_a_wait_that_ran_out_is_reported_whichever_warp_it_was(name):
+    """One thread reports for its block, and its own warp may long have been through when another one's wait runs out: it looks behind the
+    barrier at which all of them meet, and nothing leaves the block before."""
+    code = SOURCES[name]
+    assert code.count("atomicCAS(p.status") == 1 and not re.search(r"p\.status, WAIT_", code)
+    tail = code[code.rindex("__syncthreads()", 0, code.index("tcgen05.dealloc")):code.index("tcgen05.dealloc")]
+    assert re.search(r"if \(threadIdx\.x == 0 && \*abort_flag && p\.status\) atomicCAS\(p\.status, 0, ", tail)
