@@ -535,6 +535,7 @@ tt_status tt_linear_attention(const tt_linear_attention_args* args, void* cuda_s
  * mask_query_stride + j] is not 0: the bytes that tt_postprocess and tt_submit_frames write ([K][n_tools][Hm * Wm]) let each tool's query
  * read the places of its own mask.  Mask strides are in bytes, 0 or more; a query stride of 0 is one mask for all queries.
  * What a query does not see has no influence on its row, NaN and infinity included.  A query that sees nothing gets zeros.
+ * An infinity among the values that it sees is one of its row, or NaN where the key's weight is too small for fp32 (below 2^-126 of the largest).
  * scale is above 0 and below 1e38.  q_lengths: rows of out behind them are left as they were.
  * status_dev: as in tt_linear_attention.
  */
