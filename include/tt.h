@@ -501,6 +501,8 @@ tt_status tt_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, dou
  * and head, in order of the tokens, with S the head's state [head_dim (key)][head_dim (value)]:
  *   S = exp(log_decay[head]) * S + k_t v_t^T;   out_t = scale * q_t S.
  * A call of several tokens works in chunks, one of a single token per entry reads and writes the states once.
+ * An infinity or NaN in a token or a state reaches the elements of the state that the formula gives it to, as what the formula gives (an infinity that
+ * has faded by a factor too small for fp32 may be a NaN), and makes the elements of out that read those, from its token on, not finite; no earlier ones.
  * log_decay: device fp32 [heads], 0 or below (-infinity: a state that was finite is the newest token's alone).
  * state, state_out: device fp32 [num_slots][heads][head_dim][head_dim], 16-byte aligned; entry b starts from its slot of `state` and leaves its last
  * state in the same slot of state_out.  The two may be one buffer; slots that no entry names are left as they were.
@@ -535,7 +537,7 @@ tt_status tt_linear_attention(const tt_linear_attention_args* args, void* cuda_s
  * mask_query_stride + j] is not 0: the bytes that tt_postprocess and tt_submit_frames write ([K][n_tools][Hm * Wm]) let each tool's query
  * read the places of its own mask.  Mask strides are in bytes, 0 or more; a query stride of 0 is one mask for all queries.
  * What a query does not see has no influence on its row, NaN and infinity included.  A query that sees nothing gets zeros.
- * An infinity among the values that it sees is one of its row, or NaN where the key's weight is too small for fp32 (below 2^-126 of the largest).
+ * An infinity among the values that it sees is one of its row, or NaN where the key's weight is too small for fp32 (about 2^-126 of the largest).
  * scale is above 0 and below 1e38.  q_lengths: rows of out behind them are left as they were.
  * status_dev: as in tt_linear_attention.
  */

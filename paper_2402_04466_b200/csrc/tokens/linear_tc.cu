@@ -86,6 +86,25 @@ __device__ __noinline__ void own_sums(const LinearParams& p, int b, int h, int t
   for (int i = 0; i < N; ++i) out[i] = __float2bfloat16(sum[i]);
 }
 
+// Elements of a lane's part of the state behind the tokens from t0 to t1, taken token by token: keys' columns col + i where bit i of `which` is set, value column
+// `row`.  from: the state before, or null.
+template <int D>
+__device__ __noinline__ void own_state(const LinearParams& p, int b, int h, int t0, int t1, const float* from, float* to, int col, int row, uint32_t which) {
+  const int hk = h / p.group;
+  const __nv_bfloat16* k = reinterpret_cast<const __nv_bfloat16*>(p.k.p) + b * p.k.b + hk * p.k.h + col;
+  const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(p.v.p) + b * p.v.b + hk * p.v.h + row;
+  const float decay = decay_power(p.log_decay[h], 1);
+#pragma unroll 1
+  for (int i = 0; which; ++i, which >>= 1) {
+    if ((which & 1u) == 0u) continue;
+    float s = from ? from[(col + i) * D + row] : 0.f;
+    // a NaN stays one: a state that had gone bad before costs no time
+    for (int t = t0; t < t1 && !isnan(s); t += 8)
+      for (int x = t; x < min(t + 8, t1); ++x) s = fmaf(s, decay, __bfloat162float(k[x * p.k.t + i]) * __bfloat162float(v[x * p.v.t]));
+    to[(col + i) * D + row] = s;
+  }
+}
+
 template <int D, bool WITH_OUT>
 __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel(const __grid_constant__ LinearTcParams pp) {
   using C = Cfg<D, WITH_OUT>;
@@ -541,10 +560,27 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
       }
       if ((!WITH_OUT || t1 == len) && has_row) {
         float* to = WITH_OUT ? p.state_out + at : seg_state;
+        Two bad[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};      // two chains
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i)
+        for (int i = 0; i < 16 * PIECES; i += 2) bad[i / 2 & 1] = fma2_of(pack2(S[i / 16][i % 16], S[i / 16][i % 16 + 1]), pack2(0.f, 0.f), bad[i / 2 & 1]);
+        float b0, b1;
+        unpack2(add2_of(bad[0], bad[1]), b0, b1);
+        if (__builtin_expect(b0 + b1 == 0.f, 1)) {
 #pragma unroll
-          for (int x = 0; x < 16; ++x) to[(c0 + 16 * i + x) * D + row] = S[i][x];
+          for (int i = 0; i < 16 * PIECES; ++i) to[(c0 + i) * D + row] = S[i / 16][i % 16];
+        } else {
+          // the terms that K' is cut into make NaN where k v is an infinity
+#pragma unroll
+          for (int i = 0; i < PIECES; ++i) {
+            uint32_t which = 0;
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+              if (isfinite(S[i][x])) to[(c0 + 16 * i + x) * D + row] = S[i][x];
+              else which |= 1u << x;
+            }
+            own_state<D>(p, b, h, t0, t1, WITH_OUT ? from : nullptr, to, c0 + 16 * i, row, which);
+          }
+        }
       }
     }
   }

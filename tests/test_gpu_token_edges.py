@@ -55,3 +55,27 @@ def test_an_infinity_that_a_query_sees_is_an_infinity_of_its_row(cuda_device, dt
     assert not torch.isfinite(want).all() and torch.isinf(want).any()
     _same_kind(got, want, "out")
     _finite_check(got, want, ref.cross_bounds(want, size, score, D, Tk, dtype, 0.0 if dtype == FP32 else 2.0 ** -8), "out")
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,T,H,K,D", [(3, 1, 2, 1, 64), (3, 60, 2, 2, 64), (3, 333, 2, 1, 32), (3, 333, 2, 2, 128), (3, 1300, 4, 4, 64),
+                                       (3, 2900, 2, 2, 128), (40, 300, 4, 4, 64), (40, 500, 4, 2, 128), (8, 2500, 4, 4, 32)])
+def test_an_infinity_of_a_key_or_value_is_an_infinity_of_the_state(cuda_device, dtype, B, T, H, K, D):
+    """k v^T of an infinity is one wherever the other factor is not 0, and it stays one while no decay has faded to 0."""
+    g = torch.Generator(device=cuda_device).manual_seed(T + D)
+    q, k, v = (_normal(g, cuda_device, (B, T, n, D), dtype) for n in (H, K, K))
+    for x in (q, k, v):
+        x[x == 0] = 1
+    decay = torch.tensor([-0.01, -0.002, 0.0, -0.02], device=cuda_device)[:H]
+    state = torch.randn(B, H, D, D, generator=g, device=cuda_device)
+    late, early = T - 1 - T // 5, T // 7
+    k[0, late, 0, 5], k[0, early, 0, D - 1] = math.inf, -math.inf
+    v[1, late, 0, 7], v[1, early, 0, 0] = -math.inf, math.inf
+    state[2, 0, 3, 4], state[2, H - 1, 9, 0] = math.inf, -math.inf
+    v[2, T - 1, 0, D - 1] = math.inf
+    out, new = binding.linear_attention(q, k, v, decay, state, scale=0.1, state_out=torch.empty_like(state))
+    want, size, S, A = ref.linear(q, k, v, decay, state, 0.1, None)
+    assert torch.isinf(S).any(-1).any(-1)[:3].any(-1).all()
+    _same_kind(new, S, "state")
+    _same_kind(out, want, "out", signs=False)      # an infinity of the state meets q's signs, a chunk's own q k first: either sum is not finite
+    bound, state_bound = ref.linear_bounds(want, size, A, D, T, dtype, dtype == FP32 or T == 1)
+    _finite_check(new, S, state_bound, "state")
+    _finite_check(out, want, bound, "out")
