@@ -2,7 +2,7 @@
 //   S' = exp(log_decay) S + k v^T,  out = scale * q S'.
 // Bound by memory: the fp32 state is read and written once and everything else is small beside it.  A block owns a run of W value columns of
 // one head's state (the columns are independent of each other), LANES = W / 4 threads to a row, all of its loads in flight
-// together (256 streams of 8 heads of 128: 46.8 us, 5.8 TB/s, 88 % of a plain copy's rate; five of 2 heads of 64: 3.1 us, a launch).  The sum over the rows goes through shuffles and then shared memory, always in the same order.
+// together (256 streams of 8 heads of 128: 45.4 us, 6.0 TB/s, 91 % of a plain copy's rate; five of 2 heads of 64: 2.9 us, a launch).  The sum over the rows goes through shuffles and then shared memory, always in the same order.
 #include "linear_common.cuh"
 
 namespace tt {
@@ -22,30 +22,28 @@ __global__ void __launch_bounds__(256) linear_step_kernel(const __grid_constant_
   constexpr int LANES = Shape::LANES, ROWS = Shape::ROWS, STEP = Shape::THREADS / LANES, WARPS = Shape::THREADS / 32;
   __shared__ float4 sums[WARPS][LANES];
   const int b = blockIdx.z, h = blockIdx.y, col = (int)blockIdx.x * W + (int)(threadIdx.x % LANES) * 4, row = threadIdx.x / LANES;
-  const int at = p.slots ? p.slots[b] : b;
-  const bool in_range = at >= 0 && at < p.num_slots;
   const bool has = clamp_length(p.lengths, b, 1) == 1;
-  const int64_t base = ((int64_t)(in_range ? at : 0) * p.heads + h) * D * D + (int64_t)row * D + col;
+  // before any of its data is touched: the slot of an entry that is passed over may be one that an earlier entry is writing
+  const int slot = slot_of(p.slots, p.num_slots, b);
+  if (slot < 0) return;                // the whole block
+  const int64_t base = ((int64_t)slot * p.heads + h) * D * D + (int64_t)row * D + col;
   float4 s[ROWS];
   float kk[ROWS], qq[ROWS], v[4];
   const int hk = h / p.group;
   const T* q = reinterpret_cast<const T*>(p.q.p) + b * p.q.b + h * p.q.h;
   const T* k = reinterpret_cast<const T*>(p.k.p) + b * p.k.b + hk * p.k.h;
   const T* vv = reinterpret_cast<const T*>(p.v.p) + b * p.v.b + hk * p.v.h;
-  if (in_range) {
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) s[i] = *reinterpret_cast<const float4*>(p.state + base + (int64_t)i * STEP * D);
-    if (has) {
+  for (int i = 0; i < ROWS; ++i) s[i] = *reinterpret_cast<const float4*>(p.state + base + (int64_t)i * STEP * D);
+  if (has) {
 #pragma unroll
-      for (int i = 0; i < ROWS; ++i) {
-        kk[i] = to_float(k[row + i * STEP]);
-        qq[i] = to_float(q[row + i * STEP]) * p.scale;
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = to_float(vv[col + j]);
+    for (int i = 0; i < ROWS; ++i) {
+      kk[i] = to_float(k[row + i * STEP]);
+      qq[i] = to_float(q[row + i * STEP]) * p.scale;
     }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = to_float(vv[col + j]);
   }
-  if (slot_of(p.slots, p.num_slots, b) < 0) return;      // the whole block
   float* out_state = p.state_out + base;
   if (!has) {
     if (p.state_out != p.state)

@@ -116,3 +116,15 @@ def test_a_wait_that_ran_out_is_reported_whichever_warp_it_was(name):
     assert code.count("atomicCAS(p.status") == 1 and not re.search(r"p\.status, WAIT_", code)
     tail = code[code.rindex("__syncthreads()", 0, code.index("tcgen05.dealloc")):code.index("tcgen05.dealloc")]
     assert re.search(r"if \(threadIdx\.x == 0 && \*abort_flag && p\.status\) atomicCAS\(p\.status, 0, ", tail)
+
+
+@pytest.mark.parametrize("name,kernels", [("linear_step.cu", 1), ("linear_tc.cu", 1), ("linear_chunk.cu", 3)])
+def test_nothing_of_an_entry_is_read_before_its_slot_is_known_to_be_its_own(name, kernels):
+    """An entry that is passed over shares its slot with an earlier one, which may be writing it: the block leaves before it reads states or tokens."""
+    bodies = [_block(SOURCES[name], m.end()) for m in re.finditer(r"__global__", SOURCES[name])]
+    assert len(bodies) == kernels
+    for body in bodies:
+        slot = body.index("slot_of(")
+        gone = re.search(r"slot_of\([^)]*\) < 0\) return;|if \(slot < 0\) return;", body[slot:]).start() + slot
+        reads = [m.start() for m in re.finditer(r"p\.(?:state|seg_state)\b|\*reinterpret_cast<const|to_float\(|tma_load|run_chunks<|\.load\(", body)]
+        assert reads and min(reads) > gone
