@@ -440,7 +440,8 @@ tt_status tt_render_layers(const uint8_t* src_dev, int32_t K, int64_t src_frame_
  *   - precision TT_BF16 or TT_FP32 is the type of q, k, v and the outputs; sums, statistics and states are fp32;
  *   - an operand is a tt_tokens view [batch][token][head][head_dim]: the last axis is contiguous, the strides of the others are
  *     counted in elements and may come in any order; they are 0 to 2^38 (inputs: a batch or head stride of 0 shares the data along that axis)
- *     and, like the data pointer, whole multiples of 16 bytes.  Outputs overlap no input, unless a call says otherwise;
+ *     and, like the data pointer, whole multiples of 16 bytes; that of an axis of extent 1 is not looked at.  Outputs overlap no input, unless a call says
+ *     otherwise;
  *   - heads shared by groups: kv_heads divides heads, head h uses key and value head h / (heads / kv_heads);
  *   - `lengths` arrays (device, int32 [batch], NULL: all tokens) say how many tokens an entry of the batch has, and are taken
  *     as 0 or as the tensor's extent where they lie outside.  Rows behind an entry's last token are neither read

@@ -21,13 +21,14 @@ bool bad_view(const char* who, const char* name, const tt_tokens& v, int64_t bat
   if (batch * tokens * heads == 0) return false;
   if (!v.data) return set_error(TT_ERR_INVALID_ARG, "%s: %s is null", who, name), true;
   const int64_t unit = 16 / size, limit = MAX_REACH;
-  if (misaligned(v.data, 16) || v.batch_stride % unit || v.token_stride % unit || v.head_stride % unit)
-    return set_error(TT_ERR_INVALID_ARG, "%s: %s must start on 16 bytes, and its strides be whole multiples of them", who, name), true;
+  if (misaligned(v.data, 16)) return set_error(TT_ERR_INVALID_ARG, "%s: %s must start on 16 bytes", who, name), true;
   if (tokens > 1 && v.token_stride == 0) return set_error(TT_ERR_INVALID_ARG, "%s: token_stride of %s is 0", who, name), true;
   const int64_t strides[3] = {v.batch_stride, v.token_stride, v.head_stride}, extents[3] = {batch, tokens, heads};
   int64_t reach = 0;
   for (int i = 0; i < 3; ++i) {
-    if (strides[i] < 0 || strides[i] > MAX_STRIDE || (extents[i] > 1 && strides[i] > (limit - reach) / (extents[i] - 1)))
+    if (extents[i] == 1) continue;             // never stepped along: whatever it says
+    if (strides[i] % unit) return set_error(TT_ERR_INVALID_ARG, "%s: strides of %s must be whole multiples of 16 bytes", who, name), true;
+    if (strides[i] < 0 || strides[i] > MAX_STRIDE || strides[i] > (limit - reach) / (extents[i] - 1))
       return set_error(TT_ERR_INVALID_ARG, "%s: a stride of %s is negative or too large", who, name), true;
     reach += strides[i] * (extents[i] - 1);
   }
@@ -50,7 +51,10 @@ bool folded(const char* who, const char* name, const tt_tokens& v, int64_t batch
   return false;
 }
 
-View view(const tt_tokens& v) { return {v.data, v.batch_stride, v.token_stride, v.head_stride}; }
+// Strides of axes of extent 1 are taken as 0.
+View view(const tt_tokens& v, int64_t batch, int64_t tokens, int64_t heads) {
+  return {v.data, batch > 1 ? v.batch_stride : 0, tokens > 1 ? v.token_stride : 0, heads > 1 ? v.head_stride : 0};
+}
 
 bool bad_head_dim(const char* who, int32_t d) {
   if (d == 32 || d == 64 || d == 128) return false;
@@ -82,7 +86,8 @@ tt_status tt_qk_norm_rope(const tt_qk_norm_rope_args* a, void* cuda_stream) {
     return set_error(TT_ERR_INVALID_ARG, "%s: misaligned pointer", who);
   if (a->tokens == 0) return TT_OK;
   RopeParams p{};
-  p.x[0] = view(a->q); p.x[1] = view(a->k); p.y[0] = view(a->q_out); p.y[1] = view(a->k_out);
+  p.x[0] = view(a->q, a->batch, a->tokens, a->q_heads); p.x[1] = view(a->k, a->batch, a->tokens, a->k_heads);
+  p.y[0] = view(a->q_out, a->batch, a->tokens, a->q_heads); p.y[1] = view(a->k_out, a->batch, a->tokens, a->k_heads);
   p.weight[0] = a->norm ? a->q_weight : nullptr; p.weight[1] = a->norm ? a->k_weight : nullptr;
   p.positions = a->positions; p.inv_freq = a->inv_freq; p.lengths = a->lengths; p.pos_stride = a->position_stride;
   p.tokens = a->tokens; p.heads[0] = a->q_heads; p.heads[1] = a->k_heads; p.rot = a->rot_dim; p.norm = a->norm != 0;
@@ -149,7 +154,8 @@ tt_status tt_linear_attention(const tt_linear_attention_args* a, void* cuda_stre
   if (need && (!a->scratch || misaligned(a->scratch, 16) || a->scratch_bytes < need))
     return set_error(TT_ERR_INVALID_ARG, "%s: scratch is null, misaligned or smaller than %llu bytes", who, (unsigned long long)need);
   LinearParams p{};
-  p.q = view(a->q); p.k = view(a->k); p.v = view(a->v); p.o = view(a->out);
+  p.q = view(a->q, a->batch, a->tokens, a->heads); p.k = view(a->k, a->batch, a->tokens, a->kv_heads);
+  p.v = view(a->v, a->batch, a->tokens, a->kv_heads); p.o = view(a->out, a->batch, a->tokens, a->heads);
   p.log_decay = a->log_decay; p.state = a->state; p.state_out = a->state_out; p.slots = a->slots; p.lengths = a->lengths;
   p.seg_state = static_cast<float*>(a->scratch); p.status = a->status_dev;
   p.batch = a->batch; p.tokens = a->tokens; p.heads = a->heads; p.group = a->heads / a->kv_heads; p.num_slots = a->num_slots;
@@ -198,7 +204,8 @@ tt_status tt_cross_attention(const tt_cross_attention_args* a, void* cuda_stream
     return set_error(TT_ERR_INVALID_ARG, "%s: scratch is null, misaligned or smaller than %llu bytes", who, (unsigned long long)plan.scratch);
   if (a->q_tokens == 0) return TT_OK;
   CrossParams p{};
-  p.q = view(a->q); p.k = view(a->k); p.v = view(a->v); p.o = view(a->out);
+  p.q = view(a->q, a->batch, a->q_tokens, a->heads); p.k = view(a->k, a->batch, a->kv_tokens, a->kv_heads);
+  p.v = view(a->v, a->batch, a->kv_tokens, a->kv_heads); p.o = view(a->out, a->batch, a->q_tokens, a->heads);
   p.q_lengths = a->q_lengths; p.kv_lengths = a->kv_lengths; p.mask = a->mask; p.mask_b = a->mask_batch_stride; p.mask_q = a->mask_query_stride;
   p.part = static_cast<float*>(a->scratch); p.status = a->status_dev;
   p.batch = a->batch; p.q_tokens = a->q_tokens; p.kv_tokens = a->kv_tokens; p.heads = a->heads; p.group = a->heads / a->kv_heads;

@@ -79,3 +79,26 @@ def test_an_infinity_of_a_key_or_value_is_an_infinity_of_the_state(cuda_device, 
     bound, state_bound = ref.linear_bounds(want, size, A, D, T, dtype, dtype == FP32 or T == 1)
     _finite_check(new, S, state_bound, "state")
     _finite_check(out, want, bound, "out")
+
+
+# ------------------------------------------------------------------------------- views
+def _odd(x):
+    """The same tensor, its axes of extent 1 with a stride that fits nothing."""
+    return x.as_strided(x.shape, [7 if n == 1 else s for n, s in zip(x.shape[:3], x.stride())] + [1])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,T,Tk,H", [(1, 1, 1, 1), (1, 7, 300, 1), (3, 1, 200, 2), (1, 1, 9000, 2), (1, 2000, 4000, 4), (2, 1, 1, 1), (1, 300, 1, 2)])
+def test_strides_of_axes_of_extent_one_change_nothing(cuda_device, dtype, B, T, Tk, H):
+    g = torch.Generator(device=cuda_device).manual_seed(B + T)
+    q = _normal(g, cuda_device, (B, T, H, 64), dtype)
+    k, v = (_normal(g, cuda_device, (B, T, 1, 64), dtype) for _ in range(2))
+    ck, cv = (_normal(g, cuda_device, (B, Tk, 1, 64), dtype) for _ in range(2))
+    new = lambda x: _odd(torch.zeros_like(x))      # noqa: E731
+    a, b = binding.qk_norm_rope(q, k), binding.qk_norm_rope(_odd(q), _odd(k), out=(new(q), new(k)))
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+    decay, state = torch.full((H,), -0.1, device=cuda_device), torch.randn(B, H, 64, 64, generator=g, device=cuda_device)
+    a, b = (binding.linear_attention(*x, decay, state, scale=0.1, state_out=torch.empty_like(state), out=o)
+            for x, o in (((q, k, v), None), ((_odd(q), _odd(k), _odd(v)), new(q))))
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+    assert torch.equal(binding.cross_attention(q, ck, cv), binding.cross_attention(_odd(q), _odd(ck), _odd(cv), out=new(q)))

@@ -169,3 +169,17 @@ def test_host_tensors_are_refused():
         binding.cross_attention(x, x, x)
     with pytest.raises(binding.TTError):
         binding.qk_norm_rope(None, None)
+
+
+@pytest.mark.parametrize("call,later,text", [("tt_qk_norm_rope", dict(positions=None), b"positions"), ("tt_linear_attention", dict(log_decay=None), b"log_decay"),
+                                             ("tt_cross_attention", dict(mask=A, mask_batch_stride=-1), b"mask stride")])
+@pytest.mark.parametrize("view", ["q", "k", "out"])
+@pytest.mark.parametrize("axis,extents", [("batch", ("batch",)), ("token", ("tokens", "q_tokens", "kv_tokens")), ("head", ("heads", "kv_heads", "q_heads", "k_heads"))])
+@pytest.mark.parametrize("stride", [3, 0, -64, 1 << 60])
+def test_strides_of_axes_of_extent_one_are_not_looked_at(call, later, text, view, axis, extents, stride):
+    """What is refused is the argument that is checked behind the views (nothing is launched), as with strides that would do for any extent."""
+    lib = binding.load_library()
+    over = {n: 1 for n in extents if n in dict(CALLS[call]()._fields_)}
+    names = [n for n, _ in CALLS[call]()._fields_ if n in ((view,) if view != "out" else ("out", "q_out", "k_out"))]
+    assert getattr(lib, call)(C.byref(CALLS[call](**over, **later, **{f"{n}__{axis}_stride": stride for n in names})), None) == 1
+    assert text in lib.tt_last_error(None)
