@@ -102,3 +102,87 @@ def test_strides_of_axes_of_extent_one_change_nothing(cuda_device, dtype, B, T, 
             for x, o in (((q, k, v), None), ((_odd(q), _odd(k), _odd(v)), new(q))))
     assert all(torch.equal(x, y) for x, y in zip(a, b))
     assert torch.equal(binding.cross_attention(q, ck, cv), binding.cross_attention(_odd(q), _odd(ck), _odd(cv), out=new(q)))
+
+
+# ------------------------------------------------------------------------------- long runs of chunks
+@pytest.mark.parametrize("B,T,H,D", [(8, 14400, 4, 64), (38, 4000, 4, 64), (8, 14400, 4, 32), (8, 14400, 2, 128), (75, 3000, 2, 128)])
+def test_sums_of_a_long_sequence_are_rounded_not_cut_off(cuda_device, B, T, H, D):
+    """Keys and values above 0, no decay: whatever an addition cuts off is missing from the state, always on the same side.  Products start from nothing every two
+    chunks at most, 16 instructions for the largest term, which lose half a step of a sum that is half grown: 17 / 2 of at most 0.75 / 2 * 2^-23, 3.8e-7 of
+    it; what is rounded is off to either side and not in the mean.  (One sum over all chunks lost 1.3e-6.)"""
+    g = torch.Generator(device=cuda_device).manual_seed(T + D)
+    q, k, v = (torch.rand(B, T, H, D, generator=g, device=cuda_device).to(BF16) for _ in range(3))
+    _, new = binding.linear_attention(q, k, v, torch.zeros(H, device=cuda_device), torch.zeros(B, H, D, D, device=cuda_device), scale=0.01)
+    want = torch.stack([torch.einsum("thd,the->hde", x.double(), y.double()) for x, y in zip(k, v)])
+    lost = ((want - new) / want).flatten(2).mean(-1)
+    assert lost.abs().max() < 5e-7, f"{float(lost.abs().max()):.2e}"
+
+
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("B,T,H,K", [(10, 1100, 15, 15), (8, 2000, 4, 2), (8, 2500, 4, 4), (8, 4500, 4, 4), (2, 5300, 30, 10)])
+def test_linear_attention_of_many_chunks_to_a_block(cuda_device, B, T, H, K, D):
+    """Four to nine chunks to a segment, odd and even, and nine to a sequence that is not cut: every place of operands, scores and sums is used more than once."""
+    g = torch.Generator(device=cuda_device).manual_seed(T + D)
+    q, k, v = (_normal(g, cuda_device, (B, T, n, D), BF16) for n in (H, K, K))
+    decay = torch.tensor([-0.002, -0.03, 0.0, -0.7, -6.0, -math.inf], device=cuda_device).repeat(5)[:H]
+    state = torch.randn(B, H, D, D, generator=g, device=cuda_device)
+    lengths = [T - 97 * b for b in range(B)]
+    for n in (None, torch.tensor(lengths, dtype=torch.int32, device=cuda_device)):
+        out, new = binding.linear_attention(q, k, v, decay, state, scale=D ** -0.5, state_out=torch.empty_like(state), lengths=n)
+        if n is None:
+            want, size, S, A = ref.linear(q, k, v, decay, state, D ** -0.5, None)
+            bound, state_bound = ref.linear_bounds(want, size, A, D, T, BF16, False)
+            check(out, want, bound, "out")
+            check(new, S, state_bound, "state")
+        else:
+            for b, m in enumerate(lengths):
+                assert (out[b, m:] == 0).all()
+            # a sequence that ends sooner: the same rows, and the state of a call with no more tokens
+            check(out[0], want[0], bound[0], "out of the longest")
+            b, m = B - 1, lengths[-1]
+            short = ref.linear(q[b:, :m], k[b:, :m], v[b:, :m], decay, state[b:], D ** -0.5, None)
+            limits = ref.linear_bounds(short[0], short[1], short[3], D, m, BF16, False)
+            check(out[b:, :m], short[0], limits[0], "out of the shortest")
+            check(new[b:], short[2], limits[1], "state of the shortest")
+
+
+# ------------------------------------------------------------------------------- few queries, keys over several clusters
+def _scratch(B, Tq, Tk, H, K, D, masked):
+    import ctypes as C
+    a = binding.tt_cross_attention_args(C.sizeof(binding.tt_cross_attention_args), 1, B, Tq, Tk, H, K, D, 0.125)
+    a.mask = 16 if masked else None
+    return binding.load_library().tt_cross_attention_scratch_bytes(C.byref(a))
+
+
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("B,Tq,Tk,H,K", [(1, 7, 14400, 4, 4), (1, 3, 20001, 2, 1), (2, 7, 14400, 2, 2), (1, 9, 33333, 4, 2)])
+@pytest.mark.parametrize("masked", [False, True])
+def test_cross_attention_of_few_queries_on_keys_split_over_clusters(cuda_device, B, Tq, Tk, H, K, D, masked):
+    assert _scratch(B, Tq, Tk, H, K, D, masked) >= 2 * B * K * Tq * (H // K) * (D + 2) * 4      # two clusters to a tile of rows at least
+    g = torch.Generator(device=cuda_device).manual_seed(Tk + D)
+    q = _normal(g, cuda_device, (B, Tq, H, D), BF16, 3.0)
+    k, v = (_normal(g, cuda_device, (B, Tk, K, D), BF16, 1.0, s) for s in (0.0, 0.3))
+    mask = None
+    if masked:
+        mask = (torch.rand(B, Tq, Tk, generator=g, device=cuda_device) < 0.2).to(torch.uint8)
+        mask[:, 0] = 0                                   # sees nothing
+        mask[:, 1, :Tk - 5] = 0                          # the last piece only
+        mask[:, 2, 100:] = 0                             # the first only
+    for n in (None, 0, 1, 300, 9000, Tk - 1):
+        lengths = None if n is None else torch.tensor([n, Tk][:B], dtype=torch.int32, device=cuda_device)
+        got = binding.cross_attention(q, k, v, mask=mask, kv_lengths=lengths)
+        want, size, score = ref.cross(q, k, v, D ** -0.5, lengths, mask)
+        # weights are two bf16 terms: off by half a step of half a step, 2^-18, and they are summed before they are cut
+        check(got, want, ref.cross_bounds(want, size, score, D, Tk, BF16, 2.0 ** -17), f"{n} keys")
+
+
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("Tq,Tk,H,K", [(1, 2, 2, 2), (7, 480, 2, 2), (3, 5, 4, 1), (16, 70, 2, 2), (40, 1000, 4, 2)])
+def test_weights_of_few_queries_count_with_more_bits_than_a_value_has(cuda_device, Tq, Tk, H, K, D):
+    """Values that cancel: out is small beside what is summed, so a weight rounded to bf16 once (2^-8 of the sum) would show."""
+    g = torch.Generator(device=cuda_device).manual_seed(Tk + D)
+    q, k = _normal(g, cuda_device, (3, Tq, H, D), BF16, 0.5), _normal(g, cuda_device, (3, Tk, K, D), BF16)
+    v = _normal(g, cuda_device, (3, Tk, K, D), BF16, 0.1) + torch.where(torch.arange(Tk, device=cuda_device) % 2 == 0, 1.0, -1.0)[None, :, None, None].to(BF16)
+    for mask in (None, torch.ones(3, Tq, Tk, dtype=torch.uint8, device=cuda_device)):
+        want, size, score = ref.cross(q, k, v, D ** -0.5, None, mask)
+        check(binding.cross_attention(q, k, v, mask=mask), want, ref.cross_bounds(want, size, score, D, Tk, BF16, 2.0 ** -17), "out")
