@@ -19,8 +19,6 @@ namespace tt {
 namespace tok {
 namespace {
 
-typedef unsigned long long Two;        // two floats
-
 constexpr int THREADS = 256;           // 16 x 16
 constexpr int BN = 64;                 // keys of a tile
 
@@ -34,19 +32,6 @@ struct Shape {
   static constexpr size_t smem = sizeof(float) * (BM * QP + 2 * KV + BM * PP);
 };
 
-// this thread's columns of a row, as pairs: four neighbours at 4 tx (and 64 + 4 tx), two at 2 tx where D is 32
-template <int D>
-__device__ __forceinline__ void load_pairs(const float* row, int tx, Two (&f)[D / 32]) {
-  if constexpr (D == 32) {
-    f[0] = *reinterpret_cast<const Two*>(row + 2 * tx);
-  } else {
-#pragma unroll
-    for (int j = 0; j < D / 64; ++j) {
-      const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(row + 4 * tx + 64 * j);
-      f[2 * j] = v.x; f[2 * j + 1] = v.y;
-    }
-  }
-}
 // 16 bytes to shared memory without waiting for them, or zeros
 __device__ __forceinline__ void copy16(float* dst, const float* src, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(there ? 16 : 0) : "memory");

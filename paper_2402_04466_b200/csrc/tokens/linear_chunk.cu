@@ -17,8 +17,6 @@ namespace tt {
 namespace tok {
 namespace {
 
-typedef unsigned long long Two;        // two floats
-
 constexpr int THREADS = 256;           // 16 x 16
 
 template <int D>
@@ -49,18 +47,6 @@ __device__ __forceinline__ void load_columns(const float* row, int tx, float (&f
   }
 }
 
-template <int D>
-__device__ __forceinline__ void load_pairs(const float* row, int tx, Two (&f)[D / 32]) {
-  if constexpr (D == 32) {
-    f[0] = *reinterpret_cast<const Two*>(row + 2 * tx);
-  } else {
-#pragma unroll
-    for (int j = 0; j < D / 64; ++j) {
-      const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(row + 4 * tx + 64 * j);
-      f[2 * j] = v.x; f[2 * j + 1] = v.y;
-    }
-  }
-}
 // o += x y for rows ty + 16 a of x and this thread's columns of y; `n` inner steps, four at a time: a row's factors in one load
 template <int D, int A>
 __device__ __forceinline__ void multiply(Two (&o)[A][D / 32], const float* x, int pitch, const float* y, int n, int ty, int tx) {

@@ -24,8 +24,6 @@ namespace tt {
 namespace tok {
 namespace {
 
-typedef unsigned long long Two;        // two floats
-
 constexpr int CT = 128;                // tokens of a chunk
 constexpr int GROUP = 8;               // warps of a group: two to a quarter of the tokens, for half of the columns each
 // warps: the state's group, B, loads, A, one that idles, out's group (whose first warp has to be a multiple of four: its quarter of tensor memory)

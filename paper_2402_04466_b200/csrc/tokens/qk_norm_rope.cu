@@ -22,8 +22,6 @@ namespace {
 
 constexpr int THREADS = 128;
 
-typedef unsigned long long Two;        // two floats
-
 // Eight elements of a row as they lie in memory, and as pairs: lo[j] is turned with hi[j].  Runs: one of eight elements where pairs are
 // neighbours, else one of lo's and one of hi's.
 template <typename T, bool INTERLEAVED>

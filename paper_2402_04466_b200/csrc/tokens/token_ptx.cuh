@@ -58,6 +58,8 @@ __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&v)[8])
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+typedef unsigned long long Two;        // two floats
+
 // a * b + c and a + b on both halves of a pair
 __device__ __forceinline__ unsigned long long fma2_of(unsigned long long a, unsigned long long b, unsigned long long c) {
   unsigned long long r;
@@ -95,6 +97,20 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   float y;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
   return y;
+}
+
+// The columns of a row that belong to thread tx of 16, as pairs: four neighbours at 4 tx (and 64 + 4 tx), two at 2 tx where D is 32.
+template <int D>
+__device__ __forceinline__ void load_pairs(const float* row, int tx, Two (&f)[D / 32]) {
+  if constexpr (D == 32) {
+    f[0] = *reinterpret_cast<const Two*>(row + 2 * tx);
+  } else {
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) {
+      const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(row + 4 * tx + 64 * j);
+      f[2 * j] = v.x; f[2 * j + 1] = v.y;
+    }
+  }
 }
 
 // Operand tile in shared memory whose rows (one token each) run along M or N: `group_bytes` from one group of 8 tokens to the next,
