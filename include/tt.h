@@ -437,15 +437,17 @@ tt_status tt_render_layers(const uint8_t* src_dev, int32_t K, int64_t src_frame_
  * the recurrent cell with a state per stream slot, and tt_cross_attention of the tools' queries to an encoder's map.
  *
  * Common to all of them:
- *   - precision TT_BF16 or TT_FP32 is the type of q, k, v and the outputs; sums, statistics and states are fp32;
+ *   - precision TT_BF16 or TT_FP32 is the type of q, k, v and the outputs; sums, statistics and states are fp32.  Of TT_BF16 calls some
+ *     kernels round what stands between two products to bf16 once, as far as the outputs themselves are rounded: see at the calls;
+ *   - the calls serve: there is none for gradients;
  *   - an operand is a tt_tokens view [batch][token][head][head_dim]: the last axis is contiguous, the strides of the others are
  *     counted in elements and may come in any order; they are 0 to 2^38 (inputs: a batch or head stride of 0 shares the data along that axis)
  *     and, like the data pointer, whole multiples of 16 bytes; that of an axis of extent 1 is not looked at.  Outputs overlap no input, unless a call says
  *     otherwise;
  *   - heads shared by groups: kv_heads divides heads, head h uses key and value head h / (heads / kv_heads);
  *   - `lengths` arrays (device, int32 [batch], NULL: all tokens) say how many tokens an entry of the batch has, and are taken
- *     as 0 or as the tensor's extent where they lie outside.  Rows behind an entry's last token are neither read
- *     nor written, whatever they hold;
+ *     as 0 or as the tensor's extent where they lie outside.  Rows behind an entry's last token
+ *     count for nothing, whatever they hold, and are not written;
  *   - head_dim is 32, 64 or 128, anything else is TT_ERR_UNSUPPORTED;
  *   - calls are asynchronous on `cuda_stream` and may be captured into a graph; equal inputs give equal bits.  `scratch` is device memory
  *     of the size that the call's ..._scratch_bytes gives (0: none needed), 16-byte aligned, contents on entry ignored; calls that may
@@ -502,6 +504,8 @@ tt_status tt_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, dou
  * and head, in order of the tokens, with S the head's state [head_dim (key)][head_dim (value)]:
  *   S = exp(log_decay[head]) * S + k_t v_t^T;   out_t = scale * q_t S.
  * A call of several tokens works in chunks, one of a single token per entry reads and writes the states once.
+ * Of several TT_BF16 tokens the weights within a chunk (scale and decay included) and the copy of the state that q_t reads are rounded to bf16 (out is then off by
+ * 2.4e-3 of its size where a single token's, and the rounding of out alone, is 1.7e-3); the state itself is fp32 throughout.
  * An infinity or NaN in a token or a state reaches the elements of the state that the formula gives it to, as what the formula gives (an infinity that
  * has faded by a factor too small for fp32 may be a NaN), and makes the elements of out that read those, from its token on, not finite; no earlier ones.
  * log_decay: device fp32 [heads], 0 or below (-infinity: a state that was finite is the newest token's alone).
@@ -539,6 +543,8 @@ tt_status tt_linear_attention(const tt_linear_attention_args* args, void* cuda_s
  * read the places of its own mask.  Mask strides are in bytes, 0 or more; a query stride of 0 is one mask for all queries.
  * What a query does not see has no influence on its row, NaN and infinity included.  A query that sees nothing gets zeros.
  * An infinity among the values that it sees is one of its row, or NaN where the key's weight is too small for fp32 (about 2^-126 of the largest).
+ * TT_BF16 weights count with 16 bits, but are rounded to bf16 in large calls of more than 64 queries without a mask (out is then off by up to 1.9e-3 of its
+ * size, else by its own rounding, 1.7e-3); their sum is of the weights before that.
  * scale is above 0 and below 1e38.  q_lengths: rows of out behind them are left as they were.
  * status_dev: as in tt_linear_attention.
  */

@@ -627,6 +627,7 @@ def render_layers(src, src_w: int, src_h: int, src_pitch: int, masks, palette, l
 
 
 # -------------------------------------------------------------------- operators over tokens
+# They serve: results carry no gradient, whatever their inputs require.
 TT_ROPE_SCALING = {"plain": 0, "linear": 1, "base": 2, "by_parts": 3}
 # the argument structures as one packed string each: a ctypes.Structure filled field by field costs 5 us of a call, this 1 us
 _ROPE_ARGS = struct.Struct("@I9i2f" + 4 * "Pqqq" + "PPPqPP")
@@ -722,7 +723,7 @@ def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "plain"
 
 def qk_norm_rope(q, k, positions=None, inv_freq=None, q_weight=None, k_weight=None, eps: float = 1e-6, norm: bool = True,
                  interleaved: bool = False, rot_scale: float = 1.0, lengths=None, out=None, stream=None):
-    """tt_qk_norm_rope: q [B][T][Hq][D] and k [B][T][Hk][D] (either may be None), bf16 or fp32 -> (q', k').
+    """tt_qk_norm_rope: q [B][T][Hq][D] and k [B][T][Hk][D] (either may be None), bf16 or fp32 -> (q', k').  No gradient.
 
     positions int64 [B][T] or [T]; inv_freq fp64 [rot_dim / 2] (None: no rotation); weights fp32 [D]; lengths int32 [B].
     out: (q', k') to write to, which may be q and k themselves; without it rows behind an entry's length are zeros."""
@@ -773,7 +774,7 @@ def qk_norm_rope(q, k, positions=None, inv_freq=None, q_weight=None, k_weight=No
 
 def linear_attention(q, k, v, log_decay, state, scale: float = 1.0, slots=None, lengths=None, out=None, state_out=None, status=None,
                      stream=None):
-    """tt_linear_attention: q [B][T][H][D], k and v [B][T][Hkv][D], bf16 or fp32 -> (out [B][T][H][D], state_out).
+    """tt_linear_attention: q [B][T][H][D], k and v [B][T][Hkv][D], bf16 or fp32 -> (out [B][T][H][D], state_out).  No gradient.
 
     log_decay fp32 [H]; state fp32 [num_slots][H][D][D], advanced in place unless state_out is given; slots and lengths int32 [B].
     Without out, rows behind an entry's length, and those of entries that are passed over, are zeros."""
@@ -807,7 +808,7 @@ def linear_attention(q, k, v, log_decay, state, scale: float = 1.0, slots=None, 
 
 
 def cross_attention(q, k, v, scale: Optional[float] = None, kv_lengths=None, q_lengths=None, mask=None, out=None, status=None, stream=None):
-    """tt_cross_attention: q [B][Tq][H][D], k and v [B][Tk][Hkv][D], bf16 or fp32 -> [B][Tq][H][D].
+    """tt_cross_attention: q [B][Tq][H][D], k and v [B][Tk][Hkv][D], bf16 or fp32 -> [B][Tq][H][D].  No gradient.
 
     scale: 1 / sqrt(D) unless given; lengths int32 [B]; mask uint8 or bool [B][Tk] (one for all queries) or [B][Tq][Tk], 0 or False where a
     key is not seen, for instance the masks of tt_postprocess as [K][n_tools][Hm * Wm].  Without out, rows behind q_lengths are zeros."""

@@ -268,9 +268,11 @@ cudaError_t launch_typed(const CrossParams& p, const CrossPlan& plan, int D, cud
 CrossPlan cross_plan(int batch, int q_tokens, int kv_tokens, int heads, int group, int D, bool bf16, bool mask) {
   CrossPlan plan{};
   plan.splits = plan.cluster = 1;
-  // The kernel for many queries costs 16 us and 108 us per 10^6 keys x tiles of 256 queries, the one for few 6 us and 21 us per 10^6
-  // keys x tiles of 16 rows (heads of 64): 128 queries of 5 x 2 heads on 4800 keys take 23.2 us with the one and 24.4 with the other, 256 take 30.0
-  // and 36.9, of one entry 28.0 and 10.6; 64 of 8 x 4 heads on 14400 keys 56.5 and 52.4, 128 take 60.0 and 90.7.
+  // The kernel for many queries takes work from half a million keys x tiles of 16 rows on.  Both measured around that, us with the one for few and the one for
+  // many, heads of 32, 64, 128: 5 x 2 heads on 4800 keys, 128 queries (0.38 million) 18.0 17.2, 24.1 19.5, 41.5 26.6; 192 (0.58) 18.7 17.4, 24.7 21.6, 41.5 31.5;
+  // one entry's 256 queries of 2 heads (0.15) 8.8 16.9, 10.5 21.6, 15.4 32.1; 700 (0.42) 18.2 17.5, 24.1 22.1, 40.9 34.8; 8 x 4 heads on 14400 keys, 65 queries
+  // (2.3) 55.4 50.6, 81.5 52.6, 158 65.9.  So it is not taken too soon, and up to a third (heads of 64) or a half (128) too late where entries are several and
+  // keys fewer than that.  (Masks are the other kernel's whatever the size; up to 64 queries leave three quarters of a tile of 256 rows empty.)
   if (bf16 && !mask && q_tokens > 64 && kv_tokens > 0 &&
       ((int64_t)q_tokens * group + 15) / 16 * batch * (heads / group) >= 500000 / kv_tokens + 1) {
     plan.kernel = CROSS_TC;

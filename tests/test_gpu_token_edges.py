@@ -186,3 +186,11 @@ def test_weights_of_few_queries_count_with_more_bits_than_a_value_has(cuda_devic
     for mask in (None, torch.ones(3, Tq, Tk, dtype=torch.uint8, device=cuda_device)):
         want, size, score = ref.cross(q, k, v, D ** -0.5, None, mask)
         check(binding.cross_attention(q, k, v, mask=mask), want, ref.cross_bounds(want, size, score, D, Tk, BF16, 2.0 ** -17), "out")
+
+
+def test_results_carry_no_gradient(cuda_device):
+    q = torch.randn(1, 5, 2, 64, device=cuda_device, requires_grad=True)
+    w = torch.ones(64, device=cuda_device, requires_grad=True)
+    decay, state = torch.zeros(2, device=cuda_device), torch.zeros(1, 2, 64, 64, device=cuda_device)
+    for x in (*binding.qk_norm_rope(q, q, q_weight=w, k_weight=w), *binding.linear_attention(q, q, q, decay, state), binding.cross_attention(q, q, q)):
+        assert not x.requires_grad and torch.isfinite(x).all()
