@@ -15,7 +15,7 @@
 // from scores and sums, and eight make K' and carry the state.  Scores, P V, operands and K' have two places each where
 // the memory allows (heads of up to 64).  What is left in sequence is the state's product and its scaling.
 //
-// Those eight maps take 104 us, 33 of them the segments' sums and 4 the scan: 2.3 TB/s, 4800 cycles for a chunk's out and state.  What bounds it is
+// Those eight maps take 104 to 110 us by the box, 33 of them the segments' sums and 4 the scan: 2.2 TB/s, 4900 cycles for a chunk's out and state.  What bounds it is
 // not memory (36 us) but shared memory, 290 KB moved a chunk, of which K' is half, and the 16 warps that make operands of what the products left.
 #include "linear_common.cuh"
 #include "token_ptx.cuh"
@@ -189,9 +189,11 @@ __global__ void __launch_bounds__(Cfg<D, WITH_OUT>::THREADS, 1) linear_tc_kernel
   bool ok = true;
   // A whole warp waits and stops together.  Each thing of chunk c is the c-th of its barrier, or the c / PLACES-th of its place's.  Only parities are
   // told apart: a barrier that may be two things ahead of one who waits for the first has a place for each.
+  // (The wait behind the first look is the plain loop: the one whose first tries are straight-line code, of which there are twenty here, takes eight maps from 107 to
+  // 110 us.)
   auto wait = [&](uint64_t* bar, int phase, int code) {
     if (__builtin_expect(__all_sync(0xffffffffu, mbar_test(smem_u32(bar), (uint32_t)phase & 1u)), 1)) return ok;
-    ok = __all_sync(0xffffffffu, ok && mbar_wait_uniform(smem_u32(bar), (uint32_t)phase & 1u, abort_flag, s_status, WAIT_LINEAR_TC + code, WAIT_LIMIT));
+    ok = __all_sync(0xffffffffu, ok && mbar_wait(smem_u32(bar), (uint32_t)phase & 1u, abort_flag, s_status, WAIT_LINEAR_TC + code, WAIT_LIMIT));
     return ok;
   };
   auto place = [](int c) { return c & (PLACES - 1); };
