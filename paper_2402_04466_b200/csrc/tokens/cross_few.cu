@@ -9,8 +9,8 @@
 // other's, and clusters, where one to a tile of rows does not fill the device, through cross_join_kernel.
 //
 // Registers in place of the rings (two tiles of 16 keys a warp, a tile ahead) came to 2.9 TB/s on eight streams of 14400 keys:
-// latency, with 4 KB in flight per warp and most of the instructions addresses and byte permutes.  With the rings: 18.2 us, 5.0 TB/s where a plain
-// copy has 6.5; five streams of 4800 keys take 9.25 us, 2 us of it K and V, the rest a launch, a chain of loads and the joins.
+// latency, with 4 KB in flight per warp and most of the instructions addresses and byte permutes.  With the rings: 18.2 us (maps cut to 8100 to 14400 keys), 5.0 TB/s where a plain
+// copy has 6.5; five streams of 4800 keys with masks take 9.25 us, 2 us of it K and V, the rest a launch, a chain of loads and the joins.
 #include "tokens.h"
 
 #include "token_ptx.cuh"

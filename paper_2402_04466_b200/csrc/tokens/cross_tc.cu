@@ -10,7 +10,7 @@
 //
 // Bound by the warps that turn scores into weights: the exponentials alone (16 a cycle and multiprocessor) take 1024 cycles for a
 // tile of 128 x 128 whose two products take 512 with heads of 64 and 1024 with heads of 128.  Eight entries of 4 heads of 64, 4800 queries on
-// 4800 keys: 286 us, 660 TFLOP/s, 1750 cycles a tile of 128 x 128; four entries of 2 heads of 128, 4800 queries on 9100 to 14400 keys: 224 us, 1027
+// 4800 keys: 276 us, 684 TFLOP/s, 1690 cycles a tile of 128 x 128; four entries of 2 heads of 128, 4800 queries on 9000 to 14400 keys: 226 us, 1018
 // TFLOP/s.  Weights are rounded to bf16 once, as far as out itself is; their sum is of the weights before that.
 #include "tokens.h"
 
@@ -44,8 +44,8 @@ struct Cfg {
   // weights (BN / 2) and sums (D).
   static constexpr int TILES = 2, BN = D == 128 ? 64 : 128;
   // With heads of up to 64 the special-function units are what there is least of: the two tiles' warps of a quarter, which share one, take
-  // turns at their exponentials, and one does the rest of its work meanwhile (287 us where both at once take 290; with heads of 128, whose
-  // products take as long as the exponentials, 240 with turns and 224 without).
+  // turns at their exponentials, and one does the rest of its work meanwhile (276 us where both at once take 306; with heads of 128, whose
+  // products take as long as the exponentials, 241 with turns and 226 without).
   static constexpr bool TURNS = D != 128;
   static constexpr int HALVES = BN / 64;                            // weights are handed over 64 keys at a time
   static constexpr int PLACES = D == 128 ? 2 : 1;                   // of a tile's weights: those of one tile of keys are made while the last ones' product runs
@@ -532,7 +532,7 @@ int64_t grid_of(int batch, int q_tokens, int kv_tokens, int heads) {
 }
 
 template <int D>
-cudaError_t launch(CrossTcParams& p, int batch, cudaStream_t s) {      // (the join is launched ahead of the end of the kernel: 2 us)
+cudaError_t launch(CrossTcParams& p, int batch, cudaStream_t s) {      // (the join is launched ahead of the end of the kernel: two entries' 256 queries 24 us, behind it 26.5)
   using C = Cfg<D>;
   static OncePerContext once;
   cudaError_t e = once([] { return cudaFuncSetAttribute(cross_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM); });
@@ -542,7 +542,7 @@ cudaError_t launch(CrossTcParams& p, int batch, cudaStream_t s) {      // (the j
     const unsigned blocks = (unsigned)grid_of<D>(p.batch, p.q_tokens, p.kv_tokens, p.heads);
     cross_tc_kernel<D><<<blocks, C::THREADS, C::SMEM, s>>>(p);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    // eight blocks to a tile's rows: two entries' 256 queries of 4 heads of 64 on 4800 keys 25.9 us, with four 28.9 (eight maps 287.5 and 286)
+    // eight blocks to a tile's rows: two entries' 256 queries of 4 heads of 64 on 4800 keys 24 us, with four 28 (eight maps 276 and 274)
     if ((e = launch_kernel(cross_tc_join_kernel<D>, dim3(blocks, 8), 256, 0, s, p, true)) != cudaSuccess) return e;
   }
   return cudaSuccess;

@@ -9,7 +9,7 @@
 // the weights of a side; a few rows are in flight together, and nothing is shared between lanes but the sums.
 // (Rows of all heads spread over the lanes, with the angles of a step shared through shared memory, took three times the
 // instructions, most of them for addresses, and 43 to 57 us for eight maps of 14400 tokens.)
-// Eight maps of 14400 tokens of 4 + 4 heads of 64: 34.9 us, 5.3 TB/s, 81 % of a plain copy's rate; eight tokens: 3.1 us, a launch.
+// Eight maps of 14400 tokens of 4 + 4 heads of 64: 35.3 us, 5.2 TB/s, 80 % of a plain copy's rate; eight tokens: 3.1 us, a launch.
 // The angle is reduced in 64 bits (turns = position * inv_freq / 2 pi, less the nearest whole number): at position 5e6 a
 // product of 32 bits would be off by 0.3 radians.
 #include "tokens.h"
