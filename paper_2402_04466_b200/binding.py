@@ -627,7 +627,8 @@ def render_layers(src, src_w: int, src_h: int, src_pitch: int, masks, palette, l
 
 
 # -------------------------------------------------------------------- operators over tokens
-# They serve: results carry no gradient, whatever their inputs require.
+# They serve: results carry no gradient, whatever their inputs require.  `stream` (a torch stream or a handle; None: the current one) is where the kernels run and
+# results belong; the caller orders it with the streams that made the inputs.
 TT_ROPE_SCALING = {"plain": 0, "linear": 1, "base": 2, "by_parts": 3}
 # the argument structures as one packed string each: a ctypes.Structure filled field by field costs 5 us of a call, this 1 us
 _ROPE_ARGS = struct.Struct("@I9i2f" + 4 * "Pqqq" + "PPPqPP")
@@ -679,6 +680,7 @@ class _Current:
             stream = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
         if stream is not None and stream.device != device:
             _refuse(f"the stream is on {stream.device}, the tensors on {device}")
+        self.stream = stream
         self.contexts = [torch.cuda.device(device)] + ([torch.cuda.stream(stream)] if stream is not None else [])
 
     def __enter__(self):
@@ -688,6 +690,18 @@ class _Current:
     def __exit__(self, *e):
         for c in reversed(self.contexts):
             c.__exit__(*e)
+
+    def call(self, operator, *args):
+        """operator(*args) with this entered.  The tensors it is given may be let go as soon as it returns, and their memory may be another's on their own stream
+        before the kernels have run on this one: the allocator is told."""
+        with self:
+            res = operator(*args)
+        if self.stream is not None:
+            for x in args:
+                for y in x if isinstance(x, (tuple, list)) else (x,):
+                    if isinstance(y, _TORCH.mod.Tensor):
+                        y.record_stream(self.stream)
+        return res
 
 
 def _tokens(name: str, x, dtype, device):
@@ -732,8 +746,7 @@ def qk_norm_rope(q, k, positions=None, inv_freq=None, q_weight=None, k_weight=No
         _refuse("q and k are both None")
     lib, th, prec, device, away = _operator(x, stream)
     if away is not None:
-        with away:
-            return qk_norm_rope(q, k, positions, inv_freq, q_weight, k_weight, eps, norm, interleaved, rot_scale, lengths, out)
+        return away.call(qk_norm_rope, q, k, positions, inv_freq, q_weight, k_weight, eps, norm, interleaved, rot_scale, lengths, out)
     dtype, shape = x.dtype, x.shape
     if len(shape) != 4:
         _refuse("q and k must be [batch][token][head][head_dim]")
@@ -780,8 +793,7 @@ def linear_attention(q, k, v, log_decay, state, scale: float = 1.0, slots=None, 
     Without out, rows behind an entry's length, and those of entries that are passed over, are zeros."""
     lib, th, prec, device, away = _operator(q, stream)
     if away is not None:
-        with away:
-            return linear_attention(q, k, v, log_decay, state, scale, slots, lengths, out, state_out, status)
+        return away.call(linear_attention, q, k, v, log_decay, state, scale, slots, lengths, out, state_out, status)
     dtype, shape, kv_shape = q.dtype, q.shape, k.shape
     if out is None:
         out = (th.empty if lengths is None and slots is None else th.zeros)(shape, dtype=dtype, device=q.device)
@@ -814,8 +826,7 @@ def cross_attention(q, k, v, scale: Optional[float] = None, kv_lengths=None, q_l
     key is not seen, for instance the masks of tt_postprocess as [K][n_tools][Hm * Wm].  Without out, rows behind q_lengths are zeros."""
     lib, th, prec, device, away = _operator(q, stream)
     if away is not None:
-        with away:
-            return cross_attention(q, k, v, scale, kv_lengths, q_lengths, mask, out, status)
+        return away.call(cross_attention, q, k, v, scale, kv_lengths, q_lengths, mask, out, status)
     dtype, shape, kv_shape = q.dtype, q.shape, k.shape
     if out is None:
         out = (th.empty if q_lengths is None else th.zeros)(shape, dtype=dtype, device=q.device)

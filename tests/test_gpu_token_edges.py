@@ -194,3 +194,28 @@ def test_results_carry_no_gradient(cuda_device):
     decay, state = torch.zeros(2, device=cuda_device), torch.zeros(1, 2, 64, 64, device=cuda_device)
     for x in (*binding.qk_norm_rope(q, q, q_weight=w, k_weight=w), *binding.linear_attention(q, q, q, decay, state), binding.cross_attention(q, q, q)):
         assert not x.requires_grad and torch.isfinite(x).all()
+
+
+@pytest.mark.parametrize("name", ["rope", "linear", "cross"])
+def test_tensors_let_go_before_another_stream_has_read_them(cuda_device, name):
+    """A call for another stream returns before its kernels have run.  Its tensors' memory is nobody else's until they have."""
+    g = torch.Generator(device=cuda_device).manual_seed(3)
+    x = _normal(g, cuda_device, (2, 600, 2, 64), FP32)
+    decay, state = torch.full((2,), -0.1, device=cuda_device), torch.zeros(2, 2, 64, 64, device=cuda_device)
+    pos, inv = torch.arange(600, device=cuda_device), torch.from_numpy(binding.rope_frequencies(64)[0]).to(cuda_device)
+    calls = {"rope": lambda y, s: binding.qk_norm_rope(y, None, pos, inv, stream=s)[0],
+             "linear": lambda y, s: binding.linear_attention(y, y, y, decay, state, state_out=torch.zeros_like(state), stream=s)[0],
+             "cross": lambda y, s: binding.cross_attention(y, y, y, stream=s)}
+    want = calls[name](x, None)
+    side = torch.cuda.Stream()
+    calls[name](x, side)                                  # what is set up once is there
+    torch.cuda.synchronize()
+    y = x.clone()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(40_000_000)                     # some 20 ms
+    got = calls[name](y, side)
+    del y
+    others = [torch.full_like(x, math.nan) for _ in range(8)]
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and len(others) == 8
