@@ -15,7 +15,7 @@
 // from scores and sums, and eight make K' and carry the state.  Scores, P V, operands and K' have two places each where
 // the memory allows (heads of up to 64).  What is left in sequence is the state's product and its scaling.
 //
-// Those eight maps take 104 to 110 us by the box, 33 of them the segments' sums and 4 the scan: 2.2 TB/s, 4800 cycles for a chunk's out and state.  What bounds it is
+// Those eight maps take 104 to 110 us by the machine, 33 of them the segments' sums and 4 the scan: 2.2 TB/s, 4800 cycles for a chunk's out and state.  What bounds it is
 // not memory (36 us) but shared memory, 290 KB moved a chunk, of which K' is half, and the 16 warps that make operands of what the products left.
 #include "linear_common.cuh"
 #include "token_ptx.cuh"
