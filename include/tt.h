@@ -433,7 +433,7 @@ tt_status tt_render_layers(const uint8_t* src_dev, int32_t K, int64_t src_frame_
 /* ---------------------------------------------------------------------------------------
  * Operators over tokens, on caller-owned device buffers (no context needed): what a recurrent model of K streams
  * (paper, Section III-A) needs where it works on tokens, the places of a map or one query per tool, instead
- * of whole maps.  A tick's usual order is tt_qk_norm_rope on the projected queries and keys, tt_linear_attention as
+ * of whole maps.  A tick's usual order is tt_qk_norm_rope on the projected queries and keys, tt_linear_attention or tt_delta_rule as
  * the recurrent cell with a state per stream slot, and tt_cross_attention of the tools' queries to an encoder's map.
  *
  * Common to all of them:
@@ -534,6 +534,33 @@ typedef struct {
 } tt_linear_attention_args;
 uint64_t tt_linear_attention_scratch_bytes(const tt_linear_attention_args* args);   /* 0 also for arguments that the call refuses */
 tt_status tt_linear_attention(const tt_linear_attention_args* args, void* cuda_stream);
+
+/*
+ * tt_delta_rule — the gated delta rule: a recurrent cell over tokens like tt_linear_attention, with the same states, whose tokens do not only add to a state but
+ * correct what it says of their key.  For every entry of the batch and head, in order of the tokens, with S the head's state [head_dim (key)][head_dim (value)]:
+ *   S = exp(log_decay_t) * S;   u = beta_t * (v_t - S^T k_t);   S = S + k_t u^T;   out_t = scale * S^T q_t.
+ * Keys are usually of length 1 (tt_qk_norm_rope with weights of 1 / sqrt(head_dim)) and beta between 0 and 1; where beta |k|^2 is above 2 the rule diverges.
+ * qk_heads divides heads: head h, with its own values, gates, state and output, uses query and key head h / (heads / qk_heads).
+ * log_decay, beta: device fp32 [batch][tokens][heads], contiguous; log_decay is 0 or below (-infinity: a state that was finite is forgotten), NULL: no decay.
+ * state, state_out, num_slots, slots, lengths: as in tt_linear_attention.
+ * An infinity or NaN in a token or a state makes the elements of the state and of out that read it not finite, from its token on; earlier tokens, other columns of
+ * values and other heads see nothing of it.
+ */
+typedef struct {
+  uint32_t struct_size;            /* = sizeof(tt_delta_rule_args) */
+  int32_t precision;
+  int32_t batch, tokens, heads, qk_heads, head_dim, num_slots;
+  float scale;
+  int32_t reserved_;
+  tt_tokens q, k, v, out;
+  const float* log_decay;
+  const float* beta;
+  const float* state;
+  float* state_out;
+  const int32_t* slots;
+  const int32_t* lengths;
+} tt_delta_rule_args;
+tt_status tt_delta_rule(const tt_delta_rule_args* args, void* cuda_stream);
 
 /*
  * tt_cross_attention — attention of q_tokens queries to an encoder's kv_tokens states:

@@ -36,7 +36,7 @@ EXPORTED_SYMBOLS = [
     "tt_sched_complete", "tt_sched_predict_ms", "tt_sched_stats",
     "tt_preprocess", "tt_postprocess_scratch_bytes", "tt_postprocess", "tt_postprocess_static", "tt_overlay", "tt_render_layers",
     "tt_qk_norm_rope", "tt_rope_frequencies", "tt_linear_attention", "tt_linear_attention_scratch_bytes",
-    "tt_cross_attention", "tt_cross_attention_scratch_bytes",
+    "tt_delta_rule", "tt_cross_attention", "tt_cross_attention_scratch_bytes",
 ]
 TT_POSTPROCESS_STATIC_SCRATCH_BYTES = 32 << 10
 STAGE_NAMES = ["h2d", "preprocess", "enc0", "enc1", "enc2", "enc3", "convlstm", "postprocess", "overlay"]
@@ -66,6 +66,13 @@ class tt_linear_attention_args(C.Structure):
         ("scale", C.c_float), ("reserved_", C.c_int32)] + [(n, tt_tokens) for n in ("q", "k", "v", "out")] + [
         (n, C.c_void_p) for n in ("log_decay", "state", "state_out", "slots", "lengths", "status_dev", "scratch")] + [
         ("scratch_bytes", C.c_uint64)]
+
+
+class tt_delta_rule_args(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32)] + [(n, C.c_int32) for n in (
+        "precision", "batch", "tokens", "heads", "qk_heads", "head_dim", "num_slots")] + [
+        ("scale", C.c_float), ("reserved_", C.c_int32)] + [(n, tt_tokens) for n in ("q", "k", "v", "out")] + [
+        (n, C.c_void_p) for n in ("log_decay", "beta", "state", "state_out", "slots", "lengths")]
 
 
 class tt_cross_attention_args(C.Structure):
@@ -173,6 +180,7 @@ def load_library(build_if_missing: bool = True) -> C.CDLL:
     lib.tt_render_layers.argtypes = [vp, i32, i64, i32, i32, i32, vp, i32, i32, i32, vp, i32, i32, vp, vp]
     lib.tt_qk_norm_rope.argtypes = [vp, vp]
     lib.tt_rope_frequencies.argtypes = [i32, C.c_double, i32, C.c_double, C.c_double, C.c_double, C.c_double, vp, C.POINTER(f32)]
+    lib.tt_delta_rule.argtypes = [vp, vp]
     for name in ("tt_linear_attention", "tt_cross_attention"):
         getattr(lib, name).argtypes = [vp, vp]
         getattr(lib, name + "_scratch_bytes").argtypes = [vp]
@@ -633,6 +641,7 @@ TT_ROPE_SCALING = {"plain": 0, "linear": 1, "base": 2, "by_parts": 3}
 # the argument structures as one packed string each: a ctypes.Structure filled field by field costs 5 us of a call, this 1 us
 _ROPE_ARGS = struct.Struct("@I9i2f" + 4 * "Pqqq" + "PPPqPP")
 _LINEAR_ARGS = struct.Struct("@I7ifi" + 4 * "Pqqq" + "PPPPPPPQ")
+_DELTA_ARGS = struct.Struct("@I7ifi" + 4 * "Pqqq" + "PPPPPP")
 _CROSS_ARGS = struct.Struct("@I7ifi" + 4 * "Pqqq" + "PPPqqPPQ")
 _SCRATCH = struct.Struct("@PQ")      # the last two members of both
 
@@ -814,6 +823,35 @@ def linear_attention(q, k, v, log_decay, state, scale: float = 1.0, slots=None, 
         buf = th.empty(room, dtype=th.u8, device=q.device)
         args = args[:-16] + _SCRATCH.pack(buf.data_ptr(), room)
     st = lib.tt_linear_attention(args, th.current_stream(device))
+    if st:
+        _check(lib, st)
+    return out, state_out
+
+
+def delta_rule(q, k, v, log_decay, beta, state, scale: float = 1.0, slots=None, lengths=None, out=None, state_out=None, stream=None):
+    """tt_delta_rule: q and k [B][T][Hqk][D], v [B][T][H][D], bf16 or fp32 -> (out [B][T][H][D], state_out).  No gradient.
+
+    log_decay (None: no decay) and beta fp32 [B][T][H]; state fp32 [num_slots][H][D][D], advanced in place unless state_out is given; slots and lengths
+    int32 [B].  Without out, rows behind an entry's length, and those of entries that are passed over, are zeros."""
+    lib, th, prec, device, away = _operator(q, stream)
+    if away is not None:
+        return away.call(delta_rule, q, k, v, log_decay, beta, state, scale, slots, lengths, out, state_out)
+    dtype, qk_shape, shape = q.dtype, q.shape, v.shape
+    if out is None:
+        out = (th.empty if lengths is None and slots is None else th.zeros)(shape, dtype=dtype, device=q.device)
+    if state_out is None:
+        state_out = state
+    views = _tokens("q", q, dtype, device) + _tokens("k", k, dtype, device) + _tokens("v", v, dtype, device) + _tokens("out", out, dtype, device)
+    B, T, H, D = shape
+    Hk, n = qk_shape[2], state.shape[0]
+    if k.shape != qk_shape or qk_shape != (B, T, Hk, D) or out.shape != shape:
+        _refuse("q, k, v and out do not fit together")
+    states, gates = (n, H, D, D), (B, T, H)
+    args = _DELTA_ARGS.pack(_DELTA_ARGS.size, prec, B, T, H, Hk, D, n, scale, 0, *views, _array("log_decay", log_decay, th.f32, device, gates),
+                            _array("beta", beta, th.f32, device, gates), _array("state", state, th.f32, device, states),
+                            _array("state_out", state_out, th.f32, device, states), _array("slots", slots, th.i32, device, (B,)),
+                            _array("lengths", lengths, th.i32, device, (B,)))
+    st = lib.tt_delta_rule(args, th.current_stream(device))
     if st:
         _check(lib, st)
     return out, state_out

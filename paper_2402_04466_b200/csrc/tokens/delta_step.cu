@@ -1,0 +1,135 @@
+// The gated delta rule, token by token (tt_delta_rule).  With S a head's state [key][value], a = exp(log_decay):
+//   u = beta (v - a S^T k),  S' = a S + k u^T,  out = scale S'^T q = scale (a S^T q + (k . q) u).
+// The second form of out lets one pass over the state give both sums, S^T k and S^T q, so that a single meeting of the block's threads lies
+// between reading a state and writing it.  A block owns a run of W value columns of one head's state (the columns are
+// independent of each other), LANES = W / 4 threads to a row, in registers for the whole call.
+#include "linear_common.cuh"
+
+namespace tt {
+namespace tok {
+namespace {
+
+template <int D, int W>
+struct DeltaStep {
+  static constexpr int LANES = W / 4;                                   // threads to a row
+  static constexpr int THREADS = LANES * D < 256 ? LANES * D : 256;
+  static constexpr int ROWS = D * LANES / THREADS;                      // rows to a thread
+};
+
+template <typename T, int D, int W>
+__global__ void __launch_bounds__(256) delta_step_kernel(const __grid_constant__ DeltaParams p) {
+  using Shape = DeltaStep<D, W>;
+  constexpr int LANES = Shape::LANES, ROWS = Shape::ROWS, STEP = Shape::THREADS / LANES, WARPS = Shape::THREADS / 32;
+  // of either parity of tokens: a warp may be at the next one while another still reads these
+  __shared__ float4 said[2][WARPS][LANES], asked[2][WARPS][LANES];
+  __shared__ float dots[2][WARPS];
+  const int b = blockIdx.z, h = blockIdx.y, lane = threadIdx.x % LANES, col = (int)blockIdx.x * W + lane * 4, row = threadIdx.x / LANES, warp = threadIdx.x / 32;
+  const int n = clamp_length(p.lengths, b, p.tokens);
+  // before any of its data is touched: the slot of an entry that is passed over may be one that an earlier entry is writing
+  const int slot = slot_of(p.slots, p.num_slots, b);
+  if (slot < 0) return;                // the whole block
+  const int64_t base = ((int64_t)slot * p.heads + h) * D * D + (int64_t)row * D + col;
+  float4 s[ROWS];
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) s[i] = *reinterpret_cast<const float4*>(p.state + base + (int64_t)i * STEP * D);
+  const int hk = h / p.group;
+  const T* q = reinterpret_cast<const T*>(p.q.p) + b * p.q.b + hk * p.q.h + row;
+  const T* k = reinterpret_cast<const T*>(p.k.p) + b * p.k.b + hk * p.k.h + row;
+  const T* v = reinterpret_cast<const T*>(p.v.p) + b * p.v.b + h * p.v.h + col;
+  T* o = reinterpret_cast<T*>(p.o.p) + b * p.o.b + h * p.o.h + col;
+  const int64_t gates = (int64_t)b * p.tokens * p.heads + h;
+  float kk[ROWS], qq[ROWS], vv[4], fade = 1.f, beta = 0.f;
+  auto fetch = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+      kk[i] = to_float(k[t * p.k.t + i * STEP]);
+      qq[i] = to_float(q[t * p.q.t + i * STEP]);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) vv[j] = to_float(v[t * p.v.t + j]);
+    if (p.log_decay) fade = expf(p.log_decay[gates + (int64_t)t * p.heads]);
+    beta = p.beta[gates + (int64_t)t * p.heads];
+  };
+  if (n > 0) fetch(0);
+  for (int t = 0; t < n; ++t) {
+    float x[4] = {}, y[4] = {}, kq = 0.f;
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+      kq = fmaf(kk[i], qq[i], kq);
+      x[0] = fmaf(kk[i], s[i].x, x[0]); x[1] = fmaf(kk[i], s[i].y, x[1]); x[2] = fmaf(kk[i], s[i].z, x[2]); x[3] = fmaf(kk[i], s[i].w, x[3]);
+      y[0] = fmaf(qq[i], s[i].x, y[0]); y[1] = fmaf(qq[i], s[i].y, y[1]); y[2] = fmaf(qq[i], s[i].z, y[2]); y[3] = fmaf(qq[i], s[i].w, y[3]);
+    }
+#pragma unroll
+    for (int d = 16; d >= LANES; d >>= 1) {
+      kq += __shfl_xor_sync(0xFFFFFFFFu, kq, d);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        x[j] += __shfl_xor_sync(0xFFFFFFFFu, x[j], d);
+        y[j] += __shfl_xor_sync(0xFFFFFFFFu, y[j], d);
+      }
+    }
+    if (threadIdx.x % 32 < LANES) {
+      said[t & 1][warp][lane] = make_float4(x[0], x[1], x[2], x[3]);
+      asked[t & 1][warp][lane] = make_float4(y[0], y[1], y[2], y[3]);
+    }
+    if (threadIdx.x % 32 == 0) dots[t & 1][warp] = kq;
+    __syncthreads();
+    float4 sx = said[t & 1][0][lane];
+#pragma unroll
+    for (int w = 1; w < WARPS; ++w) {
+      const float4 f = said[t & 1][w][lane];
+      sx.x += f.x; sx.y += f.y; sx.z += f.z; sx.w += f.w;
+    }
+    const float u[4] = {beta * (vv[0] - fade * sx.x), beta * (vv[1] - fade * sx.y), beta * (vv[2] - fade * sx.z), beta * (vv[3] - fade * sx.w)};
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+      s[i].x = fmaf(fade, s[i].x, kk[i] * u[0]);
+      s[i].y = fmaf(fade, s[i].y, kk[i] * u[1]);
+      s[i].z = fmaf(fade, s[i].z, kk[i] * u[2]);
+      s[i].w = fmaf(fade, s[i].w, kk[i] * u[3]);
+    }
+    if (threadIdx.x < LANES) {
+      float4 sy = asked[t & 1][0][lane];
+      float dot = dots[t & 1][0];
+#pragma unroll
+      for (int w = 1; w < WARPS; ++w) {
+        const float4 f = asked[t & 1][w][lane];
+        sy.x += f.x; sy.y += f.y; sy.z += f.z; sy.w += f.w;
+        dot += dots[t & 1][w];
+      }
+      T* to = o + t * p.o.t;
+      to[0] = (T)(p.scale * fmaf(fade, sy.x, dot * u[0]));
+      to[1] = (T)(p.scale * fmaf(fade, sy.y, dot * u[1]));
+      to[2] = (T)(p.scale * fmaf(fade, sy.z, dot * u[2]));
+      to[3] = (T)(p.scale * fmaf(fade, sy.w, dot * u[3]));
+    }
+    if (t + 1 < n) fetch(t + 1);
+  }
+  if (n == 0 && p.state_out == p.state) return;
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) *reinterpret_cast<float4*>(p.state_out + base + (int64_t)i * STEP * D) = s[i];
+}
+
+template <typename T, int D, int W>
+cudaError_t launch(const DeltaParams& p, cudaStream_t s) {
+  delta_step_kernel<T, D, W><<<dim3(D / W, (unsigned)p.heads, (unsigned)p.batch), DeltaStep<D, W>::THREADS, 0, s>>>(p);
+  return cudaGetLastError();
+}
+template <typename T, int D>
+cudaError_t launch(const DeltaParams& p, cudaStream_t s) {
+  // few states: cut each into four runs of columns, so that more multiprocessors fetch
+  return (int64_t)p.batch * p.heads < 2 * PLAN_SMS ? launch<T, D, D / 4>(p, s) : launch<T, D, D>(p, s);
+}
+template <typename T>
+cudaError_t launch(const DeltaParams& p, int D, cudaStream_t s) {
+  return D == 32 ? launch<T, 32>(p, s) : D == 64 ? launch<T, 64>(p, s) : launch<T, 128>(p, s);
+}
+
+}  // namespace
+
+cudaError_t launch_delta_step(const DeltaParams& p, bool bf16, int D, cudaStream_t s) {
+  return bf16 ? launch<__nv_bfloat16>(p, D, s) : launch<float>(p, D, s);
+}
+
+}  // namespace tok
+}  // namespace tt

@@ -1,4 +1,4 @@
-// Launch interfaces of the operators over tokens (tt.h: tt_qk_norm_rope, tt_linear_attention, tt_cross_attention).
+// Launch interfaces of the operators over tokens (tt.h: tt_qk_norm_rope, tt_linear_attention, tt_delta_rule, tt_cross_attention).
 #pragma once
 
 #include "../tt_internal.h"
@@ -48,6 +48,20 @@ cudaError_t launch_linear_step(const LinearParams& p, bool bf16, int D, cudaStre
 cudaError_t launch_linear_chunk(const LinearParams& p, int D, cudaStream_t s);    // fp32, and calls without tokens
 cudaError_t launch_linear_tc(const LinearParams& p, int D, cudaStream_t s);       // bf16
 cudaError_t launch_linear_scan(const LinearParams& p, int D, cudaStream_t s);     // what segments add -> the states before them
+
+struct alignas(32) DeltaParams {
+  View q, k, v, o;
+  const float* log_decay;       // or null
+  const float* beta;
+  const float* state;
+  float* state_out;
+  const int32_t* slots;
+  const int32_t* lengths;
+  int32_t batch, tokens, heads, group;     // group: heads to a query and key head
+  int32_t num_slots;
+  float scale;
+};
+cudaError_t launch_delta_step(const DeltaParams& p, bool bf16, int D, cudaStream_t s);
 
 struct alignas(32) CrossParams {
   View q, k, v, o;

@@ -168,6 +168,34 @@ tt_status tt_linear_attention(const tt_linear_attention_args* a, void* cuda_stre
   return e == cudaSuccess ? TT_OK : set_error(TT_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
 }
 
+tt_status tt_delta_rule(const tt_delta_rule_args* a, void* cuda_stream) {
+  const char* who = "tt_delta_rule";
+  if (!a || a->struct_size != sizeof(*a)) return set_error(TT_ERR_INVALID_ARG, "%s: struct_size", who);
+  if ((a->precision != TT_FP32 && a->precision != TT_BF16) || !extent(a->batch, 1, 65535) || !extent(a->tokens, 0, MAX_EXTENT) ||
+      !extent(a->heads, 1, 4096) || !extent(a->qk_heads, 1, a->heads) || a->heads % a->qk_heads || !extent(a->num_slots, 1, MAX_EXTENT) ||
+      !std::isfinite(a->scale))
+    return set_error(TT_ERR_INVALID_ARG, "%s: bad argument", who);
+  if (bad_head_dim(who, a->head_dim)) return TT_ERR_UNSUPPORTED;
+  if (!a->slots && a->batch > a->num_slots) return set_error(TT_ERR_INVALID_ARG, "%s: more entries than slots", who);
+  const bool bf16 = a->precision == TT_BF16;
+  const int size = bf16 ? 2 : 4;
+  if (bad_view(who, "q", a->q, a->batch, a->tokens, a->qk_heads, size) || bad_view(who, "k", a->k, a->batch, a->tokens, a->qk_heads, size) ||
+      bad_view(who, "v", a->v, a->batch, a->tokens, a->heads, size) || bad_view(who, "out", a->out, a->batch, a->tokens, a->heads, size) ||
+      folded(who, "out", a->out, a->batch, a->tokens, a->heads, a->head_dim))
+    return TT_ERR_INVALID_ARG;
+  if ((a->tokens && !a->beta) || !a->state || !a->state_out || misaligned(a->log_decay, 4) || misaligned(a->beta, 4) || misaligned(a->state, 16) ||
+      misaligned(a->state_out, 16) || misaligned(a->slots, 4) || misaligned(a->lengths, 4))
+    return set_error(TT_ERR_INVALID_ARG, "%s: beta, state or state_out is null, or a pointer is misaligned (states: 16 bytes)", who);
+  DeltaParams p{};
+  p.q = view(a->q, a->batch, a->tokens, a->qk_heads); p.k = view(a->k, a->batch, a->tokens, a->qk_heads);
+  p.v = view(a->v, a->batch, a->tokens, a->heads); p.o = view(a->out, a->batch, a->tokens, a->heads);
+  p.log_decay = a->log_decay; p.beta = a->beta; p.state = a->state; p.state_out = a->state_out; p.slots = a->slots; p.lengths = a->lengths;
+  p.batch = a->batch; p.tokens = a->tokens; p.heads = a->heads; p.group = a->heads / a->qk_heads; p.num_slots = a->num_slots;
+  p.scale = a->scale;
+  const cudaError_t e = launch_delta_step(p, bf16, a->head_dim, reinterpret_cast<cudaStream_t>(cuda_stream));
+  return e == cudaSuccess ? TT_OK : set_error(TT_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
+}
+
 static tt_status check_cross(const char* who, const tt_cross_attention_args* a) {
   if (!a || a->struct_size != sizeof(*a)) return set_error(TT_ERR_INVALID_ARG, "%s: struct_size", who);
   if ((a->precision != TT_FP32 && a->precision != TT_BF16) || !extent(a->batch, 1, 65535) || !extent(a->q_tokens, 0, MAX_EXTENT) ||
