@@ -434,7 +434,7 @@ tt_status tt_render_layers(const uint8_t* src_dev, int32_t K, int64_t src_frame_
  * Operators over tokens, on caller-owned device buffers (no context needed): what a recurrent model of K streams
  * (paper, Section III-A) needs where it works on tokens, the places of a map or one query per tool, instead
  * of whole maps.  A tick's usual order is tt_qk_norm_rope on the projected queries and keys, tt_linear_attention or tt_delta_rule as
- * the recurrent cell with a state per stream slot, and tt_cross_attention of the tools' queries to an encoder's map.
+ * the recurrent cell with a state per stream slot, and tt_cross_attention or tt_differential_attention of the tools' queries to an encoder's map.
  *
  * Common to all of them:
  *   - precision TT_BF16 or TT_FP32 is the type of q, k, v and the outputs; sums, statistics and states are fp32.  Of TT_BF16 calls some
@@ -592,6 +592,42 @@ typedef struct {
 } tt_cross_attention_args;
 uint64_t tt_cross_attention_scratch_bytes(const tt_cross_attention_args* args);   /* 0 also for arguments that the call refuses */
 tt_status tt_cross_attention(const tt_cross_attention_args* args, void* cuda_stream);
+
+/*
+ * tt_differential_attention — the difference of two softmax maps over the same values, which takes away the weight that every place of a map gets:
+ *   y_i = sum_j (w1_ij - lambda w2_ij) v_j,  w1_i = softmax over the visible j of scale * (q1_i . k1_j),  w2_i the same of q2_i and k2_j,
+ * where a head's q = [q1 | q2] and k = [k1 | k2] are two halves of head_dim / 2 elements and v has head_dim;
+ *   lambda = exp(l_q1 . l_k1) - exp(l_q2 . l_k2) + lambda_init,
+ *   norm != 0:  out_i = out_scale * y_i / sqrt(mean(y_i^2) + eps) * norm_weight   (fp32 [head_dim] on the device, NULL: ones; usually out_scale = 1 - lambda_init);
+ *   norm == 0:  out_i = out_scale * y_i.
+ * lambda_vectors: device fp32, the learned l_q1, l_k1, l_q2, l_k2 one behind the other, head_dim / 2 elements each; head h's start at
+ * lambda_vectors + h * lambda_head_stride (0: all heads share them).
+ * What a query sees, the lengths, the mask, scale (usually (head_dim / 2)^-0.5), status_dev and scratch are as in tt_cross_attention, and the same for both maps.  A
+ * query that sees nothing gets zeros.  What a query does not see has no influence on its row; an infinity or NaN among the values that it sees makes the
+ * elements of y_i that read it not finite (with the norm, which reads them all, no element of the row says anything).
+ * TT_BF16 weights count with 16 bits, but are rounded to bf16 in large calls of more than 64 queries without a mask (y is then off by up to 2e-3 of the two sums'
+ * size); their sums are of the weights before that.
+ */
+typedef struct {
+  uint32_t struct_size;            /* = sizeof(tt_differential_attention_args) */
+  int32_t precision;
+  int32_t batch, q_tokens, kv_tokens, heads, kv_heads, head_dim;
+  float scale, lambda_init, eps, out_scale;
+  int32_t norm, reserved_;
+  tt_tokens q, k, v, out;
+  const float* lambda_vectors;
+  int64_t lambda_head_stride;
+  const float* norm_weight;
+  const int32_t* q_lengths;
+  const int32_t* kv_lengths;
+  const uint8_t* mask;
+  int64_t mask_batch_stride, mask_query_stride;
+  int32_t* status_dev;
+  void* scratch;
+  uint64_t scratch_bytes;
+} tt_differential_attention_args;
+uint64_t tt_differential_attention_scratch_bytes(const tt_differential_attention_args* args);   /* 0 also for arguments that the call refuses */
+tt_status tt_differential_attention(const tt_differential_attention_args* args, void* cuda_stream);
 
 #ifdef __cplusplus
 }

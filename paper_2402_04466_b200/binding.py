@@ -37,6 +37,7 @@ EXPORTED_SYMBOLS = [
     "tt_preprocess", "tt_postprocess_scratch_bytes", "tt_postprocess", "tt_postprocess_static", "tt_overlay", "tt_render_layers",
     "tt_qk_norm_rope", "tt_rope_frequencies", "tt_linear_attention", "tt_linear_attention_scratch_bytes",
     "tt_delta_rule", "tt_cross_attention", "tt_cross_attention_scratch_bytes",
+    "tt_differential_attention", "tt_differential_attention_scratch_bytes",
 ]
 TT_POSTPROCESS_STATIC_SCRATCH_BYTES = 32 << 10
 STAGE_NAMES = ["h2d", "preprocess", "enc0", "enc1", "enc2", "enc3", "convlstm", "postprocess", "overlay"]
@@ -79,6 +80,16 @@ class tt_cross_attention_args(C.Structure):
     _fields_ = [("struct_size", C.c_uint32)] + [(n, C.c_int32) for n in (
         "precision", "batch", "q_tokens", "kv_tokens", "heads", "kv_heads", "head_dim")] + [
         ("scale", C.c_float), ("reserved_", C.c_int32)] + [(n, tt_tokens) for n in ("q", "k", "v", "out")] + [
+        ("q_lengths", C.c_void_p), ("kv_lengths", C.c_void_p), ("mask", C.c_void_p), ("mask_batch_stride", C.c_int64),
+        ("mask_query_stride", C.c_int64), ("status_dev", C.c_void_p), ("scratch", C.c_void_p), ("scratch_bytes", C.c_uint64)]
+
+
+class tt_differential_attention_args(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32)] + [(n, C.c_int32) for n in (
+        "precision", "batch", "q_tokens", "kv_tokens", "heads", "kv_heads", "head_dim")] + [
+        (n, C.c_float) for n in ("scale", "lambda_init", "eps", "out_scale")] + [("norm", C.c_int32), ("reserved_", C.c_int32)] + [
+        (n, tt_tokens) for n in ("q", "k", "v", "out")] + [
+        ("lambda_vectors", C.c_void_p), ("lambda_head_stride", C.c_int64), ("norm_weight", C.c_void_p),
         ("q_lengths", C.c_void_p), ("kv_lengths", C.c_void_p), ("mask", C.c_void_p), ("mask_batch_stride", C.c_int64),
         ("mask_query_stride", C.c_int64), ("status_dev", C.c_void_p), ("scratch", C.c_void_p), ("scratch_bytes", C.c_uint64)]
 
@@ -181,7 +192,7 @@ def load_library(build_if_missing: bool = True) -> C.CDLL:
     lib.tt_qk_norm_rope.argtypes = [vp, vp]
     lib.tt_rope_frequencies.argtypes = [i32, C.c_double, i32, C.c_double, C.c_double, C.c_double, C.c_double, vp, C.POINTER(f32)]
     lib.tt_delta_rule.argtypes = [vp, vp]
-    for name in ("tt_linear_attention", "tt_cross_attention"):
+    for name in ("tt_linear_attention", "tt_cross_attention", "tt_differential_attention"):
         getattr(lib, name).argtypes = [vp, vp]
         getattr(lib, name + "_scratch_bytes").argtypes = [vp]
         getattr(lib, name + "_scratch_bytes").restype = C.c_uint64
@@ -643,7 +654,8 @@ _ROPE_ARGS = struct.Struct("@I9i2f" + 4 * "Pqqq" + "PPPqPP")
 _LINEAR_ARGS = struct.Struct("@I7ifi" + 4 * "Pqqq" + "PPPPPPPQ")
 _DELTA_ARGS = struct.Struct("@I7ifi" + 4 * "Pqqq" + "PPPPPP")
 _CROSS_ARGS = struct.Struct("@I7ifi" + 4 * "Pqqq" + "PPPqqPPQ")
-_SCRATCH = struct.Struct("@PQ")      # the last two members of both
+_DIFF_ARGS = struct.Struct("@I7i4f2i" + 4 * "Pqqq" + "PqPPPPqqPPQ")
+_SCRATCH = struct.Struct("@PQ")      # the last two members of those that may need it
 
 
 def _refuse(message: str):
@@ -730,6 +742,17 @@ def _array(name: str, x, dtype, device, shape=None) -> int:
     if x.dtype is not dtype or x.get_device() != device or not x.is_contiguous() or (shape is not None and x.shape != shape):
         _refuse(f"{name} must be a contiguous {dtype} tensor{'' if shape is None else f' of shape {shape}'} on the other tensors' device")
     return x.data_ptr()
+
+
+def _mask(mask, B, Tq, Tk, th, device):
+    """Data pointer and strides of a mask [B][Tk] or [B][Tq][Tk], zeros for None."""
+    if mask is None:
+        return 0, 0, 0
+    n = mask.dim()
+    if (mask.dtype is not th.u8 and mask.dtype is not th.bool) or mask.get_device() != device or mask.shape != ((B, Tq, Tk) if n == 3 else (B, Tk)) or \
+            (Tk > 1 and mask.stride(-1) != 1):
+        _refuse("mask must be uint8 or bool [B][Tk] or [B][Tq][Tk] on the tensors' device, contiguous along Tk")
+    return mask.data_ptr(), mask.stride(0), mask.stride(1) if n == 3 else 0
 
 
 def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0, trained: float = 0.0,
@@ -873,13 +896,7 @@ def cross_attention(q, k, v, scale: Optional[float] = None, kv_lengths=None, q_l
     _, Tk, Hk, _ = kv_shape
     if v.shape != kv_shape or kv_shape != (B, Tk, Hk, D) or out.shape != shape:
         _refuse("q, k, v and out do not fit together")
-    at, mask_b, mask_q = 0, 0, 0
-    if mask is not None:
-        n = mask.dim()
-        if (mask.dtype is not th.u8 and mask.dtype is not th.bool) or mask.get_device() != device or mask.shape != ((B, Tq, Tk) if n == 3 else (B, Tk)) or \
-                (Tk > 1 and mask.stride(-1) != 1):
-            _refuse("mask must be uint8 or bool [B][Tk] or [B][Tq][Tk] on the tensors' device, contiguous along Tk")
-        at, mask_b, mask_q = mask.data_ptr(), mask.stride(0), mask.stride(1) if n == 3 else 0
+    at, mask_b, mask_q = _mask(mask, B, Tq, Tk, th, device)
     args = _CROSS_ARGS.pack(_CROSS_ARGS.size, prec, B, Tq, Tk, H, Hk, D, D ** -0.5 if scale is None else scale, 0, *views,
                             _array("q_lengths", q_lengths, th.i32, device, (B,)), _array("kv_lengths", kv_lengths, th.i32, device, (B,)),
                             at, mask_b, mask_q, _array("status", status, th.i32, device), 0, 0)
@@ -888,6 +905,42 @@ def cross_attention(q, k, v, scale: Optional[float] = None, kv_lengths=None, q_l
         buf = th.empty(room, dtype=th.u8, device=q.device)
         args = args[:-16] + _SCRATCH.pack(buf.data_ptr(), room)
     st = lib.tt_cross_attention(args, th.current_stream(device))
+    if st:
+        _check(lib, st)
+    return out
+
+
+def differential_attention(q, k, v, lambda_vectors, lambda_init: float, scale: Optional[float] = None, norm: bool = True, norm_weight=None, eps: float = 1e-5,
+                           out_scale: Optional[float] = None, kv_lengths=None, q_lengths=None, mask=None, out=None, status=None, stream=None):
+    """tt_differential_attention: q [B][Tq][H][D], k and v [B][Tk][Hkv][D], bf16 or fp32 -> [B][Tq][H][D].  No gradient.
+
+    The first half of a head's queries and keys makes one map, the second half the other.  lambda_vectors fp32 [4][D / 2], shared by the heads, or [H][4][D / 2]:
+    l_q1, l_k1, l_q2, l_k2.  scale: (D / 2)^-0.5 unless given; out_scale: 1 - lambda_init with the norm and 1 without; norm_weight fp32 [D].
+    Lengths, mask and out as in cross_attention."""
+    lib, th, prec, device, away = _operator(q, stream)
+    if away is not None:
+        return away.call(differential_attention, q, k, v, lambda_vectors, lambda_init, scale, norm, norm_weight, eps, out_scale, kv_lengths, q_lengths, mask, out,
+                         status)
+    dtype, shape, kv_shape = q.dtype, q.shape, k.shape
+    if out is None:
+        out = (th.empty if q_lengths is None else th.zeros)(shape, dtype=dtype, device=q.device)
+    views = _tokens("q", q, dtype, device) + _tokens("k", k, dtype, device) + _tokens("v", v, dtype, device) + _tokens("out", out, dtype, device)
+    B, Tq, H, D = shape
+    _, Tk, Hk, _ = kv_shape
+    if v.shape != kv_shape or kv_shape != (B, Tk, Hk, D) or out.shape != shape:
+        _refuse("q, k, v and out do not fit together")
+    each = lambda_vectors.dim() == 3
+    vectors = _array("lambda_vectors", lambda_vectors, th.f32, device, (H, 4, D // 2) if each else (4, D // 2))
+    args = _DIFF_ARGS.pack(_DIFF_ARGS.size, prec, B, Tq, Tk, H, Hk, D, (D / 2) ** -0.5 if scale is None else scale, lambda_init, eps,
+                           (1 - lambda_init if norm else 1.0) if out_scale is None else out_scale, norm, 0, *views, vectors, 2 * D if each else 0,
+                           _array("norm_weight", norm_weight, th.f32, device, (D,)), _array("q_lengths", q_lengths, th.i32, device, (B,)),
+                           _array("kv_lengths", kv_lengths, th.i32, device, (B,)), *_mask(mask, B, Tq, Tk, th, device),
+                           _array("status", status, th.i32, device), 0, 0)
+    room = lib.tt_differential_attention_scratch_bytes(args)
+    if room:
+        buf = th.empty(room, dtype=th.u8, device=q.device)
+        args = args[:-16] + _SCRATCH.pack(buf.data_ptr(), room)
+    st = lib.tt_differential_attention(args, th.current_stream(device))
     if st:
         _check(lib, st)
     return out

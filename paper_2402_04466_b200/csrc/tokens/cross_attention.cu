@@ -40,8 +40,8 @@ __device__ __forceinline__ bool all_finite(float4 f) {
   return isfinite(f.x) && isfinite(f.y) && isfinite(f.z) && isfinite(f.w);
 }
 
-template <int D, int BM>
-__global__ void __launch_bounds__(THREADS) cross_kernel(const __grid_constant__ CrossParams p) {
+template <int D, int BM, int MAPS>
+__global__ void __launch_bounds__(THREADS) cross_kernel(const __grid_constant__ ParamsOf<MAPS> p) {
   using S = Shape<D, BM>;
   constexpr int A = S::A, N = S::N, E = S::E, QP = S::QP, PP = S::PP;
   extern __shared__ float4 raw[];
@@ -63,15 +63,17 @@ __global__ void __launch_bounds__(THREADS) cross_kernel(const __grid_constant__ 
     if (row0 + r < rows) f = *reinterpret_cast<const float4*>(q + (int64_t)((row0 + r) / p.group) * p.q.t + (row0 + r) % p.group * p.q.h + c);
     *reinterpret_cast<float4*>(qs + r * QP + c) = f;
   }
-  float m[A], l[A];
-  Two o[A][E / 2];                     // pairs of neighbouring columns
+  float m[MAPS][A], l[MAPS][A];
+  Two o[MAPS][A][E / 2];               // pairs of neighbouring columns
 #pragma unroll
-  for (int a = 0; a < A; ++a) {
-    m[a] = -INFINITY;
-    l[a] = 0.f;
+  for (int w = 0; w < MAPS; ++w)
 #pragma unroll
-    for (int c = 0; c < E / 2; ++c) o[a][c] = pack2(0.f, 0.f);
-  }
+    for (int a = 0; a < A; ++a) {
+      m[w][a] = -INFINITY;
+      l[w][a] = 0.f;
+#pragma unroll
+      for (int c = 0; c < E / 2; ++c) o[w][a][c] = pack2(0.f, 0.f);
+    }
   auto fetch = [&](int j, float* dst) {
     for (int i = threadIdx.x; i < BN * (D / 4); i += THREADS) {
       const int r = i / (D / 4), c = i % (D / 4) * 4;
@@ -92,180 +94,247 @@ __global__ void __launch_bounds__(THREADS) cross_kernel(const __grid_constant__ 
       for (int i = threadIdx.x; i < BN * (D / 4); i += THREADS) odd |= !all_finite(*reinterpret_cast<const float4*>(vs + i * 4));      // its own copies
     const bool careful = __syncthreads_or(odd) && p.mask;      // the tile is there, and the one before has been read: the next one takes its place
     if (j + BN < j1) fetch(j + BN, kv + ((j - j0) / BN + 1 & 1) * S::KV);
-    float s[A][N];
-    {
-      Two acc[A][N];                   // even and odd elements
 #pragma unroll
-      for (int a = 0; a < A; ++a)
-#pragma unroll
-        for (int c = 0; c < N; ++c) acc[a][c] = pack2(0.f, 0.f);
-#pragma unroll 4
-      for (int e = 0; e < D; e += 4) {
-        ulonglong2 x[A], y[N];
-#pragma unroll
-        for (int a = 0; a < A; ++a) x[a] = *reinterpret_cast<const ulonglong2*>(qs + (ty + 16 * a) * QP + e);
-#pragma unroll
-        for (int c = 0; c < N; ++c) y[c] = *reinterpret_cast<const ulonglong2*>(ks + (tx + 16 * c) * QP + e);
+    for (int w = 0; w < MAPS; ++w) {
+      if (w > 0) __syncwarp();           // the last map's weights have been read
+      float s[A][N];
+      {
+        Two acc[A][N];                   // even and odd elements
 #pragma unroll
         for (int a = 0; a < A; ++a)
 #pragma unroll
-          for (int c = 0; c < N; ++c) acc[a][c] = fma2_of(x[a].y, y[c].y, fma2_of(x[a].x, y[c].x, acc[a][c]));
-      }
+          for (int c = 0; c < N; ++c) acc[a][c] = pack2(0.f, 0.f);
+#pragma unroll 4
+        for (int e = w * (D / MAPS); e < (w + 1) * (D / MAPS); e += 4) {
+          ulonglong2 x[A], y[N];
 #pragma unroll
-      for (int a = 0; a < A; ++a)
+          for (int a = 0; a < A; ++a) x[a] = *reinterpret_cast<const ulonglong2*>(qs + (ty + 16 * a) * QP + e);
 #pragma unroll
-        for (int c = 0; c < N; ++c) {
-          float lo, hi;
-          unpack2(acc[a][c], lo, hi);
-          s[a][c] = lo + hi;
+          for (int c = 0; c < N; ++c) y[c] = *reinterpret_cast<const ulonglong2*>(ks + (tx + 16 * c) * QP + e);
+#pragma unroll
+          for (int a = 0; a < A; ++a)
+#pragma unroll
+            for (int c = 0; c < N; ++c) acc[a][c] = fma2_of(x[a].y, y[c].y, fma2_of(x[a].x, y[c].x, acc[a][c]));
         }
-    }
-    const bool whole = !p.mask && j + BN <= j1;      // every key of the tile is seen by every row
 #pragma unroll
-    for (int a = 0; a < A; ++a) {
-      bool seen[N];
+        for (int a = 0; a < A; ++a)
 #pragma unroll
-      for (int c = 0; c < N; ++c) seen[c] = true;
-      if (!whole) {
-        const int row = row0 + ty + 16 * a;
-        const uint8_t* mask = p.mask && row < rows ? p.mask + b * p.mask_b + (int64_t)(row / p.group) * p.mask_q + j : nullptr;
-#pragma unroll
-        for (int c = 0; c < N; ++c) {
-          const int at = tx + 16 * c;
-          seen[c] = j + at < j1 && (!mask || mask[at]);
-          if (!seen[c]) s[a][c] = -INFINITY;
-        }
+          for (int c = 0; c < N; ++c) {
+            float lo, hi;
+            unpack2(acc[a][c], lo, hi);
+            s[a][c] = lo + hi;
+          }
       }
-      float top = s[a][0];
+      const bool whole = !p.mask && j + BN <= j1;      // every key of the tile is seen by every row
 #pragma unroll
-      for (int c = 1; c < N; ++c) top = fmaxf(top, s[a][c]);
+      for (int a = 0; a < A; ++a) {
+        bool seen[N];
 #pragma unroll
-      for (int x = 8; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
-      top *= p.scale_log2;
-      const float now = fmaxf(m[a], top), base = now == -INFINITY ? 0.f : now;
-      const float fade = exp2_fast(m[a] - base);
-      m[a] = now;
-      float add = 0.f;
+        for (int c = 0; c < N; ++c) seen[c] = true;
+        if (!whole) {
+          const int row = row0 + ty + 16 * a;
+          const uint8_t* mask = p.mask && row < rows ? p.mask + b * p.mask_b + (int64_t)(row / p.group) * p.mask_q + j : nullptr;
 #pragma unroll
-      for (int c = 0; c < N; ++c) {
-        const float w = seen[c] ? exp2_fast(fmaf(s[a][c], p.scale_log2, -base)) : -0.f;
-        add += w;
-        ps[(ty + 16 * a) * PP + tx + 16 * c] = w;
-      }
-      l[a] = fmaf(l[a], fade, add);    // this thread's share of the keys
-      const Two f2 = pack2(fade, fade);
-#pragma unroll
-      for (int c = 0; c < E / 2; ++c) o[a][c] = mul2_of(o[a][c], f2);
-    }
-    __syncwarp();                      // a row's 16 threads are half a warp
-    if (!careful) {
-#pragma unroll 2
-      for (int i = 0; i < BN; i += 4) {  // four keys: a row's weights in one load
-        float4 w[A];
-#pragma unroll
-        for (int a = 0; a < A; ++a) w[a] = *reinterpret_cast<const float4*>(ps + (ty + 16 * a) * PP + i);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          Two y[E / 2];
-          load_pairs<D>(vs + (i + k) * D, tx, y);
-#pragma unroll
-          for (int a = 0; a < A; ++a) {
-            const float x = k == 0 ? w[a].x : k == 1 ? w[a].y : k == 2 ? w[a].z : w[a].w;
-            const Two x2 = pack2(x, x);
-#pragma unroll
-            for (int c = 0; c < E / 2; ++c) o[a][c] = fma2_of(x2, y[c], o[a][c]);
+          for (int c = 0; c < N; ++c) {
+            const int at = tx + 16 * c;
+            seen[c] = j + at < j1 && (!mask || mask[at]);
+            if (!seen[c]) s[a][c] = -INFINITY;
           }
         }
+        float top = s[a][0];
+#pragma unroll
+        for (int c = 1; c < N; ++c) top = fmaxf(top, s[a][c]);
+#pragma unroll
+        for (int x = 8; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
+        top *= p.scale_log2;
+        const float now = fmaxf(m[w][a], top), base = now == -INFINITY ? 0.f : now;
+        const float fade = exp2_fast(m[w][a] - base);
+        m[w][a] = now;
+        float add = 0.f;
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+          const float weight = seen[c] ? exp2_fast(fmaf(s[a][c], p.scale_log2, -base)) : -0.f;
+          add += weight;
+          ps[(ty + 16 * a) * PP + tx + 16 * c] = weight;
+        }
+        l[w][a] = fmaf(l[w][a], fade, add);    // this thread's share of the keys
+        const Two f2 = pack2(fade, fade);
+#pragma unroll
+        for (int c = 0; c < E / 2; ++c) o[w][a][c] = mul2_of(o[w][a][c], f2);
       }
-    } else {
+      __syncwarp();                      // a row's 16 threads are half a warp
+      if (!careful) {
+#pragma unroll 2
+        for (int i = 0; i < BN; i += 4) {  // four keys: a row's weights in one load
+          float4 row4[A];
+#pragma unroll
+          for (int a = 0; a < A; ++a) row4[a] = *reinterpret_cast<const float4*>(ps + (ty + 16 * a) * PP + i);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            Two y[E / 2];
+            load_pairs<D>(vs + (i + k) * D, tx, y);
+#pragma unroll
+            for (int a = 0; a < A; ++a) {
+              const float x = k == 0 ? row4[a].x : k == 1 ? row4[a].y : k == 2 ? row4[a].z : row4[a].w;
+              const Two x2 = pack2(x, x);
+#pragma unroll
+              for (int c = 0; c < E / 2; ++c) o[w][a][c] = fma2_of(x2, y[c], o[w][a][c]);
+            }
+          }
+        }
+      } else {
 #pragma unroll 1
-      for (int i = 0; i < BN; ++i) {
-        Two y[E / 2];
-        load_pairs<D>(vs + i * D, tx, y);
+        for (int i = 0; i < BN; ++i) {
+          Two y[E / 2];
+          load_pairs<D>(vs + i * D, tx, y);
 #pragma unroll
-        for (int a = 0; a < A; ++a) {
-          const float x = ps[(ty + 16 * a) * PP + i];
-          if (!signbit(x))
+          for (int a = 0; a < A; ++a) {
+            const float x = ps[(ty + 16 * a) * PP + i];
+            if (!signbit(x))
 #pragma unroll
-            for (int c = 0; c < E / 2; ++c) o[a][c] = fma2_of(pack2(x, x), y[c], o[a][c]);
+              for (int c = 0; c < E / 2; ++c) o[w][a][c] = fma2_of(pack2(x, x), y[c], o[w][a][c]);
+          }
         }
       }
     }
   }
+  if (MAPS == 1 || p.splits > 1) {
 #pragma unroll
-  for (int a = 0; a < A; ++a) {
+    for (int w = 0; w < MAPS; ++w)
 #pragma unroll
-    for (int x = 8; x > 0; x >>= 1) l[a] += __shfl_xor_sync(0xFFFFFFFFu, l[a], x);
-    const int row = row0 + ty + 16 * a;
-    if (row >= rows) continue;
-    const float inv = p.splits > 1 ? 1.f : l[a] == 0.f ? 0.f : 1.f / l[a];
-    const Part to = part_of(p, D, b, hk, row);
-    if (p.splits > 1 && tx == 0) to.stat[split] = make_float2(m[a], l[a]);
-    float* dst = p.splits > 1 ? to.sum + (int64_t)split * D
-                              : reinterpret_cast<float*>(p.o.p) + b * p.o.b + (int64_t)(row / p.group) * p.o.t + ((int64_t)hk * p.group + row % p.group) * p.o.h;
-    const Two i2 = pack2(inv, inv);
+      for (int a = 0; a < A; ++a) {
 #pragma unroll
-    for (int c = 0; c < E / 2; ++c) *reinterpret_cast<Two*>(dst + (D == 32 ? 2 * tx : 4 * tx + (c & 1) * 2 + (c >> 1) * 64)) = mul2_of(o[a][c], i2);
+        for (int x = 8; x > 0; x >>= 1) l[w][a] += __shfl_xor_sync(0xFFFFFFFFu, l[w][a], x);
+        const int row = row0 + ty + 16 * a;
+        if (row >= rows) continue;
+        const float inv = p.splits > 1 ? 1.f : l[w][a] == 0.f ? 0.f : 1.f / l[w][a];
+        const Part to = part_of<MAPS>(p, D, b, hk, row, w);
+        if (p.splits > 1 && tx == 0) to.stat[split] = make_float2(m[w][a], l[w][a]);
+        float* dst = p.splits > 1 ? to.sum + (int64_t)split * D
+                                  : reinterpret_cast<float*>(p.o.p) + b * p.o.b + (int64_t)(row / p.group) * p.o.t + ((int64_t)hk * p.group + row % p.group) * p.o.h;
+        const Two i2 = pack2(inv, inv);
+#pragma unroll
+        for (int c = 0; c < E / 2; ++c) *reinterpret_cast<Two*>(dst + (D == 32 ? 2 * tx : 4 * tx + (c & 1) * 2 + (c >> 1) * 64)) = mul2_of(o[w][a][c], i2);
+      }
+  }
+  if constexpr (MAPS == 2) {
+    if (p.splits == 1)
+#pragma unroll
+      for (int a = 0; a < A; ++a) {
+        const int row = row0 + ty + 16 * a;      // the other half of the warp has another one
+        const int head = hk * p.group + row % p.group;
+        // both halves' heads, one behind the other: a whole warp works out either
+        const float low = lambda_of(p.end, D / 2, __shfl_sync(0xFFFFFFFFu, head, 0)), high = lambda_of(p.end, D / 2, __shfl_sync(0xFFFFFFFFu, head, 16));
+        const float lambda = threadIdx.x % 32 < 16 ? low : high;
+        float inv[2];
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+#pragma unroll
+          for (int x = 8; x > 0; x >>= 1) l[w][a] += __shfl_xor_sync(0xFFFFFFFFu, l[w][a], x);
+          inv[w] = l[w][a] == 0.f ? 0.f : 1.f / l[w][a];
+        }
+        const Two one = pack2(inv[0], inv[0]), two = pack2(-lambda * inv[1], -lambda * inv[1]);
+        Two y[E / 2], sq = pack2(0.f, 0.f);
+#pragma unroll
+        for (int c = 0; c < E / 2; ++c) {
+          y[c] = fma2_of(o[1][a][c], two, mul2_of(o[0][a][c], one));
+          sq = fma2_of(y[c], y[c], sq);
+        }
+        float s0, s1;
+        unpack2(sq, s0, s1);
+        s0 += s1;
+#pragma unroll
+        for (int x = 8; x > 0; x >>= 1) s0 += __shfl_xor_sync(0xFFFFFFFFu, s0, x);
+        const float gain = row_gain<D>(p.end, s0);
+        if (row >= rows) continue;
+        float* dst = reinterpret_cast<float*>(p.o.p) + b * p.o.b + (int64_t)(row / p.group) * p.o.t + (int64_t)head * p.o.h;
+#pragma unroll
+        for (int c = 0; c < E / 2; ++c) {
+          const int d = D == 32 ? 2 * tx : 4 * tx + (c & 1) * 2 + (c >> 1) * 64;
+          *reinterpret_cast<Two*>(dst + d) = mul2_of(y[c], pack2(gain * norm_weight(p.end, d), gain * norm_weight(p.end, d + 1)));
+        }
+      }
   }
 }
 
 // One warp per row: out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s.
-template <typename T, int D>
-__global__ void __launch_bounds__(128) cross_join_kernel(const __grid_constant__ CrossParams p) {
+template <typename T, int D, int MAPS>
+__global__ void __launch_bounds__(128) cross_join_kernel(const __grid_constant__ ParamsOf<MAPS> p) {
   constexpr int E = D / 32;
   const int lane = threadIdx.x % 32, row = (int)blockIdx.x * 4 + (int)threadIdx.x / 32, hk = blockIdx.y, b = blockIdx.z;
   if (row >= clamp_length(p.q_lengths, b, p.q_tokens) * p.group) return;
   const int keys = clamp_length(p.kv_lengths, b, p.kv_tokens);
   const int n = p.split_keys == 0 ? p.splits : keys > p.split_keys ? (keys + p.split_keys - 1) / p.split_keys : 1;
-  const Part from = part_of(p, D, b, hk, row);
-  float top = -INFINITY;
-  for (int s = lane; s < n; s += 32) top = fmaxf(top, from.stat[s].x);
+  float y[MAPS][E];
 #pragma unroll
-  for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
-  if (top == -INFINITY) top = 0.f;
-  float o[E] = {}, l = 0.f;
+  for (int w = 0; w < MAPS; ++w) {
+    const Part from = part_of<MAPS>(p, D, b, hk, row, w);
+    float top = -INFINITY;
+    for (int s = lane; s < n; s += 32) top = fmaxf(top, from.stat[s].x);
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
+    if (top == -INFINITY) top = 0.f;
+    float o[E] = {}, l = 0.f;
 #pragma unroll 8                       // the loads of eight splits in flight together
-  for (int s = 0; s < n; ++s) {
-    const float2 st = from.stat[s];
-    const float f = exp2f(st.x - top);
-    l = fmaf(f, st.y, l);
+    for (int s = 0; s < n; ++s) {
+      const float2 st = from.stat[s];
+      const float f = exp2f(st.x - top);
+      l = fmaf(f, st.y, l);
 #pragma unroll
-    for (int c = 0; c < E; ++c) o[c] = fmaf(f, from.sum[(int64_t)s * D + lane * E + c], o[c]);
+      for (int c = 0; c < E; ++c) o[c] = fmaf(f, from.sum[(int64_t)s * D + lane * E + c], o[c]);
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int c = 0; c < E; ++c) y[w][c] = o[c] * inv;
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  T* dst = reinterpret_cast<T*>(p.o.p) + b * p.o.b + (int64_t)(row / p.group) * p.o.t + ((int64_t)hk * p.group + row % p.group) * p.o.h;
+  const int head = hk * p.group + row % p.group;
+  T* dst = reinterpret_cast<T*>(p.o.p) + b * p.o.b + (int64_t)(row / p.group) * p.o.t + (int64_t)head * p.o.h;
+  if constexpr (MAPS == 2) {
+    const float lambda = lambda_of(p.end, D / 2, head);
+    float squares = 0.f;
 #pragma unroll
-  for (int c = 0; c < E; ++c) dst[lane * E + c] = (T)(o[c] * inv);
+    for (int c = 0; c < E; ++c) {
+      y[0][c] = fmaf(-lambda, y[1][c], y[0][c]);
+      squares = fmaf(y[0][c], y[0][c], squares);
+    }
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) squares += __shfl_xor_sync(0xFFFFFFFFu, squares, x);
+    const float gain = row_gain<D>(p.end, squares);
+#pragma unroll
+    for (int c = 0; c < E; ++c) y[0][c] *= gain * norm_weight(p.end, lane * E + c);
+  }
+#pragma unroll
+  for (int c = 0; c < E; ++c) dst[lane * E + c] = (T)y[0][c];
 }
 
-template <int D, int BM>
-cudaError_t launch_scalar(const CrossParams& p, cudaStream_t s) {
+template <int D, int BM, int MAPS>
+cudaError_t launch_scalar(const ParamsOf<MAPS>& p, cudaStream_t s) {
   const size_t smem = Shape<D, BM>::smem;
   static OncePerContext once;
-  cudaError_t e = once([&] { return cudaFuncSetAttribute(cross_kernel<D, BM>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
+  cudaError_t e = once([&] { return cudaFuncSetAttribute(cross_kernel<D, BM, MAPS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
   if (e != cudaSuccess) return e;
   const int64_t tiles = ((int64_t)p.q_tokens * p.group + BM - 1) / BM;
-  cross_kernel<D, BM><<<dim3((unsigned)(tiles * p.splits), (unsigned)(p.heads / p.group), (unsigned)p.batch), THREADS, smem, s>>>(p);
+  cross_kernel<D, BM, MAPS><<<dim3((unsigned)(tiles * p.splits), (unsigned)(p.heads / p.group), (unsigned)p.batch), THREADS, smem, s>>>(p);
   return cudaGetLastError();
 }
-template <typename T, int D>
-cudaError_t launch_typed(const CrossParams& p, const CrossPlan& plan, cudaStream_t s) {
+template <typename T, int D, int MAPS>
+cudaError_t launch_typed(const ParamsOf<MAPS>& p, const CrossPlan& plan, cudaStream_t s) {
   cudaError_t e = cudaSuccess;
-  if constexpr (sizeof(T) == 2) e = launch_cross_few(p, D, plan.warps, s);
-  else e = plan.rows == 16 ? launch_scalar<D, 16>(p, s) : launch_scalar<D, 64>(p, s);
+  if constexpr (sizeof(T) == 2) e = launch_cross_few<MAPS>(p, D, plan.warps, s);
+  else e = plan.rows == 16 ? launch_scalar<D, 16, MAPS>(p, s) : launch_scalar<D, 64, MAPS>(p, s);
   if (e != cudaSuccess || p.splits == 1) return e;
   const int64_t rows = (int64_t)p.q_tokens * p.group;
-  cross_join_kernel<T, D><<<dim3((unsigned)((rows + 3) / 4), (unsigned)(p.heads / p.group), (unsigned)p.batch), 128, 0, s>>>(p);
+  cross_join_kernel<T, D, MAPS><<<dim3((unsigned)((rows + 3) / 4), (unsigned)(p.heads / p.group), (unsigned)p.batch), 128, 0, s>>>(p);
   return cudaGetLastError();
 }
-template <typename T>
-cudaError_t launch_typed(const CrossParams& p, const CrossPlan& plan, int D, cudaStream_t s) {
-  return D == 32 ? launch_typed<T, 32>(p, plan, s) : D == 64 ? launch_typed<T, 64>(p, plan, s) : launch_typed<T, 128>(p, plan, s);
+template <typename T, int MAPS>
+cudaError_t launch_typed(const ParamsOf<MAPS>& p, const CrossPlan& plan, int D, cudaStream_t s) {
+  return D == 32 ? launch_typed<T, 32, MAPS>(p, plan, s) : D == 64 ? launch_typed<T, 64, MAPS>(p, plan, s) : launch_typed<T, 128, MAPS>(p, plan, s);
 }
 
 }  // namespace
 
-CrossPlan cross_plan(int batch, int q_tokens, int kv_tokens, int heads, int group, int D, bool bf16, bool mask) {
+CrossPlan cross_plan(int batch, int q_tokens, int kv_tokens, int heads, int group, int D, bool bf16, bool mask, int maps) {
   CrossPlan plan{};
   plan.splits = plan.cluster = 1;
   // The kernel for many queries takes work from half a million keys x tiles of 16 rows on.  Both measured around that, us with the one for few and the one for
@@ -273,7 +342,7 @@ CrossPlan cross_plan(int batch, int q_tokens, int kv_tokens, int heads, int grou
   // one entry's 256 queries of 2 heads (0.15) 8.8 16.9, 10.5 21.6, 15.4 32.1; 700 (0.42) 18.2 17.5, 24.1 22.1, 40.9 34.8; 8 x 4 heads on 14400 keys, 65 queries
   // (2.3) 55.4 50.6, 81.5 52.6, 158 65.9.  So it is not taken too soon, and up to a third (heads of 64) or a half (128) too late where entries are several and
   // keys fewer than that.  (Masks are the other kernel's whatever the size; up to 64 queries leave three quarters of a tile of 256 rows empty.)
-  if (bf16 && !mask && q_tokens > 64 && kv_tokens > 0 &&
+  if (maps == 1 && bf16 && !mask && q_tokens > 64 && kv_tokens > 0 &&
       ((int64_t)q_tokens * group + 15) / 16 * batch * (heads / group) >= 500000 / kv_tokens + 1) {
     plan.kernel = CROSS_TC;
     plan.scratch = cross_tc_scratch(batch, q_tokens, kv_tokens, heads, D);
@@ -306,14 +375,18 @@ CrossPlan cross_plan(int batch, int q_tokens, int kv_tokens, int heads, int grou
     plan.split_keys = each > 0 ? (int)each : BN;
     plan.splits = kv_tokens > 0 ? (int)(((int64_t)kv_tokens + each - 1) / each) : 1;
   }
-  plan.scratch = plan.splits > 1 ? (uint64_t)(rows * batch * (heads / group)) * (uint64_t)plan.splits * (uint64_t)(D + 2) * 4u : 0u;
+  plan.scratch = plan.splits > 1 ? (uint64_t)(rows * maps * batch * (heads / group)) * (uint64_t)plan.splits * (uint64_t)(D + 2) * 4u : 0u;
   return plan;
 }
 
-cudaError_t launch_cross(const CrossParams& p, const CrossPlan& plan, bool bf16, int D, cudaStream_t s) {
-  if (plan.kernel == CROSS_TC) return launch_cross_tc(p, D, s);
-  return bf16 ? launch_typed<__nv_bfloat16>(p, plan, D, s) : launch_typed<float>(p, plan, D, s);
+template <int MAPS>
+cudaError_t launch_cross(const ParamsOf<MAPS>& p, const CrossPlan& plan, bool bf16, int D, cudaStream_t s) {
+  if constexpr (MAPS == 1)
+    if (plan.kernel == CROSS_TC) return launch_cross_tc(p, D, s);
+  return bf16 ? launch_typed<__nv_bfloat16, MAPS>(p, plan, D, s) : launch_typed<float, MAPS>(p, plan, D, s);
 }
+template cudaError_t launch_cross<1>(const CrossParams&, const CrossPlan&, bool, int, cudaStream_t);
+template cudaError_t launch_cross<2>(const DiffParams&, const CrossPlan&, bool, int, cudaStream_t);
 
 }  // namespace tok
 }  // namespace tt

@@ -21,14 +21,16 @@ namespace {
 
 constexpr int MAX_CLUSTER = 8;
 
+template <int MAPS>
 struct CrossFewParams {
   TensorMap128 map_k, map_v;                   // [D][token][head][batch], box of Few::KEYS tokens
-  CrossParams c;
+  ParamsOf<MAPS> c;
   int32_t k_h, k_b, v_h, v_b;                  // 0 where the axis is shared, else 1
 };
 
-template <int D, int W>
+template <int D, int W, int M>
 struct Few {
+  static constexpr int MAPS = M;               // 2: differential attention, a map of either half of the heads
   static constexpr int WARPS = W;
   static constexpr int THREADS = WARPS * 32;
   static constexpr int STAGES = 3;
@@ -43,7 +45,7 @@ struct Few {
   static constexpr int OP = D + 8;             // pitch of the joint sums
   static constexpr int SMEM = WARPS * RING + 1024;
   static constexpr int BLOCKS = W == 4 ? 2 : 1;                   // to a multiprocessor
-  static_assert(WARPS * 16 * OP * 4 <= WARPS * RING, "the sums take the rings' place");
+  static_assert(MAPS * WARPS * 16 * OP * 4 <= WARPS * RING, "the sums take the rings' place");
 };
 
 __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -60,7 +62,7 @@ __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
 template <int D>
 __device__ __forceinline__ uint32_t run_at(int row, int run) {
   if (D == 32) return (uint32_t)(row * 64 + ((run ^ (row >> 1 & 3)) << 4));
-  return (uint32_t)((run >> 3) * Few<D, 4>::SLAB_BYTES + row * 128 + (((run & 7) ^ (row & 7)) << 4));
+  return (uint32_t)((run >> 3) * Few<D, 4, 1>::SLAB_BYTES + row * 128 + (((run & 7) ^ (row & 7)) << 4));
 }
 // A pair of floats from the same place in the shared memory of block `rank` of the cluster.
 __device__ __forceinline__ float2 cluster_load(const float2* at, int rank, int cluster) {
@@ -86,7 +88,7 @@ __device__ __noinline__ void sums_again(const CrossParams& p, int b, int hk, int
   }
   for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
   for (int j = first; j < j1; j += step)
-    for (int key = j; key < min(j1, j + Few<D, 4>::KEYS); ++key) {
+    for (int key = j; key < min(j1, j + Few<D, 4, 1>::KEYS); ++key) {
       float w[2];
       for (int r = 0; r < 2; ++r) {
         float s = 0.f;
@@ -100,15 +102,16 @@ __device__ __noinline__ void sums_again(const CrossParams& p, int b, int hk, int
     }
 }
 
-template <int D, bool MASK, int W>
-__global__ void __launch_bounds__(Few<D, W>::THREADS, Few<D, W>::BLOCKS) cross_few_kernel(const __grid_constant__ CrossFewParams pp) {
-  using F = Few<D, W>;
-  const CrossParams& p = pp.c;
+template <int D, bool MASK, int W, int MAPS>
+__global__ void __launch_bounds__(Few<D, W, MAPS>::THREADS, Few<D, W, MAPS>::BLOCKS) cross_few_kernel(const __grid_constant__ CrossFewParams<MAPS> pp) {
+  using F = Few<D, W, MAPS>;
+  const ParamsOf<MAPS>& p = pp.c;
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t s_full[F::WARPS][F::STAGES];
-  __shared__ float2 s_ml[F::WARPS][16];
-  __shared__ float s_sum[16][D];
-  __shared__ float2 s_stat[16];
+  __shared__ float2 s_ml[MAPS][F::WARPS][16];
+  __shared__ float s_sum[MAPS][16][D];
+  __shared__ float2 s_stat[MAPS][16];
+  __shared__ float s_lambda[16];
   uint8_t* ring0 = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int pieces = p.splits * p.cluster;
@@ -179,10 +182,20 @@ __global__ void __launch_bounds__(Few<D, W>::THREADS, Few<D, W>::BLOCKS) cross_f
     }
     fetch_mask(first);
   }
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-  float o[F::NT][4];
+  if constexpr (MAPS == 2) {
+    for (int r = warp; r < 16; r += F::WARPS) {
+      const float f = lambda_of(p.end, D / 2, hk * p.group + (row0 + r) % p.group);
+      if (lane == 0) s_lambda[r] = f;
+    }
+  }
+  float m[MAPS][2], l[MAPS][2], o[MAPS][F::NT][4];
 #pragma unroll
-  for (int i = 0; i < F::NT; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+  for (int w = 0; w < MAPS; ++w) {
+    m[w][0] = m[w][1] = -INFINITY;
+    l[w][0] = l[w][1] = 0.f;
+#pragma unroll
+    for (int i = 0; i < F::NT; ++i) o[w][i][0] = o[w][i][1] = o[w][i][2] = o[w][i][3] = 0.f;
+  }
   const float c = p.scale_log2;
 
   int stage = 0;
@@ -207,60 +220,64 @@ __global__ void __launch_bounds__(Few<D, W>::THREADS, Few<D, W>::BLOCKS) cross_f
         asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(vs + run_at<D>(rem + i / (D / 8), i % (D / 8))), "r"(0u) : "memory");
       __syncwarp();
     }
-    float s[F::NK][4];                         // keys 8 n + 2t, 8 n + 2t + 1 for rows g, g + 8
+    float s[MAPS][F::NK][4];                   // keys 8 n + 2t, 8 n + 2t + 1 for rows g, g + 8
 #pragma unroll
     for (int n = 0; n < F::NK; ++n) {
-      s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+#pragma unroll
+      for (int w = 0; w < MAPS; ++w) s[w][n][0] = s[w][n][1] = s[w][n][2] = s[w][n][3] = 0.f;
 #pragma unroll
       for (int x = 0; x < D / 32; ++x) {       // 32 elements of 8 keys
         uint32_t f[4];
         ldmatrix4<false>(f, ks + run_at<D>(8 * n + (lane & 7), 4 * x + (lane >> 3)));
-        mma16816(s[n], q[2 * x], f[0], f[1]);
-        mma16816(s[n], q[2 * x + 1], f[2], f[3]);
+        mma16816(s[2 * x / (D / 16 / MAPS)][n], q[2 * x], f[0], f[1]);
+        mma16816(s[(2 * x + 1) / (D / 16 / MAPS)][n], q[2 * x + 1], f[2], f[3]);
       }
     }
-    if (rem < F::KEYS) {
+#pragma unroll
+    for (int w = 0; w < MAPS; ++w) {
+      if (rem < F::KEYS) {
+#pragma unroll
+        for (int n = 0; n < F::NK; ++n)
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            if (8 * n + 2 * t + (x & 1) >= rem) s[w][n][x] = -INFINITY;
+      }
+      if (MASK) {
+#pragma unroll
+        for (int n = 0; n < F::NK; ++n)
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            if ((seen[n][x >> 1] & (x & 1 ? 0xFF00u : 0xFFu)) == 0u) s[w][n][x] = -INFINITY;
+      }
+      float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+      for (int n = 0; n < F::NK; ++n) {
+        top[0] = max3(top[0], s[w][n][0], s[w][n][1]);
+        top[1] = max3(top[1], s[w][n][2], s[w][n][3]);
+      }
+      if (__any_sync(0xffffffffu, top[0] * c > m[w][0] + 8.f || top[1] * c > m[w][1] + 8.f)) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          float now = top[r] * c;
+          now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, 1));
+          now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, 2));
+          now = fmaxf(now, m[w][r]);
+          const float fade = now == -INFINITY ? 1.f : exp2_fast(m[w][r] - now);
+          m[w][r] = now;
+          l[w][r] *= fade;
+#pragma unroll
+          for (int i = 0; i < F::NT; ++i) { o[w][i][2 * r] *= fade; o[w][i][2 * r + 1] *= fade; }
+        }
+      }
+      const float base[2] = {m[w][0] == -INFINITY ? 0.f : m[w][0], m[w][1] == -INFINITY ? 0.f : m[w][1]};
 #pragma unroll
       for (int n = 0; n < F::NK; ++n)
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
-          if (8 * n + 2 * t + (x & 1) >= rem) s[n][x] = -INFINITY;
+        for (int x = 0; x < 4; ++x) {
+          s[w][n][x] = exp2_fast(fmaf(s[w][n][x], c, -base[x >> 1]));
+          l[w][x >> 1] += s[w][n][x];
+        }
     }
-    if (MASK) {
-#pragma unroll
-      for (int n = 0; n < F::NK; ++n)
-#pragma unroll
-        for (int x = 0; x < 4; ++x)
-          if ((seen[n][x >> 1] & (x & 1 ? 0xFF00u : 0xFFu)) == 0u) s[n][x] = -INFINITY;
-    }
-    float top[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-    for (int n = 0; n < F::NK; ++n) {
-      top[0] = max3(top[0], s[n][0], s[n][1]);
-      top[1] = max3(top[1], s[n][2], s[n][3]);
-    }
-    if (__any_sync(0xffffffffu, top[0] * c > m[0] + 8.f || top[1] * c > m[1] + 8.f)) {
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        float now = top[r] * c;
-        now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, 1));
-        now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, 2));
-        now = fmaxf(now, m[r]);
-        const float fade = now == -INFINITY ? 1.f : exp2_fast(m[r] - now);
-        m[r] = now;
-        l[r] *= fade;
-#pragma unroll
-        for (int i = 0; i < F::NT; ++i) { o[i][2 * r] *= fade; o[i][2 * r + 1] *= fade; }
-      }
-    }
-    const float base[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};
-#pragma unroll
-    for (int n = 0; n < F::NK; ++n)
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        s[n][x] = exp2_fast(fmaf(s[n][x], c, -base[x >> 1]));
-        l[x >> 1] += s[n][x];
-      }
     bool careful = false;
     if (MASK) {
       // an infinity or NaN among the values: times 0 it is a NaN, which the sum then keeps
@@ -277,21 +294,26 @@ __global__ void __launch_bounds__(Few<D, W>::THREADS, Few<D, W>::BLOCKS) cross_f
     if (!MASK || !careful) {
 #pragma unroll
       for (int k = 0; k < F::NK / 2; ++k) {    // 16 keys
-        uint32_t hi[4], lo[4];
+        uint32_t hi[MAPS][4], lo[MAPS][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float a = s[2 * k + (i >> 1)][2 * (i & 1)], e = s[2 * k + (i >> 1)][2 * (i & 1) + 1];
-          hi[i] = pack_bf16(a, e);
-          lo[i] = pack_bf16(a - __uint_as_float(hi[i] << 16), e - __uint_as_float(hi[i] & 0xFFFF0000u));
-        }
+        for (int w = 0; w < MAPS; ++w)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float a = s[w][2 * k + (i >> 1)][2 * (i & 1)], e = s[w][2 * k + (i >> 1)][2 * (i & 1) + 1];
+            hi[w][i] = pack_bf16(a, e);
+            lo[w][i] = pack_bf16(a - __uint_as_float(hi[w][i] << 16), e - __uint_as_float(hi[w][i] & 0xFFFF0000u));
+          }
 #pragma unroll
         for (int x = 0; x < D / 16; ++x) {     // 16 columns
           uint32_t f[4];
           ldmatrix4<true>(f, vs + run_at<D>(16 * k + (lane & 15), 2 * x + (lane >> 4)));
-          mma16816(o[2 * x], hi, f[0], f[1]);
-          mma16816(o[2 * x], lo, f[0], f[1]);
-          mma16816(o[2 * x + 1], hi, f[2], f[3]);
-          mma16816(o[2 * x + 1], lo, f[2], f[3]);
+#pragma unroll
+          for (int w = 0; w < MAPS; ++w) {
+            mma16816(o[w][2 * x], hi[w], f[0], f[1]);
+            mma16816(o[w][2 * x], lo[w], f[0], f[1]);
+            mma16816(o[w][2 * x + 1], hi[w], f[2], f[3]);
+            mma16816(o[w][2 * x + 1], lo[w], f[2], f[3]);
+          }
         }
       }
     } else {
@@ -301,11 +323,12 @@ __global__ void __launch_bounds__(Few<D, W>::THREADS, Few<D, W>::BLOCKS) cross_f
 #pragma unroll 1
         for (int kk = 0; kk < 8 && 8 * n + kk < rem; ++kk) {
           const int from = (lane & ~3) | (kk >> 1), key = 8 * n + kk;
-          float mine[2];
+          float mine[MAPS][2];
           uint32_t sees[2];
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
-            mine[r] = __shfl_sync(0xffffffffu, kk & 1 ? s[n][2 * r + 1] : s[n][2 * r], from);
+#pragma unroll
+            for (int w = 0; w < MAPS; ++w) mine[w][r] = __shfl_sync(0xffffffffu, kk & 1 ? s[w][n][2 * r + 1] : s[w][n][2 * r], from);
             sees[r] = __shfl_sync(0xffffffffu, seen[n][r] >> (8 * (kk & 1)) & 0xFFu, from);
           }
 #pragma unroll
@@ -313,8 +336,11 @@ __global__ void __launch_bounds__(Few<D, W>::THREADS, Few<D, W>::BLOCKS) cross_f
             uint32_t u;
             asm volatile("ld.shared.b32 %0, [%1];" : "=r"(u) : "r"(vs + run_at<D>(key, i) + (uint32_t)(4 * t)));
             const float v0 = __uint_as_float(u << 16), v1 = __uint_as_float(u & 0xFFFF0000u);
-            if (sees[0]) { o[i][0] = fmaf(mine[0], v0, o[i][0]); o[i][1] = fmaf(mine[0], v1, o[i][1]); }
-            if (sees[1]) { o[i][2] = fmaf(mine[1], v0, o[i][2]); o[i][3] = fmaf(mine[1], v1, o[i][3]); }
+#pragma unroll
+            for (int w = 0; w < MAPS; ++w) {
+              if (sees[0]) { o[w][i][0] = fmaf(mine[w][0], v0, o[w][i][0]); o[w][i][1] = fmaf(mine[w][0], v1, o[w][i][1]); }
+              if (sees[1]) { o[w][i][2] = fmaf(mine[w][1], v0, o[w][i][2]); o[w][i][3] = fmaf(mine[w][1], v1, o[w][i][3]); }
+            }
           }
         }
     }
@@ -322,72 +348,77 @@ __global__ void __launch_bounds__(Few<D, W>::THREADS, Few<D, W>::BLOCKS) cross_f
     if (lane == 0 && j + F::STAGES * STEP < j1) load(j + F::STAGES * STEP, stage);
     if (++stage == F::STAGES) { stage = 0; phase ^= 1u; }
   }
-  if (!MASK) {
+  if constexpr (!MASK && MAPS == 1) {
     // (under a mask every tile's values are looked at before they are used; here that took eight streams' 14400 keys from 18.2 to 20.0 us)
     float odd[4] = {0.f, 0.f, 0.f, 0.f};       // four chains
 #pragma unroll
     for (int i = 0; i < F::NT; ++i)
 #pragma unroll
-      for (int x = 0; x < 4; ++x) odd[x] = fmaf(o[i][x], 0.f, odd[x]);
+      for (int x = 0; x < 4; ++x) odd[x] = fmaf(o[0][i][x], 0.f, odd[x]);
     if (__builtin_expect(__any_sync(0xffffffffu, odd[0] + odd[1] + (odd[2] + odd[3]) != 0.f), 0)) {
-      const float top[2] = {m[0], m[1]};
+      const float top[2] = {m[0][0], m[0][1]};
       float again[F::NT][4];
       sums_again<D>(p, b, hk, row0, rows, first, j1, STEP, top, again);
 #pragma unroll
       for (int i = 0; i < F::NT; ++i)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) o[i][x] = again[i][x];
+        for (int x = 0; x < 4; ++x) o[0][i][x] = again[i][x];
     }
   }
 
   // join the warps: row r of the tile, element d.  The sums take the place of the rings, whose copies have all landed.
   __syncthreads();
-  float* s_o = reinterpret_cast<float*>(ring0);      // [WARPS][16][OP]
+  float* s_o = reinterpret_cast<float*>(ring0);      // [MAPS][WARPS][16][OP]
 #pragma unroll
-  for (int r = 0; r < 2; ++r) {
-    l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
-    l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
-    if (t == 0) s_ml[warp][g + 8 * r] = make_float2(m[r], l[r]);
+  for (int w = 0; w < MAPS; ++w)
 #pragma unroll
-    for (int i = 0; i < F::NT; ++i) *reinterpret_cast<float2*>(s_o + (warp * 16 + g + 8 * r) * F::OP + 8 * i + 2 * t) = make_float2(o[i][2 * r], o[i][2 * r + 1]);
-  }
-  __syncthreads();
-  for (int i = threadIdx.x; i < 16 * (D / 2); i += F::THREADS) {
-    const int r = i / (D / 2), d = i % (D / 2) * 2;
-    float top = -INFINITY;
+    for (int r = 0; r < 2; ++r) {
+      l[w][r] += __shfl_xor_sync(0xffffffffu, l[w][r], 1);
+      l[w][r] += __shfl_xor_sync(0xffffffffu, l[w][r], 2);
+      if (t == 0) s_ml[w][warp][g + 8 * r] = make_float2(m[w][r], l[w][r]);
 #pragma unroll
-    for (int x = 0; x < F::WARPS; ++x) top = fmaxf(top, s_ml[x][r].x);
-    const float base = top == -INFINITY ? 0.f : top;
-    float a = 0.f, e = 0.f, total = 0.f;
-#pragma unroll
-    for (int x = 0; x < F::WARPS; ++x) {
-      const float2 ml = s_ml[x][r], v = *reinterpret_cast<const float2*>(s_o + (x * 16 + r) * F::OP + d);
-      const float f = exp2_fast(ml.x - base);
-      total = fmaf(f, ml.y, total);
-      a = fmaf(f, v.x, a);
-      e = fmaf(f, v.y, e);
+      for (int i = 0; i < F::NT; ++i)
+        *reinterpret_cast<float2*>(s_o + ((w * F::WARPS + warp) * 16 + g + 8 * r) * F::OP + 8 * i + 2 * t) = make_float2(o[w][i][2 * r], o[w][i][2 * r + 1]);
     }
-    *reinterpret_cast<float2*>(&s_sum[r][d]) = make_float2(a, e);
-    if (d == 0) s_stat[r] = make_float2(top, total);
-  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < MAPS; ++w)
+    for (int i = threadIdx.x; i < 16 * (D / 2); i += F::THREADS) {
+      const int r = i / (D / 2), d = i % (D / 2) * 2;
+      float top = -INFINITY;
+#pragma unroll
+      for (int x = 0; x < F::WARPS; ++x) top = fmaxf(top, s_ml[w][x][r].x);
+      const float base = top == -INFINITY ? 0.f : top;
+      float a = 0.f, e = 0.f, total = 0.f;
+#pragma unroll
+      for (int x = 0; x < F::WARPS; ++x) {
+        const float2 ml = s_ml[w][x][r], v = *reinterpret_cast<const float2*>(s_o + ((w * F::WARPS + x) * 16 + r) * F::OP + d);
+        const float f = exp2_fast(ml.x - base);
+        total = fmaf(f, ml.y, total);
+        a = fmaf(f, v.x, a);
+        e = fmaf(f, v.y, e);
+      }
+      *reinterpret_cast<float2*>(&s_sum[w][r][d]) = make_float2(a, e);
+      if (d == 0) s_stat[w][r] = make_float2(top, total);
+    }
   // join the blocks of the cluster: each takes its share of the elements from all of them
   if (p.cluster > 1) cluster_sync_all();
   else __syncthreads();
   const int rank = p.cluster > 1 ? (int)cluster_ctarank() : 0;
-  for (int i = rank * F::THREADS + threadIdx.x; i < 16 * (D / 2); i += F::THREADS * p.cluster) {
-    const int r = i / (D / 2), d = i % (D / 2) * 2, row = row0 + r;
-    if (row >= rows) break;
+  // elements d and d + 1 of row r, map w, of all blocks: sums, total and maximum
+  auto joined = [&](int w, int r, int d, float& top, float& total) {
     float2 stat[MAX_CLUSTER], sum[MAX_CLUSTER];
-    float top = -INFINITY;
+    top = -INFINITY;
 #pragma unroll
     for (int x = 0; x < MAX_CLUSTER; ++x)
       if (x < p.cluster) {
-        stat[x] = cluster_load(&s_stat[r], x, p.cluster);
-        sum[x] = cluster_load(reinterpret_cast<float2*>(&s_sum[r][d]), x, p.cluster);
+        stat[x] = cluster_load(&s_stat[w][r], x, p.cluster);
+        sum[x] = cluster_load(reinterpret_cast<float2*>(&s_sum[w][r][d]), x, p.cluster);
         top = fmaxf(top, stat[x].x);
       }
     const float base = top == -INFINITY ? 0.f : top;
-    float a = 0.f, e = 0.f, total = 0.f;
+    float a = 0.f, e = 0.f;
+    total = 0.f;
 #pragma unroll
     for (int x = 0; x < MAX_CLUSTER; ++x)
       if (x < p.cluster) {
@@ -396,47 +427,94 @@ __global__ void __launch_bounds__(Few<D, W>::THREADS, Few<D, W>::BLOCKS) cross_f
         a = fmaf(f, sum[x].x, a);
         e = fmaf(f, sum[x].y, e);
       }
-    if (p.splits > 1) {
-      const Part to = part_of(p, D, b, hk, row);
-      const int split = piece / p.cluster;
-      if (d == 0) to.stat[split] = make_float2(top, total);
-      *reinterpret_cast<float2*>(to.sum + (int64_t)split * D + d) = make_float2(a, e);
-    } else {
-      const float inv = total == 0.f ? 0.f : 1.f / total;
-      __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.o.p) + b * p.o.b + (int64_t)(row / p.group) * p.o.t + ((int64_t)hk * p.group + row % p.group) * p.o.h;
-      *reinterpret_cast<uint32_t*>(dst + d) = pack_bf16(a * inv, e * inv);
-    }
+    return make_float2(a, e);
+  };
+  if (MAPS == 1 || p.splits > 1) {
+#pragma unroll
+    for (int w = 0; w < MAPS; ++w)
+      for (int i = rank * F::THREADS + threadIdx.x; i < 16 * (D / 2); i += F::THREADS * p.cluster) {
+        const int r = i / (D / 2), d = i % (D / 2) * 2, row = row0 + r;
+        if (row >= rows) break;
+        float top, total;
+        const float2 sum = joined(w, r, d, top, total);
+        if (p.splits > 1) {
+          const Part to = part_of<MAPS>(p, D, b, hk, row, w);
+          const int split = piece / p.cluster;
+          if (d == 0) to.stat[split] = make_float2(top, total);
+          *reinterpret_cast<float2*>(to.sum + (int64_t)split * D + d) = sum;
+        } else {
+          const float inv = total == 0.f ? 0.f : 1.f / total;
+          __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.o.p) + b * p.o.b + (int64_t)(row / p.group) * p.o.t + ((int64_t)hk * p.group + row % p.group) * p.o.h;
+          *reinterpret_cast<uint32_t*>(dst + d) = pack_bf16(sum.x * inv, sum.y * inv);
+        }
+      }
+  }
+  if constexpr (MAPS == 2) {
+    // a warp to a row, whose norm takes all of its elements
+    if (p.splits == 1)
+      for (int r = rank * F::WARPS + warp; r < 16 && row0 + r < rows; r += F::WARPS * p.cluster) {
+        constexpr int E = (D + 63) / 64;       // pairs of a lane (heads of 32: of the first 16 lanes)
+        const int row = row0 + r;
+        float2 y[E];
+        float squares = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const int d = 64 * e + 2 * lane;
+          y[e] = make_float2(0.f, 0.f);
+          if (d < D) {
+            float top, total;
+            const float2 one = joined(0, r, d, top, total);
+            const float i1 = total == 0.f ? 0.f : 1.f / total;
+            const float2 two = joined(1, r, d, top, total);
+            const float i2 = total == 0.f ? 0.f : s_lambda[r] / total;
+            y[e] = make_float2(one.x * i1 - two.x * i2, one.y * i1 - two.y * i2);
+          }
+          squares = fmaf(y[e].x, y[e].x, fmaf(y[e].y, y[e].y, squares));
+        }
+#pragma unroll
+        for (int x = 16; x > 0; x >>= 1) squares += __shfl_xor_sync(0xffffffffu, squares, x);
+        const float gain = row_gain<D>(p.end, squares);
+        __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.o.p) + b * p.o.b + (int64_t)(row / p.group) * p.o.t + ((int64_t)hk * p.group + row % p.group) * p.o.h;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const int d = 64 * e + 2 * lane;
+          if (d < D) *reinterpret_cast<uint32_t*>(dst + d) = pack_bf16(y[e].x * gain * norm_weight(p.end, d), y[e].y * gain * norm_weight(p.end, d + 1));
+        }
+      }
   }
   if (p.cluster > 1) cluster_sync_all();       // no block leaves while another reads its sums
 }
 
-template <int D, bool MASK, int W>
-cudaError_t launch(const CrossFewParams& p, cudaStream_t s) {
-  using F = Few<D, W>;
+template <int D, bool MASK, int W, int MAPS>
+cudaError_t launch(const CrossFewParams<MAPS>& p, cudaStream_t s) {
+  using F = Few<D, W, MAPS>;
   static OncePerContext once;
-  const cudaError_t e = once([] { return cudaFuncSetAttribute(cross_few_kernel<D, MASK, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::SMEM); });
+  const cudaError_t e = once([] { return cudaFuncSetAttribute(cross_few_kernel<D, MASK, W, MAPS>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::SMEM); });
   if (e != cudaSuccess) return e;
   const int64_t tiles = ((int64_t)p.c.q_tokens * p.c.group + 15) / 16;
-  return launch_kernel(cross_few_kernel<D, MASK, W>, dim3((unsigned)(tiles * p.c.splits * p.c.cluster), (unsigned)(p.c.heads / p.c.group), (unsigned)p.c.batch),
+  return launch_kernel(cross_few_kernel<D, MASK, W, MAPS>, dim3((unsigned)(tiles * p.c.splits * p.c.cluster), (unsigned)(p.c.heads / p.c.group), (unsigned)p.c.batch),
                        F::THREADS, F::SMEM, s, p, false, p.c.cluster);
 }
-template <int D>
-cudaError_t launch(const CrossParams& c, int warps, cudaStream_t s) {
-  CrossFewParams p{};
-  const int kv_heads = c.heads / c.group, keys = Few<D, 4>::KEYS;
+template <int D, int MAPS>
+cudaError_t launch(const ParamsOf<MAPS>& c, int warps, cudaStream_t s) {
+  CrossFewParams<MAPS> p{};
+  const int kv_heads = c.heads / c.group, keys = Few<D, 4, MAPS>::KEYS;
   if (c.kv_tokens > 0 && (!token_map(&p.map_k, c.k, D, c.kv_tokens, kv_heads, c.batch, keys) || !token_map(&p.map_v, c.v, D, c.kv_tokens, kv_heads, c.batch, keys)))
     return cudaErrorInvalidValue;
   p.c = c;
   p.k_h = c.k.h != 0; p.k_b = c.k.b != 0; p.v_h = c.v.h != 0; p.v_b = c.v.b != 0;
-  if (warps == 8) return p.c.mask ? launch<D, true, 8>(p, s) : launch<D, false, 8>(p, s);
-  return p.c.mask ? launch<D, true, 4>(p, s) : launch<D, false, 4>(p, s);
+  if (warps == 8) return p.c.mask ? launch<D, true, 8, MAPS>(p, s) : launch<D, false, 8, MAPS>(p, s);
+  return p.c.mask ? launch<D, true, 4, MAPS>(p, s) : launch<D, false, 4, MAPS>(p, s);
 }
 
 }  // namespace
 
-cudaError_t launch_cross_few(const CrossParams& p, int D, int warps, cudaStream_t s) {
-  return D == 32 ? launch<32>(p, warps, s) : D == 64 ? launch<64>(p, warps, s) : launch<128>(p, warps, s);
+template <int MAPS>
+cudaError_t launch_cross_few(const ParamsOf<MAPS>& p, int D, int warps, cudaStream_t s) {
+  return D == 32 ? launch<32, MAPS>(p, warps, s) : D == 64 ? launch<64, MAPS>(p, warps, s) : launch<128, MAPS>(p, warps, s);
 }
+template cudaError_t launch_cross_few<1>(const CrossParams&, int, int, cudaStream_t);
+template cudaError_t launch_cross_few<2>(const DiffParams&, int, int, cudaStream_t);
 
 }  // namespace tok
 }  // namespace tt

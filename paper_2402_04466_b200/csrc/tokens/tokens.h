@@ -1,5 +1,8 @@
-// Launch interfaces of the operators over tokens (tt.h: tt_qk_norm_rope, tt_linear_attention, tt_delta_rule, tt_cross_attention).
+// Launch interfaces of the operators over tokens (tt.h: tt_qk_norm_rope, tt_linear_attention, tt_delta_rule, tt_cross_attention,
+// tt_differential_attention).
 #pragma once
+
+#include <type_traits>
 
 #include "../tt_internal.h"
 
@@ -76,6 +79,19 @@ struct alignas(32) CrossParams {
   int32_t cluster;              // blocks that share a piece
   float scale_log2;             // scale * log2(e)
 };
+// Differential attention is cross attention with two maps, each of one half of a head's queries and keys, over the same values, and an end of its own.
+struct DiffEnd {
+  const float* lambda;          // four vectors of head_dim / 2
+  int64_t lambda_h;             // from one head's to the next's, 0: shared
+  const float* weight;          // of the norm, or null
+  float lambda_init, eps, out_scale;
+  int32_t norm;
+};
+struct alignas(32) DiffParams : CrossParams {
+  DiffEnd end;
+};
+template <int MAPS>
+using ParamsOf = std::conditional_t<MAPS == 2, DiffParams, CrossParams>;
 enum { CROSS_SCALAR = 0, CROSS_TC = 1, CROSS_FEW = 2 };
 struct CrossPlan {
   int32_t kernel;               // one of CROSS_...
@@ -84,10 +100,12 @@ struct CrossPlan {
   int32_t splits, split_keys, cluster;
   uint64_t scratch;
 };
-CrossPlan cross_plan(int batch, int q_tokens, int kv_tokens, int heads, int group, int D, bool bf16, bool mask);
-cudaError_t launch_cross(const CrossParams& p, const CrossPlan& plan, bool bf16, int D, cudaStream_t s);
+CrossPlan cross_plan(int batch, int q_tokens, int kv_tokens, int heads, int group, int D, bool bf16, bool mask, int maps);
+template <int MAPS>
+cudaError_t launch_cross(const ParamsOf<MAPS>& p, const CrossPlan& plan, bool bf16, int D, cudaStream_t s);
 
-cudaError_t launch_cross_few(const CrossParams& p, int D, int warps, cudaStream_t s);   // splits > 1: the join is the caller's
+template <int MAPS>
+cudaError_t launch_cross_few(const ParamsOf<MAPS>& p, int D, int warps, cudaStream_t s);   // splits > 1: the join is the caller's
 cudaError_t launch_cross_tc(const CrossParams& p, int D, cudaStream_t s);         // kv_tokens > 0
 uint64_t cross_tc_scratch(int batch, int q_tokens, int kv_tokens, int heads, int D);
 
@@ -101,16 +119,41 @@ __device__ __forceinline__ int clamp_length(const int32_t* lengths, int b, int e
   return n < 0 ? 0 : n > extent ? extent : n;
 }
 
-// Where a row's partial results lie: [batch][kv head][row][split], maximum and total first, then the sums.
+// Where a row's partial results lie: [batch][kv head][row][map][split], maximum and total first, then the sums.
 struct Part {
   float2* stat;
   float* sum;
 };
-__device__ __forceinline__ Part part_of(const CrossParams& p, int D, int b, int hk, int row) {
-  const int64_t rows = (int64_t)p.q_tokens * p.group, all = rows * p.batch * (p.heads / p.group);
-  const int64_t at = (((int64_t)b * (p.heads / p.group) + hk) * rows + row) * p.splits;
+template <int MAPS>
+__device__ __forceinline__ Part part_of(const CrossParams& p, int D, int b, int hk, int row, int map) {
+  const int64_t rows = (int64_t)p.q_tokens * p.group * MAPS, all = rows * p.batch * (p.heads / p.group);
+  const int64_t at = (((int64_t)b * (p.heads / p.group) + hk) * rows + (int64_t)row * MAPS + map) * p.splits;
   return {reinterpret_cast<float2*>(p.part + all * p.splits * D) + at, p.part + at * D};
 }
+
+// lambda of head h; a whole warp calls it.
+__device__ __forceinline__ float lambda_of(const DiffEnd& e, int half, int h) {
+  const float* v = e.lambda + h * e.lambda_h;
+  float a = 0.f, c = 0.f;
+  for (int i = threadIdx.x % 32; i < half; i += 32) {
+    a = fmaf(v[i], v[half + i], a);
+    c = fmaf(v[2 * half + i], v[3 * half + i], c);
+  }
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) {
+    a += __shfl_xor_sync(0xFFFFFFFFu, a, x);
+    c += __shfl_xor_sync(0xFFFFFFFFu, c, x);
+  }
+  return expf(a) - expf(c) + e.lambda_init;
+}
+// What a row's difference is multiplied by, from the sum of its squares: a row of zeros stays one, whatever eps is.
+template <int D>
+__device__ __forceinline__ float row_gain(const DiffEnd& e, float squares) {
+  if (!e.norm) return e.out_scale;
+  const float mean = fmaf(squares, 1.f / D, e.eps);
+  return mean == 0.f ? 0.f : e.out_scale * rsqrtf(mean);
+}
+__device__ __forceinline__ float norm_weight(const DiffEnd& e, int d) { return e.norm && e.weight ? __ldg(e.weight + d) : 1.f; }
 
 }  // namespace tok
 }  // namespace tt

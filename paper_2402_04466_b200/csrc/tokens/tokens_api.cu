@@ -196,7 +196,11 @@ tt_status tt_delta_rule(const tt_delta_rule_args* a, void* cuda_stream) {
   return e == cudaSuccess ? TT_OK : set_error(TT_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
 }
 
-static tt_status check_cross(const char* who, const tt_cross_attention_args* a) {
+}  // extern "C"
+
+// What tt_cross_attention and tt_differential_attention have in common: their arguments but for the end's have the same names.
+template <typename Args>
+static tt_status check_cross(const char* who, const Args* a) {
   if (!a || a->struct_size != sizeof(*a)) return set_error(TT_ERR_INVALID_ARG, "%s: struct_size", who);
   if ((a->precision != TT_FP32 && a->precision != TT_BF16) || !extent(a->batch, 1, 65535) || !extent(a->q_tokens, 0, MAX_EXTENT) ||
       !extent(a->kv_tokens, 0, MAX_EXTENT) || !extent(a->heads, 1, 4096) || !extent(a->kv_heads, 1, a->heads) || a->heads % a->kv_heads ||
@@ -205,20 +209,13 @@ static tt_status check_cross(const char* who, const tt_cross_attention_args* a) 
   if (bad_head_dim(who, a->head_dim)) return TT_ERR_UNSUPPORTED;
   return TT_OK;
 }
-static CrossPlan plan_of(const tt_cross_attention_args* a) {
-  return cross_plan(a->batch, a->q_tokens, a->kv_tokens, a->heads, a->heads / a->kv_heads, a->head_dim, a->precision == TT_BF16, a->mask != nullptr);
+template <typename Args>
+static CrossPlan plan_of(const Args* a, int maps) {
+  return cross_plan(a->batch, a->q_tokens, a->kv_tokens, a->heads, a->heads / a->kv_heads, a->head_dim, a->precision == TT_BF16, a->mask != nullptr, maps);
 }
-
-uint64_t tt_cross_attention_scratch_bytes(const tt_cross_attention_args* a) {
-  return check_cross("tt_cross_attention_scratch_bytes", a) == TT_OK ? plan_of(a).scratch : 0;
-}
-
-tt_status tt_cross_attention(const tt_cross_attention_args* a, void* cuda_stream) {
-  const char* who = "tt_cross_attention";
-  const tt_status st = check_cross(who, a);
-  if (st != TT_OK) return st;
-  const bool bf16 = a->precision == TT_BF16;
-  const int size = bf16 ? 2 : 4;
+template <typename Args>
+static tt_status check_cross_operands(const char* who, const Args* a, const CrossPlan& plan) {
+  const int size = a->precision == TT_BF16 ? 2 : 4;
   if (bad_view(who, "q", a->q, a->batch, a->q_tokens, a->heads, size) || bad_view(who, "k", a->k, a->batch, a->kv_tokens, a->kv_heads, size) ||
       bad_view(who, "v", a->v, a->batch, a->kv_tokens, a->kv_heads, size) || bad_view(who, "out", a->out, a->batch, a->q_tokens, a->heads, size) ||
       folded(who, "out", a->out, a->batch, a->q_tokens, a->heads, a->head_dim))
@@ -227,11 +224,12 @@ tt_status tt_cross_attention(const tt_cross_attention_args* a, void* cuda_stream
     return set_error(TT_ERR_INVALID_ARG, "%s: a length array or status_dev is misaligned", who);
   if (a->mask && (!extent(a->mask_batch_stride, 0, MAX_REACH / a->batch) || !extent(a->mask_query_stride, 0, MAX_REACH / (a->q_tokens + 1ll))))
     return set_error(TT_ERR_INVALID_ARG, "%s: a mask stride is negative or too large", who);
-  const CrossPlan plan = plan_of(a);
   if (plan.scratch && (!a->scratch || misaligned(a->scratch, 16) || a->scratch_bytes < plan.scratch))
     return set_error(TT_ERR_INVALID_ARG, "%s: scratch is null, misaligned or smaller than %llu bytes", who, (unsigned long long)plan.scratch);
-  if (a->q_tokens == 0) return TT_OK;
-  CrossParams p{};
+  return TT_OK;
+}
+template <typename Args>
+static void fill_cross(CrossParams& p, const Args* a, const CrossPlan& plan) {
   p.q = view(a->q, a->batch, a->q_tokens, a->heads); p.k = view(a->k, a->batch, a->kv_tokens, a->kv_heads);
   p.v = view(a->v, a->batch, a->kv_tokens, a->kv_heads); p.o = view(a->out, a->batch, a->q_tokens, a->heads);
   p.q_lengths = a->q_lengths; p.kv_lengths = a->kv_lengths; p.mask = a->mask; p.mask_b = a->mask_batch_stride; p.mask_q = a->mask_query_stride;
@@ -239,7 +237,48 @@ tt_status tt_cross_attention(const tt_cross_attention_args* a, void* cuda_stream
   p.batch = a->batch; p.q_tokens = a->q_tokens; p.kv_tokens = a->kv_tokens; p.heads = a->heads; p.group = a->heads / a->kv_heads;
   p.splits = plan.splits; p.split_keys = plan.split_keys; p.cluster = plan.cluster;
   p.scale_log2 = (float)((double)a->scale * 1.4426950408889634074);
-  const cudaError_t e = launch_cross(p, plan, bf16, a->head_dim, reinterpret_cast<cudaStream_t>(cuda_stream));
+}
+
+extern "C" {
+
+uint64_t tt_cross_attention_scratch_bytes(const tt_cross_attention_args* a) {
+  return check_cross("tt_cross_attention_scratch_bytes", a) == TT_OK ? plan_of(a, 1).scratch : 0;
+}
+
+tt_status tt_cross_attention(const tt_cross_attention_args* a, void* cuda_stream) {
+  const char* who = "tt_cross_attention";
+  tt_status st = check_cross(who, a);
+  if (st != TT_OK) return st;
+  const CrossPlan plan = plan_of(a, 1);
+  if ((st = check_cross_operands(who, a, plan)) != TT_OK) return st;
+  if (a->q_tokens == 0) return TT_OK;
+  CrossParams p{};
+  fill_cross(p, a, plan);
+  const cudaError_t e = launch_cross<1>(p, plan, a->precision == TT_BF16, a->head_dim, reinterpret_cast<cudaStream_t>(cuda_stream));
+  return e == cudaSuccess ? TT_OK : set_error(TT_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
+}
+
+uint64_t tt_differential_attention_scratch_bytes(const tt_differential_attention_args* a) {
+  return check_cross("tt_differential_attention_scratch_bytes", a) == TT_OK ? plan_of(a, 2).scratch : 0;
+}
+
+tt_status tt_differential_attention(const tt_differential_attention_args* a, void* cuda_stream) {
+  const char* who = "tt_differential_attention";
+  tt_status st = check_cross(who, a);
+  if (st != TT_OK) return st;
+  if (!std::isfinite(a->lambda_init) || !std::isfinite(a->out_scale) || (a->norm && !(a->eps >= 0.f && std::isfinite(a->eps))) ||
+      !extent(a->lambda_head_stride, 0, MAX_STRIDE))
+    return set_error(TT_ERR_INVALID_ARG, "%s: lambda_init, out_scale, eps or lambda_head_stride", who);
+  if (!a->lambda_vectors || misaligned(a->lambda_vectors, 4) || misaligned(a->norm_weight, 4))
+    return set_error(TT_ERR_INVALID_ARG, "%s: lambda_vectors is null, or it or norm_weight misaligned", who);
+  const CrossPlan plan = plan_of(a, 2);
+  if ((st = check_cross_operands(who, a, plan)) != TT_OK) return st;
+  if (a->q_tokens == 0) return TT_OK;
+  DiffParams p{};
+  fill_cross(p, a, plan);
+  p.end.lambda = a->lambda_vectors; p.end.lambda_h = a->lambda_head_stride; p.end.weight = a->norm_weight;
+  p.end.lambda_init = a->lambda_init; p.end.eps = a->eps; p.end.out_scale = a->out_scale; p.end.norm = a->norm != 0;
+  const cudaError_t e = launch_cross<2>(p, plan, a->precision == TT_BF16, a->head_dim, reinterpret_cast<cudaStream_t>(cuda_stream));
   return e == cudaSuccess ? TT_OK : set_error(TT_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
 }
 
