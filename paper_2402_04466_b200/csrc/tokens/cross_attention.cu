@@ -342,10 +342,10 @@ CrossPlan cross_plan(int batch, int q_tokens, int kv_tokens, int heads, int grou
   // one entry's 256 queries of 2 heads (0.15) 8.8 16.9, 10.5 21.6, 15.4 32.1; 700 (0.42) 18.2 17.5, 24.1 22.1, 40.9 34.8; 8 x 4 heads on 14400 keys, 65 queries
   // (2.3) 55.4 50.6, 81.5 52.6, 158 65.9.  So it is not taken too soon, and up to a third (heads of 64) or a half (128) too late where entries are several and
   // keys fewer than that.  (Masks are the other kernel's whatever the size; up to 64 queries leave three quarters of a tile of 256 rows empty.)
-  if (maps == 1 && bf16 && !mask && q_tokens > 64 && kv_tokens > 0 &&
+  if (bf16 && !mask && q_tokens > 64 && kv_tokens > 0 &&
       ((int64_t)q_tokens * group + 15) / 16 * batch * (heads / group) >= 500000 / kv_tokens + 1) {
     plan.kernel = CROSS_TC;
-    plan.scratch = cross_tc_scratch(batch, q_tokens, kv_tokens, heads, D);
+    plan.scratch = cross_tc_scratch(batch, q_tokens, kv_tokens, heads, D, maps);
     return plan;
   }
   const int64_t rows = (int64_t)q_tokens * group;
@@ -381,8 +381,7 @@ CrossPlan cross_plan(int batch, int q_tokens, int kv_tokens, int heads, int grou
 
 template <int MAPS>
 cudaError_t launch_cross(const ParamsOf<MAPS>& p, const CrossPlan& plan, bool bf16, int D, cudaStream_t s) {
-  if constexpr (MAPS == 1)
-    if (plan.kernel == CROSS_TC) return launch_cross_tc(p, D, s);
+  if (plan.kernel == CROSS_TC) return launch_cross_tc<MAPS>(p, D, s);
   return bf16 ? launch_typed<__nv_bfloat16, MAPS>(p, plan, D, s) : launch_typed<float, MAPS>(p, plan, D, s);
 }
 template cudaError_t launch_cross<1>(const CrossParams&, const CrossPlan&, bool, int, cudaStream_t);

@@ -26,7 +26,7 @@ constexpr int BM = 128;                      // queries of a tile
 constexpr int MAX_ENTRIES = 256;             // of the batch in a launch: their work is added up in shared memory
 constexpr int LEAST = 512;                   // keys to a block, at least: fewer cost more in the join than they save
 
-struct CrossTcParams {
+struct CrossTcBase {
   TensorMap128 map_q, map_k, map_v;      // [D][token][head][batch], boxes of 128 queries and of BN keys
   View o;
   const int32_t* q_lengths;
@@ -37,11 +37,17 @@ struct CrossTcParams {
   int32_t q_h, q_b, k_h, k_b, v_h, v_b;  // 0 where the axis is shared, else 1
   float scale_log2;
 };
+template <int MAPS>
+struct CrossTcParams : CrossTcBase {};
+template <>
+struct CrossTcParams<2> : CrossTcBase {
+  DiffEnd end;
+};
 
-template <int D>
+template <int D, int MAPS>
 struct Cfg {
   // Two tiles of queries to a block, one block to a multiprocessor; each tile has columns of tensor memory of its own for scores (BN),
-  // weights (BN / 2) and sums (D).
+  // weights (BN / 2) and sums (D).  Of differential attention (MAPS = 2) the two are the two maps of one tile of queries.
   static constexpr int TILES = 2, BN = D == 128 ? 64 : 128;
   // With heads of up to 64 the special-function units are what there is least of: the two tiles' warps of a quarter, which share one, take
   // turns at their exponentials, and one does the rest of its work meanwhile (276 us where both at once take 306; with heads of 128, whose
@@ -49,7 +55,8 @@ struct Cfg {
   static constexpr bool TURNS = D != 128;
   static constexpr int HALVES = BN / 64;                            // weights are handed over 64 keys at a time
   static constexpr int PLACES = D == 128 ? 2 : 1;                   // of a tile's weights: those of one tile of keys are made while the last ones' product runs
-  static constexpr int ROWS = TILES * BM;
+  static constexpr int QTILES = TILES / MAPS, ROWS = QTILES * BM;   // of queries
+  static constexpr int KSTEPS = D / 16 / MAPS;                      // products of 16 elements to a map's scores
   static constexpr int ROW = D == 32 ? 64 : 128;                    // bytes of a row in a slab
   static constexpr int SLABS = D == 128 ? 2 : 1;
   static constexpr int Q_SLAB = BM * ROW, KV_SLAB = BN * ROW;
@@ -58,8 +65,9 @@ struct Cfg {
   static constexpr int STAGES = 4;
   static constexpr int THREADS = TILES * (128 + 64);
   static constexpr uint32_t P_COL = TILES * BN, O_COL = P_COL + TILES * PLACES * BN / 2, TMEM = 512;
-  static constexpr int SMEM = TILES * Q_BYTES + 2 * STAGES * KV_BYTES + 512 + 1024;
-  static constexpr int64_t PART = (int64_t)ROWS * (D + 2);          // floats of a partial result
+  static constexpr int SMEM = QTILES * Q_BYTES + 2 * STAGES * KV_BYTES + 512 + 1024;
+  static constexpr int PROWS = TILES * BM;                          // rows of a partial result, of either map
+  static constexpr int64_t PART = (int64_t)PROWS * (D + 2);         // its floats
   static_assert(O_COL + TILES * D <= TMEM && SMEM + 6 * 1024 <= 227 * 1024, "tensor and shared memory");
 };
 
@@ -68,8 +76,8 @@ struct Work {
   int64_t before[MAX_ENTRIES + 1];       // iterations before an entry's
   int32_t rows[MAX_ENTRIES], keys[MAX_ENTRIES];
 };
-template <int D>
-__device__ __forceinline__ void add_up(Work& w, const CrossTcParams& p) {
+template <typename C>
+__device__ __forceinline__ void add_up(Work& w, const CrossTcBase& p) {
   for (int i = threadIdx.x; i < p.batch; i += blockDim.x) {
     w.rows[i] = clamp_length(p.q_lengths, p.b0 + i, p.q_tokens);
     w.keys[i] = clamp_length(p.kv_lengths, p.b0 + i, p.kv_tokens);
@@ -79,7 +87,7 @@ __device__ __forceinline__ void add_up(Work& w, const CrossTcParams& p) {
     int64_t sum = 0;
     for (int i0 = 0; i0 < p.batch; i0 += 32) {
       const int i = i0 + threadIdx.x;
-      int64_t mine = i < p.batch ? (int64_t)((w.rows[i] + Cfg<D>::ROWS - 1) / Cfg<D>::ROWS) * p.heads * max(1, (w.keys[i] + Cfg<D>::BN - 1) / Cfg<D>::BN) : 0;
+      int64_t mine = i < p.batch ? (int64_t)((w.rows[i] + C::ROWS - 1) / C::ROWS) * p.heads * max(1, (w.keys[i] + C::BN - 1) / C::BN) : 0;
       for (int o = 1; o < 32; o <<= 1) {
         const int64_t other = __shfl_up_sync(0xffffffffu, mine, o);
         if ((int)threadIdx.x >= o) mine += other;
@@ -91,10 +99,10 @@ __device__ __forceinline__ void add_up(Work& w, const CrossTcParams& p) {
   }
   __syncthreads();
 }
-template <int D>
-__device__ __forceinline__ int64_t share_of(const Work& w, const CrossTcParams& p) {
+template <typename C>
+__device__ __forceinline__ int64_t share_of(const Work& w, const CrossTcBase& p) {
   const int64_t each = (w.before[p.batch] + gridDim.x - 1) / gridDim.x;
-  return each < LEAST / Cfg<D>::BN ? LEAST / Cfg<D>::BN : each;
+  return each < LEAST / C::BN ? LEAST / C::BN : each;
 }
 
 // A block's way through its work: the run it is at, and the step to the next.
@@ -102,41 +110,43 @@ struct Cursor {
   int64_t at, end;
   int b, h, row0, j0, j1, n;             // entry, head, first row; of the tile's n tiles of keys those from j0 to j1
   __device__ __forceinline__ bool done() const { return at >= end; }
-  template <int D>
-  __device__ __forceinline__ void find(const Work& w, const CrossTcParams& p) {
+  template <typename C>
+  __device__ __forceinline__ void find(const Work& w, const CrossTcBase& p) {
     if (done()) return;
     while (w.before[b + 1] <= at) ++b;
-    n = max(1, (w.keys[b] + Cfg<D>::BN - 1) / Cfg<D>::BN);
-    const int tiles = (w.rows[b] + Cfg<D>::ROWS - 1) / Cfg<D>::ROWS;
+    n = max(1, (w.keys[b] + C::BN - 1) / C::BN);
+    const int tiles = (w.rows[b] + C::ROWS - 1) / C::ROWS;
     const int64_t rel = at - w.before[b], t = rel / n;
     h = (int)(t / tiles);
-    row0 = (int)(t - (int64_t)h * tiles) * Cfg<D>::ROWS;
+    row0 = (int)(t - (int64_t)h * tiles) * C::ROWS;
     j0 = (int)(rel - t * n);
     j1 = (int)min((int64_t)n, j0 + (end - at));
   }
-  template <int D>
-  __device__ __forceinline__ void start(const Work& w, const CrossTcParams& p) {
-    const int64_t each = share_of<D>(w, p);
+  template <typename C>
+  __device__ __forceinline__ void start(const Work& w, const CrossTcBase& p) {
+    const int64_t each = share_of<C>(w, p);
     at = min((int64_t)blockIdx.x * each, w.before[p.batch]);
     end = min(at + each, w.before[p.batch]);
     b = 0;
-    find<D>(w, p);
+    find<C>(w, p);
   }
-  template <int D>
-  __device__ __forceinline__ void next(const Work& w, const CrossTcParams& p) {
+  template <typename C>
+  __device__ __forceinline__ void next(const Work& w, const CrossTcBase& p) {
     at += j1 - j0;
-    find<D>(w, p);
+    find<C>(w, p);
   }
 };
 
-template <int D>
-__global__ void __launch_bounds__(Cfg<D>::THREADS, 1) cross_tc_kernel(const __grid_constant__ CrossTcParams p) {
-  using C = Cfg<D>;
+template <int D, int MAPS>
+__global__ void __launch_bounds__(Cfg<D, MAPS>::THREADS, 1) cross_tc_kernel(const __grid_constant__ CrossTcParams<MAPS> p) {
+  using C = Cfg<D, MAPS>;
   constexpr int STAGES = C::STAGES, TILES = C::TILES;
   extern __shared__ uint8_t smem_raw[];
   __shared__ Work work;
+  __shared__ __align__(8) uint64_t met[4];     // the two maps' warps of a quarter: twice at the end of a run
+  __shared__ float s_end[2][2][BM];            // [1 or lambda, then that over a row's total; squares][map][query]
   uint8_t* s_q = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  uint8_t* s_k = s_q + TILES * C::Q_BYTES;
+  uint8_t* s_k = s_q + C::QTILES * C::Q_BYTES;
   uint8_t* s_v = s_k + STAGES * C::KV_BYTES;
   uint64_t* qfull = reinterpret_cast<uint64_t*>(s_v + STAGES * C::KV_BYTES);
   uint64_t* qempty = qfull + 1;                // the empty ones are signalled by every tile's warp
@@ -170,13 +180,15 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) cross_tc_kernel(const __gr
       for (int x = 0; x < C::PLACES; ++x) mbar_init(smem_u32(pdone + C::PLACES * t + x), 1);
     }
     for (int x = 0; x < 8; ++x) mbar_init(smem_u32(turns + x), 1);
+    if (MAPS == 2)
+      for (int x = 0; x < 4; ++x) mbar_init(smem_u32(met + x), 2);
     *abort_flag = 0;
     *s_status = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  add_up<D>(work, p);
+  add_up<C>(work, p);
   Cursor cur;
-  cur.start<D>(work, p);
+  cur.start<C>(work, p);
   if (cur.done()) return;                      // the whole block
   if (warp == TILES * 4) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(C::TMEM) : "memory");
@@ -231,7 +243,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) cross_tc_kernel(const __gr
       }
       ++aj;
       if (--left == 0) {                       // on to the next run
-        ahead.next<D>(work, p);
+        ahead.next<C>(work, p);
         if (__shfl_sync(0xffffffffu, (int)ahead.done(), 0) == 0) {
           ab = __shfl_sync(0xffffffffu, p.b0 + ahead.b, 0);
           ah = __shfl_sync(0xffffffffu, ahead.h / p.group, 0);
@@ -243,11 +255,11 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) cross_tc_kernel(const __gr
     uint32_t stage = 0, phase = 0, runs = 0, it = 0;
     if (keys) {
       constexpr uint32_t QK = make_idesc(BM, C::BN);
-      const uint64_t q0 = make_smem_desc(smem_u32(s_q + t * C::Q_BYTES), 8 * C::ROW, C::LAYOUT), k0 = make_smem_desc(smem_u32(s_k), 8 * C::ROW, C::LAYOUT);
+      const uint64_t q0 = make_smem_desc(smem_u32(s_q + (MAPS == 1 ? t * C::Q_BYTES : 0)), 8 * C::ROW, C::LAYOUT), k0 = make_smem_desc(smem_u32(s_k), 8 * C::ROW, C::LAYOUT);
       auto load_queries = [&]() {
         if (issuer && loads) {
-          mbar_arrive_expect_tx(smem_u32(qfull), TILES * C::Q_BYTES);
-          for (int i = 0; i < TILES; ++i)
+          mbar_arrive_expect_tx(smem_u32(qfull), C::QTILES * C::Q_BYTES);
+          for (int i = 0; i < C::QTILES; ++i)
             for (int s = 0; s < C::SLABS; ++s)
               tma_load_4d(smem_u32(s_q + i * C::Q_BYTES + s * C::Q_SLAB), &p.map_q, smem_u32(qfull), s * 64, cur.row0 + i * BM, cur.h * p.q_h, (p.b0 + cur.b) * p.q_b);
         }
@@ -266,13 +278,15 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) cross_tc_kernel(const __gr
           if (issuer) {
             const uint64_t kd = k0 + (uint64_t)stage * (C::KV_BYTES >> 4);
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k)
-              umma_bf16(scores, q0 + (uint64_t)((k / 4) * (C::Q_SLAB >> 4) + (k % 4) * 2), kd + (uint64_t)((k / 4) * (C::KV_SLAB >> 4) + (k % 4) * 2), QK, k > 0);
+            for (int x = 0; x < C::KSTEPS; ++x) {
+              const int k = MAPS == 1 ? x : t * C::KSTEPS + x;      // a map has its half of the elements
+              umma_bf16(scores, q0 + (uint64_t)((k / 4) * (C::Q_SLAB >> 4) + (k % 4) * 2), kd + (uint64_t)((k / 4) * (C::KV_SLAB >> 4) + (k % 4) * 2), QK, x > 0);
+            }
             umma_commit(smem_u32(sfull + t));
             umma_commit(smem_u32(kempty + stage));
             if (j + 1 == n) umma_commit(smem_u32(qempty));      // the run's queries have been read behind this product
           }
-          if (j + 1 == n) cur.next<D>(work, p);
+          if (j + 1 == n) cur.next<C>(work, p);
           // the tile's place is free when every tile of queries has read it (a parity of another tile's sfull would not do: that tile may
           // be two iterations ahead)
           if (loads) {
@@ -297,7 +311,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) cross_tc_kernel(const __gr
         const int n = __shfl_sync(0xffffffffu, cur.j1 - cur.j0, 0);
         // keys of the run's last tile: fewer than BN where it is the last of all
         const int rem = __shfl_sync(0xffffffffu, work.keys[cur.b] - (cur.j1 - 1) * C::BN, 0);
-        cur.next<D>(work, p);
+        cur.next<C>(work, p);
         for (int j = 0; j < n; ++j, ++it) {
           arrived(full + stage, phase, 0x38 + (int)stage);
           if (j + 1 == n && rem < C::BN) {
@@ -335,7 +349,18 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) cross_tc_kernel(const __gr
     }
   } else {
     // ------------------------------------------------------------------------------ weights
-    const int t = warp >> 2, quarter = warp & 3, r = t * BM + quarter * 32 + lane;      // row of the block's tile
+    const int t = warp >> 2, quarter = warp & 3, r = t * BM + quarter * 32 + lane;      // row of the block's tiles
+    const int query = MAPS == 1 ? r : quarter * 32 + lane;
+    uint32_t meetings = 0;
+    // both maps' warps of a quarter have come here: what each wrote before, the other reads behind it
+    auto meet = [&](int code) {
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(met + quarter));
+      const bool go = wait_all(met + quarter, meetings++, code);
+      tc_fence_after();
+      return go;
+    };
     const uint32_t s_addr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(t * C::BN);
     const uint32_t p_addr = tmem + ((uint32_t)(quarter * 32) << 16) + C::P_COL + (uint32_t)(t * C::PLACES * (C::BN / 2));
     const uint32_t o_addr = tmem + ((uint32_t)(quarter * 32) << 16) + C::O_COL + (uint32_t)(t * D);
@@ -344,6 +369,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) cross_tc_kernel(const __gr
     uint32_t it = 0;
     while (ok && !cur.done()) {
       const int count = cur.j1 - cur.j0, last_keys = work.keys[cur.b] - (cur.j1 - 1) * C::BN;      // of the run's last tile: all of its places or fewer
+      if constexpr (MAPS == 2) s_end[0][t][query] = t == 1 ? lambda_of(p.end, D / 2, cur.h) : 1.f;      // kept there until the run's end
       float m = -INFINITY;
       unsigned long long l[4] = {pack2(0.f, 0.f), pack2(0.f, 0.f), pack2(0.f, 0.f), pack2(0.f, 0.f)};      // four chains
       for (int j = 0; j < count; ++j, ++it) {
@@ -431,8 +457,44 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) cross_tc_kernel(const __gr
       float a0, a1;
       unpack2(add2_of(add2_of(l[0], l[1]), add2_of(l[2], l[3])), a0, a1);
       const float total = a0 + a1;
-      const bool here = cur.row0 + r < work.rows[cur.b];
-      if (cur.j0 == 0 && cur.j1 == cur.n) {
+      const bool here = cur.row0 + query < work.rows[cur.b];
+      if (MAPS == 2 && cur.j0 == 0 && cur.j1 == cur.n) {
+        // Each map's warp takes half of the columns of both maps' sums, which are in the same lanes of tensor memory.  Behind the second
+        // meeting the sums have been read, and the next run's products may overwrite them.
+        if constexpr (MAPS == 2) {
+          constexpr int CHUNKS = D / 32;         // of 16 columns, to a half
+          s_end[0][t][query] = total == 0.f ? 0.f : s_end[0][t][query] / total;
+          if (!meet(0x70 + t)) break;
+          const float first = s_end[0][0][query], second = s_end[0][1][query];
+          const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16) + C::O_COL + (uint32_t)(t * (D / 2));
+          float y[D / 2], squares = 0.f;
+#pragma unroll
+          for (int i = 0; i < CHUNKS; ++i) {
+            uint32_t a[16], e[16];
+            __syncwarp();
+            tmem_ld16_async(at + 16 * i, a);
+            tmem_ld16_async(at + D + 16 * i, e);
+            tmem_wait_ld();
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+              const float f = fmaf(__uint_as_float(a[x]), first, -(__uint_as_float(e[x]) * second));
+              y[16 * i + x] = f;
+              squares = fmaf(f, f, squares);
+            }
+          }
+          s_end[1][t][query] = squares;
+          if (!meet(0x72 + t)) break;
+          const float gain = row_gain<D>(p.end, s_end[1][0][query] + s_end[1][1][query]);
+          if (here) {
+            __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.o.p) + (p.b0 + cur.b) * p.o.b + (int64_t)(cur.row0 + query) * p.o.t + cur.h * p.o.h + t * (D / 2);
+#pragma unroll
+            for (int x = 0; x < D / 2; x += 8) {
+              auto two = [&](int i) { return pack_bf16(y[i] * gain * norm_weight(p.end, t * (D / 2) + i), y[i + 1] * gain * norm_weight(p.end, t * (D / 2) + i + 1)); };
+              *reinterpret_cast<uint4*>(dst + x) = make_uint4(two(x), two(x + 2), two(x + 4), two(x + 6));
+            }
+          }
+        }
+      } else if (cur.j0 == 0 && cur.j1 == cur.n) {
         const float inv = total == 0.f ? 0.f : 1.f / total;      // nothing seen: zeros
         __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.o.p) + (p.b0 + cur.b) * p.o.b + (int64_t)(cur.row0 + r) * p.o.t + cur.h * p.o.h;
 #pragma unroll
@@ -451,7 +513,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) cross_tc_kernel(const __gr
       } else {
         float* place = p.part + ((int64_t)blockIdx.x * 2 + (cur.j0 == 0)) * C::PART;
         reinterpret_cast<float2*>(place)[r] = make_float2(m * c, total);
-        float* dst = place + 2 * C::ROWS + r * D;
+        float* dst = place + 2 * C::PROWS + r * D;
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) {
           uint32_t o[32];
@@ -464,7 +526,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) cross_tc_kernel(const __gr
           }
         }
       }
-      cur.next<D>(work, p);
+      cur.next<C>(work, p);
     }
   }
 
@@ -486,29 +548,29 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, 1) cross_tc_kernel(const __gr
 
 // One block per block of the kernel above: if its run begins inside a tile and is the first to do so, it joins the tile's parts, from the
 // run that the tile begins in (second place) to the one that it ends in (first places).  out = sum 2^(m_s - m) o_s / sum 2^(m_s - m) l_s.
-template <int D>
-__global__ void __launch_bounds__(256) cross_tc_join_kernel(const __grid_constant__ CrossTcParams p) {
-  using C = Cfg<D>;
+template <int D, int MAPS>
+__global__ void __launch_bounds__(256) cross_tc_join_kernel(const __grid_constant__ CrossTcParams<MAPS> p) {
+  using C = Cfg<D, MAPS>;
   __shared__ Work work;
-  add_up<D>(work, p);
+  add_up<C>(work, p);
   Cursor cur;
-  cur.start<D>(work, p);
+  cur.start<C>(work, p);
   pdl_wait();                                  // also of blocks that have nothing to do: the grid ends behind the kernel above
   if (cur.done() || cur.j0 == 0) return;
-  const int64_t each = share_of<D>(work, p), from = cur.at - cur.j0, first = from / each;
+  const int64_t each = share_of<C>(work, p), from = cur.at - cur.j0, first = from / each;
   if (first + 1 != blockIdx.x) return;
   const int64_t last = (from + cur.n - 1) / each;
   const float* before = p.part + (first * 2 + 1) * C::PART;
   constexpr int LANES = D / 4;
-  for (int r = threadIdx.x / LANES + (int)blockIdx.y * (256 / LANES); r < C::ROWS && cur.row0 + r < work.rows[cur.b]; r += 256 / LANES * (int)gridDim.y) {
-    const int d = threadIdx.x % LANES * 4;
+  const int d = threadIdx.x % LANES * 4;
+  auto joined = [&](int r) {
     float2 st = reinterpret_cast<const float2*>(before)[r];
     float m = st.x, l = st.y;
-    float4 o = *reinterpret_cast<const float4*>(before + 2 * C::ROWS + r * D + d);
+    float4 o = *reinterpret_cast<const float4*>(before + 2 * C::PROWS + r * D + d);
     for (int64_t i = first + 1; i <= last; ++i) {
       const float* place = p.part + i * 2 * C::PART;
       st = reinterpret_cast<const float2*>(place)[r];
-      const float4 x = *reinterpret_cast<const float4*>(place + 2 * C::ROWS + r * D + d);
+      const float4 x = *reinterpret_cast<const float4*>(place + 2 * C::PROWS + r * D + d);
       const float now = fmaxf(m, st.x), base = now == -INFINITY ? 0.f : now;
       const float f = exp2_fast(m - base), g = exp2_fast(st.x - base);
       m = now;
@@ -516,34 +578,56 @@ __global__ void __launch_bounds__(256) cross_tc_join_kernel(const __grid_constan
       o = make_float4(o.x * f + x.x * g, o.y * f + x.y * g, o.z * f + x.z * g, o.w * f + x.w * g);
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
+    return make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+  };
+  auto store = [&](int r, float4 o) {
     __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(p.o.p) + (p.b0 + cur.b) * p.o.b + (int64_t)(cur.row0 + r) * p.o.t + cur.h * p.o.h + d;
-    *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+    *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(o.x, o.y), pack_bf16(o.z, o.w));
+  };
+  const int r0 = threadIdx.x / LANES + (int)blockIdx.y * (256 / LANES), step = 256 / LANES * (int)gridDim.y;
+  if constexpr (MAPS == 1) {
+    for (int r = r0; r < C::ROWS && cur.row0 + r < work.rows[cur.b]; r += step) store(r, joined(r));
+  } else {
+    const float lambda = lambda_of(p.end, D / 2, cur.h);
+    const float w[4] = {norm_weight(p.end, d), norm_weight(p.end, d + 1), norm_weight(p.end, d + 2), norm_weight(p.end, d + 3)};
+    for (int r = r0; r < C::ROWS; r += step) {   // as often for all lanes of a warp
+      const bool here = cur.row0 + r < work.rows[cur.b];
+      float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (here) {
+        const float4 a = joined(r), e = joined(BM + r);
+        y = make_float4(fmaf(-lambda, e.x, a.x), fmaf(-lambda, e.y, a.y), fmaf(-lambda, e.z, a.z), fmaf(-lambda, e.w, a.w));
+      }
+      float squares = fmaf(y.x, y.x, fmaf(y.y, y.y, fmaf(y.z, y.z, y.w * y.w)));
+#pragma unroll
+      for (int x = LANES / 2; x > 0; x >>= 1) squares += __shfl_xor_sync(0xffffffffu, squares, x);
+      const float gain = row_gain<D>(p.end, squares);
+      if (here) store(r, make_float4(y.x * gain * w[0], y.y * gain * w[1], y.z * gain * w[2], y.w * gain * w[3]));
+    }
   }
 }
 
 // Blocks of a launch over `batch` entries: one to a multiprocessor, fewer where a block would get less than LEAST keys.
-template <int D>
+template <typename C>
 int64_t grid_of(int batch, int q_tokens, int kv_tokens, int heads) {
-  using C = Cfg<D>;
   const int64_t most = (int64_t)PLAN_SMS, tiles = (int64_t)((q_tokens + C::ROWS - 1) / C::ROWS) * heads * batch, n = (kv_tokens + C::BN - 1) / C::BN;
   if (tiles >= most * (LEAST / C::BN)) return most;
   const int64_t blocks = (tiles * n + LEAST / C::BN - 1) / (LEAST / C::BN);
   return blocks < most ? blocks : most;
 }
 
-template <int D>
-cudaError_t launch(CrossTcParams& p, int batch, cudaStream_t s) {      // (the join is launched ahead of the end of the kernel: two entries' 256 queries 24 us, behind it 26.5)
-  using C = Cfg<D>;
+template <int D, int MAPS>
+cudaError_t launch(CrossTcParams<MAPS>& p, int batch, cudaStream_t s) {      // (the join is launched ahead of the end of the kernel: two entries' 256 queries 24 us, behind it 26.5)
+  using C = Cfg<D, MAPS>;
   static OncePerContext once;
-  cudaError_t e = once([] { return cudaFuncSetAttribute(cross_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM); });
+  cudaError_t e = once([] { return cudaFuncSetAttribute(cross_tc_kernel<D, MAPS>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM); });
   if (e != cudaSuccess) return e;
   for (p.b0 = 0; p.b0 < batch; p.b0 += MAX_ENTRIES) {
     p.batch = batch - p.b0 < MAX_ENTRIES ? batch - p.b0 : MAX_ENTRIES;
-    const unsigned blocks = (unsigned)grid_of<D>(p.batch, p.q_tokens, p.kv_tokens, p.heads);
-    cross_tc_kernel<D><<<blocks, C::THREADS, C::SMEM, s>>>(p);
+    const unsigned blocks = (unsigned)grid_of<C>(p.batch, p.q_tokens, p.kv_tokens, p.heads);
+    cross_tc_kernel<D, MAPS><<<blocks, C::THREADS, C::SMEM, s>>>(p);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     // eight blocks to a tile's rows: two entries' 256 queries of 4 heads of 64 on 4800 keys 24 us, with four 28 (eight maps 276 and 274)
-    if ((e = launch_kernel(cross_tc_join_kernel<D>, dim3(blocks, 8), 256, 0, s, p, true)) != cudaSuccess) return e;
+    if ((e = launch_kernel(cross_tc_join_kernel<D, MAPS>, dim3(blocks, 8), 256, 0, s, p, true)) != cudaSuccess) return e;
   }
   return cudaSuccess;
 }
@@ -568,17 +652,23 @@ bool token_map(TensorMap128* map, const View& v, int D, int tokens, int heads, i
             D == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-uint64_t cross_tc_scratch(int batch, int q_tokens, int kv_tokens, int heads, int D) {
+template <int MAPS>
+static uint64_t scratch_of(int entries, int q_tokens, int kv_tokens, int heads, int D) {
+  auto floats = [&](auto c) {
+    using C = decltype(c);
+    return grid_of<C>(entries, q_tokens, kv_tokens, heads) * C::PART;
+  };
+  return (uint64_t)(D == 32 ? floats(Cfg<32, MAPS>{}) : D == 64 ? floats(Cfg<64, MAPS>{}) : floats(Cfg<128, MAPS>{})) * 2u * 4u;
+}
+uint64_t cross_tc_scratch(int batch, int q_tokens, int kv_tokens, int heads, int D, int maps) {
   const int entries = batch < MAX_ENTRIES ? batch : MAX_ENTRIES;
-  const int64_t floats = D == 32   ? grid_of<32>(entries, q_tokens, kv_tokens, heads) * Cfg<32>::PART
-                         : D == 64 ? grid_of<64>(entries, q_tokens, kv_tokens, heads) * Cfg<64>::PART
-                                   : grid_of<128>(entries, q_tokens, kv_tokens, heads) * Cfg<128>::PART;
-  return (uint64_t)floats * 2u * 4u;
+  return maps == 1 ? scratch_of<1>(entries, q_tokens, kv_tokens, heads, D) : scratch_of<2>(entries, q_tokens, kv_tokens, heads, D);
 }
 
-cudaError_t launch_cross_tc(const CrossParams& c, int D, cudaStream_t s) {
-  CrossTcParams p{};
-  const int kv_heads = c.heads / c.group, keys = D == 128 ? Cfg<128>::BN : Cfg<64>::BN;
+template <int MAPS>
+cudaError_t launch_cross_tc(const ParamsOf<MAPS>& c, int D, cudaStream_t s) {
+  CrossTcParams<MAPS> p{};
+  const int kv_heads = c.heads / c.group, keys = D == 128 ? Cfg<128, MAPS>::BN : Cfg<64, MAPS>::BN;
   if (!token_map(&p.map_q, c.q, D, c.q_tokens, c.heads, c.batch) || !token_map(&p.map_k, c.k, D, c.kv_tokens, kv_heads, c.batch, keys) ||
       !token_map(&p.map_v, c.v, D, c.kv_tokens, kv_heads, c.batch, keys))
     return cudaErrorInvalidValue;
@@ -586,8 +676,11 @@ cudaError_t launch_cross_tc(const CrossParams& c, int D, cudaStream_t s) {
   p.q_tokens = c.q_tokens; p.kv_tokens = c.kv_tokens; p.heads = c.heads; p.group = c.group;
   p.q_h = c.q.h != 0; p.q_b = c.q.b != 0; p.k_h = c.k.h != 0; p.k_b = c.k.b != 0; p.v_h = c.v.h != 0; p.v_b = c.v.b != 0;
   p.scale_log2 = c.scale_log2;
-  return D == 32 ? launch<32>(p, c.batch, s) : D == 64 ? launch<64>(p, c.batch, s) : launch<128>(p, c.batch, s);
+  if constexpr (MAPS == 2) p.end = c.end;
+  return D == 32 ? launch<32, MAPS>(p, c.batch, s) : D == 64 ? launch<64, MAPS>(p, c.batch, s) : launch<128, MAPS>(p, c.batch, s);
 }
+template cudaError_t launch_cross_tc<1>(const CrossParams&, int, cudaStream_t);
+template cudaError_t launch_cross_tc<2>(const DiffParams&, int, cudaStream_t);
 
 }  // namespace tok
 }  // namespace tt

@@ -106,8 +106,9 @@ cudaError_t launch_cross(const ParamsOf<MAPS>& p, const CrossPlan& plan, bool bf
 
 template <int MAPS>
 cudaError_t launch_cross_few(const ParamsOf<MAPS>& p, int D, int warps, cudaStream_t s);   // splits > 1: the join is the caller's
-cudaError_t launch_cross_tc(const CrossParams& p, int D, cudaStream_t s);         // kv_tokens > 0
-uint64_t cross_tc_scratch(int batch, int q_tokens, int kv_tokens, int heads, int D);
+template <int MAPS>
+cudaError_t launch_cross_tc(const ParamsOf<MAPS>& p, int D, cudaStream_t s);      // kv_tokens > 0
+uint64_t cross_tc_scratch(int batch, int q_tokens, int kv_tokens, int heads, int D, int maps);
 
 // Tensor map of a bf16 view, boxes of `box` tokens of one head.  An axis of stride 0 has one place.
 bool token_map(TensorMap128* map, const View& v, int D, int tokens, int heads, int batch, int box = 128);
