@@ -64,7 +64,8 @@ struct alignas(32) DeltaParams {
   int32_t num_slots;
   float scale;
 };
-cudaError_t launch_delta_step(const DeltaParams& p, bool bf16, int D, cudaStream_t s);
+cudaError_t launch_delta_step(const DeltaParams& p, bool bf16, int D, cudaStream_t s);      // token by token
+cudaError_t launch_delta_chunk(const DeltaParams& p, bool bf16, int D, cudaStream_t s);     // a window of tokens at a time
 
 struct alignas(32) CrossParams {
   View q, k, v, o;

@@ -192,7 +192,8 @@ tt_status tt_delta_rule(const tt_delta_rule_args* a, void* cuda_stream) {
   p.log_decay = a->log_decay; p.beta = a->beta; p.state = a->state; p.state_out = a->state_out; p.slots = a->slots; p.lengths = a->lengths;
   p.batch = a->batch; p.tokens = a->tokens; p.heads = a->heads; p.group = a->heads / a->qk_heads; p.num_slots = a->num_slots;
   p.scale = a->scale;
-  const cudaError_t e = launch_delta_step(p, bf16, a->head_dim, reinterpret_cast<cudaStream_t>(cuda_stream));
+  const cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
+  const cudaError_t e = a->tokens > 1 ? launch_delta_chunk(p, bf16, a->head_dim, s) : launch_delta_step(p, bf16, a->head_dim, s);
   return e == cudaSuccess ? TT_OK : set_error(TT_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
 }
 
