@@ -3,17 +3,18 @@
 // Within a window let G_i be the sum of log_decay up to and including token i.  The corrections u_i then solve a triangular system,
 //   u_i + sum_{j<i} beta_i e^(G_i - G_j) (k_i . k_j) u_j = beta_i (v_i - e^G_i S^T k_i)   or   (1 + A) U = R,
 //   out_i = scale (e^G_i S^T q_i + sum_{j<=i} e^(G_i - G_j) (q_i . k_j) u_j),   S' = e^G_C S + sum_j e^(G_C - G_j) k_j u_j^T.
-// T = (1 + A)^-1 and the weights P of U in out depend on no state: half of the block's warps work them out for the next window while the other half takes this one's
-// state along, which is the chain that bounds a sequence:  S -> R -> U = T R -> S'.
+// What bounds a sequence is the chain S -> R -> U = (1 + A)^-1 R -> S'.  A block has four groups of four warps, each with one kind of work on a window of its own, which
+// meet once a window: two windows ahead, A; one ahead, its inverse; the chain; and out, whose last product is taken a window behind.
 //
 // A block owns NS runs of 16 value columns of one head's state (the columns are independent of each other).  Everything on the chain is kept transposed, columns of
-// values along M: the accumulators of one m16n8k16 product are then the other operand's registers of the next, X^T = S^T K^T, U^T = R^T T^T,
-// S'^T = U'^T K, and what warps exchange lies in shared memory as those registers, 16 bytes to a lane.  (A tcgen05 product of 16 columns takes 40 cycles however few
-// its columns are, and its way through tensor memory twice that: the chain would be longer, not shorter.)
+// values along M: the accumulators of one m16n8k16 product are then the other operand's registers of the next.  Each warp of the chain has a quarter of the keys' elements of the
+// state in registers, as sums and as operands: X^T = S^T K^T comes in four parts, which the warps add up where they read them, then U^T = R^T T^T and
+// S'^T = U'^T K.  R and U go from warp to warp as operands' registers, 16 bytes to a lane.  (A tcgen05 product of 16 columns takes 40 cycles however few its
+// columns are, and its way through tensor memory twice that: the chain would be longer, not shorter.)
 //
 // The state is fp32, and so is everything between two products: an operand that is not bf16 to begin with is cut into three bf16 terms (8 + 8 + 8 bits), of whose
-// products those of 2^-16 and more count.  Only what out alone reads is rounded further: in bf16 calls S, U and P count with 16 bits.  (P rounded to bf16 once
-// is not enough: of keys that repeat the corrections are many times larger than what is left of their sum.)
+// products those of 2^-16 and more count.  Only what out alone reads is rounded further: in bf16 calls S, U and P (the weights of U in out) count with 16 bits.  (P rounded
+// to bf16 once is not enough: of keys that repeat the corrections are many times larger than what is left of their sum.)
 #include "linear_common.cuh"
 
 #include "token_ptx.cuh"
@@ -22,31 +23,33 @@ namespace tt {
 namespace tok {
 namespace {
 
-constexpr int C = 32;                        // tokens of a window
-constexpr int GROUP = 128;                   // threads of the chain, and of the preparation
-constexpr int THREADS = 2 * GROUP;
+constexpr int GROUP = 128;                   // threads of a group: the chain, out, the inverse, A
+constexpr int THREADS = 4 * GROUP;
+enum { CHAIN = 0, OUT = 1, INVERSE = 2, SYSTEM = 3 };
 
-template <typename T, int D, int NS>
+template <typename T_, int D_, int C_, int NS_>
 struct Shape {
+  using T = T_;
+  static constexpr int D = D_, C = C_, NS = NS_;
   static constexpr int TERMS = sizeof(T) == 2 ? 1 : 3;       // of queries and keys
   static constexpr int SEEN = sizeof(T) == 2 ? 2 : 3;        // of S, U and P in out
   static constexpr int KS = D / 16;                          // products along a key
-  static constexpr int NT = D / 8 / 4;                       // tiles of 8 keys' elements of the state to a warp
+  static constexpr int NT = D / 32;                          // tiles of 8 keys' elements of the state to a warp
+  static constexpr int SK = NT > 1 ? NT / 2 : 1;             // products along those
+  static constexpr int TT = C / 8, TK = C / 16;              // tiles of tokens, products along them
   static constexpr int COLS = 16 * NS;
-  static constexpr int KP = D + 8, PP = C + 8, TP = C + 4, VP = COLS + 16 / (int)sizeof(T);   // pitches
-  static constexpr int TILE = C * KP;                        // bf16 elements of one term of keys or queries
-  static constexpr int STAGES = 3;
-  // bf16 tiles are copied where they are used; fp32 ones wait in `raw` to be cut, and their terms have two places
-  static constexpr int PLACES = TERMS == 1 ? STAGES : 2;
-  static constexpr int RAW = TERMS == 1 ? 0 : 2 * C * (D + 4) * 4;
-  static constexpr int KQ = PLACES * 2 * TERMS * TILE * 2;
-  static constexpr int V = STAGES * C * VP * (int)sizeof(T);
-  static constexpr int TRI = 2 * C * TP * 4, Y = 16 * 20 * 4, P = 2 * SEEN * C * PP * 2;
-  static constexpr int S = NS * 3 * KS * 512, R = NS * 3 * (C / 16) * 512, U = NS * (3 + SEEN) * (C / 16) * 512;
-  static constexpr int OUT = C * VP * (int)sizeof(T);
-  static constexpr int GATES = 2 * (4 * C + 4) * 4;
-  static constexpr int SMEM = RAW + KQ + V + TRI + Y + P + S + R + U + OUT + GATES;
-  static_assert(SMEM + 1024 <= 227 * 1024, "shared memory");
+  static constexpr int KP = D + 8, AP = C + 4, VP = COLS + 16 / (int)sizeof(T), QP = TERMS == 1 ? D + 8 : D + 4;   // pitches
+  static constexpr int TILE = C * KP;                        // bf16 elements of one term of a window's keys
+  // a window's keys are fetched three steps ahead; fp32 ones wait in `raw` to be cut
+  static constexpr int K_PLACES = TERMS == 1 ? 4 : 3, V_PLACES = 4, G_PLACES = 4;
+  static constexpr int RAW = TERMS == 1 ? 0 : C * (D + 4) * 4;
+  static constexpr int K = K_PLACES * TERMS * TILE * 2, Q = 2 * C * QP * (int)sizeof(T), V = V_PLACES * C * VP * (int)sizeof(T);
+  static constexpr int TRI = 2 * C * AP * 4, Y = C == 64 ? 32 * 36 * 4 : 16 * 20 * 4, INV = 2 * TT * TK * 3 * 256;
+  static constexpr int X = NS * 4 * TT * 512, R = NS * 3 * TK * 512, U = NS * 3 * TK * 512, SEEN_U = 2 * NS * SEEN * TK * 512, S = 2 * NS * SEEN * KS * 512;
+  static constexpr int O = C * VP * (int)sizeof(T);
+  static constexpr int GATES = G_PLACES * (5 * C + 4) * 4;
+  static constexpr int SMEM = RAW + K + Q + V + TRI + Y + INV + X + R + U + SEEN_U + S + O + GATES;
+  static constexpr bool FITS = SMEM + 1024 <= 227 * 1024;
 };
 
 // a pair as three bf16 terms; a in the lower halves
@@ -58,14 +61,17 @@ __device__ __forceinline__ void cut(float a, float b, uint32_t (&t)[3]) {
     b -= __uint_as_float(t[i] & 0xFFFF0000u);
   }
 }
-// acc += A B, A of TA terms and B of TB: what is below the last term of the longer of the two is left out, and the products of the largest terms add up apart
+// acc += A B, A of TA terms and B of TB, small products first: what is below the last term of the longer of the two is left out
 template <int TA, int TB>
-__device__ __forceinline__ void product(float (&most)[4], float (&rest)[4], const uint32_t (&a)[TA][4], const uint32_t (&b)[TB][2]) {
+__device__ __forceinline__ void product(float (&acc)[4], const uint32_t (&a)[TA][4], const uint32_t (&b)[TB][2]) {
+  constexpr int MOST = TA > TB ? TA : TB;
 #pragma unroll
-  for (int i = 0; i < TA; ++i)
+  for (int sum = MOST - 1; sum >= 0; --sum)
 #pragma unroll
-    for (int j = 0; j < TB; ++j)
-      if (i + j < (TA > TB ? TA : TB)) mma16816(i + j == 0 ? most : rest, a[i], b[j][0], b[j][1]);
+    for (int i = 0; i < TA; ++i)
+#pragma unroll
+      for (int j = 0; j < TB; ++j)
+        if (i + j == sum) mma16816(acc, a[i], b[j][0], b[j][1]);
 }
 __device__ __forceinline__ void load16(uint32_t (&r)[4], const uint32_t* p) {
   const uint4 v = *reinterpret_cast<const uint4*>(p);
@@ -84,476 +90,686 @@ __device__ __forceinline__ void barrier(int id) { asm volatile("barrier.sync %0,
 __device__ __forceinline__ void copy16(void* dst, const void* src, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ bool finite2(uint32_t u) { return (u & 0x7F800000u) != 0x7F800000u && (u & 0x7F80u) != 0x7F80u; }
 template <typename T>
 __device__ __forceinline__ bool all_finite(uint4 v) {
   if (sizeof(T) == 2) return finite2(v.x) && finite2(v.y) && finite2(v.z) && finite2(v.w);
   return isfinite(__uint_as_float(v.x)) && isfinite(__uint_as_float(v.y)) && isfinite(__uint_as_float(v.z)) && isfinite(__uint_as_float(v.w));
 }
-// gates of a window's tokens; `odd`: something in its keys, values or gates is not finite
+// Gates of a window's tokens.  G is a sum in 64 bits of log2(e) log_decay, kept as a pair of floats: what counts are differences of far larger sums.
+template <int C>
 struct Gates {
-  float beta[C], up[C], down[C], sum[C];     // e^G, e^(G_C - G)
-  float whole, low;                          // e^G_C
-  int odd, pad;
+  float2 sum[C];                             // G
+  float beta[C], up[C], down[C];             // e^G, e^(G_C - G)
+  float whole;                               // e^G_C
+  int odd;                                   // something in the window's keys, values or gates is not finite
+  int pad[2];
+};
+__device__ __forceinline__ float fade_of(float2 to, float2 from) { return exp2_fast((to.x - from.x) + (to.y - from.y)); }
+
+// A group's rows of a window, 16 bytes to a thread and pass
+template <typename T, int ROWLEN, int C>
+struct Rows {
+  static constexpr int EACH = 16 / (int)sizeof(T), ROW = ROWLEN / EACH, STEP = GROUP / ROW, PASSES = (C + STEP - 1) / STEP;
+  const T* src;
+  int64_t stride;
+  int row, col;
+  __device__ __forceinline__ Rows(const T* base, int64_t token_stride, int tid) : src(base), stride(token_stride), row(tid / ROW), col(tid % ROW * EACH) {}
+  __device__ __forceinline__ void fetch(T* dst, int pitch, int first, int n) const {
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+      const int r = row + i * STEP;
+      if (STEP * PASSES > C && r >= C) break;
+      const bool there = first + r < n;
+      copy16(dst + r * pitch + col, src + (there ? (int64_t)(first + r) * stride : 0) + col, there);
+    }
+  }
+  __device__ __forceinline__ bool finite(const T* dst, int pitch) const {
+    bool fine = true;
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+      const int r = row + i * STEP;
+      if (STEP * PASSES > C && r >= C) break;
+      fine &= all_finite<T>(*reinterpret_cast<const uint4*>(dst + r * pitch + col));
+    }
+    return fine;
+  }
 };
 
-template <typename T, int D, int NS>
-__global__ void __launch_bounds__(THREADS) delta_chunk_kernel(const __grid_constant__ DeltaParams p) {
-  using H = Shape<T, D, NS>;
-  constexpr int TERMS = H::TERMS, SEEN = H::SEEN, KS = H::KS, NT = H::NT, COLS = H::COLS, KP = H::KP, PP = H::PP, TP = H::TP, VP = H::VP;
+template <typename H>
+__global__ void __launch_bounds__(THREADS, 1) delta_chunk_kernel(const __grid_constant__ DeltaParams p) {
+  using T = typename H::T;
+  constexpr int D = H::D, C = H::C, NS = H::NS, TERMS = H::TERMS, SEEN = H::SEEN, KS = H::KS, NT = H::NT, SK = H::SK, TT = H::TT, TK = H::TK, COLS = H::COLS, KP = H::KP,
+                AP = H::AP, VP = H::VP, QP = H::QP;
   extern __shared__ __align__(16) uint8_t smem[];
-  uint8_t* at = smem;
+  uint8_t* place = smem;
   auto room = [&](int bytes) {
-    uint8_t* r = at;
-    at += bytes;
+    uint8_t* r = place;
+    place += bytes;
     return r;
   };
-  float* raw = reinterpret_cast<float*>(room(H::RAW));                       // [keys, queries][C][D + 4]
-  __nv_bfloat16* kq = reinterpret_cast<__nv_bfloat16*>(room(H::KQ));         // [place][keys, queries][term][C][KP]
-  T* vs = reinterpret_cast<T*>(room(H::V));                                  // [stage][C][VP]
-  float* tri = reinterpret_cast<float*>(room(H::TRI));                       // [parity][C][TP]: A, then T
-  float* y = reinterpret_cast<float*>(room(H::Y));                           // [16][20]
-  __nv_bfloat16* ps = reinterpret_cast<__nv_bfloat16*>(room(H::P));          // [parity][SEEN terms][C][PP]
-  uint32_t* s_frag = reinterpret_cast<uint32_t*>(room(H::S));                // [run][term][KS][lane][4]
-  uint32_t* r_frag = reinterpret_cast<uint32_t*>(room(H::R));                // [run][term][C / 16][lane][4]
-  uint32_t* u_frag = reinterpret_cast<uint32_t*>(room(H::U));                // [run][3 faded terms, SEEN plain ones][C / 16][lane][4]
-  T* outs = reinterpret_cast<T*>(room(H::OUT));                              // [C][VP]
-  Gates* gates = reinterpret_cast<Gates*>(at);                               // [parity]
-  static_assert(sizeof(Gates) * 2 == H::GATES, "gates");
+  float* raw = reinterpret_cast<float*>(room(H::RAW));                       // [C][D + 4]
+  __nv_bfloat16* keys = reinterpret_cast<__nv_bfloat16*>(room(H::K));        // [place][term][C][KP]
+  T* queries = reinterpret_cast<T*>(room(H::Q));                             // [parity][C][QP]
+  T* values = reinterpret_cast<T*>(room(H::V));                              // [place][C][VP]
+  float* tri = reinterpret_cast<float*>(room(H::TRI));                       // [parity][C][AP]: A, then its inverse
+  float* y = reinterpret_cast<float*>(room(H::Y));
+  uint32_t* inverse = reinterpret_cast<uint32_t*>(room(H::INV));             // [parity][tile][TK][term][lane][2]
+  float* x_part = reinterpret_cast<float*>(room(H::X));                      // [run][warp][tile][lane][4]
+  uint32_t* r_frag = reinterpret_cast<uint32_t*>(room(H::R));                // [run][term][TK][lane][4]
+  uint32_t* u_frag = reinterpret_cast<uint32_t*>(room(H::U));                // [run][term][TK][lane][4], faded to the window's end
+  uint32_t* u_seen = reinterpret_cast<uint32_t*>(room(H::SEEN_U));           // [parity][run][term][TK][lane][4]
+  uint32_t* s_seen = reinterpret_cast<uint32_t*>(room(H::S));                // [parity][run][term][KS][lane][4]
+  T* outs = reinterpret_cast<T*>(room(H::O));                                // [C][VP]
+  Gates<C>* gates = reinterpret_cast<Gates<C>*>(place);                      // [place]
+  static_assert(sizeof(Gates<C>) * H::G_PLACES == H::GATES, "gates");
 
   const int b = blockIdx.z, h = blockIdx.y, col0 = (int)blockIdx.x * COLS;
   const int n = clamp_length(p.lengths, b, p.tokens);
   // before any of its data is touched: the slot of an entry that is passed over may be one that an earlier entry is writing
   const int slot = slot_of(p.slots, p.num_slots, b);
   if (slot < 0) return;                // the whole block
-  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int tid = threadIdx.x % GROUP, windows = (n + C - 1) / C;
-  const int hk = h / p.group;
-  const int64_t state = ((int64_t)slot * p.heads + h) * D * D + col0;
-
-  // ------------------------------------------------------------------------------- preparation
+  const int role = __shfl_sync(0xffffffffu, (int)(threadIdx.x / GROUP), 0), warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5) & 3, 0);
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, tid = threadIdx.x % GROUP;
+  const int windows = (n + C - 1) / C, hk = h / p.group;
   const T* q = reinterpret_cast<const T*>(p.q.p) + b * p.q.b + hk * p.q.h;
   const T* k = reinterpret_cast<const T*>(p.k.p) + b * p.k.b + hk * p.k.h;
   const T* v = reinterpret_cast<const T*>(p.v.p) + b * p.v.b + h * p.v.h + col0;
+  T* o = reinterpret_cast<T*>(p.o.p) + b * p.o.b + h * p.o.h + col0;
   const int64_t gate0 = (int64_t)b * p.tokens * p.heads + h;
-  constexpr int EACH = 16 / (int)sizeof(T), ROW = D / EACH, VROW = COLS / EACH;      // elements of a copy, copies of a row
-  auto fetch = [&](int w) {
-    T* kd;
-    int pitch;
-    if constexpr (TERMS == 1) {
-      kd = reinterpret_cast<T*>(kq) + (w % H::PLACES) * 2 * H::TILE;
-      pitch = KP;
-    } else {
-      kd = reinterpret_cast<T*>(raw);
-      pitch = D + 4;
-    }
-    for (int i = tid; i < 2 * C * ROW; i += GROUP) {
-      const int side = i / (C * ROW), r = i / ROW % C, c = i % ROW * EACH;
-      const bool there = w * C + r < n;
-      const int64_t token = there ? w * C + r : 0;
-      copy16(kd + (side * C + r) * pitch + c, side ? q + token * p.q.t + c : k + token * p.k.t + c, there);
-    }
-    for (int i = tid; i < C * VROW; i += GROUP) {
-      const int r = i / VROW, c = i % VROW * EACH;
-      const bool there = w * C + r < n;
-      copy16(vs + ((w % H::STAGES) * C + r) * VP + c, v + (int64_t)(there ? w * C + r : 0) * p.v.t + c, there);
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-  };
-  float next_decay = 0.f, next_beta = 0.f;     // of the first warp's tokens of the window that is prepared next
-  auto fetch_gates = [&](int w) {
-    const int token = w * C + lane;
-    next_decay = next_beta = 0.f;
-    if (warp != 4 || token >= n) return;
-    if (p.log_decay) next_decay = p.log_decay[gate0 + (int64_t)token * p.heads];
-    next_beta = p.beta[gate0 + (int64_t)token * p.heads];
-  };
-  auto prepare = [&](int w) {
-    const int parity = w & 1;
-    Gates& gt = gates[parity];
-    asm volatile("cp.async.wait_group 0;" ::: "memory");
-    bool odd = false;
-    // its own copies
-    for (int i = tid; i < C * ROW; i += GROUP) {
-      const int r = i / ROW, c = i % ROW * EACH;
-      const T* from = TERMS == 1 ? reinterpret_cast<const T*>(kq) + (w % H::PLACES) * 2 * H::TILE + r * KP + c : reinterpret_cast<const T*>(raw) + r * (D + 4) + c;
-      odd |= !all_finite<T>(*reinterpret_cast<const uint4*>(from));
-    }
-    for (int i = tid; i < C * VROW; i += GROUP)
-      odd |= !all_finite<T>(*reinterpret_cast<const uint4*>(vs + ((w % H::STAGES) * C + i / VROW) * VP + i % VROW * EACH));
-    if (warp == 4) {
-      // sums in 64 bits: what counts are differences of them, and a token may fade by any factor.  -infinity: all of it, like -10^5.
-      odd |= !isfinite(next_beta) || !(next_decay < INFINITY);
-      const double mine = next_decay < -1e5f ? -1e5 : (double)next_decay;
-      double sum = mine;
+  const int64_t state = ((int64_t)slot * p.heads + h) * D * D + col0;
+  auto keys_of = [&](int w) { return keys + (w % H::K_PLACES) * TERMS * H::TILE; };
+  auto values_of = [&](int w) { return values + (w % H::V_PLACES) * C * VP; };
+  auto gates_of = [&](int w) -> Gates<C>& { return gates[w % H::G_PLACES]; };
+
+  if (role == SYSTEM) {
+    // ------------------------------------------------------------------------------- A, two windows ahead
+    const Rows<T, D, C> k_rows(k, p.k.t, tid);
+    const Rows<T, COLS, C> v_rows(v, p.v.t, tid);
+    auto fetch = [&](int w) {
+      if constexpr (TERMS == 1) k_rows.fetch(reinterpret_cast<T*>(keys_of(w)), KP, w * C, n);
+      else k_rows.fetch(reinterpret_cast<T*>(raw), D + 4, w * C, n);
+      v_rows.fetch(values_of(w), VP, w * C, n);
+      copies_commit();
+    };
+    constexpr int PER = C / 32;                  // tokens of a lane of the first warp
+    float decay[PER] = {}, beta[PER] = {};
+    auto fetch_gates = [&](int w) {
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const double other = __shfl_up_sync(0xffffffffu, sum, o);
-        if (lane >= o) sum += other;
+      for (int i = 0; i < PER; ++i) {
+        const int token = w * C + lane * PER + i;
+        decay[i] = beta[i] = 0.f;
+        if (token < n) {
+          if (p.log_decay) decay[i] = p.log_decay[gate0 + (int64_t)token * p.heads];
+          beta[i] = p.beta[gate0 + (int64_t)token * p.heads];
+        }
       }
-      const double all = __shfl_sync(0xffffffffu, sum, 31);
-      gt.beta[lane] = next_beta;
-      gt.up[lane] = expf((float)sum);
-      gt.down[lane] = expf((float)(all - sum));
-      // differences are taken from this and, for what it lacks, `low`, which is the same for all of them: sums are counted from the window's middle
-      gt.sum[lane] = (float)sum;
-      reinterpret_cast<float*>(y)[lane] = (float)(sum - (double)(float)sum);
-      if (lane == 0) gt.whole = expf((float)all);
+    };
+    if (windows > 0) {
+      if (warp == 0) fetch_gates(0);
+      fetch(0);
     }
-    odd = named_barrier_or(2, GROUP, odd);
-    if (tid == 0) gt.odd = odd;
-    __nv_bfloat16* ks = kq + (w % H::PLACES) * 2 * TERMS * H::TILE;
-    __nv_bfloat16* qs = ks + TERMS * H::TILE;
-    if constexpr (TERMS == 3) {
-      for (int i = tid; i < 2 * C * (D / 2); i += GROUP) {
-        const int side = i / (C * (D / 2)), r = i / (D / 2) % C, c = i % (D / 2) * 2;
-        const float2 f = *reinterpret_cast<const float2*>(raw + (side * C + r) * (D + 4) + c);
-        uint32_t terms[3];
-        cut(f.x, f.y, terms);
+    for (int step = -2; step <= windows; ++step) {
+      const int w = step + 2;
+      if (w < windows) {
+        Gates<C>& gt = gates_of(w);
+        copies_wait();
+        bool odd = !v_rows.finite(values_of(w), VP);
+        if constexpr (TERMS == 1) odd |= !k_rows.finite(reinterpret_cast<const T*>(keys_of(w)), KP);
+        else odd |= !k_rows.finite(reinterpret_cast<const T*>(raw), D + 4);
+        if (warp == 0) {
+          double mine[PER], sum = 0.0;
 #pragma unroll
-        for (int x = 0; x < 3; ++x) *reinterpret_cast<uint32_t*>(ks + (side * 3 + x) * H::TILE + r * KP + c) = terms[x];
+          for (int i = 0; i < PER; ++i) {
+            odd |= !isfinite(beta[i]) || !(decay[i] < INFINITY);
+            // -infinity: all of it, like -10^5
+            sum += decay[i] < -1e5f ? -1e5 * 1.4426950408889634074 : (double)decay[i] * 1.4426950408889634074;
+            mine[i] = sum;
+          }
+#pragma unroll
+          for (int d = 1; d < 32; d <<= 1) {
+            const double other = __shfl_up_sync(0xffffffffu, sum, d);
+            if (lane >= d) sum += other;
+          }
+          const double all = __shfl_sync(0xffffffffu, sum, 31), before = sum - mine[PER - 1];
+#pragma unroll
+          for (int i = 0; i < PER; ++i) {
+            const double G = before + mine[i];
+            const int at = lane * PER + i;
+            gt.sum[at] = make_float2((float)G, (float)(G - (double)(float)G));
+            gt.beta[at] = beta[i];
+            gt.up[at] = exp2f((float)G);
+            gt.down[at] = exp2f((float)(all - G));
+          }
+          // the one factor that a state meets again and again: its error would add up
+          if (lane == 31) gt.whole = (float)exp2(all);
+        }
+        odd = named_barrier_or(1 + SYSTEM, GROUP, odd);
+        if (tid == 0) gt.odd = odd;
+        __nv_bfloat16* ks = keys_of(w);
+        if constexpr (TERMS == 3) {
+          for (int i = tid; i < C * (D / 2); i += GROUP) {
+            const int r = i / (D / 2), c = i % (D / 2) * 2;
+            const float2 f = *reinterpret_cast<const float2*>(raw + r * (D + 4) + c);
+            uint32_t terms[3];
+            cut(f.x, f.y, terms);
+#pragma unroll
+            for (int x = 0; x < 3; ++x) *reinterpret_cast<uint32_t*>(ks + x * H::TILE + r * KP + c) = terms[x];
+          }
+          barrier(1 + SYSTEM);
+        }
+        if (w + 1 < windows) {
+          fetch(w + 1);
+          if (warp == 0) fetch_gates(w + 1);
+        }
+        // 16 rows to a warp, or to two that share their columns' tiles: those up to the diagonal's
+        constexpr int SHARE = 4 / TK;
+        const int strip = warp % TK, first = warp / TK;
+        float acc[TT / SHARE][4];
+#pragma unroll
+        for (int i = 0; i < TT / SHARE; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
+#pragma unroll
+        for (int x = 0; x < KS; x += 2) {        // 32 elements
+          uint32_t a[2][TERMS][4];
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int i = 0; i < TERMS; ++i) ldmatrix4<false>(a[e][i], smem_u32(ks + i * H::TILE + (16 * strip + (lane & 15)) * KP + (x + e) * 16 + (lane >> 4) * 8));
+#pragma unroll
+          for (int i = 0; i < TT / SHARE; ++i) {
+            const int c = first + SHARE * i;
+            if (c < 2 * strip + 2) {
+              uint32_t one[TERMS][2], two[TERMS][2];
+#pragma unroll
+              for (int e = 0; e < TERMS; ++e) {
+                uint32_t f[4];
+                ldmatrix4<false>(f, smem_u32(ks + e * H::TILE + (8 * c + (lane & 7)) * KP + x * 16 + (lane >> 3) * 8));
+                one[e][0] = f[0]; one[e][1] = f[1]; two[e][0] = f[2]; two[e][1] = f[3];
+              }
+              product(acc[i], a[0], one);
+              product(acc[i], a[1], two);
+            }
+          }
+        }
+        float* A = tri + (w & 1) * C * AP;
+        const int i0 = 16 * strip + g;
+        const float2 sums[2] = {gt.sum[i0], gt.sum[i0 + 8]};
+        const float betas[2] = {gt.beta[i0], gt.beta[i0 + 8]};
+#pragma unroll
+        for (int i = 0; i < TT / SHARE; ++i) {
+          const int c = first + SHARE * i;
+          if (c < 2 * strip + 2) {
+            const int j = 8 * c + 2 * t;
+            const float4 from = *reinterpret_cast<const float4*>(gt.sum + j);
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              const float f0 = betas[r] * fade_of(sums[r], make_float2(from.x, from.y)) * acc[i][2 * r], f1 = betas[r] * fade_of(sums[r], make_float2(from.z, from.w)) * acc[i][2 * r + 1];
+              *reinterpret_cast<float2*>(A + (i0 + 8 * r) * AP + j) = make_float2(j < i0 + 8 * r ? f0 : 0.f, j + 1 < i0 + 8 * r ? f1 : 0.f);
+            }
+          }
+        }
       }
-      barrier(2);
+      __syncthreads();
     }
-    if (w + 1 < windows) {
-      fetch(w + 1);
-      fetch_gates(w + 1);
+  } else if (role == INVERSE) {
+    // ------------------------------------------------------------------------------- (1 + A)^-1, a window ahead
+    for (int step = -2; step <= windows; ++step) {
+      const int w = step + 1;
+      if (w >= 0 && w < windows) {
+        float* A = tri + (w & 1) * C * AP;
+        // what lies beside a pair of those blocks is read as part of a block of 32
+        if (C == 64) *reinterpret_cast<float4*>(A + (warp >> 1) * 32 * (AP + 1) + (tid & 63) / 4 * AP + 16 + tid % 4 * 4) = make_float4(0.f, 0.f, 0.f, 0.f);
+        // blocks of 16 on the diagonal, a column to a lane
+        if (warp < TK) {
+          float* at = A + warp * 16 * (AP + 1);
+          const int j = lane & 15;
+          float x[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            float a[16];
+#pragma unroll
+            for (int m = 0; m < i; m += 4) {
+              const float4 f = *reinterpret_cast<const float4*>(at + i * AP + m);
+              a[m] = f.x; a[m + 1] = f.y; a[m + 2] = f.z; a[m + 3] = f.w;
+            }
+            float sum = i == j ? 1.f : 0.f;
+#pragma unroll
+            for (int m = 0; m < i; ++m) sum = fmaf(-a[m], x[m], sum);
+            x[i] = sum;
+          }
+          __syncwarp();
+          if (lane < 16)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) at[i * AP + j] = x[i];
+        }
+        barrier(1 + INVERSE);
+        // what lies below a pair of blocks: -T_11 (A_10 T_00); blocks of 16, then of 32
+        auto below = [&](float* block, int m, const float* left, int left_pitch, const float* right, int right_pitch, float* to, int to_pitch, float sign, int r0, int rows, int c) {
+#pragma unroll 2
+          for (int r = r0; r < r0 + rows; ++r) {
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int e = 0; e < m; e += 4) {
+              const float4 a = *reinterpret_cast<const float4*>(left + r * left_pitch + e);
+#pragma unroll
+              for (int z = 0; z < 4; ++z) {
+                const float f = z == 0 ? a.x : z == 1 ? a.y : z == 2 ? a.z : a.w;
+                const float4 x = *reinterpret_cast<const float4*>(right + (e + z) * right_pitch + c);
+                sum = make_float4(fmaf(f, x.x, sum.x), fmaf(f, x.y, sum.y), fmaf(f, x.z, sum.z), fmaf(f, x.w, sum.w));
+              }
+            }
+            *reinterpret_cast<float4*>(to + r * to_pitch + c) = make_float4(sign * sum.x, sign * sum.y, sign * sum.z, sign * sum.w);
+          }
+        };
+        {
+          // a pair of blocks to two warps, or (one pair) to all four
+          const int pair = C == 64 ? warp >> 1 : 0, at = C == 64 ? tid & 63 : tid;
+          float* top = A + pair * 32 * (AP + 1);
+          float* bottom = top + 16 * AP;
+          float* part = y + pair * 16 * 20;
+          const int c = at % 4 * 4, r = at / 4;
+          if (r < 16) below(top, 16, bottom, AP, top, AP, part, 20, 1.f, r, 1, c);
+          barrier(1 + INVERSE);
+          if (r < 16) below(top, 16, bottom + 16, AP, part, 20, bottom, AP, -1.f, r, 1, c);
+          barrier(1 + INVERSE);
+        }
+        if constexpr (C == 64) {
+          float* bottom = A + 32 * AP;
+          const int c = tid % 8 * 4, r = tid / 8 * 2;
+          below(A, 32, bottom, AP, A, AP, y, 36, 1.f, r, 2, c);
+          barrier(1 + INVERSE);
+          below(A, 32, bottom + 32, AP, y, 36, bottom, AP, -1.f, r, 2, c);
+          barrier(1 + INVERSE);
+        }
+        // as the second operand's registers
+        uint32_t* to = inverse + (w & 1) * TT * TK * 3 * 64;
+        for (int i = warp; i < TT * TK; i += 4) {
+          const int tile = i / TK, x = i % TK;
+          if (x > tile / 2) continue;
+          uint32_t terms[2][3];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float2 f = *reinterpret_cast<const float2*>(A + (8 * tile + g) * AP + 16 * x + 8 * e + 2 * t);
+            cut(f.x, f.y, terms[e]);
+          }
+#pragma unroll
+          for (int e = 0; e < 3; ++e) *reinterpret_cast<uint2*>(to + ((i * 3 + e) * 32 + lane) * 2) = make_uint2(terms[0][e], terms[1][e]);
+        }
+      }
+      __syncthreads();
     }
-    // A and P: 16 rows to a warp, their columns up to the diagonal's
-    const int job = warp - 4, strip = job < 2 ? 1 : 0, rows = 16 * strip;
-    const bool keys = (job & 1) == 0;
-    const __nv_bfloat16* left = keys ? ks : qs;
-    float acc[4][4], rest[4][4];
+  } else if (role == OUT) {
+    // ------------------------------------------------------------------------------- out
+    // 16 tokens to a warp, or to two that share the runs of columns
+    constexpr int SHARE = 4 / TK, MINE = (NS + SHARE - 1) / SHARE;
+    constexpr int EACH = 16 / (int)sizeof(T);
+    const int strip = warp % TK, first = warp / TK, i0 = 16 * strip;
+    const Rows<T, D, C> q_rows(q, p.q.t, tid);
+    float acc[MINE][2][4];               // columns of values 16 x g and + 8, tokens 8 e + 2 t and + 1 of the strip
+    uint32_t weights[TK][2][SEEN][2];
+    for (int step = -2; step <= windows; ++step) {
+      // the last product of the window before
+      if (step >= 1 && first < NS && !gates_of(step - 1).odd) {
+        const int w = step - 1;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+        for (int m = 0; m < MINE; ++m) {
+          const int i = first + SHARE * m;
+          if (i >= NS) break;
 #pragma unroll
-      for (int x = 0; x < 4; ++x) acc[i][x] = rest[i][x] = 0.f;
+          for (int x = 0; x < TK; ++x)
+            if (x <= strip) {
+              uint32_t a[SEEN][4];
 #pragma unroll
-    for (int x = 0; x < KS; x += 2) {          // 32 elements
-      uint32_t a[2][TERMS][4];
+              for (int e = 0; e < SEEN; ++e) load16(a[e], u_seen + ((((w & 1) * NS + i) * SEEN + e) * TK + x) * 128 + lane * 4);
+              product(acc[m][0], a, weights[x][0]);
+              product(acc[m][1], a, weights[x][1]);
+            }
 #pragma unroll
-      for (int e = 0; e < 2; ++e)
+          for (int e = 0; e < 2; ++e) {
+            T* to = outs + (i0 + 8 * e + 2 * t) * VP + 16 * i + g;
+            to[0] = (T)acc[m][e][0];
+            to[VP] = (T)acc[m][e][1];
+            to[8] = (T)acc[m][e][2];
+            to[VP + 8] = (T)acc[m][e][3];
+          }
+          __syncwarp();
+          for (int e = lane; e < 16 * (16 / EACH); e += 32) {
+            const int r = i0 + e / (16 / EACH), c = 16 * i + e % (16 / EACH) * EACH;
+            if (w * C + r < n) *reinterpret_cast<uint4*>(o + (int64_t)(w * C + r) * p.o.t + c) = *reinterpret_cast<const uint4*>(outs + r * VP + c);
+          }
+        }
+        __syncwarp();
+      }
+      if (step >= -1 && step + 1 < windows) {
+        q_rows.fetch(queries + ((step + 1) & 1) * C * QP, QP, (step + 1) * C, n);
+        copies_commit();
+      }
+      if (step >= 0 && step < windows && first < NS) {
+        const int w = step;
+        const T* qs = queries + (w & 1) * C * QP;
+        const __nv_bfloat16* ks = keys_of(w);
+        const Gates<C>& gt = gates_of(w);
+        float dots[TT][4];
 #pragma unroll
-        for (int i = 0; i < TERMS; ++i) ldmatrix4<false>(a[e][i], smem_u32(left + i * H::TILE + (rows + (lane & 15)) * KP + (x + e) * 16 + (lane >> 4) * 8));
+        for (int i = 0; i < TT; ++i) dots[i][0] = dots[i][1] = dots[i][2] = dots[i][3] = 0.f;
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
-        if (c < 2 * strip + 2) {
+        for (int m = 0; m < MINE; ++m)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) acc[m][e][0] = acc[m][e][1] = acc[m][e][2] = acc[m][e][3] = 0.f;
+#pragma unroll
+        for (int x = 0; x < KS; ++x) {
+          // the strip's queries as the first operand; as the second, registers 0 and 2 are its first eight tokens, 1 and 3 the others
+          uint32_t a[TERMS][4];
+          if constexpr (TERMS == 1) {
+            ldmatrix4<false>(a[0], smem_u32(qs + (i0 + (lane & 15)) * QP + x * 16 + (lane >> 4) * 8));
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float2 f = *reinterpret_cast<const float2*>(qs + (i0 + g + 8 * (e & 1)) * QP + x * 16 + 8 * (e >> 1) + 2 * t);
+              uint32_t terms[3];
+              cut(f.x, f.y, terms);
+#pragma unroll
+              for (int c = 0; c < 3; ++c) a[c][e] = terms[c];
+            }
+          }
           uint32_t one[TERMS][2], two[TERMS][2];
 #pragma unroll
-          for (int i = 0; i < TERMS; ++i) {
-            uint32_t f[4];
-            ldmatrix4<false>(f, smem_u32(ks + i * H::TILE + (8 * c + (lane & 7)) * KP + x * 16 + (lane >> 3) * 8));
-            one[i][0] = f[0]; one[i][1] = f[1]; two[i][0] = f[2]; two[i][1] = f[3];
+          for (int e = 0; e < TERMS; ++e) {
+            one[e][0] = a[e][0]; one[e][1] = a[e][2];
+            two[e][0] = a[e][1]; two[e][1] = a[e][3];
           }
-          product(acc[c], rest[c], a[0], one);
-          product(acc[c], rest[c], a[1], two);
+#pragma unroll
+          for (int m = 0; m < MINE; ++m) {
+            const int i = first + SHARE * m;
+            if (i >= NS) break;
+            uint32_t f[SEEN][4];
+#pragma unroll
+            for (int e = 0; e < SEEN; ++e) load16(f[e], s_seen + ((((w & 1) * NS + i) * SEEN + e) * KS + x) * 128 + lane * 4);
+            product(acc[m][0], f, one);
+            product(acc[m][1], f, two);
+          }
+#pragma unroll
+          for (int c = 0; c < TT; c += 2)
+            if (c <= 2 * strip) {
+              uint32_t left[TERMS][2], right[TERMS][2];
+#pragma unroll
+              for (int e = 0; e < TERMS; ++e) {
+                uint32_t f[4];
+                ldmatrix4<false>(f, smem_u32(ks + e * H::TILE + (8 * c + (lane & 7) + 8 * (lane >> 4)) * KP + x * 16 + ((lane >> 3) & 1) * 8));
+                left[e][0] = f[0]; left[e][1] = f[1]; right[e][0] = f[2]; right[e][1] = f[3];
+              }
+              product(dots[c], a, left);
+              product(dots[c + 1], a, right);
+            }
         }
-    }
-    float* A = tri + parity * C * TP;
-    const float* low = y;
+        // P, and the part of the state
+        const int at = i0 + g;
+        const float2 sums[2] = {gt.sum[at], gt.sum[at + 8]};
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
-      if (c < 2 * strip + 2)
+        for (int c = 0; c < TT; ++c)
+          if (c < 2 * strip + 2) {
+            const int j = 8 * c + 2 * t;
+            const float4 from = *reinterpret_cast<const float4*>(gt.sum + j);
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const int i = rows + g + 8 * r, j = 8 * c + 2 * t;
-          const float si = gt.sum[i], li = low[i];
-          float f[2];
+            for (int r = 0; r < 2; ++r) {
+              const float f0 = p.scale * fade_of(sums[r], make_float2(from.x, from.y)) * dots[c][2 * r], f1 = p.scale * fade_of(sums[r], make_float2(from.z, from.w)) * dots[c][2 * r + 1];
+              uint32_t terms[3];
+              cut(j <= at + 8 * r ? f0 : 0.f, j + 1 <= at + 8 * r ? f1 : 0.f, terms);
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const bool there = keys ? j + x < i : j + x <= i;
-            const float fade = expf((si - gt.sum[j + x]) + (li - low[j + x]));
-            f[x] = there ? (keys ? gt.beta[i] : p.scale) * fade * (acc[c][2 * r + x] + rest[c][2 * r + x]) : 0.f;
+              for (int e = 0; e < SEEN; ++e) weights[c >> 1][r][e][c & 1] = terms[e];
+            }
           }
-          if (keys) {
-            *reinterpret_cast<float2*>(A + i * TP + j) = make_float2(f[0], f[1]);
-          } else {
-            uint32_t terms[3];
-            cut(f[0], f[1], terms);
-#pragma unroll
-            for (int x = 0; x < SEEN; ++x) *reinterpret_cast<uint32_t*>(ps + (parity * SEEN + x) * C * PP + i * PP + j) = terms[x];
-          }
-        }
-    barrier(2);
-    // the inverses of both diagonal blocks, a column to a lane
-    if (job < 2) {
-      float* at = A + job * 16 * (TP + 1);
-      const int j = lane & 15;
-      float x[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        float sum = i == j ? 1.f : 0.f;
-#pragma unroll
-        for (int m = 0; m < i; ++m) sum = fmaf(-at[i * TP + m], x[m], sum);
-        x[i] = sum;
-      }
-      __syncwarp();
-      if (lane < 16)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) at[i * TP + j] = x[i];
-    }
-    barrier(2);
-    // the block below: -T_11 (A_10 T_00)
-    const int r = tid / 8, c = tid % 8 * 2;
-    {
-      float2 sum = make_float2(0.f, 0.f);
-#pragma unroll
-      for (int m = 0; m < 16; ++m) {
-        const float a = A[(16 + r) * TP + m];
-        const float2 x = *reinterpret_cast<const float2*>(A + m * TP + c);
-        sum = make_float2(fmaf(a, x.x, sum.x), fmaf(a, x.y, sum.y));
-      }
-      *reinterpret_cast<float2*>(y + r * 20 + c) = sum;
-    }
-    barrier(2);
-    {
-      float2 sum = make_float2(0.f, 0.f);
-#pragma unroll
-      for (int m = 0; m < 16; ++m) {
-        const float a = A[(16 + r) * TP + 16 + m];
-        const float2 x = *reinterpret_cast<const float2*>(y + m * 20 + c);
-        sum = make_float2(fmaf(-a, x.x, sum.x), fmaf(-a, x.y, sum.y));
-      }
-      *reinterpret_cast<float2*>(A + (16 + r) * TP + c) = sum;
-    }
-  };
-
-  // ------------------------------------------------------------------------------- the chain
-  // rows: value columns 16 s + g and + 8; columns: elements 2t and 2t + 1 of the warp's tiles of 8
-  float s[NS][NT][4];
-  auto keep_state = [&]() {
-#pragma unroll
-    for (int i = 0; i < NS; ++i)
-#pragma unroll
-      for (int x = 0; x < NT; ++x) keep<3>(s_frag + i * 3 * KS * 128, KS * 128, lane, warp * NT + x, s[i][x]);
-  };
-  T* o = reinterpret_cast<T*>(p.o.p) + b * p.o.b + h * p.o.h + col0;
-  auto advance = [&](int w) {
-    const int parity = w & 1;
-    const Gates& gt = gates[parity];
-    const float* T_ = tri + parity * C * TP;
-    const __nv_bfloat16* ks = kq + (w % H::PLACES) * 2 * TERMS * H::TILE;
-    const __nv_bfloat16* qs = ks + TERMS * H::TILE;
-    // this warp's tokens: 8 warp .. 8 warp + 7, products along tokens up to theirs
-    const int steps = warp / 2 + 1;
-    uint32_t tf[2][3][2];
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float2 f = x < steps ? *reinterpret_cast<const float2*>(T_ + (8 * warp + g) * TP + 16 * x + 8 * e + 2 * t) : make_float2(0.f, 0.f);
-        uint32_t terms[3];
-        cut(f.x, f.y, terms);
-#pragma unroll
-        for (int i = 0; i < 3; ++i) tf[x][i][e] = terms[i];
-      }
-    }
-    const int token = 8 * warp + 2 * t;
-    const float2 beta = *reinterpret_cast<const float2*>(gt.beta + token), up = *reinterpret_cast<const float2*>(gt.up + token),
-                 down = *reinterpret_cast<const float2*>(gt.down + token);
-    // S^T K^T and S^T Q^T
-    float x0[NS][4], x1[NS][4], o0[NS][4], o1[NS][4];
-#pragma unroll
-    for (int i = 0; i < NS; ++i)
-#pragma unroll
-      for (int x = 0; x < 4; ++x) x0[i][x] = x1[i][x] = o0[i][x] = o1[i][x] = 0.f;
-#pragma unroll
-    for (int x = 0; x < KS; x += 2) {
-      uint32_t kf[2][TERMS][2], qf[2][TERMS][2];
-#pragma unroll
-      for (int i = 0; i < TERMS; ++i) {
-        uint32_t f[4];
-        const int at = i * H::TILE + (8 * warp + (lane & 7)) * KP + x * 16 + (lane >> 3) * 8;
-        ldmatrix4<false>(f, smem_u32(ks + at));
-        kf[0][i][0] = f[0]; kf[0][i][1] = f[1]; kf[1][i][0] = f[2]; kf[1][i][1] = f[3];
-        ldmatrix4<false>(f, smem_u32(qs + at));
-        qf[0][i][0] = f[0]; qf[0][i][1] = f[1]; qf[1][i][0] = f[2]; qf[1][i][1] = f[3];
-      }
-#pragma unroll
-      for (int i = 0; i < NS; ++i)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          uint32_t a[3][4];
+          const float2 up = *reinterpret_cast<const float2*>(gt.up + i0 + 8 * e + 2 * t);
 #pragma unroll
-          for (int c = 0; c < 3; ++c) load16(a[c], s_frag + ((i * 3 + c) * KS + x + e) * 128 + lane * 4);
-          product(x0[i], x1[i], a, kf[e]);
-          product(o0[i], o1[i], reinterpret_cast<const uint32_t(&)[SEEN][4]>(a), qf[e]);
+          for (int m = 0; m < MINE; ++m) {
+            acc[m][e][0] *= p.scale * up.x; acc[m][e][1] *= p.scale * up.y;
+            acc[m][e][2] *= p.scale * up.x; acc[m][e][3] *= p.scale * up.y;
+          }
         }
-    }
-#pragma unroll
-    for (int i = 0; i < NS; ++i) {
-      const T* vv = vs + ((w % H::STAGES) * C + token) * VP + 16 * i + g;
-      float r[4];
-      r[0] = beta.x * fmaf(-up.x, x0[i][0] + x1[i][0], to_float(vv[0]));
-      r[1] = beta.y * fmaf(-up.y, x0[i][1] + x1[i][1], to_float(vv[VP]));
-      r[2] = beta.x * fmaf(-up.x, x0[i][2] + x1[i][2], to_float(vv[8]));
-      r[3] = beta.y * fmaf(-up.y, x0[i][3] + x1[i][3], to_float(vv[VP + 8]));
-      keep<3>(r_frag + i * 3 * (C / 16) * 128, (C / 16) * 128, lane, warp, r);
-#pragma unroll
-      for (int x = 0; x < 4; ++x) o0[i][x] = (o0[i][x] + o1[i][x]) * (p.scale * (x & 1 ? up.y : up.x));
-    }
-    barrier(1);
-    // U^T = R^T T^T
-#pragma unroll
-    for (int i = 0; i < NS; ++i) {
-      float u0[4] = {}, u1[4] = {};
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-        if (x < steps) {
-          uint32_t a[3][4];
-#pragma unroll
-          for (int c = 0; c < 3; ++c) load16(a[c], r_frag + ((i * 3 + c) * (C / 16) + x) * 128 + lane * 4);
-          product(u0, u1, a, tf[x]);
-        }
-#pragma unroll
-      for (int x = 0; x < 4; ++x) u0[x] += u1[x];
-      uint32_t* to = u_frag + i * (3 + SEEN) * (C / 16) * 128;
-      keep<SEEN>(to + 3 * (C / 16) * 128, (C / 16) * 128, lane, warp, u0);
-      u0[0] *= down.x; u0[1] *= down.y; u0[2] *= down.x; u0[3] *= down.y;
-      keep<3>(to, (C / 16) * 128, lane, warp, u0);
-    }
-    barrier(1);
-    // S'^T = e^G_C S^T + U'^T K
-    uint32_t pf[2][SEEN][2];
-#pragma unroll
-    for (int i = 0; i < SEEN; ++i) {
-      uint32_t f[4];
-      ldmatrix4<false>(f, smem_u32(ps + (parity * SEEN + i) * C * PP + (8 * warp + (lane & 7)) * PP + (lane >> 3) * 8));
-      pf[0][i][0] = f[0]; pf[0][i][1] = f[1]; pf[1][i][0] = f[2]; pf[1][i][1] = f[3];
-    }
-    const float whole = gt.whole;
-#pragma unroll
-    for (int i = 0; i < NS; ++i) {
-      uint32_t a[2][3][4];
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int c = 0; c < 3; ++c) load16(a[x][c], u_frag + ((i * (3 + SEEN) + c) * (C / 16) + x) * 128 + lane * 4);
-#pragma unroll
-      for (int m = 0; m < NT; ++m) {
-        float d0[4] = {}, d1[4] = {};
-        uint32_t one[TERMS][2], two[TERMS][2];
-#pragma unroll
-        for (int c = 0; c < TERMS; ++c) {
-          uint32_t f[4];
-          ldmatrix4<true>(f, smem_u32(ks + c * H::TILE + lane * KP + (warp * NT + m) * 8));
-          one[c][0] = f[0]; one[c][1] = f[1]; two[c][0] = f[2]; two[c][1] = f[3];
-        }
-        product(d0, d1, a[0], one);
-        product(d0, d1, a[1], two);
-#pragma unroll
-        for (int x = 0; x < 4; ++x) s[i][m][x] = fmaf(whole, s[i][m][x], d0[x] + d1[x]);
       }
+      copies_wait();
+      __syncthreads();
     }
-    keep_state();
-    // out: behind the state, which the others wait for
-#pragma unroll
-    for (int i = 0; i < NS; ++i) {
-#pragma unroll
-      for (int x = 0; x < 4; ++x) o1[i][x] = 0.f;
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-        if (x < steps) {
-          uint32_t a[SEEN][4];
-#pragma unroll
-          for (int c = 0; c < SEEN; ++c) load16(a[c], u_frag + ((i * (3 + SEEN) + 3 + c) * (C / 16) + x) * 128 + lane * 4);
-          product(o0[i], o1[i], a, pf[x]);
-        }
-      T* to = outs + token * VP + 16 * i + g;
-      to[0] = (T)(o0[i][0] + o1[i][0]);
-      to[VP] = (T)(o0[i][1] + o1[i][1]);
-      to[8] = (T)(o0[i][2] + o1[i][2]);
-      to[VP + 8] = (T)(o0[i][3] + o1[i][3]);
-    }
-    __syncwarp();
-    for (int i = lane; i < 8 * VROW; i += 32) {
-      const int r = 8 * warp + i / VROW, c = i % VROW * EACH;
-      if (w * C + r < n) *reinterpret_cast<uint4*>(o + (int64_t)(w * C + r) * p.o.t + c) = *reinterpret_cast<const uint4*>(outs + r * VP + c);
-    }
-    __syncwarp();
-  };
-  // A window with something in it that is not finite, token by token, a value column to a thread: the weights of 0 that a window's products give earlier tokens would
-  // make NaN of it.
-  auto advance_slowly = [&](int w) {
-    float* st = reinterpret_cast<float*>(s_frag);      // [COLS][D + 1]
-    static_assert(COLS * (D + 1) * 4 <= H::S + H::R, "the state takes its operands' place");
-    auto each = [&](auto f) {
-#pragma unroll
-      for (int i = 0; i < NS; ++i)
-#pragma unroll
-        for (int x = 0; x < NT; ++x)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) f(s[i][x][e], st[(16 * i + g + 8 * (e >> 1)) * (D + 1) + (warp * NT + x) * 8 + 2 * t + (e & 1)]);
-    };
-    each([](float& mine, float& there) { there = mine; });
-    barrier(1);
-    if (tid < COLS) {
-      float* mine = st + tid * (D + 1);
-      for (int i = w * C; i < min(n, w * C + C); ++i) {
-        const T* kk = k + (int64_t)i * p.k.t;
-        const T* qq = q + (int64_t)i * p.q.t;
-        const float fade = p.log_decay ? expf(p.log_decay[gate0 + (int64_t)i * p.heads]) : 1.f;
-        float said = 0.f, sum = 0.f;
-        for (int e = 0; e < D; ++e) said = fmaf(to_float(kk[e]), fade * mine[e], said);
-        const float u = p.beta[gate0 + (int64_t)i * p.heads] * (to_float(v[(int64_t)i * p.v.t + tid]) - said);
-        for (int e = 0; e < D; ++e) {
-          mine[e] = fmaf(fade, mine[e], to_float(kk[e]) * u);
-          sum = fmaf(to_float(qq[e]), mine[e], sum);
-        }
-        o[(int64_t)i * p.o.t + tid] = (T)(p.scale * sum);
-      }
-    }
-    barrier(1);
-    each([](float& mine, float& there) { mine = there; });
-    barrier(1);                        // the state's operands take the place back
-    keep_state();
-  };
-
-  if (warp < 4) {
+  } else {
+    // ------------------------------------------------------------------------------- the chain
+    // rows: value columns 16 i + g and + 8; columns: elements 2t and 2t + 1 of the warp's tiles of 8
+    float s[NS][NT][4];
 #pragma unroll
     for (int i = 0; i < NS; ++i)
 #pragma unroll
       for (int x = 0; x < NT; ++x)
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[i][x][e] = p.state[state + (int64_t)((warp * NT + x) * 8 + 2 * t + (e & 1)) * D + 16 * i + g + 8 * (e >> 1)];
-    keep_state();
-  } else if (windows > 0) {
-    fetch_gates(0);
-    fetch(0);
-    prepare(0);
-  }
-  __syncthreads();
-  for (int w = 0; w < windows; ++w) {
-    if (warp >= 4) {
-      if (w + 1 < windows) prepare(w + 1);
-    } else if (gates[w & 1].odd) {
-      advance_slowly(w);
-    } else {
-      advance(w);
+    // the state before window w as an operand: what it says of the window's keys, this warp's part, and its terms for out
+    auto ask = [&](int w) {
+      const __nv_bfloat16* ks = keys_of(w);
+#pragma unroll
+      for (int i = 0; i < NS; ++i) {
+        uint32_t a[SK][3][4];
+#pragma unroll
+        for (int x = 0; x < NT; ++x)
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            uint32_t terms[3];
+            cut(s[i][x][2 * r], s[i][x][2 * r + 1], terms);
+#pragma unroll
+            for (int e = 0; e < 3; ++e) {
+              a[x / 2][e][2 * (x & 1) + r] = terms[e];
+              if (NT == 1) a[0][e][2 + r] = 0u;
+            }
+          }
+        float acc[TT][4];
+#pragma unroll
+        for (int c = 0; c < TT; ++c) acc[c][0] = acc[c][1] = acc[c][2] = acc[c][3] = 0.f;
+        // four blocks of 8 tokens x 8 elements a load: 4 / NT tiles of tokens
+#pragma unroll
+        for (int c = 0; c < TT; c += 4 / NT) {
+          uint32_t f[TERMS][4];
+#pragma unroll
+          for (int e = 0; e < TERMS; ++e)
+            ldmatrix4<false>(f[e], smem_u32(ks + e * H::TILE + (8 * (c + (lane >> 3) / NT) + (lane & 7)) * KP + (warp * NT + (lane >> 3) % NT) * 8));
+#pragma unroll
+          for (int z = 0; z < 4 / NT; ++z)
+#pragma unroll
+            for (int x = 0; x < SK; ++x) {
+              uint32_t one[TERMS][2];
+#pragma unroll
+              for (int e = 0; e < TERMS; ++e) {
+                one[e][0] = f[e][z * NT + 2 * x];
+                one[e][1] = NT == 1 ? 0u : f[e][(z * NT + 2 * x + 1) % 4];
+              }
+              product(acc[c + z], a[x], one);
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < TT; ++c) *reinterpret_cast<float4*>(x_part + ((i * 4 + warp) * TT + c) * 128 + lane * 4) = make_float4(acc[c][0], acc[c][1], acc[c][2], acc[c][3]);
+#pragma unroll
+        for (int e = 0; e < SEEN; ++e) {
+          uint32_t* to = s_seen + (((w & 1) * NS + i) * SEEN + e) * KS * 128 + lane * 4;
+          if (NT == 1) {
+            *reinterpret_cast<uint2*>(to + (warp >> 1) * 128 + (warp & 1) * 2) = make_uint2(a[0][e][0], a[0][e][1]);
+          } else {
+#pragma unroll
+            for (int x = 0; x < SK; ++x) *reinterpret_cast<uint4*>(to + (warp * SK + x) * 128) = make_uint4(a[x][e][0], a[x][e][1], a[x][e][2], a[x][e][3]);
+          }
+        }
+      }
+    };
+    constexpr int MINE = TT / 4;           // tiles of tokens whose R and U are this warp's: one near either end, for theirs are long and short sums
+    auto advance = [&](int w) {
+      const __nv_bfloat16* ks = keys_of(w);
+      const T* vs = values_of(w);
+      const Gates<C>& gt = gates_of(w);
+      const uint32_t* inv = inverse + (w & 1) * TT * TK * 3 * 64;
+      float2 down[MINE];
+#pragma unroll
+      for (int m = 0; m < MINE; ++m) {
+        const int tile = m == 0 ? warp : TT - 1 - warp, token = 8 * tile + 2 * t;
+        const float2 beta = *reinterpret_cast<const float2*>(gt.beta + token), up = *reinterpret_cast<const float2*>(gt.up + token);
+        down[m] = *reinterpret_cast<const float2*>(gt.down + token);
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+          float4 x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = *reinterpret_cast<const float4*>(x_part + ((i * 4 + e) * TT + tile) * 128 + lane * 4);
+          const T* vv = vs + token * VP + 16 * i + g;
+          float r[4];
+          r[0] = beta.x * fmaf(-up.x, (x[0].x + x[1].x) + (x[2].x + x[3].x), to_float(vv[0]));
+          r[1] = beta.y * fmaf(-up.y, (x[0].y + x[1].y) + (x[2].y + x[3].y), to_float(vv[VP]));
+          r[2] = beta.x * fmaf(-up.x, (x[0].z + x[1].z) + (x[2].z + x[3].z), to_float(vv[8]));
+          r[3] = beta.y * fmaf(-up.y, (x[0].w + x[1].w) + (x[2].w + x[3].w), to_float(vv[VP + 8]));
+          keep<3>(r_frag + i * 3 * TK * 128, TK * 128, lane, tile, r);
+        }
+      }
+      barrier(1 + CHAIN);
+      // U^T = R^T T^T
+#pragma unroll
+      for (int i = 0; i < NS; ++i) {
+        float u[MINE][2][4];
+#pragma unroll
+        for (int m = 0; m < MINE; ++m)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) u[m][0][e] = u[m][1][e] = 0.f;
+#pragma unroll
+        for (int x = 0; x < TK; ++x) {
+          uint32_t a[3][4];
+          if (x <= (MINE == 1 ? warp : TT - 1 - warp) / 2) {
+#pragma unroll
+            for (int e = 0; e < 3; ++e) load16(a[e], r_frag + ((i * 3 + e) * TK + x) * 128 + lane * 4);
+          }
+#pragma unroll
+          for (int m = 0; m < MINE; ++m) {
+            const int tile = m == 0 ? warp : TT - 1 - warp;
+            if (x <= tile / 2) {
+              uint32_t f[3][2];
+#pragma unroll
+              for (int e = 0; e < 3; ++e) {
+                const uint2 z = *reinterpret_cast<const uint2*>(inv + (((tile * TK + x) * 3 + e) * 32 + lane) * 2);
+                f[e][0] = z.x; f[e][1] = z.y;
+              }
+              product(u[m][x & 1], a, f);
+            }
+          }
+        }
+#pragma unroll
+        for (int m = 0; m < MINE; ++m) {
+          const int tile = m == 0 ? warp : TT - 1 - warp;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) u[m][0][e] += u[m][1][e];
+          keep<SEEN>(u_seen + ((w & 1) * NS + i) * SEEN * TK * 128, TK * 128, lane, tile, u[m][0]);
+          u[m][0][0] *= down[m].x; u[m][0][1] *= down[m].y; u[m][0][2] *= down[m].x; u[m][0][3] *= down[m].y;
+          keep<3>(u_frag + i * 3 * TK * 128, TK * 128, lane, tile, u[m][0]);
+        }
+      }
+      barrier(1 + CHAIN);
+      // S'^T = e^G_C S^T + U'^T K
+      const float whole = gt.whole;
+#pragma unroll
+      for (int i = 0; i < NS; ++i) {
+        float d[NT][2][4];
+#pragma unroll
+        for (int m = 0; m < NT; ++m)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) d[m][0][e] = d[m][1][e] = 0.f;
+#pragma unroll
+        for (int x = 0; x < TK; x += 2) {
+          uint32_t a[2][3][4];
+#pragma unroll
+          for (int z = 0; z < 2; ++z)
+#pragma unroll
+            for (int e = 0; e < 3; ++e) load16(a[z][e], u_frag + ((i * 3 + e) * TK + x + z) * 128 + lane * 4);
+#pragma unroll
+          for (int m = 0; m < NT; ++m) {
+            uint32_t one[TERMS][2], two[TERMS][2];
+#pragma unroll
+            for (int e = 0; e < TERMS; ++e) {
+              uint32_t f[4];
+              ldmatrix4<true>(f, smem_u32(ks + e * H::TILE + (16 * x + lane) * KP + (warp * NT + m) * 8));
+              one[e][0] = f[0]; one[e][1] = f[1]; two[e][0] = f[2]; two[e][1] = f[3];
+            }
+            product(d[m][0], a[0], one);
+            product(d[m][1], a[1], two);
+          }
+        }
+#pragma unroll
+        for (int m = 0; m < NT; ++m)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[i][m][e] = fmaf(whole, s[i][m][e], d[m][0][e] + d[m][1][e]);
+      }
+    };
+    // A window with something in it that is not finite, token by token, a value column to a thread: the weights of 0 that a window's products give earlier tokens would
+    // make NaN of it.
+    auto advance_slowly = [&](int w) {
+      float* st = x_part;                  // [COLS][D + 1]
+      static_assert(COLS * (D + 1) * 4 <= H::X + H::R, "the state takes the place of the chain's operands");
+      auto each = [&](auto f) {
+#pragma unroll
+        for (int i = 0; i < NS; ++i)
+#pragma unroll
+          for (int x = 0; x < NT; ++x)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f(s[i][x][e], st[(16 * i + g + 8 * (e >> 1)) * (D + 1) + (warp * NT + x) * 8 + 2 * t + (e & 1)]);
+      };
+      each([](float& mine, float& there) { there = mine; });
+      barrier(1 + CHAIN);
+      if (tid < COLS) {
+        float* mine = st + tid * (D + 1);
+        for (int i = w * C; i < min(n, w * C + C); ++i) {
+          const T* kk = k + (int64_t)i * p.k.t;
+          const T* qq = q + (int64_t)i * p.q.t;
+          const float fade = p.log_decay ? expf(p.log_decay[gate0 + (int64_t)i * p.heads]) : 1.f;
+          float said = 0.f, sum = 0.f;
+          for (int e = 0; e < D; ++e) said = fmaf(to_float(kk[e]), fade * mine[e], said);
+          const float u = p.beta[gate0 + (int64_t)i * p.heads] * (to_float(v[(int64_t)i * p.v.t + tid]) - said);
+          for (int e = 0; e < D; ++e) {
+            mine[e] = fmaf(fade, mine[e], to_float(kk[e]) * u);
+            sum = fmaf(to_float(qq[e]), mine[e], sum);
+          }
+          o[(int64_t)i * p.o.t + tid] = (T)(p.scale * sum);
+        }
+      }
+      barrier(1 + CHAIN);
+      each([](float& mine, float& there) { mine = there; });
+      barrier(1 + CHAIN);                  // the operands take the place back
+    };
+    for (int step = -2; step <= windows; ++step) {
+      if (step >= 0 && step < windows) {
+        if (gates_of(step).odd) advance_slowly(step);
+        else advance(step);
+      }
+      if (step >= -1 && step + 1 < windows) ask(step + 1);
+      __syncthreads();
     }
-    __syncthreads();                   // the next window is prepared, this one's places are free
+    if (windows > 0 || p.state_out != p.state)
+#pragma unroll
+      for (int i = 0; i < NS; ++i)
+#pragma unroll
+        for (int x = 0; x < NT; ++x)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) p.state_out[state + (int64_t)((warp * NT + x) * 8 + 2 * t + (e & 1)) * D + 16 * i + g + 8 * (e >> 1)] = s[i][x][e];
   }
-  if (warp < 4 && (windows > 0 || p.state_out != p.state))
-#pragma unroll
-    for (int i = 0; i < NS; ++i)
-#pragma unroll
-      for (int x = 0; x < NT; ++x)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) p.state_out[state + (int64_t)((warp * NT + x) * 8 + 2 * t + (e & 1)) * D + 16 * i + g + 8 * (e >> 1)] = s[i][x][e];
 }
 
-template <typename T, int D, int NS>
-cudaError_t launch(const DeltaParams& p, cudaStream_t s) {
-  using H = Shape<T, D, NS>;
+template <typename H>
+cudaError_t launch_shape(const DeltaParams& p, cudaStream_t s) {
+  static_assert(H::FITS, "shared memory");
   static OncePerContext once;
-  const cudaError_t e = once([] { return cudaFuncSetAttribute(delta_chunk_kernel<T, D, NS>, cudaFuncAttributeMaxDynamicSharedMemorySize, H::SMEM); });
+  const cudaError_t e = once([] { return cudaFuncSetAttribute(delta_chunk_kernel<H>, cudaFuncAttributeMaxDynamicSharedMemorySize, H::SMEM); });
   if (e != cudaSuccess) return e;
-  delta_chunk_kernel<T, D, NS><<<dim3(D / H::COLS, (unsigned)p.heads, (unsigned)p.batch), THREADS, H::SMEM, s>>>(p);
+  delta_chunk_kernel<H><<<dim3(H::D / H::COLS, (unsigned)p.heads, (unsigned)p.batch), THREADS, H::SMEM, s>>>(p);
   return cudaGetLastError();
 }
 template <typename T, int D>
 cudaError_t launch(const DeltaParams& p, cudaStream_t s) {
-  return (int64_t)p.batch * p.heads * (D / 16) < 4 * PLAN_SMS ? launch<T, D, 1>(p, s) : launch<T, D, 2>(p, s);
+  const int64_t runs = (int64_t)p.batch * p.heads * (D / 16);
+  if constexpr (Shape<T, D, 64, 1>::FITS)
+    if (runs <= PLAN_SMS) return launch_shape<Shape<T, D, 64, 1>>(p, s);
+  if constexpr (Shape<T, D, 32, 2>::FITS)
+    if (runs > 2 * PLAN_SMS) return launch_shape<Shape<T, D, 32, 2>>(p, s);
+  return launch_shape<Shape<T, D, 32, 1>>(p, s);
 }
 template <typename T>
 cudaError_t launch(const DeltaParams& p, int D, cudaStream_t s) {
