@@ -23,20 +23,21 @@ namespace tt {
 namespace tok {
 namespace {
 
+constexpr int C = 32;                        // tokens of a window
+constexpr int TT = C / 8, TK = C / 16;       // tiles of them, products along them
 constexpr int GROUP = 128;                   // threads of a group: the chain, out, the inverse, A
 constexpr int THREADS = 4 * GROUP;
 enum { CHAIN = 0, OUT = 1, INVERSE = 2, SYSTEM = 3 };
 
-template <typename T_, int D_, int C_, int NS_>
+template <typename T_, int D_, int NS_>
 struct Shape {
   using T = T_;
-  static constexpr int D = D_, C = C_, NS = NS_;
+  static constexpr int D = D_, NS = NS_;
   static constexpr int TERMS = sizeof(T) == 2 ? 1 : 3;       // of queries and keys
   static constexpr int SEEN = sizeof(T) == 2 ? 2 : 3;        // of S, U and P in out
   static constexpr int KS = D / 16;                          // products along a key
   static constexpr int NT = D / 32;                          // tiles of 8 keys' elements of the state to a warp
   static constexpr int SK = NT > 1 ? NT / 2 : 1;             // products along those
-  static constexpr int TT = C / 8, TK = C / 16;              // tiles of tokens, products along them
   static constexpr int COLS = 16 * NS;
   static constexpr int KP = D + 8, AP = C + 4, VP = COLS + 16 / (int)sizeof(T), QP = TERMS == 1 ? D + 8 : D + 4;   // pitches
   static constexpr int TILE = C * KP;                        // bf16 elements of one term of a window's keys
@@ -44,11 +45,11 @@ struct Shape {
   static constexpr int K_PLACES = TERMS == 1 ? 4 : 3, V_PLACES = 4, G_PLACES = 4;
   static constexpr int RAW = TERMS == 1 ? 0 : C * (D + 4) * 4;
   static constexpr int K = K_PLACES * TERMS * TILE * 2, Q = 2 * C * QP * (int)sizeof(T), V = V_PLACES * C * VP * (int)sizeof(T);
-  static constexpr int TRI = 2 * C * AP * 4, Y = C == 64 ? 32 * 36 * 4 : 16 * 20 * 4, INV = 2 * TT * TK * 3 * 256;
+  static constexpr int TRI = 2 * C * AP * 4, INV = 2 * TT * TK * 3 * 256;
   static constexpr int X = NS * 4 * TT * 512, R = NS * 3 * TK * 512, U = NS * 3 * TK * 512, SEEN_U = 2 * NS * SEEN * TK * 512, S = 2 * NS * SEEN * KS * 512;
   static constexpr int O = C * VP * (int)sizeof(T);
   static constexpr int GATES = G_PLACES * (5 * C + 4) * 4;
-  static constexpr int SMEM = RAW + K + Q + V + TRI + Y + INV + X + R + U + SEEN_U + S + O + GATES;
+  static constexpr int SMEM = RAW + K + Q + V + TRI + INV + X + R + U + SEEN_U + S + O + GATES;
   static constexpr bool FITS = SMEM + 1024 <= 227 * 1024;
 };
 
@@ -72,6 +73,14 @@ __device__ __forceinline__ void product(float (&acc)[4], const uint32_t (&a)[TA]
 #pragma unroll
       for (int j = 0; j < TB; ++j)
         if (i + j == sum) mma16816(acc, a[i], b[j][0], b[j][1]);
+}
+// The same for a product that the chain waits for: 35 cycles an instruction behind another of the same sums, so each size of product has its own.
+__device__ __forceinline__ void product_apart(float (&acc)[3][4], const uint32_t (&a)[3][4], const uint32_t (&b)[3][2]) {
+#pragma unroll
+  for (int i = 0; i < 3; ++i)
+#pragma unroll
+    for (int sum = 2; sum >= 0; --sum)
+      if (i <= sum) mma16816(acc[sum], a[i], b[sum - i][0], b[sum - i][1]);
 }
 __device__ __forceinline__ void load16(uint32_t (&r)[4], const uint32_t* p) {
   const uint4 v = *reinterpret_cast<const uint4*>(p);
@@ -99,7 +108,6 @@ __device__ __forceinline__ bool all_finite(uint4 v) {
   return isfinite(__uint_as_float(v.x)) && isfinite(__uint_as_float(v.y)) && isfinite(__uint_as_float(v.z)) && isfinite(__uint_as_float(v.w));
 }
 // Gates of a window's tokens.  G is a sum in 64 bits of log2(e) log_decay, kept as a pair of floats: what counts are differences of far larger sums.
-template <int C>
 struct Gates {
   float2 sum[C];                             // G
   float beta[C], up[C], down[C];             // e^G, e^(G_C - G)
@@ -107,10 +115,30 @@ struct Gates {
   int odd;                                   // something in the window's keys, values or gates is not finite
   int pad[2];
 };
+// 2^x for x of 0 and below, as pair: to half a step of the result and little more, where exp2f is off by two.  By a Taylor polynomial of e^(y ln 2), |y| <= 1/2.
+__device__ __forceinline__ float exp2_pair(float hi, float lo) {
+  if (!(hi > -150.f)) return hi == hi ? 0.f : hi;
+  const float whole = rintf(hi), y = ((hi - whole) + lo) * 0.693147181f;
+  float f = 1.f / 5040.f;
+  f = fmaf(f, y, 1.f / 720.f);
+  f = fmaf(f, y, 1.f / 120.f);
+  f = fmaf(f, y, 1.f / 24.f);
+  f = fmaf(f, y, 1.f / 6.f);
+  f = fmaf(f, y, 0.5f);
+  f = fmaf(f, y, 1.f);
+  f = fmaf(f, y, 1.f);
+  return scalbnf(f, (int)whole);
+}
+// an 8 x 8 block of pairs' terms, rows for columns
+__device__ __forceinline__ uint32_t transposed(uint32_t u) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(u));
+  return r;
+}
 __device__ __forceinline__ float fade_of(float2 to, float2 from) { return exp2_fast((to.x - from.x) + (to.y - from.y)); }
 
 // A group's rows of a window, 16 bytes to a thread and pass
-template <typename T, int ROWLEN, int C>
+template <typename T, int ROWLEN>
 struct Rows {
   static constexpr int EACH = 16 / (int)sizeof(T), ROW = ROWLEN / EACH, STEP = GROUP / ROW, PASSES = (C + STEP - 1) / STEP;
   const T* src;
@@ -141,7 +169,7 @@ struct Rows {
 template <typename H>
 __global__ void __launch_bounds__(THREADS, 1) delta_chunk_kernel(const __grid_constant__ DeltaParams p) {
   using T = typename H::T;
-  constexpr int D = H::D, C = H::C, NS = H::NS, TERMS = H::TERMS, SEEN = H::SEEN, KS = H::KS, NT = H::NT, SK = H::SK, TT = H::TT, TK = H::TK, COLS = H::COLS, KP = H::KP,
+  constexpr int D = H::D, NS = H::NS, TERMS = H::TERMS, SEEN = H::SEEN, KS = H::KS, NT = H::NT, SK = H::SK, COLS = H::COLS, KP = H::KP,
                 AP = H::AP, VP = H::VP, QP = H::QP;
   extern __shared__ __align__(16) uint8_t smem[];
   uint8_t* place = smem;
@@ -155,7 +183,6 @@ __global__ void __launch_bounds__(THREADS, 1) delta_chunk_kernel(const __grid_co
   T* queries = reinterpret_cast<T*>(room(H::Q));                             // [parity][C][QP]
   T* values = reinterpret_cast<T*>(room(H::V));                              // [place][C][VP]
   float* tri = reinterpret_cast<float*>(room(H::TRI));                       // [parity][C][AP]: A, then its inverse
-  float* y = reinterpret_cast<float*>(room(H::Y));
   uint32_t* inverse = reinterpret_cast<uint32_t*>(room(H::INV));             // [parity][tile][TK][term][lane][2]
   float* x_part = reinterpret_cast<float*>(room(H::X));                      // [run][warp][tile][lane][4]
   uint32_t* r_frag = reinterpret_cast<uint32_t*>(room(H::R));                // [run][term][TK][lane][4]
@@ -163,8 +190,8 @@ __global__ void __launch_bounds__(THREADS, 1) delta_chunk_kernel(const __grid_co
   uint32_t* u_seen = reinterpret_cast<uint32_t*>(room(H::SEEN_U));           // [parity][run][term][TK][lane][4]
   uint32_t* s_seen = reinterpret_cast<uint32_t*>(room(H::S));                // [parity][run][term][KS][lane][4]
   T* outs = reinterpret_cast<T*>(room(H::O));                                // [C][VP]
-  Gates<C>* gates = reinterpret_cast<Gates<C>*>(place);                      // [place]
-  static_assert(sizeof(Gates<C>) * H::G_PLACES == H::GATES, "gates");
+  Gates* gates = reinterpret_cast<Gates*>(place);                      // [place]
+  static_assert(sizeof(Gates) * H::G_PLACES == H::GATES, "gates");
 
   const int b = blockIdx.z, h = blockIdx.y, col0 = (int)blockIdx.x * COLS;
   const int n = clamp_length(p.lengths, b, p.tokens);
@@ -182,30 +209,25 @@ __global__ void __launch_bounds__(THREADS, 1) delta_chunk_kernel(const __grid_co
   const int64_t state = ((int64_t)slot * p.heads + h) * D * D + col0;
   auto keys_of = [&](int w) { return keys + (w % H::K_PLACES) * TERMS * H::TILE; };
   auto values_of = [&](int w) { return values + (w % H::V_PLACES) * C * VP; };
-  auto gates_of = [&](int w) -> Gates<C>& { return gates[w % H::G_PLACES]; };
+  auto gates_of = [&](int w) -> Gates& { return gates[w % H::G_PLACES]; };
 
   if (role == SYSTEM) {
     // ------------------------------------------------------------------------------- A, two windows ahead
-    const Rows<T, D, C> k_rows(k, p.k.t, tid);
-    const Rows<T, COLS, C> v_rows(v, p.v.t, tid);
+    const Rows<T, D> k_rows(k, p.k.t, tid);
+    const Rows<T, COLS> v_rows(v, p.v.t, tid);
     auto fetch = [&](int w) {
       if constexpr (TERMS == 1) k_rows.fetch(reinterpret_cast<T*>(keys_of(w)), KP, w * C, n);
       else k_rows.fetch(reinterpret_cast<T*>(raw), D + 4, w * C, n);
       v_rows.fetch(values_of(w), VP, w * C, n);
       copies_commit();
     };
-    constexpr int PER = C / 32;                  // tokens of a lane of the first warp
-    float decay[PER] = {}, beta[PER] = {};
+    float decay = 0.f, beta = 0.f;               // of a lane's token, in the first warp
     auto fetch_gates = [&](int w) {
-#pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        const int token = w * C + lane * PER + i;
-        decay[i] = beta[i] = 0.f;
-        if (token < n) {
-          if (p.log_decay) decay[i] = p.log_decay[gate0 + (int64_t)token * p.heads];
-          beta[i] = p.beta[gate0 + (int64_t)token * p.heads];
-        }
-      }
+      const int token = w * C + lane;
+      decay = beta = 0.f;
+      if (token >= n) return;
+      if (p.log_decay) decay = p.log_decay[gate0 + (int64_t)token * p.heads];
+      beta = p.beta[gate0 + (int64_t)token * p.heads];
     };
     if (windows > 0) {
       if (warp == 0) fetch_gates(0);
@@ -214,37 +236,28 @@ __global__ void __launch_bounds__(THREADS, 1) delta_chunk_kernel(const __grid_co
     for (int step = -2; step <= windows; ++step) {
       const int w = step + 2;
       if (w < windows) {
-        Gates<C>& gt = gates_of(w);
+        Gates& gt = gates_of(w);
         copies_wait();
         bool odd = !v_rows.finite(values_of(w), VP);
         if constexpr (TERMS == 1) odd |= !k_rows.finite(reinterpret_cast<const T*>(keys_of(w)), KP);
         else odd |= !k_rows.finite(reinterpret_cast<const T*>(raw), D + 4);
         if (warp == 0) {
-          double mine[PER], sum = 0.0;
-#pragma unroll
-          for (int i = 0; i < PER; ++i) {
-            odd |= !isfinite(beta[i]) || !(decay[i] < INFINITY);
-            // -infinity: all of it, like -10^5
-            sum += decay[i] < -1e5f ? -1e5 * 1.4426950408889634074 : (double)decay[i] * 1.4426950408889634074;
-            mine[i] = sum;
-          }
+          odd |= !isfinite(beta) || !(decay < INFINITY);
+          // -infinity: all of it, like -10^5
+          double sum = (decay < -1e5f ? -1e5 : (double)decay) * 1.4426950408889634074;
 #pragma unroll
           for (int d = 1; d < 32; d <<= 1) {
             const double other = __shfl_up_sync(0xffffffffu, sum, d);
             if (lane >= d) sum += other;
           }
-          const double all = __shfl_sync(0xffffffffu, sum, 31), before = sum - mine[PER - 1];
-#pragma unroll
-          for (int i = 0; i < PER; ++i) {
-            const double G = before + mine[i];
-            const int at = lane * PER + i;
-            gt.sum[at] = make_float2((float)G, (float)(G - (double)(float)G));
-            gt.beta[at] = beta[i];
-            gt.up[at] = exp2f((float)G);
-            gt.down[at] = exp2f((float)(all - G));
-          }
+          const float hi = (float)sum, lo = (float)(sum - (double)hi);
+          const float2 all = make_float2(__shfl_sync(0xffffffffu, hi, 31), __shfl_sync(0xffffffffu, lo, 31));
+          gt.sum[lane] = make_float2(hi, lo);
+          gt.beta[lane] = beta;
+          gt.up[lane] = exp2f(hi + lo);
+          gt.down[lane] = exp2f((all.x - hi) + (all.y - lo));
           // the one factor that a state meets again and again: its error would add up
-          if (lane == 31) gt.whole = (float)exp2(all);
+          if (lane == 31) gt.whole = exp2_pair(hi, lo);
         }
         odd = named_barrier_or(1 + SYSTEM, GROUP, odd);
         if (tid == 0) gt.odd = odd;
@@ -319,11 +332,11 @@ __global__ void __launch_bounds__(THREADS, 1) delta_chunk_kernel(const __grid_co
       const int w = step + 1;
       if (w >= 0 && w < windows) {
         float* A = tri + (w & 1) * C * AP;
-        // what lies beside a pair of those blocks is read as part of a block of 32
-        if (C == 64) *reinterpret_cast<float4*>(A + (warp >> 1) * 32 * (AP + 1) + (tid & 63) / 4 * AP + 16 + tid % 4 * 4) = make_float4(0.f, 0.f, 0.f, 0.f);
-        // blocks of 16 on the diagonal, a column to a lane
-        if (warp < TK) {
-          float* at = A + warp * 16 * (AP + 1);
+        uint32_t* to = inverse + (w & 1) * TT * TK * 3 * 64;
+        auto put = [&](int tile, int x, int e, uint32_t b0, uint32_t b1) { *reinterpret_cast<uint2*>(to + (((tile * TK + x) * 3 + e) * 32 + lane) * 2) = make_uint2(b0, b1); };
+        // the two blocks of 16 on the diagonal, a column to a lane
+        float* block = A + warp * 16 * (AP + 1);
+        if (warp < 2) {
           const int j = lane & 15;
           float x[16];
 #pragma unroll
@@ -331,70 +344,88 @@ __global__ void __launch_bounds__(THREADS, 1) delta_chunk_kernel(const __grid_co
             float a[16];
 #pragma unroll
             for (int m = 0; m < i; m += 4) {
-              const float4 f = *reinterpret_cast<const float4*>(at + i * AP + m);
+              const float4 f = *reinterpret_cast<const float4*>(block + i * AP + m);
               a[m] = f.x; a[m + 1] = f.y; a[m + 2] = f.z; a[m + 3] = f.w;
             }
-            float sum = i == j ? 1.f : 0.f;
+            float sum = i == j ? 1.f : 0.f, other = 0.f;      // two chains
 #pragma unroll
-            for (int m = 0; m < i; ++m) sum = fmaf(-a[m], x[m], sum);
-            x[i] = sum;
+            for (int m = 0; m < i; ++m)
+              if (m & 1) other = fmaf(-a[m], x[m], other);
+              else sum = fmaf(-a[m], x[m], sum);
+            x[i] = sum + other;
           }
           __syncwarp();
           if (lane < 16)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) at[i * AP + j] = x[i];
+            for (int i = 0; i < 16; ++i) block[i * AP + j] = x[i];
         }
         barrier(1 + INVERSE);
-        // what lies below a pair of blocks: -T_11 (A_10 T_00); blocks of 16, then of 32
-        auto below = [&](float* block, int m, const float* left, int left_pitch, const float* right, int right_pitch, float* to, int to_pitch, float sign, int r0, int rows, int c) {
-#pragma unroll 2
-          for (int r = r0; r < r0 + rows; ++r) {
-            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int e = 0; e < m; e += 4) {
-              const float4 a = *reinterpret_cast<const float4*>(left + r * left_pitch + e);
+        if (warp < 2) {
+          // as the second operand's registers of U's product
 #pragma unroll
-              for (int z = 0; z < 4; ++z) {
-                const float f = z == 0 ? a.x : z == 1 ? a.y : z == 2 ? a.z : a.w;
-                const float4 x = *reinterpret_cast<const float4*>(right + (e + z) * right_pitch + c);
-                sum = make_float4(fmaf(f, x.x, sum.x), fmaf(f, x.y, sum.y), fmaf(f, x.z, sum.z), fmaf(f, x.w, sum.w));
-              }
+          for (int i = 0; i < 2; ++i) {
+            uint32_t terms[2][3];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float2 f = *reinterpret_cast<const float2*>(block + (8 * i + g) * AP + 8 * e + 2 * t);
+              cut(f.x, f.y, terms[e]);
             }
-            *reinterpret_cast<float4*>(to + r * to_pitch + c) = make_float4(sign * sum.x, sign * sum.y, sign * sum.z, sign * sum.w);
-          }
-        };
-        {
-          // a pair of blocks to two warps, or (one pair) to all four
-          const int pair = C == 64 ? warp >> 1 : 0, at = C == 64 ? tid & 63 : tid;
-          float* top = A + pair * 32 * (AP + 1);
-          float* bottom = top + 16 * AP;
-          float* part = y + pair * 16 * 20;
-          const int c = at % 4 * 4, r = at / 4;
-          if (r < 16) below(top, 16, bottom, AP, top, AP, part, 20, 1.f, r, 1, c);
-          barrier(1 + INVERSE);
-          if (r < 16) below(top, 16, bottom + 16, AP, part, 20, bottom, AP, -1.f, r, 1, c);
-          barrier(1 + INVERSE);
-        }
-        if constexpr (C == 64) {
-          float* bottom = A + 32 * AP;
-          const int c = tid % 8 * 4, r = tid / 8 * 2;
-          below(A, 32, bottom, AP, A, AP, y, 36, 1.f, r, 2, c);
-          barrier(1 + INVERSE);
-          below(A, 32, bottom + 32, AP, y, 36, bottom, AP, -1.f, r, 2, c);
-          barrier(1 + INVERSE);
-        }
-        // as the second operand's registers
-        uint32_t* to = inverse + (w & 1) * TT * TK * 3 * 64;
-        for (int i = warp; i < TT * TK; i += 4) {
-          const int tile = i / TK, x = i % TK;
-          if (x > tile / 2) continue;
-          uint32_t terms[2][3];
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float2 f = *reinterpret_cast<const float2*>(A + (8 * tile + g) * AP + 16 * x + 8 * e + 2 * t);
-            cut(f.x, f.y, terms[e]);
+            for (int e = 0; e < 3; ++e) put(2 * warp + i, warp, e, terms[0][e], terms[1][e]);
           }
+        } else if (warp == 2) {
+          // the block below, -T_11 A_10 T_00, transposed as the chain is: (T_00^T A_10^T) T_11^T
+          uint32_t a[3][4], f[2][3][2];
 #pragma unroll
-          for (int e = 0; e < 3; ++e) *reinterpret_cast<uint2*>(to + ((i * 3 + e) * 32 + lane) * 2) = make_uint2(terms[0][e], terms[1][e]);
+          for (int e = 0; e < 4; ++e) {
+            uint32_t terms[3];
+            const float* from = A + (2 * t + 8 * (e >> 1)) * AP + g + 8 * (e & 1);
+            cut(from[0], from[AP], terms);
+#pragma unroll
+            for (int c = 0; c < 3; ++c) a[c][e] = terms[c];
+          }
+          auto second = [&](const float* rows) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                uint32_t terms[3];
+                const float2 x = *reinterpret_cast<const float2*>(rows + (8 * i + g) * AP + 8 * e + 2 * t);
+                cut(x.x, x.y, terms);
+#pragma unroll
+                for (int c = 0; c < 3; ++c) f[i][c][e] = terms[c];
+              }
+          };
+          float sums[2][3][4];
+          auto multiply = [&](float sign) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+#pragma unroll
+              for (int c = 0; c < 3; ++c) sums[i][c][0] = sums[i][c][1] = sums[i][c][2] = sums[i][c][3] = 0.f;
+              product_apart(sums[i], a, f[i]);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) sums[i][0][e] = sign * (sums[i][0][e] + (sums[i][1][e] + sums[i][2][e]));
+            }
+          };
+          second(A + 16 * AP);
+          multiply(1.f);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            uint32_t terms[3];
+            cut(sums[e >> 1][0][2 * (e & 1)], sums[e >> 1][0][2 * (e & 1) + 1], terms);
+#pragma unroll
+            for (int c = 0; c < 3; ++c) a[c][e] = terms[c];
+          }
+          second(A + 16 * (AP + 1));
+          multiply(-1.f);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            uint32_t low[3], high[3];
+            cut(sums[i][0][0], sums[i][0][1], low);
+            cut(sums[i][0][2], sums[i][0][3], high);
+#pragma unroll
+            for (int e = 0; e < 3; ++e) put(2 + i, 0, e, transposed(low[e]), transposed(high[e]));
+          }
         }
       }
       __syncthreads();
@@ -405,7 +436,7 @@ __global__ void __launch_bounds__(THREADS, 1) delta_chunk_kernel(const __grid_co
     constexpr int SHARE = 4 / TK, MINE = (NS + SHARE - 1) / SHARE;
     constexpr int EACH = 16 / (int)sizeof(T);
     const int strip = warp % TK, first = warp / TK, i0 = 16 * strip;
-    const Rows<T, D, C> q_rows(q, p.q.t, tid);
+    const Rows<T, D> q_rows(q, p.q.t, tid);
     float acc[MINE][2][4];               // columns of values 16 x g and + 8, tokens 8 e + 2 t and + 1 of the strip
     uint32_t weights[TK][2][SEEN][2];
     for (int step = -2; step <= windows; ++step) {
@@ -449,7 +480,7 @@ __global__ void __launch_bounds__(THREADS, 1) delta_chunk_kernel(const __grid_co
         const int w = step;
         const T* qs = queries + (w & 1) * C * QP;
         const __nv_bfloat16* ks = keys_of(w);
-        const Gates<C>& gt = gates_of(w);
+        const Gates& gt = gates_of(w);
         float dots[TT][4];
 #pragma unroll
         for (int i = 0; i < TT; ++i) dots[i][0] = dots[i][1] = dots[i][2] = dots[i][3] = 0.f;
@@ -598,106 +629,87 @@ __global__ void __launch_bounds__(THREADS, 1) delta_chunk_kernel(const __grid_co
         }
       }
     };
-    constexpr int MINE = TT / 4;           // tiles of tokens whose R and U are this warp's: one near either end, for theirs are long and short sums
     auto advance = [&](int w) {
       const __nv_bfloat16* ks = keys_of(w);
       const T* vs = values_of(w);
-      const Gates<C>& gt = gates_of(w);
-      const uint32_t* inv = inverse + (w & 1) * TT * TK * 3 * 64;
-      float2 down[MINE];
+      const Gates& gt = gates_of(w);
+      // R, U: of tokens 8 warp .. 8 warp + 7, whose sums over tokens reach up to them
+      const int token = 8 * warp + 2 * t;
+      const bool both = warp >= 2;
+      uint32_t inv[2][3][2];
 #pragma unroll
-      for (int m = 0; m < MINE; ++m) {
-        const int tile = m == 0 ? warp : TT - 1 - warp, token = 8 * tile + 2 * t;
-        const float2 beta = *reinterpret_cast<const float2*>(gt.beta + token), up = *reinterpret_cast<const float2*>(gt.up + token);
-        down[m] = *reinterpret_cast<const float2*>(gt.down + token);
+      for (int x = 0; x < 2; ++x)
+        if (x == 0 || both)
 #pragma unroll
-        for (int i = 0; i < NS; ++i) {
-          float4 x[4];
+          for (int e = 0; e < 3; ++e) {
+            const uint2 z = *reinterpret_cast<const uint2*>(inverse + ((((w & 1) * TT + warp) * TK + x) * 3 + e) * 64 + lane * 2);
+            inv[x][e][0] = z.x; inv[x][e][1] = z.y;
+          }
+      const float2 beta = *reinterpret_cast<const float2*>(gt.beta + token), up = *reinterpret_cast<const float2*>(gt.up + token),
+                   down = *reinterpret_cast<const float2*>(gt.down + token);
+      const float whole = gt.whole;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x[e] = *reinterpret_cast<const float4*>(x_part + ((i * 4 + e) * TT + tile) * 128 + lane * 4);
-          const T* vv = vs + token * VP + 16 * i + g;
-          float r[4];
-          r[0] = beta.x * fmaf(-up.x, (x[0].x + x[1].x) + (x[2].x + x[3].x), to_float(vv[0]));
-          r[1] = beta.y * fmaf(-up.y, (x[0].y + x[1].y) + (x[2].y + x[3].y), to_float(vv[VP]));
-          r[2] = beta.x * fmaf(-up.x, (x[0].z + x[1].z) + (x[2].z + x[3].z), to_float(vv[8]));
-          r[3] = beta.y * fmaf(-up.y, (x[0].w + x[1].w) + (x[2].w + x[3].w), to_float(vv[VP + 8]));
-          keep<3>(r_frag + i * 3 * TK * 128, TK * 128, lane, tile, r);
-        }
+      for (int i = 0; i < NS; ++i) {
+        float4 x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = *reinterpret_cast<const float4*>(x_part + ((i * 4 + e) * TT + warp) * 128 + lane * 4);
+        const T* vv = vs + token * VP + 16 * i + g;
+        float r[4];
+        r[0] = beta.x * fmaf(-up.x, (x[0].x + x[1].x) + (x[2].x + x[3].x), to_float(vv[0]));
+        r[1] = beta.y * fmaf(-up.y, (x[0].y + x[1].y) + (x[2].y + x[3].y), to_float(vv[VP]));
+        r[2] = beta.x * fmaf(-up.x, (x[0].z + x[1].z) + (x[2].z + x[3].z), to_float(vv[8]));
+        r[3] = beta.y * fmaf(-up.y, (x[0].w + x[1].w) + (x[2].w + x[3].w), to_float(vv[VP + 8]));
+        keep<3>(r_frag + i * 3 * TK * 128, TK * 128, lane, warp, r);
       }
       barrier(1 + CHAIN);
       // U^T = R^T T^T
 #pragma unroll
       for (int i = 0; i < NS; ++i) {
-        float u[MINE][2][4];
+        float u[2][3][4];
 #pragma unroll
-        for (int m = 0; m < MINE; ++m)
+        for (int x = 0; x < 2; ++x) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) u[m][0][e] = u[m][1][e] = 0.f;
-#pragma unroll
-        for (int x = 0; x < TK; ++x) {
-          uint32_t a[3][4];
-          if (x <= (MINE == 1 ? warp : TT - 1 - warp) / 2) {
+          for (int e = 0; e < 3; ++e) u[x][e][0] = u[x][e][1] = u[x][e][2] = u[x][e][3] = 0.f;
+          if (x == 0 || both) {
+            uint32_t a[3][4];
 #pragma unroll
             for (int e = 0; e < 3; ++e) load16(a[e], r_frag + ((i * 3 + e) * TK + x) * 128 + lane * 4);
-          }
-#pragma unroll
-          for (int m = 0; m < MINE; ++m) {
-            const int tile = m == 0 ? warp : TT - 1 - warp;
-            if (x <= tile / 2) {
-              uint32_t f[3][2];
-#pragma unroll
-              for (int e = 0; e < 3; ++e) {
-                const uint2 z = *reinterpret_cast<const uint2*>(inv + (((tile * TK + x) * 3 + e) * 32 + lane) * 2);
-                f[e][0] = z.x; f[e][1] = z.y;
-              }
-              product(u[m][x & 1], a, f);
-            }
+            product_apart(u[x], a, inv[x]);
           }
         }
+        float sum[4];
 #pragma unroll
-        for (int m = 0; m < MINE; ++m) {
-          const int tile = m == 0 ? warp : TT - 1 - warp;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) u[m][0][e] += u[m][1][e];
-          keep<SEEN>(u_seen + ((w & 1) * NS + i) * SEEN * TK * 128, TK * 128, lane, tile, u[m][0]);
-          u[m][0][0] *= down[m].x; u[m][0][1] *= down[m].y; u[m][0][2] *= down[m].x; u[m][0][3] *= down[m].y;
-          keep<3>(u_frag + i * 3 * TK * 128, TK * 128, lane, tile, u[m][0]);
-        }
+        for (int e = 0; e < 4; ++e) sum[e] = (u[0][0][e] + u[1][0][e]) + ((u[0][1][e] + u[1][1][e]) + (u[0][2][e] + u[1][2][e]));
+        const float faded[4] = {sum[0] * down.x, sum[1] * down.y, sum[2] * down.x, sum[3] * down.y};
+        keep<3>(u_frag + i * 3 * TK * 128, TK * 128, lane, warp, faded);
+        keep<SEEN>(u_seen + ((w & 1) * NS + i) * SEEN * TK * 128, TK * 128, lane, warp, sum);
       }
+      uint32_t kf[NT][2][TERMS][2];
+#pragma unroll
+      for (int m = 0; m < NT; ++m)
+#pragma unroll
+        for (int e = 0; e < TERMS; ++e) {
+          uint32_t f[4];
+          ldmatrix4<true>(f, smem_u32(ks + e * H::TILE + lane * KP + (warp * NT + m) * 8));
+          kf[m][0][e][0] = f[0]; kf[m][0][e][1] = f[1]; kf[m][1][e][0] = f[2]; kf[m][1][e][1] = f[3];
+        }
       barrier(1 + CHAIN);
       // S'^T = e^G_C S^T + U'^T K
-      const float whole = gt.whole;
 #pragma unroll
       for (int i = 0; i < NS; ++i) {
-        float d[NT][2][4];
+        uint32_t a[2][3][4];
 #pragma unroll
-        for (int m = 0; m < NT; ++m)
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) d[m][0][e] = d[m][1][e] = 0.f;
+          for (int e = 0; e < 3; ++e) load16(a[x][e], u_frag + ((i * 3 + e) * TK + x) * 128 + lane * 4);
 #pragma unroll
-        for (int x = 0; x < TK; x += 2) {
-          uint32_t a[2][3][4];
+        for (int m = 0; m < NT; ++m) {
+          float d[2][4] = {};
+          product(d[0], a[0], kf[m][0]);
+          product(d[1], a[1], kf[m][1]);
 #pragma unroll
-          for (int z = 0; z < 2; ++z)
-#pragma unroll
-            for (int e = 0; e < 3; ++e) load16(a[z][e], u_frag + ((i * 3 + e) * TK + x + z) * 128 + lane * 4);
-#pragma unroll
-          for (int m = 0; m < NT; ++m) {
-            uint32_t one[TERMS][2], two[TERMS][2];
-#pragma unroll
-            for (int e = 0; e < TERMS; ++e) {
-              uint32_t f[4];
-              ldmatrix4<true>(f, smem_u32(ks + e * H::TILE + (16 * x + lane) * KP + (warp * NT + m) * 8));
-              one[e][0] = f[0]; one[e][1] = f[1]; two[e][0] = f[2]; two[e][1] = f[3];
-            }
-            product(d[m][0], a[0], one);
-            product(d[m][1], a[1], two);
-          }
+          for (int e = 0; e < 4; ++e) s[i][m][e] = fmaf(whole, s[i][m][e], d[0][e] + d[1][e]);
         }
-#pragma unroll
-        for (int m = 0; m < NT; ++m)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[i][m][e] = fmaf(whole, s[i][m][e], d[m][0][e] + d[m][1][e]);
       }
     };
     // A window with something in it that is not finite, token by token, a value column to a thread: the weights of 0 that a window's products give earlier tokens would
@@ -765,11 +777,9 @@ cudaError_t launch_shape(const DeltaParams& p, cudaStream_t s) {
 template <typename T, int D>
 cudaError_t launch(const DeltaParams& p, cudaStream_t s) {
   const int64_t runs = (int64_t)p.batch * p.heads * (D / 16);
-  if constexpr (Shape<T, D, 64, 1>::FITS)
-    if (runs <= PLAN_SMS) return launch_shape<Shape<T, D, 64, 1>>(p, s);
-  if constexpr (Shape<T, D, 32, 2>::FITS)
-    if (runs > 2 * PLAN_SMS) return launch_shape<Shape<T, D, 32, 2>>(p, s);
-  return launch_shape<Shape<T, D, 32, 1>>(p, s);
+  if constexpr (Shape<T, D, 2>::FITS)
+    if (runs > 2 * PLAN_SMS) return launch_shape<Shape<T, D, 2>>(p, s);
+  return launch_shape<Shape<T, D, 1>>(p, s);
 }
 template <typename T>
 cudaError_t launch(const DeltaParams& p, int D, cudaStream_t s) {
