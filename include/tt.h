@@ -542,7 +542,7 @@ tt_status tt_linear_attention(const tt_linear_attention_args* args, void* cuda_s
  * Keys are usually of length 1 (tt_qk_norm_rope with weights of 1 / sqrt(head_dim)) and beta between 0 and 1; where beta |k|^2 is above 2 the rule diverges.
  * qk_heads divides heads: head h, with its own values, gates, state and output, uses query and key head h / (heads / qk_heads).
  * log_decay, beta: device fp32 [batch][tokens][heads], contiguous; log_decay is 0 or below (-infinity: a state that was finite is forgotten), NULL: no decay.
- * state, state_out, num_slots, slots, lengths: as in tt_linear_attention.
+ * state, state_out, num_slots, slots, lengths, scratch: as in tt_linear_attention.
  * An infinity or NaN in a token or a state makes the elements of the state and of out that read it not finite, from its token on; earlier tokens, other columns of
  * values and other heads see nothing of it.
  */
@@ -559,7 +559,10 @@ typedef struct {
   float* state_out;
   const int32_t* slots;
   const int32_t* lengths;
+  void* scratch;
+  uint64_t scratch_bytes;
 } tt_delta_rule_args;
+uint64_t tt_delta_rule_scratch_bytes(const tt_delta_rule_args* args);   /* 0 also for arguments that the call refuses */
 tt_status tt_delta_rule(const tt_delta_rule_args* args, void* cuda_stream);
 
 /*

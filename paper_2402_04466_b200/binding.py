@@ -36,7 +36,7 @@ EXPORTED_SYMBOLS = [
     "tt_sched_complete", "tt_sched_predict_ms", "tt_sched_stats",
     "tt_preprocess", "tt_postprocess_scratch_bytes", "tt_postprocess", "tt_postprocess_static", "tt_overlay", "tt_render_layers",
     "tt_qk_norm_rope", "tt_rope_frequencies", "tt_linear_attention", "tt_linear_attention_scratch_bytes",
-    "tt_delta_rule", "tt_cross_attention", "tt_cross_attention_scratch_bytes",
+    "tt_delta_rule", "tt_delta_rule_scratch_bytes", "tt_cross_attention", "tt_cross_attention_scratch_bytes",
     "tt_differential_attention", "tt_differential_attention_scratch_bytes",
 ]
 TT_POSTPROCESS_STATIC_SCRATCH_BYTES = 32 << 10
@@ -73,7 +73,7 @@ class tt_delta_rule_args(C.Structure):
     _fields_ = [("struct_size", C.c_uint32)] + [(n, C.c_int32) for n in (
         "precision", "batch", "tokens", "heads", "qk_heads", "head_dim", "num_slots")] + [
         ("scale", C.c_float), ("reserved_", C.c_int32)] + [(n, tt_tokens) for n in ("q", "k", "v", "out")] + [
-        (n, C.c_void_p) for n in ("log_decay", "beta", "state", "state_out", "slots", "lengths")]
+        (n, C.c_void_p) for n in ("log_decay", "beta", "state", "state_out", "slots", "lengths", "scratch")] + [("scratch_bytes", C.c_uint64)]
 
 
 class tt_cross_attention_args(C.Structure):
@@ -191,8 +191,7 @@ def load_library(build_if_missing: bool = True) -> C.CDLL:
     lib.tt_render_layers.argtypes = [vp, i32, i64, i32, i32, i32, vp, i32, i32, i32, vp, i32, i32, vp, vp]
     lib.tt_qk_norm_rope.argtypes = [vp, vp]
     lib.tt_rope_frequencies.argtypes = [i32, C.c_double, i32, C.c_double, C.c_double, C.c_double, C.c_double, vp, C.POINTER(f32)]
-    lib.tt_delta_rule.argtypes = [vp, vp]
-    for name in ("tt_linear_attention", "tt_cross_attention", "tt_differential_attention"):
+    for name in ("tt_linear_attention", "tt_delta_rule", "tt_cross_attention", "tt_differential_attention"):
         getattr(lib, name).argtypes = [vp, vp]
         getattr(lib, name + "_scratch_bytes").argtypes = [vp]
         getattr(lib, name + "_scratch_bytes").restype = C.c_uint64
@@ -652,7 +651,7 @@ TT_ROPE_SCALING = {"plain": 0, "linear": 1, "base": 2, "by_parts": 3}
 # the argument structures as one packed string each: a ctypes.Structure filled field by field costs 5 us of a call, this 1 us
 _ROPE_ARGS = struct.Struct("@I9i2f" + 4 * "Pqqq" + "PPPqPP")
 _LINEAR_ARGS = struct.Struct("@I7ifi" + 4 * "Pqqq" + "PPPPPPPQ")
-_DELTA_ARGS = struct.Struct("@I7ifi" + 4 * "Pqqq" + "PPPPPP")
+_DELTA_ARGS = struct.Struct("@I7ifi" + 4 * "Pqqq" + "PPPPPPPQ")
 _CROSS_ARGS = struct.Struct("@I7ifi" + 4 * "Pqqq" + "PPPqqPPQ")
 _DIFF_ARGS = struct.Struct("@I7i4f2i" + 4 * "Pqqq" + "PqPPPPqqPPQ")
 _SCRATCH = struct.Struct("@PQ")      # the last two members of those that may need it
@@ -873,7 +872,11 @@ def delta_rule(q, k, v, log_decay, beta, state, scale: float = 1.0, slots=None, 
     args = _DELTA_ARGS.pack(_DELTA_ARGS.size, prec, B, T, H, Hk, D, n, scale, 0, *views, _array("log_decay", log_decay, th.f32, device, gates),
                             _array("beta", beta, th.f32, device, gates), _array("state", state, th.f32, device, states),
                             _array("state_out", state_out, th.f32, device, states), _array("slots", slots, th.i32, device, (B,)),
-                            _array("lengths", lengths, th.i32, device, (B,)))
+                            _array("lengths", lengths, th.i32, device, (B,)), 0, 0)
+    room = lib.tt_delta_rule_scratch_bytes(args) if T > 1 else 0
+    if room:
+        buf = th.empty(room, dtype=th.u8, device=q.device)
+        args = args[:-16] + _SCRATCH.pack(buf.data_ptr(), room)
     st = lib.tt_delta_rule(args, th.current_stream(device))
     if st:
         _check(lib, st)

@@ -63,9 +63,13 @@ struct alignas(32) DeltaParams {
   int32_t batch, tokens, heads, group;     // group: heads to a query and key head
   int32_t num_slots;
   float scale;
+  int32_t first_window, windows;           // of several tokens: windows first_window .. + windows - 1 of every sequence, in order
+  void* records;                           // [batch][heads][windows]: DeltaRecord
 };
 cudaError_t launch_delta_step(const DeltaParams& p, bool bf16, int D, cudaStream_t s);      // token by token
-cudaError_t launch_delta_chunk(const DeltaParams& p, bool bf16, int D, cudaStream_t s);     // a window of tokens at a time
+cudaError_t launch_delta_prepare(const DeltaParams& p, bool bf16, int D, cudaStream_t s);   // of every window, what depends on no state
+cudaError_t launch_delta_chunk(DeltaParams p, bool bf16, int D, cudaStream_t s);            // a window of tokens at a time, prepared range by range
+uint64_t delta_scratch(int batch, int tokens, int heads, bool bf16);
 
 struct alignas(32) CrossParams {
   View q, k, v, o;

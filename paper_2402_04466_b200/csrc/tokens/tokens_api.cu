@@ -168,8 +168,7 @@ tt_status tt_linear_attention(const tt_linear_attention_args* a, void* cuda_stre
   return e == cudaSuccess ? TT_OK : set_error(TT_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
 }
 
-tt_status tt_delta_rule(const tt_delta_rule_args* a, void* cuda_stream) {
-  const char* who = "tt_delta_rule";
+static tt_status check_delta(const char* who, const tt_delta_rule_args* a) {
   if (!a || a->struct_size != sizeof(*a)) return set_error(TT_ERR_INVALID_ARG, "%s: struct_size", who);
   if ((a->precision != TT_FP32 && a->precision != TT_BF16) || !extent(a->batch, 1, 65535) || !extent(a->tokens, 0, MAX_EXTENT) ||
       !extent(a->heads, 1, 4096) || !extent(a->qk_heads, 1, a->heads) || a->heads % a->qk_heads || !extent(a->num_slots, 1, MAX_EXTENT) ||
@@ -177,6 +176,18 @@ tt_status tt_delta_rule(const tt_delta_rule_args* a, void* cuda_stream) {
     return set_error(TT_ERR_INVALID_ARG, "%s: bad argument", who);
   if (bad_head_dim(who, a->head_dim)) return TT_ERR_UNSUPPORTED;
   if (!a->slots && a->batch > a->num_slots) return set_error(TT_ERR_INVALID_ARG, "%s: more entries than slots", who);
+  return TT_OK;
+}
+
+uint64_t tt_delta_rule_scratch_bytes(const tt_delta_rule_args* a) {
+  if (check_delta("tt_delta_rule_scratch_bytes", a) != TT_OK || a->tokens <= 1) return 0;
+  return delta_scratch(a->batch, a->tokens, a->heads, a->precision == TT_BF16);
+}
+
+tt_status tt_delta_rule(const tt_delta_rule_args* a, void* cuda_stream) {
+  const char* who = "tt_delta_rule";
+  const tt_status st = check_delta(who, a);
+  if (st != TT_OK) return st;
   const bool bf16 = a->precision == TT_BF16;
   const int size = bf16 ? 2 : 4;
   if (bad_view(who, "q", a->q, a->batch, a->tokens, a->qk_heads, size) || bad_view(who, "k", a->k, a->batch, a->tokens, a->qk_heads, size) ||
@@ -186,12 +197,15 @@ tt_status tt_delta_rule(const tt_delta_rule_args* a, void* cuda_stream) {
   if ((a->tokens && !a->beta) || !a->state || !a->state_out || misaligned(a->log_decay, 4) || misaligned(a->beta, 4) || misaligned(a->state, 16) ||
       misaligned(a->state_out, 16) || misaligned(a->slots, 4) || misaligned(a->lengths, 4))
     return set_error(TT_ERR_INVALID_ARG, "%s: beta, state or state_out is null, or a pointer is misaligned (states: 16 bytes)", who);
+  const uint64_t need = tt_delta_rule_scratch_bytes(a);
+  if (need && (!a->scratch || misaligned(a->scratch, 16) || a->scratch_bytes < need))
+    return set_error(TT_ERR_INVALID_ARG, "%s: scratch is null, misaligned or smaller than %llu bytes", who, (unsigned long long)need);
   DeltaParams p{};
   p.q = view(a->q, a->batch, a->tokens, a->qk_heads); p.k = view(a->k, a->batch, a->tokens, a->qk_heads);
   p.v = view(a->v, a->batch, a->tokens, a->heads); p.o = view(a->out, a->batch, a->tokens, a->heads);
   p.log_decay = a->log_decay; p.beta = a->beta; p.state = a->state; p.state_out = a->state_out; p.slots = a->slots; p.lengths = a->lengths;
   p.batch = a->batch; p.tokens = a->tokens; p.heads = a->heads; p.group = a->heads / a->qk_heads; p.num_slots = a->num_slots;
-  p.scale = a->scale;
+  p.scale = a->scale; p.records = a->scratch;
   const cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
   const cudaError_t e = a->tokens > 1 ? launch_delta_chunk(p, bf16, a->head_dim, s) : launch_delta_step(p, bf16, a->head_dim, s);
   return e == cudaSuccess ? TT_OK : set_error(TT_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));

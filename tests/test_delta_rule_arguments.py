@@ -34,7 +34,7 @@ def _view(at, B, T, H, D):
 def _delta(**over):
     B, T, H, K, D = 2, 3, 4, 2, 64
     a = S(C.sizeof(S), 1, B, T, H, K, D, 5, 0.125, 0, _view(A, B, T, K, D), _view(A + 0x10000, B, T, K, D), _view(A + 0x20000, B, T, H, D),
-          _view(A + 0x30000, B, T, H, D), A, A, A, A, None, None)
+          _view(A + 0x30000, B, T, H, D), A, A, A, A, None, None, A, 1 << 40)
     for name, value in over.items():
         at, part = (getattr(a, name.split("__")[0]), name.split("__")[1]) if "__" in name else (a, name)
         setattr(at, part, value)
@@ -46,7 +46,8 @@ def _delta(**over):
     dict(heads=8192, qk_heads=8192), dict(num_slots=0), dict(num_slots=1), dict(scale=math.nan), dict(scale=math.inf), dict(q__data=None), dict(q__data=A + 8),
     dict(k__data=A + 2), dict(v__data=None), dict(out__data=A + 4), dict(q__token_stride=4), dict(k__head_stride=1), dict(v__batch_stride=-64),
     dict(v__token_stride=1 << 50), dict(k__token_stride=0), dict(out__batch_stride=0), dict(out__head_stride=32), dict(beta=None), dict(beta=A + 2),
-    dict(log_decay=A + 1), dict(state=None), dict(state_out=None), dict(state=A + 4), dict(state_out=A + 8), dict(slots=A + 2), dict(lengths=A + 1)])
+    dict(log_decay=A + 1), dict(state=None), dict(state_out=None), dict(state=A + 4), dict(state_out=A + 8), dict(slots=A + 2), dict(lengths=A + 1), dict(scratch=None),
+    dict(scratch=A + 8), dict(scratch_bytes=64)])
 def test_refusals(over):
     lib = binding.load_library()
     assert lib.tt_delta_rule(C.byref(_delta(**over)), None) == 1
