@@ -25,13 +25,15 @@ struct DeltaRecord {
 };
 __host__ __device__ constexpr int delta_place(int tile, int x) { return tile < 2 ? tile : 2 * tile - 2 + x; }
 
-// a pair as three bf16 terms; a in the lower halves
+// a pair as three bf16 terms, a in the lower halves: the upper eight bits of what is left, cut off, which for the last term is all of it
 __device__ __forceinline__ void cut(float a, float b, uint32_t (&t)[3]) {
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
-    t[i] = pack_bf16(a, b);
-    a -= __uint_as_float(t[i] << 16);
-    b -= __uint_as_float(t[i] & 0xFFFF0000u);
+    t[i] = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+    if (i < 2) {
+      a -= __uint_as_float(__float_as_uint(a) & 0xFFFF0000u);
+      b -= __uint_as_float(__float_as_uint(b) & 0xFFFF0000u);
+    }
   }
 }
 // acc += A B, A of TA terms and B of TB, small products first: what is below the last term of the longer of the two is left out
@@ -67,6 +69,8 @@ __device__ __forceinline__ void keep(uint32_t* to, int term, int lane, int n, co
 #pragma unroll
   for (int i = 0; i < TERMS; ++i) *reinterpret_cast<uint2*>(to + i * term + (n >> 1) * 128 + lane * 4 + (n & 1) * 2) = make_uint2(lo[i], hi[i]);
 }
+template <int THREADS>
+__device__ __forceinline__ void barrier_of(int id) { asm volatile("barrier.sync %0, %1;" ::"r"(id), "n"(THREADS) : "memory"); }
 __device__ __forceinline__ void copy16(void* dst, const void* src, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(there ? 16 : 0) : "memory");
 }

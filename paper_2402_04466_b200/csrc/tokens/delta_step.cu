@@ -4,6 +4,7 @@
 // between reading a state and writing it.  A block owns a run of W value columns of one head's state (the columns are
 // independent of each other), LANES = W / 4 threads to a row, in registers for the whole call.
 #include "linear_common.cuh"
+#include <cstdlib>
 
 namespace tt {
 namespace tok {
@@ -118,6 +119,10 @@ cudaError_t launch(const DeltaParams& p, cudaStream_t s) {
 template <typename T, int D>
 cudaError_t launch(const DeltaParams& p, cudaStream_t s) {
   // few states: cut each into four runs of columns, so that more multiprocessors fetch
+  const char* e = getenv("DW"); const int w = e ? atoi(e) : 0;
+  if (w == 1) return launch<T, D, D>(p, s);
+  if (w == 2) return launch<T, D, D / 2>(p, s);
+  if (w == 4) return launch<T, D, D / 4>(p, s);
   return (int64_t)p.batch * p.heads < 2 * PLAN_SMS ? launch<T, D, D / 4>(p, s) : launch<T, D, D>(p, s);
 }
 template <typename T>
