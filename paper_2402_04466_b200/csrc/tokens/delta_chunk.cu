@@ -15,7 +15,6 @@
 // products those of 2^-16 and more count.  Only what out alone reads is rounded further: in bf16 calls S, U and P count with 16 bits.  (P rounded
 // to bf16 once is not enough: of keys that repeat the corrections are many times larger than what is left of their sum.)
 #include "delta_common.cuh"
-#include <cstdlib>
 
 namespace tt {
 namespace tok {
@@ -23,19 +22,19 @@ namespace {
 
 constexpr int C = DELTA_C, TT = DELTA_TT, TK = DELTA_TK, GROUP = DELTA_GROUP;
 
-// G warps of the chain and OG of out to a run, RUNS runs to a block
-template <typename T_, int D_, int G_, int OG_, int RUNS_>
+// G warps to a run, RUNS runs to a block
+template <typename T_, int D_, int G_, int RUNS_>
 struct Shape {
   using T = T_;
-  static constexpr int D = D_, G = G_, OG = OG_, RUNS = RUNS_;
+  static constexpr int D = D_, G = G_, RUNS = RUNS_;
   static constexpr int TERMS = sizeof(T) == 2 ? 1 : 3;       // of keys
   static constexpr int SEEN = sizeof(T) == 2 ? 2 : 3;        // of S, U and P in out
-  using Record = DeltaRecord<SEEN, false>;
-  static constexpr int CHAIN = G * RUNS, OUT = OG * RUNS;    // warps
-  static constexpr int THREADS = (CHAIN + OUT) * 32 + GROUP;
+  using Record = DeltaRecord<SEEN>;
+  static constexpr int CHAIN = G * RUNS;                     // warps of the chain, and of out
+  static constexpr int THREADS = 2 * CHAIN * 32 + GROUP;
   static constexpr int KS = D / 16;                          // products along a key
   static constexpr int SK = KS / G, NT = 2 * SK;             // of them a warp's, and its tiles of 8 keys' elements of the state
-  static constexpr int MINE = TT / G, OUT_MINE = TT / OG;    // tiles of tokens of a warp
+  static constexpr int MINE = TT / G;                        // tiles of tokens of a warp
   static constexpr int COLS = 16 * RUNS;
   static constexpr int KP = D + 8, VP = COLS + 16 / (int)sizeof(T), QP = TERMS == 1 ? D + 8 : D + 4, OP = 16 + 16 / (int)sizeof(T);   // pitches
   static constexpr int TILE = C * KP;                        // bf16 elements of one term of a window's keys
@@ -55,12 +54,11 @@ template <typename H>
 __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid_constant__ DeltaParams p) {
   using T = typename H::T;
   using Record = typename H::Record;
-  constexpr int D = H::D, G = H::G, OG = H::OG, RUNS = H::RUNS, TERMS = H::TERMS, SEEN = H::SEEN, KS = H::KS, SK = H::SK, NT = H::NT, MINE = H::MINE, COLS = H::COLS, KP = H::KP, VP = H::VP, QP = H::QP,
+  constexpr int D = H::D, G = H::G, RUNS = H::RUNS, TERMS = H::TERMS, SEEN = H::SEEN, KS = H::KS, SK = H::SK, NT = H::NT, MINE = H::MINE, COLS = H::COLS, KP = H::KP, VP = H::VP, QP = H::QP,
                 OP = H::OP;
   constexpr int EACH = 16 / (int)sizeof(T);
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ int slow[2][RUNS];                                              // [parity]: the window was taken token by token
-  __shared__ int odd_flags[RUNS][G];
   __shared__ float shares[RUNS][G][2][16];                                   // of either sum of a token taken so
   uint8_t* place = smem;
   auto room = [&](int bytes) {
@@ -99,9 +97,9 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
   auto values_of = [&](int w) { return values + (w % H::PLACES) * C * VP; };
   auto record_of = [&](int w) -> Record& { return records[w % H::PLACES]; };
 
-  if (all_warp >= H::CHAIN + H::OUT) {
+  if (all_warp >= 2 * H::CHAIN) {
     // ------------------------------------------------------------------------------- loads
-    const int tid = threadIdx.x - (H::CHAIN + H::OUT) * 32;
+    const int tid = threadIdx.x - 2 * H::CHAIN * 32;
     const Rows<T, D> k_rows(k, p.k.t, tid), q_rows(q, p.q.t, tid);
     const Rows<T, COLS> v_rows(v, p.v.t, tid);
     const uint8_t* left = reinterpret_cast<const uint8_t*>(reinterpret_cast<const Record*>(p.records) + ((int64_t)b * p.heads + h) * p.windows);
@@ -146,8 +144,7 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
     }
   } else if (all_warp >= H::CHAIN) {
     // ------------------------------------------------------------------------------- out
-    constexpr int MINE = H::OUT_MINE;
-    const int run = (all_warp - H::CHAIN) / OG, warp = (all_warp - H::CHAIN) % OG;      // tiles of tokens warp, warp + OG, ...
+    const int run = (all_warp - H::CHAIN) / G, warp = (all_warp - H::CHAIN) % G;      // tiles of tokens warp, warp + G, ...
     T* stage = outs + run * C * OP;
     float acc[MINE][2][4];               // columns of values g and g + 8, tokens 2t and 2t + 1
     uint32_t weights[MINE][TK][SEEN][2];
@@ -162,7 +159,7 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
           for (int e = 0; e < SEEN; ++e) load16(a[x][e], u_seen + ((((w & 1) * RUNS + run) * SEEN + e) * TK + x) * 128 + lane * 4);
 #pragma unroll
         for (int m = 0; m < MINE; ++m) {
-          const int tile = warp + OG * m;
+          const int tile = warp + G * m;
 #pragma unroll
           for (int x = 0; x < TK; ++x)
             if (x <= tile / 2) product(acc[m][x], a[x], weights[m][x]);
@@ -175,7 +172,7 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
         __syncwarp();
 #pragma unroll
         for (int e = lane; e < MINE * 8 * (16 / EACH); e += 32) {
-          const int i = e / (16 / EACH), r = 8 * (warp + OG * (i / 8)) + i % 8, c = e % (16 / EACH) * EACH;
+          const int i = e / (16 / EACH), r = 8 * (warp + G * (i / 8)) + i % 8, c = e % (16 / EACH) * EACH;
           const int token = token0 + w * C + r;
           if (token < n) *reinterpret_cast<uint4*>(o + (int64_t)token * p.o.t + 16 * run + c) = *reinterpret_cast<const uint4*>(stage + r * OP + c);
         }
@@ -187,7 +184,7 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
         const Record& record = record_of(w);
 #pragma unroll
         for (int m = 0; m < MINE; ++m) {
-          const int tile = warp + OG * m;
+          const int tile = warp + G * m;
 #pragma unroll
           for (int x = 0; x < TK; ++x)
             if (x <= tile / 2)
@@ -208,7 +205,7 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
             for (int e = 0; e < SEEN; ++e) load16(a[z][e], s_seen + ((((w & 1) * RUNS + run) * SEEN + e) * KS + x + z) * 128 + lane * 4);
 #pragma unroll
           for (int m = 0; m < MINE; ++m) {
-            const int i0 = 8 * (warp + OG * m);
+            const int i0 = 8 * (warp + G * m);
             uint32_t f[2][TERMS][2];
             if constexpr (TERMS == 1) {
               uint32_t z[4];
@@ -230,7 +227,7 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
         }
 #pragma unroll
         for (int m = 0; m < MINE; ++m) {
-          const float2 up = *reinterpret_cast<const float2*>(record.up + 8 * (warp + OG * m) + 2 * t);
+          const float2 up = *reinterpret_cast<const float2*>(record.up + 8 * (warp + G * m) + 2 * t);
           const float gain[2] = {p.scale * up.x, p.scale * up.y};
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
@@ -315,11 +312,7 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
           if constexpr (G > 1) {
             barrier_of<32 * G>(2 + run);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              r[e] = 0.f;
-#pragma unroll
-              for (int m = 0; m < G; ++m) r[e] += shares[run][m][which][g + 8 * e];
-            }
+            for (int e = 0; e < 2; ++e) r[e] = shares[run][0][which][g + 8 * e] + shares[run][1][which][g + 8 * e];
           }
         };
 #pragma unroll
@@ -347,20 +340,6 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
       const __nv_bfloat16* ks = keys_of(w);
       const T* vs = values_of(w) + 16 * run + g;
       const Record& record = record_of(w);
-      uint32_t inv[MINE][TK][3][2];
-      auto fetch_inverse = [&]() {
-#pragma unroll
-        for (int m = 0; m < MINE; ++m)
-#pragma unroll
-          for (int x = 0; x < TK; ++x)
-            if (x <= (warp + G * m) / 2)
-#pragma unroll
-              for (int e = 0; e < 3; ++e) {
-                const uint2 z = *reinterpret_cast<const uint2*>(record.inverse[delta_place(warp + G * m, x)][e][lane]);
-                inv[m][x][e][0] = z.x; inv[m][x][e][1] = z.y;
-              }
-      };
-      if (G > 1) fetch_inverse();      // on its way while R is worked out
       // R and U are this warp's of tiles of tokens warp, warp + G, ...
       float2 down[MINE];
       float r[MINE][4];
@@ -376,14 +355,9 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
 #pragma unroll
           for (int e = 0; e < 4; ++e) x[e] = says[m][e];
         } else {
-          float4 part[G];
-#pragma unroll
-          for (int e = 0; e < G; ++e) part[e] = *reinterpret_cast<const float4*>(x_part + ((run * G + e) * TT + tile) * 128 + lane * 4);
-#pragma unroll
-          for (int d = 1; d < G; d *= 2)
-#pragma unroll
-            for (int e = 0; e + d < G; e += 2 * d) { part[e].x += part[e + d].x; part[e].y += part[e + d].y; part[e].z += part[e + d].z; part[e].w += part[e + d].w; }
-          x[0] = part[0].x; x[1] = part[0].y; x[2] = part[0].z; x[3] = part[0].w;
+          const float4 a = *reinterpret_cast<const float4*>(x_part + ((run * G) * TT + tile) * 128 + lane * 4);
+          const float4 c = *reinterpret_cast<const float4*>(x_part + ((run * G + 1) * TT + tile) * 128 + lane * 4);
+          x[0] = a.x + c.x; x[1] = a.y + c.y; x[2] = a.z + c.z; x[3] = a.w + c.w;
         }
         r[m][0] = beta.x * fmaf(-up.x, x[0], to_float(vv[0]));
         r[m][1] = beta.y * fmaf(-up.y, x[1], to_float(vv[VP]));
@@ -392,12 +366,13 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
         odd |= fmaf(r[m][0], 0.f, fmaf(r[m][1], 0.f, fmaf(r[m][2], 0.f, r[m][3] * 0.f))) != 0.f;
         if constexpr (G > 1) keep<3>(r_frag + run * 3 * TK * 128, TK * 128, lane, tile, r[m]);
       }
-      odd = __any_sync(0xffffffffu, odd);
-      if constexpr (G > 1) {
-        if (lane == 0) odd_flags[run][warp] = odd;
-        barrier_of<32 * G>(2 + run);     // (one that joins the flags as well takes 100 cycles more)
-#pragma unroll
-        for (int m = 0; m < G; ++m) odd |= odd_flags[run][m] != 0;
+      // something in the window or the state is not finite: nothing has been changed yet
+      if constexpr (G == 1) odd = __any_sync(0xffffffffu, odd);
+      else odd = named_barrier_or(2 + run, 32 * G, odd);
+      if (lane == 0 && warp == 0) slow[w & 1][run] = odd;
+      if (__builtin_expect(odd, 0)) {
+        advance_slowly(w);
+        return;
       }
       // U^T = R^T T^T
       uint32_t a[TK][3][4];
@@ -420,12 +395,20 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
         }
       };
       operand(r_frag, r);
-      if (G == 1) fetch_inverse();
       float u[MINE][4];
       {
         float sums[MINE][2][4] = {};
 #pragma unroll
         for (int x = 0; x < TK; ++x) {
+          uint32_t f[MINE][3][2];
+#pragma unroll
+          for (int m = 0; m < MINE; ++m)
+            if (x <= (warp + G * m) / 2)
+#pragma unroll
+              for (int e = 0; e < 3; ++e) {
+                const uint2 z = *reinterpret_cast<const uint2*>(record.inverse[delta_place(warp + G * m, x)][e][lane]);
+                f[m][e][0] = z.x; f[m][e][1] = z.y;
+              }
           // small products first, tiles side by side
 #pragma unroll
           for (int sum = 2; sum >= 0; --sum)
@@ -433,19 +416,12 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
             for (int i = 0; i <= sum; ++i)
 #pragma unroll
               for (int m = 0; m < MINE; ++m)
-                if (x <= (warp + G * m) / 2) mma16816(sums[m][(x + i) & 1], a[x][i], inv[m][x][sum - i][0], inv[m][x][sum - i][1]);
+                if (x <= (warp + G * m) / 2) mma16816(sums[m][(x + i) & 1], a[x][i], f[m][sum - i][0], f[m][sum - i][1]);
         }
 #pragma unroll
         for (int m = 0; m < MINE; ++m)
 #pragma unroll
           for (int e = 0; e < 4; ++e) u[m][e] = sums[m][0][e] + sums[m][1][e];
-      }
-      if (lane == 0 && warp == 0) slow[w & 1][run] = odd;
-      // something in the window or the state is not finite: nothing has been changed yet
-      if (__builtin_expect(odd, 0)) {
-        if (G > 1) barrier_of<32 * G>(2 + run);
-        advance_slowly(w);
-        return;
       }
 #pragma unroll
       for (int m = 0; m < MINE; ++m) {
@@ -506,38 +482,38 @@ cudaError_t launch_shape(const DeltaParams& p, cudaStream_t s) {
   delta_chunk_kernel<H><<<dim3(H::D / H::COLS, (unsigned)p.heads, (unsigned)p.batch), H::THREADS, H::SMEM, s>>>(p);
   return cudaGetLastError();
 }
+template <typename T, int D>
+cudaError_t launch(const DeltaParams& p, cudaStream_t s) {
+  const int64_t runs = (int64_t)p.batch * p.heads * (D / 16);
+  if constexpr (sizeof(T) == 2) {
+    if (runs > 2 * PLAN_SMS) return launch_shape<Shape<T, D, 1, D == 32 ? 2 : 4>>(p, s);
+  }
+  return launch_shape<Shape<T, D, 2, 1>>(p, s);
+}
+template <typename T>
+cudaError_t launch(const DeltaParams& p, int D, cudaStream_t s) {
+  return D == 32 ? launch<T, 32>(p, s) : D == 64 ? launch<T, 64>(p, s) : launch<T, 128>(p, s);
+}
+
 }  // namespace
 
-// Whether the runs are so few that the chain goes a step ahead of itself, a block to a run (delta_look.cu); fp32 calls always do.
-static bool looks(int batch, int heads, int D, bool bf16) {
-  const char* ev = getenv("DG"); const int dg = ev ? atoi(ev) : 0;
-  if (dg) return !bf16 || dg == 2;
-  return !bf16 || (int64_t)batch * heads * (D / 16) <= 2 * PLAN_SMS;
-}
-static int64_t record_bytes(bool bf16, bool look) {
-  return bf16 ? look ? sizeof(DeltaRecord<2, true>) : sizeof(DeltaRecord<2, false>) : sizeof(DeltaRecord<3, true>);
-}
 // Windows to a range: records of one fit `most` bytes, or there is but one window to a range.
-static int range_of(int batch, int tokens, int heads, int64_t record) {
+static int range_of(int batch, int tokens, int heads, bool bf16) {
   constexpr int64_t most = 96 << 20;
-  const int64_t each = (int64_t)batch * heads * record, all = ((int64_t)tokens + C - 1) / C;
+  const int64_t each = (int64_t)batch * heads * (int64_t)(bf16 ? sizeof(DeltaRecord<2>) : sizeof(DeltaRecord<3>)), all = ((int64_t)tokens + C - 1) / C;
   const int64_t fit = most / each < 1 ? 1 : most / each, ranges = (all + fit - 1) / fit;
   return (int)((all + ranges - 1) / ranges);
 }
-uint64_t delta_scratch(int batch, int tokens, int heads, int D, bool bf16) {
-  const int64_t record = record_bytes(bf16, looks(batch, heads, D, bf16));
-  return (uint64_t)batch * heads * range_of(batch, tokens, heads, record) * record;
+uint64_t delta_scratch(int batch, int tokens, int heads, bool bf16) {
+  return (uint64_t)batch * heads * range_of(batch, tokens, heads, bf16) * (bf16 ? sizeof(DeltaRecord<2>) : sizeof(DeltaRecord<3>));
 }
 
 cudaError_t launch_delta_chunk(DeltaParams p, bool bf16, int D, cudaStream_t s) {
   const int all = (p.tokens + C - 1) / C;
-  const bool look = looks(p.batch, p.heads, D, bf16);
-  p.windows = range_of(p.batch, p.tokens, p.heads, record_bytes(bf16, look));
+  p.windows = range_of(p.batch, p.tokens, p.heads, bf16);
   for (p.first_window = 0; p.first_window < all; p.first_window += p.windows) {
-    cudaError_t e = launch_delta_prepare(p, bf16, look, D, s);
-    if (e != cudaSuccess) return e;
-    if (look) e = launch_delta_look(p, bf16, D, s);
-    else e = D == 32 ? launch_shape<Shape<__nv_bfloat16, 32, 1, 1, 2>>(p, s) : D == 64 ? launch_shape<Shape<__nv_bfloat16, 64, 1, 1, 4>>(p, s) : launch_shape<Shape<__nv_bfloat16, 128, 1, 1, 4>>(p, s);
+    cudaError_t e = launch_delta_prepare(p, bf16, D, s);
+    if (e == cudaSuccess) e = bf16 ? launch<__nv_bfloat16>(p, D, s) : launch<float>(p, D, s);
     if (e != cudaSuccess) return e;
     p.state = p.state_out;
   }

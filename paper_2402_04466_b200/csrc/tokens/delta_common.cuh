@@ -13,23 +13,16 @@ constexpr int DELTA_TT = DELTA_C / 8, DELTA_TK = DELTA_C / 16;      // tiles of 
 constexpr int DELTA_GROUP = 128;             // threads that work together
 
 // What is worked out of a window's keys, queries and gates, for every head: the inverse of its triangular system and the weights of its corrections in out, as the
-// second operand's registers of products, for tile of 8 tokens `tile` the products along 16 tokens x = 0 .. tile / 2; where LOOK, the products of its keys with the
-// next window's, a tile of those at a time; and the gates.
-struct DeltaCross {
-  uint32_t next[DELTA_TT][DELTA_TK][3][32][2];
-};
-struct DeltaNothing {};
-template <int SEEN_, bool LOOK_>
-struct DeltaRecord : std::conditional_t<LOOK_, DeltaCross, DeltaNothing> {
-  static constexpr int SEEN = SEEN_, PLACES = 6;           // (tile, x)
-  static constexpr bool LOOK = LOOK_;
+// second operand's registers of products, for tile of 8 tokens `tile` the products along 16 tokens x = 0 .. tile / 2, and the gates.
+template <int SEEN>
+struct DeltaRecord {
+  static constexpr int PLACES = 6;           // (tile, x)
   uint32_t inverse[PLACES][3][32][2];        // [][term][lane][]
   uint32_t weights[PLACES][SEEN][32][2];
   float beta[DELTA_C], up[DELTA_C], down[DELTA_C];      // G: the sum of log_decay up to and including a token; e^G, e^(G_C - G)
   float whole;                               // e^G_C
   float pad[31];
 };
-static_assert(sizeof(DeltaRecord<2, false>) == 8192 && sizeof(DeltaRecord<2, true>) == 8192 + 6144, "records");
 __host__ __device__ constexpr int delta_place(int tile, int x) { return tile < 2 ? tile : 2 * tile - 2 + x; }
 
 // a pair as three bf16 terms, a in the lower halves: the upper eight bits of what is left, cut off, which for the last term is all of it

@@ -4,7 +4,7 @@
 // out reads them with the weights P_ij = scale e^(G_i - G_j) (q_i . k_j), j <= i.  A block takes a window: A and P by products of 16 rows to a warp, the
 // inverses of both diagonal blocks of 16 by substitution, a column to a lane, and the block below them as -T_11 A_10 T_00, by products again.  All of it counts with
 // fp32's bits: operands that are not bf16 to begin with are cut into three bf16 terms.  (P of bf16 calls: 16 bits.)  The windows of all sequences run at once; the chain
-// of states, delta_chunk.cu or delta_look.cu, reads what is left here as the registers it needs.
+// of states, delta_chunk.cu, reads what is left here as the registers it needs.
 #include "delta_common.cuh"
 
 namespace tt {
@@ -13,15 +13,13 @@ namespace {
 
 constexpr int C = DELTA_C, TT = DELTA_TT, TK = DELTA_TK;
 
-template <typename T_, int D_, bool LOOK_>
+template <typename T_, int D_>
 struct Shape {
   using T = T_;
   static constexpr int D = D_;
-  static constexpr bool LOOK = LOOK_;
   static constexpr int TERMS = sizeof(T) == 2 ? 1 : 3, SEEN = sizeof(T) == 2 ? 2 : 3;
   static constexpr int KS = D / 16, KP = D + 8, AP = C + 4, TILE = C * KP;
-  static constexpr int TILES = LOOK ? 3 : 2;                  // of keys, queries, and the next window's keys
-  static constexpr int SMEM = TILES * TERMS * TILE * 2 + C * AP * 4, BLOCKS = TERMS == 1 ? 5 : 2;          // to a multiprocessor
+  static constexpr int BLOCKS = TERMS == 1 ? 5 : 3;          // to a multiprocessor
 };
 
 // 2^x for x of 0 and below, as pair: to half a step of the result and little more, where exp2f is off by two.  By a Taylor polynomial of e^(y ln 2), |y| <= 1/2.
@@ -52,10 +50,9 @@ __global__ void __launch_bounds__(DELTA_GROUP, H::BLOCKS) delta_prepare_kernel(c
   using T = typename H::T;
   constexpr int D = H::D, TERMS = H::TERMS, SEEN = H::SEEN, KS = H::KS, KP = H::KP, AP = H::AP;
   extern __shared__ __align__(16) uint8_t smem[];
-  __nv_bfloat16* ks = reinterpret_cast<__nv_bfloat16*>(smem);                // [keys, queries, next keys][term][C][KP]
+  __nv_bfloat16* ks = reinterpret_cast<__nv_bfloat16*>(smem);                // [keys, queries][term][C][KP]
   __nv_bfloat16* qs = ks + TERMS * H::TILE;
-  __nv_bfloat16* next = qs + TERMS * H::TILE;
-  float* A = reinterpret_cast<float*>(ks + H::TILES * TERMS * H::TILE);                 // [C][AP]: A, then its inverse
+  float* A = reinterpret_cast<float*>(qs + TERMS * H::TILE);                 // [C][AP]: A, then its inverse
   __shared__ float2 sums[C];                                                 // log2(e) G as a pair of floats: what counts are differences of far larger sums
   __shared__ float betas[C];
   const int b = blockIdx.z, h = blockIdx.y, w = p.first_window + blockIdx.x;
@@ -65,8 +62,7 @@ __global__ void __launch_bounds__(DELTA_GROUP, H::BLOCKS) delta_prepare_kernel(c
   const int hk = h / p.group;
   const T* q = reinterpret_cast<const T*>(p.q.p) + b * p.q.b + hk * p.q.h;
   const T* k = reinterpret_cast<const T*>(p.k.p) + b * p.k.b + hk * p.k.h;
-  using Record = DeltaRecord<SEEN, H::LOOK>;
-  Record& record = reinterpret_cast<Record*>(p.records)[((int64_t)b * p.heads + h) * p.windows + blockIdx.x];
+  DeltaRecord<SEEN>& record = reinterpret_cast<DeltaRecord<SEEN>*>(p.records)[((int64_t)b * p.heads + h) * p.windows + blockIdx.x];
   float decay = 0.f, beta = 0.f;
   if (warp == 0) {
     const int token = w * C + lane;
@@ -80,13 +76,12 @@ __global__ void __launch_bounds__(DELTA_GROUP, H::BLOCKS) delta_prepare_kernel(c
   if constexpr (TERMS == 1) {
     k_rows.fetch(reinterpret_cast<T*>(ks), KP, w * C, n);
     q_rows.fetch(reinterpret_cast<T*>(qs), KP, w * C, n);
-    if (H::LOOK) k_rows.fetch(reinterpret_cast<T*>(next), KP, (w + 1) * C, n);
     copies_commit();
   } else {
-    for (int i = tid; i < H::TILES * C * (D / 4); i += DELTA_GROUP) {
-      const int side = i / (C * (D / 4)), r = i / (D / 4) % C, c = i % (D / 4) * 4, token = (side == 2 ? w + 1 : w) * C + r;
+    for (int i = tid; i < 2 * C * (D / 4); i += DELTA_GROUP) {
+      const int side = i / (C * (D / 4)), r = i / (D / 4) % C, c = i % (D / 4) * 4;
       float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (token < n) f = *reinterpret_cast<const float4*>((side == 1 ? q + (int64_t)token * p.q.t : k + (int64_t)token * p.k.t) + c);
+      if (w * C + r < n) f = *reinterpret_cast<const float4*>((side ? q + (int64_t)(w * C + r) * p.q.t : k + (int64_t)(w * C + r) * p.k.t) + c);
       uint32_t low[3], high[3];
       cut(f.x, f.y, low);
       cut(f.z, f.w, high);
@@ -181,32 +176,6 @@ __global__ void __launch_bounds__(DELTA_GROUP, H::BLOCKS) delta_prepare_kernel(c
               *reinterpret_cast<uint2*>(record.weights[delta_place(2 * strip + r, x)][e][lane]) = make_uint2(terms[r][2 * x][e], terms[r][2 * x + 1][e]);
     }
   }
-  if constexpr (H::LOOK) {
-    // the next window's keys on this one's: 16 rows and 16 columns to a warp
-    const int strip = warp & 1, x = warp >> 1;
-    float acc[2][4] = {};
-#pragma unroll 2
-    for (int y = 0; y < KS; ++y) {
-      uint32_t a[TERMS][4], one[TERMS][2], two[TERMS][2];
-#pragma unroll
-      for (int e = 0; e < TERMS; ++e) {
-        uint32_t f[4];
-        ldmatrix4<false>(a[e], smem_u32(next + e * H::TILE + (16 * strip + (lane & 15)) * KP + y * 16 + (lane >> 4) * 8));
-        ldmatrix4<false>(f, smem_u32(ks + e * H::TILE + (16 * x + (lane & 7) + 8 * (lane >> 4)) * KP + y * 16 + ((lane >> 3) & 1) * 8));
-        one[e][0] = f[0]; one[e][1] = f[1]; two[e][0] = f[2]; two[e][1] = f[3];
-      }
-      product(acc[0], a, one);
-      product(acc[1], a, two);
-    }
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      uint32_t low[3], high[3];
-      cut(acc[0][2 * r], acc[0][2 * r + 1], low);
-      cut(acc[1][2 * r], acc[1][2 * r + 1], high);
-#pragma unroll
-      for (int e = 0; e < 3; ++e) *reinterpret_cast<uint2*>(record.next[2 * strip + r][x][e][lane]) = make_uint2(low[e], high[e]);
-    }
-  }
   __syncthreads();
   auto put = [&](int tile, int x, int e, uint32_t b0, uint32_t b1) { *reinterpret_cast<uint2*>(record.inverse[delta_place(tile, x)][e][lane]) = make_uint2(b0, b1); };
   // the two blocks of 16 on the diagonal, a column to a lane
@@ -295,24 +264,25 @@ __global__ void __launch_bounds__(DELTA_GROUP, H::BLOCKS) delta_prepare_kernel(c
   }
 }
 
-template <typename H>
-cudaError_t launch_shape(const DeltaParams& p, cudaStream_t s) {
+template <typename T, int D>
+cudaError_t launch(const DeltaParams& p, cudaStream_t s) {
+  using H = Shape<T, D>;
+  constexpr int SMEM = 2 * H::TERMS * H::TILE * 2 + C * H::AP * 4;
   static OncePerContext once;
-  const cudaError_t e = once([] { return cudaFuncSetAttribute(delta_prepare_kernel<H>, cudaFuncAttributeMaxDynamicSharedMemorySize, H::SMEM); });
+  const cudaError_t e = once([] { return cudaFuncSetAttribute(delta_prepare_kernel<H>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM); });
   if (e != cudaSuccess) return e;
-  delta_prepare_kernel<H><<<dim3((unsigned)p.windows, (unsigned)p.heads, (unsigned)p.batch), DELTA_GROUP, H::SMEM, s>>>(p);
+  delta_prepare_kernel<H><<<dim3((unsigned)p.windows, (unsigned)p.heads, (unsigned)p.batch), DELTA_GROUP, SMEM, s>>>(p);
   return cudaGetLastError();
 }
-template <typename T, bool LOOK>
+template <typename T>
 cudaError_t launch(const DeltaParams& p, int D, cudaStream_t s) {
-  return D == 32 ? launch_shape<Shape<T, 32, LOOK>>(p, s) : D == 64 ? launch_shape<Shape<T, 64, LOOK>>(p, s) : launch_shape<Shape<T, 128, LOOK>>(p, s);
+  return D == 32 ? launch<T, 32>(p, s) : D == 64 ? launch<T, 64>(p, s) : launch<T, 128>(p, s);
 }
 
 }  // namespace
 
-cudaError_t launch_delta_prepare(const DeltaParams& p, bool bf16, bool look, int D, cudaStream_t s) {
-  if (!bf16) return launch<float, true>(p, D, s);
-  return look ? launch<__nv_bfloat16, true>(p, D, s) : launch<__nv_bfloat16, false>(p, D, s);
+cudaError_t launch_delta_prepare(const DeltaParams& p, bool bf16, int D, cudaStream_t s) {
+  return bf16 ? launch<__nv_bfloat16>(p, D, s) : launch<float>(p, D, s);
 }
 
 }  // namespace tok

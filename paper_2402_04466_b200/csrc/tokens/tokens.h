@@ -67,10 +67,9 @@ struct alignas(32) DeltaParams {
   void* records;                           // [batch][heads][windows]: DeltaRecord
 };
 cudaError_t launch_delta_step(const DeltaParams& p, bool bf16, int D, cudaStream_t s);      // token by token
-cudaError_t launch_delta_prepare(const DeltaParams& p, bool bf16, bool look, int D, cudaStream_t s);      // of every window, what depends on no state
-cudaError_t launch_delta_look(const DeltaParams& p, bool bf16, int D, cudaStream_t s);      // the chain of states of few runs
+cudaError_t launch_delta_prepare(const DeltaParams& p, bool bf16, int D, cudaStream_t s);   // of every window, what depends on no state
 cudaError_t launch_delta_chunk(DeltaParams p, bool bf16, int D, cudaStream_t s);            // a window of tokens at a time, prepared range by range
-uint64_t delta_scratch(int batch, int tokens, int heads, int D, bool bf16);
+uint64_t delta_scratch(int batch, int tokens, int heads, bool bf16);
 
 struct alignas(32) CrossParams {
   View q, k, v, o;
