@@ -22,25 +22,25 @@ namespace {
 
 constexpr int C = DELTA_C, TT = DELTA_TT, TK = DELTA_TK, GROUP = DELTA_GROUP;
 
-// G warps to a run, RUNS runs to a block
-template <typename T_, int D_, int G_, int RUNS_>
+// G warps of the chain and OG of out to a run, RUNS runs to a block
+template <typename T_, int D_, int G_, int OG_, int RUNS_>
 struct Shape {
   using T = T_;
-  static constexpr int D = D_, G = G_, RUNS = RUNS_;
+  static constexpr int D = D_, G = G_, OG = OG_, RUNS = RUNS_;
   static constexpr int TERMS = sizeof(T) == 2 ? 1 : 3;       // of keys
   static constexpr int SEEN = sizeof(T) == 2 ? 2 : 3;        // of S, U and P in out
   using Record = DeltaRecord<SEEN>;
-  static constexpr int CHAIN = G * RUNS;                     // warps of the chain, and of out
-  static constexpr int THREADS = 2 * CHAIN * 32 + GROUP;
+  static constexpr int CHAIN = G * RUNS, OUT = OG * RUNS;    // warps
+  static constexpr int THREADS = (CHAIN + OUT) * 32 + GROUP;
   static constexpr int KS = D / 16;                          // products along a key
   static constexpr int SK = KS / G, NT = 2 * SK;             // of them a warp's, and its tiles of 8 keys' elements of the state
-  static constexpr int MINE = TT / G;                        // tiles of tokens of a warp
+  static constexpr int MINE = TT / G, OUT_MINE = TT / OG;    // tiles of tokens of a warp
   static constexpr int COLS = 16 * RUNS;
   static constexpr int KP = D + 8, VP = COLS + 16 / (int)sizeof(T), QP = TERMS == 1 ? D + 8 : D + 4, OP = 16 + 16 / (int)sizeof(T);   // pitches
   static constexpr int TILE = C * KP;                        // bf16 elements of one term of a window's keys
   // Windows in flight.  Keys are waited for two steps ahead of the chain, which asks a step ahead, the rest one: what is fetched has places for those and the
   // chain's.  fp32 keys wait in `raw` to be cut.
-  static constexpr int AHEAD = TERMS == 1 ? 2 : 1, PLACES = AHEAD + 2, K_PLACES = TERMS == 1 ? AHEAD + 3 : 3;
+  static constexpr int AHEAD = TERMS == 1 ? 2 : 1, PLACES = AHEAD + 2, K_PLACES = TERMS == 1 ? (G == 1 ? AHEAD + 3 : 8) : 3;
   static constexpr int RAW = TERMS == 1 ? 0 : AHEAD * C * (D + 4) * 4;
   static constexpr int K = K_PLACES * TERMS * TILE * 2, Q = PLACES * C * QP * (int)sizeof(T), V = PLACES * C * VP * (int)sizeof(T);
   static constexpr int RECORDS = PLACES * (int)sizeof(Record);
@@ -54,11 +54,11 @@ template <typename H>
 __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid_constant__ DeltaParams p) {
   using T = typename H::T;
   using Record = typename H::Record;
-  constexpr int D = H::D, G = H::G, RUNS = H::RUNS, TERMS = H::TERMS, SEEN = H::SEEN, KS = H::KS, SK = H::SK, NT = H::NT, MINE = H::MINE, COLS = H::COLS, KP = H::KP, VP = H::VP, QP = H::QP,
+  constexpr int D = H::D, G = H::G, OG = H::OG, RUNS = H::RUNS, TERMS = H::TERMS, SEEN = H::SEEN, KS = H::KS, SK = H::SK, NT = H::NT, MINE = H::MINE, COLS = H::COLS, KP = H::KP, VP = H::VP, QP = H::QP,
                 OP = H::OP;
   constexpr int EACH = 16 / (int)sizeof(T);
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ int slow[2][RUNS];                                              // [parity]: the window was taken token by token
+  __shared__ int slow[4][RUNS];                                              // [window % 4]: the window is taken token by token
   __shared__ float shares[RUNS][G][2][16];                                   // of either sum of a token taken so
   uint8_t* place = smem;
   auto room = [&](int bytes) {
@@ -82,9 +82,12 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
   const int token0 = p.first_window * C, n = clamp_length(p.lengths, b, p.tokens);
   // before any of its data is touched: the slot of an entry that is passed over may be one that an earlier entry is writing
   const int slot = slot_of(p.slots, p.num_slots, b);
-  if (slot < 0) return;                // the whole block
   const int windows = n > token0 ? min(p.windows, (n - token0 + C - 1) / C) : 0;
-  if (windows == 0 && (p.first_window > 0 || p.state_out == p.state)) return;
+  if (slot < 0 || (windows == 0 && (p.first_window > 0 || p.state_out == p.state))) {
+    pdl_wait();                        // the grid ends behind the preparation's
+    return;                            // the whole block
+  }
+  if (threadIdx.x < 4 * RUNS) slow[threadIdx.x / RUNS][threadIdx.x % RUNS] = 0;
   const int all_warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int hk = h / p.group;
@@ -92,18 +95,19 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
   const T* k = reinterpret_cast<const T*>(p.k.p) + b * p.k.b + hk * p.k.h;
   const T* v = reinterpret_cast<const T*>(p.v.p) + b * p.v.b + h * p.v.h + col0;
   T* o = reinterpret_cast<T*>(p.o.p) + b * p.o.b + h * p.o.h + col0;
-  auto keys_of = [&](int w) { return keys + (w % H::K_PLACES) * TERMS * H::TILE; };
-  auto queries_of = [&](int w) { return queries + (w % H::PLACES) * C * QP; };
-  auto values_of = [&](int w) { return values + (w % H::PLACES) * C * VP; };
-  auto record_of = [&](int w) -> Record& { return records[w % H::PLACES]; };
+  auto keys_of = [&](int w) { return keys + ((uint32_t)w % H::K_PLACES) * TERMS * H::TILE; };
+  auto queries_of = [&](int w) { return queries + ((uint32_t)w % H::PLACES) * C * QP; };
+  auto values_of = [&](int w) { return values + ((uint32_t)w % H::PLACES) * C * VP; };
+  auto record_of = [&](int w) -> Record& { return records[(uint32_t)w % H::PLACES]; };
 
-  if (all_warp >= 2 * H::CHAIN) {
+  if (all_warp >= H::CHAIN + H::OUT) {
     // ------------------------------------------------------------------------------- loads
-    const int tid = threadIdx.x - 2 * H::CHAIN * 32;
+    const int tid = threadIdx.x - (H::CHAIN + H::OUT) * 32;
     const Rows<T, D> k_rows(k, p.k.t, tid), q_rows(q, p.q.t, tid);
     const Rows<T, COLS> v_rows(v, p.v.t, tid);
     const uint8_t* left = reinterpret_cast<const uint8_t*>(reinterpret_cast<const Record*>(p.records) + ((int64_t)b * p.heads + h) * p.windows);
     auto raw_of = [&](int w) { return reinterpret_cast<T*>(raw) + (w % H::AHEAD) * C * (D + 4); };
+    pdl_wait();                                  // for the records
     // window w's keys and what else window w - 1 needs; nothing behind the last, but counted as the others are
     auto fetch = [&](int w) {
       if (w < windows) {
@@ -144,13 +148,14 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
     }
   } else if (all_warp >= H::CHAIN) {
     // ------------------------------------------------------------------------------- out
-    const int run = (all_warp - H::CHAIN) / G, warp = (all_warp - H::CHAIN) % G;      // tiles of tokens warp, warp + G, ...
+    constexpr int MINE = H::OUT_MINE;
+    const int run = (all_warp - H::CHAIN) / OG, warp = (all_warp - H::CHAIN) % OG;      // tiles of tokens warp, warp + OG, ...
     T* stage = outs + run * C * OP;
     float acc[MINE][2][4];               // columns of values g and g + 8, tokens 2t and 2t + 1
     uint32_t weights[MINE][TK][SEEN][2];
     for (int step = -2; step <= windows; ++step) {
       // the last product of the window before
-      if (step >= 1 && !slow[(step - 1) & 1][run]) {
+      if (step >= 1 && !slow[(step - 1) & 3][run]) {
         const int w = step - 1;
         uint32_t a[TK][SEEN][4];
 #pragma unroll
@@ -159,7 +164,7 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
           for (int e = 0; e < SEEN; ++e) load16(a[x][e], u_seen + ((((w & 1) * RUNS + run) * SEEN + e) * TK + x) * 128 + lane * 4);
 #pragma unroll
         for (int m = 0; m < MINE; ++m) {
-          const int tile = warp + G * m;
+          const int tile = warp + OG * m;
 #pragma unroll
           for (int x = 0; x < TK; ++x)
             if (x <= tile / 2) product(acc[m][x], a[x], weights[m][x]);
@@ -172,7 +177,7 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
         __syncwarp();
 #pragma unroll
         for (int e = lane; e < MINE * 8 * (16 / EACH); e += 32) {
-          const int i = e / (16 / EACH), r = 8 * (warp + G * (i / 8)) + i % 8, c = e % (16 / EACH) * EACH;
+          const int i = e / (16 / EACH), r = 8 * (warp + OG * (i / 8)) + i % 8, c = e % (16 / EACH) * EACH;
           const int token = token0 + w * C + r;
           if (token < n) *reinterpret_cast<uint4*>(o + (int64_t)token * p.o.t + 16 * run + c) = *reinterpret_cast<const uint4*>(stage + r * OP + c);
         }
@@ -184,7 +189,7 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
         const Record& record = record_of(w);
 #pragma unroll
         for (int m = 0; m < MINE; ++m) {
-          const int tile = warp + G * m;
+          const int tile = warp + OG * m;
 #pragma unroll
           for (int x = 0; x < TK; ++x)
             if (x <= tile / 2)
@@ -205,7 +210,7 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
             for (int e = 0; e < SEEN; ++e) load16(a[z][e], s_seen + ((((w & 1) * RUNS + run) * SEEN + e) * KS + x + z) * 128 + lane * 4);
 #pragma unroll
           for (int m = 0; m < MINE; ++m) {
-            const int i0 = 8 * (warp + G * m);
+            const int i0 = 8 * (warp + OG * m);
             uint32_t f[2][TERMS][2];
             if constexpr (TERMS == 1) {
               uint32_t z[4];
@@ -227,7 +232,7 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
         }
 #pragma unroll
         for (int m = 0; m < MINE; ++m) {
-          const float2 up = *reinterpret_cast<const float2*>(record.up + 8 * (warp + G * m) + 2 * t);
+          const float2 up = *reinterpret_cast<const float2*>(record.up + 8 * (warp + OG * m) + 2 * t);
           const float gain[2] = {p.scale * up.x, p.scale * up.y};
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
@@ -253,8 +258,6 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
     float says[TT][4];
     auto ask = [&](int w) {
       const __nv_bfloat16* ks = keys_of(w);
-#pragma unroll
-      for (int c = 0; c < TT; ++c) says[c][0] = says[c][1] = says[c][2] = says[c][3] = 0.f;
 #pragma unroll
       for (int x = 0; x < SK; ++x) {
         uint32_t a[3][4];
@@ -284,7 +287,10 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
           for (int i = 0; i < 3; ++i)
 #pragma unroll
             for (int c = 0; c < TT; ++c)
-              if (sum - i >= 0 && sum - i < TERMS) mma16816(says[c], a[i], f[c][sum - i][0], f[c][sum - i][1]);
+              if (sum - i >= 0 && sum - i < TERMS) {
+                if (x == 0 && sum == 2 && i == (TERMS == 1 ? 2 : 0)) mma16816_first(says[c], a[i], f[c][sum - i][0], f[c][sum - i][1]);
+                else mma16816(says[c], a[i], f[c][sum - i][0], f[c][sum - i][1]);
+              }
       }
       if constexpr (G > 1)
 #pragma unroll
@@ -312,7 +318,11 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
           if constexpr (G > 1) {
             barrier_of<32 * G>(2 + run);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) r[e] = shares[run][0][which][g + 8 * e] + shares[run][1][which][g + 8 * e];
+            for (int e = 0; e < 2; ++e) {
+              r[e] = 0.f;
+#pragma unroll
+              for (int m = 0; m < G; ++m) r[e] += shares[run][m][which][g + 8 * e];
+            }
           }
         };
 #pragma unroll
@@ -340,6 +350,20 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
       const __nv_bfloat16* ks = keys_of(w);
       const T* vs = values_of(w) + 16 * run + g;
       const Record& record = record_of(w);
+      uint32_t inv[MINE][TK][3][2];
+      auto fetch_inverse = [&]() {
+#pragma unroll
+        for (int m = 0; m < MINE; ++m)
+#pragma unroll
+          for (int x = 0; x < TK; ++x)
+            if (x <= (warp + G * m) / 2)
+#pragma unroll
+              for (int e = 0; e < 3; ++e) {
+                const uint2 z = *reinterpret_cast<const uint2*>(record.inverse[delta_place(warp + G * m, x)][e][lane]);
+                inv[m][x][e][0] = z.x; inv[m][x][e][1] = z.y;
+              }
+      };
+      if (G > 1) fetch_inverse();      // on its way while R is worked out
       // R and U are this warp's of tiles of tokens warp, warp + G, ...
       float2 down[MINE];
       float r[MINE][4];
@@ -355,9 +379,14 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
 #pragma unroll
           for (int e = 0; e < 4; ++e) x[e] = says[m][e];
         } else {
-          const float4 a = *reinterpret_cast<const float4*>(x_part + ((run * G) * TT + tile) * 128 + lane * 4);
-          const float4 c = *reinterpret_cast<const float4*>(x_part + ((run * G + 1) * TT + tile) * 128 + lane * 4);
-          x[0] = a.x + c.x; x[1] = a.y + c.y; x[2] = a.z + c.z; x[3] = a.w + c.w;
+          float4 part[G];
+#pragma unroll
+          for (int e = 0; e < G; ++e) part[e] = *reinterpret_cast<const float4*>(x_part + ((run * G + e) * TT + tile) * 128 + lane * 4);
+#pragma unroll
+          for (int d = 1; d < G; d *= 2)
+#pragma unroll
+            for (int e = 0; e + d < G; e += 2 * d) { part[e].x += part[e + d].x; part[e].y += part[e + d].y; part[e].z += part[e + d].z; part[e].w += part[e + d].w; }
+          x[0] = part[0].x; x[1] = part[0].y; x[2] = part[0].z; x[3] = part[0].w;
         }
         r[m][0] = beta.x * fmaf(-up.x, x[0], to_float(vv[0]));
         r[m][1] = beta.y * fmaf(-up.y, x[1], to_float(vv[VP]));
@@ -366,14 +395,10 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
         odd |= fmaf(r[m][0], 0.f, fmaf(r[m][1], 0.f, fmaf(r[m][2], 0.f, r[m][3] * 0.f))) != 0.f;
         if constexpr (G > 1) keep<3>(r_frag + run * 3 * TK * 128, TK * 128, lane, tile, r[m]);
       }
-      // something in the window or the state is not finite: nothing has been changed yet
-      if constexpr (G == 1) odd = __any_sync(0xffffffffu, odd);
-      else odd = named_barrier_or(2 + run, 32 * G, odd);
-      if (lane == 0 && warp == 0) slow[w & 1][run] = odd;
-      if (__builtin_expect(odd, 0)) {
-        advance_slowly(w);
-        return;
-      }
+      if (odd) slow[w & 3][run] = 1;
+      // (a barrier that joins flags takes 100 cycles more)
+      if constexpr (G > 1) barrier_of<32 * G>(2 + run);
+      else __syncwarp();
       // U^T = R^T T^T
       uint32_t a[TK][3][4];
       auto operand = [&](const uint32_t* frag, const float (&x)[MINE][4]) {
@@ -395,33 +420,34 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
         }
       };
       operand(r_frag, r);
+      if (G == 1) fetch_inverse();
       float u[MINE][4];
       {
-        float sums[MINE][2][4] = {};
+        // small products first, tiles side by side, either 16 tokens apart
+        float sums[MINE][TK][4];
 #pragma unroll
-        for (int x = 0; x < TK; ++x) {
-          uint32_t f[MINE][3][2];
+        for (int sum = 2; sum >= 0; --sum)
 #pragma unroll
-          for (int m = 0; m < MINE; ++m)
-            if (x <= (warp + G * m) / 2)
+          for (int i = 0; i <= sum; ++i)
 #pragma unroll
-              for (int e = 0; e < 3; ++e) {
-                const uint2 z = *reinterpret_cast<const uint2*>(record.inverse[delta_place(warp + G * m, x)][e][lane]);
-                f[m][e][0] = z.x; f[m][e][1] = z.y;
-              }
-          // small products first, tiles side by side
-#pragma unroll
-          for (int sum = 2; sum >= 0; --sum)
-#pragma unroll
-            for (int i = 0; i <= sum; ++i)
+            for (int x = 0; x < TK; ++x)
 #pragma unroll
               for (int m = 0; m < MINE; ++m)
-                if (x <= (warp + G * m) / 2) mma16816(sums[m][(x + i) & 1], a[x][i], f[m][sum - i][0], f[m][sum - i][1]);
-        }
+                if (x <= (warp + G * m) / 2) {
+                  if (sum == 2 && i == 0) mma16816_first(sums[m][x], a[x][i], inv[m][x][sum - i][0], inv[m][x][sum - i][1]);
+                  else mma16816(sums[m][x], a[x][i], inv[m][x][sum - i][0], inv[m][x][sum - i][1]);
+                }
 #pragma unroll
         for (int m = 0; m < MINE; ++m)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) u[m][e] = sums[m][0][e] + sums[m][1][e];
+          for (int e = 0; e < 4; ++e) u[m][e] = warp + G * m >= 2 ? sums[m][0][e] + sums[m][1][e] : sums[m][0][e];
+      }
+      if (lane == 0 && warp == 0) slow[(w + 2) & 3][run] = 0;      // out was through with that two windows ago
+      // something in the window or the state is not finite: nothing has been changed yet
+      if (__builtin_expect(slow[w & 3][run], 0)) {
+        if (G > 1) barrier_of<32 * G>(2 + run);
+        advance_slowly(w);
+        return;
       }
 #pragma unroll
       for (int m = 0; m < MINE; ++m) {
@@ -445,7 +471,7 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
             ldmatrix4<true>(y, smem_u32(ks + e * H::TILE + lane * KP + (warp * NT + m + z) * 8));
             f[z][0][e][0] = y[0]; f[z][0][e][1] = y[1]; f[z][1][e][0] = y[2]; f[z][1][e][1] = y[3];
           }
-        float d[2][2][4] = {};
+        float d[2][2][4];
 #pragma unroll
         for (int sum = 2; sum >= 0; --sum)
 #pragma unroll
@@ -454,7 +480,10 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
             for (int z = 0; z < 2; ++z)
 #pragma unroll
               for (int x = 0; x < 2; ++x)
-                if (sum - i < TERMS) mma16816(d[z][x], a[x][i], f[z][x][sum - i][0], f[z][x][sum - i][1]);
+                if (sum - i < TERMS) {
+                  if (sum == 2 && i == (TERMS == 1 ? 2 : 0)) mma16816_first(d[z][x], a[x][i], f[z][x][sum - i][0], f[z][x][sum - i][1]);
+                  else mma16816(d[z][x], a[x][i], f[z][x][sum - i][0], f[z][x][sum - i][1]);
+                }
 #pragma unroll
         for (int z = 0; z < 2; ++z)
 #pragma unroll
@@ -479,16 +508,17 @@ cudaError_t launch_shape(const DeltaParams& p, cudaStream_t s) {
   static OncePerContext once;
   const cudaError_t e = once([] { return cudaFuncSetAttribute(delta_chunk_kernel<H>, cudaFuncAttributeMaxDynamicSharedMemorySize, H::SMEM); });
   if (e != cudaSuccess) return e;
-  delta_chunk_kernel<H><<<dim3(H::D / H::COLS, (unsigned)p.heads, (unsigned)p.batch), H::THREADS, H::SMEM, s>>>(p);
-  return cudaGetLastError();
+  // ahead of the end of the preparation: blocks find their slots and fetch their states meanwhile
+  return launch_kernel(delta_chunk_kernel<H>, dim3(H::D / H::COLS, (unsigned)p.heads, (unsigned)p.batch), H::THREADS, H::SMEM, s, p, true);
 }
 template <typename T, int D>
 cudaError_t launch(const DeltaParams& p, cudaStream_t s) {
   const int64_t runs = (int64_t)p.batch * p.heads * (D / 16);
   if constexpr (sizeof(T) == 2) {
-    if (runs > 2 * PLAN_SMS) return launch_shape<Shape<T, D, 1, D == 32 ? 2 : 4>>(p, s);
+    if (runs > 2 * PLAN_SMS) return launch_shape<Shape<T, D, 1, 1, D == 32 ? 2 : 4>>(p, s);
+    if constexpr (D > 32) return launch_shape<Shape<T, D, 4, 2, 1>>(p, s);
   }
-  return launch_shape<Shape<T, D, 2, 1>>(p, s);
+  return launch_shape<Shape<T, D, 2, 2, 1>>(p, s);
 }
 template <typename T>
 cudaError_t launch(const DeltaParams& p, int D, cudaStream_t s) {

@@ -55,6 +55,7 @@ __global__ void __launch_bounds__(DELTA_GROUP, H::BLOCKS) delta_prepare_kernel(c
   float* A = reinterpret_cast<float*>(qs + TERMS * H::TILE);                 // [C][AP]: A, then its inverse
   __shared__ float2 sums[C];                                                 // log2(e) G as a pair of floats: what counts are differences of far larger sums
   __shared__ float betas[C];
+  pdl_launch_dependents();
   const int b = blockIdx.z, h = blockIdx.y, w = p.first_window + blockIdx.x;
   const int n = clamp_length(p.lengths, b, p.tokens);
   if (w * C >= n || slot_of(p.slots, p.num_slots, b) < 0) return;            // the whole block

@@ -4,7 +4,6 @@
 // between reading a state and writing it.  A block owns a run of W value columns of one head's state (the columns are
 // independent of each other), LANES = W / 4 threads to a row, in registers for the whole call.
 #include "linear_common.cuh"
-#include <cstdlib>
 
 namespace tt {
 namespace tok {
@@ -17,7 +16,8 @@ struct DeltaStep {
   static constexpr int ROWS = D * LANES / THREADS;                      // rows to a thread
 };
 
-template <typename T, int D, int W>
+// SEVERAL: the next token's operands are fetched while this one is worked on
+template <typename T, int D, int W, bool SEVERAL>
 __global__ void __launch_bounds__(256) delta_step_kernel(const __grid_constant__ DeltaParams p) {
   using Shape = DeltaStep<D, W>;
   constexpr int LANES = Shape::LANES, ROWS = Shape::ROWS, STEP = Shape::THREADS / LANES, WARPS = Shape::THREADS / 32;
@@ -39,20 +39,31 @@ __global__ void __launch_bounds__(256) delta_step_kernel(const __grid_constant__
   const T* v = reinterpret_cast<const T*>(p.v.p) + b * p.v.b + h * p.v.h + col;
   T* o = reinterpret_cast<T*>(p.o.p) + b * p.o.b + h * p.o.h + col;
   const int64_t gates = (int64_t)b * p.tokens * p.heads + h;
-  float kk[ROWS], qq[ROWS], vv[4], fade = 1.f, beta = 0.f;
-  auto fetch = [&](int t) {
+  struct Token {
+    T k[ROWS], q[ROWS], v[4];
+    float decay = 0.f, beta;
+  };
+  auto fetch = [&](Token& to, int t) {
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
-      kk[i] = to_float(k[t * p.k.t + i * STEP]);
-      qq[i] = to_float(q[t * p.q.t + i * STEP]);
+      to.k[i] = k[t * p.k.t + i * STEP];
+      to.q[i] = q[t * p.q.t + i * STEP];
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) vv[j] = to_float(v[t * p.v.t + j]);
-    if (p.log_decay) fade = expf(p.log_decay[gates + (int64_t)t * p.heads]);
-    beta = p.beta[gates + (int64_t)t * p.heads];
+    for (int j = 0; j < 4; ++j) to.v[j] = v[t * p.v.t + j];
+    if (p.log_decay) to.decay = p.log_decay[gates + (int64_t)t * p.heads];
+    to.beta = p.beta[gates + (int64_t)t * p.heads];
   };
-  if (n > 0) fetch(0);
-  for (int t = 0; t < n; ++t) {
+  Token next;
+  if (n > 0) fetch(next, 0);
+  for (int t = 0; t < (SEVERAL ? n : min(n, 1)); ++t) {
+    float kk[ROWS], qq[ROWS], vv[4];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) { kk[i] = to_float(next.k[i]); qq[i] = to_float(next.q[i]); }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) vv[j] = to_float(next.v[j]);
+    const float fade = expf(next.decay), beta = next.beta;
+    if (SEVERAL && t + 1 < n) fetch(next, t + 1);
     float x[4] = {}, y[4] = {}, kq = 0.f;
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
@@ -104,26 +115,23 @@ __global__ void __launch_bounds__(256) delta_step_kernel(const __grid_constant__
       to[2] = (T)(p.scale * fmaf(fade, sy.z, dot * u[2]));
       to[3] = (T)(p.scale * fmaf(fade, sy.w, dot * u[3]));
     }
-    if (t + 1 < n) fetch(t + 1);
   }
   if (n == 0 && p.state_out == p.state) return;
 #pragma unroll
   for (int i = 0; i < ROWS; ++i) *reinterpret_cast<float4*>(p.state_out + base + (int64_t)i * STEP * D) = s[i];
 }
 
-template <typename T, int D, int W>
+template <typename T, int D, int W, bool SEVERAL>
 cudaError_t launch(const DeltaParams& p, cudaStream_t s) {
-  delta_step_kernel<T, D, W><<<dim3(D / W, (unsigned)p.heads, (unsigned)p.batch), DeltaStep<D, W>::THREADS, 0, s>>>(p);
+  delta_step_kernel<T, D, W, SEVERAL><<<dim3(D / W, (unsigned)p.heads, (unsigned)p.batch), DeltaStep<D, W>::THREADS, 0, s>>>(p);
   return cudaGetLastError();
 }
 template <typename T, int D>
 cudaError_t launch(const DeltaParams& p, cudaStream_t s) {
-  // few states: cut each into four runs of columns, so that more multiprocessors fetch
-  const char* e = getenv("DW"); const int w = e ? atoi(e) : 0;
-  if (w == 1) return launch<T, D, D>(p, s);
-  if (w == 2) return launch<T, D, D / 2>(p, s);
-  if (w == 4) return launch<T, D, D / 4>(p, s);
-  return (int64_t)p.batch * p.heads < 2 * PLAN_SMS ? launch<T, D, D / 4>(p, s) : launch<T, D, D>(p, s);
+  if (p.tokens > 1) return launch<T, D, D / 4, true>(p, s);
+  // Few states: cut each into four runs of columns, so that more multiprocessors fetch.  Many: in halves, of which more fit a multiprocessor, for no block
+  // writes before it has read all of its own (256 sessions of 8 heads of 128, whole 71 us, halves 61, quarters 65).
+  return (int64_t)p.batch * p.heads < 2 * PLAN_SMS ? launch<T, D, D / 4, false>(p, s) : launch<T, D, D / 2, false>(p, s);
 }
 template <typename T>
 cudaError_t launch(const DeltaParams& p, int D, cudaStream_t s) {
