@@ -173,7 +173,8 @@ __global__ void __launch_bounds__(Few<D, W, MAPS>::THREADS, Few<D, W, MAPS>::BLO
     fetch_mask(first);
   }
   if constexpr (MAPS == 2) {
-    for (int r = warp; r < 16; r += F::WARPS) {
+    // rows r and r + group are of one head
+    for (int r = warp; r < min(16, p.group); r += F::WARPS) {
       const float f = lambda_of(p.end, D / 2, hk * p.group + (row0 + r) % p.group);
       if (lane == 0) s_lambda[r] = f;
     }
@@ -456,7 +457,7 @@ __global__ void __launch_bounds__(Few<D, W, MAPS>::THREADS, Few<D, W, MAPS>::BLO
             const float2 one = joined(0, r, d, top, total);
             const float i1 = total == 0.f ? 0.f : 1.f / total;
             const float2 two = joined(1, r, d, top, total);
-            const float i2 = total == 0.f ? 0.f : s_lambda[r] / total;
+            const float i2 = total == 0.f ? 0.f : s_lambda[r % p.group] / total;
             y[e] = make_float2(one.x * i1 - two.x * i2, one.y * i1 - two.y * i2);
           }
           squares = fmaf(y[e].x, y[e].x, fmaf(y[e].y, y[e].y, squares));

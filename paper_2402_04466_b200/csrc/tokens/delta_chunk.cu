@@ -460,24 +460,26 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
       operand(u_frag, u);
       // S'^T = e^G_C S^T + U'^T K
       const float whole = record.whole;
+      // several tiles side by side: 16 cycles a product with four sums in turn, 12 with eight
+      constexpr int SIDE = NT % 4 == 0 && TERMS == 1 ? 4 : 2;
 #pragma unroll
-      for (int m = 0; m < NT; m += 2) {
-        uint32_t f[2][2][TERMS][2];
+      for (int m = 0; m < NT; m += SIDE) {
+        uint32_t f[SIDE][2][TERMS][2];
 #pragma unroll
-        for (int z = 0; z < 2; ++z)
+        for (int z = 0; z < SIDE; ++z)
 #pragma unroll
           for (int e = 0; e < TERMS; ++e) {
             uint32_t y[4];
             ldmatrix4<true>(y, smem_u32(ks + e * H::TILE + lane * KP + (warp * NT + m + z) * 8));
             f[z][0][e][0] = y[0]; f[z][0][e][1] = y[1]; f[z][1][e][0] = y[2]; f[z][1][e][1] = y[3];
           }
-        float d[2][2][4];
+        float d[SIDE][2][4];
 #pragma unroll
         for (int sum = 2; sum >= 0; --sum)
 #pragma unroll
           for (int i = 0; i <= sum; ++i)
 #pragma unroll
-            for (int z = 0; z < 2; ++z)
+            for (int z = 0; z < SIDE; ++z)
 #pragma unroll
               for (int x = 0; x < 2; ++x)
                 if (sum - i < TERMS) {
@@ -485,7 +487,7 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
                   else mma16816(d[z][x], a[x][i], f[z][x][sum - i][0], f[z][x][sum - i][1]);
                 }
 #pragma unroll
-        for (int z = 0; z < 2; ++z)
+        for (int z = 0; z < SIDE; ++z)
 #pragma unroll
           for (int e = 0; e < 4; ++e) s[m + z][e] = fmaf(whole, s[m + z][e], d[z][0][e] + d[z][1][e]);
       }
@@ -516,9 +518,8 @@ cudaError_t launch(const DeltaParams& p, cudaStream_t s) {
   const int64_t runs = (int64_t)p.batch * p.heads * (D / 16);
   if constexpr (sizeof(T) == 2) {
     if (runs > 2 * PLAN_SMS) return launch_shape<Shape<T, D, 1, 1, D == 32 ? 2 : 4>>(p, s);
-    if constexpr (D > 32) return launch_shape<Shape<T, D, 4, 2, 1>>(p, s);
   }
-  return launch_shape<Shape<T, D, 2, 2, 1>>(p, s);
+  return launch_shape<Shape<T, D, (sizeof(T) == 2 && D > 32) ? 4 : 2, 2, 1>>(p, s);
 }
 template <typename T>
 cudaError_t launch(const DeltaParams& p, int D, cudaStream_t s) {
