@@ -22,12 +22,12 @@ namespace {
 constexpr int THREADS = 256;           // 16 x 16
 constexpr int BN = 64;                 // keys of a tile
 
-template <int D, int BM>
+template <int D, int BM, int MAPS>
 struct Shape {
   static constexpr int A = BM / 16;                     // rows to a thread
   static constexpr int N = BN / 16;                     // keys to a thread
   static constexpr int E = D / 16;                      // columns to a thread
-  static constexpr int QP = D + 4, PP = BN + 4;
+  static constexpr int QP = D + 4, PP = MAPS * BN + 4;   // weights of two maps lie side by side
   static constexpr int KV = BN * (QP + D);              // a tile's keys and values, of which two are in shared memory
   static constexpr size_t smem = sizeof(float) * (BM * QP + 2 * KV + BM * PP);
 };
@@ -41,8 +41,8 @@ __device__ __forceinline__ bool all_finite(float4 f) {
 }
 
 template <int D, int BM, int MAPS>
-__global__ void __launch_bounds__(THREADS) cross_kernel(const __grid_constant__ ParamsOf<MAPS> p) {
-  using S = Shape<D, BM>;
+__global__ void __launch_bounds__(THREADS, MAPS == 2 && D == 32 && BM == 64 ? 2 : 0) cross_kernel(const __grid_constant__ ParamsOf<MAPS> p) {
+  using S = Shape<D, BM, MAPS>;
   constexpr int A = S::A, N = S::N, E = S::E, QP = S::QP, PP = S::PP;
   extern __shared__ float4 raw[];
   float* qs = reinterpret_cast<float*>(raw);
@@ -74,6 +74,12 @@ __global__ void __launch_bounds__(THREADS) cross_kernel(const __grid_constant__ 
 #pragma unroll
       for (int c = 0; c < E / 2; ++c) o[w][a][c] = pack2(0.f, 0.f);
     }
+  Two both[MAPS == 2 ? A : 1][MAPS == 2 ? E : 1];      // of two maps: a column's sums of either
+  if (MAPS == 2)
+#pragma unroll
+    for (int a = 0; a < (MAPS == 2 ? A : 1); ++a)
+#pragma unroll
+      for (int c = 0; c < (MAPS == 2 ? E : 1); ++c) both[a][c] = pack2(0.f, 0.f);
   auto fetch = [&](int j, float* dst) {
     for (int i = threadIdx.x; i < BN * (D / 4); i += THREADS) {
       const int r = i / (D / 4), c = i % (D / 4) * 4;
@@ -94,109 +100,190 @@ __global__ void __launch_bounds__(THREADS) cross_kernel(const __grid_constant__ 
       for (int i = threadIdx.x; i < BN * (D / 4); i += THREADS) odd |= !all_finite(*reinterpret_cast<const float4*>(vs + i * 4));      // its own copies
     const bool careful = __syncthreads_or(odd) && p.mask;      // the tile is there, and the one before has been read: the next one takes its place
     if (j + BN < j1) fetch(j + BN, kv + ((j - j0) / BN + 1 & 1) * S::KV);
+    float s[MAPS][A][N];
 #pragma unroll
     for (int w = 0; w < MAPS; ++w) {
-      if (w > 0) __syncwarp();           // the last map's weights have been read
-      float s[A][N];
-      {
-        Two acc[A][N];                   // even and odd elements
+      Two acc[A][N];                   // even and odd elements
 #pragma unroll
-        for (int a = 0; a < A; ++a)
+      for (int a = 0; a < A; ++a)
 #pragma unroll
-          for (int c = 0; c < N; ++c) acc[a][c] = pack2(0.f, 0.f);
+        for (int c = 0; c < N; ++c) acc[a][c] = pack2(0.f, 0.f);
 #pragma unroll 4
-        for (int e = w * (D / MAPS); e < (w + 1) * (D / MAPS); e += 4) {
-          ulonglong2 x[A], y[N];
+      for (int e = w * (D / MAPS); e < (w + 1) * (D / MAPS); e += 4) {
+        ulonglong2 x[A], y[N];
 #pragma unroll
-          for (int a = 0; a < A; ++a) x[a] = *reinterpret_cast<const ulonglong2*>(qs + (ty + 16 * a) * QP + e);
+        for (int a = 0; a < A; ++a) x[a] = *reinterpret_cast<const ulonglong2*>(qs + (ty + 16 * a) * QP + e);
 #pragma unroll
-          for (int c = 0; c < N; ++c) y[c] = *reinterpret_cast<const ulonglong2*>(ks + (tx + 16 * c) * QP + e);
-#pragma unroll
-          for (int a = 0; a < A; ++a)
-#pragma unroll
-            for (int c = 0; c < N; ++c) acc[a][c] = fma2_of(x[a].y, y[c].y, fma2_of(x[a].x, y[c].x, acc[a][c]));
-        }
+        for (int c = 0; c < N; ++c) y[c] = *reinterpret_cast<const ulonglong2*>(ks + (tx + 16 * c) * QP + e);
 #pragma unroll
         for (int a = 0; a < A; ++a)
 #pragma unroll
-          for (int c = 0; c < N; ++c) {
-            float lo, hi;
-            unpack2(acc[a][c], lo, hi);
-            s[a][c] = lo + hi;
-          }
+          for (int c = 0; c < N; ++c) acc[a][c] = fma2_of(x[a].y, y[c].y, fma2_of(x[a].x, y[c].x, acc[a][c]));
       }
-      const bool whole = !p.mask && j + BN <= j1;      // every key of the tile is seen by every row
 #pragma unroll
-      for (int a = 0; a < A; ++a) {
-        bool seen[N];
+      for (int a = 0; a < A; ++a)
 #pragma unroll
-        for (int c = 0; c < N; ++c) seen[c] = true;
-        if (!whole) {
-          const int row = row0 + ty + 16 * a;
-          const uint8_t* mask = p.mask && row < rows ? p.mask + b * p.mask_b + (int64_t)(row / p.group) * p.mask_q + j : nullptr;
-#pragma unroll
-          for (int c = 0; c < N; ++c) {
-            const int at = tx + 16 * c;
-            seen[c] = j + at < j1 && (!mask || mask[at]);
-            if (!seen[c]) s[a][c] = -INFINITY;
-          }
+        for (int c = 0; c < N; ++c) {
+          float lo, hi;
+          unpack2(acc[a][c], lo, hi);
+          s[w][a][c] = lo + hi;
         }
-        float top = s[a][0];
+    }
+    const bool whole = !p.mask && j + BN <= j1;      // every key of the tile is seen by every row
 #pragma unroll
-        for (int c = 1; c < N; ++c) top = fmaxf(top, s[a][c]);
+    for (int a = 0; a < A; ++a) {
+      bool seen[N];
+#pragma unroll
+      for (int c = 0; c < N; ++c) seen[c] = true;
+      if (!whole) {
+        const int row = row0 + ty + 16 * a;
+        const uint8_t* mask = p.mask && row < rows ? p.mask + b * p.mask_b + (int64_t)(row / p.group) * p.mask_q + j : nullptr;
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+          const int at = tx + 16 * c;
+          seen[c] = j + at < j1 && (!mask || mask[at]);
+          if (!seen[c])
+#pragma unroll
+            for (int w = 0; w < MAPS; ++w) s[w][a][c] = -INFINITY;
+        }
+      }
+      if constexpr (MAPS == 1) {
+        float top = s[0][a][0];
+#pragma unroll
+        for (int c = 1; c < N; ++c) top = fmaxf(top, s[0][a][c]);
 #pragma unroll
         for (int x = 8; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
         top *= p.scale_log2;
-        const float now = fmaxf(m[w][a], top), base = now == -INFINITY ? 0.f : now;
-        const float fade = exp2_fast(m[w][a] - base);
-        m[w][a] = now;
+        const float now = fmaxf(m[0][a], top), base = now == -INFINITY ? 0.f : now;
+        const float fade = exp2_fast(m[0][a] - base);
+        m[0][a] = now;
         float add = 0.f;
 #pragma unroll
         for (int c = 0; c < N; ++c) {
-          const float weight = seen[c] ? exp2_fast(fmaf(s[a][c], p.scale_log2, -base)) : -0.f;
+          const float weight = seen[c] ? exp2_fast(fmaf(s[0][a][c], p.scale_log2, -base)) : -0.f;
           add += weight;
           ps[(ty + 16 * a) * PP + tx + 16 * c] = weight;
         }
-        l[w][a] = fmaf(l[w][a], fade, add);    // this thread's share of the keys
+        l[0][a] = fmaf(l[0][a], fade, add);    // this thread's share of the keys
         const Two f2 = pack2(fade, fade);
 #pragma unroll
-        for (int c = 0; c < E / 2; ++c) o[w][a][c] = mul2_of(o[w][a][c], f2);
-      }
-      __syncwarp();                      // a row's 16 threads are half a warp
-      if (!careful) {
-#pragma unroll 2
-        for (int i = 0; i < BN; i += 4) {  // four keys: a row's weights in one load
-          float4 row4[A];
-#pragma unroll
-          for (int a = 0; a < A; ++a) row4[a] = *reinterpret_cast<const float4*>(ps + (ty + 16 * a) * PP + i);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            Two y[E / 2];
-            load_pairs<D>(vs + (i + k) * D, tx, y);
-#pragma unroll
-            for (int a = 0; a < A; ++a) {
-              const float x = k == 0 ? row4[a].x : k == 1 ? row4[a].y : k == 2 ? row4[a].z : row4[a].w;
-              const Two x2 = pack2(x, x);
-#pragma unroll
-              for (int c = 0; c < E / 2; ++c) o[w][a][c] = fma2_of(x2, y[c], o[w][a][c]);
-            }
-          }
-        }
+        for (int c = 0; c < E / 2; ++c) o[0][a][c] = mul2_of(o[0][a][c], f2);
       } else {
-#pragma unroll 1
-        for (int i = 0; i < BN; ++i) {
-          Two y[E / 2];
-          load_pairs<D>(vs + i * D, tx, y);
+        // The maxima only move when a weight would pass 2^8: sixteen threads to a row agree on them by four shuffles each.
+        float top[2];
 #pragma unroll
-          for (int a = 0; a < A; ++a) {
-            const float x = ps[(ty + 16 * a) * PP + i];
-            if (!signbit(x))
+        for (int w = 0; w < 2; ++w) {
+          top[w] = s[w][a][0];
 #pragma unroll
-              for (int c = 0; c < E / 2; ++c) o[w][a][c] = fma2_of(pack2(x, x), y[c], o[w][a][c]);
+          for (int c = 1; c < N; ++c) top[w] = fmaxf(top[w], s[w][a][c]);
+          top[w] *= p.scale_log2;
+        }
+        if (__any_sync(0xFFFFFFFFu, top[0] > m[0][a] + 8.f || top[1] > m[1][a] + 8.f)) {
+          float fade[2];
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+#pragma unroll
+            for (int x = 8; x > 0; x >>= 1) top[w] = fmaxf(top[w], __shfl_xor_sync(0xFFFFFFFFu, top[w], x));
+            const float now = fmaxf(m[w][a], top[w]);
+            fade[w] = now == -INFINITY ? 1.f : exp2_fast(m[w][a] - now);
+            m[w][a] = now;
+            l[w][a] *= fade[w];
           }
+          const Two f2 = pack2(fade[0], fade[1]);
+#pragma unroll
+          for (int c = 0; c < E; ++c) both[a][c] = mul2_of(both[a][c], f2);
+        }
+        const float base[2] = {m[0][a] == -INFINITY ? 0.f : m[0][a], m[1][a] == -INFINITY ? 0.f : m[1][a]};
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+          float weight[2];
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+            weight[w] = seen[c] ? exp2_fast(fmaf(s[w][a][c], p.scale_log2, -base[w])) : -0.f;
+            l[w][a] += weight[w];
+          }
+          *reinterpret_cast<float2*>(ps + (ty + 16 * a) * PP + 2 * (tx + 16 * c)) = make_float2(weight[0], weight[1]);
         }
       }
     }
+    __syncwarp();                      // a row's 16 threads are half a warp
+    if constexpr (MAPS == 2) {
+      // both maps' weights of two keys in one load, as the pairs that the multiply-adds take
+      auto add_up = [&](auto some) {           // some: not every key of every row
+#pragma unroll 2
+        for (int i = 0; i < BN; i += 2) {
+          Two y[2][E / 2], column[2][E];
+          load_pairs<D>(vs + i * D, tx, y[0]);
+          load_pairs<D>(vs + (i + 1) * D, tx, y[1]);
+#pragma unroll
+          for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int c = 0; c < E / 2; ++c) {
+              float lo, hi;
+              unpack2(y[k][c], lo, hi);
+              column[k][2 * c] = pack2(lo, lo);
+              column[k][2 * c + 1] = pack2(hi, hi);
+            }
+#pragma unroll
+          for (int a = 0; a < A; ++a) {
+            const ulonglong2 x = *reinterpret_cast<const ulonglong2*>(ps + (ty + 16 * a) * PP + 2 * i);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const Two w2 = k == 0 ? x.x : x.y;
+              if (!decltype(some)::value || (w2 >> 31 & 1) == 0)      // a weight of -0 is of a key that the row does not see
+#pragma unroll
+                for (int c = 0; c < E; ++c) both[a][c] = fma2_of(w2, column[k][c], both[a][c]);
+            }
+          }
+        }
+      };
+      if (careful) add_up(std::true_type{});
+      else add_up(std::false_type{});
+    } else if (!careful) {
+#pragma unroll 2
+      for (int i = 0; i < BN; i += 4) {  // four keys: a row's weights in one load
+        float4 row4[A];
+#pragma unroll
+        for (int a = 0; a < A; ++a) row4[a] = *reinterpret_cast<const float4*>(ps + (ty + 16 * a) * PP + i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          Two y[E / 2];
+          load_pairs<D>(vs + (i + k) * D, tx, y);
+#pragma unroll
+          for (int a = 0; a < A; ++a) {
+            const float x = k == 0 ? row4[a].x : k == 1 ? row4[a].y : k == 2 ? row4[a].z : row4[a].w;
+            const Two x2 = pack2(x, x);
+#pragma unroll
+            for (int c = 0; c < E / 2; ++c) o[0][a][c] = fma2_of(x2, y[c], o[0][a][c]);
+          }
+        }
+      }
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < BN; ++i) {
+        Two y[E / 2];
+        load_pairs<D>(vs + i * D, tx, y);
+#pragma unroll
+        for (int a = 0; a < A; ++a) {
+          const float x = ps[(ty + 16 * a) * PP + i];
+          if (!signbit(x))
+#pragma unroll
+            for (int c = 0; c < E / 2; ++c) o[0][a][c] = fma2_of(pack2(x, x), y[c], o[0][a][c]);
+        }
+      }
+    }
+  }
+  if constexpr (MAPS == 2) {
+#pragma unroll
+    for (int a = 0; a < A; ++a)
+#pragma unroll
+      for (int c = 0; c < E / 2; ++c) {
+        float x[2][2];
+        unpack2(both[a][2 * c], x[0][0], x[1][0]);
+        unpack2(both[a][2 * c + 1], x[0][1], x[1][1]);
+        o[0][a][c] = pack2(x[0][0], x[0][1]);
+        o[1][a][c] = pack2(x[1][0], x[1][1]);
+      }
   }
   if (MAPS == 1 || p.splits > 1) {
 #pragma unroll
@@ -309,7 +396,7 @@ __global__ void __launch_bounds__(128) cross_join_kernel(const __grid_constant__
 
 template <int D, int BM, int MAPS>
 cudaError_t launch_scalar(const ParamsOf<MAPS>& p, cudaStream_t s) {
-  const size_t smem = Shape<D, BM>::smem;
+  const size_t smem = Shape<D, BM, MAPS>::smem;
   static OncePerContext once;
   cudaError_t e = once([&] { return cudaFuncSetAttribute(cross_kernel<D, BM, MAPS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
   if (e != cudaSuccess) return e;
