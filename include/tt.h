@@ -608,7 +608,7 @@ tt_status tt_cross_attention(const tt_cross_attention_args* args, void* cuda_str
  * What a query sees, the lengths, the mask, scale (usually (head_dim / 2)^-0.5), status_dev and scratch are as in tt_cross_attention, and the same for both maps.  A
  * query that sees nothing gets zeros.  What a query does not see has no influence on its row; an infinity or NaN among the values that it sees makes the
  * elements of y_i that read it not finite (with the norm, which reads them all, no element of the row says anything).
- * TT_BF16 weights count with 16 bits, but are rounded to bf16 in large calls of more than 64 queries without a mask (y is then off by up to 2e-3 of the two sums'
+ * TT_BF16 weights count with 16 bits, but are rounded to bf16 in large calls of more than 32 queries without a mask (y is then off by up to 2e-3 of the two sums'
  * size); their sums are of the weights before that.
  */
 typedef struct {

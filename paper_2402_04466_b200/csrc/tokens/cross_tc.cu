@@ -53,6 +53,9 @@ struct Cfg {
   // turns at their exponentials, and one does the rest of its work meanwhile (276 us where both at once take 306; with heads of 128, whose
   // products take as long as the exponentials, 241 with turns and 226 without).
   static constexpr bool TURNS = D != 128;
+  // Differential attention with heads of 128 has twice as many exponentials to its products: one in four is taken on the fp32 units (396 us where none is 412, a third 396; with
+  // heads of up to 64, whose scores leave no registers for it, a quarter of them took 583 instead of 546).
+  static constexpr bool POLYNOMIAL = MAPS == 2 && D == 128;
   static constexpr int HALVES = BN / 64;                            // weights are handed over 64 keys at a time
   static constexpr int PLACES = D == 128 ? 2 : 1;                   // of a tile's weights: those of one tile of keys are made while the last ones' product runs
   static constexpr int QTILES = TILES / MAPS, ROWS = QTILES * BM;   // of queries
@@ -69,6 +72,30 @@ struct Cfg {
   static constexpr int PROWS = TILES * BM;                          // rows of a partial result, of either map
   static constexpr int64_t PART = (int64_t)PROWS * (D + 2);         // its floats
   static_assert(O_COL + TILES * D <= TMEM && SMEM + 6 * 1024 <= 227 * 1024, "tensor and shared memory");
+};
+
+// 2^lo and 2^hi on the fp32 units, to 4 10^-6: the nearest whole number n goes to the exponent (Cody and Waite), and 2^f, |f| <= 1/2, is the polynomial of degree 4 through its
+// values at the Chebyshev points.  Arguments are below 2^7; what is below -127 becomes 2^-127, and a NaN stays one.
+constexpr float P0 = 1.f, P1 = 0.693121045f, P2 = 0.24022349f, P3 = 0.0559219758f, P4 = 0.00966636852f;
+struct Polynomial {
+  Two p0, p1, p2, p3, p4, magic;
+  // A pair of constants, from when `now` is known: what the compiler may make at any time it keeps in registers throughout, of which there are none left.
+  static __device__ __forceinline__ Two pair_of(float x, uint32_t now) {
+    Two r;
+    asm("mov.b64 %0, {%1, %1};  // %2" : "=l"(r) : "f"(x), "r"(now));
+    return r;
+  }
+  __device__ __forceinline__ explicit Polynomial(uint32_t now)
+      : p0(pair_of(P0, now)), p1(pair_of(P1, now)), p2(pair_of(P2, now)), p3(pair_of(P3, now)), p4(pair_of(P4, now)), magic(pair_of(12582912.f + 127.f, now)) {}      // 1.5 2^23: a sum's last bits are n + 127
+  __device__ __forceinline__ void operator()(float& lo, float& hi) const {
+    asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(lo));
+    asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(hi));
+    const Two a = pack2(lo, hi), t = add2_of(a, magic), f = sub2_of(a, sub2_of(t, magic));
+    float t0, t1;
+    unpack2(t, t0, t1);
+    const Two y = fma2_of(fma2_of(fma2_of(fma2_of(p4, f, p3), f, p2), f, p1), f, p0);
+    unpack2(mul2_of(y, pack2(__uint_as_float(__float_as_uint(t0) << 23), __uint_as_float(__float_as_uint(t1) << 23))), lo, hi);
+  }
 };
 
 // The launch's work: iterations (tile of queries x tile of keys) in the order entry, head, tile of queries, tile of keys.
@@ -430,13 +457,18 @@ __global__ void __launch_bounds__(Cfg<D, MAPS>::THREADS, 1) cross_tc_kernel(cons
 #pragma unroll
       for (int i = 0; i < C::BN / 32; ++i) {
         uint32_t w[16];
+        const Polynomial polynomial(v[i][0]);
 #pragma unroll
         for (int x = 0; x < 16; ++x) {
           float lo, hi;
           const unsigned long long a = fma2_of(pack2(__uint_as_float(v[i][2 * x]), __uint_as_float(v[i][2 * x + 1])), c2, mc2);
           unpack2(a, lo, hi);
-          lo = exp2_fast(lo);
-          hi = exp2_fast(hi);
+          if (C::POLYNOMIAL && x % 4 == 3) {
+            polynomial(lo, hi);
+          } else {
+            lo = exp2_fast(lo);
+            hi = exp2_fast(hi);
+          }
           l[x & 3] = add2_of(l[x & 3], pack2(lo, hi));
           w[x] = pack_bf16(lo, hi);
         }

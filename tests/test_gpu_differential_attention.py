@@ -40,7 +40,7 @@ def _case(dev, seed, B, Tq, Tk, H, K, D, dtype, layout="plain", sharp=1.0, each=
 
 def _once(Tq, dtype, mask):
     """How weights may be rounded: to 16 bits, in large calls without a mask to bf16."""
-    return 0.0 if dtype == FP32 else 2.0 ** -16 if Tq <= 64 or mask is not None else 2.0 ** -8
+    return 0.0 if dtype == FP32 else 2.0 ** -16 if Tq <= 32 or mask is not None else 2.0 ** -8
 
 
 def _check(got, q, k, v, vectors, init, name, scale=None, n=None, mask=None, rows=None, **kw):
@@ -65,7 +65,7 @@ def test_differential_attention(cuda_device, dtype, B, Tq, Tk, H, K, D):
         _check(got, q, k, v, vectors, init, layout, **kw)
 
 
-@pytest.mark.parametrize("B,Tq,Tk,H,K,D", [(2, 1100, 1300, 4, 4, 64), (2, 700, 2049, 2, 1, 128), (3, 999, 1500, 4, 2, 32), (1, 4000, 700, 2, 2, 64), (5, 150, 4800, 2, 2, 128),
+@pytest.mark.parametrize("B,Tq,Tk,H,K,D", [(2, 1100, 1300, 4, 4, 64), (2, 700, 2049, 2, 1, 128), (3, 999, 1500, 4, 2, 32), (1, 4000, 700, 2, 2, 64), (5, 150, 4800, 2, 2, 128), (3, 33, 14400, 4, 2, 128), (8, 40, 9001, 4, 4, 64),
                                            (300, 70, 130, 2, 2, 64)])
 def test_many_queries(cuda_device, B, Tq, Tk, H, K, D):
     q, k, v, vectors, w = _case(cuda_device, Tq, B, Tq, Tk, H, K, D, BF16, "fused", each=True)
