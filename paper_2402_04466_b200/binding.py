@@ -932,7 +932,7 @@ def differential_attention(q, k, v, lambda_vectors, lambda_init: float, scale: O
     _, Tk, Hk, _ = kv_shape
     if v.shape != kv_shape or kv_shape != (B, Tk, Hk, D) or out.shape != shape:
         _refuse("q, k, v and out do not fit together")
-    each = lambda_vectors.dim() == 3
+    each = lambda_vectors is not None and lambda_vectors.dim() == 3
     vectors = _array("lambda_vectors", lambda_vectors, th.f32, device, (H, 4, D // 2) if each else (4, D // 2))
     args = _DIFF_ARGS.pack(_DIFF_ARGS.size, prec, B, Tq, Tk, H, Hk, D, (D / 2) ** -0.5 if scale is None else scale, lambda_init, eps,
                            (1 - lambda_init if norm else 1.0) if out_scale is None else out_scale, norm, 0, *views, vectors, 2 * D if each else 0,

@@ -39,9 +39,10 @@ def delta(q, k, v, log_decay, beta, state, scale=1.0, lengths=None):
 
 
 def bounds(out, size, state_size, D, T, dtype, several):
-    """A token's own roundings: its sums of D products (half a step each when rounded, a whole one where an adder cuts off) with chunks of up to 64 tokens, of which two
-    in a row are taken where a chunk's inverse is; the number of tokens whose errors add up is what their decay leaves of T, and independent
-    errors add up as the root of that.  With several bf16 tokens the weights within a chunk are rounded to bf16 once."""
+    """A token's own roundings: its sums of D products (half a step each when rounded, a whole one where an adder cuts off) with windows of up to 64 tokens, of which two
+    in a row are taken where a window's inverse is; the number of tokens whose errors add up is what their decay leaves of T, and independent
+    errors add up as the root of that.  Of several bf16 tokens out reads the state, the corrections of a window and their weights with 16 bits each, which is off by up to
+    2^-15, and a window's corrections are up to 32 of the column's length: 3 * 32 * 2^-15 of it are less than 2^-8."""
     n = (2 * D + 2 * 64 + 16) * max(1.0, T) ** 0.5 / 4
     # what fades below fp32's normal range (2^-126, whole steps of 2^-149) keeps fewer bits, the factor exp(log_decay) itself among it
     low = 2.0 ** -126

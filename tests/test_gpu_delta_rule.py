@@ -82,10 +82,10 @@ def test_delta_rule(cuda_device, dtype, B, T, H, K, D):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("T", [1, 2, 60, 65, 400])
-@pytest.mark.parametrize("D", [64, 128])
-def test_slots_and_lengths(cuda_device, dtype, T, D):
+@pytest.mark.parametrize("H,D", [(2, 64), (2, 128), (40, 32), (14, 64), (8, 128)])
+def test_slots_and_lengths(cuda_device, dtype, T, H, D):
     """Slots in any order; entries without tokens, of one, of all and of more; rows behind the last token hold NaN and stay as they are, as do slots that no entry has."""
-    B, H, n = 9, 2, 13
+    B, n = 9, 13
     q, k, v, decay, beta, state = _case(cuda_device, T, B, T, H, 1, D, dtype, "fused", slots=n)
     want_lengths = [T, 0, 1, T // 2, T + 7, -3, T, T, T]
     slots = torch.tensor([4, 12, 0, 7, 9, 3, 4, -1, 13], dtype=torch.int32, device=cuda_device)      # the sixth takes the first's, two are out of range
@@ -171,11 +171,11 @@ def test_long_sequences(cuda_device, dtype, B, T, H, D):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("H,D", [(2, 32), (2, 64), (2, 128), (40, 32), (20, 64), (10, 128)])
 @pytest.mark.parametrize("T", [1, 130])
-def test_what_is_not_finite_goes_where_the_formula_takes_it(cuda_device, dtype, D, T):
+def test_what_is_not_finite_goes_where_the_formula_takes_it(cuda_device, dtype, H, D, T):
     """An infinity or NaN in q makes its own row of out not finite, one in v its column, one in k or a gate its head, each from its token on; nothing before it."""
-    B, H = 6, 2
+    B = 6
     for seed, at in ((0, 0), (1, T // 2), (2, T - 1)):
         q, k, v, decay, beta, state = _case(cuda_device, seed + D, B, T, H, H, D, dtype)
         k[k == 0] = 0.01
@@ -194,6 +194,27 @@ def test_what_is_not_finite_goes_where_the_formula_takes_it(cuda_device, dtype, 
         for got, exact, off in ((out, want, bound), (new, S, state_bound)):
             fine = torch.isfinite(exact) & torch.isfinite(off)
             check(got[fine], exact[fine], off[fine], "finite part")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,T,H,D", [(64, 1000, 8, 32), (70, 70, 190, 32), (24, 1700, 10, 64)])
+def test_more_windows_than_are_prepared_at_once(cuda_device, dtype, B, T, H, D):
+    """Entries that end in each of the ranges of windows, at their borders, and before the first; slots, of which two entries share one."""
+    q, k, v, decay, beta, state = _case(cuda_device, T, B, T, H, 1, D, dtype, slots=B + 2)
+    n = [(0, 1, 32, 33, 511, 512, 513, T // 2, T - 1, T)[b % 10] for b in range(B)]
+    n = [min(x, T) for x in n]
+    slots = torch.arange(B + 1, 1, -1, dtype=torch.int32, device=cuda_device)
+    slots[7] = slots[3]
+    lengths, before, new = torch.tensor(n, dtype=torch.int32, device=cuda_device), state.clone(), torch.full_like(state, 5.0)
+    out, _ = binding.delta_rule(q, k, v, decay, beta, state, scale=0.7, slots=slots, lengths=lengths, state_out=new)
+    assert torch.equal(state, before)
+    own = [b for b in range(B) if b != 7]
+    at, mine = slots[own].long(), torch.tensor(own, device=cuda_device)
+    _check(out[mine], new[at], *(x[mine] for x in (q, k, v, decay, beta)), before[at], 0.7, [n[b] for b in own], "ranges")
+    left = [i for i in range(B + 2) if i not in at.tolist()]
+    assert (new[left] == 5).all() and (out[7] == 0).all() and all((out[b, n[b]:] == 0).all() for b in own)
+    again, _ = binding.delta_rule(q, k, v, decay, beta, state, scale=0.7, slots=slots, lengths=lengths)
+    assert torch.equal(again, out) and torch.equal(state[at], new[at]) and torch.equal(state[left], before[left])
 
 
 def test_no_tokens(cuda_device):
@@ -292,3 +313,42 @@ def test_refusals_of_tensors(cuda_device):
         with pytest.raises(binding.TTError):
             bad()
     torch.cuda.synchronize()
+
+
+def test_results_carry_no_gradient(cuda_device):
+    for T in (1, 40):
+        x = torch.randn(1, T, 2, 64, device=cuda_device, requires_grad=True)
+        g = torch.full((1, T, 2), 0.01, device=cuda_device, requires_grad=True)
+        for y in binding.delta_rule(x, x, x, None, g, torch.zeros(1, 2, 64, 64, device=cuda_device)):
+            assert not y.requires_grad and torch.isfinite(y).all()
+
+
+@pytest.mark.parametrize("T", [1, 600])
+def test_tensors_let_go_before_another_stream_has_read_them(cuda_device, T):
+    x, _, _, decay, beta, state = _case(cuda_device, 6, 2, T, 2, 2, 64, FP32)
+    call = lambda y, f, s: binding.delta_rule(y, y, y, f, beta, state, state_out=torch.zeros_like(state), stream=s)[0]      # noqa: E731
+    want = call(x, decay, None)
+    side = torch.cuda.Stream()
+    call(x, decay, side)                                  # what is set up once is there
+    torch.cuda.synchronize()
+    y, f = x.clone(), decay.clone()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(40_000_000)                     # some 20 ms
+    got = call(y, f, side)
+    del y, f
+    others = [torch.full_like(z, math.nan) for _ in range(8) for z in (x, decay)]
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and len(others) == 16
+
+
+def test_two_calls_at_once(cuda_device):
+    """On two streams, each with records and states of its own."""
+    cases = [_case(cuda_device, s, 3, 700, 6, 3, 64, BF16) for s in (7, 8)]
+    want = [[x.clone() for x in binding.delta_rule(*c, state_out=torch.empty_like(c[5]))] for c in cases]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        got = [binding.delta_rule(*c, state_out=torch.empty_like(c[5]), stream=s) for c, s in zip(cases, streams)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for x, y in zip(got, want) for a, b in zip(x, y))

@@ -242,10 +242,36 @@ def test_refusals_of_tensors(cuda_device):
     mask = torch.ones(2, 4, 4, dtype=torch.uint8, device=cuda_device)
     f = binding.differential_attention
     for bad in (lambda: f(q.half(), q.half(), q.half(), a, 0.3), lambda: f(q, q.float(), q.float(), a, 0.3), lambda: f(q, q, q[:, :3], a, 0.3), lambda: f(q, q[:1], q[:1], a, 0.3),
-                lambda: f(q, q, q, a[:, :16], 0.3), lambda: f(q, q, q, a.double(), 0.3), lambda: f(q, q, q, a[None], 0.3), lambda: f(q, q, q, a.cpu(), 0.3),
+                lambda: f(q, q, q, None, 0.3), lambda: f(q, q, q, a[:, :16], 0.3), lambda: f(q, q, q, a.double(), 0.3), lambda: f(q, q, q, a[None], 0.3), lambda: f(q, q, q, a.cpu(), 0.3),
                 lambda: f(q, q, q, a.T.contiguous().T, 0.3), lambda: f(q, q, q, a, math.nan), lambda: f(q, q, q, a, 0.3, norm_weight=a[0]), lambda: f(q, q, q, a, 0.3, eps=-1.0),
                 lambda: f(q, q, q, a, 0.3, scale=0.0), lambda: f(q, q, q, a, 0.3, kv_lengths=n.long()), lambda: f(q, q, q, a, 0.3, mask=mask[:, :3]),
                 lambda: f(q, q, q, a, 0.3, mask=mask.int()), lambda: f(q, q, q, a, 0.3, out=q[:1].expand(2, -1, -1, -1)), lambda: f(q[..., ::2], q[..., ::2], q[..., ::2], a, 0.3)):
         with pytest.raises(binding.TTError):
             bad()
     torch.cuda.synchronize()
+
+
+def test_results_carry_no_gradient(cuda_device):
+    x = torch.randn(1, 40, 2, 64, device=cuda_device, requires_grad=True)
+    a = torch.zeros(4, 32, device=cuda_device, requires_grad=True)
+    for y in (binding.differential_attention(x, x, x, a, 0.3), binding.differential_attention(x[:, :1], x, x, a, 0.3)):
+        assert not y.requires_grad and torch.isfinite(y).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_tensors_let_go_before_another_stream_has_read_them(cuda_device, dtype):
+    q, k, v, vectors, w = _case(cuda_device, 6, 2, 600, 600, 2, 2, 64, dtype)
+    call = lambda y, a, s: binding.differential_attention(q, k, y, a, 0.3, norm_weight=w, stream=s)      # noqa: E731
+    want = call(v, vectors, None)
+    side = torch.cuda.Stream()
+    call(v, vectors, side)                                # what is set up once is there
+    torch.cuda.synchronize()
+    y, a = v.clone(), vectors.clone()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(40_000_000)                     # some 20 ms
+    got = call(y, a, side)
+    del y, a
+    others = [torch.full_like(z, math.nan) for _ in range(8) for z in (v, vectors)]
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and len(others) == 16
