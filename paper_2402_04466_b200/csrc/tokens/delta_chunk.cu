@@ -108,6 +108,7 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
     const uint8_t* left = reinterpret_cast<const uint8_t*>(reinterpret_cast<const Record*>(p.records) + ((int64_t)b * p.heads + h) * p.windows);
     auto raw_of = [&](int w) { return reinterpret_cast<T*>(raw) + (w % H::AHEAD) * C * (D + 4); };
     pdl_wait();                                  // for the records
+    if (p.more) pdl_launch_dependents();
     // window w's keys and what else window w - 1 needs; nothing behind the last, but counted as the others are
     auto fetch = [&](int w) {
       if (w < windows) {
@@ -249,6 +250,7 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
     const int64_t state = ((int64_t)slot * p.heads + h) * D * D + col0 + 16 * run;
     // columns of values g and g + 8; the keys' elements 2t and 2t + 1 of the warp's tiles of 8
     float s[NT][4];
+    if (p.first_window > 0) pdl_wait();          // for the states of the range before
     auto at = [&](int x, int e) { return (int64_t)((warp * NT + x) * 8 + 2 * t + (e & 1)) * D + g + 8 * (e >> 1); };
 #pragma unroll
     for (int x = 0; x < NT; ++x)
@@ -528,21 +530,30 @@ cudaError_t launch(const DeltaParams& p, int D, cudaStream_t s) {
 
 }  // namespace
 
-// Windows to a range: records of one fit `most` bytes, or there is but one window to a range.
-static int range_of(int batch, int tokens, int heads, bool bf16) {
-  constexpr int64_t most = 96 << 20;
+// The windows are prepared and taken in ranges: a range's preparation runs beside the chain of the range before, with records of its own, both launched ahead of the
+// end of what is before them.  Eight maps of 14400 tokens, 4 heads of 64: ranges one behind the other 442 us, beside each other 414; with a first range of a quarter, whose
+// preparation alone has nothing beside it, 417.  A range more is 5 us more, so there is one as long as its records fit `most` bytes, of which two lie in the L2 cache.
+static int range_of(int batch, int tokens, int heads, bool bf16, uint64_t* bytes) {
+  constexpr int64_t most = 48 << 20;
   const int64_t each = (int64_t)batch * heads * (int64_t)(bf16 ? sizeof(DeltaRecord<2>) : sizeof(DeltaRecord<3>)), all = ((int64_t)tokens + C - 1) / C;
-  const int64_t fit = most / each < 1 ? 1 : most / each, ranges = (all + fit - 1) / fit;
-  return (int)((all + ranges - 1) / ranges);
+  const int64_t fit = most / each < 1 ? 1 : most / each, ranges = (all + fit - 1) / fit, windows = (all + ranges - 1) / ranges;
+  *bytes = (uint64_t)(windows * each);
+  return (int)windows;
 }
 uint64_t delta_scratch(int batch, int tokens, int heads, bool bf16) {
-  return (uint64_t)batch * heads * range_of(batch, tokens, heads, bf16) * (bf16 ? sizeof(DeltaRecord<2>) : sizeof(DeltaRecord<3>));
+  uint64_t bytes;
+  const int windows = range_of(batch, tokens, heads, bf16, &bytes);
+  return windows * C < tokens ? 2 * bytes : bytes;
 }
 
 cudaError_t launch_delta_chunk(DeltaParams p, bool bf16, int D, cudaStream_t s) {
+  uint8_t* const room = static_cast<uint8_t*>(p.records);
+  uint64_t bytes;
+  p.windows = range_of(p.batch, p.tokens, p.heads, bf16, &bytes);
   const int all = (p.tokens + C - 1) / C;
-  p.windows = range_of(p.batch, p.tokens, p.heads, bf16);
   for (p.first_window = 0; p.first_window < all; p.first_window += p.windows) {
+    p.more = p.first_window + p.windows < all;
+    p.records = room + p.first_window / p.windows % 2 * bytes;
     cudaError_t e = launch_delta_prepare(p, bf16, D, s);
     if (e == cudaSuccess) e = bf16 ? launch<__nv_bfloat16>(p, D, s) : launch<float>(p, D, s);
     if (e != cudaSuccess) return e;

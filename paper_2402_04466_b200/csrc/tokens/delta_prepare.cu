@@ -58,7 +58,12 @@ __global__ void __launch_bounds__(DELTA_GROUP, H::BLOCKS) delta_prepare_kernel(c
   pdl_launch_dependents();
   const int b = blockIdx.z, h = blockIdx.y, w = p.first_window + blockIdx.x;
   const int n = clamp_length(p.lengths, b, p.tokens);
-  if (w * C >= n || slot_of(p.slots, p.num_slots, b) < 0) return;            // the whole block
+  // Behind the chain of the range before, which it runs beside, it ends behind that, so that what waits for the one has waited for the other: one block sees to it.
+  const bool holds = p.first_window > 0 && (blockIdx.x | blockIdx.y | blockIdx.z) == 0;
+  if (w * C >= n || slot_of(p.slots, p.num_slots, b) < 0) {
+    if (holds) pdl_wait();
+    return;                                                                  // the whole block
+  }
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3, tid = threadIdx.x;
   const int hk = h / p.group;
   const T* q = reinterpret_cast<const T*>(p.q.p) + b * p.q.b + hk * p.q.h;
@@ -263,6 +268,7 @@ __global__ void __launch_bounds__(DELTA_GROUP, H::BLOCKS) delta_prepare_kernel(c
 #pragma unroll
     for (int e = 0; e < 3; ++e) put(warp, 0, e, transposed(low[e]), transposed(high[e]));
   }
+  if (holds) pdl_wait();
 }
 
 template <typename T, int D>
@@ -272,8 +278,7 @@ cudaError_t launch(const DeltaParams& p, cudaStream_t s) {
   static OncePerContext once;
   const cudaError_t e = once([] { return cudaFuncSetAttribute(delta_prepare_kernel<H>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM); });
   if (e != cudaSuccess) return e;
-  delta_prepare_kernel<H><<<dim3((unsigned)p.windows, (unsigned)p.heads, (unsigned)p.batch), DELTA_GROUP, SMEM, s>>>(p);
-  return cudaGetLastError();
+  return launch_kernel(delta_prepare_kernel<H>, dim3((unsigned)p.windows, (unsigned)p.heads, (unsigned)p.batch), DELTA_GROUP, SMEM, s, p, p.first_window > 0);
 }
 template <typename T>
 cudaError_t launch(const DeltaParams& p, int D, cudaStream_t s) {

@@ -65,6 +65,7 @@ struct alignas(32) DeltaParams {
   float scale;
   int32_t first_window, windows;           // of several tokens: windows first_window .. + windows - 1 of every sequence, in order
   void* records;                           // [batch][heads][windows]: DeltaRecord
+  int32_t more;                            // windows follow, whose preparation may begin
 };
 cudaError_t launch_delta_step(const DeltaParams& p, bool bf16, int D, cudaStream_t s);      // token by token
 cudaError_t launch_delta_prepare(const DeltaParams& p, bool bf16, int D, cudaStream_t s);   // of every window, what depends on no state

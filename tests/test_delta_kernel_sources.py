@@ -39,5 +39,9 @@ def test_records_are_read_behind_the_preparation():
     assert "pdl_wait();" in before
     loads, rest = body[body.index("left ="):].split("pdl_wait();", 1)
     assert "copy16(" not in loads and "copy16(" in rest and body.count("p.records") == 1
-    # nothing else comes from global memory that the preparation writes
-    assert "pdl_launch_dependents" not in body and "pdl_launch_dependents();" in _body("delta_prepare.cu")
+    # the next range's preparation, which writes the other records, begins when this one's is through, and ends behind this chain
+    assert body.count("pdl_launch_dependents();") == 1 and body.index("pdl_launch_dependents();") > body.index("left =") + len(loads)
+    assert re.search(r"if \(p\.first_window > 0\) pdl_wait\(\);", body[:body.index("= p.state[")])      # and the states of the range before
+    prepare = _body("delta_prepare.cu")
+    assert prepare.count("if (holds) pdl_wait();") == 2 and prepare.rstrip().endswith("if (holds) pdl_wait();")
+    assert re.search(r"holds = p\.first_window > 0 && \(blockIdx\.x \| blockIdx\.y \| blockIdx\.z\) == 0", prepare)
