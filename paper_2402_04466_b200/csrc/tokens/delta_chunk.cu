@@ -134,13 +134,18 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
         barrier_of<GROUP>(1);
         __nv_bfloat16* ks = keys_of(w);
         const float* from = reinterpret_cast<const float*>(raw_of(w));
-        for (int i = tid; i < C * (D / 2); i += GROUP) {
-          const int r = i / (D / 2), c = i % (D / 2) * 2;
-          const float2 f = *reinterpret_cast<const float2*>(from + r * (D + 4) + c);
-          uint32_t terms[3];
-          cut(f.x, f.y, terms);
+        constexpr int PASSES = C * (D / 4) / GROUP;
+        float4 f[PASSES];
 #pragma unroll
-          for (int x = 0; x < 3; ++x) *reinterpret_cast<uint32_t*>(ks + x * H::TILE + r * KP + c) = terms[x];
+        for (int i = 0; i < PASSES; ++i) f[i] = *reinterpret_cast<const float4*>(from + (tid + i * GROUP) / (D / 4) * (D + 4) + (tid + i * GROUP) % (D / 4) * 4);
+#pragma unroll
+        for (int i = 0; i < PASSES; ++i) {
+          uint32_t low[3], high[3];
+          cut(f[i].x, f[i].y, low);
+          cut(f[i].z, f[i].w, high);
+#pragma unroll
+          for (int x = 0; x < 3; ++x)
+            *reinterpret_cast<uint2*>(ks + x * H::TILE + (tid + i * GROUP) / (D / 4) * KP + (tid + i * GROUP) % (D / 4) * 4) = make_uint2(low[x], high[x]);
         }
         barrier_of<GROUP>(1);
       }
@@ -515,13 +520,19 @@ cudaError_t launch_shape(const DeltaParams& p, cudaStream_t s) {
   // ahead of the end of the preparation: blocks find their slots and fetch their states meanwhile
   return launch_kernel(delta_chunk_kernel<H>, dim3(H::D / H::COLS, (unsigned)p.heads, (unsigned)p.batch), H::THREADS, H::SMEM, s, p, true);
 }
+// One warp to a run where runs are many, four where they are few, and one for heads of 32, whose state is one warp's worth.  Measured, us:
+//   bf16, heads of 64, 128 runs of 14400 tokens: one 823, four 442; heads of 128, 2048 runs of 497 tokens: one 158, four 236;
+//   fp32, heads of 64, 16 runs of 4801 tokens: one 440, four 215; 512 runs of 1000: one 138, four 228 (of heads of 128 four runs do not fit a block);
+//   heads of 32, 8 runs of 4801 tokens: one 151 bf16 and 208 fp32, two 172 and 246; 256 runs of 1000: one 52 and 75, two 58 and 82.
 template <typename T, int D>
 cudaError_t launch(const DeltaParams& p, cudaStream_t s) {
-  const int64_t runs = (int64_t)p.batch * p.heads * (D / 16);
-  if constexpr (sizeof(T) == 2) {
-    if (runs > 2 * PLAN_SMS) return launch_shape<Shape<T, D, 1, 1, D == 32 ? 2 : 4>>(p, s);
+  if constexpr (D == 32) {
+    return launch_shape<Shape<T, D, 1, 1, 2>>(p, s);
+  } else {
+    if constexpr (Shape<T, D, 1, 1, 4>::FITS)
+      if ((int64_t)p.batch * p.heads * (D / 16) > 2 * PLAN_SMS) return launch_shape<Shape<T, D, 1, 1, 4>>(p, s);
+    return launch_shape<Shape<T, D, 4, sizeof(T) == 2 ? 2 : 4, 1>>(p, s);
   }
-  return launch_shape<Shape<T, D, (sizeof(T) == 2 && D > 32) ? 4 : 2, 2, 1>>(p, s);
 }
 template <typename T>
 cudaError_t launch(const DeltaParams& p, int D, cudaStream_t s) {
