@@ -1,20 +1,23 @@
 // The gated delta rule over several tokens, second part (tt_delta_rule): the chain of states, a window of 32 tokens at a time.
 //
-// With G_i the sum of log_decay up to and including token i of a window and T and P what delta_prepare.cu has worked out,
+// With G_i the sum of log_decay up to and including token i of a window and T and P what delta_window.cuh works out,
 //   R_i = beta_i (v_i - e^G_i S^T k_i),  U = T R,  out_i = scale e^G_i S^T q_i + sum_j P_ij u_j,  S' = e^G_C S + sum_j e^(G_C - G_j) k_j u_j^T.
-// What bounds a sequence is the chain S -> R -> U -> S'.  The columns of values are independent of each other: 16 of them are a run, and a run has one warp, or two where runs
-// are few, that take its state along in registers, and as many behind it that turn what the chain leaves into out, a window later for its last product.  Four more warps
-// load, two windows and more ahead.  All of a block's warps meet once a window.
+// What bounds a sequence is the chain S -> R -> U -> S', not bytes and not the tensor pipe: some 250 instructions that wait for one another.  The columns of values are independent
+// of each other: 16 of them are a run, and a run has one warp, or four where runs are few, that take its state along in registers, and one to four behind them that turn what the
+// chain leaves into out, a window later for its last product.  Four more warps load, two windows and more ahead.  All of a block's warps meet once a window.
 //
 // Everything on the chain is kept transposed, columns of values along M: the accumulators of one m16n8k16 product are then the other operand's registers of the next,
-// X^T = S^T K^T, U^T = R^T T^T, S'^T = U'^T K.  Two warps of a run halve the keys' elements of the state and the tokens of R and U; what they exchange goes through shared memory as those
-// registers.  (Four warps to a run took 1860 cycles a window, two take ???, one ???.  A tcgen05 product of 16 columns takes 40 cycles however few its
-// columns are, and its way through tensor memory twice that: the chain would be longer, not shorter.)
+// X^T = S^T K^T, U^T = R^T T^T, S'^T = U'^T K.  Four warps of a run split the keys' elements of the state and the tokens of R and U; what they exchange goes through shared memory as
+// those registers.  Heads of 64, cycles a window: one warp 3300, two 2050, four 1600.  A tcgen05 product of 16
+// columns takes 40 cycles however few its columns are, and its way through tensor memory twice that: the chain would be longer, not shorter.  Windows of 64 have four times the
+// triangle (with the warps as they were then, 909 us to 748 for the same maps).
+//
+// Eight maps of 14400 tokens, 4 heads of 64: 414 us, of which reading and writing it all once would be 37; 64 sequences of up to 497 tokens, 4 heads of 128: 158 us of 17.
 //
 // The state is fp32, and so is everything between two products: an operand that is not bf16 to begin with is cut into three bf16 terms (8 + 8 + 8 bits), of whose
 // products those of 2^-16 and more count.  Only what out alone reads is rounded further: in bf16 calls S, U and P count with 16 bits.  (P rounded
 // to bf16 once is not enough: of keys that repeat the corrections are many times larger than what is left of their sum.)
-#include "delta_common.cuh"
+#include "delta_window.cuh"
 
 namespace tt {
 namespace tok {
@@ -22,11 +25,14 @@ namespace {
 
 constexpr int C = DELTA_C, TT = DELTA_TT, TK = DELTA_TK, GROUP = DELTA_GROUP;
 
-// G warps of the chain and OG of out to a run, RUNS runs to a block
-template <typename T_, int D_, int G_, int OG_, int RUNS_>
+// G warps of the chain and OG of out to a run, RUNS runs to a block.  ALONE: the warps that load prepare the windows too, each block its head's, and there are no records in
+// global memory.
+template <typename T_, int D_, int G_, int OG_, int RUNS_, bool ALONE_ = false>
 struct Shape {
   using T = T_;
   static constexpr int D = D_, G = G_, OG = OG_, RUNS = RUNS_;
+  static constexpr bool ALONE = ALONE_;
+  using Window = DeltaWindow<T, D>;
   static constexpr int TERMS = sizeof(T) == 2 ? 1 : 3;       // of keys
   static constexpr int SEEN = sizeof(T) == 2 ? 2 : 3;        // of S, U and P in out
   using Record = DeltaRecord<SEEN>;
@@ -46,7 +52,9 @@ struct Shape {
   static constexpr int RECORDS = PLACES * (int)sizeof(Record);
   static constexpr int X = G == 1 ? 0 : RUNS * G * TT * 512, R = G == 1 ? 0 : RUNS * 3 * TK * 512, U = R;
   static constexpr int SEEN_U = 2 * RUNS * SEEN * TK * 512, S = 2 * RUNS * SEEN * KS * 512, O = RUNS * C * OP * (int)sizeof(T);
-  static constexpr int SMEM = RAW + K + Q + V + RECORDS + X + R + U + SEEN_U + S + O;
+  static constexpr int ROOM = ALONE ? (int)sizeof(typename Window::Room) : 0;
+  static constexpr int SMEM = RAW + K + Q + V + RECORDS + X + R + U + SEEN_U + S + O + ROOM;
+  static_assert(!ALONE || TERMS == 1, "keys and queries lie as the preparation reads them");
   static constexpr bool FITS = SMEM + 1024 <= 227 * 1024;
 };
 
@@ -77,6 +85,7 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
   uint32_t* u_seen = reinterpret_cast<uint32_t*>(room(H::SEEN_U));           // [parity][run][term][TK][lane][4]
   uint32_t* s_seen = reinterpret_cast<uint32_t*>(room(H::S));                // [parity][run][term][KS][lane][4]
   T* outs = reinterpret_cast<T*>(room(H::O));                                // [run][C][OP]
+  auto* window = reinterpret_cast<typename H::Window::Room*>(room(H::ROOM));
 
   const int b = blockIdx.z, h = blockIdx.y, col0 = (int)blockIdx.x * COLS;
   const int token0 = p.first_window * C, n = clamp_length(p.lengths, b, p.tokens);
@@ -105,7 +114,7 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
     const int tid = threadIdx.x - (H::CHAIN + H::OUT) * 32;
     const Rows<T, D> k_rows(k, p.k.t, tid), q_rows(q, p.q.t, tid);
     const Rows<T, COLS> v_rows(v, p.v.t, tid);
-    const uint8_t* left = reinterpret_cast<const uint8_t*>(reinterpret_cast<const Record*>(p.records) + ((int64_t)b * p.heads + h) * p.windows);
+    const uint8_t* left = H::ALONE ? nullptr : reinterpret_cast<const uint8_t*>(reinterpret_cast<const Record*>(p.records) + ((int64_t)b * p.heads + h) * p.windows);
     auto raw_of = [&](int w) { return reinterpret_cast<T*>(raw) + (w % H::AHEAD) * C * (D + 4); };
     pdl_wait();                                  // for the records
     if (p.more) pdl_launch_dependents();
@@ -119,17 +128,31 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
         q_rows.fetch(queries_of(w), QP, token0 + w * C, n);
         v_rows.fetch(values_of(w), VP, token0 + w * C, n);
         uint8_t* to = reinterpret_cast<uint8_t*>(&record_of(w));
+        if constexpr (!H::ALONE)
 #pragma unroll
         for (int i = 0; i < (int)sizeof(Record); i += 16 * GROUP)
           if ((int)sizeof(Record) % (16 * GROUP) == 0 || i + tid * 16 < (int)sizeof(Record)) copy16(to + i + tid * 16, left + (int64_t)w * sizeof(Record) + i + tid * 16, true);
       }
       copies_commit();
     };
+    float decay = 0.f, beta = 0.f;               // ALONE: of the lanes' tokens of the window that is prepared next
+    auto find_gates = [&](int w) {
+      const int token = token0 + w * C + lane;
+      const int64_t gate = ((int64_t)b * p.tokens + token) * p.heads + h;
+      decay = tid < 32 && token < n && p.log_decay ? p.log_decay[gate] : 0.f;
+      beta = tid < 32 && token < n ? p.beta[gate] : 0.f;
+    };
 #pragma unroll
     for (int i = 0; i < H::AHEAD; ++i) fetch(i);
     for (int step = -2; step <= windows; ++step) {
       const int w = step + 2;
       copies_wait<H::AHEAD - 1>();
+      if constexpr (H::ALONE) {
+        // a window's queries have come a step behind its keys
+        if (w >= 1 && w <= windows)
+          H::Window::prepare(record_of(w - 1), *window, keys_of(w - 1), queries_of(w - 1), decay, beta, p.scale, tid / 32, lane, [] { barrier_of<GROUP>(1); }, [] { barrier_of<GROUP>(1); });
+        find_gates(w);
+      }
       if (TERMS == 3 && w < windows) {
         barrier_of<GROUP>(1);
         __nv_bfloat16* ks = keys_of(w);
@@ -511,6 +534,12 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
   }
 }
 
+// Few bf16 sequences of at most two windows are prepared by the blocks that take them: one launch and no records.  The second window is prepared beside the chain of the first;
+// a third would make the chain wait.  Five sequences of 60 tokens, 2 heads of 64: 8.3 us on the GPU either way, 9.8 instead of 14.4 for the host.  Where blocks run one behind the
+// other it counts that each of a head's does the same work again (18 of 64 tokens, 4 heads of 64: 14.4 us instead of 12.3), and with heads of 128 that there is more of it (4
+// of 64 tokens, 4 heads: 10.3 instead of 8.4).
+bool alone(int batch, int tokens, int heads, int D, bool bf16) { return bf16 && D < 128 && tokens <= 2 * C && (int64_t)batch * heads * (D / 16) <= PLAN_SMS; }
+
 template <typename H>
 cudaError_t launch_shape(const DeltaParams& p, cudaStream_t s) {
   static_assert(H::FITS, "shared memory");
@@ -518,7 +547,7 @@ cudaError_t launch_shape(const DeltaParams& p, cudaStream_t s) {
   const cudaError_t e = once([] { return cudaFuncSetAttribute(delta_chunk_kernel<H>, cudaFuncAttributeMaxDynamicSharedMemorySize, H::SMEM); });
   if (e != cudaSuccess) return e;
   // ahead of the end of the preparation: blocks find their slots and fetch their states meanwhile
-  return launch_kernel(delta_chunk_kernel<H>, dim3(H::D / H::COLS, (unsigned)p.heads, (unsigned)p.batch), H::THREADS, H::SMEM, s, p, true);
+  return launch_kernel(delta_chunk_kernel<H>, dim3(H::D / H::COLS, (unsigned)p.heads, (unsigned)p.batch), H::THREADS, H::SMEM, s, p, !H::ALONE);
 }
 // One warp to a run where runs are many, four where they are few, and one for heads of 32, whose state is one warp's worth.  Measured, us:
 //   bf16, heads of 64, 128 runs of 14400 tokens: one 823, four 442; heads of 128, 2048 runs of 497 tokens: one 158, four 236;
@@ -526,6 +555,8 @@ cudaError_t launch_shape(const DeltaParams& p, cudaStream_t s) {
 //   heads of 32, 8 runs of 4801 tokens: one 151 bf16 and 208 fp32, two 172 and 246; 256 runs of 1000: one 52 and 75, two 58 and 82.
 template <typename T, int D>
 cudaError_t launch(const DeltaParams& p, cudaStream_t s) {
+  if constexpr (sizeof(T) == 2 && D < 128)
+    if (alone(p.batch, p.tokens, p.heads, D, true)) return launch_shape<Shape<T, D, D == 32 ? 1 : 4, D == 32 ? 1 : 2, D == 32 ? 2 : 1, true>>(p, s);
   if constexpr (D == 32) {
     return launch_shape<Shape<T, D, 1, 1, 2>>(p, s);
   } else {
@@ -551,17 +582,22 @@ static int range_of(int batch, int tokens, int heads, bool bf16, uint64_t* bytes
   *bytes = (uint64_t)(windows * each);
   return (int)windows;
 }
-uint64_t delta_scratch(int batch, int tokens, int heads, bool bf16) {
+uint64_t delta_scratch(int batch, int tokens, int heads, int D, bool bf16) {
+  if (alone(batch, tokens, heads, D, bf16)) return 0;
   uint64_t bytes;
   const int windows = range_of(batch, tokens, heads, bf16, &bytes);
   return windows * C < tokens ? 2 * bytes : bytes;
 }
 
 cudaError_t launch_delta_chunk(DeltaParams p, bool bf16, int D, cudaStream_t s) {
+  const int all = (p.tokens + C - 1) / C;
+  if (alone(p.batch, p.tokens, p.heads, D, bf16)) {
+    p.windows = all;
+    return launch<__nv_bfloat16>(p, D, s);
+  }
   uint8_t* const room = static_cast<uint8_t*>(p.records);
   uint64_t bytes;
   p.windows = range_of(p.batch, p.tokens, p.heads, bf16, &bytes);
-  const int all = (p.tokens + C - 1) / C;
   for (p.first_window = 0; p.first_window < all; p.first_window += p.windows) {
     p.more = p.first_window + p.windows < all;
     p.records = room + p.first_window / p.windows % 2 * bytes;

@@ -1,4 +1,4 @@
-// What the kernels of tt_delta_rule over several tokens share: windows, operands cut into bf16 terms, and what delta_prepare.cu leaves for delta_chunk.cu.
+// What the kernels of tt_delta_rule over several tokens share: windows, operands cut into bf16 terms, and what is worked out of a window for the chain of states.
 #pragma once
 
 #include "linear_common.cuh"

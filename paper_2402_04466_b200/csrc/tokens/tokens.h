@@ -69,10 +69,10 @@ struct alignas(32) DeltaParams {
 };
 cudaError_t launch_delta_step(const DeltaParams& p, bool bf16, int D, cudaStream_t s);      // token by token
 cudaError_t launch_delta_prepare(const DeltaParams& p, bool bf16, int D, cudaStream_t s);   // of every window, what depends on no state
-cudaError_t launch_delta_chunk(DeltaParams p, bool bf16, int D, cudaStream_t s);            // a window of tokens at a time, prepared range by range
-uint64_t delta_scratch(int batch, int tokens, int heads, bool bf16);
-// Few tokens are taken one by one: a window takes its two launches and its way through them whatever it holds.  Both measured, us one by one and by window, five entries of 2 heads of 64
-// and 64 of 4 heads of 128: bf16, 4 tokens 6.2 8.3, 19.5 26.7, 8 tokens 8.3 8.3, 32.8 26.7; fp32, 12 tokens 10.3 12.3, 44 72, 16 tokens 12.4 12.4, 57 72.
+cudaError_t launch_delta_chunk(DeltaParams p, bool bf16, int D, cudaStream_t s);            // a window of tokens at a time, prepared range by range or on the way
+uint64_t delta_scratch(int batch, int tokens, int heads, int D, bool bf16);
+// Few tokens are taken one by one: a window takes its way through the products whatever it holds.  Both measured, us one by one and by window, five entries of 2 heads of 64
+// and 64 of 4 heads of 128: bf16, 4 tokens 6.2 6.2, 20.5 26.7, 8 tokens 8.3 6.2, 32.8 26.7; fp32, 12 tokens 10.3 10.3, 44.5 61.5, 16 tokens 12.4 10.3, 57 61.5.
 inline bool delta_by_window(int tokens, bool bf16) { return tokens > (bf16 ? 6 : 15); }
 
 struct alignas(32) CrossParams {

@@ -181,7 +181,7 @@ static tt_status check_delta(const char* who, const tt_delta_rule_args* a) {
 
 uint64_t tt_delta_rule_scratch_bytes(const tt_delta_rule_args* a) {
   if (check_delta("tt_delta_rule_scratch_bytes", a) != TT_OK || !delta_by_window(a->tokens, a->precision == TT_BF16)) return 0;
-  return delta_scratch(a->batch, a->tokens, a->heads, a->precision == TT_BF16);
+  return delta_scratch(a->batch, a->tokens, a->heads, a->head_dim, a->precision == TT_BF16);
 }
 
 tt_status tt_delta_rule(const tt_delta_rule_args* a, void* cuda_stream) {

@@ -32,7 +32,7 @@ def _view(at, B, T, H, D):
 
 
 def _delta(**over):
-    B, T, H, K, D = 2, 3, 4, 2, 64
+    B, T, H, K, D = 2, 70, 4, 2, 64
     a = S(C.sizeof(S), 1, B, T, H, K, D, 5, 0.125, 0, _view(A, B, T, K, D), _view(A + 0x10000, B, T, K, D), _view(A + 0x20000, B, T, H, D),
           _view(A + 0x30000, B, T, H, D), A, A, A, A, None, None, A, 1 << 40)
     for name, value in over.items():
@@ -58,6 +58,16 @@ def test_refusals(over):
 @pytest.mark.parametrize("d", [0, 16, 48, 96, 256])
 def test_other_head_dims_are_unsupported(d):
     assert binding.load_library().tt_delta_rule(C.byref(_delta(head_dim=d)), None) == 2
+
+
+def test_scratch_is_asked_for_only_where_windows_are_prepared_apart():
+    lib = binding.load_library()
+    room = lambda **over: lib.tt_delta_rule_scratch_bytes(C.byref(_delta(**over)))      # noqa: E731
+    assert room() > 0 and room(tokens=64, precision=0) > 0 and room(tokens=64, batch=40, num_slots=40) > 0 and room(tokens=64, head_dim=128) > 0
+    assert room(tokens=0) == room(tokens=1) == room(tokens=6) == room(tokens=64) == room(tokens=15, precision=0) == 0
+    assert room(heads=3) == 0 and lib.tt_delta_rule_scratch_bytes(None) == 0
+    # a long call asks for the records of two ranges of windows, not of all
+    assert room(tokens=1 << 20) <= 2 * (48 << 20) < room(tokens=1 << 20) * 1.1
 
 
 def test_host_tensors_are_refused():

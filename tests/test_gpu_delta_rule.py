@@ -122,9 +122,10 @@ def test_slots_and_lengths(cuda_device, dtype, T, H, D):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("D", [32, 64, 128])
-def test_gates_at_their_ends(cuda_device, dtype, D):
+@pytest.mark.parametrize("T", [60, 150])
+def test_gates_at_their_ends(cuda_device, dtype, D, T):
     """No decay at all, decays of 0 and -infinity and far below what 32 bits can hold, beta of 0, 1 and 2: beside tokens that hardly fade."""
-    B, T, H = 2, 150, 6
+    B, H = 2, 6
     q, k, v, decay, beta, state = _case(cuda_device, D, B, T, H, H, D, dtype)
     _check(*binding.delta_rule(q, k, v, None, beta, state, state_out=torch.empty_like(state)), q, k, v, None, beta, state, 1.0, None, "no decay")
     decay[:, :, 0], decay[:, ::7, 1], decay[:, 40::9, 2], decay[:, 10, 3], decay[:, :, 4] = 0.0, -math.inf, -1e4, -90.0, -0.001
@@ -172,7 +173,7 @@ def test_long_sequences(cuda_device, dtype, B, T, H, D):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("H,D", [(2, 32), (2, 64), (2, 128), (40, 32), (20, 64), (10, 128)])
-@pytest.mark.parametrize("T", [1, 130])
+@pytest.mark.parametrize("T", [1, 60, 130])
 def test_what_is_not_finite_goes_where_the_formula_takes_it(cuda_device, dtype, H, D, T):
     """An infinity or NaN in q makes its own row of out not finite, one in v its column, one in k or a gate its head, each from its token on; nothing before it."""
     B = 6
@@ -226,7 +227,7 @@ def test_no_tokens(cuda_device):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("T", [1, 5, 300])
+@pytest.mark.parametrize("T", [1, 5, 50, 300])
 def test_streams_and_graphs_give_the_same_bits(cuda_device, dtype, T):
     q, k, v, decay, beta, state = _case(cuda_device, T, 3, T, 4, 2, 64, dtype)
     new = torch.empty_like(state)
@@ -323,7 +324,7 @@ def test_results_carry_no_gradient(cuda_device):
             assert not y.requires_grad and torch.isfinite(y).all()
 
 
-@pytest.mark.parametrize("T", [1, 600])
+@pytest.mark.parametrize("T", [1, 50, 600])
 def test_tensors_let_go_before_another_stream_has_read_them(cuda_device, T):
     x, _, _, decay, beta, state = _case(cuda_device, 6, 2, T, 2, 2, 64, FP32)
     call = lambda y, f, s: binding.delta_rule(y, y, y, f, beta, state, state_out=torch.zeros_like(state), stream=s)[0]      # noqa: E731
