@@ -129,10 +129,16 @@ cudaError_t launch(const DeltaParams& p, cudaStream_t s) {
 }
 template <typename T, int D>
 cudaError_t launch(const DeltaParams& p, cudaStream_t s) {
-  if (p.tokens > 1) return launch<T, D, D / 4, true>(p, s);
-  // Few states: cut each into four runs of columns, so that more multiprocessors fetch.  Many: in halves, of which more fit a multiprocessor, for no block
-  // writes before it has read all of its own (256 sessions of 8 heads of 128, whole 71 us, halves 49, quarters 65).
-  return (int64_t)p.batch * p.heads < 2 * PLAN_SMS ? launch<T, D, D / 4, false>(p, s) : launch<T, D, D / 2, false>(p, s);
+  // Columns to a block: the fewer, the more multiprocessors fetch a state and the more threads share a row's sums, which is what a token takes.  Whole, halves and quarters, us:
+  // 256 sessions of 8 heads of 128, a token 46.7 45.1 51.3, six tokens 133 124 164; of 64 12.7 16.5 28.7, 41 66 125; of 32 8.3 8.3 10.3, 33 31 33;
+  // five sessions, six tokens of heads of 128 10.3 8.2 10.2, of 64 8.2 6.2 8.2.
+  const auto run = [&](auto several) {
+    constexpr bool S = decltype(several)::value;
+    if constexpr (D == 64)
+      if ((int64_t)p.batch * p.heads >= PLAN_SMS) return launch<T, D, 64, S>(p, s);
+    return launch<T, D, D / 2, S>(p, s);
+  };
+  return p.tokens > 1 ? run(std::true_type()) : run(std::false_type());
 }
 template <typename T>
 cudaError_t launch(const DeltaParams& p, int D, cudaStream_t s) {

@@ -72,8 +72,11 @@ cudaError_t launch_delta_prepare(const DeltaParams& p, bool bf16, int D, cudaStr
 cudaError_t launch_delta_chunk(DeltaParams p, bool bf16, int D, cudaStream_t s);            // a window of tokens at a time, prepared range by range or on the way
 uint64_t delta_scratch(int batch, int tokens, int heads, int D, bool bf16);
 // Few tokens are taken one by one: a window takes its way through the products whatever it holds.  Both measured, us one by one and by window, five entries of 2 heads of 64
-// and 64 of 4 heads of 128: bf16, 4 tokens 6.2 6.2, 20.5 26.7, 8 tokens 8.3 6.2, 32.8 26.7; fp32, 12 tokens 10.3 10.3, 44.5 61.5, 16 tokens 12.4 10.3, 57 61.5.
-inline bool delta_by_window(int tokens, bool bf16) { return tokens > (bf16 ? 6 : 15); }
+// and 256 of 8 heads of 128: bf16, 8 tokens 8.2 6.2, 153 181, 12 tokens 10.3 6.2, 211 182; fp32, 12 tokens 10.3 10.3, 208 491, 16 tokens 12.3 10.3, 266 503, 24 tokens
+// 16.4 10.3, 383 528.
+inline bool delta_by_window(int batch, int tokens, int heads, int D, bool bf16) {
+  return tokens > (bf16 ? 8 : D == 128 && (int64_t)batch * heads >= PLAN_SMS ? 24 : 12);
+}
 
 struct alignas(32) CrossParams {
   View q, k, v, o;

@@ -180,7 +180,7 @@ static tt_status check_delta(const char* who, const tt_delta_rule_args* a) {
 }
 
 uint64_t tt_delta_rule_scratch_bytes(const tt_delta_rule_args* a) {
-  if (check_delta("tt_delta_rule_scratch_bytes", a) != TT_OK || !delta_by_window(a->tokens, a->precision == TT_BF16)) return 0;
+  if (check_delta("tt_delta_rule_scratch_bytes", a) != TT_OK || !delta_by_window(a->batch, a->tokens, a->heads, a->head_dim, a->precision == TT_BF16)) return 0;
   return delta_scratch(a->batch, a->tokens, a->heads, a->head_dim, a->precision == TT_BF16);
 }
 
@@ -207,7 +207,7 @@ tt_status tt_delta_rule(const tt_delta_rule_args* a, void* cuda_stream) {
   p.batch = a->batch; p.tokens = a->tokens; p.heads = a->heads; p.group = a->heads / a->qk_heads; p.num_slots = a->num_slots;
   p.scale = a->scale; p.records = a->scratch;
   const cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
-  const cudaError_t e = delta_by_window(a->tokens, bf16) ? launch_delta_chunk(p, bf16, a->head_dim, s) : launch_delta_step(p, bf16, a->head_dim, s);
+  const cudaError_t e = delta_by_window(a->batch, a->tokens, a->heads, a->head_dim, bf16) ? launch_delta_chunk(p, bf16, a->head_dim, s) : launch_delta_step(p, bf16, a->head_dim, s);
   return e == cudaSuccess ? TT_OK : set_error(TT_ERR_CUDA, "%s: %s", who, cudaGetErrorString(e));
 }
 

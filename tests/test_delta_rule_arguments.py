@@ -64,7 +64,8 @@ def test_scratch_is_asked_for_only_where_windows_are_prepared_apart():
     lib = binding.load_library()
     room = lambda **over: lib.tt_delta_rule_scratch_bytes(C.byref(_delta(**over)))      # noqa: E731
     assert room() > 0 and room(tokens=64, precision=0) > 0 and room(tokens=64, batch=40, num_slots=40) > 0 and room(tokens=64, head_dim=128) > 0
-    assert room(tokens=0) == room(tokens=1) == room(tokens=6) == room(tokens=64) == room(tokens=15, precision=0) == 0
+    assert room(tokens=0) == room(tokens=1) == room(tokens=8) == room(tokens=64) == room(tokens=12, precision=0) == 0
+    assert room(tokens=24, precision=0, batch=40, num_slots=40, head_dim=128) == 0 < room(tokens=25, precision=0, batch=40, num_slots=40, head_dim=128)
     assert room(heads=3) == 0 and lib.tt_delta_rule_scratch_bytes(None) == 0
     # a long call asks for the records of two ranges of windows, not of all
     assert room(tokens=1 << 20) <= 2 * (48 << 20) < room(tokens=1 << 20) * 1.1

@@ -66,7 +66,8 @@ def _check(out, state, q, k, v, decay, beta, before, scale, lengths, name):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("B,T,H,K,D", [
-    (1, 1, 1, 1, 32), (5, 1, 2, 2, 64), (3, 1, 4, 2, 128), (200, 1, 4, 4, 64), (2, 2, 2, 1, 64), (2, 3, 1, 1, 128), (1, 15, 2, 2, 64), (1, 16, 3, 3, 32), (2, 17, 4, 1, 128),
+    (1, 1, 1, 1, 32), (5, 1, 2, 2, 64), (3, 1, 4, 2, 128), (200, 1, 4, 4, 64), (2, 2, 2, 1, 64), (2, 3, 1, 1, 128), (2, 8, 2, 2, 64), (1, 9, 4, 2, 64), (200, 6, 4, 4, 64), (90, 5, 2, 1, 32), (80, 4, 2, 2, 128), (2, 12, 2, 2, 32), (3, 13, 2, 1, 64),
+    (40, 24, 4, 4, 128), (40, 25, 4, 4, 128), (1, 15, 2, 2, 64), (1, 16, 3, 3, 32), (2, 17, 4, 1, 128),
     (2, 31, 2, 2, 64), (2, 32, 2, 2, 128), (2, 33, 2, 1, 32), (3, 60, 2, 2, 64), (1, 63, 2, 2, 128), (2, 64, 2, 2, 64), (2, 65, 2, 2, 32), (2, 127, 2, 1, 128), (2, 128, 2, 2, 64),
     (1, 129, 4, 2, 64), (2, 200, 2, 2, 32), (2, 333, 2, 1, 128), (1, 1000, 2, 2, 64), (40, 97, 4, 4, 64), (20, 190, 8, 4, 128), (90, 70, 4, 2, 32)])
 def test_delta_rule(cuda_device, dtype, B, T, H, K, D):
