@@ -173,8 +173,8 @@ __global__ void __launch_bounds__(Few<D, W, MAPS>::THREADS, Few<D, W, MAPS>::BLO
     fetch_mask(first);
   }
   if constexpr (MAPS == 2) {
-    // rows r and r + group are of one head
-    for (int r = warp; r < min(16, p.group); r += F::WARPS) {
+    // rows r and r + group are of one head; the last warps have the fewest keys
+    for (int r = F::WARPS - 1 - warp; r < min(16, p.group); r += F::WARPS) {
       const float f = lambda_of(p.end, D / 2, hk * p.group + (row0 + r) % p.group);
       if (lane == 0) s_lambda[r] = f;
     }
@@ -372,26 +372,34 @@ __global__ void __launch_bounds__(Few<D, W, MAPS>::THREADS, Few<D, W, MAPS>::BLO
         *reinterpret_cast<float2*>(s_o + ((w * F::WARPS + warp) * 16 + g + 8 * r) * F::OP + 8 * i + 2 * t) = make_float2(o[w][i][2 * r], o[w][i][2 * r + 1]);
     }
   __syncthreads();
+  const int live = min(16, rows - row0);
+  for (int i = threadIdx.x; i < MAPS * live * (D / 2); i += F::THREADS) {
+    const int d = i % (D / 2) * 2, w = MAPS == 2 && i / (D / 2) >= live, r = i / (D / 2) - w * live;
+    float top = -INFINITY;
 #pragma unroll
-  for (int w = 0; w < MAPS; ++w)
-    for (int i = threadIdx.x; i < 16 * (D / 2); i += F::THREADS) {
-      const int r = i / (D / 2), d = i % (D / 2) * 2;
-      float top = -INFINITY;
+    for (int x = 0; x < F::WARPS; ++x) top = fmaxf(top, s_ml[w][x][r].x);
+    const float base = top == -INFINITY ? 0.f : top;
+    float a = 0.f, e = 0.f, total = 0.f;
 #pragma unroll
-      for (int x = 0; x < F::WARPS; ++x) top = fmaxf(top, s_ml[w][x][r].x);
-      const float base = top == -INFINITY ? 0.f : top;
-      float a = 0.f, e = 0.f, total = 0.f;
-#pragma unroll
-      for (int x = 0; x < F::WARPS; ++x) {
-        const float2 ml = s_ml[w][x][r], v = *reinterpret_cast<const float2*>(s_o + ((w * F::WARPS + x) * 16 + r) * F::OP + d);
-        const float f = exp2_fast(ml.x - base);
-        total = fmaf(f, ml.y, total);
-        a = fmaf(f, v.x, a);
-        e = fmaf(f, v.y, e);
-      }
-      *reinterpret_cast<float2*>(&s_sum[w][r][d]) = make_float2(a, e);
-      if (d == 0) s_stat[w][r] = make_float2(top, total);
+    for (int x = 0; x < F::WARPS; ++x) {
+      const float2 ml = s_ml[w][x][r], v = *reinterpret_cast<const float2*>(s_o + ((w * F::WARPS + x) * 16 + r) * F::OP + d);
+      const float f = exp2_fast(ml.x - base);
+      total = fmaf(f, ml.y, total);
+      a = fmaf(f, v.x, a);
+      e = fmaf(f, v.y, e);
     }
+    *reinterpret_cast<float2*>(&s_sum[w][r][d]) = make_float2(a, e);
+    if (d == 0) s_stat[w][r] = make_float2(top, total);
+  }
+  constexpr int E = (D + 63) / 64;             // pairs of a lane in a row (heads of 32: of the first 16 lanes)
+  float2 weight[MAPS == 2 ? E : 1];            // of the norm: on its way while the cluster meets
+  if constexpr (MAPS == 2) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int d = 64 * e + 2 * lane;
+      weight[e] = d < D ? make_float2(norm_weight(p.end, d), norm_weight(p.end, d + 1)) : make_float2(0.f, 0.f);
+    }
+  }
   // join the blocks of the cluster: each takes its share of the elements from all of them
   if (p.cluster > 1) cluster_sync_all();
   else __syncthreads();
@@ -444,7 +452,6 @@ __global__ void __launch_bounds__(Few<D, W, MAPS>::THREADS, Few<D, W, MAPS>::BLO
     // a warp to a row, whose norm takes all of its elements
     if (p.splits == 1)
       for (int r = rank * F::WARPS + warp; r < 16 && row0 + r < rows; r += F::WARPS * p.cluster) {
-        constexpr int E = (D + 63) / 64;       // pairs of a lane (heads of 32: of the first 16 lanes)
         const int row = row0 + r;
         float2 y[E];
         float squares = 0.f;
@@ -469,7 +476,7 @@ __global__ void __launch_bounds__(Few<D, W, MAPS>::THREADS, Few<D, W, MAPS>::BLO
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           const int d = 64 * e + 2 * lane;
-          if (d < D) *reinterpret_cast<uint32_t*>(dst + d) = pack_bf16(y[e].x * gain * norm_weight(p.end, d), y[e].y * gain * norm_weight(p.end, d + 1));
+          if (d < D) *reinterpret_cast<uint32_t*>(dst + d) = pack_bf16(y[e].x * gain * weight[e].x, y[e].y * gain * weight[e].y);
         }
       }
   }
