@@ -542,7 +542,8 @@ tt_status tt_linear_attention(const tt_linear_attention_args* args, void* cuda_s
  * Keys are usually of length 1 (tt_qk_norm_rope with weights of 1 / sqrt(head_dim)) and beta between 0 and 1; where beta |k|^2 is above 2 the rule diverges.
  * qk_heads divides heads: head h, with its own values, gates, state and output, uses query and key head h / (heads / qk_heads).
  * log_decay, beta: device fp32 [batch][tokens][heads], contiguous; log_decay is 0 or below (-infinity: a state that was finite is forgotten), NULL: no decay.
- * state, state_out, num_slots, slots, lengths, scratch: as in tt_linear_attention.
+ * state, state_out, num_slots, slots, lengths, scratch: as in tt_linear_attention.  The state counts with fp32's bits whatever the precision; of several TT_BF16 tokens out reads the state and
+ * the tokens' corrections with 16 bits, so that it is off by its own rounding and little more.
  * An infinity or NaN in a token or a state makes the elements of the state and of out that read it not finite, from its token on; earlier tokens, other columns of
  * values and other heads see nothing of it.
  */

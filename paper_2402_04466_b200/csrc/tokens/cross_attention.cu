@@ -10,6 +10,8 @@
 // over one of keys and values on 4096 keys take 46.6 us, 1.1 GFLOP of products (15 us of the units alone) and 2 us of exponentials.  (Weights kept
 // twice, as the pairs that the multiply-adds take: fewer instructions, more loads, 55 us.)
 //
+// Differential attention (MAPS = 2): scores of either half of a head's columns, weights of both maps side by side, every value read once for both: the same sizes 67.7 us (as two passes 90).
+//
 // A masked weight is kept as -0: it adds nothing to a finite value, and where a tile of V holds an infinity or NaN its sign
 // tells the slow loop to leave it out.
 #include "token_ptx.cuh"
