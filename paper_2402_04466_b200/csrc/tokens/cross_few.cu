@@ -14,7 +14,7 @@
 //
 // Differential attention (MAPS = 2, tt_differential_attention): the two halves of a head's columns make two maps of scores, for the same number of products, and each tile of values meets
 // both maps' weights while its registers are there, for twice as many.  The joins take both maps; a warp to a row ends with lambda and the norm, which reads the whole row.  The
-// same eight streams 27.3 us, of which K and V would be 14; the same five with masks 14.4; clips of 60 keys 6.2.
+// same eight streams 25.3 us, of which K and V would be 14; the same five with masks 12.4; clips of 60 keys 6.2.
 #include "tokens.h"
 
 #include "token_ptx.cuh"
@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(Few<D, W, MAPS>::THREADS, Few<D, W, MAPS>::BLO
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t s_full[F::WARPS][F::STAGES];
   __shared__ float2 s_ml[MAPS][F::WARPS][16];
-  __shared__ float s_sum[MAPS][16][D];
+  __shared__ __align__(16) float s_sum[MAPS][16][D];
   __shared__ float2 s_stat[MAPS][16];
   __shared__ float s_lambda[16];
   uint8_t* ring0 = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -377,22 +377,26 @@ __global__ void __launch_bounds__(Few<D, W, MAPS>::THREADS, Few<D, W, MAPS>::BLO
     }
   __syncthreads();
   const int live = min(16, rows - row0);
-  for (int i = threadIdx.x; i < MAPS * live * (D / 2); i += F::THREADS) {
-    const int d = i % (D / 2) * 2, w = MAPS == 2 && i / (D / 2) >= live, r = i / (D / 2) - w * live;
+  for (int i = threadIdx.x; i < MAPS * live * (D / 4); i += F::THREADS) {
+    const int d = i % (D / 4) * 4, w = MAPS == 2 && i / (D / 4) >= live, r = i / (D / 4) - w * live;
     float top = -INFINITY;
 #pragma unroll
     for (int x = 0; x < F::WARPS; ++x) top = fmaxf(top, s_ml[w][x][r].x);
     const float base = top == -INFINITY ? 0.f : top;
-    float a = 0.f, e = 0.f, total = 0.f;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    float total = 0.f;
 #pragma unroll
     for (int x = 0; x < F::WARPS; ++x) {
-      const float2 ml = s_ml[w][x][r], v = *reinterpret_cast<const float2*>(s_o + ((w * F::WARPS + x) * 16 + r) * F::OP + d);
+      const float2 ml = s_ml[w][x][r];
+      const float4 v = *reinterpret_cast<const float4*>(s_o + ((w * F::WARPS + x) * 16 + r) * F::OP + d);
       const float f = exp2_fast(ml.x - base);
       total = fmaf(f, ml.y, total);
-      a = fmaf(f, v.x, a);
-      e = fmaf(f, v.y, e);
+      sum.x = fmaf(f, v.x, sum.x);
+      sum.y = fmaf(f, v.y, sum.y);
+      sum.z = fmaf(f, v.z, sum.z);
+      sum.w = fmaf(f, v.w, sum.w);
     }
-    *reinterpret_cast<float2*>(&s_sum[w][r][d]) = make_float2(a, e);
+    *reinterpret_cast<float4*>(&s_sum[w][r][d]) = sum;
     if (d == 0) s_stat[w][r] = make_float2(top, total);
   }
   constexpr int E = (D + 63) / 64;             // pairs of a lane in a row (heads of 32: of the first 16 lanes)
@@ -457,22 +461,40 @@ __global__ void __launch_bounds__(Few<D, W, MAPS>::THREADS, Few<D, W, MAPS>::BLO
     if (p.splits == 1)
       for (int r = rank * F::WARPS + warp; r < 16 && row0 + r < rows; r += F::WARPS * p.cluster) {
         const int row = row0 + r;
+        // all loads first: the sums' of both maps, and block x's maximum and total to lane x, map 2's to lane 8 + x
+        float2 sums[2][E][MAX_CLUSTER];
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+#pragma unroll
+            for (int x = 0; x < MAX_CLUSTER; ++x)
+              sums[w][e][x] = x < p.cluster && 64 * e + 2 * lane < D ? cluster_load(reinterpret_cast<float2*>(&s_sum[w][r][64 * e + 2 * lane]), x, p.cluster) : make_float2(0.f, 0.f);
+        const float2 stat = lane < 16 && (lane & 7) < p.cluster ? cluster_load(&s_stat[lane >> 3][r], lane & 7, p.cluster) : make_float2(-INFINITY, 0.f);
+        float top = stat.x;
+#pragma unroll
+        for (int x = 4; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+        float f = exp2_fast(stat.x - (top == -INFINITY ? 0.f : top)), total = f * stat.y;
+#pragma unroll
+        for (int x = 4; x > 0; x >>= 1) total += __shfl_xor_sync(0xffffffffu, total, x);
+        f *= total == 0.f ? 0.f : (lane < 8 ? 1.f : -s_lambda[r % p.group]) / total;
         float2 y[E];
         float squares = 0.f;
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const int d = 64 * e + 2 * lane;
-          y[e] = make_float2(0.f, 0.f);
-          if (d < D) {
-            float top, total;
-            const float2 one = joined(0, r, d, top, total);
-            const float i1 = total == 0.f ? 0.f : 1.f / total;
-            const float2 two = joined(1, r, d, top, total);
-            const float i2 = total == 0.f ? 0.f : s_lambda[r % p.group] / total;
-            y[e] = make_float2(one.x * i1 - two.x * i2, one.y * i1 - two.y * i2);
+        for (int e = 0; e < E; ++e) y[e] = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+#pragma unroll
+          for (int x = 0; x < MAX_CLUSTER; ++x) {
+            const float share = __shfl_sync(0xffffffffu, f, 8 * w + x);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+              y[e].x = fmaf(share, sums[w][e][x].x, y[e].x);
+              y[e].y = fmaf(share, sums[w][e][x].y, y[e].y);
+            }
           }
-          squares = fmaf(y[e].x, y[e].x, fmaf(y[e].y, y[e].y, squares));
-        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) squares = fmaf(y[e].x, y[e].x, fmaf(y[e].y, y[e].y, squares));
 #pragma unroll
         for (int x = 16; x > 0; x >>= 1) squares += __shfl_xor_sync(0xffffffffu, squares, x);
         const float gain = row_gain<D>(p.end, squares);

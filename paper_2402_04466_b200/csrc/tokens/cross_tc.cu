@@ -14,7 +14,7 @@
 // TFLOP/s.  Weights are rounded to bf16 once, as far as out itself is; their sum is of the weights before that.
 //
 // Differential attention (MAPS = 2, tt_differential_attention): the two tiles of a block are the two maps of one tile of queries, each with scores from its half of the columns, and the same tile of
-// values for both; where a tile ends their sums meet in shared memory for lambda and the norm.  Twice the exponentials to half the products of scores: the same sizes 544 us with heads of 64 (the
+// values for both; where a tile ends each map's warps read half of the columns of both maps' sums for lambda and the norm, whose squares they add up through shared memory.  Twice the exponentials to half the products of scores: the same sizes 544 us with heads of 64 (the
 // exponentials alone 325) and 396 with heads of 128.
 #include "tokens.h"
 

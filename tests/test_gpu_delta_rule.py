@@ -217,6 +217,16 @@ def test_more_windows_than_are_prepared_at_once(cuda_device, dtype, B, T, H, D):
     assert (new[left] == 5).all() and (out[7] == 0).all() and all((out[b, n[b]:] == 0).all() for b in own)
     again, _ = binding.delta_rule(q, k, v, decay, beta, state, scale=0.7, slots=slots, lengths=lengths)
     assert torch.equal(again, out) and torch.equal(state[at], new[at]) and torch.equal(state[left], before[left])
+    # captured, and replayed twice in place
+    want = [binding.delta_rule(q, k, v, decay, beta, state, scale=0.7, slots=slots, lengths=lengths)[0] for _ in range(2)][1]
+    cell, graph = before.clone(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got, _ = binding.delta_rule(q, k, v, decay, beta, cell, scale=0.7, slots=slots, lengths=lengths)
+    cell.copy_(before)
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and torch.equal(cell, state)
 
 
 def test_no_tokens(cuda_device):
