@@ -2,7 +2,7 @@
 //
 // With G_i the sum of log_decay up to and including token i of a window and T and P what delta_window.cuh works out,
 //   R_i = beta_i (v_i - e^G_i S^T k_i),  U = T R,  out_i = scale e^G_i S^T q_i + sum_j P_ij u_j,  S' = e^G_C S + sum_j e^(G_C - G_j) k_j u_j^T.
-// What bounds a sequence is the chain S -> R -> U -> S', not bytes and not the tensor pipe: some 250 instructions that wait for one another.  The columns of values are independent
+// What bounds a sequence is the chain S -> R -> U -> S', not bytes and not the tensor pipe: instructions that wait for one another.  The columns of values are independent
 // of each other: 16 of them are a run, and a run has one warp, or four where runs are few, that take its state along in registers, and one to four behind them that turn what the
 // chain leaves into out, a window later for its last product.  Four more warps load, two windows and more ahead.  All of a block's warps meet once a window.
 //
