@@ -12,7 +12,7 @@
 // columns takes 40 cycles however few its columns are, and its way through tensor memory twice that: the chain would be longer, not shorter.  Windows of 64 have four times the
 // triangle (with the warps as they were then, 909 us to 748 for the same maps).
 //
-// Eight maps of 14400 tokens, 4 heads of 64: 414 us, of which reading and writing it all once would be 37; 64 sequences of up to 497 tokens, 4 heads of 128: 158 us of 17.
+// Eight maps of 14400 tokens, 4 heads of 64: 421 us, of which reading and writing it all once would be 37; 64 sequences of up to 497 tokens, 4 heads of 128: 158 us of 17.
 //
 // The state is fp32, and so is everything between two products: an operand that is not bf16 to begin with is cut into three bf16 terms (8 + 8 + 8 bits), of whose
 // products those of 2^-16 and more count.  Only what out alone reads is rounded further: in bf16 calls S, U and P count with 16 bits.  (P rounded
@@ -326,7 +326,8 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
 #pragma unroll
         for (int c = 0; c < TT; ++c) *reinterpret_cast<float4*>(x_part + ((run * G + warp) * TT + c) * 128 + lane * 4) = make_float4(says[c][0], says[c][1], says[c][2], says[c][3]);
     };
-    // A window with something in it that is not finite, token by token: the weights of 0 that a window's products give earlier tokens would make NaN of it.
+    // A window with something in it that is not finite, or of whose products one is not, token by token: the weights of 0 that a window's products give earlier tokens would
+    // make NaN of it.
     auto advance_slowly = [&](int w) {
       const int64_t gate0 = (int64_t)b * p.tokens * p.heads + h;
       for (int i = token0 + w * C; i < min(n, token0 + w * C + C); ++i) {
@@ -397,7 +398,6 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
       // R and U are this warp's of tiles of tokens warp, warp + G, ...
       float2 down[MINE];
       float r[MINE][4];
-      bool odd = false;
 #pragma unroll
       for (int m = 0; m < MINE; ++m) {
         const int tile = warp + G * m, token = 8 * tile + 2 * t;
@@ -422,11 +422,8 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
         r[m][1] = beta.y * fmaf(-up.y, x[1], to_float(vv[VP]));
         r[m][2] = beta.x * fmaf(-up.x, x[2], to_float(vv[8]));
         r[m][3] = beta.y * fmaf(-up.y, x[3], to_float(vv[VP + 8]));
-        odd |= fmaf(r[m][0], 0.f, fmaf(r[m][1], 0.f, fmaf(r[m][2], 0.f, r[m][3] * 0.f))) != 0.f;
         if constexpr (G > 1) keep<3>(r_frag + run * 3 * TK * 128, TK * 128, lane, tile, r[m]);
       }
-      if (odd) slow[w & 3][run] = 1;
-      // (a barrier that joins flags takes 100 cycles more)
       if constexpr (G > 1) barrier_of<32 * G>(2 + run);
       else __syncwarp();
       // U^T = R^T T^T
@@ -473,11 +470,16 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
           for (int e = 0; e < 4; ++e) u[m][e] = warp + G * m >= 2 ? sums[m][0][e] + sums[m][1][e] : sums[m][0][e];
       }
       if (lane == 0 && warp == 0) slow[(w + 2) & 3][run] = 0;      // out was through with that two windows ago
-      // something in the window or the state is not finite: nothing has been changed yet
-      if (__builtin_expect(slow[w & 3][run], 0)) {
-        if (G > 1) barrier_of<32 * G>(2 + run);
-        advance_slowly(w);
-        return;
+      // A correction that is not finite (of R, as a diagonal of T is 1, of T, or as a sum): the window is taken token by token, from the state that is still there.
+      if constexpr (G == 1) {
+        bool odd = false;
+#pragma unroll
+        for (int m = 0; m < MINE; ++m) odd |= fmaf(u[m][0], 0.f, fmaf(u[m][1], 0.f, fmaf(u[m][2], 0.f, u[m][3] * 0.f))) != 0.f;
+        if (__builtin_expect(__any_sync(0xffffffffu, odd), 0)) {
+          if (lane == 0) slow[w & 3][run] = 1;
+          advance_slowly(w);
+          return;
+        }
       }
 #pragma unroll
       for (int m = 0; m < MINE; ++m) {
@@ -516,6 +518,19 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
                   if (sum == 2 && i == (TERMS == 1 ? 2 : 0)) mma16816_first(d[z][x], a[x][i], f[z][x][sum - i][0], f[z][x][sum - i][1]);
                   else mma16816(d[z][x], a[x][i], f[z][x][sum - i][0], f[z][x][sum - i][1]);
                 }
+        if (G > 1 && m == 0) {
+          // each of the run's warps has all of its corrections and comes to the same (with a flag behind the barrier eight maps take 423 us instead of 421)
+          __nv_bfloat162 odd = __float2bfloat162_rn(0.f);
+#pragma unroll
+          for (int x = 0; x < TK; ++x)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) odd = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&a[x][0][e]), __float2bfloat162_rn(0.f), odd);
+          if (__builtin_expect(__any_sync(0xffffffffu, (*reinterpret_cast<const uint32_t*>(&odd) & 0x7FFF7FFFu) != 0u), 0)) {
+            if (lane == 0) slow[w & 3][run] = 1;
+            advance_slowly(w);
+            return;
+          }
+        }
 #pragma unroll
         for (int z = 0; z < SIDE; ++z)
 #pragma unroll

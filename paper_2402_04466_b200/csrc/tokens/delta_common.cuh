@@ -19,7 +19,7 @@ struct DeltaRecord {
   static constexpr int PLACES = 6;           // (tile, x)
   uint32_t inverse[PLACES][3][32][2];        // [][term][lane][]
   uint32_t weights[PLACES][SEEN][32][2];
-  float beta[DELTA_C], up[DELTA_C], down[DELTA_C];      // G: the sum of log_decay up to and including a token; e^G, e^(G_C - G)
+  float beta[DELTA_C], up[DELTA_C], down[DELTA_C];      // G: the sum of log_decay up to and including a token; e^G, e^(G_C - G).  beta: NaN among them where a weight is not finite
   float whole;                               // e^G_C
   float pad[31];
 };

@@ -113,6 +113,7 @@ __device__ __forceinline__ void DeltaWindow<T, D>::prepare(DeltaRecord<SEEN>& re
     const float gains[2] = {keys ? betas[i0] : scale, keys ? betas[i0 + 8] : scale};
     // the weights' registers: rows i0 of an accumulator are columns of the second operand
     uint32_t terms[2][TT][3];
+    float odd = 0.f;
 #pragma unroll
     for (int c = 0; c < TT; ++c)
       if (c < 2 * strip + 2) {
@@ -128,10 +129,15 @@ __device__ __forceinline__ void DeltaWindow<T, D>::prepare(DeltaRecord<SEEN>& re
             if (keys ? j + x >= i : j + x > i) f[x] = 0.f;
           }
           if (keys) *reinterpret_cast<float2*>(A + i * AP + j) = make_float2(f[0], f[1]);
-          else cut(f[0], f[1], terms[r][c]);
+          else {
+            cut(f[0], f[1], terms[r][c]);
+            odd = fmaf(f[0], 0.f, fmaf(f[1], 0.f, odd));
+          }
         }
       }
     if (!keys) {
+      // q_i . k_j may pass what 32 bits hold where u_j or the decay between is 0 and out sees nothing of it.  A NaN in place of a beta makes the chain take the window token by token.
+      if (__any_sync(0xffffffffu, odd != 0.f) && lane == 0) record.beta[16 * strip] = NAN;
 #pragma unroll
       for (int r = 0; r < 2; ++r)
 #pragma unroll

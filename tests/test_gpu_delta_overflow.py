@@ -1,0 +1,67 @@
+"""The gated delta rule where products pass what 32 bits hold although the rule itself stays finite: sums over a window that the formula never forms, and states that a decay takes back."""
+import math
+
+import pytest
+import torch
+
+import delta_reference as ref
+from paper_2402_04466_b200 import binding
+from test_gpu_delta_rule import TYPES, _case, _check
+from token_reference import check
+
+pytestmark = pytest.mark.gpu
+
+HEADS = [(2, 32), (2, 64), (2, 128), (40, 32), (20, 64), (10, 128)]
+
+
+def _call(q, k, v, decay, beta, state, **kw):
+    return binding.delta_rule(q, k, v, decay, beta, state, state_out=torch.full_like(state, math.nan), **kw)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("H,D", HEADS)
+@pytest.mark.parametrize("T", [60, 65, 150])
+def test_products_of_two_keys(cuda_device, dtype, H, D, T):
+    """Two keys of 1e20 whose corrections are 0: k_i . k_j is no number of 32 bits, and the rule never asks for it."""
+    B = 4
+    q, k, v, decay, beta, state = _case(cuda_device, D + T, B, T, H, H, D, dtype)
+    for b, (i, j) in enumerate(((5, 9), (12, 20), (33, 59))):      # in a half of a window, over both halves, in the second window
+        k[b, i, 0], k[b, j, 0] = 1e20, 1e20
+        beta[b, i, 0] = beta[b, j, 0] = 0.0
+    _check(*_call(q, k, v, decay, beta, state), q, k, v, decay, beta, state, 1.0, None, "keys")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("H,D", HEADS)
+@pytest.mark.parametrize("T", [60, 65, 150])
+def test_products_of_a_query_and_an_earlier_key(cuda_device, dtype, H, D, T):
+    """A query of 1e20 behind a key of 1e20 that corrected nothing, and one behind a decay that forgot what the key left."""
+    B = 4
+    q, k, v, decay, beta, state = _case(cuda_device, D + T, B, T, H, H, D, dtype)
+    for b, (i, j) in enumerate(((5, 9), (12, 20), (33, 59))):
+        k[b, i, 0], q[b, j, 0], beta[b, i, 0] = 1e20, 1e20, 0.0
+    k[3, 8, 1], q[3, 14, 1], decay[3, 11, 1] = 1e15, 1e25, -math.inf
+    beta[3, 8, 1] = 2.0 ** -110      # beta |k|^2 is 0.1 at most
+    _check(*_call(q, k, v, decay, beta, state), q, k, v, decay, beta, state, 1.0, None, "queries")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("H,D", HEADS)
+@pytest.mark.parametrize("T", [60, 65, 150])
+@pytest.mark.parametrize("length", [3.0, 10.0])
+def test_tokens_before_a_state_overflows(cuda_device, dtype, H, D, T, length):
+    """One key again and again, so long that every token makes the state eight times, or a hundred times, larger: what is not finite at last is not
+    finite for the tokens before."""
+    B, first = 2, 35
+    q, k, v, _, beta, state = _case(cuda_device, D, B, T, H, H, D, dtype)
+    k[0, first:, 0] = length * D ** -0.5
+    beta[0, first:, 0] = 1.0
+    out, new = _call(q, k, v, None, beta, state)
+    want, size, S, A = ref.delta(q, k, v, None, beta, state)
+    # An error grows as the state does, by |k|^2 - 1 a token, in every column alike: it is measured against the longest column, and a token adds a sum's roundings of that.
+    widest = size.amax(-1, keepdim=True)
+    some = ((2 * D + 16) * T * ref.STEP + (2.0 ** -8 if dtype == torch.bfloat16 else 0.0)) * widest + ref.half_step(dtype) * want.abs()
+    held = (widest < 1e34).expand_as(want)
+    assert held[0, :first + 13, 0].all() and held[1].all() and held[0, :, 1].all()
+    check(out[held], want[held], some[held], "before")
+    assert torch.isfinite(new[1]).all() and torch.isfinite(new[0, 1:]).all()
