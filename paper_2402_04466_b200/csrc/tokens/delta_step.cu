@@ -1,6 +1,6 @@
 // The gated delta rule, token by token (tt_delta_rule).  With S a head's state [key][value], a = exp(log_decay):
-//   u = beta (v - a S^T k),  S' = a S + k u^T,  out = scale S'^T q = scale (a S^T q + (k . q) u).
-// The second form of out lets one pass over the state give both sums, S^T k and S^T q, so that a single meeting of the block's threads lies
+//   F = a S,  u = beta (v - F^T k),  S' = F + k u^T,  out = scale S'^T q = scale (F^T q + (k . q) u).
+// The second form of out lets one pass over the state give both sums, F^T k and F^T q, so that a single meeting of the block's threads lies
 // between reading a state and writing it.  A block owns a run of W value columns of one head's state (the columns are
 // independent of each other), LANES = W / 4 threads to a row, in registers for the whole call: a token by itself reads and writes each state once, and that bounds
 // many states (256 sessions of 8 heads of 128, 268 MB: 49 us, 84 % of the rate of a copy).  Few states are bound by the launch (4.2 us); a further token takes 1 us.
@@ -17,9 +17,10 @@ struct DeltaStep {
   static constexpr int ROWS = D * LANES / THREADS;                      // rows to a thread
 };
 
-// SEVERAL: the next token's operands are fetched while this one is worked on
+// SEVERAL: the next token's operands are fetched while this one is worked on.  (Bounds on registers: without them the path of products that overflow costs 24 fp32 tokens of 256 x 8 heads
+// of 128 100 us of the 397 that they take.)
 template <typename T, int D, int W, bool SEVERAL>
-__global__ void __launch_bounds__(256) delta_step_kernel(const __grid_constant__ DeltaParams p) {
+__global__ void __launch_bounds__(256, !SEVERAL ? 0 : D == 128 ? 2 : 3) delta_step_kernel(const __grid_constant__ DeltaParams p) {
   using Shape = DeltaStep<D, W>;
   constexpr int LANES = Shape::LANES, ROWS = Shape::ROWS, STEP = Shape::THREADS / LANES, WARPS = Shape::THREADS / 32;
   // of either parity of tokens: a warp may be at the next one while another still reads these
@@ -69,6 +70,8 @@ __global__ void __launch_bounds__(256) delta_step_kernel(const __grid_constant__
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
       kq = fmaf(kk[i], qq[i], kq);
+      // before the sums: those of a state that the decay takes back may pass what 32 bits hold
+      s[i].x *= fade; s[i].y *= fade; s[i].z *= fade; s[i].w *= fade;
       x[0] = fmaf(kk[i], s[i].x, x[0]); x[1] = fmaf(kk[i], s[i].y, x[1]); x[2] = fmaf(kk[i], s[i].z, x[2]); x[3] = fmaf(kk[i], s[i].w, x[3]);
       y[0] = fmaf(qq[i], s[i].x, y[0]); y[1] = fmaf(qq[i], s[i].y, y[1]); y[2] = fmaf(qq[i], s[i].z, y[2]); y[3] = fmaf(qq[i], s[i].w, y[3]);
     }
@@ -93,13 +96,13 @@ __global__ void __launch_bounds__(256) delta_step_kernel(const __grid_constant__
       const float4 f = said[t & 1][w][lane];
       sx.x += f.x; sx.y += f.y; sx.z += f.z; sx.w += f.w;
     }
-    const float u[4] = {beta * (vv[0] - fade * sx.x), beta * (vv[1] - fade * sx.y), beta * (vv[2] - fade * sx.z), beta * (vv[3] - fade * sx.w)};
+    const float u[4] = {beta * (vv[0] - sx.x), beta * (vv[1] - sx.y), beta * (vv[2] - sx.z), beta * (vv[3] - sx.w)};
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
-      s[i].x = fmaf(fade, s[i].x, kk[i] * u[0]);
-      s[i].y = fmaf(fade, s[i].y, kk[i] * u[1]);
-      s[i].z = fmaf(fade, s[i].z, kk[i] * u[2]);
-      s[i].w = fmaf(fade, s[i].w, kk[i] * u[3]);
+      s[i].x = fmaf(kk[i], u[0], s[i].x);
+      s[i].y = fmaf(kk[i], u[1], s[i].y);
+      s[i].z = fmaf(kk[i], u[2], s[i].z);
+      s[i].w = fmaf(kk[i], u[3], s[i].w);
     }
     if (threadIdx.x < LANES) {
       float4 sy = asked[t & 1][0][lane];
@@ -110,11 +113,20 @@ __global__ void __launch_bounds__(256) delta_step_kernel(const __grid_constant__
         sy.x += f.x; sy.y += f.y; sy.z += f.z; sy.w += f.w;
         dot += dots[t & 1][w];
       }
+      float sum[4] = {fmaf(dot, u[0], sy.x), fmaf(dot, u[1], sy.y), fmaf(dot, u[2], sy.z), fmaf(dot, u[3], sy.w)};
+      if (__builtin_expect(!isfinite(dot), 0)) {
+        // k . q passes what 32 bits hold, or an element is not finite: q (k u) then, as the state has it
+        sum[0] = sy.x; sum[1] = sy.y; sum[2] = sy.z; sum[3] = sy.w;
+#pragma unroll 1
+        for (int i = 0; i < D; ++i) {
+          const float ki = to_float(k[t * p.k.t - row + i]), qi = to_float(q[t * p.q.t - row + i]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) sum[j] = fmaf(qi, ki * u[j], sum[j]);
+        }
+      }
       T* to = o + t * p.o.t;
-      to[0] = (T)(p.scale * fmaf(fade, sy.x, dot * u[0]));
-      to[1] = (T)(p.scale * fmaf(fade, sy.y, dot * u[1]));
-      to[2] = (T)(p.scale * fmaf(fade, sy.z, dot * u[2]));
-      to[3] = (T)(p.scale * fmaf(fade, sy.w, dot * u[3]));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) to[j] = (T)(p.scale * sum[j]);
     }
   }
   if (n == 0 && p.state_out == p.state) return;

@@ -18,6 +18,17 @@ def _call(q, k, v, decay, beta, state, **kw):
     return binding.delta_rule(q, k, v, decay, beta, state, state_out=torch.full_like(state, math.nan), **kw)
 
 
+def _element_by_element(got, q, k, v, decay, beta, state):
+    """Against the columns as they stood.  (In the mean _check counts errors as independent and against the state that is left.  Where one large state fades, exp(log_decay) is off by
+    up to two steps for all of it alike, 2^-22 by itself against 2.6 * 2^-23 in the mean that heads of 32 are allowed, and a correction that takes 1 - beta |k|^2 of it, a fiftieth,
+    leaves fifty times the share.)"""
+    want, size, S, A = ref.delta(q, k, v, decay, beta, state)
+    assert torch.isfinite(want).all() and torch.isfinite(S).all()
+    bound, state_bound = ref.bounds(want, size, A, v.shape[3], v.shape[1], v.dtype, v.shape[1] > 1)
+    check(got[0], want, bound, "out")
+    check(got[1], S, state_bound, "state")
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("H,D", HEADS)
 @pytest.mark.parametrize("T", [60, 65, 150])
@@ -65,3 +76,27 @@ def test_tokens_before_a_state_overflows(cuda_device, dtype, H, D, T, length):
     assert held[0, :first + 13, 0].all() and held[1].all() and held[0, :, 1].all()
     check(out[held], want[held], some[held], "before")
     assert torch.isfinite(new[1]).all() and torch.isfinite(new[0, 1:]).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("H,D", HEADS)
+@pytest.mark.parametrize("T", [1, 2, 8, 60, 150])
+def test_product_of_a_token_s_query_and_key(cuda_device, dtype, H, D, T):
+    """Both of 1e20, with a correction of 0, at the first and last token."""
+    q, k, v, decay, beta, state = _case(cuda_device, D + T, 3, T, H, H, D, dtype)
+    for b, t in ((0, 0), (1, T - 1)):
+        q[b, t, 0], k[b, t, 0], beta[b, t, 0] = 1e20, 1e20, 0.0
+    _check(*_call(q, k, v, decay, beta, state), q, k, v, decay, beta, state, 1.0, None, "one token")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("H,D", HEADS + [(8, 128)])
+@pytest.mark.parametrize("T", [1, 2, 8])
+def test_a_state_that_is_forgotten(cuda_device, dtype, H, D, T):
+    """Elements of 1e38, which a key of length 1 adds up to more than 32 bits hold: all of it fades before it is read, at once or to some thousand."""
+    B = 20 if D == 128 and H == 8 else 3
+    q, k, v, decay, beta, state = _case(cuda_device, D + T, B, T, H, H, D, dtype)
+    q[:2, 0, 0], k[:2, 0, 0] = 0.9 * D ** -0.5, 0.9 * D ** -0.5
+    state[:2, 0] = 1e38
+    decay[0, 0, 0], decay[1, 0, 0] = -math.inf, -80.0
+    _element_by_element(_call(q, k, v, decay, beta, state), q, k, v, decay, beta, state)
