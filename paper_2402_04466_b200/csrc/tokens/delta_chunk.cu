@@ -12,7 +12,7 @@
 // columns takes 40 cycles however few its columns are, and its way through tensor memory twice that: the chain would be longer, not shorter.  Windows of 64 have four times the
 // triangle (with the warps as they were then, 909 us to 748 for the same maps).
 //
-// Eight maps of 14400 tokens, 4 heads of 64: 421 us, of which reading and writing it all once would be 37; 64 sequences of up to 497 tokens, 4 heads of 128: 158 us of 17.
+// Eight maps of 14400 tokens, 4 heads of 64: 426 us, of which reading and writing it all once would be 37; 64 sequences of up to 497 tokens, 4 heads of 128: 158 us of 17.
 //
 // The state is fp32, and so is everything between two products: an operand that is not bf16 to begin with is cut into three bf16 terms (8 + 8 + 8 bits), of whose
 // products those of 2^-16 and more count.  Only what out alone reads is rounded further: in bf16 calls S, U and P count with 16 bits.  (P rounded
@@ -57,6 +57,28 @@ struct Shape {
   static_assert(!ALONE || TERMS == 1, "keys and queries lie as the preparation reads them");
   static constexpr bool FITS = SMEM + 1024 <= 227 * 1024;
 };
+
+// A tile's S^T (e^G q): `state` the lane's registers of S^T, q its token's elements, up that token's e^G
+template <typename H>
+__device__ __noinline__ float4 read_faded(const uint32_t* state, const typename H::T* q, float up) {
+  float sum[4] = {};
+#pragma unroll 1
+  for (int x = 0; x < H::KS; ++x) {
+    uint32_t a[H::SEEN][4], f[3][2];
+#pragma unroll
+    for (int e = 0; e < H::SEEN; ++e) load16(a[e], state + (e * H::KS + x) * 128);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const typename H::T* z = q + x * 16 + 8 * e;
+      uint32_t terms[3];
+      cut(up * to_float(z[0]), up * to_float(z[1]), terms);
+#pragma unroll
+      for (int c = 0; c < 3; ++c) f[c][e] = terms[c];
+    }
+    product(sum, a, f);
+  }
+  return make_float4(sum[0], sum[1], sum[2], sum[3]);
+}
 
 template <typename H>
 __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid_constant__ DeltaParams p) {
@@ -259,6 +281,16 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
             product(acc[m][1], a[1], f[1]);
           }
         }
+        // S^T q may pass what 32 bits hold where what the window's decay leaves of it does not: S^T (e^G q) then
+        bool odd = false;
+        if (record.whole < 0x1p-24f) {
+          float sum = 0.f;
+#pragma unroll
+          for (int m = 0; m < MINE; ++m)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum = fmaf(acc[m][0][e] + acc[m][1][e], 0.f, sum);
+          odd = __any_sync(0xffffffffu, sum != 0.f);
+        }
 #pragma unroll
         for (int m = 0; m < MINE; ++m) {
           const float2 up = *reinterpret_cast<const float2*>(record.up + 8 * (warp + OG * m) + 2 * t);
@@ -267,6 +299,14 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
           for (int e = 0; e < 4; ++e) {
             acc[m][0][e] = (acc[m][0][e] + acc[m][1][e]) * gain[e & 1];
             acc[m][1][e] = 0.f;
+          }
+        }
+        if (__builtin_expect(odd, 0)) {
+#pragma unroll
+          for (int m = 0; m < MINE; ++m) {
+            const int i0 = 8 * (warp + OG * m);
+            const float4 sum = read_faded<H>(s_seen + ((w & 1) * RUNS + run) * SEEN * KS * 128 + lane * 4, qs + (i0 + g) * QP + 2 * t, record.up[i0 + g]);
+            acc[m][0][0] = p.scale * sum.x; acc[m][0][1] = p.scale * sum.y; acc[m][0][2] = p.scale * sum.z; acc[m][0][3] = p.scale * sum.w;
           }
         }
       }

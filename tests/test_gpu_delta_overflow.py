@@ -100,3 +100,19 @@ def test_a_state_that_is_forgotten(cuda_device, dtype, H, D, T):
     state[:2, 0] = 1e38
     decay[0, 0, 0], decay[1, 0, 0] = -math.inf, -80.0
     _element_by_element(_call(q, k, v, decay, beta, state), q, k, v, decay, beta, state)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("H,D", HEADS)
+@pytest.mark.parametrize("T", [60, 65, 150])
+def test_a_state_that_is_forgotten_within_a_window(cuda_device, dtype, H, D, T):
+    """The same by windows, with keys of which such a state says nothing, so that only the queries' sums pass 32 bits: at the first token, and where the second window begins."""
+    q, k, v, decay, beta, state = _case(cuda_device, D + T, 4, T, H, H, D, dtype)
+    sign = torch.ones(D, device=cuda_device)
+    sign[1::2] = -1
+    state[:3, 0] = 1e38
+    q[:2, 0, 0], k[:2, 0, 0] = 0.9 * D ** -0.5, (0.9 * D ** -0.5 * sign).to(dtype)
+    decay[0, 0, 0], decay[1, 0, 0] = -math.inf, -80.0
+    q[2, :32, 0], k[2, :32, 0], beta[2, :32, 0], decay[2, :32, 0] = 0.0, 0.0, 0.0, 0.0
+    q[2, 32, 0], k[2, 32, 0], decay[2, 32, 0] = 0.9 * D ** -0.5, (0.9 * D ** -0.5 * sign).to(dtype), -math.inf
+    _element_by_element(_call(q, k, v, decay, beta, state), q, k, v, decay, beta, state)
