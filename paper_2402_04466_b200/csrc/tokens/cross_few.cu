@@ -14,7 +14,8 @@
 //
 // Differential attention (MAPS = 2, tt_differential_attention): the two halves of a head's columns make two maps of scores, for the same number of products, and each tile of values meets
 // both maps' weights while its registers are there, for twice as many.  The joins take both maps; a warp to a row ends with lambda and the norm, which reads the whole row.  The
-// same eight streams 25.3 us, of which K and V would be 14; the same five with masks 12.4; clips of 60 keys 6.2.
+// same eight streams 25.3 us, of which K and V would be 14; the same five with masks 12.4; clips of 60 keys 6.2.  With heads of 128 eight streams of 14400 keys take 46.3 us call by call (88.2 with
+// the block's sums beside the rings, where two blocks did not fit a multiprocessor).
 #include "tokens.h"
 
 #include "token_ptx.cuh"
@@ -48,8 +49,11 @@ struct Few {
   static constexpr int NT = D / 8;             // products across the columns of the sums
   static constexpr int OP = D + 8;             // pitch of the joint sums
   static constexpr int SMEM = WARPS * RING + 1024;
-  static constexpr int BLOCKS = W == 4 ? 2 : 1;                   // to a multiprocessor
-  static_assert(MAPS * WARPS * 16 * OP * 4 <= WARPS * RING, "the sums take the rings' place");
+  static constexpr int SUMS = MAPS * WARPS * 16 * OP * 4;         // bytes of the warps' sums, behind which lie the block's
+  static_assert(SUMS + MAPS * 16 * D * 4 <= WARPS * RING, "the sums take the rings' place");
+  static constexpr int BLOCKS = W == 4 ? 2 : 1;                   // to a multiprocessor: cross_plan counts on them
+  static constexpr int STATIC = WARPS * STAGES * 8 + MAPS * (WARPS + 1) * 16 * 8 + 16 * 4;
+  static_assert(BLOCKS * (SMEM + STATIC + 1024) <= 228 * 1024, "shared memory, of which each block takes 1 KB more");
 };
 
 // Where row `row`'s run `run` of 8 elements lies in a swizzled half of a tile.
@@ -103,7 +107,6 @@ __global__ void __launch_bounds__(Few<D, W, MAPS>::THREADS, Few<D, W, MAPS>::BLO
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t s_full[F::WARPS][F::STAGES];
   __shared__ float2 s_ml[MAPS][F::WARPS][16];
-  __shared__ __align__(16) float s_sum[MAPS][16][D];
   __shared__ float2 s_stat[MAPS][16];
   __shared__ float s_lambda[16];
   uint8_t* ring0 = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -364,6 +367,7 @@ __global__ void __launch_bounds__(Few<D, W, MAPS>::THREADS, Few<D, W, MAPS>::BLO
   // join the warps: row r of the tile, element d.  The sums take the place of the rings, whose copies have all landed.
   __syncthreads();
   float* s_o = reinterpret_cast<float*>(ring0);      // [MAPS][WARPS][16][OP]
+  auto& s_sum = *reinterpret_cast<float (*)[MAPS][16][D]>(ring0 + F::SUMS);      // the block's: in the same place in every block of a cluster
 #pragma unroll
   for (int w = 0; w < MAPS; ++w)
 #pragma unroll

@@ -1,0 +1,34 @@
+"""What the plan of cross and differential attention takes for granted of their kernel for few queries (no GPU needed)."""
+import os
+import re
+
+import pytest
+
+TOKENS = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2402_04466_b200", "csrc", "tokens")
+SIZES = {"uint64_t": 8, "float2": 8, "float": 4}
+
+
+def _shared_bytes(D, warps, maps):
+    """-> (static, dynamic) bytes of a block, from the declarations."""
+    code = re.sub(r"/\*.*?\*/|//[^\n]*", "", open(os.path.join(TOKENS, "cross_few.cu")).read(), flags=re.S)
+    few = dict(D=D, W=warps, M=maps)
+    for name, value in re.findall(r"static constexpr int (\w+) = ([^;]+);", code[code.index("struct Few"):code.index("run_at")]):
+        value = re.sub(r"(.+?) \? (.+?) : (.+)", r"(\2) if (\1) else (\3)", value).replace("/", "//")
+        few[name] = eval(value, {}, few)
+    static = 0
+    for kind, dims in re.findall(r"(?<!extern )__shared__ (?:__align__\(\d+\) )?(\w+) \w+((?:\[[^\]]+\])+);", code):
+        n = SIZES[kind]
+        for d in re.findall(r"\[([^\]]+)\]", dims):
+            n *= eval(d.replace("F::", ""), {}, few | dict(MAPS=maps))
+        static += n
+    return static, few["SMEM"]
+
+
+@pytest.mark.parametrize("maps", [1, 2])
+@pytest.mark.parametrize("D", [32, 64, 128])
+def test_as_many_blocks_fit_a_multiprocessor_as_the_plan_counts_on(D, maps):
+    """cross_plan makes up to two blocks of four warps to a multiprocessor, or one of eight.  A multiprocessor has 228 KB, of which each block takes 1 KB more than it asks for."""
+    for warps, blocks in ((4, 2), (8, 1)):
+        static, dynamic = _shared_bytes(D, warps, maps)
+        assert static >= warps * 3 * 8 + maps * 17 * 8 * warps // 2 and dynamic >= warps * 24576      # the declarations were read
+        assert blocks * (static + dynamic + 1024) <= 228 * 1024, (static, dynamic)
