@@ -431,11 +431,11 @@ CrossPlan cross_plan(int batch, int q_tokens, int kv_tokens, int heads, int grou
   // one entry's 256 queries of 2 heads (0.15) 8.8 16.9, 10.5 21.6, 15.4 32.1; 700 (0.42) 18.2 17.5, 24.1 22.1, 40.9 34.8; 8 x 4 heads on 14400 keys, 65 queries
   // (2.3) 55.4 50.6, 81.5 52.6, 158 65.9.  So it is not taken too soon, and up to a third (heads of 64) or a half (128) too late where entries are several and
   // keys fewer than that.  (Masks are the other kernel's whatever the size; up to 64 queries leave three quarters of a tile of 256 rows empty.)
-  // Of two maps (differential attention) the sums are twice as many, and a tile of the kernel for many has 128 queries: it takes work from 0.2 million on, 0.1 with heads of 128,
-  // and 33 queries.  Measured in the same way: 5 x 2 heads on 4800 keys, 33 queries (0.14 million) 14.6 22.7, 16.6 22.8, 41.1 26.8; 65 (0.24) 24.8 22.7, 29.0 23.0, 76 34; 256
-  // (0.77) 41 25, 57 31, 119 43; one entry's 256 queries of 2 heads (0.15) 14.6 22.7, 16.6 24.8, 58 37; 400 (0.24) 24.7 22.7, 28.9 24.8, 77 39; 8 x 4 heads on 14400 keys, 33
-  // queries (1.4) 53.5 53.6, 78 58, 166 68.
-  const int64_t border = maps == 1 ? 500000 : D == 128 ? 100000 : 200000;
+  // Of two maps (differential attention) the sums are twice as many, and a tile of the kernel for many has 128 queries: it takes work from 0.2 million on,
+  // and 33 queries.  Measured in the same way: 5 x 2 heads on 4800 keys, 33 queries (0.14 million) 14.6 22.7, 16.6 22.8, 22.5 26.6; 65 (0.24) 24.8 22.7, 29.0 23.0, 40.8 32.8; 128
+  // (0.38) 25.1 22.6, 34.8 26.7, 57.7 39.1; one entry's 256 queries of 2 heads (0.15) 14.6 22.7, 16.6 24.8, 21.9 37.6; 400 (0.24) 24.7 22.7, 28.9 24.8, 39.8 38.9; 8 x 4 heads on 14400
+  // keys, 33 queries (1.4) 53.5 53.6, 78 58, 134 74.  (Too soon, up to a third, for two entries' 65 queries of 2 heads on 14400 keys, 0.29 million: 18.4 32.7, 24.6 32.8, 41.0 51.2.)
+  const int64_t border = maps == 1 ? 500000 : 200000;
   if (bf16 && !mask && q_tokens > (maps == 1 ? 64 : 32) && kv_tokens > 0 &&
       ((int64_t)q_tokens * group + 15) / 16 * batch * (heads / group) >= border / kv_tokens + 1) {
     plan.kernel = CROSS_TC;
