@@ -460,8 +460,12 @@ CrossPlan cross_plan(int batch, int q_tokens, int kv_tokens, int heads, int grou
     plan.kernel = CROSS_SCALAR;
     plan.rows = rows <= 16 ? 16 : 64;
     const int64_t blocks = (rows + plan.rows - 1) / plan.rows * batch * (heads / group);
-    // split the keys where the row tiles are fewer than two to a multiprocessor, down to two tiles of keys to a block
-    int64_t splits = blocks > 0 ? 2 * PLAN_SMS / blocks : 1;
+    // Split the keys where the row tiles are fewer than two to a multiprocessor, down to two tiles of keys to a block.  Of two maps two blocks with 64 rows fit a multiprocessor with heads
+    // of 32 only (registers, and shared memory by 3 KB with heads of 64), and blocks with 16 rows lose more by twice the parts to join than the second gains: one to a multiprocessor then.  Both
+    // measured, us with one and with two: 1023 queries of 2 heads on 4096 keys, heads of 32 75.6 67.7, of 64 108.8 116.7, of 128 185.6 192.6; 300 queries, heads of 64 49 64, of
+    // 128 75 96; 7 queries of 5 x 2 heads on 4800 keys 26.6 28.7, 36.9 38.9, 53.3 60.0.
+    const int64_t fit = maps == 2 && !(D == 32 && plan.rows == 64) ? 1 : 2;
+    int64_t splits = blocks > 0 ? fit * PLAN_SMS / blocks : 1;
     const int64_t most = ((int64_t)kv_tokens + 2 * BN - 1) / (2 * BN);
     if (splits > most) splits = most;
     if (splits < 1) splits = 1;
