@@ -71,11 +71,14 @@ cudaError_t launch_delta_step(const DeltaParams& p, bool bf16, int D, cudaStream
 cudaError_t launch_delta_prepare(const DeltaParams& p, bool bf16, int D, cudaStream_t s);   // of every window, what depends on no state
 cudaError_t launch_delta_chunk(DeltaParams p, bool bf16, int D, cudaStream_t s);            // a window of tokens at a time, prepared range by range or on the way
 uint64_t delta_scratch(int batch, int tokens, int heads, int D, bool bf16);
-// Few tokens are taken one by one: a window takes its way through the products whatever it holds.  Both measured, us one by one and by window, five entries of 2 heads of 64
-// and 256 of 8 heads of 128: bf16, 8 tokens 8.2 6.2, 153 181, 12 tokens 10.3 6.2, 211 182; fp32, 12 tokens 10.3 10.3, 208 491, 16 tokens 12.3 10.3, 266 503, 24 tokens
-// 16.4 10.3, 383 528.
+// Few tokens are taken one by one: a window takes its way through the products whatever it holds.  Both measured, us one by one and by window.  bf16, 8 and 12 tokens, heads of 32, 64, 128: five
+// entries of 2 heads 5.1 5.6, 7.0 6.3; 7.6 6.3, 9.8 6.3; 9.1 6.4, 11.9 7.0; 256 of 8 heads 37 50, 53 52; 56 72, 78 72; 156 191, 218 191.  fp32, 12 and 16 tokens, heads of 32 and 64: five entries
+// 6.4 7.8, 8.3 7.7; 9.7 9.0, 11.9 9.0; 256 53 66, 70 67; 78 102, 100 103.  fp32 windows of heads of 128 take longest and have a block to a multiprocessor: five entries, 12 tokens 12.0 11.1; 160
+// states (few more than multiprocessors, which is two rounds of blocks one by one) 24 tokens 49 51, 28 56 53; 296 states 32 tokens 79 89, 33 82 125, 48 115 127, 56 132 129; 2048 states 24 tokens
+// 396 561, 33 532 836, 48 760 853.
 inline bool delta_by_window(int batch, int tokens, int heads, int D, bool bf16) {
-  return tokens > (bf16 ? 8 : D == 128 && (int64_t)batch * heads >= PLAN_SMS ? 24 : 12);
+  const int64_t states = (int64_t)batch * heads;
+  return tokens > (bf16 ? 8 : D < 128 || states < PLAN_SMS ? 12 : states < 2 * PLAN_SMS ? 24 : 48);
 }
 
 struct alignas(32) CrossParams {

@@ -7,7 +7,7 @@ import torch
 import delta_reference as ref
 from paper_2402_04466_b200 import binding
 from test_gpu_delta_overflow import _element_by_element
-from test_gpu_delta_rule import BF16, TYPES, _case
+from test_gpu_delta_rule import BF16, FP32, TYPES, _case, _check
 
 pytestmark = pytest.mark.gpu
 
@@ -39,3 +39,16 @@ def test_rows_of_several_bf16_tokens(cuda_device, B, T, H, K, D, alike):
     rounded = want.to(BF16).double()
     off = float((out.double() - rounded).norm() / want.norm())
     assert off < 3 ** 0.5 * 2.0 ** -10.5, f"off by {off:.2e}"
+
+
+@pytest.mark.parametrize("B,T", [(74, 25), (74, 33), (74, 48), (74, 49), (73, 25), (80, 47)])
+def test_many_fp32_states_of_heads_of_128(cuda_device, B, T):
+    """On either side of the border between token by token and windows, with lengths and slots."""
+    q, k, v, decay, beta, state = _case(cuda_device, B + T, B, T, 4, 2, 128, FP32, slots=B + 1)
+    n = [T - b % 5 if b % 7 else b % 3 for b in range(B)]
+    lengths, slots = torch.tensor(n, dtype=torch.int32, device=cuda_device), torch.arange(B, 0, -1, dtype=torch.int32, device=cuda_device)
+    before = state.clone()
+    out, _ = binding.delta_rule(q, k, v, decay, beta, state, lengths=lengths, slots=slots)
+    at = slots.long()
+    _check(out, state[at], q, k, v, decay, beta, before[at], 1.0, n, "many")
+    assert torch.equal(state[0], before[0]) and all((out[b, n[b]:] == 0).all() for b in range(B))
