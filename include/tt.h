@@ -544,8 +544,8 @@ tt_status tt_linear_attention(const tt_linear_attention_args* args, void* cuda_s
  * log_decay, beta: device fp32 [batch][tokens][heads], contiguous; log_decay is 0 or below (-infinity: a state that was finite is forgotten), NULL: no decay.
  * state, state_out, num_slots, slots, lengths, scratch: as in tt_linear_attention.  The state counts with fp32's bits whatever the precision; of several TT_BF16 tokens out reads the state and
  * the tokens' corrections with 16 bits, so that it is off by its own rounding and little more.
- * An infinity or NaN in a token or a state makes the elements of the state and of out that read it not finite, from its token on; earlier tokens, other columns of
- * values and other heads see nothing of it.
+ * An infinity or NaN in a token or a state, or a state that passes what fp32 holds, makes the elements of the state and of out that read it not finite, from its token on; earlier tokens,
+ * other columns of values and other heads see nothing of it.
  */
 typedef struct {
   uint32_t struct_size;            /* = sizeof(tt_delta_rule_args) */
@@ -610,7 +610,7 @@ tt_status tt_cross_attention(const tt_cross_attention_args* args, void* cuda_str
  * query that sees nothing gets zeros.  What a query does not see has no influence on its row; an infinity or NaN among the values that it sees makes the
  * elements of y_i that read it not finite (with the norm, which reads them all, no element of the row says anything).
  * TT_BF16 weights count with 16 bits, but are rounded to bf16 in large calls of more than 32 queries without a mask (y is then off by up to 2e-3 of the two sums'
- * size); their sums are of the weights before that.
+ * size); their sums are of the weights before that.  In those calls one exponential in four is off by up to 4e-6 of itself with heads of 128, all others by 2^-22.
  */
 typedef struct {
   uint32_t struct_size;            /* = sizeof(tt_differential_attention_args) */

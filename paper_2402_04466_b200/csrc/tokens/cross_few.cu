@@ -14,7 +14,7 @@
 //
 // Differential attention (MAPS = 2, tt_differential_attention): the two halves of a head's columns make two maps of scores, for the same number of products, and each tile of values meets
 // both maps' weights while its registers are there, for twice as many.  The joins take both maps; a warp to a row ends with lambda and the norm, which reads the whole row.  The
-// same eight streams 25.3 us, of which K and V would be 14; the same five with masks 12.4; clips of 60 keys 6.2.  With heads of 128 eight streams of 14400 keys take 46.3 us call by call (88.2 with
+// same eight streams 23.6 us, of which K and V would be 14; the same five with masks 11.5; clips of 60 keys 5.1.  With heads of 128 eight streams of 14400 keys take 46.3 us call by call (88.2 with
 // the block's sums beside the rings, where two blocks did not fit a multiprocessor).
 #include "tokens.h"
 

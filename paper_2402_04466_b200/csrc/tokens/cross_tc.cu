@@ -14,8 +14,8 @@
 // TFLOP/s.  Weights are rounded to bf16 once, as far as out itself is; their sum is of the weights before that.
 //
 // Differential attention (MAPS = 2, tt_differential_attention): the two tiles of a block are the two maps of one tile of queries, each with scores from its half of the columns, and the same tile of
-// values for both; where a tile ends each map's warps read half of the columns of both maps' sums for lambda and the norm, whose squares they add up through shared memory.  Twice the exponentials to half the products of scores: the same sizes 544 us with heads of 64 (the
-// exponentials alone 325) and 396 with heads of 128.
+// values for both; where a tile ends each map's warps read half of the columns of both maps' sums for lambda and the norm, whose squares they add up through shared memory.  Twice the exponentials to half the products of scores: the same sizes 542 us with heads of 64 (the
+// exponentials alone 325) and 390 with heads of 128 (415 to 450 where calls go on for long: the clock falls from 1965 to 1750-1840 MHz).
 #include "tokens.h"
 
 #include <cuda.h>
@@ -79,7 +79,7 @@ struct Cfg {
 };
 
 // 2^lo and 2^hi on the fp32 units, to 4 10^-6: the nearest whole number n goes to the exponent (Cody and Waite), and 2^f, |f| <= 1/2, is the polynomial of degree 4 through its
-// values at the Chebyshev points.  Arguments are below 2^7; what is below -127 becomes 2^-127, and a NaN stays one.
+// values at the Chebyshev points.  Arguments are below 2^7; what is below -126.5 becomes 0, and a NaN stays one.
 constexpr float P0 = 1.f, P1 = 0.693121045f, P2 = 0.24022349f, P3 = 0.0559219758f, P4 = 0.00966636852f;
 struct Polynomial {
   Two p0, p1, p2, p3, p4, magic;

@@ -12,7 +12,7 @@
 // columns takes 40 cycles however few its columns are, and its way through tensor memory twice that: the chain would be longer, not shorter.  Windows of 64 have four times the
 // triangle (with the warps as they were then, 909 us to 748 for the same maps).
 //
-// Eight maps of 14400 tokens, 4 heads of 64: 426 us, of which reading and writing it all once would be 37; 64 sequences of up to 497 tokens, 4 heads of 128: 158 us of 17.
+// Eight maps of 14400 tokens, 4 heads of 64: 423 us, of which reading and writing it all once would be 37; 64 sequences of up to 497 tokens, 4 heads of 128: 155 us of 17.
 //
 // The state is fp32, and so is everything between two products: an operand that is not bf16 to begin with is cut into three bf16 terms (8 + 8 + 8 bits), of whose
 // products those of 2^-16 and more count.  Only what out alone reads is rounded further: in bf16 calls S, U and P count with 16 bits.  (P rounded
@@ -605,9 +605,9 @@ cudaError_t launch_shape(const DeltaParams& p, cudaStream_t s) {
   return launch_kernel(delta_chunk_kernel<H>, dim3(H::D / H::COLS, (unsigned)p.heads, (unsigned)p.batch), H::THREADS, H::SMEM, s, p, !H::ALONE);
 }
 // One warp to a run where runs are many, four where they are few, and one for heads of 32, whose state is one warp's worth.  Measured, us:
-//   bf16, heads of 64, 128 runs of 14400 tokens: one 823, four 442; heads of 128, 2048 runs of 497 tokens: one 158, four 236;
-//   fp32, heads of 64, 16 runs of 4801 tokens: one 440, four 215; 512 runs of 1000: one 138, four 228 (of heads of 128 four runs do not fit a block);
-//   heads of 32, 8 runs of 4801 tokens: one 151 bf16 and 208 fp32, two 172 and 246; 256 runs of 1000: one 52 and 75, two 58 and 82.
+//   bf16, heads of 64, 128 runs of 14400 tokens: one 747, four 423; heads of 128, 2048 runs of 497 tokens: one 203, four 289;
+//   fp32, heads of 64, 16 runs of 4801 tokens: one 452, four 210; 512 runs of 1000: one 148, four 233 (of heads of 128 four runs do not fit a block);
+//   heads of 32, 8 runs of 4801 tokens: one 150 bf16 and 199 fp32, two 155 and 231; 256 runs of 1000: one 53 and 77, two 54 and 83.
 template <typename T, int D>
 cudaError_t launch(const DeltaParams& p, cudaStream_t s) {
   if constexpr (sizeof(T) == 2 && D < 128)
@@ -628,7 +628,7 @@ cudaError_t launch(const DeltaParams& p, int D, cudaStream_t s) {
 }  // namespace
 
 // The windows are prepared and taken in ranges: a range's preparation runs beside the chain of the range before, with records of its own, both launched ahead of the
-// end of what is before them.  Eight maps of 14400 tokens, 4 heads of 64: ranges one behind the other 442 us, beside each other 414; with a first range of a quarter, whose
+// end of what is before them.  Eight maps of 14400 tokens, 4 heads of 64, when they took 414 us: ranges one behind the other 442; with a first range of a quarter, whose
 // preparation alone has nothing beside it, 417.  A range more is 5 us more, so there is one as long as its records fit `most` bytes, of which two lie in the L2 cache.
 static int range_of(int batch, int tokens, int heads, bool bf16, uint64_t* bytes) {
   constexpr int64_t most = 48 << 20;

@@ -1,6 +1,6 @@
 // The gated delta rule over several tokens, first part (tt_delta_rule): of every window of 32 tokens and head, what depends on no state.
 // A block takes a window as delta_window.cuh says.  The windows of all sequences run at once; the chain of states, delta_chunk.cu, reads what is left here as the registers
-// it needs.  225 windows of 32 heads of 64: 34 us, bound by the substitutions' and products' latencies at five blocks to a multiprocessor.
+// it needs.  150 windows of 32 heads of 64, a third of eight maps: 26.6 us, bound by the substitutions' and products' latencies at five blocks to a multiprocessor.
 #include "delta_window.cuh"
 
 namespace tt {

@@ -3,7 +3,7 @@
 // The second form of out lets one pass over the state give both sums, F^T k and F^T q, so that a single meeting of the block's threads lies
 // between reading a state and writing it.  A block owns a run of W value columns of one head's state (the columns are
 // independent of each other), LANES = W / 4 threads to a row, in registers for the whole call: a token by itself reads and writes each state once, and that bounds
-// many states (256 sessions of 8 heads of 128, 268 MB: 49 us, 84 % of the rate of a copy).  Few states are bound by the launch (4.2 us); a further token takes 1 us.
+// many states (256 sessions of 8 heads of 128, 268 MB: 47 us, 88 % of the rate of a copy; 48 call by call).  Few states are bound by the launch (2.2 us); a further token takes 0.8 us.
 #include "linear_common.cuh"
 
 namespace tt {
@@ -142,8 +142,8 @@ cudaError_t launch(const DeltaParams& p, cudaStream_t s) {
 template <typename T, int D>
 cudaError_t launch(const DeltaParams& p, cudaStream_t s) {
   // Columns to a block: the fewer, the more multiprocessors fetch a state and the more threads share a row's sums, which is what a token takes.  Whole, halves and quarters, us:
-  // 256 sessions of 8 heads of 128, a token 46.7 45.1 51.3, six tokens 133 124 164; of 64 12.7 16.5 28.7, 41 66 125; of 32 8.3 8.3 10.3, 33 31 33;
-  // five sessions, six tokens of heads of 128 10.3 8.2 10.2, of 64 8.2 6.2 8.2.
+  // 256 sessions of 8 heads of 128, a token 60.1 46.6 53.0, six tokens 125 126 185; of 64 16.8 20.8 33.5, 46 77 135; of 32 9.7 9.6 10.4, 33 30 31;
+  // five sessions, six tokens of heads of 128 11.7 7.6 6.3, of 64 6.3 6.3 5.6.
   const auto run = [&](auto several) {
     constexpr bool S = decltype(several)::value;
     if constexpr (D == 64)
