@@ -12,7 +12,7 @@
 // columns takes 40 cycles however few its columns are, and its way through tensor memory twice that: the chain would be longer, not shorter.  Windows of 64 have four times the
 // triangle (with the warps as they were then, 909 us to 748 for the same maps).
 //
-// Eight maps of 14400 tokens, 4 heads of 64: 423 us, of which reading and writing it all once would be 37; 64 sequences of up to 497 tokens, 4 heads of 128: 155 us of 17.
+// Eight maps of 14400 tokens, 4 heads of 64: 410 us, of which reading and writing it all once would be 37; 64 sequences of up to 497 tokens, 4 heads of 128: 154 us of 17.
 //
 // The state is fp32, and so is everything between two products: an operand that is not bf16 to begin with is cut into three bf16 terms (8 + 8 + 8 bits), of whose
 // products those of 2^-16 and more count.  Only what out alone reads is rounded further: in bf16 calls S, U and P count with 16 bits.  (P rounded
@@ -78,6 +78,70 @@ __device__ __noinline__ float4 read_faded(const uint32_t* state, const typename 
     product(sum, a, f);
   }
   return make_float4(sum[0], sum[1], sum[2], sum[3]);
+}
+
+// A window from token `first` on with something in it that is not finite, or of whose products one is not, token by token: the weights of 0 that a window's products give earlier tokens
+// would make NaN of it.  s: a warp's part of the state of run `run`, whose G warps come here together.
+template <typename H>
+__device__ __forceinline__ void take_one_by_one(const DeltaParams& p, float (&s)[H::NT][4], float (&shares)[H::G][2][16], int b, int h, int first, int n, int run, int warp, const typename H::T* k,
+                                             const typename H::T* q, const typename H::T* v, typename H::T* o) {
+  using T = typename H::T;
+  constexpr int G = H::G, NT = H::NT;
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int64_t gate0 = (int64_t)b * p.tokens * p.heads + h;
+  for (int i = first; i < min(n, first + C); ++i) {
+    const T* kk = k + (int64_t)i * p.k.t + warp * NT * 8 + 2 * t;
+    const T* qq = q + (int64_t)i * p.q.t + warp * NT * 8 + 2 * t;
+    const float fade = p.log_decay ? expf(p.log_decay[gate0 + (int64_t)i * p.heads]) : 1.f;
+    auto sum_of = [&](const T* x, int which, float (&r)[2]) {
+      r[0] = r[1] = 0.f;
+#pragma unroll
+      for (int m = 0; m < NT; ++m)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[e >> 1] = fmaf(to_float(x[8 * m + (e & 1)]), s[m][e], r[e >> 1]);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        r[e] += __shfl_xor_sync(0xffffffffu, r[e], 1);
+        r[e] += __shfl_xor_sync(0xffffffffu, r[e], 2);
+        if (G > 1 && t == 0) shares[warp][which][g + 8 * e] = r[e];
+      }
+      if constexpr (G > 1) {
+        barrier_of<32 * G>(2 + run);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          r[e] = 0.f;
+#pragma unroll
+          for (int m = 0; m < G; ++m) r[e] += shares[m][which][g + 8 * e];
+        }
+      }
+    };
+#pragma unroll
+    for (int m = 0; m < NT; ++m)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[m][e] *= fade;
+    float said[2], sum[2];
+    sum_of(kk, 0, said);
+    const float beta = p.beta[gate0 + (int64_t)i * p.heads];
+    const T* vv = v + (int64_t)i * p.v.t + 16 * run + g;
+    const float u[2] = {beta * (to_float(vv[0]) - said[0]), beta * (to_float(vv[8]) - said[1])};
+#pragma unroll
+    for (int m = 0; m < NT; ++m)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[m][e] = fmaf(to_float(kk[8 * m + (e & 1)]), u[e >> 1], s[m][e]);
+    sum_of(qq, 1, sum);
+    if (warp == 0 && t == 0) {
+      T* to = o + (int64_t)i * p.o.t + 16 * run + g;
+      to[0] = (T)(p.scale * sum[0]);
+      to[8] = (T)(p.scale * sum[1]);
+    }
+  }
+}
+
+// The same out of line, not in the way of what runs always: 2 x 4801 fp32 tokens 211 -> 207 us.
+template <typename H>
+__device__ __noinline__ void take_one_by_one_apart(const DeltaParams& p, float (&s)[H::NT][4], float (&shares)[H::G][2][16], int b, int h, int first, int n, int run, int warp, const typename H::T* k,
+                                                   const typename H::T* q, const typename H::T* v, typename H::T* o) {
+  take_one_by_one<H>(p, s, shares, b, h, first, n, run, warp, k, q, v, o);
 }
 
 template <typename H>
@@ -326,6 +390,11 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
       for (int e = 0; e < 4; ++e) s[x][e] = p.state[state + at(x, e)];
     // what the state before window w says of the window's keys, or this warp's part of it
     float says[TT][4];
+    // Several warps to a run: whether a correction was not finite is known while the next window's keys are asked for; then the state is set back.  (Looked for before the state is
+    // changed: eight maps of 14400 tokens 426 us instead of 413, call by call.)
+    float before[G == 1 ? 1 : NT][4];
+    uint32_t odd = 0;
+    bool again = false;
     auto ask = [&](int w) {
       const __nv_bfloat16* ks = keys_of(w);
 #pragma unroll
@@ -362,60 +431,26 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
                 else mma16816(says[c], a[i], f[c][sum - i][0], f[c][sum - i][1]);
               }
       }
+      if constexpr (G > 1) again = __any_sync(0xffffffffu, odd != 0) != 0;
       if constexpr (G > 1)
 #pragma unroll
         for (int c = 0; c < TT; ++c) *reinterpret_cast<float4*>(x_part + ((run * G + warp) * TT + c) * 128 + lane * 4) = make_float4(says[c][0], says[c][1], says[c][2], says[c][3]);
     };
-    // A window with something in it that is not finite, or of whose products one is not, token by token: the weights of 0 that a window's products give earlier tokens would
-    // make NaN of it.
     auto advance_slowly = [&](int w) {
-      const int64_t gate0 = (int64_t)b * p.tokens * p.heads + h;
-      for (int i = token0 + w * C; i < min(n, token0 + w * C + C); ++i) {
-        const T* kk = k + (int64_t)i * p.k.t + warp * NT * 8 + 2 * t;
-        const T* qq = q + (int64_t)i * p.q.t + warp * NT * 8 + 2 * t;
-        const float fade = p.log_decay ? expf(p.log_decay[gate0 + (int64_t)i * p.heads]) : 1.f;
-        auto sum_of = [&](const T* x, int which, float (&r)[2]) {
-          r[0] = r[1] = 0.f;
-#pragma unroll
-          for (int m = 0; m < NT; ++m)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) r[e >> 1] = fmaf(to_float(x[8 * m + (e & 1)]), s[m][e], r[e >> 1]);
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            r[e] += __shfl_xor_sync(0xffffffffu, r[e], 1);
-            r[e] += __shfl_xor_sync(0xffffffffu, r[e], 2);
-            if (G > 1 && t == 0) shares[run][warp][which][g + 8 * e] = r[e];
-          }
-          if constexpr (G > 1) {
-            barrier_of<32 * G>(2 + run);
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              r[e] = 0.f;
-#pragma unroll
-              for (int m = 0; m < G; ++m) r[e] += shares[run][m][which][g + 8 * e];
-            }
-          }
-        };
-#pragma unroll
-        for (int m = 0; m < NT; ++m)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[m][e] *= fade;
-        float said[2], sum[2];
-        sum_of(kk, 0, said);
-        const float beta = p.beta[gate0 + (int64_t)i * p.heads];
-        const T* vv = v + (int64_t)i * p.v.t + 16 * run + g;
-        const float u[2] = {beta * (to_float(vv[0]) - said[0]), beta * (to_float(vv[8]) - said[1])};
-#pragma unroll
-        for (int m = 0; m < NT; ++m)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[m][e] = fmaf(to_float(kk[8 * m + (e & 1)]), u[e >> 1], s[m][e]);
-        sum_of(qq, 1, sum);
-        if (warp == 0 && t == 0) {
-          T* to = o + (int64_t)i * p.o.t + 16 * run + g;
-          to[0] = (T)(p.scale * sum[0]);
-          to[8] = (T)(p.scale * sum[1]);
-        }
+      if constexpr (H::ALONE) {                  // a kernel that needs a stack takes the host half a microsecond more to launch
+        take_one_by_one<H>(p, s, shares[run], b, h, token0 + w * C, n, run, warp, k, q, v, o);
+        return;
       }
+      float held[NT][4];
+#pragma unroll
+      for (int m = 0; m < NT; ++m)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) held[m][e] = s[m][e];
+      take_one_by_one_apart<H>(p, held, shares[run], b, h, token0 + w * C, n, run, warp, k, q, v, o);
+#pragma unroll
+      for (int m = 0; m < NT; ++m)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[m][e] = held[m][e];
     };
     auto advance = [&](int w) {
       const __nv_bfloat16* ks = keys_of(w);
@@ -510,7 +545,7 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
           for (int e = 0; e < 4; ++e) u[m][e] = warp + G * m >= 2 ? sums[m][0][e] + sums[m][1][e] : sums[m][0][e];
       }
       if (lane == 0 && warp == 0) slow[(w + 2) & 3][run] = 0;      // out was through with that two windows ago
-      // A correction that is not finite (of R, as a diagonal of T is 1, of T, or as a sum): the window is taken token by token, from the state that is still there.
+      // A correction that is not finite (of R, as a diagonal of T is 1, of T, or as a sum): the window is taken token by token, from the state before it.
       if constexpr (G == 1) {
         bool odd = false;
 #pragma unroll
@@ -528,8 +563,23 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
         u[m][0] *= down[m].x; u[m][1] *= down[m].y; u[m][2] *= down[m].x; u[m][3] *= down[m].y;
         if constexpr (G > 1) keep<3>(u_frag + run * 3 * TK * 128, TK * 128, lane, tile, u[m]);
       }
-      if constexpr (G > 1) barrier_of<32 * G>(2 + run);
+      if constexpr (G > 1) {
+        barrier_of<32 * G>(2 + run);
+#pragma unroll
+        for (int m = 0; m < NT; ++m)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) before[m][e] = s[m][e];
+      }
       operand(u_frag, u);
+      if constexpr (G > 1) {
+        // each of the run's warps has all of its corrections here, and comes to the same
+        __nv_bfloat162 sum = __float2bfloat162_rn(0.f);
+#pragma unroll
+        for (int x = 0; x < TK; ++x)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&a[x][0][e]), __float2bfloat162_rn(0.f), sum);
+        odd = *reinterpret_cast<const uint32_t*>(&sum) & 0x7FFF7FFFu;
+      }
       // S'^T = e^G_C S^T + U'^T K
       const float whole = record.whole;
       // several tiles side by side: 16 cycles a product with four sums in turn, 12 with eight
@@ -558,19 +608,6 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
                   if (sum == 2 && i == (TERMS == 1 ? 2 : 0)) mma16816_first(d[z][x], a[x][i], f[z][x][sum - i][0], f[z][x][sum - i][1]);
                   else mma16816(d[z][x], a[x][i], f[z][x][sum - i][0], f[z][x][sum - i][1]);
                 }
-        if (G > 1 && m == 0) {
-          // each of the run's warps has all of its corrections and comes to the same (with a flag behind the barrier eight maps take 423 us instead of 421)
-          __nv_bfloat162 odd = __float2bfloat162_rn(0.f);
-#pragma unroll
-          for (int x = 0; x < TK; ++x)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) odd = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&a[x][0][e]), __float2bfloat162_rn(0.f), odd);
-          if (__builtin_expect(__any_sync(0xffffffffu, (*reinterpret_cast<const uint32_t*>(&odd) & 0x7FFF7FFFu) != 0u), 0)) {
-            if (lane == 0) slow[w & 3][run] = 1;
-            advance_slowly(w);
-            return;
-          }
-        }
 #pragma unroll
         for (int z = 0; z < SIDE; ++z)
 #pragma unroll
@@ -579,7 +616,23 @@ __global__ void __launch_bounds__(H::THREADS, 1) delta_chunk_kernel(const __grid
     };
     for (int step = -2; step <= windows; ++step) {
       if (step >= 0 && step < windows) advance(step);
-      if (step >= -1 && step + 1 < windows) ask(step + 1);
+      if constexpr (G == 1) {
+        if (step >= -1 && step + 1 < windows) ask(step + 1);
+      } else {
+#pragma unroll 1
+        for (int turn = 0; turn < 2; ++turn) {     // the second where the window has been taken token by token
+          if (step >= -1 && step + 1 < windows) ask(step + 1);
+          else again = __any_sync(0xffffffffu, odd != 0) != 0;
+          if (__builtin_expect(turn == 1 || !again, 1)) break;
+          if (lane == 0) slow[step & 3][run] = 1;
+          odd = 0;
+#pragma unroll
+          for (int m = 0; m < NT; ++m)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[m][e] = before[m][e];
+          advance_slowly(step);
+        }
+      }
       __syncthreads();
     }
 #pragma unroll
@@ -605,8 +658,8 @@ cudaError_t launch_shape(const DeltaParams& p, cudaStream_t s) {
   return launch_kernel(delta_chunk_kernel<H>, dim3(H::D / H::COLS, (unsigned)p.heads, (unsigned)p.batch), H::THREADS, H::SMEM, s, p, !H::ALONE);
 }
 // One warp to a run where runs are many, four where they are few, and one for heads of 32, whose state is one warp's worth.  Measured, us:
-//   bf16, heads of 64, 128 runs of 14400 tokens: one 747, four 423; heads of 128, 2048 runs of 497 tokens: one 203, four 289;
-//   fp32, heads of 64, 16 runs of 4801 tokens: one 452, four 210; 512 runs of 1000: one 148, four 233 (of heads of 128 four runs do not fit a block);
+//   bf16, heads of 64, 128 runs of 14400 tokens: one 747, four 410; heads of 128, 2048 runs of 497 tokens: one 201, four 289;
+//   fp32, heads of 64, 16 runs of 4801 tokens: one 452, four 207; 512 runs of 1000: one 148, four 233 (of heads of 128 four runs do not fit a block);
 //   heads of 32, 8 runs of 4801 tokens: one 150 bf16 and 199 fp32, two 155 and 231; 256 runs of 1000: one 53 and 77, two 54 and 83.
 template <typename T, int D>
 cudaError_t launch(const DeltaParams& p, cudaStream_t s) {
